@@ -312,6 +312,88 @@ int ad_vocab_argmax_static(const void* x, const void* emb, int32_t dtype, int32_
 int ad_linear(const void* x, const void* W, const float* bias, int32_t dtype, int32_t M, int32_t K,
               int32_t N, float* y, int32_t* status, void* stream);
 
+/* ---- key/value cache in 8 bits -------------------------------------------------------------------------------
+ * (No counterpart in the paper: for decoders that are built from operator-level calls, and for contexts whose cache would not
+ * fit in BF16.)  One step of such a decoder appends the keys and values of the block's tokens (ad_cache_append), attends over
+ * prefix and block (ad_cache_attention), and decides what stays (ad_accept_sampled, or a comparison with ad_vocab_argmax's
+ * ids).  As in a handle, rolling back is a shorter length: nothing moves, and what lies beyond a row's length is overwritten.
+ *
+ * A cache is cut into blocks of tokens.  A block holds, for every key/value head, `block` tokens' codes and one scale for the
+ * keys and one for the values; a code stands for (its value in the format) * scale.
+ *
+ * ad_cache_append chooses as a block's scale the smallest power of two (2^-126 at least) that brings the largest of the block's
+ * numbers into the format: of the tokens in front of the row's length and of the new ones, and of nothing else, so that drafts
+ * which were written and given up leave no trace in it.  Numbers are rounded to nearest, ties to even.  Tokens that were there
+ * already get new codes when the scale changes: exact in E4M3 except for what becomes subnormal, and in INT8 together with all
+ * earlier roundings less than one step (scale) of the largest scale that the block has had.  Infinities become the largest code
+ * of their sign; a NaN becomes 0 and latches AD_ERR_ARG.
+ *
+ * Rows b = 0 .. B-1 of a batch bring off[b + 1] - off[b] tokens each (0 = the row is left alone), packed in row order into
+ * arrays of M tokens; len[b] tokens of the row are in the cache already.  off [B + 1] and len [B] are device arrays; the host
+ * only gives bounds, so that calls can be captured into graphs.  A row whose tokens exceed max_new or lie outside of 0 .. M, or
+ * that the table sends to a block which does not exist (only blocks with tokens in them are looked up), latches AD_ERR_ARG in
+ * *status; one whose tokens do not fit table_stride blocks latches AD_ERR_CAPACITY.  What concerns such a row or block is left
+ * out, the rest is done.  status: optional device int, 0 before; the first error stays.
+ * Different rows may share blocks that are full (a common prefix).  A block that a call writes must belong to one row. */
+enum { AD_CACHE_E4M3 = 0,     /* sign, 4 bits of exponent, 3 of mantissa; largest code 448.  No code written is a NaN. */
+       AD_CACHE_INT8 = 1 };   /* -127 .. 127 */
+typedef struct ad_kv_cache {
+  void* k_codes;             /* [n_blocks, n_kv_heads, block, head_dim] bytes, 16-byte aligned */
+  void* v_codes;
+  float* k_scale;            /* [n_blocks, n_kv_heads] */
+  float* v_scale;
+  const int32_t* table;      /* [B, table_stride]: block i of row b; NULL: block b * table_stride + i */
+  int32_t table_stride;      /* blocks of a row */
+  int32_t n_blocks, n_kv_heads;
+  int32_t block;             /* tokens of a block: 16, 32, 64 or 128 */
+  int32_t head_dim;          /* 32, 64 or 128 */
+  int32_t format;            /* AD_CACHE_* */
+} ad_kv_cache;
+
+/* Writes k, v [M, n_kv_heads, head_dim] (dtype as given; tokens token_stride numbers apart, so that parts of a wider array need
+ * no copy; 16-byte aligned) to positions len[b] .. of the rows.  The codes of positions behind the last new token of a block
+ * stay as they were. */
+int ad_cache_append(const ad_kv_cache* cache, const void* k, const void* v, int32_t dtype, int64_t token_stride,
+                    const int32_t* off, const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t* status, void* stream);
+
+/* Reads positions start[b] .. of the rows back into k, v [M, n_kv_heads, head_dim] in dtype, rounded once. */
+int ad_cache_read(const ad_kv_cache* cache, void* k, void* v, int32_t dtype, const int32_t* off, const int32_t* start, int32_t B,
+                  int32_t M, int32_t max_tokens, int32_t* status, void* stream);
+
+/* out [M, n_heads, head_dim] = softmax(scale q k^T) v of queries q [M, n_heads, head_dim] (dtype; tokens q_stride numbers apart,
+ * 16-byte aligned), n_heads a multiple of n_kv_heads (query head h reads key/value head h / (n_heads / n_kv_heads)).
+ * causal != 0 (self-attention of a block, appended before): query i of row b sees the row's first len[b] + i + 1 positions;
+ * causal == 0 (keys of an encoder): all queries of the row see its first len[b].  A query that sees nothing gets zeros.
+ * Positions beyond are never looked at.  max_keys: longest row to plan for; longer ones are computed as well, only slower.
+ * Probabilities and sums are held in FP32; with BF16 queries the probabilities are rounded to 11 bits in front of the product
+ * with the values, with FP32 ones to 22.  scratch: ad_cache_attention_scratch_bytes() of device memory, 256-byte aligned (NULL
+ * when that is 0); calls that may overlap need scratch of their own. */
+size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* cache, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys);
+int ad_cache_attention(const ad_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads,
+                       const int32_t* off, const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t max_keys,
+                       int32_t causal, float scale, void* out, void* scratch, size_t scratch_bytes, int32_t* status, void* stream);
+
+/* Verification for sampled decoding: the counterpart of the greedy decision (Eq. 7) when the output is to be distributed as the
+ * verifier's probabilities, whatever was drafted.  target [M, vocab] (dtype, rows target_stride scores apart) holds the
+ * verifier's scores of the block positions, packed in row order as ad_debug_logits leaves them; draft [M, vocab] the scores that
+ * the drafts were sampled from, with the same temperature, or NULL for drafts that were not sampled (copied from the source:
+ * their own probability is one).  drafts [B, kmax] as in ad_verify_block; k_b = off[b + 1] - off[b] <= kmax.
+ * With p, q = softmax(scores / temperature): position i keeps its draft d while u[b][i] * q_i(d) < p_i(d); the first one that does
+ * not takes the lowest id at which the running sum of max(p_i - q_i, 0), over ids in order, exceeds r[b] times its total (of p_i
+ * alone where the draft is a negative slot), and is the last.  So k_b = 1 with draft -1 is plain sampling.  u [B, kmax] and
+ * r [B] are uniform in [0, 1).  Comparisons are decided as in 64-bit arithmetic.
+ * tokens [B, kmax] receives the verified tokens and -1 behind them, n_accepted [B] their count: 1 .. k_b, cut at the first
+ * accepted `eos` (negative: none); 0 for idle rows.  ad_force_commit takes both as they are.
+ * Scores of -inf are probability 0, +inf share all of it; a NaN counts as -inf.  A position without any score above -inf takes id 0.
+ * A draft >= vocab counts as a negative slot and latches AD_ERR_ARG; so does a row outside of 0 .. M or longer than kmax,
+ * which comes back as idle.  scratch: device memory, 256-byte aligned, ad_accept_sampled_scratch_bytes() of it; calls that may
+ * overlap need scratch of their own. */
+size_t ad_accept_sampled_scratch_bytes(int32_t M, int32_t vocab, int32_t with_draft);
+int ad_accept_sampled(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int32_t dtype,
+                      float temperature, int32_t vocab, const int32_t* off, const int32_t* drafts, int32_t kmax, int32_t B,
+                      int32_t M, const float* u, const float* r, int32_t eos, int32_t* tokens, int32_t* n_accepted,
+                      void* scratch, size_t scratch_bytes, int32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,13 +17,15 @@ LIB_PATH = os.environ.get("AD_LIB_PATH", os.path.join(_HERE, "libad_b200.so"))
 AD_OK, AD_ERR_ARG, AD_ERR_STATE, AD_ERR_CAPACITY, AD_ERR_TIMEOUT, AD_ERR_CUDA = 0, -1, -2, -3, -4, -5
 AD_DTYPE_FP32, AD_DTYPE_BF16 = 0, 1
 AD_MODE_IAD, AD_MODE_GAD = 0, 1
+AD_CACHE_E4M3, AD_CACHE_INT8 = 0, 1
 
 EXPORTS = [
     "ad_weight_counts", "ad_query_workspace", "ad_create", "ad_destroy", "ad_last_error", "ad_encode",
     "ad_verify_block", "ad_commit", "ad_force_commit", "ad_generate", "ad_draft_block", "ad_get_state", "ad_sync", "ad_set_acceptance",
     "ad_debug_logits", "ad_debug_encoder_memory", "ad_debug_stage_timeline", "ad_debug_profile_verify", "ad_vocab_argmax_scratch_bytes", "ad_vocab_argmax",
     "ad_vocab_argmax_static", "ad_debug_graph_count", "ad_debug_projection_shapes", "ad_debug_wait_probe", "ad_debug_grid_barrier_probe",
-    "ad_linear",
+    "ad_linear", "ad_cache_append", "ad_cache_read", "ad_cache_attention_scratch_bytes", "ad_cache_attention", "ad_accept_sampled_scratch_bytes",
+    "ad_accept_sampled",
 ]
 
 
@@ -53,6 +55,11 @@ class Stats(C.Structure):
                 ("kernel_launches", C.c_int64)]
 
 
+class KvCacheStruct(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scale", "v_scale", "table")] + \
+               [(n, C.c_int32) for n in ("table_stride", "n_blocks", "n_kv_heads", "block", "head_dim", "format")]
+
+
 class AdError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"aggressive_decoding error {code}: {msg}")
@@ -72,6 +79,7 @@ def load():
                           "there is no fallback path")
     lib = C.CDLL(LIB_PATH)
     vp, i32, sz = C.c_void_p, C.c_int32, C.c_size_t
+    cache, i64, f32 = C.POINTER(KvCacheStruct), C.c_int64, C.c_float
     sig = {
         "ad_weight_counts": (C.c_int, [C.POINTER(ModelCfg), C.POINTER(sz), C.POINTER(sz)]),
         "ad_query_workspace": (C.c_int, [C.POINTER(ModelCfg), C.POINTER(sz)]),
@@ -95,6 +103,12 @@ def load():
         "ad_vocab_argmax": (C.c_int, [vp, vp, i32, i32, i32, i32, vp, vp, sz, vp, vp]),
         "ad_vocab_argmax_static": (C.c_int, [vp, vp, i32, i32, i32, i32, vp, vp, vp]),
         "ad_linear": (C.c_int, [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]),
+        "ad_cache_append": (C.c_int, [cache, vp, vp, i32, i64, vp, vp, i32, i32, i32, vp, vp]),
+        "ad_cache_read": (C.c_int, [cache, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp]),
+        "ad_cache_attention_scratch_bytes": (sz, [cache, i32, i32, i32, i32]),
+        "ad_cache_attention": (C.c_int, [cache, vp, i32, i64, i32, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, sz, vp, vp]),
+        "ad_accept_sampled_scratch_bytes": (sz, [i32, i32, i32]),
+        "ad_accept_sampled": (C.c_int, [vp, i64, vp, i64, i32, f32, i32, vp, vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, sz, vp, vp]),
         "ad_debug_graph_count": (C.c_int, [vp, vp]),
         "ad_debug_projection_shapes": (C.c_int, [C.POINTER(ModelCfg), vp, i32, vp]),
         "ad_debug_wait_probe": (C.c_int, [vp, i32, vp, vp]),
@@ -424,3 +438,204 @@ def linear(x_t, W_t, bias_t=None, status_t=None):
         raise AdError(rc, "ad_linear")
     stream.synchronize()
     return y
+
+
+# ---------------------------------------------------------------------------------------------------------
+# 8-bit key/value cache and sampled verification.  These calls are asynchronous on torch's current stream of the tensors' device, allocate
+# results and scratch through torch, and can be captured into graphs.
+# ---------------------------------------------------------------------------------------------------------
+def _refuse(entry, why):
+    raise AdError(AD_ERR_ARG, f"{entry}: {why}")
+
+
+def _number_type(entry, t):
+    import torch
+    if t.dtype is torch.bfloat16:
+        return AD_DTYPE_BF16
+    if t.dtype is torch.float32:
+        return AD_DTYPE_FP32
+    _refuse(entry, f"{t.dtype} is neither float32 nor bfloat16")
+
+
+def _index_arrays(entry, dev, *arrays):
+    import torch
+    for a, shape in arrays:
+        if a.dtype is not torch.int32 or a.device != dev or a.shape != shape or not a.is_contiguous():
+            _refuse(entry, f"offsets, lengths, tables and drafts are contiguous int32 tensors on {dev}; wanted {shape}, got {tuple(a.shape)}")
+
+
+def _status_pointer(entry, dev, status_t):
+    if status_t is None:
+        return None
+    _index_arrays(entry, dev, (status_t, (1,)))
+    return status_t.data_ptr()
+
+
+def _on_device(dev, call):
+    """call(raw stream) with dev current; the stream is torch's current one of dev."""
+    import torch
+    if torch._C._cuda_getDevice() == dev.index:
+        return call(torch._C._cuda_getCurrentRawStream(dev.index))
+    with torch.cuda.device(dev):
+        return call(torch._C._cuda_getCurrentRawStream(dev.index))
+
+
+def _scratch(like, nbytes):
+    """(tensor to keep, 256-byte aligned address) of nbytes of scratch."""
+    import torch
+    t = torch.empty(nbytes + 256, dtype=torch.uint8, device=like.device)
+    return t, (t.data_ptr() + 255) // 256 * 256
+
+
+def _raise(lib, rc):
+    msg = lib.ad_last_error(None)
+    raise AdError(rc, msg.decode() if msg else "")
+
+
+class KvCache:
+    """Key/value cache in 8 bits: blocks of `block` tokens with one scale per head and block (format "e4m3" or "int8").
+
+    table [rows, row_blocks] (int32, on the device) names the blocks of each row; without one, row b owns blocks
+    b * row_blocks .. (b + 1) * row_blocks - 1.  `tensors` = (k_codes, v_codes, k_scale, v_scale) adopts existing memory; otherwise
+    the cache is allocated here."""
+
+    def __init__(self, n_blocks, n_kv_heads, head_dim, block=32, fmt="e4m3", table=None, row_blocks=None, device="cuda:0", tensors=None):
+        import torch
+        entry = "KvCache"
+        if fmt not in ("e4m3", "int8"):
+            _refuse(entry, f"unknown format {fmt!r}")
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            _refuse(entry, "the cache lives on a CUDA device")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.fmt, self.n_blocks, self.n_kv_heads, self.head_dim, self.block = fmt, int(n_blocks), int(n_kv_heads), int(head_dim), int(block)
+        dt = torch.float8_e4m3fn if fmt == "e4m3" else torch.int8
+        shape = (self.n_blocks, self.n_kv_heads, self.block, self.head_dim)
+        if tensors is None:
+            codes = [torch.zeros(shape, dtype=torch.uint8, device=self.device).view(dt) for _ in range(2)]
+            tensors = (*codes, *(torch.ones(shape[:2], dtype=torch.float32, device=self.device) for _ in range(2)))
+        for t, want, s in zip(tensors, (dt, dt, torch.float32, torch.float32), (shape, shape, shape[:2], shape[:2])):
+            if t.dtype is not want or t.shape != s or t.device != self.device or not t.is_contiguous():
+                _refuse(entry, f"codes are contiguous {dt} {shape}, scales float32 {shape[:2]}, on {self.device}")
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale = tensors
+        if row_blocks is None:
+            row_blocks = table.shape[1] if table is not None else self.n_blocks
+        if table is not None:
+            _index_arrays(entry, self.device, (table, (table.shape[0], row_blocks)))
+        self.table, self.row_blocks = table, int(row_blocks)
+        self.struct = KvCacheStruct(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                                    table.data_ptr() if table is not None else None, self.row_blocks, self.n_blocks, self.n_kv_heads, self.block,
+                                    self.head_dim, AD_CACHE_E4M3 if fmt == "e4m3" else AD_CACHE_INT8)
+        self._ref = C.byref(self.struct)
+
+    def _batch(self, entry, off_t, len_t):
+        """Rows of a batch: off_t [B + 1], len_t [B]."""
+        B = len_t.shape[0]
+        _index_arrays(entry, self.device, (off_t, (B + 1,)), (len_t, (B,)))
+        if self.table is not None and self.table.shape[0] < B:
+            _refuse(entry, f"the table has {self.table.shape[0]} rows, the batch {B}")
+        return B
+
+    def _tokens(self, entry, t, heads):
+        """Numbers between tokens of t [M, heads, head_dim], whose heads lie next to each other."""
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.device != self.device:
+            _refuse(entry, f"wanted [tokens, {heads}, {self.head_dim}] on {self.device}, got {tuple(t.shape)} on {t.device}")
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.head_dim):
+            _refuse(entry, "the numbers of a token must lie next to each other")
+        return t.stride(0) if t.shape[0] > 1 else heads * self.head_dim
+
+
+def cache_append(cache, k_t, v_t, off_t, len_t, max_new, status_t=None):
+    """Writes k_t, v_t [M, n_kv_heads, head_dim] (float32 or bfloat16, views of a wider array as well) behind the len_t[b] tokens of every row."""
+    entry, lib = "ad_cache_append", load()
+    B, dtype = cache._batch(entry, off_t, len_t), _number_type(entry, k_t)
+    stride = cache._tokens(entry, k_t, cache.n_kv_heads)
+    if v_t.dtype != k_t.dtype or v_t.shape != k_t.shape or cache._tokens(entry, v_t, cache.n_kv_heads) != stride:
+        _refuse(entry, "keys and values must agree in type, shape and stride")
+    status = _status_pointer(entry, cache.device, status_t)
+    rc = _on_device(cache.device, lambda stream: lib.ad_cache_append(
+        cache._ref, k_t.data_ptr(), v_t.data_ptr(), dtype, stride, off_t.data_ptr(), len_t.data_ptr(), B, k_t.shape[0], max_new, status, stream))
+    if rc != AD_OK:
+        _raise(lib, rc)
+
+
+def cache_read(cache, off_t, start_t, tokens, max_tokens, dtype=None, status_t=None):
+    """Positions start_t[b] .. of every row, off_t[b + 1] - off_t[b] of them: (k, v) [tokens, n_kv_heads, head_dim] in dtype (default bfloat16).
+    Tokens that no row covers are left uninitialised."""
+    import torch
+    entry, lib = "ad_cache_read", load()
+    B = cache._batch(entry, off_t, start_t)
+    k, v = (torch.empty((tokens, cache.n_kv_heads, cache.head_dim), dtype=dtype or torch.bfloat16, device=cache.device) for _ in range(2))
+    code, status = _number_type(entry, k), _status_pointer(entry, cache.device, status_t)
+    rc = _on_device(cache.device, lambda stream: lib.ad_cache_read(
+        cache._ref, k.data_ptr(), v.data_ptr(), code, off_t.data_ptr(), start_t.data_ptr(), B, tokens, max_tokens, status, stream))
+    if rc != AD_OK:
+        _raise(lib, rc)
+    return k, v
+
+
+def cache_attention(cache, q_t, off_t, len_t, max_new, max_keys, causal=True, scale=None, out=None, status_t=None):
+    """Attention of q_t [M, n_heads, head_dim] over the cache; returns [M, n_heads, head_dim] in q_t's type (`out`, if given).  Causal: query i of
+    row b sees len_t[b] + i + 1 positions (its block has been appended), otherwise all see len_t[b].  scale: head_dim ** -0.5 unless given."""
+    import torch
+    entry, lib = "ad_cache_attention", load()
+    B, dtype = cache._batch(entry, off_t, len_t), _number_type(entry, q_t)
+    if q_t.dim() != 3:
+        _refuse(entry, "queries are [tokens, heads, head_dim]")
+    M, H = q_t.shape[:2]
+    stride = cache._tokens(entry, q_t, H)
+    if out is None:
+        out = torch.empty((M, H, cache.head_dim), dtype=q_t.dtype, device=cache.device)
+    elif out.dtype != q_t.dtype or out.shape != q_t.shape or out.device != cache.device or not out.is_contiguous():
+        _refuse(entry, "the result is a contiguous tensor like the queries")
+    status = _status_pointer(entry, cache.device, status_t)
+    scale = cache.head_dim ** -0.5 if scale is None else float(scale)
+
+    def call(stream):
+        nbytes = lib.ad_cache_attention_scratch_bytes(cache._ref, H, B, max_new, max_keys)
+        keep, scratch = _scratch(q_t, nbytes) if nbytes else (None, None)
+        return lib.ad_cache_attention(cache._ref, q_t.data_ptr(), dtype, stride, H, off_t.data_ptr(), len_t.data_ptr(), B, M, max_new, max_keys,
+                                      1 if causal else 0, scale, out.data_ptr(), scratch, nbytes, status, stream)
+
+    rc = _on_device(cache.device, call)
+    if rc != AD_OK:
+        _raise(lib, rc)
+    return out
+
+
+def accept_sampled(target_t, draft_t, drafts_t, off_t, u_t, r_t, temperature=1.0, eos=-1, status_t=None):
+    """Sampled verification of drafts_t [B, kmax] against scores target_t [M, vocab] (and the drafter's, draft_t, or None for drafts that were not
+    sampled) with uniform numbers u_t [B, kmax] and r_t [B].  Returns (tokens [B, kmax], n_accepted [B])."""
+    import torch
+    entry, lib = "ad_accept_sampled", load()
+    dev, dtype = target_t.device, _number_type(entry, target_t)
+    if dev.type != "cuda":
+        _refuse(entry, "scores live on a CUDA device")
+    if drafts_t.dim() != 2 or target_t.dim() != 2:
+        _refuse(entry, "drafts are [rows, kmax], scores [tokens, vocab]")
+    B, kmax = drafts_t.shape
+    M, V = target_t.shape
+    _index_arrays(entry, dev, (drafts_t, (B, kmax)), (off_t, (B + 1,)))
+    for x, shape in ((u_t, (B, kmax)), (r_t, (B,))):
+        if x.dtype is not torch.float32 or x.shape != shape or x.device != dev or not x.is_contiguous():
+            _refuse(entry, f"random numbers are contiguous float32 tensors on {dev}; wanted {shape}, got {tuple(x.shape)}")
+    for x in (target_t, draft_t):
+        if x is not None and (x.dtype != target_t.dtype or x.shape != target_t.shape or x.device != dev or (V > 1 and x.stride(1) != 1)):
+            _refuse(entry, "scores are [tokens, vocab], a row's next to each other, the drafter's like the verifier's")
+    strides = [V if x is None or M < 2 else x.stride(0) for x in (target_t, draft_t)]
+    status = _status_pointer(entry, dev, status_t)
+    tokens = torch.empty((B, kmax), dtype=torch.int32, device=dev)
+    count = torch.empty(B, dtype=torch.int32, device=dev)
+
+    def call(stream):
+        nbytes = lib.ad_accept_sampled_scratch_bytes(M, V, 0 if draft_t is None else 1)
+        keep, scratch = _scratch(target_t, nbytes)
+        return lib.ad_accept_sampled(target_t.data_ptr(), strides[0], None if draft_t is None else draft_t.data_ptr(), strides[1], dtype, temperature, V,
+                                     off_t.data_ptr(), drafts_t.data_ptr(), kmax, B, M, u_t.data_ptr(), r_t.data_ptr(), eos, tokens.data_ptr(),
+                                     count.data_ptr(), scratch, nbytes, status, stream)
+
+    rc = _on_device(dev, call)
+    if rc != AD_OK:
+        _raise(lib, rc)
+    return tokens, count

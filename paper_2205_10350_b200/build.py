@@ -7,8 +7,8 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libad_b200.so")
-SOURCES = ["ad_api.cu"]
-HEADERS = ["ad_common.cuh", "gemm_tc.cuh", "gemm_tc_pair.cuh", "gemm_simt.cuh", "gemm_few.cuh", "attention.cuh", "attention_few.cuh", "attention_mma.cuh", "ffn_few.cuh", "sublayer_f32.cuh", "steps.cuh", "accept.cuh", "grid_sync.cuh", "mega.cuh"]
+SOURCES = ["ad_api.cu", "cache_api.cu"]
+HEADERS = ["ad_common.cuh", "gemm_tc.cuh", "gemm_tc_pair.cuh", "gemm_simt.cuh", "gemm_few.cuh", "attention.cuh", "attention_few.cuh", "attention_mma.cuh", "ffn_few.cuh", "sublayer_f32.cuh", "steps.cuh", "accept.cuh", "grid_sync.cuh", "mega.cuh", "kv_cache.cuh", "cache_attention.cuh", "accept_sampled.cuh", "op_launch.h"]
 
 
 def _stale() -> bool:
@@ -27,7 +27,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + f".{os.getpid()}.tmp"
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-cudart", "shared", "-rdc=true", "-lcudadevrt"]
+           "-shared", "-Xcompiler", "-fPIC", "-cudart", "shared", "-rdc=true", "-lcudadevrt", "--threads", "2"]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES] + ["-o", tmp]

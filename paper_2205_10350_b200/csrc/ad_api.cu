@@ -25,6 +25,7 @@
 #include "gemm_tc_pair.cuh"
 #include "grid_sync.cuh"
 #include "mega.cuh"
+#include "op_launch.h"
 #include "steps.cuh"
 #include "sublayer_f32.cuh"
 
@@ -2713,6 +2714,17 @@ extern "C" int ad_vocab_argmax_static(const void* x, const void* emb, int32_t dt
                                               : "ad_vocab_argmax_static: encoding a TMA descriptor or launching a kernel failed");
   return AD_OK;
 }
+
+// ---- what the operator-level entry points of cache_api.cu share (op_launch.h) ----
+int ad::op_fail(int code, const char* entry, const char* why) noexcept {
+  try {
+    return fail(nullptr, code, std::string(entry) + ": " + why);
+  } catch (...) {                     // (no memory for the message)
+    return code;
+  }
+}
+int ad::op_num_sms() { return num_sms(); }
+bool ad::op_early_launch() { return use_pdl(); }
 
 #ifdef AD_TRACE
 // Timeline dump of a tracing build: copies up to cap stamps to the host and optionally clears the buffer.

@@ -1,0 +1,188 @@
+// Operator-level entry points of the 8-bit key/value cache and of sampled verification, declared in include/aggressive_decoding.h.
+#include <limits.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "accept_sampled.cuh"
+#include "ad_common.cuh"
+#include "cache_attention.cuh"
+#include "kv_cache.cuh"
+#include "op_launch.h"
+
+using namespace ad;
+
+namespace {
+
+constexpr int kMaxNew = 1 << 19;       // tokens of a row in one call (grid dimensions)
+constexpr int kMaxRows = 65535;
+
+bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+bool known_dtype(int32_t t) { return t == AD_DTYPE_FP32 || t == AD_DTYPE_BF16; }
+size_t dtype_bytes(int32_t t) { return t == AD_DTYPE_FP32 ? 4 : 2; }
+
+// Why a cache cannot be worked on, or null.
+const char* cache_fault(const ad_kv_cache* c, int32_t B) {
+  if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return "null cache";
+  if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16)) return "codes must be 16-byte aligned";
+  if (c->format != AD_CACHE_E4M3 && c->format != AD_CACHE_INT8) return "unknown format";
+  if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128) return "blocks hold 16, 32, 64 or 128 tokens";
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return "heads are 32, 64 or 128 wide";
+  if (c->n_blocks < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 4096 || c->table_stride < 1) return "sizes must be positive (and at most 4096 heads)";
+  if ((int64_t)c->table_stride * c->block > INT_MAX - kMaxNew) return "a row's capacity must stay below 2^31 - 2^19 tokens";
+  if (!c->table && (int64_t)B * c->table_stride > c->n_blocks) return "without a table there must be B * table_stride blocks";
+  return nullptr;
+}
+
+const char* batch_fault(const int32_t* off, const int32_t* len, int32_t B, int32_t M, int32_t max_new) {
+  if (!off || !len) return "null offsets or lengths";
+  if (B < 1 || B > kMaxRows) return "1 to 65535 rows";
+  if (M < 0) return "negative number of tokens";
+  if (max_new < 1 || max_new > kMaxNew) return "1 to 2^19 tokens of a row";
+  return nullptr;
+}
+
+kv::Cache device_cache(const ad_kv_cache* c) {
+  kv::Cache d;
+  d.codes[0] = static_cast<uint8_t*>(c->k_codes); d.codes[1] = static_cast<uint8_t*>(c->v_codes);
+  d.scale[0] = c->k_scale; d.scale[1] = c->v_scale;
+  d.table = c->table; d.table_stride = c->table_stride; d.n_blocks = c->n_blocks; d.heads = c->n_kv_heads; d.block = c->block;
+  return d;
+}
+
+template <typename T, typename F> struct Types { typedef T Num; typedef F Fmt; };
+// Calls f with the number and code types of a call.
+template <typename Fn>
+cudaError_t by_types(int32_t dtype, int32_t format, Fn f) {
+  if (dtype == AD_DTYPE_FP32) return format == AD_CACHE_E4M3 ? f(Types<float, kv::E4m3>()) : f(Types<float, kv::Int8>());
+  return format == AD_CACHE_E4M3 ? f(Types<bf16, kv::E4m3>()) : f(Types<bf16, kv::Int8>());
+}
+
+int arg_fault(const char* entry, const char* why) { return op_fail(AD_ERR_ARG, entry, why); }
+int launched(const char* entry, cudaError_t e) { return e == cudaSuccess ? AD_OK : op_fail(AD_ERR_CUDA, entry, cudaGetErrorString(e)); }
+
+dim3 tile_grid(const ad_kv_cache* c, int32_t B, int32_t max_new) {
+  return dim3(2 * c->n_kv_heads, (max_new + c->block - 2) / c->block + 1, B);
+}
+dim3 tile_threads(const ad_kv_cache* c) { return dim3(std::max(32, c->block * c->head_dim / (8 * kv::VECS))); }
+
+}  // namespace
+
+extern "C" int ad_cache_append(const ad_kv_cache* c, const void* k, const void* v, int32_t dtype, int64_t token_stride, const int32_t* off,
+                               const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t* status, void* stream) {
+  const char* entry = "ad_cache_append";
+  if (const char* why = batch_fault(off, len, B, M, max_new)) return arg_fault(entry, why);
+  if (const char* why = cache_fault(c, B)) return arg_fault(entry, why);
+  if (!known_dtype(dtype)) return arg_fault(entry, "unknown dtype");
+  if (M == 0) return AD_OK;
+  if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return arg_fault(entry, "keys and values must be 16-byte aligned");
+  if (token_stride < (int64_t)c->n_kv_heads * c->head_dim || token_stride % (int64_t)(16 / dtype_bytes(dtype)))
+    return arg_fault(entry, "tokens must be a multiple of 16 bytes apart, and not overlap");
+  const kv::Cache d = device_cache(c);
+  return launched(entry, by_types(dtype, c->format, [&](auto t) {
+    typedef typename decltype(t)::Num T;
+    return launch_op(kv::cache_append_kernel<T, typename decltype(t)::Fmt>, tile_grid(c, B, max_new), tile_threads(c), dim3(), 0,
+                     static_cast<cudaStream_t>(stream), d, static_cast<const T*>(k), static_cast<const T*>(v), (size_t)token_stride,
+                     (int)c->head_dim, off, len, (int)M, (int)max_new, status);
+  }));
+}
+
+extern "C" int ad_cache_read(const ad_kv_cache* c, void* k, void* v, int32_t dtype, const int32_t* off, const int32_t* start, int32_t B, int32_t M,
+                             int32_t max_tokens, int32_t* status, void* stream) {
+  const char* entry = "ad_cache_read";
+  if (const char* why = batch_fault(off, start, B, M, max_tokens)) return arg_fault(entry, why);
+  if (const char* why = cache_fault(c, B)) return arg_fault(entry, why);
+  if (!known_dtype(dtype)) return arg_fault(entry, "unknown dtype");
+  if (M == 0) return AD_OK;
+  if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return arg_fault(entry, "keys and values must be 16-byte aligned");
+  const kv::Cache d = device_cache(c);
+  return launched(entry, by_types(dtype, c->format, [&](auto t) {
+    typedef typename decltype(t)::Num T;
+    return launch_op(kv::cache_read_kernel<T, typename decltype(t)::Fmt>, tile_grid(c, B, max_tokens), tile_threads(c), dim3(), 0,
+                     static_cast<cudaStream_t>(stream), d, static_cast<T*>(k), static_cast<T*>(v), (int)c->head_dim, off, start, (int)M,
+                     (int)max_tokens, status);
+  }));
+}
+
+extern "C" size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
+  (void)c; (void)n_heads; (void)B; (void)max_new; (void)max_keys;
+  return 0;
+}
+
+extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
+                                  const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, int32_t causal, float scale, void* out,
+                                  void* scratch, size_t scratch_bytes, int32_t* status, void* stream) {
+  const char* entry = "ad_cache_attention";
+  if (const char* why = batch_fault(off, len, B, M, max_new)) return arg_fault(entry, why);
+  if (const char* why = cache_fault(c, B)) return arg_fault(entry, why);
+  if (!known_dtype(dtype)) return arg_fault(entry, "unknown dtype");
+  if (n_heads < 1 || n_heads % c->n_kv_heads || n_heads > 65535) return arg_fault(entry, "query heads must be a multiple of the cache's (and at most 65535)");
+  if (max_new > 65535) return arg_fault(entry, "at most 65535 queries of a row");
+  if (max_keys < 0) return arg_fault(entry, "negative number of keys");
+  if (!(scale > 0.f) || !(scale < INFINITY)) return arg_fault(entry, "the scale must be positive and finite");
+  if (M == 0) return AD_OK;
+  if (!q || !out || !aligned(q, 16) || !aligned(out, 16)) return arg_fault(entry, "queries and result must be 16-byte aligned");
+  if (q_stride < (int64_t)n_heads * c->head_dim || q_stride % (int64_t)(16 / dtype_bytes(dtype)))
+    return arg_fault(entry, "queries must be a multiple of 16 bytes apart, and not overlap");
+  if (scratch_bytes < ad_cache_attention_scratch_bytes(c, n_heads, B, max_new, max_keys)) return op_fail(AD_ERR_CAPACITY, entry, "scratch too small");
+  (void)scratch;
+  kv::AttendParams a;
+  a.c = device_cache(c); a.q = q; a.q_stride = (size_t)q_stride; a.out = out; a.n_heads = n_heads; a.M = M; a.max_new = max_new; a.off = off; a.len = len;
+  a.causal = causal != 0; a.scale = scale * (float)M_LOG2E; a.status = status;
+  return launched(entry, by_types(dtype, c->format, [&](auto t) {
+    typedef typename decltype(t)::Num T;
+    typedef typename decltype(t)::Fmt F;
+    auto kernel = c->head_dim == 32 ? kv::cache_attention_kernel<T, F, 32> : c->head_dim == 64 ? kv::cache_attention_kernel<T, F, 64> : kv::cache_attention_kernel<T, F, 128>;
+    return launch_op(kernel, dim3(n_heads, max_new, B), dim3(32), dim3(), 0, static_cast<cudaStream_t>(stream), a);
+  }));
+}
+
+namespace {
+// Parts a row's scores are split into: four CTAs an SM where there are few rows, as long as every thread has a vector; at least so many that no
+// thread adds up more than 32 vectors.
+int score_parts(int32_t rows, int32_t vocab) {
+  const int vecs = (vocab + 3) / 4;                                  // (FP32's; BF16 has half as many)
+  const int least = (vecs + 32 * sampled::STAT_THREADS - 1) / (32 * sampled::STAT_THREADS);
+  const int most = std::max(1, vecs / (2 * sampled::STAT_THREADS));
+  const int fill = (4 * op_num_sms() + std::max(rows, 1) - 1) / std::max(rows, 1);
+  return std::max(least, std::min(most, fill));
+}
+}  // namespace
+
+extern "C" size_t ad_accept_sampled_scratch_bytes(int32_t M, int32_t vocab, int32_t with_draft) {
+  if (M < 0 || M > INT_MAX / 2 || vocab < 1 || vocab > (1 << 24)) return 0;
+  const int z = with_draft ? 2 : 1;
+  return (size_t)std::max(M, 1) * z * score_parts(M * z, vocab) * sizeof(sampled::Stat);
+}
+
+extern "C" int ad_accept_sampled(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int32_t dtype, float temperature,
+                                 int32_t vocab, const int32_t* off, const int32_t* drafts, int32_t kmax, int32_t B, int32_t M, const float* u,
+                                 const float* r, int32_t eos, int32_t* tokens, int32_t* n_accepted, void* scratch, size_t scratch_bytes,
+                                 int32_t* status, void* stream) {
+  const char* entry = "ad_accept_sampled";
+  if (!off || !drafts || !u || !r || !tokens || !n_accepted) return arg_fault(entry, "null argument");
+  if (!known_dtype(dtype)) return arg_fault(entry, "unknown dtype");
+  if (B < 1 || B > kMaxRows || kmax < 1 || kmax > kMaxNew || M < 0 || M > INT_MAX / 2 || vocab < 1 || vocab > (1 << 24)) return arg_fault(entry, "size out of range");
+  if (!(temperature >= 1e-30f) || !(temperature < INFINITY)) return arg_fault(entry, "the temperature must be positive (1e-30 at least) and finite");
+  if (M > 0 && !target) return arg_fault(entry, "null scores");
+  if (!aligned(target, dtype_bytes(dtype)) || !aligned(draft, dtype_bytes(dtype))) return arg_fault(entry, "misaligned scores");
+  if (target_stride < vocab || (draft && draft_stride < vocab)) return arg_fault(entry, "rows of scores overlap");
+  if (scratch_bytes < ad_accept_sampled_scratch_bytes(M, vocab, draft != nullptr)) return op_fail(AD_ERR_CAPACITY, entry, "scratch too small");
+  if (!scratch || !aligned(scratch, 256)) return arg_fault(entry, "scratch must be 256-byte aligned");
+  sampled::Params p;
+  p.score[0] = target; p.score[1] = M > 0 ? draft : nullptr; p.stride[0] = (size_t)target_stride; p.stride[1] = draft ? (size_t)draft_stride : 0;
+  const int z = p.score[1] ? 2 : 1;
+  p.vocab = vocab; p.parts = score_parts(M * z, vocab); p.M = M; p.B = B; p.kmax = kmax; p.eos = eos;
+  p.inv_t = 1.0 / (double)temperature; p.c = (float)(M_LOG2E * p.inv_t);
+  p.off = off; p.drafts = drafts; p.u = u; p.r = r; p.stats = static_cast<sampled::Stat*>(scratch); p.tokens = tokens; p.n_acc = n_accepted; p.status = status;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
+  if (M > 0)
+    e = launch_op(dtype == AD_DTYPE_BF16 ? sampled::score_stats_kernel<bf16> : sampled::score_stats_kernel<float>, dim3(M, p.parts, z),
+                  dim3(sampled::STAT_THREADS), dim3(), 0, st, p);
+  const int cluster = vocab > 4096 ? sampled::MAX_CLUSTER : 1;
+  if (e == cudaSuccess)
+    e = launch_op(dtype == AD_DTYPE_BF16 ? sampled::accept_sampled_kernel<bf16> : sampled::accept_sampled_kernel<float>, dim3(B * cluster),
+                  dim3(sampled::ACCEPT_THREADS), dim3(cluster), 0, st, p);
+  return launched(entry, e);
+}

@@ -1,0 +1,216 @@
+// Key/value cache in 8 bits with one scale per block of tokens and head: writing the tokens of a block into it and reading tokens back.
+#pragma once
+
+#include <cuda_fp16.h>
+#include <limits.h>
+
+#include "ad_common.cuh"
+
+namespace ad {
+namespace kv {
+
+// Codes, four at a time: `encode4` rounds to nearest, ties to even, and saturates; `decode4` is exact.
+struct E4m3 {
+  static constexpr float TOP = 448.f;
+  static __device__ __forceinline__ uint32_t encode4(const float* x) {
+    uint32_t w;
+    asm("{ .reg .b16 l, h; cvt.rn.satfinite.e4m3x2.f32 l, %2, %1; cvt.rn.satfinite.e4m3x2.f32 h, %4, %3; mov.b32 %0, {l, h}; }"
+        : "=r"(w) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]));
+    return w;
+  }
+  static __device__ __forceinline__ void decode4(uint32_t w, float* x) {
+    uint32_t a, b;
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(a), "=r"(b) : "r"(w));
+    const float2 p = __half22float2(*reinterpret_cast<__half2*>(&a)), q = __half22float2(*reinterpret_cast<__half2*>(&b));
+    x[0] = p.x; x[1] = p.y; x[2] = q.x; x[3] = q.y;
+  }
+};
+struct Int8 {
+  static constexpr float TOP = 127.f;
+  static __device__ __forceinline__ uint32_t encode4(const float* x) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= (uint32_t)(uint8_t)(int8_t)__float2int_rn(fminf(fmaxf(x[i], -TOP), TOP)) << (8 * i);
+    return w;
+  }
+  static __device__ __forceinline__ void decode4(uint32_t w, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i));
+  }
+};
+
+// The smallest power of two s with amax / s <= TOP (2^-126 at least; 1 where there is nothing but zeros).  TOP = 1.75 * 2^8 or 1.984375 * 2^6:
+// with amax = f * 2^e, 1 <= f < 2, s is 2^(e - 8) or 2^(e - 6) while f is within TOP's mantissa and twice that beyond it.
+template <typename F>
+__device__ __forceinline__ float block_scale(float amax) {
+  if (amax == 0.f) return 1.f;
+  const uint32_t top = __float_as_uint(F::TOP), a = __float_as_uint(amax);
+  const int e = (int)(a >> 23) - (int)(top >> 23) + ((a & 0x7fffffu) > (top & 0x7fffffu) ? 1 : 0);
+  return __uint_as_float((uint32_t)max(e + 127, 1) << 23);             // (a subnormal amax has a >> 23 == 0: the smallest scale)
+}
+
+struct Cache {
+  uint8_t* codes[2];             // keys, values: [n_blocks, heads, block, dim]
+  float* scale[2];               // [n_blocks, heads]
+  const int* table;              // [B, table_stride] or null
+  int table_stride, n_blocks, heads, block;
+  // block i of row b; negative when the table names none that exists
+  __host__ __device__ __forceinline__ int find(int b, int i) const {
+    const int id = table ? table[(size_t)b * table_stride + i] : b * table_stride + i;
+    return (unsigned)id < (unsigned)n_blocks ? id : -1;
+  }
+};
+
+// Whether a row's n tokens o .. o + n - 1 of M can go to positions p .. of it (in_row = n), or look at its first p (in_row = 0): AD_OK or what is wrong.
+__host__ __device__ __forceinline__ int row_fault(const Cache& c, int o, int n, int p, int M, int max_new, int in_row) {
+  if (o < 0 || n < 0 || n > max_new || o > M - n || p < 0) return AD_ERR_ARG;
+  return p > c.table_stride * c.block - in_row ? AD_ERR_CAPACITY : AD_OK;
+}
+// The tokens off[b] .. off[b + 1] of row b, in the row from position len[b] on or (outside) only looking at it.  False: nothing to do; what cannot be
+// done is latched.
+__device__ __forceinline__ bool row_tokens(const Cache& c, const int* off, const int* len, int b, int M, int max_new, bool outside, int* status, int& o,
+                                           int& n, int& p) {
+  o = __ldcg(off + b);
+  const long long d = (long long)__ldcg(off + b + 1) - o;
+  n = d < -1 || d > INT_MAX ? -1 : (int)d;
+  p = __ldcg(len + b);
+  if (n == 0) return false;
+  const int fault = row_fault(c, o, n, p, M, max_new, outside ? 0 : n);
+  if (fault != AD_OK) latch_error(status, fault);
+  return fault == AD_OK;
+}
+
+// Eight consecutive numbers of FP32 or BF16.
+__device__ __forceinline__ void load8(const float* p, float* x) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16* p, float* x) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void store8(float* p, const float* x) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store8(bf16* p, const float* x) {
+  __nv_bfloat162 w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+  *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(w);
+}
+
+// Writes row b's new tokens into the blocks they fall in.  A block's scale comes from what it holds afterwards: the tokens in front (what their
+// codes stand for) and the new ones, so that tokens which were written and then given up leave no trace in it.  Scales are powers of two: a live
+// code that gets another scale is only moved by whole binary places, exact in E4M3 above the subnormals of the new scale, and in INT8 off by half a
+// step of the new scale; steps at least double from one rounding to the next, so all of a value's roundings together stay below one step of the
+// largest scale that its block ever had.
+// One CTA per block of tokens, head and keys / values; its numbers stay in registers between the maximum and the codes, so that everything is read
+// and written once.  Bound by bytes.
+// grid = (2 * heads, blocks a row's new tokens may touch, B), block = max(32, block * dim / 32) threads.
+constexpr int VECS = 4;                // vectors of eight numbers a thread holds
+template <typename T, typename F>
+__global__ void __launch_bounds__(512)
+cache_append_kernel(Cache c, const T* __restrict__ k, const T* __restrict__ v, size_t stride, int dim, const int* __restrict__ off,
+                    const int* __restrict__ len, int M, int max_new, int* status) {
+  __shared__ float s_max[16];
+  pdl_launch();
+  pdl_wait();
+  const int b = blockIdx.z, which = blockIdx.x & 1, head = blockIdx.x >> 1;
+  int o, n, p;
+  if (!row_tokens(c, off, len, b, M, max_new, false, status, o, n, p)) return;
+  const int i = p / c.block + blockIdx.y, base = i * c.block;
+  if (base >= p + n) return;
+  const int id = c.find(b, i);
+  if (id < 0) { latch_error(status, AD_ERR_ARG); return; }
+  const int live = max(p - base, 0), end = min(p + n - base, c.block);          // tokens in front, end of the new ones
+  uint8_t* codes = (which ? c.codes[1] : c.codes[0]) + ((size_t)id * c.heads + head) * c.block * dim;
+  float* scale = (which ? c.scale[1] : c.scale[0]) + (size_t)id * c.heads + head;
+  const T* src = (which ? v : k) + (size_t)head * dim;
+  const float old = live ? __ldcg(scale) : 1.f;
+  const int per_token = dim / 8, vecs = c.block * per_token;
+
+  float x[VECS][8], amax = 0.f;
+  bool nan = false;
+#pragma unroll
+  for (int u = 0; u < VECS; ++u) {
+    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
+    if (e < vecs && t < live) {
+      const uint2 w = __ldcg(reinterpret_cast<const uint2*>(codes + t * dim + d));
+      F::decode4(w.x, x[u]);
+      F::decode4(w.y, x[u] + 4);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[u][j] *= old;
+    } else if (e < vecs && t < end) {
+      load8(src + (size_t)(o + base + t - p) * stride + d, x[u]);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < VECS; ++u)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float a = fabsf(x[u][j]);
+      if (a < INFINITY) amax = fmaxf(amax, a);                                  // (infinities saturate, whatever the scale)
+      else if (a != a) { nan = true; x[u][j] = 0.f; }
+    }
+  if (nan) latch_error(status, AD_ERR_ARG);
+  amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
+  if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = amax;
+  __syncthreads();
+  for (int w = 0; w < (int)blockDim.x >> 5; ++w) amax = fmaxf(amax, s_max[w]);
+  const float s = block_scale<F>(amax), inv = 1.f / s;                          // (both powers of two)
+#pragma unroll
+  for (int u = 0; u < VECS; ++u) {
+    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 8;
+    if (e >= vecs || t >= end || (t < live && s == old)) continue;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[u][j] *= inv;
+    *reinterpret_cast<uint2*>(codes + t * dim + d) = make_uint2(F::encode4(x[u]), F::encode4(x[u] + 4));
+  }
+  if (threadIdx.x == 0) *scale = s;
+}
+
+// Reads tokens start[b] .. of row b back into k, v [M, heads, dim].  grid and block as above.
+template <typename T, typename F>
+__global__ void __launch_bounds__(512)
+cache_read_kernel(Cache c, T* __restrict__ k, T* __restrict__ v, int dim, const int* __restrict__ off, const int* __restrict__ start, int M, int max_tokens,
+                  int* status) {
+  pdl_launch();
+  pdl_wait();
+  const int b = blockIdx.z, which = blockIdx.x & 1, head = blockIdx.x >> 1;
+  int o, n, p;
+  if (!row_tokens(c, off, start, b, M, max_tokens, false, status, o, n, p)) return;
+  const int i = p / c.block + blockIdx.y, base = i * c.block;
+  if (base >= p + n) return;
+  const int id = c.find(b, i);
+  if (id < 0) { latch_error(status, AD_ERR_ARG); return; }
+  const int from = max(p - base, 0), end = min(p + n - base, c.block);
+  const uint8_t* codes = (which ? c.codes[1] : c.codes[0]) + ((size_t)id * c.heads + head) * c.block * dim;
+  const float s = __ldcg((which ? c.scale[1] : c.scale[0]) + (size_t)id * c.heads + head);
+  T* dst = (which ? v : k) + (size_t)head * dim;
+  const int per_token = dim / 8, vecs = c.block * per_token;
+  uint2 w[VECS];
+#pragma unroll
+  for (int u = 0; u < VECS; ++u) {
+    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 8;
+    if (e < vecs && t >= from && t < end) w[u] = __ldcg(reinterpret_cast<const uint2*>(codes + t * dim + d));
+  }
+#pragma unroll
+  for (int u = 0; u < VECS; ++u) {
+    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 8;
+    if (e >= vecs || t < from || t >= end) continue;
+    float x[8];
+    F::decode4(w[u].x, x);
+    F::decode4(w[u].y, x + 4);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= s;
+    store8(dst + (size_t)(o + base + t - p) * c.heads * dim + d, x);
+  }
+}
+
+}  // namespace kv
+}  // namespace ad
