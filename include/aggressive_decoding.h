@@ -365,10 +365,12 @@ int ad_cache_read(const ad_kv_cache* cache, void* k, void* v, int32_t dtype, con
  * causal != 0 (self-attention of a block, appended before): query i of row b sees the row's first len[b] + i + 1 positions;
  * causal == 0 (keys of an encoder): all queries of the row see its first len[b].  A query that sees nothing gets zeros.
  * Positions beyond are never looked at.  max_keys: longest row to plan for; longer ones are computed as well, only slower.
- * Probabilities and sums are held in FP32; with BF16 queries the probabilities are rounded to 11 bits in front of the product
- * with the values, with FP32 ones to 22.  scratch: ad_cache_attention_scratch_bytes() of device memory, 256-byte aligned (NULL
- * when that is 0); calls that may overlap need scratch of their own. */
-size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* cache, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys);
+ * Probabilities and sums are held in FP32.  In front of the product with the values, probabilities (times the scale of the
+ * values' block) are rounded to 11 bits with BF16 queries, to 22 with FP32 ones, and no finer than 2^-37 of a query's largest.
+ * scratch: ad_cache_attention_scratch_bytes() of device memory, 256-byte aligned (NULL when that is 0); calls that may overlap
+ * need scratch of their own. */
+size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* cache, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new,
+                                        int32_t max_keys);
 int ad_cache_attention(const ad_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads,
                        const int32_t* off, const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t max_keys,
                        int32_t causal, float scale, void* out, void* scratch, size_t scratch_bytes, int32_t* status, void* stream);

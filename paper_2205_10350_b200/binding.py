@@ -105,7 +105,7 @@ def load():
         "ad_linear": (C.c_int, [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]),
         "ad_cache_append": (C.c_int, [cache, vp, vp, i32, i64, vp, vp, i32, i32, i32, vp, vp]),
         "ad_cache_read": (C.c_int, [cache, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp]),
-        "ad_cache_attention_scratch_bytes": (sz, [cache, i32, i32, i32, i32]),
+        "ad_cache_attention_scratch_bytes": (sz, [cache, i32, i32, i32, i32, i32]),
         "ad_cache_attention": (C.c_int, [cache, vp, i32, i64, i32, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, sz, vp, vp]),
         "ad_accept_sampled_scratch_bytes": (sz, [i32, i32, i32]),
         "ad_accept_sampled": (C.c_int, [vp, i64, vp, i64, i32, f32, i32, vp, vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, sz, vp, vp]),
@@ -593,7 +593,7 @@ def cache_attention(cache, q_t, off_t, len_t, max_new, max_keys, causal=True, sc
     scale = cache.head_dim ** -0.5 if scale is None else float(scale)
 
     def call(stream):
-        nbytes = lib.ad_cache_attention_scratch_bytes(cache._ref, H, B, max_new, max_keys)
+        nbytes = lib.ad_cache_attention_scratch_bytes(cache._ref, dtype, H, B, max_new, max_keys)
         keep, scratch = _scratch(q_t, nbytes) if nbytes else (None, None)
         return lib.ad_cache_attention(cache._ref, q_t.data_ptr(), dtype, stride, H, off_t.data_ptr(), len_t.data_ptr(), B, M, max_new, max_keys,
                                       1 if causal else 0, scale, out.data_ptr(), scratch, nbytes, status, stream)

@@ -2723,6 +2723,7 @@ int ad::op_fail(int code, const char* entry, const char* why) noexcept {
     return code;
   }
 }
+int ad::op_device() { return current_device(); }
 int ad::op_num_sms() { return num_sms(); }
 bool ad::op_early_launch() { return use_pdl(); }
 

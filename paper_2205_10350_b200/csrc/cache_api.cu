@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "accept_sampled.cuh"
 #include "ad_common.cuh"
@@ -104,9 +105,53 @@ extern "C" int ad_cache_read(const ad_kv_cache* c, void* k, void* v, int32_t dty
   }));
 }
 
-extern "C" size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
-  (void)c; (void)n_heads; (void)B; (void)max_new; (void)max_keys;
-  return 0;
+namespace {
+struct AttendPlan { int mt, row_tiles, splits; };
+// Rows of queries a CTA takes: 16 where that is all there are, else 32.  Keys are split while CTAs do not fill the GPU's shared memory once and every
+// warp has two units at least.
+AttendPlan attend_plan(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
+  AttendPlan plan;
+  const int rows = max_new * (n_heads / c->n_kv_heads);
+  plan.mt = rows <= 16 ? 1 : 2;
+  plan.row_tiles = (rows + 16 * plan.mt - 1) / (16 * plan.mt);
+  const int resident = std::max(1, std::min(6, 227 * 1024 / (kv::att_smem(c->head_dim, plan.mt, dtype == AD_DTYPE_FP32) + 1024)));
+  const int64_t base = (int64_t)B * c->n_kv_heads * plan.row_tiles;
+  const int units = (max_keys + kv::UNIT - 1) / kv::UNIT;
+  plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)op_num_sms() * resident / base, units / (2 * kv::ATT_WARPS), 256}));
+  return plan;
+}
+size_t attend_part_bytes(const ad_kv_cache* c, const AttendPlan& plan, int32_t B) {
+  return plan.splits == 1 ? 0 : (size_t)B * c->n_kv_heads * plan.row_tiles * 16 * plan.mt * plan.splits * (c->head_dim + 2) * sizeof(float);
+}
+bool attend_sizes(const ad_kv_cache* c, int32_t n_heads, int32_t max_new) {
+  return n_heads >= 1 && n_heads <= 65535 && n_heads % c->n_kv_heads == 0 && (int64_t)max_new * (n_heads / c->n_kv_heads) <= (1 << 24);
+}
+
+template <typename T, typename F, int DIM, int MT>
+cudaError_t launch_attention(const kv::AttendParams& a, int B, cudaStream_t st) {
+  static std::atomic<uint64_t> raised{0};              // devices on which the kernel may use its shared memory
+  auto kernel = kv::cache_attention_kernel<T, F, DIM, MT>;
+  constexpr int smem = kv::att_smem(DIM, MT, sizeof(T) == 4);
+  const uint64_t bit = 1ull << op_device();
+  if (!(raised.load(std::memory_order_relaxed) & bit)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    raised.fetch_or(bit, std::memory_order_relaxed);
+  }
+  cudaError_t e = launch_op(kernel, dim3(a.row_tiles * a.splits, a.c.heads, B), dim3(32 * kv::ATT_WARPS), dim3(), smem, st, a);
+  if (e == cudaSuccess && a.splits > 1)
+    e = launch_op(kv::cache_attention_join_kernel<T, DIM, MT>, dim3((a.row_tiles * 16 * MT * (DIM / 8) + 127) / 128, a.c.heads, B), dim3(128), dim3(), 0, st, a);
+  return e;
+}
+template <typename T, typename F, int MT>
+cudaError_t launch_attention_dim(const kv::AttendParams& a, int dim, int B, cudaStream_t st) {
+  return dim == 32 ? launch_attention<T, F, 32, MT>(a, B, st) : dim == 64 ? launch_attention<T, F, 64, MT>(a, B, st) : launch_attention<T, F, 128, MT>(a, B, st);
+}
+}  // namespace
+
+extern "C" size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
+  if (cache_fault(c, B) || B < 1 || max_new < 1 || max_keys < 0 || !known_dtype(dtype) || !attend_sizes(c, n_heads, max_new)) return 0;
+  return attend_part_bytes(c, attend_plan(c, dtype, n_heads, B, max_new, max_keys), B);
 }
 
 extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
@@ -116,24 +161,26 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
   if (const char* why = batch_fault(off, len, B, M, max_new)) return arg_fault(entry, why);
   if (const char* why = cache_fault(c, B)) return arg_fault(entry, why);
   if (!known_dtype(dtype)) return arg_fault(entry, "unknown dtype");
-  if (n_heads < 1 || n_heads % c->n_kv_heads || n_heads > 65535) return arg_fault(entry, "query heads must be a multiple of the cache's (and at most 65535)");
-  if (max_new > 65535) return arg_fault(entry, "at most 65535 queries of a row");
+  if (!attend_sizes(c, n_heads, max_new)) return arg_fault(entry, "query heads must be a multiple of the cache's, at most 65535, and max_new times their ratio at most 2^24");
   if (max_keys < 0) return arg_fault(entry, "negative number of keys");
   if (!(scale > 0.f) || !(scale < INFINITY)) return arg_fault(entry, "the scale must be positive and finite");
   if (M == 0) return AD_OK;
   if (!q || !out || !aligned(q, 16) || !aligned(out, 16)) return arg_fault(entry, "queries and result must be 16-byte aligned");
   if (q_stride < (int64_t)n_heads * c->head_dim || q_stride % (int64_t)(16 / dtype_bytes(dtype)))
     return arg_fault(entry, "queries must be a multiple of 16 bytes apart, and not overlap");
-  if (scratch_bytes < ad_cache_attention_scratch_bytes(c, n_heads, B, max_new, max_keys)) return op_fail(AD_ERR_CAPACITY, entry, "scratch too small");
-  (void)scratch;
+  const AttendPlan plan = attend_plan(c, dtype, n_heads, B, max_new, max_keys);
+  const size_t need = attend_part_bytes(c, plan, B);
+  if (scratch_bytes < need) return op_fail(AD_ERR_CAPACITY, entry, "scratch too small");
+  if (need && (!scratch || !aligned(scratch, 256))) return arg_fault(entry, "scratch must be 256-byte aligned");
   kv::AttendParams a;
   a.c = device_cache(c); a.q = q; a.q_stride = (size_t)q_stride; a.out = out; a.n_heads = n_heads; a.M = M; a.max_new = max_new; a.off = off; a.len = len;
   a.causal = causal != 0; a.scale = scale * (float)M_LOG2E; a.status = status;
+  a.row_tiles = plan.row_tiles; a.splits = plan.splits; a.part = static_cast<float*>(scratch);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
   return launched(entry, by_types(dtype, c->format, [&](auto t) {
     typedef typename decltype(t)::Num T;
     typedef typename decltype(t)::Fmt F;
-    auto kernel = c->head_dim == 32 ? kv::cache_attention_kernel<T, F, 32> : c->head_dim == 64 ? kv::cache_attention_kernel<T, F, 64> : kv::cache_attention_kernel<T, F, 128>;
-    return launch_op(kernel, dim3(n_heads, max_new, B), dim3(32), dim3(), 0, static_cast<cudaStream_t>(stream), a);
+    return plan.mt == 1 ? launch_attention_dim<T, F, 1>(a, c->head_dim, B, st) : launch_attention_dim<T, F, 2>(a, c->head_dim, B, st);
   }));
 }
 

@@ -1,6 +1,8 @@
 // Attention of the tokens of a block over the 8-bit key/value cache (kv_cache.cuh).
 #pragma once
 
+#include <float.h>
+
 #include "kv_cache.cuh"
 
 namespace ad {
@@ -17,55 +19,492 @@ struct AttendParams {
   int causal;
   float scale;             // softmax scale times log2(e)
   int* status;
+  int row_tiles, splits;   // row tiles a row's queries may have; parts its keys are split into
+  float* part;             // splits > 1: [tile rows][splits][dim] sums, then [tile rows][splits] maxima and sums of exponentials
 };
 
-// One warp per query and head: lanes share the head's numbers, keys one after the other, running maximum and sum of the softmax in FP32.
-// grid = (n_heads, max_new, B), block = 32.
-template <typename T, typename F, int DIM>
-__global__ void __launch_bounds__(32)
+constexpr int UNIT = 32;               // keys that a warp works on at a time
+constexpr int ATT_WARPS = 4;
+__host__ __device__ constexpr int att_stages(int dim) { return dim == 128 ? 3 : 4; }
+__host__ __device__ constexpr int att_stage_bytes(int dim) { return 2 * UNIT * dim + 16; }
+__host__ __device__ constexpr int att_q_bytes(int dim, int mt, bool fp32) { return mt * (dim / 16) * 512 * (fp32 ? 2 : 1); }
+__host__ __device__ constexpr int att_smem(int dim, int mt, bool fp32) {
+  return att_q_bytes(dim, mt, fp32) + ATT_WARPS * att_stages(dim) * att_stage_bytes(dim);
+}
+
+// 2^x to 2^-22 of itself; 0 for -inf.
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t w;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+  return w;
+}
+__device__ __forceinline__ float2 unpack_f16(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
+// What rounding a pair to FP16 leaves over, in FP16.
+__device__ __forceinline__ uint32_t rest_f16(float lo, float hi, uint32_t w) {
+  const float2 f = unpack_f16(w);
+  return pack_f16(lo - f.x, hi - f.y);
+}
+__device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Four codes to FP16, exactly: lo holds the first two, hi the others.
+__device__ __forceinline__ void codes_f16(E4m3, uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+__device__ __forceinline__ void codes_f16(Int8, uint32_t w, uint32_t& lo, uint32_t& hi) {
+  // c + 128 as the low byte of 0x6400 is 1152 + c
+  w ^= 0x80808080u;
+  const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
+  const __half2 bias = __float2half2_rn(1152.f);
+  const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), y = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
+  lo = *reinterpret_cast<const uint32_t*>(&x);
+  hi = *reinterpret_cast<const uint32_t*>(&y);
+}
+__device__ __forceinline__ void cp4(void* smem_dst, const void* gmem_src) {
+  const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(smem_dst));
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(s), "l"(gmem_src) : "memory");
+}
+
+// Key (of a unit) that column n of score tile nt stands for.  The scores of a thread's columns 2c, 2c + 1 in tiles 2j, 2j + 1 are, as they lie, its
+// part of the probabilities' operand of the second product; this order makes them keys 16 j + c + {0, 4, 8, 12}, which reads values without bank conflicts.
+__device__ __forceinline__ int unit_key(int nt, int n) { return 16 * (nt >> 1) + (n >> 1) + 4 * ((nt & 1) * 2 + (n & 1)); }
+
+// Attention of 16 MT rows (queries of one row of the batch times the query heads that share a key/value head) over a part of the row's keys.
+//
+// What a number goes through.  Codes are exact in FP16, and so are queries once a power of two has brought the row's largest to 2^13 (BF16 has 8 bits;
+// FP32 goes in as two FP16 numbers, 22 bits, and so do its probabilities).  Scores are FP32: the keys' scale, the softmax scale and the query's power
+// of two come in one factor per block and row.  Probabilities meet the values' scale before they are rounded: p * vs, as a multiple of its largest
+// value so far in the row (2^d times what the softmax's own maximum m stands for), times 2^14: nothing that matters comes near FP16's subnormals,
+// however far the blocks' scales are apart.  Sums, maxima and results are FP32.
+//
+// Why this shape.  What has to be read is 2 * dim bytes a key; 16 rows make 64 operations a byte of it, which mma.sync delivers several times over, so the kernel
+// is a stream of the cache with as little as possible per byte: each warp copies its own units of 32 keys through its own ring in shared memory
+// (16-byte asynchronous copies, zeros where no key is), nothing but __syncwarp between them, and keeps maximum, sum and result in registers until its
+// keys are through; the four warps' results are joined at the end.  The 16-byte pieces lie in shared memory so that both products' operands come out
+// of it whole, in the registers where mma wants them, without a transposition: dims and keys may be summed in any order.
+// grid = (row_tiles * splits, heads, B), block = 32 * ATT_WARPS.
+template <typename T, typename F, int DIM, int MT>
+__global__ void __launch_bounds__(32 * ATT_WARPS)
 cache_attention_kernel(AttendParams a) {
-  constexpr int PER = DIM / 32;
+  constexpr bool WIDE = sizeof(T) == 4;               // two FP16 numbers for each query and probability
+  constexpr int HL = WIDE ? 2 : 1;
+  constexpr int KSTEPS = DIM / 16, NT = DIM / 8, ROWS = 16 * MT;
+  constexpr int STAGES = att_stages(DIM), STAGE = att_stage_bytes(DIM), COPIES = DIM / 16;
+  constexpr float P_TOP = 16384.f;
+  constexpr int P_BITS = 14;
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ float s_rf[ROWS];
+  uint4* sq = reinterpret_cast<uint4*>(smem);          // [HL][MT][KSTEPS][lane]: operands as mma wants them
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+  unsigned char* ring = smem + att_q_bytes(DIM, MT, WIDE) + warp * STAGES * STAGE;
   pdl_launch();
   pdl_wait();
-  const int b = blockIdx.z, i = blockIdx.y, head = blockIdx.x, lane = threadIdx.x;
+  const int b = blockIdx.z, kvh = blockIdx.y, rt = blockIdx.x % a.row_tiles, split = blockIdx.x / a.row_tiles;
   int o, n, p;
-  if (!row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, o, n, p) || i >= n) return;
-  const int keys = a.causal ? p + i + 1 : p, kvh = head / (a.n_heads / a.c.heads);
-  const T* q = static_cast<const T*>(a.q) + (size_t)(o + i) * a.q_stride + (size_t)head * DIM + lane * PER;
-  T* out = static_cast<T*>(a.out) + ((size_t)(o + i) * a.n_heads + head) * DIM + lane * PER;
-  float qv[PER], acc[PER], m = -INFINITY, sum = 0.f;
+  if (!row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, o, n, p)) return;
+  const int group = a.n_heads / a.c.heads, rows = n * group, r0 = rt * ROWS;
+  if (r0 >= rows) return;
+  const int r_last = min(r0 + ROWS, rows) - 1;
+  auto visible = [&](int r) { return a.causal ? p + min(r, r_last) / group + 1 : p; };
+  const int vis_min = visible(r0), vis_max = visible(r_last);
+  const int units = (vis_max + UNIT - 1) / UNIT, workers = a.splits * ATT_WARPS, w = split * ATT_WARPS + warp;
+  const int u0 = (int)((long long)units * w / workers), u1 = (int)((long long)units * (w + 1) / workers);
+
+  // ---- the ring ----
+  const uint8_t* kc = a.c.codes[0];
+  const uint8_t* vc = a.c.codes[1];
+  const int block = a.c.block, pieces = block == 16 ? 2 : 1;     // blocks that a unit lies in
+  int ids[2] = {0, 0}, id_base = u0;                             // lane i: block(s) of unit id_base + i
+  auto look_up = [&](int base) {
+    id_base = base;
+    const int u = base + lane;
 #pragma unroll
-  for (int j = 0; j < PER; ++j) { qv[j] = to_f32(q[j]); acc[j] = 0.f; }
-  for (int j0 = 0; j0 < keys; j0 += a.c.block) {
-    const int id = a.c.find(b, j0 / a.c.block);
-    if (id < 0) { latch_error(a.status, AD_ERR_ARG); continue; }
-    const size_t tile = (size_t)id * a.c.heads + kvh;
-    const float ks = a.c.scale[0][tile], vs = a.c.scale[1][tile];
-    for (int t = 0; t < a.c.block && j0 + t < keys; ++t) {
-      const uint8_t* kc = a.c.codes[0] + (tile * a.c.block + t) * DIM + lane * PER;
-      const uint8_t* vc = a.c.codes[1] + (tile * a.c.block + t) * DIM + lane * PER;
-      float kx[4], vx[4], s = 0.f;
-      uint32_t kw = 0, vw = 0;
+    for (int z = 0; z < 2; ++z) {
+      const int pos = u * UNIT + 16 * z;
+      ids[z] = u < u1 && pos < vis_max && z < pieces ? a.c.find(b, pos / block) : 0;
+      if (ids[z] < 0) latch_error(a.status, AD_ERR_ARG);
+    }
+  };
+  auto issue = [&](int u, int stage) {
+    if (u >= u1) return;
+    if (u - id_base >= 32) look_up(u);
+    unsigned char* st = ring + stage * STAGE;
+    const int first = u * UNIT;
+    size_t tile[2];
+    bool there[2];
 #pragma unroll
-      for (int j = 0; j < PER; ++j) { kw |= (uint32_t)kc[j] << (8 * j); vw |= (uint32_t)vc[j] << (8 * j); }
-      F::decode4(kw, kx);
-      F::decode4(vw, vx);
+    for (int z = 0; z < 2; ++z) {
+      const int id = __shfl_sync(0xffffffffu, ids[z], u - id_base);
+      there[z] = id >= 0;
+      tile[z] = (size_t)max(id, 0) * a.c.heads + kvh;
+    }
+    const int in_block = first & (block - 1);
 #pragma unroll
-      for (int j = 0; j < PER; ++j) s += qv[j] * kx[j];
+    for (int i = 0; i < COPIES; ++i) {
+      const int byte = i * 512 + lane * 16, key = byte / DIM, x = byte % DIM / 16;           // key of the unit, 16-byte piece of it
+      const int z = pieces == 2 && i >= COPIES / 2 ? 1 : 0;
+      const size_t src = tile[z] * block * DIM + (pieces == 2 ? byte - z * 16 * DIM : in_block * DIM + byte);
+      const bool on = there[z] && first + key < vis_max;
+      // keys in the order of score columns, values in the order of keys
+      const int col = (key >> 4) * 16 + ((key >> 3) & 1) * 8 + ((key & 3) << 1) + ((key >> 2) & 1);
+      const int kx = DIM == 128 ? x ^ ((col & 1) << 2) : x;
+      const int vx = DIM == 128 ? x ^ ((key & 3) << 1) : DIM == 64 ? x ^ (((key >> 1) & 1) << 1) : x;
+      cp16(st + col * DIM + kx * 16, kc + src, on);
+      cp16(st + UNIT * DIM + key * DIM + vx * 16, vc + src, on);
+    }
+    if (lane < 4) {                                               // ks0, ks1, vs0, vs1; negative: no such block
+      const int z = lane & 1;
+      float* dst = reinterpret_cast<float*>(st + 2 * UNIT * DIM) + lane;
+      const bool need = z < pieces && first + 16 * z < vis_max;
+      if (need && (z ? there[1] : there[0])) cp4(dst, (lane < 2 ? a.c.scale[0] : a.c.scale[1]) + (z ? tile[1] : tile[0]));
+      else *dst = need && lane < 2 ? -1.f : 1.f;
+    }
+  };
+  look_up(u0);
 #pragma unroll
-      for (int w = 16; w; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
-      s *= ks * a.scale;
-      const float top = fmaxf(m, s);
-      const float keep = m == top ? 1.f : exp2f(m - top), e = exp2f(s - top);
-      m = top;
-      sum = sum * keep + e;
+  for (int s = 0; s < STAGES - 1; ++s) {
+    issue(u0 + s, s);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+
+  // ---- queries: the row's power of two, FP16, into operand order ----
+  // Thread's dims in step j: 64 (j / 4) + 16 c + 4 (j % 4) + 0 .. 3 (DIM = 32: 8 c + 4 j + 0 .. 3)
+  for (int r = warp; r < ROWS; r += ATT_WARPS) {
+    constexpr int PER = DIM / 32;
+    const int row = r0 + r;
+    float x[PER], top = 0.f;
 #pragma unroll
-      for (int j = 0; j < PER; ++j) acc[j] = acc[j] * keep + e * (vs * vx[j]);
+    for (int i = 0; i < PER; ++i) x[i] = 0.f;
+    if (row <= r_last) {
+      const T* q = static_cast<const T*>(a.q) + (size_t)(o + row / group) * a.q_stride + ((size_t)kvh * group + row % group) * DIM + lane * PER;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) { x[i] = to_f32(q[i]); top = fmaxf(top, fabsf(x[i])); }
+    }
+    const uint32_t e = min(max(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23, 27u), 253u);     // exponent, 2^-100 .. 2^126
+    const float up = __uint_as_float((267u - e) << 23);            // 2^(13 - exponent)
+    if (lane == 0) s_rf[r] = a.scale * (1.f / up);
+#pragma unroll
+    for (int i = 0; i < PER; i += (PER > 1 ? 2 : 1)) {
+      // one number (DIM = 32) or pairs
+      const int d = lane * PER + i;
+      const int j = DIM == 32 ? (d >> 2) & 1 : (d >> 6) * 4 + ((d >> 2) & 3), cc = DIM == 32 ? d >> 3 : (d >> 4) & 3, half = (d >> 1) & 1;
+      const int mt = r >> 4, word = half * 2 + ((r >> 3) & 1), ln = (r & 7) * 4 + cc;
+      const float y0 = x[i] * up, y1 = PER > 1 ? x[PER > 1 ? i + 1 : 0] * up : 0.f;
+      const uint32_t hi = pack_f16(y0, y1), lo = rest_f16(y0, y1, hi);
+#pragma unroll
+      for (int h = 0; h < HL; ++h) {
+        unsigned char* dst = reinterpret_cast<unsigned char*>(sq + ((h * MT + mt) * KSTEPS + j) * 32 + ln) + word * 4;
+        if (PER > 1) *reinterpret_cast<uint32_t*>(dst) = h ? lo : hi;
+        else reinterpret_cast<uint16_t*>(dst)[d & 1] = (uint16_t)(h ? lo : hi);
+      }
     }
   }
-  const float inv = keys ? 1.f / sum : 0.f;
+  __syncthreads();
+  float rf[MT][2], m[MT][2], d[MT][2], l[MT][2], acc[MT][NT][4];
+  bool large = false;                                 // scores whose steps in FP32 are a quarter and more
+  int vis[MT][2];
 #pragma unroll
-  for (int j = 0; j < PER; ++j) out[j] = from_f32<T>(acc[j] * inv);
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = t * 16 + h * 8 + g;
+      rf[t][h] = s_rf[r];
+      vis[t][h] = visible(r0 + r);
+      m[t][h] = d[t][h] = -INFINITY;
+      l[t][h] = 0.f;
+    }
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[t][i][j] = 0.f;
+  // queries of few steps stay in registers
+  constexpr bool Q_REGS = HL * MT * KSTEPS <= 8;
+  uint4 qr[Q_REGS ? HL : 1][Q_REGS ? MT : 1][Q_REGS ? KSTEPS : 1];
+  if constexpr (Q_REGS) {
+#pragma unroll
+    for (int h = 0; h < HL; ++h)
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int j = 0; j < KSTEPS; ++j) qr[h][t][j] = sq[((h * MT + t) * KSTEPS + j) * 32 + lane];
+  }
+
+  int stage = 0;
+  for (int u = u0; u < u1; ++u) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+    __syncwarp();
+    issue(u + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    const unsigned char* st = ring + stage * STAGE;
+    stage = stage == STAGES - 1 ? 0 : stage + 1;
+    const float4 sc = *reinterpret_cast<const float4*>(st + 2 * UNIT * DIM);
+    // ---- scores ----
+    float s[MT][4][4];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[t][nt][j] = 0.f;
+    constexpr int RAW = KSTEPS < 4 ? KSTEPS : 4;       // words of codes of one load
+#pragma unroll
+    for (int hh = 0; hh < KSTEPS / RAW; ++hh) {
+      uint32_t raw[4][RAW];
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt) {
+        const unsigned char* row = st + (nt * 8 + g) * DIM;
+        if constexpr (DIM == 32) {
+          const uint2 v = *reinterpret_cast<const uint2*>(row + c * 8);
+          raw[nt][0] = v.x; raw[nt][1] = v.y;
+        } else {
+          const int x = hh * 4 + c;
+          const uint4 v = *reinterpret_cast<const uint4*>(row + (DIM == 128 ? x ^ ((g & 1) << 2) : x) * 16);
+          raw[nt][0] = v.x; raw[nt][1] = v.y; raw[nt][RAW - 2] = v.z; raw[nt][RAW - 1] = v.w;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < RAW; ++j) {
+        uint4 qf[HL][MT];
+#pragma unroll
+        for (int h = 0; h < HL; ++h)
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            if constexpr (Q_REGS) qf[h][t] = qr[h][t][hh * RAW + j];
+            else qf[h][t] = sq[((h * MT + t) * KSTEPS + hh * RAW + j) * 32 + lane];
+          }
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+          uint32_t b0, b1;
+          codes_f16(F(), raw[nt][j], b0, b1);
+#pragma unroll
+          for (int h = HL - 1; h >= 0; --h)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) mma_f16(s[t][nt], reinterpret_cast<const uint32_t*>(&qf[h][t]), b0, b1);
+        }
+      }
+    }
+    if (u * UNIT + UNIT > vis_min || sc.x < 0.f || sc.y < 0.f) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (u * UNIT + unit_key(nt, 2 * c + (j & 1)) >= vis[t][j >> 1] || (pieces == 2 && nt >= 2 ? sc.y : sc.x) < 0.f) s[t][nt][j] = -INFINITY;
+    }
+    // ---- probabilities ----
+    float ks[2] = {fabsf(sc.x), pieces == 2 ? fabsf(sc.y) : fabsf(sc.x)};
+    float ve[2], vm[2];                                // the values' scales as a power of two and a number from 1 to 2 (times 2^14)
+    {
+      const uint32_t v0 = __float_as_uint(sc.z), v1 = pieces == 2 ? __float_as_uint(sc.w) : v0;
+      ve[0] = (float)((int)(v0 >> 23) - 127); ve[1] = (float)((int)(v1 >> 23) - 127);
+      vm[0] = __uint_as_float((v0 & 0x7fffffu) | 0x3f800000u) * P_TOP; vm[1] = __uint_as_float((v1 & 0x7fffffu) | 0x3f800000u) * P_TOP;
+    }
+    float ref[MT][2], top[MT][2], tod[MT][2], tk[MT][2][2];
+    bool moved = false;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float x0 = fmaxf(fmaxf(s[t][0][2 * h], s[t][0][2 * h + 1]), fmaxf(s[t][1][2 * h], s[t][1][2 * h + 1]));
+        float x1 = fmaxf(fmaxf(s[t][2][2 * h], s[t][2][2 * h + 1]), fmaxf(s[t][3][2 * h], s[t][3][2 * h + 1]));
+        if (pieces == 1) x0 = x1 = fmaxf(x0, x1);
+        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
+        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
+        if (pieces == 2) {
+          x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
+          x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
+        } else {
+          x1 = x0;
+        }
+        tk[t][h][0] = fmaxf(rf[t][h] * ks[0], FLT_MIN);
+        tk[t][h][1] = fmaxf(rf[t][h] * ks[1], FLT_MIN);
+        x0 = ceilf(x0 * tk[t][h][0]);                  // references are whole numbers: what goes from one to another is an exact power of two
+        x1 = ceilf(x1 * tk[t][h][1]);
+        top[t][h] = fmaxf(m[t][h], fmaxf(x0, x1));
+        ref[t][h] = top[t][h] == -INFINITY ? 0.f : top[t][h];
+        tod[t][h] = fmaxf(d[t][h] + (m[t][h] - ref[t][h]), fmaxf(x0 - ref[t][h] + ve[0], x1 - ref[t][h] + ve[1]));
+        moved |= top[t][h] != m[t][h] || tod[t][h] != d[t][h];
+      }
+    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float less = m[t][h] - ref[t][h], keep = ex2(less);
+          const float keep_o = tod[t][h] == -INFINITY ? 0.f : ex2(less + (d[t][h] - tod[t][h]));
+          m[t][h] = top[t][h];
+          d[t][h] = tod[t][h];
+          l[t][h] *= keep;
+#pragma unroll
+          for (int i = 0; i < NT; ++i) { acc[t][i][2 * h] *= keep_o; acc[t][i][2 * h + 1] *= keep_o; }
+          large |= fabsf(ref[t][h]) > 4194304.f;
+        }
+      large = __any_sync(0xffffffffu, large);
+    }
+    if (large) {                                       // the exponent below then is a difference of rounded scores, as the maximum is one of them
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) s[t][nt][2 * h + j] *= tk[t][h][nt >> 1];
+          tk[t][h][0] = tk[t][h][1] = 1.f;
+        }
+    }
+    uint32_t pf[HL][MT][2][4];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const float f = ex2(fminf(ve[z] - d[t][h], 100.f)) * vm[z];
+#pragma unroll
+          for (int nn = 0; nn < 2; ++nn) {
+            const float p0 = ex2(fmaf(s[t][2 * z + nn][2 * h], tk[t][h][z], -ref[t][h])), p1 = ex2(fmaf(s[t][2 * z + nn][2 * h + 1], tk[t][h][z], -ref[t][h]));
+            l[t][h] += p0 + p1;
+            const float y0 = p0 * f, y1 = p1 * f;
+            pf[0][t][z][nn * 2 + h] = pack_f16(y0, y1);
+            if constexpr (WIDE) pf[HL - 1][t][z][nn * 2 + h] = rest_f16(y0, y1, pf[0][t][z][nn * 2 + h]);
+          }
+        }
+      }
+    // ---- times values ----
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      constexpr int WORDS = DIM / 32;                  // words of a key's codes that the thread reads
+      uint32_t v[4][WORDS];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = 16 * j + c + 4 * i;
+        const unsigned char* row = st + UNIT * DIM + key * DIM;
+        if constexpr (DIM == 128) {
+          const uint4 x = *reinterpret_cast<const uint4*>(row + ((g ^ ((key & 3) << 1)) * 16));
+          v[i][0] = x.x; v[i][1] = x.y; v[i][WORDS - 2] = x.z; v[i][WORDS - 1] = x.w;
+        } else if constexpr (DIM == 64) {
+          const uint2 x = *reinterpret_cast<const uint2*>(row + ((g >> 1) ^ (((key >> 1) & 1) << 1)) * 16 + (g & 1) * 8);
+          v[i][0] = x.x; v[i][WORDS - 1] = x.y;
+        } else {
+          v[i][0] = *reinterpret_cast<const uint32_t*>(row + g * 4);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < WORDS; ++x)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t w0 = __byte_perm(v[0][x], v[1][x], y ? 0x7362 : 0x5140), w1 = __byte_perm(v[2][x], v[3][x], y ? 0x7362 : 0x5140);
+          uint32_t b0[2], b1[2];
+          codes_f16(F(), w0, b0[0], b0[1]);
+          codes_f16(F(), w1, b1[0], b1[1]);
+#pragma unroll
+          for (int d = 0; d < 2; ++d)
+#pragma unroll
+            for (int h = HL - 1; h >= 0; --h)
+#pragma unroll
+              for (int t = 0; t < MT; ++t) mma_f16(acc[t][4 * x + 2 * y + d], pf[h][t][j], b0[d], b1[d]);
+        }
+    }
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+
+  // ---- the warps' results together.  A thread holds dims DIM/4 * c .. of its rows, column tile i the i-th and (second column) the DIM/8 + i-th. ----
+  constexpr int PITCH = DIM + 4;
+  float* so = reinterpret_cast<float*>(smem);                     // [warps][ROWS][PITCH]
+  float* sm = so + ATT_WARPS * ROWS * PITCH;                      // [warps][ROWS] maxima, then sums
+  float* sl = sm + ATT_WARPS * ROWS;
+  static_assert((ATT_WARPS * ROWS * (PITCH + 2)) * 4 <= att_smem(DIM, MT, WIDE), "results fit where the ring was");
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = t * 16 + h * 8 + g;
+      float sum = l[t][h];
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      const float f = m[t][h] == -INFINITY && sum == 0.f ? 0.f : ex2(d[t][h] - (float)P_BITS);
+      float* dst = so + (warp * ROWS + r) * PITCH + c * (DIM / 4);
+#pragma unroll
+      for (int i = 0; i < NT; ++i) { dst[i] = acc[t][i][2 * h] * f; dst[DIM / 8 + i] = acc[t][i][2 * h + 1] * f; }
+      if (c == 0) { sm[warp * ROWS + r] = m[t][h]; sl[warp * ROWS + r] = sum; }
+    }
+  __syncthreads();
+  constexpr int LANES = DIM / 8, AT_ONCE = 32 * ATT_WARPS / LANES;      // threads a row, each eight dims
+  const int d0 = tid % LANES * 8;
+  const size_t tile_row = (((size_t)b * a.c.heads + kvh) * a.row_tiles + rt) * ROWS, all_rows = (size_t)gridDim.z * gridDim.y * a.row_tiles * ROWS;
+  for (int r = tid / LANES; r < ROWS && r0 + r <= r_last; r += AT_ONCE) {
+    float top = -INFINITY, sum = 0.f, x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = 0.f;
+#pragma unroll
+    for (int v = 0; v < ATT_WARPS; ++v) top = fmaxf(top, sm[v * ROWS + r]);
+#pragma unroll
+    for (int v = 0; v < ATT_WARPS; ++v) {
+      const float mv = sm[v * ROWS + r], f = mv == top ? 1.f : ex2(mv - top);
+      if (sl[v * ROWS + r] == 0.f) continue;            // (no key)
+      sum += sl[v * ROWS + r] * f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * f;
+    }
+    if (a.splits > 1) {
+      const size_t slot = (tile_row + r) * a.splits + split;
+      store8(a.part + slot * DIM + d0, x);
+      if (d0 == 0) reinterpret_cast<float2*>(a.part + all_rows * a.splits * DIM)[slot] = make_float2(top, sum);
+    } else {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= inv;
+      const int row = r0 + r;
+      store8(static_cast<T*>(a.out) + ((size_t)(o + row / group) * a.n_heads + kvh * group + row % group) * DIM + d0, x);
+    }
+  }
+}
+
+// Joins the parts of a row's keys, in their order: DIM / 8 threads a row.  grid = (ceil(row_tiles * ROWS * DIM / 8 / 128), heads, B), block = 128.
+template <typename T, int DIM, int MT>
+__global__ void __launch_bounds__(128)
+cache_attention_join_kernel(AttendParams a) {
+  constexpr int ROWS = 16 * MT, LANES = DIM / 8;
+  pdl_launch();
+  pdl_wait();
+  const int b = blockIdx.z, kvh = blockIdx.y, r = (blockIdx.x * 128 + threadIdx.x) / LANES, d0 = threadIdx.x % LANES * 8;
+  int o, n, p;
+  if (!row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, o, n, p)) return;
+  const int group = a.n_heads / a.c.heads;
+  if (r >= n * group) return;
+  const size_t all_rows = (size_t)gridDim.z * gridDim.y * a.row_tiles * ROWS;
+  const size_t slot = (((size_t)b * a.c.heads + kvh) * a.row_tiles * ROWS + r) * a.splits;
+  const float2* ml = reinterpret_cast<const float2*>(a.part + all_rows * a.splits * DIM) + slot;
+  float top = -INFINITY, sum = 0.f, x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = 0.f;
+  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, __ldcg(&ml[s].x));
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 v = __ldcg(ml + s);
+    if (v.y == 0.f) continue;
+    const float f = v.x == top ? 1.f : ex2(v.x - top);
+    sum += v.y * f;
+    float y[8];
+    load8(a.part + (slot + s) * DIM + d0, y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] += y[i] * f;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] *= inv;
+  store8(static_cast<T*>(a.out) + ((size_t)(o + r / group) * a.n_heads + kvh * group + r % group) * DIM + d0, x);
 }
 
 }  // namespace kv

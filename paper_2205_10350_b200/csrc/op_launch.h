@@ -9,7 +9,8 @@ namespace ad {
 
 // Records "entry: why" as the message that ad_last_error(NULL) returns, and returns the code.
 int op_fail(int code, const char* entry, const char* why) noexcept;
-// SMs of the current device.
+// The current device (0 .. 63), and its SMs.
+int op_device();
 int op_num_sms();
 // Whether kernels may begin before their predecessor in the stream has ended (they wait for it themselves).
 bool op_early_launch();

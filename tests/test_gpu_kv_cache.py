@@ -67,12 +67,13 @@ class Model:
         return x.transpose(0, 2, 1, 3).reshape(-1, x.shape[1], x.shape[3])[:n]
 
     def attend(self, q, off, lens, causal, scale):
-        """(result, sum of |p v|, sum of |q k| at its largest) of every query and head."""
-        out, weight, size = np.zeros(q.shape), np.zeros(q.shape), np.zeros(q.shape[:2])
+        """(result, sum of |p v|, sum of |q k| at its largest, largest p * scale times the sum of |codes|) of every query and head."""
+        out, weight, size, floor = np.zeros(q.shape), np.zeros(q.shape), np.zeros(q.shape[:2]), np.zeros(q.shape)
         group = q.shape[1] // self.codes[0].shape[1]
         for b, p in enumerate(lens):
             n = off[b + 1] - off[b]
             k, v = (self.values(z, b, p + n if causal else p) for z in range(2))
+            scales = np.repeat([self.scale[1][self.block_id(b, i)] for i in range((len(v) + self.block - 1) // self.block)], self.block, 0)[: len(v)]
             for i in range(n):
                 keys = p + i + 1 if causal else p
                 if not keys:
@@ -84,7 +85,9 @@ class Model:
                     w /= w.sum()
                     out[off[b] + i, h], weight[off[b] + i, h] = w @ vv, w @ np.abs(vv)
                     size[off[b] + i, h] = (np.abs(kk) @ np.abs(qq)).max() * scale
-        return out, weight, size
+                    sv = scales[:keys, h // group]
+                    floor[off[b] + i, h] = (w * sv).max() * (np.abs(vv) / sv[:, None]).sum(0)
+        return out, weight, size, floor
 
 
 def ints(x):
@@ -268,15 +271,17 @@ def test_rows_that_cannot_be_done_are_latched_and_the_others_done(what, code):
 # ---------------------------------------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------------------------------------
-def bound(dtype, want, weight, size, keys, dim):
+def bound(dtype, want, weight, size, floor, keys, dim):
     """How far a result may be off.  A score: dim products and their sum, the scales and the query's 22 bits (2^-24 and 2^-22 of sum |q k|, as
     exponents); an exponential 2^-21; sums over keys 2^-24 each addition; both numerator and denominator.  BF16 besides: probabilities of 11 bits,
-    and the result's own half step."""
+    and the result's own half step.  A probability times its block's scale goes into the product as an FP16 number that is 2^13
+    to 2^15 for the largest so far in the row (whose reference is a whole exponent); FP16's steps are 2^-24 at the least, so one that is too small for
+    11 bits is off by at most 2^-25 there, 2^-38 of the largest, times its code."""
     e = (dim + 8) * 2.0 ** -24 + 2.0 ** -22
     rel = 2 * (e * size[..., None] + 2.0 ** -21 + keys * 2.0 ** -24) + 2.0 ** -22
-    tol = rel * weight + 1e-37
+    tol = rel * weight + 2.0 ** -38 * floor + 1e-37
     if dtype == "bf16":
-        tol = (rel + 2.0 ** -11) * weight + 2.0 ** -8 * np.abs(want) * 1.01 + 1e-37
+        tol = (rel + 2.0 ** -11) * weight + 2.0 ** -38 * floor + 2.0 ** -8 * np.abs(want) * 1.01 + 1e-37
     return tol
 
 
@@ -287,9 +292,9 @@ def attend_and_check(cache, model, q, new, lens, causal, dtype, max_keys=None, s
     got = binding.cache_attention(cache, q, ints(off), ints(lens), max_new=max(new), max_keys=longest if max_keys is None else max_keys, causal=causal,
                                   scale=scale, status_t=status)
     assert int(status.item()) == 0
-    want, weight, size = model.attend(q.cpu().double().numpy(), off, lens, causal, q.shape[2] ** -0.5 if scale is None else scale)
+    want, weight, size, floor = model.attend(q.cpu().double().numpy(), off, lens, causal, q.shape[2] ** -0.5 if scale is None else scale)
     err = np.abs(got.double().cpu().numpy() - want)
-    tol = bound(dtype, want, weight, size, longest, q.shape[2])
+    tol = bound(dtype, want, weight, size, floor, longest, q.shape[2])
     assert got.dtype is q.dtype and (err <= tol).all(), (float(err.max()), float((err / tol).max()))
     return got
 
@@ -446,10 +451,10 @@ def test_calls_on_another_stream_and_in_a_graph():
             graph.replay()
             outs.append(res.clone())
         model.append(xs[:, 1], xs[:, 2], [0, 2, 4], [p + 2 * rep for p in lens])
-        want, weight, size = model.attend(xs[:, 0], [0, 2, 4], [p + 2 * rep for p in lens], True, dim ** -0.5)
+        want, weight, size, floor = model.attend(xs[:, 0], [0, 2, 4], [p + 2 * rep for p in lens], True, dim ** -0.5)
         torch.cuda.synchronize()
         err = np.abs(outs[rep].double().cpu().numpy() - want)
-        assert (err <= bound("bf16", want, weight, size, 160, dim)).all()
+        assert (err <= bound("bf16", want, weight, size, floor, 160, dim)).all()
 
 
 def test_calls_that_are_refused():
