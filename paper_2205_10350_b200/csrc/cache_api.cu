@@ -106,32 +106,34 @@ extern "C" int ad_cache_read(const ad_kv_cache* c, void* k, void* v, int32_t dty
 }
 
 namespace {
-struct AttendPlan { int mt, row_tiles, splits; };
-// Rows of queries a CTA takes: 16 where that is all there are, else 32.  Keys are split while CTAs do not fill the GPU's shared memory once and every
-// warp has two units at least.
+struct AttendPlan { int nq, row_tiles, splits, chunk; };
+// Rows of queries a CTA takes: 8 or 16 where that is all there are, else 32.  Keys are split into parts of the same length for all rows, so that a
+// ragged batch keeps the GPU busy to its end: short enough for CTAs to fill the GPU's shared memory once, two units a warp at least.
 AttendPlan attend_plan(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
   AttendPlan plan;
   const int rows = max_new * (n_heads / c->n_kv_heads);
-  plan.mt = rows <= 16 ? 1 : 2;
-  plan.row_tiles = (rows + 16 * plan.mt - 1) / (16 * plan.mt);
-  const int resident = std::max(1, std::min(6, 227 * 1024 / (kv::att_smem(c->head_dim, plan.mt, dtype == AD_DTYPE_FP32) + 1024)));
+  plan.nq = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+  plan.row_tiles = (rows + 8 * plan.nq - 1) / (8 * plan.nq);
+  const int resident = std::max(1, std::min(6, 227 * 1024 / (kv::att_smem(c->head_dim, plan.nq, dtype == AD_DTYPE_FP32) + 1024)));
   const int64_t base = (int64_t)B * c->n_kv_heads * plan.row_tiles;
-  const int units = (max_keys + kv::UNIT - 1) / kv::UNIT;
-  plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)op_num_sms() * resident / base, units / (2 * kv::ATT_WARPS), 256}));
+  const int units = std::max(1, (max_keys + kv::UNIT - 1) / kv::UNIT);
+  const int64_t wanted = std::min<int64_t>(((int64_t)op_num_sms() * resident + base - 1) / base, 256);
+  plan.chunk = (int)std::max<int64_t>((units + wanted - 1) / wanted, 2 * kv::ATT_WARPS);
+  plan.splits = (units + plan.chunk - 1) / plan.chunk;
   return plan;
 }
 size_t attend_part_bytes(const ad_kv_cache* c, const AttendPlan& plan, int32_t B) {
-  return plan.splits == 1 ? 0 : (size_t)B * c->n_kv_heads * plan.row_tiles * 16 * plan.mt * plan.splits * (c->head_dim + 2) * sizeof(float);
+  return plan.splits == 1 ? 0 : (size_t)B * c->n_kv_heads * plan.row_tiles * 8 * plan.nq * plan.splits * (c->head_dim + 2) * sizeof(float);
 }
 bool attend_sizes(const ad_kv_cache* c, int32_t n_heads, int32_t max_new) {
   return n_heads >= 1 && n_heads <= 65535 && n_heads % c->n_kv_heads == 0 && (int64_t)max_new * (n_heads / c->n_kv_heads) <= (1 << 24);
 }
 
-template <typename T, typename F, int DIM, int MT>
+template <typename T, typename F, int DIM, int NQ>
 cudaError_t launch_attention(const kv::AttendParams& a, int B, cudaStream_t st) {
   static std::atomic<uint64_t> raised{0};              // devices on which the kernel may use its shared memory
-  auto kernel = kv::cache_attention_kernel<T, F, DIM, MT>;
-  constexpr int smem = kv::att_smem(DIM, MT, sizeof(T) == 4);
+  auto kernel = kv::cache_attention_kernel<T, F, DIM, NQ>;
+  constexpr int smem = kv::att_smem(DIM, NQ, sizeof(T) == 4);
   const uint64_t bit = 1ull << op_device();
   if (!(raised.load(std::memory_order_relaxed) & bit)) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -140,12 +142,12 @@ cudaError_t launch_attention(const kv::AttendParams& a, int B, cudaStream_t st) 
   }
   cudaError_t e = launch_op(kernel, dim3(a.row_tiles * a.splits, a.c.heads, B), dim3(32 * kv::ATT_WARPS), dim3(), smem, st, a);
   if (e == cudaSuccess && a.splits > 1)
-    e = launch_op(kv::cache_attention_join_kernel<T, DIM, MT>, dim3((a.row_tiles * 16 * MT * (DIM / 8) + 127) / 128, a.c.heads, B), dim3(128), dim3(), 0, st, a);
+    e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ>, dim3((a.row_tiles * 8 * NQ * (DIM / 8) + 127) / 128, a.c.heads, B), dim3(128), dim3(), 0, st, a);
   return e;
 }
-template <typename T, typename F, int MT>
+template <typename T, typename F, int NQ>
 cudaError_t launch_attention_dim(const kv::AttendParams& a, int dim, int B, cudaStream_t st) {
-  return dim == 32 ? launch_attention<T, F, 32, MT>(a, B, st) : dim == 64 ? launch_attention<T, F, 64, MT>(a, B, st) : launch_attention<T, F, 128, MT>(a, B, st);
+  return dim == 32 ? launch_attention<T, F, 32, NQ>(a, B, st) : dim == 64 ? launch_attention<T, F, 64, NQ>(a, B, st) : launch_attention<T, F, 128, NQ>(a, B, st);
 }
 }  // namespace
 
@@ -175,12 +177,13 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
   kv::AttendParams a;
   a.c = device_cache(c); a.q = q; a.q_stride = (size_t)q_stride; a.out = out; a.n_heads = n_heads; a.M = M; a.max_new = max_new; a.off = off; a.len = len;
   a.causal = causal != 0; a.scale = scale * (float)M_LOG2E; a.status = status;
-  a.row_tiles = plan.row_tiles; a.splits = plan.splits; a.part = static_cast<float*>(scratch);
+  a.row_tiles = plan.row_tiles; a.splits = plan.splits; a.chunk = plan.chunk; a.part = static_cast<float*>(scratch);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return launched(entry, by_types(dtype, c->format, [&](auto t) {
     typedef typename decltype(t)::Num T;
     typedef typename decltype(t)::Fmt F;
-    return plan.mt == 1 ? launch_attention_dim<T, F, 1>(a, c->head_dim, B, st) : launch_attention_dim<T, F, 2>(a, c->head_dim, B, st);
+    return plan.nq == 1 ? launch_attention_dim<T, F, 1>(a, c->head_dim, B, st) : plan.nq == 2 ? launch_attention_dim<T, F, 2>(a, c->head_dim, B, st)
+                                                                                           : launch_attention_dim<T, F, 4>(a, c->head_dim, B, st);
   }));
 }
 

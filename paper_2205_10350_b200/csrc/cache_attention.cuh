@@ -19,17 +19,20 @@ struct AttendParams {
   int causal;
   float scale;             // softmax scale times log2(e)
   int* status;
-  int row_tiles, splits;   // row tiles a row's queries may have; parts its keys are split into
+  int row_tiles, splits;   // tiles of rows that queries may need; parts that keys may be split into
+  int chunk;               // units of a part
   float* part;             // splits > 1: [tile rows][splits][dim] sums, then [tile rows][splits] maxima and sums of exponentials
+  // units of a part of a row with that many units
+  __host__ __device__ __forceinline__ int part_units(int units) const { const int least = (units + splits - 1) / splits; return least > chunk ? least : chunk; }
 };
 
 constexpr int UNIT = 32;               // keys that a warp works on at a time
 constexpr int ATT_WARPS = 4;
 __host__ __device__ constexpr int att_stages(int dim) { return dim == 128 ? 3 : 4; }
 __host__ __device__ constexpr int att_stage_bytes(int dim) { return 2 * UNIT * dim + 16; }
-__host__ __device__ constexpr int att_q_bytes(int dim, int mt, bool fp32) { return mt * (dim / 16) * 512 * (fp32 ? 2 : 1); }
-__host__ __device__ constexpr int att_smem(int dim, int mt, bool fp32) {
-  return att_q_bytes(dim, mt, fp32) + ATT_WARPS * att_stages(dim) * att_stage_bytes(dim);
+__host__ __device__ constexpr int att_q_bytes(int dim, int nq, bool fp32) { return (nq + 1) / 2 * (dim / 16) * 512 * (fp32 ? 2 : 1); }
+__host__ __device__ constexpr int att_smem(int dim, int nq, bool fp32) {
+  return att_q_bytes(dim, nq, fp32) + ATT_WARPS * att_stages(dim) * att_stage_bytes(dim);
 }
 
 // 2^x to 2^-22 of itself; 0 for -inf.
@@ -50,7 +53,7 @@ __device__ __forceinline__ uint32_t rest_f16(float lo, float hi, uint32_t w) {
   return pack_f16(lo - f.x, hi - f.y);
 }
 __device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -76,7 +79,7 @@ __device__ __forceinline__ void cp4(void* smem_dst, const void* gmem_src) {
 // part of the probabilities' operand of the second product; this order makes them keys 16 j + c + {0, 4, 8, 12}, which reads values without bank conflicts.
 __device__ __forceinline__ int unit_key(int nt, int n) { return 16 * (nt >> 1) + (n >> 1) + 4 * ((nt & 1) * 2 + (n & 1)); }
 
-// Attention of 16 MT rows (queries of one row of the batch times the query heads that share a key/value head) over a part of the row's keys.
+// Attention of 8 NQ rows (queries of one row of the batch times the query heads that share a key/value head) over a part of the row's keys.
 //
 // What a number goes through.  Codes are exact in FP16, and so are queries once a power of two has brought the row's largest to 2^13 (BF16 has 8 bits;
 // FP32 goes in as two FP16 numbers, 22 bits, and so do its probabilities).  Scores are FP32: the keys' scale, the softmax scale and the query's power
@@ -90,12 +93,12 @@ __device__ __forceinline__ int unit_key(int nt, int n) { return 16 * (nt >> 1) +
 // keys are through; the four warps' results are joined at the end.  The 16-byte pieces lie in shared memory so that both products' operands come out
 // of it whole, in the registers where mma wants them, without a transposition: dims and keys may be summed in any order.
 // grid = (row_tiles * splits, heads, B), block = 32 * ATT_WARPS.
-template <typename T, typename F, int DIM, int MT>
+template <typename T, typename F, int DIM, int NQ>
 __global__ void __launch_bounds__(32 * ATT_WARPS)
 cache_attention_kernel(AttendParams a) {
   constexpr bool WIDE = sizeof(T) == 4;               // two FP16 numbers for each query and probability
   constexpr int HL = WIDE ? 2 : 1;
-  constexpr int KSTEPS = DIM / 16, NT = DIM / 8, ROWS = 16 * MT;
+  constexpr int KSTEPS = DIM / 16, ND = DIM / 16, MT = (NQ + 1) / 2, ROWS = 8 * NQ;
   constexpr int STAGES = att_stages(DIM), STAGE = att_stage_bytes(DIM), COPIES = DIM / 16;
   constexpr float P_TOP = 16384.f;
   constexpr int P_BITS = 14;
@@ -103,7 +106,7 @@ cache_attention_kernel(AttendParams a) {
   __shared__ float s_rf[ROWS];
   uint4* sq = reinterpret_cast<uint4*>(smem);          // [HL][MT][KSTEPS][lane]: operands as mma wants them
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
-  unsigned char* ring = smem + att_q_bytes(DIM, MT, WIDE) + warp * STAGES * STAGE;
+  unsigned char* ring = smem + att_q_bytes(DIM, NQ, WIDE) + warp * STAGES * STAGE;
   pdl_launch();
   pdl_wait();
   const int b = blockIdx.z, kvh = blockIdx.y, rt = blockIdx.x % a.row_tiles, split = blockIdx.x / a.row_tiles;
@@ -114,8 +117,10 @@ cache_attention_kernel(AttendParams a) {
   const int r_last = min(r0 + ROWS, rows) - 1;
   auto visible = [&](int r) { return a.causal ? p + min(r, r_last) / group + 1 : p; };
   const int vis_min = visible(r0), vis_max = visible(r_last);
-  const int units = (vis_max + UNIT - 1) / UNIT, workers = a.splits * ATT_WARPS, w = split * ATT_WARPS + warp;
-  const int u0 = (int)((long long)units * w / workers), u1 = (int)((long long)units * (w + 1) / workers);
+  const int units = (vis_max + UNIT - 1) / UNIT, per_part = a.part_units(units);
+  const int first_unit = split * per_part, part_units = min(units - first_unit, per_part);
+  if (part_units <= 0 && split > 0) return;
+  const int u0 = first_unit + part_units * warp / ATT_WARPS, u1 = first_unit + part_units * (warp + 1) / ATT_WARPS;
 
   // ---- the ring ----
   const uint8_t* kc = a.c.codes[0];
@@ -176,20 +181,20 @@ cache_attention_kernel(AttendParams a) {
 
   // ---- queries: the row's power of two, FP16, into operand order ----
   // Thread's dims in step j: 64 (j / 4) + 16 c + 4 (j % 4) + 0 .. 3 (DIM = 32: 8 c + 4 j + 0 .. 3)
-  for (int r = warp; r < ROWS; r += ATT_WARPS) {
+  for (int r = warp; r < 16 * MT; r += ATT_WARPS) {
     constexpr int PER = DIM / 32;
     const int row = r0 + r;
     float x[PER], top = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) x[i] = 0.f;
-    if (row <= r_last) {
+    if (r < ROWS && row <= r_last) {
       const T* q = static_cast<const T*>(a.q) + (size_t)(o + row / group) * a.q_stride + ((size_t)kvh * group + row % group) * DIM + lane * PER;
 #pragma unroll
       for (int i = 0; i < PER; ++i) { x[i] = to_f32(q[i]); top = fmaxf(top, fabsf(x[i])); }
     }
     const uint32_t e = min(max(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23, 27u), 253u);     // exponent, 2^-100 .. 2^126
     const float up = __uint_as_float((267u - e) << 23);            // 2^(13 - exponent)
-    if (lane == 0) s_rf[r] = a.scale * (1.f / up);
+    if (lane == 0 && r < ROWS) s_rf[r] = a.scale * (1.f / up);
 #pragma unroll
     for (int i = 0; i < PER; i += (PER > 1 ? 2 : 1)) {
       // one number (DIM = 32) or pairs
@@ -207,25 +212,21 @@ cache_attention_kernel(AttendParams a) {
     }
   }
   __syncthreads();
-  float rf[MT][2], m[MT][2], d[MT][2], l[MT][2], acc[MT][NT][4];
+  // Scores: thread's row g of each eight, columns as above.  Results: dims DIM / 8 * g .. of rows 2 c and 2 c + 1 of each eight.
+  float rf[NQ], m[NQ], d[NQ], l[NQ], acc[NQ][ND][4];
   bool large = false;                                 // scores whose steps in FP32 are a quarter and more
-  int vis[MT][2];
+  int vis[NQ];
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+  for (int q = 0; q < NQ; ++q) {
+    rf[q] = s_rf[q * 8 + g];
+    vis[q] = visible(r0 + q * 8 + g);
+    m[q] = d[q] = -INFINITY;
+    l[q] = 0.f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = t * 16 + h * 8 + g;
-      rf[t][h] = s_rf[r];
-      vis[t][h] = visible(r0 + r);
-      m[t][h] = d[t][h] = -INFINITY;
-      l[t][h] = 0.f;
-    }
+    for (int i = 0; i < ND; ++i)
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[t][i][j] = 0.f;
+      for (int j = 0; j < 4; ++j) acc[q][i][j] = 0.f;
+  }
   // queries of few steps stay in registers
   constexpr bool Q_REGS = HL * MT * KSTEPS <= 8;
   uint4 qr[Q_REGS ? HL : 1][Q_REGS ? MT : 1][Q_REGS ? KSTEPS : 1];
@@ -294,12 +295,12 @@ cache_attention_kernel(AttendParams a) {
     }
     if (u * UNIT + UNIT > vis_min || sc.x < 0.f || sc.y < 0.f) {
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
+      for (int q = 0; q < NQ; ++q)
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (u * UNIT + unit_key(nt, 2 * c + (j & 1)) >= vis[t][j >> 1] || (pieces == 2 && nt >= 2 ? sc.y : sc.x) < 0.f) s[t][nt][j] = -INFINITY;
+          for (int j = 0; j < 2; ++j)
+            if (u * UNIT + unit_key(nt, 2 * c + j) >= vis[q] || (pieces == 2 && nt >= 2 ? sc.y : sc.x) < 0.f) s[q / 2][nt][2 * (q & 1) + j] = -INFINITY;
     }
     // ---- probabilities ----
     float ks[2] = {fabsf(sc.x), pieces == 2 ? fabsf(sc.y) : fabsf(sc.x)};
@@ -309,76 +310,69 @@ cache_attention_kernel(AttendParams a) {
       ve[0] = (float)((int)(v0 >> 23) - 127); ve[1] = (float)((int)(v1 >> 23) - 127);
       vm[0] = __uint_as_float((v0 & 0x7fffffu) | 0x3f800000u) * P_TOP; vm[1] = __uint_as_float((v1 & 0x7fffffu) | 0x3f800000u) * P_TOP;
     }
-    float ref[MT][2], top[MT][2], tod[MT][2], tk[MT][2][2];
+    float ref[NQ], top[NQ], tod[NQ], tk[NQ][2];
     bool moved = false;
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float x0 = fmaxf(fmaxf(s[t][0][2 * h], s[t][0][2 * h + 1]), fmaxf(s[t][1][2 * h], s[t][1][2 * h + 1]));
-        float x1 = fmaxf(fmaxf(s[t][2][2 * h], s[t][2][2 * h + 1]), fmaxf(s[t][3][2 * h], s[t][3][2 * h + 1]));
-        if (pieces == 1) x0 = x1 = fmaxf(x0, x1);
-        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
-        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
-        if (pieces == 2) {
-          x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
-          x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
-        } else {
-          x1 = x0;
-        }
-        tk[t][h][0] = fmaxf(rf[t][h] * ks[0], FLT_MIN);
-        tk[t][h][1] = fmaxf(rf[t][h] * ks[1], FLT_MIN);
-        x0 = ceilf(x0 * tk[t][h][0]);                  // references are whole numbers: what goes from one to another is an exact power of two
-        x1 = ceilf(x1 * tk[t][h][1]);
-        top[t][h] = fmaxf(m[t][h], fmaxf(x0, x1));
-        ref[t][h] = top[t][h] == -INFINITY ? 0.f : top[t][h];
-        tod[t][h] = fmaxf(d[t][h] + (m[t][h] - ref[t][h]), fmaxf(x0 - ref[t][h] + ve[0], x1 - ref[t][h] + ve[1]));
-        moved |= top[t][h] != m[t][h] || tod[t][h] != d[t][h];
+    for (int q = 0; q < NQ; ++q) {
+      const float(*sq4)[4] = s[q / 2];
+      const int h = 2 * (q & 1);
+      float x0 = fmaxf(fmaxf(sq4[0][h], sq4[0][h + 1]), fmaxf(sq4[1][h], sq4[1][h + 1]));
+      float x1 = fmaxf(fmaxf(sq4[2][h], sq4[2][h + 1]), fmaxf(sq4[3][h], sq4[3][h + 1]));
+      if (pieces == 1) x0 = x1 = fmaxf(x0, x1);
+      x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
+      x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
+      if (pieces == 2) {
+        x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
+        x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
+      } else {
+        x1 = x0;
       }
+      tk[q][0] = fmaxf(rf[q] * ks[0], FLT_MIN);
+      tk[q][1] = fmaxf(rf[q] * ks[1], FLT_MIN);
+      x0 = ceilf(x0 * tk[q][0]);                       // references are whole numbers: what goes from one to another is an exact power of two
+      x1 = ceilf(x1 * tk[q][1]);
+      top[q] = fmaxf(m[q], fmaxf(x0, x1));
+      ref[q] = top[q] == -INFINITY ? 0.f : top[q];
+      tod[q] = fmaxf(d[q] + (m[q] - ref[q]), fmaxf(x0 - ref[q] + ve[0], x1 - ref[q] + ve[1]));
+      moved |= top[q] != m[q] || tod[q] != d[q];
+    }
     if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
+      for (int q = 0; q < NQ; ++q) {
+        const float less = m[q] - ref[q], keep_o = tod[q] == -INFINITY ? 0.f : ex2(less + (d[q] - tod[q]));
+        m[q] = top[q];
+        d[q] = tod[q];
+        l[q] *= ex2(less);
+        const float k0 = __shfl_sync(0xffffffffu, keep_o, 8 * c), k1 = __shfl_sync(0xffffffffu, keep_o, 8 * c + 4);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float less = m[t][h] - ref[t][h], keep = ex2(less);
-          const float keep_o = tod[t][h] == -INFINITY ? 0.f : ex2(less + (d[t][h] - tod[t][h]));
-          m[t][h] = top[t][h];
-          d[t][h] = tod[t][h];
-          l[t][h] *= keep;
-#pragma unroll
-          for (int i = 0; i < NT; ++i) { acc[t][i][2 * h] *= keep_o; acc[t][i][2 * h + 1] *= keep_o; }
-          large |= fabsf(ref[t][h]) > 4194304.f;
-        }
+        for (int i = 0; i < ND; ++i) { acc[q][i][0] *= k0; acc[q][i][1] *= k1; acc[q][i][2] *= k0; acc[q][i][3] *= k1; }
+        large |= fabsf(ref[q]) > 4194304.f;
+      }
       large = __any_sync(0xffffffffu, large);
     }
     if (large) {                                       // the exponent below then is a difference of rounded scores, as the maximum is one of them
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
+      for (int q = 0; q < NQ; ++q) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
-          for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) s[t][nt][2 * h + j] *= tk[t][h][nt >> 1];
-          tk[t][h][0] = tk[t][h][1] = 1.f;
-        }
+          for (int j = 0; j < 2; ++j) s[q / 2][nt][2 * (q & 1) + j] *= tk[q][nt >> 1];
+        tk[q][0] = tk[q][1] = 1.f;
+      }
     }
-    uint32_t pf[HL][MT][2][4];
+    uint32_t pf[HL][NQ][4];                            // [score tile]: two keys' probabilities of row g, as the second product's operand
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
+    for (int q = 0; q < NQ; ++q)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int z = 0; z < 2; ++z) {
+        const float f = ex2(fminf(ve[z] - d[q], 100.f)) * vm[z];
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const float f = ex2(fminf(ve[z] - d[t][h], 100.f)) * vm[z];
-#pragma unroll
-          for (int nn = 0; nn < 2; ++nn) {
-            const float p0 = ex2(fmaf(s[t][2 * z + nn][2 * h], tk[t][h][z], -ref[t][h])), p1 = ex2(fmaf(s[t][2 * z + nn][2 * h + 1], tk[t][h][z], -ref[t][h]));
-            l[t][h] += p0 + p1;
-            const float y0 = p0 * f, y1 = p1 * f;
-            pf[0][t][z][nn * 2 + h] = pack_f16(y0, y1);
-            if constexpr (WIDE) pf[HL - 1][t][z][nn * 2 + h] = rest_f16(y0, y1, pf[0][t][z][nn * 2 + h]);
-          }
+        for (int nt = 2 * z; nt < 2 * z + 2; ++nt) {
+          const float p0 = ex2(fmaf(s[q / 2][nt][2 * (q & 1)], tk[q][z], -ref[q])), p1 = ex2(fmaf(s[q / 2][nt][2 * (q & 1) + 1], tk[q][z], -ref[q]));
+          l[q] += p0 + p1;
+          const float y0 = p0 * f, y1 = p1 * f;
+          pf[0][q][nt] = pack_f16(y0, y1);
+          if constexpr (WIDE) pf[HL - 1][q][nt] = rest_f16(y0, y1, pf[0][q][nt]);
         }
       }
     // ---- times values ----
@@ -405,41 +399,41 @@ cache_attention_kernel(AttendParams a) {
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const uint32_t w0 = __byte_perm(v[0][x], v[1][x], y ? 0x7362 : 0x5140), w1 = __byte_perm(v[2][x], v[3][x], y ? 0x7362 : 0x5140);
-          uint32_t b0[2], b1[2];
-          codes_f16(F(), w0, b0[0], b0[1]);
-          codes_f16(F(), w1, b1[0], b1[1]);
+          uint32_t av[4];                              // dims DIM / 8 * g + 4 x + 2 y and the next one, four keys
+          codes_f16(F(), w0, av[0], av[1]);
+          codes_f16(F(), w1, av[2], av[3]);
 #pragma unroll
-          for (int d = 0; d < 2; ++d)
+          for (int h = HL - 1; h >= 0; --h)
 #pragma unroll
-            for (int h = HL - 1; h >= 0; --h)
-#pragma unroll
-              for (int t = 0; t < MT; ++t) mma_f16(acc[t][4 * x + 2 * y + d], pf[h][t][j], b0[d], b1[d]);
+            for (int q = 0; q < NQ; ++q) mma_f16(acc[q][2 * x + y], av, pf[h][q][2 * j], pf[h][q][2 * j + 1]);
         }
     }
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   __syncthreads();
 
-  // ---- the warps' results together.  A thread holds dims DIM/4 * c .. of its rows, column tile i the i-th and (second column) the DIM/8 + i-th. ----
+  // ---- the warps' results together ----
   constexpr int PITCH = DIM + 4;
   float* so = reinterpret_cast<float*>(smem);                     // [warps][ROWS][PITCH]
-  float* sm = so + ATT_WARPS * ROWS * PITCH;                      // [warps][ROWS] maxima, then sums
+  float* sm = so + ATT_WARPS * ROWS * PITCH;                      // [warps][ROWS] maxima, sums, exponents of the results
   float* sl = sm + ATT_WARPS * ROWS;
-  static_assert((ATT_WARPS * ROWS * (PITCH + 2)) * 4 <= att_smem(DIM, MT, WIDE), "results fit where the ring was");
+  float* sd = sl + ATT_WARPS * ROWS;
+  static_assert((ATT_WARPS * ROWS * (PITCH + 3)) * 4 <= att_smem(DIM, NQ, WIDE), "results fit where the ring was");
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+  for (int q = 0; q < NQ; ++q) {
+    float* dst = so + (warp * ROWS + q * 8 + 2 * c) * PITCH + g * (DIM / 8);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = t * 16 + h * 8 + g;
-      float sum = l[t][h];
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      const float f = m[t][h] == -INFINITY && sum == 0.f ? 0.f : ex2(d[t][h] - (float)P_BITS);
-      float* dst = so + (warp * ROWS + r) * PITCH + c * (DIM / 4);
+    for (int i = 0; i < ND; ++i)
 #pragma unroll
-      for (int i = 0; i < NT; ++i) { dst[i] = acc[t][i][2 * h] * f; dst[DIM / 8 + i] = acc[t][i][2 * h + 1] * f; }
-      if (c == 0) { sm[warp * ROWS + r] = m[t][h]; sl[warp * ROWS + r] = sum; }
+      for (int j = 0; j < 2; ++j) *reinterpret_cast<float2*>(dst + j * PITCH + 2 * i) = make_float2(acc[q][i][j], acc[q][i][2 + j]);
+    float sum = l[q];
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    if (c == 0) {
+      const int r = warp * ROWS + q * 8 + g;
+      sm[r] = m[q]; sl[r] = sum; sd[r] = d[q] - (float)P_BITS;
     }
+  }
   __syncthreads();
   constexpr int LANES = DIM / 8, AT_ONCE = 32 * ATT_WARPS / LANES;      // threads a row, each eight dims
   const int d0 = tid % LANES * 8;
@@ -452,13 +446,13 @@ cache_attention_kernel(AttendParams a) {
     for (int v = 0; v < ATT_WARPS; ++v) top = fmaxf(top, sm[v * ROWS + r]);
 #pragma unroll
     for (int v = 0; v < ATT_WARPS; ++v) {
-      const float mv = sm[v * ROWS + r], f = mv == top ? 1.f : ex2(mv - top);
-      if (sl[v * ROWS + r] == 0.f) continue;            // (no key)
-      sum += sl[v * ROWS + r] * f;
+      const float mv = sm[v * ROWS + r], lv = sl[v * ROWS + r], f = mv == top ? 1.f : ex2(mv - top), fo = ex2(sd[v * ROWS + r]) * f;
+      if (lv == 0.f) continue;                          // (no key)
+      sum += lv * f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * f;
+      for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * fo;
     }
-    if (a.splits > 1) {
+    if (per_part < units) {
       const size_t slot = (tile_row + r) * a.splits + split;
       store8(a.part + slot * DIM + d0, x);
       if (d0 == 0) reinterpret_cast<float2*>(a.part + all_rows * a.splits * DIM)[slot] = make_float2(top, sum);
@@ -472,11 +466,12 @@ cache_attention_kernel(AttendParams a) {
   }
 }
 
-// Joins the parts of a row's keys, in their order: DIM / 8 threads a row.  grid = (ceil(row_tiles * ROWS * DIM / 8 / 128), heads, B), block = 128.
-template <typename T, int DIM, int MT>
+// Joins the parts of a row's keys, in their order, where there is more than one: DIM / 8 threads a row.
+// grid = (ceil(row_tiles * ROWS * DIM / 8 / 128), heads, B), block = 128.
+template <typename T, int DIM, int NQ>
 __global__ void __launch_bounds__(128)
 cache_attention_join_kernel(AttendParams a) {
-  constexpr int ROWS = 16 * MT, LANES = DIM / 8;
+  constexpr int ROWS = 8 * NQ, LANES = DIM / 8;
   pdl_launch();
   pdl_wait();
   const int b = blockIdx.z, kvh = blockIdx.y, r = (blockIdx.x * 128 + threadIdx.x) / LANES, d0 = threadIdx.x % LANES * 8;
@@ -484,14 +479,18 @@ cache_attention_join_kernel(AttendParams a) {
   if (!row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, o, n, p)) return;
   const int group = a.n_heads / a.c.heads;
   if (r >= n * group) return;
+  // as many parts as the row's tile has been split into
+  const int r_last = min(r / ROWS * ROWS + ROWS, n * group) - 1, units = ((a.causal ? p + r_last / group + 1 : p) + UNIT - 1) / UNIT;
+  const int per_part = a.part_units(units), parts = (units + per_part - 1) / per_part;
+  if (parts <= 1) return;
   const size_t all_rows = (size_t)gridDim.z * gridDim.y * a.row_tiles * ROWS;
   const size_t slot = (((size_t)b * a.c.heads + kvh) * a.row_tiles * ROWS + r) * a.splits;
   const float2* ml = reinterpret_cast<const float2*>(a.part + all_rows * a.splits * DIM) + slot;
   float top = -INFINITY, sum = 0.f, x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = 0.f;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, __ldcg(&ml[s].x));
-  for (int s = 0; s < a.splits; ++s) {
+  for (int s = 0; s < parts; ++s) top = fmaxf(top, __ldcg(&ml[s].x));
+  for (int s = 0; s < parts; ++s) {
     const float2 v = __ldcg(ml + s);
     if (v.y == 0.f) continue;
     const float f = v.x == top ? 1.f : ex2(v.x - top);
