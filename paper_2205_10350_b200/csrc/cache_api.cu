@@ -1,6 +1,7 @@
 // Operator-level entry points of the 8-bit key/value cache and of sampled verification, declared in include/aggressive_decoding.h.
 #include <limits.h>
 #include <math.h>
+#include <stdlib.h>
 
 #include <algorithm>
 #include <atomic>
@@ -106,6 +107,7 @@ extern "C" int ad_cache_read(const ad_kv_cache* c, void* k, void* v, int32_t dty
 }
 
 namespace {
+const int64_t kWaves = getenv("AD_W") ? atoi(getenv("AD_W")) : 3;
 struct AttendPlan { int nq, row_tiles, splits, chunk; };
 // Rows of queries a CTA takes: 8 or 16 where that is all there are, else 32.  Keys are split into parts of the same length for all rows, so that a
 // ragged batch keeps the GPU busy to its end: short enough for CTAs to fill the GPU's shared memory once, two units a warp at least.
@@ -117,7 +119,7 @@ AttendPlan attend_plan(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int
   const int resident = std::max(1, std::min(6, 227 * 1024 / (kv::att_smem(c->head_dim, plan.nq, dtype == AD_DTYPE_FP32) + 1024)));
   const int64_t base = (int64_t)B * c->n_kv_heads * plan.row_tiles;
   const int units = std::max(1, (max_keys + kv::UNIT - 1) / kv::UNIT);
-  const int64_t wanted = std::min<int64_t>(((int64_t)op_num_sms() * resident + base - 1) / base, 256);
+  const int64_t wanted = std::min<int64_t>((kWaves * op_num_sms() * resident + base - 1) / base, kv::MAX_SPLITS);
   plan.chunk = (int)std::max<int64_t>((units + wanted - 1) / wanted, 2 * kv::ATT_WARPS);
   plan.splits = (units + plan.chunk - 1) / plan.chunk;
   return plan;
@@ -141,8 +143,11 @@ cudaError_t launch_attention(const kv::AttendParams& a, int B, cudaStream_t st) 
     raised.fetch_or(bit, std::memory_order_relaxed);
   }
   cudaError_t e = launch_op(kernel, dim3(a.row_tiles * a.splits, a.c.heads, B), dim3(32 * kv::ATT_WARPS), dim3(), smem, st, a);
-  if (e == cudaSuccess && a.splits > 1)
-    e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ>, dim3((a.row_tiles * 8 * NQ * (DIM / 8) + 127) / 128, a.c.heads, B), dim3(128), dim3(), 0, st, a);
+  if (e == cudaSuccess && a.splits > 1) {
+    const int rows = a.row_tiles * 8 * NQ, groups = 512 / DIM;
+    if (a.splits > kv::FEW_SPLITS) e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, true>, dim3(rows, a.c.heads, B), dim3(128), dim3(), 0, st, a);
+    else e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, false>, dim3((rows + groups - 1) / groups, a.c.heads, B), dim3(128), dim3(), 0, st, a);
+  }
   return e;
 }
 template <typename T, typename F, int NQ>

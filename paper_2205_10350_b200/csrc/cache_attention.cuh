@@ -28,6 +28,7 @@ struct AttendParams {
 
 constexpr int UNIT = 32;               // keys that a warp works on at a time
 constexpr int ATT_WARPS = 4;
+constexpr int MAX_SPLITS = 256, FEW_SPLITS = 8;      // parts at most; parts that one thread joins
 __host__ __device__ constexpr int att_stages(int dim) { return dim == 128 ? 3 : 4; }
 __host__ __device__ constexpr int att_stage_bytes(int dim) { return 2 * UNIT * dim + 16; }
 __host__ __device__ constexpr int att_q_bytes(int dim, int nq, bool fp32) { return (nq + 1) / 2 * (dim / 16) * 512 * (fp32 ? 2 : 1); }
@@ -40,6 +41,37 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// log2 x: the exponent as it is, which is all there is to a power of two, and the mantissa's to 2^-22.
+__device__ __forceinline__ float lg2(float x) {
+  const uint32_t w = __float_as_uint(x);
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(__uint_as_float((w & 0x7fffffu) | 0x3f800000u)));
+  return (float)((int)(w >> 23) - 127) + y;
+}
+// Two FP32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{ .reg .b64 a, b, c, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mov.b64 c, {%6, %7}; fma.rn.f32x2 d, a, b, c; mov.b64 {%0, %1}, d; }"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{ .reg .b64 a, b, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; add.rn.f32x2 d, a, b; mov.b64 {%0, %1}, d; }"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{ .reg .b64 a, b, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mul.rn.f32x2 d, a, b; mov.b64 {%0, %1}, d; }"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t w;
@@ -100,7 +132,6 @@ cache_attention_kernel(AttendParams a) {
   constexpr int HL = WIDE ? 2 : 1;
   constexpr int KSTEPS = DIM / 16, ND = DIM / 16, MT = (NQ + 1) / 2, ROWS = 8 * NQ;
   constexpr int STAGES = att_stages(DIM), STAGE = att_stage_bytes(DIM), COPIES = DIM / 16;
-  constexpr float P_TOP = 16384.f;
   constexpr int P_BITS = 14;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ float s_rf[ROWS];
@@ -304,21 +335,16 @@ cache_attention_kernel(AttendParams a) {
     }
     // ---- probabilities ----
     float ks[2] = {fabsf(sc.x), pieces == 2 ? fabsf(sc.y) : fabsf(sc.x)};
-    float ve[2], vm[2];                                // the values' scales as a power of two and a number from 1 to 2 (times 2^14)
-    {
-      const uint32_t v0 = __float_as_uint(sc.z), v1 = pieces == 2 ? __float_as_uint(sc.w) : v0;
-      ve[0] = (float)((int)(v0 >> 23) - 127); ve[1] = (float)((int)(v1 >> 23) - 127);
-      vm[0] = __uint_as_float((v0 & 0x7fffffu) | 0x3f800000u) * P_TOP; vm[1] = __uint_as_float((v1 & 0x7fffffu) | 0x3f800000u) * P_TOP;
-    }
+    const float ve[2] = {lg2(sc.z), pieces == 2 ? lg2(sc.w) : lg2(sc.z)};
     float ref[NQ], top[NQ], tod[NQ], tk[NQ][2];
     bool moved = false;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       const float(*sq4)[4] = s[q / 2];
       const int h = 2 * (q & 1);
-      float x0 = fmaxf(fmaxf(sq4[0][h], sq4[0][h + 1]), fmaxf(sq4[1][h], sq4[1][h + 1]));
-      float x1 = fmaxf(fmaxf(sq4[2][h], sq4[2][h + 1]), fmaxf(sq4[3][h], sq4[3][h + 1]));
-      if (pieces == 1) x0 = x1 = fmaxf(x0, x1);
+      float x0 = fmaxf(max3(sq4[0][h], sq4[0][h + 1], sq4[1][h]), sq4[1][h + 1]), x1 = max3(sq4[2][h], sq4[2][h + 1], sq4[3][h]);
+      if (pieces == 1) x0 = max3(x0, x1, sq4[3][h + 1]);
+      else x1 = fmaxf(x1, sq4[3][h + 1]);
       x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
       x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
       if (pieces == 2) {
@@ -345,7 +371,10 @@ cache_attention_kernel(AttendParams a) {
         l[q] *= ex2(less);
         const float k0 = __shfl_sync(0xffffffffu, keep_o, 8 * c), k1 = __shfl_sync(0xffffffffu, keep_o, 8 * c + 4);
 #pragma unroll
-        for (int i = 0; i < ND; ++i) { acc[q][i][0] *= k0; acc[q][i][1] *= k1; acc[q][i][2] *= k0; acc[q][i][3] *= k1; }
+        for (int i = 0; i < ND; ++i) {
+          const float2 y0 = mul2(make_float2(acc[q][i][0], acc[q][i][1]), make_float2(k0, k1)), y1 = mul2(make_float2(acc[q][i][2], acc[q][i][3]), make_float2(k0, k1));
+          acc[q][i][0] = y0.x; acc[q][i][1] = y0.y; acc[q][i][2] = y1.x; acc[q][i][3] = y1.y;
+        }
         large |= fabsf(ref[q]) > 4194304.f;
       }
       large = __any_sync(0xffffffffu, large);
@@ -365,15 +394,22 @@ cache_attention_kernel(AttendParams a) {
     for (int q = 0; q < NQ; ++q)
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
-        const float f = ex2(fminf(ve[z] - d[q], 100.f)) * vm[z];
+        // p, as a share of the softmax's maximum, times 2^(14 + e), e = log2(values' scale) - d: what goes into the second product.  Its sum is taken
+        // as it is and brought back afterwards, which the bounds on e keep inside FP32 (beyond them the values do not count, or the probability).
+        const float e = (float)P_BITS + fminf(fmaxf(ve[z] - d[q], -100.f), 100.f), less = e - ref[q];
+        const float2 t2 = make_float2(tk[q][z], tk[q][z]), r2 = large ? make_float2(-ref[q], -ref[q]) : make_float2(less, less);
+        float2 sum;
 #pragma unroll
         for (int nt = 2 * z; nt < 2 * z + 2; ++nt) {
-          const float p0 = ex2(fmaf(s[q / 2][nt][2 * (q & 1)], tk[q][z], -ref[q])), p1 = ex2(fmaf(s[q / 2][nt][2 * (q & 1) + 1], tk[q][z], -ref[q]));
-          l[q] += p0 + p1;
-          const float y0 = p0 * f, y1 = p1 * f;
-          pf[0][q][nt] = pack_f16(y0, y1);
-          if constexpr (WIDE) pf[HL - 1][q][nt] = rest_f16(y0, y1, pf[0][q][nt]);
+          float2 y = fma2(make_float2(s[q / 2][nt][2 * (q & 1)], s[q / 2][nt][2 * (q & 1) + 1]), t2, r2);
+          if (large) { y.x += e; y.y += e; }
+          y.x = ex2(y.x);
+          y.y = ex2(y.y);
+          sum = nt == 2 * z ? y : add2(sum, y);
+          pf[0][q][nt] = pack_f16(y.x, y.y);
+          if constexpr (WIDE) pf[HL - 1][q][nt] = rest_f16(y.x, y.y, pf[0][q][nt]);
         }
+        l[q] = fmaf(sum.x + sum.y, ex2(-e), l[q]);
       }
     // ---- times values ----
 #pragma unroll
@@ -466,15 +502,20 @@ cache_attention_kernel(AttendParams a) {
   }
 }
 
-// Joins the parts of a row's keys, in their order, where there is more than one: DIM / 8 threads a row.
-// grid = (ceil(row_tiles * ROWS * DIM / 8 / 128), heads, B), block = 128.
-template <typename T, int DIM, int NQ>
+// Joins the parts of a row's keys, where there is more than one.  Four dims a thread, so that 128 threads are 128 / (DIM / 4) groups: SHARED, they take
+// a row's parts in turn and add up in their order, else each has a row of its own.  Bound by latency: maxima and sums of all parts are loaded at once
+// (each lane of a warp one part), results eight parts ahead.
+// grid = (rows, or rows / groups, heads, B), block = 128.
+template <typename T, int DIM, int NQ, bool SHARED>
 __global__ void __launch_bounds__(128)
 cache_attention_join_kernel(AttendParams a) {
-  constexpr int ROWS = 8 * NQ, LANES = DIM / 8;
+  constexpr int ROWS = 8 * NQ, LANES = DIM / 4, GROUPS = 128 / LANES;
+  __shared__ float4 s_x[SHARED ? GROUPS - 1 : 1][LANES];
+  __shared__ float s_w[SHARED ? MAX_SPLITS : 1];
   pdl_launch();
   pdl_wait();
-  const int b = blockIdx.z, kvh = blockIdx.y, r = (blockIdx.x * 128 + threadIdx.x) / LANES, d0 = threadIdx.x % LANES * 8;
+  const int tid = threadIdx.x, grp = tid / LANES, d0 = tid % LANES * 4;
+  const int b = blockIdx.z, kvh = blockIdx.y, r = SHARED ? blockIdx.x : blockIdx.x * GROUPS + grp;
   int o, n, p;
   if (!row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, o, n, p)) return;
   const int group = a.n_heads / a.c.heads;
@@ -486,24 +527,71 @@ cache_attention_join_kernel(AttendParams a) {
   const size_t all_rows = (size_t)gridDim.z * gridDim.y * a.row_tiles * ROWS;
   const size_t slot = (((size_t)b * a.c.heads + kvh) * a.row_tiles * ROWS + r) * a.splits;
   const float2* ml = reinterpret_cast<const float2*>(a.part + all_rows * a.splits * DIM) + slot;
-  float top = -INFINITY, sum = 0.f, x[8];
+  const float* part = a.part + slot * DIM + d0;
+  float sum = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float4 y, float f) { x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w); };
+  if constexpr (SHARED) {
+    // every warp for itself: maxima, weights, and their sum
+    const int lane = tid & 31;
+    float top = -INFINITY;
+    float2 v[MAX_SPLITS / 32];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = 0.f;
-  for (int s = 0; s < parts; ++s) top = fmaxf(top, __ldcg(&ml[s].x));
-  for (int s = 0; s < parts; ++s) {
-    const float2 v = __ldcg(ml + s);
-    if (v.y == 0.f) continue;
-    const float f = v.x == top ? 1.f : ex2(v.x - top);
-    sum += v.y * f;
-    float y[8];
-    load8(a.part + (slot + s) * DIM + d0, y);
+    for (int i = 0; i < MAX_SPLITS / 32; ++i) {
+      v[i] = i * 32 + lane < parts ? __ldcg(ml + i * 32 + lane) : make_float2(-INFINITY, 0.f);
+      top = fmaxf(top, v[i].x);
+    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] += y[i] * f;
+    for (int w = 16; w; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+#pragma unroll
+    for (int i = 0; i < MAX_SPLITS / 32; ++i) {
+      const float f = v[i].y == 0.f ? 0.f : v[i].x == top ? 1.f : ex2(v[i].x - top);      // (no key: nothing, whatever the maxima)
+      sum += v[i].y * f;
+      if (tid < 32 && i * 32 + lane < parts) s_w[i * 32 + lane] = f;
+    }
+#pragma unroll
+    for (int w = 16; w; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+    __syncthreads();
+    for (int s0 = grp; s0 < parts; s0 += 8 * GROUPS) {
+      float4 y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (s0 + i * GROUPS < parts) y[i] = __ldcg(reinterpret_cast<const float4*>(part + (size_t)(s0 + i * GROUPS) * DIM));
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (s0 + i * GROUPS < parts) add(y[i], s_w[s0 + i * GROUPS]);
+    }
+    if (grp > 0) s_x[grp - 1][tid % LANES] = x;
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int i = 0; i < GROUPS - 1; ++i) add(s_x[i][tid], 1.f);
+  } else {
+    float top = -INFINITY;
+    float2 v[FEW_SPLITS];
+    float4 y[FEW_SPLITS];
+#pragma unroll
+    for (int i = 0; i < FEW_SPLITS; ++i) {
+      v[i] = i < parts ? __ldcg(ml + i) : make_float2(-INFINITY, 0.f);
+      if (i < parts) y[i] = __ldcg(reinterpret_cast<const float4*>(part + (size_t)i * DIM));
+      top = fmaxf(top, v[i].x);
+    }
+#pragma unroll
+    for (int i = 0; i < FEW_SPLITS; ++i) {
+      if (i >= parts || v[i].y == 0.f) continue;
+      const float f = v[i].x == top ? 1.f : ex2(v[i].x - top);
+      sum = fmaf(v[i].y, f, sum);
+      add(y[i], f);
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] *= inv;
-  store8(static_cast<T*>(a.out) + ((size_t)(o + r / group) * a.n_heads + kvh * group + r % group) * DIM + d0, x);
+  T* out = static_cast<T*>(a.out) + ((size_t)(o + r / group) * a.n_heads + kvh * group + r % group) * DIM + d0;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(out) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+  } else {
+    __nv_bfloat162 w[2] = {__floats2bfloat162_rn(x.x * inv, x.y * inv), __floats2bfloat162_rn(x.z * inv, x.w * inv)};
+    *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(w);
+  }
 }
 
 }  // namespace kv
