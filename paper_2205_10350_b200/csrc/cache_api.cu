@@ -116,7 +116,7 @@ AttendPlan attend_plan(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int
   const int rows = max_new * (n_heads / c->n_kv_heads);
   plan.nq = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   plan.row_tiles = (rows + 8 * plan.nq - 1) / (8 * plan.nq);
-  const int resident = std::max(1, std::min(6, 227 * 1024 / (kv::att_smem(c->head_dim, plan.nq, dtype == AD_DTYPE_FP32) + 1024)));
+  const int resident = kv::att_resident(c->head_dim, plan.nq);
   const int64_t base = (int64_t)B * c->n_kv_heads * plan.row_tiles;
   const int units = std::max(1, (max_keys + kv::UNIT - 1) / kv::UNIT);
   const int64_t wanted = std::min<int64_t>((kWaves * op_num_sms() * resident + base - 1) / base, kv::MAX_SPLITS);
@@ -131,10 +131,10 @@ bool attend_sizes(const ad_kv_cache* c, int32_t n_heads, int32_t max_new) {
   return n_heads >= 1 && n_heads <= 65535 && n_heads % c->n_kv_heads == 0 && (int64_t)max_new * (n_heads / c->n_kv_heads) <= (1 << 24);
 }
 
-template <typename T, typename F, int DIM, int NQ>
-cudaError_t launch_attention(const kv::AttendParams& a, int B, cudaStream_t st) {
+template <typename T, typename F, int DIM, int NQ, bool TWO>
+cudaError_t launch_attention_part(const kv::AttendParams& a, int B, cudaStream_t st) {
   static std::atomic<uint64_t> raised{0};              // devices on which the kernel may use its shared memory
-  auto kernel = kv::cache_attention_kernel<T, F, DIM, NQ>;
+  auto kernel = kv::cache_attention_kernel<T, F, DIM, NQ, TWO>;
   constexpr int smem = kv::att_smem(DIM, NQ, sizeof(T) == 4);
   const uint64_t bit = 1ull << op_device();
   if (!(raised.load(std::memory_order_relaxed) & bit)) {
@@ -142,7 +142,11 @@ cudaError_t launch_attention(const kv::AttendParams& a, int B, cudaStream_t st) 
     if (e != cudaSuccess) return e;
     raised.fetch_or(bit, std::memory_order_relaxed);
   }
-  cudaError_t e = launch_op(kernel, dim3(a.row_tiles * a.splits, a.c.heads, B), dim3(32 * kv::ATT_WARPS), dim3(), smem, st, a);
+  return launch_op(kernel, dim3(a.row_tiles * a.splits, a.c.heads, B), dim3(32 * kv::ATT_WARPS), dim3(), smem, st, a);
+}
+template <typename T, typename F, int DIM, int NQ>
+cudaError_t launch_attention(const kv::AttendParams& a, int B, cudaStream_t st) {
+  cudaError_t e = a.c.block == 16 ? launch_attention_part<T, F, DIM, NQ, true>(a, B, st) : launch_attention_part<T, F, DIM, NQ, false>(a, B, st);
   if (e == cudaSuccess && a.splits > 1) {
     const int rows = a.row_tiles * 8 * NQ, groups = 512 / DIM;
     if (a.splits > kv::FEW_SPLITS) e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, true>, dim3(rows, a.c.heads, B), dim3(128), dim3(), 0, st, a);

@@ -29,11 +29,15 @@ struct AttendParams {
 constexpr int UNIT = 32;               // keys that a warp works on at a time
 constexpr int ATT_WARPS = 4;
 constexpr int MAX_SPLITS = 256, FEW_SPLITS = 8;      // parts at most; parts that one thread joins
-__host__ __device__ constexpr int att_stages(int dim) { return dim == 128 ? 3 : 4; }
+__host__ __device__ constexpr int att_stages(int dim, int nq) { return dim == 128 ? (nq == 4 ? 3 : 2) : dim == 64 ? 3 : 4; }
+// CTAs an SM: what registers and shared memory allow.
+__host__ __device__ constexpr int att_resident(int dim, int nq) {
+  return dim == 128 ? (nq == 4 ? 2 : 3) : dim == 64 ? (nq == 1 ? 4 : 3) : (nq == 1 ? 5 : nq == 2 ? 4 : 3);
+}
 __host__ __device__ constexpr int att_stage_bytes(int dim) { return 2 * UNIT * dim + 16; }
 __host__ __device__ constexpr int att_q_bytes(int dim, int nq, bool fp32) { return (nq + 1) / 2 * (dim / 16) * 512 * (fp32 ? 2 : 1); }
 __host__ __device__ constexpr int att_smem(int dim, int nq, bool fp32) {
-  return att_q_bytes(dim, nq, fp32) + ATT_WARPS * att_stages(dim) * att_stage_bytes(dim);
+  return att_q_bytes(dim, nq, fp32) + ATT_WARPS * att_stages(dim, nq) * att_stage_bytes(dim);
 }
 
 // 2^x to 2^-22 of itself; 0 for -inf.
@@ -102,6 +106,16 @@ __device__ __forceinline__ void codes_f16(Int8, uint32_t w, uint32_t& lo, uint32
   lo = *reinterpret_cast<const uint32_t*>(&x);
   hi = *reinterpret_cast<const uint32_t*>(&y);
 }
+// The same for the first product, which takes multiples of them plus a bias: (code + BIAS) / FACTOR, with BIAS times the sum of a row's query (and
+// its sign) where the product starts from.  INT8's c + 128 alone in FP16's low byte is that many times 2^-24.
+template <typename F> struct KeyCodes { static constexpr float BIAS = 0.f, FACTOR = 1.f; };
+template <> struct KeyCodes<Int8> { static constexpr float BIAS = 128.f, FACTOR = 16777216.f; };
+__device__ __forceinline__ void key_codes_f16(E4m3 f, uint32_t w, uint32_t& lo, uint32_t& hi) { codes_f16(f, w, lo, hi); }
+__device__ __forceinline__ void key_codes_f16(Int8, uint32_t w, uint32_t& lo, uint32_t& hi) {
+  w ^= 0x80808080u;
+  lo = __byte_perm(w, 0u, 0x4140);
+  hi = __byte_perm(w, 0u, 0x4342);
+}
 __device__ __forceinline__ void cp4(void* smem_dst, const void* gmem_src) {
   const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(smem_dst));
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(s), "l"(gmem_src) : "memory");
@@ -124,17 +138,18 @@ __device__ __forceinline__ int unit_key(int nt, int n) { return 16 * (nt >> 1) +
 // (16-byte asynchronous copies, zeros where no key is), nothing but __syncwarp between them, and keeps maximum, sum and result in registers until its
 // keys are through; the four warps' results are joined at the end.  The 16-byte pieces lie in shared memory so that both products' operands come out
 // of it whole, in the registers where mma wants them, without a transposition: dims and keys may be summed in any order.
+// TWO: blocks of 16 tokens, two in a unit.
 // grid = (row_tiles * splits, heads, B), block = 32 * ATT_WARPS.
-template <typename T, typename F, int DIM, int NQ>
-__global__ void __launch_bounds__(32 * ATT_WARPS)
+template <typename T, typename F, int DIM, int NQ, bool TWO>
+__global__ void __launch_bounds__(32 * ATT_WARPS, att_resident(DIM, NQ))
 cache_attention_kernel(AttendParams a) {
   constexpr bool WIDE = sizeof(T) == 4;               // two FP16 numbers for each query and probability
   constexpr int HL = WIDE ? 2 : 1;
   constexpr int KSTEPS = DIM / 16, ND = DIM / 16, MT = (NQ + 1) / 2, ROWS = 8 * NQ;
-  constexpr int STAGES = att_stages(DIM), STAGE = att_stage_bytes(DIM), COPIES = DIM / 16;
+  constexpr int STAGES = att_stages(DIM, NQ), STAGE = att_stage_bytes(DIM), COPIES = DIM / 16;
   constexpr int P_BITS = 14;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ float s_rf[ROWS];
+  __shared__ float s_rf[ROWS], s_start[ROWS];
   uint4* sq = reinterpret_cast<uint4*>(smem);          // [HL][MT][KSTEPS][lane]: operands as mma wants them
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
   unsigned char* ring = smem + att_q_bytes(DIM, NQ, WIDE) + warp * STAGES * STAGE;
@@ -154,51 +169,58 @@ cache_attention_kernel(AttendParams a) {
   const int u0 = first_unit + part_units * warp / ATT_WARPS, u1 = first_unit + part_units * (warp + 1) / ATT_WARPS;
 
   // ---- the ring ----
-  const uint8_t* kc = a.c.codes[0];
-  const uint8_t* vc = a.c.codes[1];
-  const int block = a.c.block, pieces = block == 16 ? 2 : 1;     // blocks that a unit lies in
+  const int block = a.c.block;
   int ids[2] = {0, 0}, id_base = u0;                             // lane i: block(s) of unit id_base + i
   auto look_up = [&](int base) {
     id_base = base;
     const int u = base + lane;
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
+    for (int z = 0; z < (TWO ? 2 : 1); ++z) {
       const int pos = u * UNIT + 16 * z;
-      ids[z] = u < u1 && pos < vis_max && z < pieces ? a.c.find(b, pos / block) : 0;
+      ids[z] = u < u1 && pos < vis_max ? a.c.find(b, pos / block) : 0;
       if (ids[z] < 0) latch_error(a.status, AD_ERR_ARG);
     }
   };
+  // Piece i of a thread's copies: byte 512 i + 16 lane of a unit's keys or values.  In shared memory keys lie in the order of score columns, values in
+  // their own, both with their 16-byte pieces exchanged so that eight threads that read at once meet all banks.  What depends on the thread is the same for
+  // every piece (for every other one, at DIM = 128), the rest is a constant.
+  const int my_key = lane * 16 / DIM, my_x = lane * 16 % DIM / 16;
+  const int my_col = ((my_key >> 3) & 1) * 8 + ((my_key & 3) << 1) + ((my_key >> 2) & 1);
+  const uint32_t ring_s = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+  const uint32_t k_dst = ring_s + my_col * DIM + my_x * 16, k_odd = ring_s + my_col * DIM + (DIM == 128 ? my_x ^ 4 : my_x) * 16;
+  const uint32_t v_dst = ring_s + UNIT * DIM + my_key * DIM + (DIM == 128 ? my_x ^ ((my_key & 3) << 1) : DIM == 64 ? my_x ^ (((my_key >> 1) & 1) << 1) : my_x) * 16;
   auto issue = [&](int u, int stage) {
     if (u >= u1) return;
     if (u - id_base >= 32) look_up(u);
-    unsigned char* st = ring + stage * STAGE;
     const int first = u * UNIT;
+    const uint32_t so = stage * STAGE;
     size_t tile[2];
     bool there[2];
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      const int id = __shfl_sync(0xffffffffu, ids[z], u - id_base);
+      const int id = z == 0 || TWO ? __shfl_sync(0xffffffffu, ids[z], u - id_base) : 0;
       there[z] = id >= 0;
       tile[z] = (size_t)max(id, 0) * a.c.heads + kvh;
     }
-    const int in_block = first & (block - 1);
+    const size_t src = (tile[0] * block + (TWO ? 0 : first & (block - 1))) * DIM + lane * 16;
+    const uint8_t* ks = a.c.codes[0] + src;
+    const uint8_t* vs = a.c.codes[1] + src;
+    const ptrdiff_t second = TWO ? (ptrdiff_t)(tile[1] - tile[0]) * 16 * DIM - 16 * DIM : 0;     // from where the second half would lie to where it does
+    const bool whole = first + UNIT <= vis_max && there[0] && (!TWO || there[1]);
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
-      const int byte = i * 512 + lane * 16, key = byte / DIM, x = byte % DIM / 16;           // key of the unit, 16-byte piece of it
-      const int z = pieces == 2 && i >= COPIES / 2 ? 1 : 0;
-      const size_t src = tile[z] * block * DIM + (pieces == 2 ? byte - z * 16 * DIM : in_block * DIM + byte);
-      const bool on = there[z] && first + key < vis_max;
-      // keys in the order of score columns, values in the order of keys
-      const int col = (key >> 4) * 16 + ((key >> 3) & 1) * 8 + ((key & 3) << 1) + ((key >> 2) & 1);
-      const int kx = DIM == 128 ? x ^ ((col & 1) << 2) : x;
-      const int vx = DIM == 128 ? x ^ ((key & 3) << 1) : DIM == 64 ? x ^ (((key >> 1) & 1) << 1) : x;
-      cp16(st + col * DIM + kx * 16, kc + src, on);
-      cp16(st + UNIT * DIM + key * DIM + vx * 16, vc + src, on);
+      const uint32_t kd = (DIM == 128 && (i & 1) ? k_odd : k_dst) + so + (DIM == 128 ? (16 * (i >> 2) + 8 * ((i >> 1) & 1) + (i & 1)) * DIM : i * 512);
+      const uint32_t vd = v_dst + so + i * 512;
+      const ptrdiff_t at = i * 512 + (TWO && i >= COPIES / 2 ? second : 0);
+      const int z = TWO && i >= COPIES / 2 ? 1 : 0;
+      const int n = whole || (there[z] && first + my_key + i * (512 / DIM) < vis_max) ? 16 : 0;   // zeros where there is no key
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(kd), "l"(ks + at), "r"(n) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vd), "l"(vs + at), "r"(n) : "memory");
     }
     if (lane < 4) {                                               // ks0, ks1, vs0, vs1; negative: no such block
       const int z = lane & 1;
-      float* dst = reinterpret_cast<float*>(st + 2 * UNIT * DIM) + lane;
-      const bool need = z < pieces && first + 16 * z < vis_max;
+      float* dst = reinterpret_cast<float*>(ring + stage * STAGE + 2 * UNIT * DIM) + lane;
+      const bool need = (z == 0 || TWO) && first + 16 * z < vis_max;
       if (need && (z ? there[1] : there[0])) cp4(dst, (lane < 2 ? a.c.scale[0] : a.c.scale[1]) + (z ? tile[1] : tile[0]));
       else *dst = need && lane < 2 ? -1.f : 1.f;
     }
@@ -225,7 +247,7 @@ cache_attention_kernel(AttendParams a) {
     }
     const uint32_t e = min(max(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23, 27u), 253u);     // exponent, 2^-100 .. 2^126
     const float up = __uint_as_float((267u - e) << 23);            // 2^(13 - exponent)
-    if (lane == 0 && r < ROWS) s_rf[r] = a.scale * (1.f / up);
+    float total = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; i += (PER > 1 ? 2 : 1)) {
       // one number (DIM = 32) or pairs
@@ -234,6 +256,10 @@ cache_attention_kernel(AttendParams a) {
       const int mt = r >> 4, word = half * 2 + ((r >> 3) & 1), ln = (r & 7) * 4 + cc;
       const float y0 = x[i] * up, y1 = PER > 1 ? x[PER > 1 ? i + 1 : 0] * up : 0.f;
       const uint32_t hi = pack_f16(y0, y1), lo = rest_f16(y0, y1, hi);
+      if constexpr (KeyCodes<F>::BIAS != 0.f) {
+        const float2 h2 = unpack_f16(hi), l2 = unpack_f16(lo);
+        total += h2.x + h2.y + (WIDE ? l2.x + l2.y : 0.f);
+      }
 #pragma unroll
       for (int h = 0; h < HL; ++h) {
         unsigned char* dst = reinterpret_cast<unsigned char*>(sq + ((h * MT + mt) * KSTEPS + j) * 32 + ln) + word * 4;
@@ -241,15 +267,22 @@ cache_attention_kernel(AttendParams a) {
         else reinterpret_cast<uint16_t*>(dst)[d & 1] = (uint16_t)(h ? lo : hi);
       }
     }
+#pragma unroll
+    for (int w = 16; w; w >>= 1) total += __shfl_xor_sync(0xffffffffu, total, w);
+    if (lane == 0 && r < ROWS) {
+      s_rf[r] = a.scale * (1.f / up) * KeyCodes<F>::FACTOR;
+      s_start[r] = -KeyCodes<F>::BIAS / KeyCodes<F>::FACTOR * total;
+    }
   }
   __syncthreads();
   // Scores: thread's row g of each eight, columns as above.  Results: dims DIM / 8 * g .. of rows 2 c and 2 c + 1 of each eight.
-  float rf[NQ], m[NQ], d[NQ], l[NQ], acc[NQ][ND][4];
+  float rf[NQ], start[NQ], m[NQ], d[NQ], l[NQ], acc[NQ][ND][4];
   bool large = false;                                 // scores whose steps in FP32 are a quarter and more
   int vis[NQ];
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
     rf[q] = s_rf[q * 8 + g];
+    start[q] = s_start[q * 8 + g];
     vis[q] = visible(r0 + q * 8 + g);
     m[q] = d[q] = -INFINITY;
     l[q] = 0.f;
@@ -259,7 +292,7 @@ cache_attention_kernel(AttendParams a) {
       for (int j = 0; j < 4; ++j) acc[q][i][j] = 0.f;
   }
   // queries of few steps stay in registers
-  constexpr bool Q_REGS = HL * MT * KSTEPS <= 8;
+  constexpr bool Q_REGS = HL * MT * KSTEPS <= 4;
   uint4 qr[Q_REGS ? HL : 1][Q_REGS ? MT : 1][Q_REGS ? KSTEPS : 1];
   if constexpr (Q_REGS) {
 #pragma unroll
@@ -286,7 +319,7 @@ cache_attention_kernel(AttendParams a) {
 #pragma unroll
       for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[t][nt][j] = 0.f;
+        for (int j = 0; j < 4; ++j) s[t][nt][j] = KeyCodes<F>::BIAS != 0.f && 2 * t + (j >> 1) < NQ ? start[2 * t + (j >> 1) < NQ ? 2 * t + (j >> 1) : 0] : 0.f;
     constexpr int RAW = KSTEPS < 4 ? KSTEPS : 4;       // words of codes of one load
 #pragma unroll
     for (int hh = 0; hh < KSTEPS / RAW; ++hh) {
@@ -316,7 +349,7 @@ cache_attention_kernel(AttendParams a) {
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt) {
           uint32_t b0, b1;
-          codes_f16(F(), raw[nt][j], b0, b1);
+          key_codes_f16(F(), raw[nt][j], b0, b1);
 #pragma unroll
           for (int h = HL - 1; h >= 0; --h)
 #pragma unroll
@@ -331,11 +364,11 @@ cache_attention_kernel(AttendParams a) {
         for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
           for (int j = 0; j < 2; ++j)
-            if (u * UNIT + unit_key(nt, 2 * c + j) >= vis[q] || (pieces == 2 && nt >= 2 ? sc.y : sc.x) < 0.f) s[q / 2][nt][2 * (q & 1) + j] = -INFINITY;
+            if (u * UNIT + unit_key(nt, 2 * c + j) >= vis[q] || (TWO && nt >= 2 ? sc.y : sc.x) < 0.f) s[q / 2][nt][2 * (q & 1) + j] = -INFINITY;
     }
     // ---- probabilities ----
-    float ks[2] = {fabsf(sc.x), pieces == 2 ? fabsf(sc.y) : fabsf(sc.x)};
-    const float ve[2] = {lg2(sc.z), pieces == 2 ? lg2(sc.w) : lg2(sc.z)};
+    float ks[2] = {fabsf(sc.x), TWO ? fabsf(sc.y) : fabsf(sc.x)};
+    const float ve[2] = {lg2(sc.z), TWO ? lg2(sc.w) : lg2(sc.z)};
     float ref[NQ], top[NQ], tod[NQ], tk[NQ][2];
     bool moved = false;
 #pragma unroll
@@ -343,11 +376,11 @@ cache_attention_kernel(AttendParams a) {
       const float(*sq4)[4] = s[q / 2];
       const int h = 2 * (q & 1);
       float x0 = fmaxf(max3(sq4[0][h], sq4[0][h + 1], sq4[1][h]), sq4[1][h + 1]), x1 = max3(sq4[2][h], sq4[2][h + 1], sq4[3][h]);
-      if (pieces == 1) x0 = max3(x0, x1, sq4[3][h + 1]);
+      if (!TWO) x0 = max3(x0, x1, sq4[3][h + 1]);
       else x1 = fmaxf(x1, sq4[3][h + 1]);
       x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
       x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
-      if (pieces == 2) {
+      if (TWO) {
         x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
         x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
       } else {
@@ -356,10 +389,11 @@ cache_attention_kernel(AttendParams a) {
       tk[q][0] = fmaxf(rf[q] * ks[0], FLT_MIN);
       tk[q][1] = fmaxf(rf[q] * ks[1], FLT_MIN);
       x0 = ceilf(x0 * tk[q][0]);                       // references are whole numbers: what goes from one to another is an exact power of two
-      x1 = ceilf(x1 * tk[q][1]);
+      x1 = TWO ? ceilf(x1 * tk[q][1]) : x0;
       top[q] = fmaxf(m[q], fmaxf(x0, x1));
       ref[q] = top[q] == -INFINITY ? 0.f : top[q];
-      tod[q] = fmaxf(d[q] + (m[q] - ref[q]), fmaxf(x0 - ref[q] + ve[0], x1 - ref[q] + ve[1]));
+      tod[q] = fmaxf(d[q] + (m[q] - ref[q]), x0 - ref[q] + ve[0]);
+      if (TWO) tod[q] = fmaxf(tod[q], x1 - ref[q] + ve[1]);
       moved |= top[q] != m[q] || tod[q] != d[q];
     }
     if (__any_sync(0xffffffffu, moved)) {
@@ -385,8 +419,9 @@ cache_attention_kernel(AttendParams a) {
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) s[q / 2][nt][2 * (q & 1) + j] *= tk[q][nt >> 1];
+          for (int j = 0; j < 2; ++j) s[q / 2][nt][2 * (q & 1) + j] = __fsub_rn(__fmul_rn(s[q / 2][nt][2 * (q & 1) + j], tk[q][nt >> 1]), ref[q]);
         tk[q][0] = tk[q][1] = 1.f;
+        ref[q] = 0.f;
       }
     }
     uint32_t pf[HL][NQ][4];                            // [score tile]: two keys' probabilities of row g, as the second product's operand
@@ -397,12 +432,11 @@ cache_attention_kernel(AttendParams a) {
         // p, as a share of the softmax's maximum, times 2^(14 + e), e = log2(values' scale) - d: what goes into the second product.  Its sum is taken
         // as it is and brought back afterwards, which the bounds on e keep inside FP32 (beyond them the values do not count, or the probability).
         const float e = (float)P_BITS + fminf(fmaxf(ve[z] - d[q], -100.f), 100.f), less = e - ref[q];
-        const float2 t2 = make_float2(tk[q][z], tk[q][z]), r2 = large ? make_float2(-ref[q], -ref[q]) : make_float2(less, less);
+        const float2 t2 = make_float2(tk[q][z], tk[q][z]), r2 = make_float2(less, less);
         float2 sum;
 #pragma unroll
         for (int nt = 2 * z; nt < 2 * z + 2; ++nt) {
           float2 y = fma2(make_float2(s[q / 2][nt][2 * (q & 1)], s[q / 2][nt][2 * (q & 1) + 1]), t2, r2);
-          if (large) { y.x += e; y.y += e; }
           y.x = ex2(y.x);
           y.y = ex2(y.y);
           sum = nt == 2 * z ? y : add2(sum, y);
