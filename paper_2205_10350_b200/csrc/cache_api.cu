@@ -1,7 +1,6 @@
 // Operator-level entry points of the 8-bit key/value cache and of sampled verification, declared in include/aggressive_decoding.h.
 #include <limits.h>
 #include <math.h>
-#include <stdlib.h>
 
 #include <algorithm>
 #include <atomic>
@@ -67,6 +66,7 @@ dim3 tile_grid(const ad_kv_cache* c, int32_t B, int32_t max_new) {
   return dim3(2 * c->n_kv_heads, (max_new + c->block - 2) / c->block + 1, B);
 }
 dim3 tile_threads(const ad_kv_cache* c) { return dim3(std::max(32, c->block * c->head_dim / (8 * kv::VECS))); }
+dim3 read_threads(const ad_kv_cache* c) { return dim3(std::max(32, c->block * c->head_dim / (16 * kv::READ_VECS))); }
 
 }  // namespace
 
@@ -100,39 +100,39 @@ extern "C" int ad_cache_read(const ad_kv_cache* c, void* k, void* v, int32_t dty
   const kv::Cache d = device_cache(c);
   return launched(entry, by_types(dtype, c->format, [&](auto t) {
     typedef typename decltype(t)::Num T;
-    return launch_op(kv::cache_read_kernel<T, typename decltype(t)::Fmt>, tile_grid(c, B, max_tokens), tile_threads(c), dim3(), 0,
+    return launch_op(kv::cache_read_kernel<T, typename decltype(t)::Fmt>, tile_grid(c, B, max_tokens), read_threads(c), dim3(), 0,
                      static_cast<cudaStream_t>(stream), d, static_cast<T*>(k), static_cast<T*>(v), (int)c->head_dim, off, start, (int)M,
                      (int)max_tokens, status);
   }));
 }
 
 namespace {
-const int64_t kWaves = getenv("AD_W") ? atoi(getenv("AD_W")) : 3;
-struct AttendPlan { int nq, row_tiles, splits, chunk; };
-// Rows of queries a CTA takes: 8 or 16 where that is all there are, else 32.  Keys are split into parts of the same length for all rows, so that a
-// ragged batch keeps the GPU busy to its end: short enough for CTAs to fill the GPU's shared memory once, two units a warp at least.
-AttendPlan attend_plan(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
+constexpr int kGranule = 8, kItemFixed = 16;
+struct AttendPlan { int nq, row_tiles, grid, granule; bool shared; };
+// Rows of queries a CTA takes: 8 or 16 where that is all there are, else 32.
+AttendPlan attend_plan(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
   AttendPlan plan;
   const int rows = max_new * (n_heads / c->n_kv_heads);
   plan.nq = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   plan.row_tiles = (rows + 8 * plan.nq - 1) / (8 * plan.nq);
-  const int resident = kv::att_resident(c->head_dim, plan.nq);
-  const int64_t base = (int64_t)B * c->n_kv_heads * plan.row_tiles;
-  const int units = std::max(1, (max_keys + kv::UNIT - 1) / kv::UNIT);
-  const int64_t wanted = std::min<int64_t>((kWaves * op_num_sms() * resident + base - 1) / base, kv::MAX_SPLITS);
-  plan.chunk = (int)std::max<int64_t>((units + wanted - 1) / wanted, 2 * kv::ATT_WARPS);
-  plan.splits = (units + plan.chunk - 1) / plan.chunk;
+  const int64_t items = (int64_t)B * c->n_kv_heads * plan.row_tiles, resident = op_num_sms() * kv::att_resident(c->head_dim, plan.nq);
+  const int pieces = std::max(1, (max_keys + kv::UNIT - 1) / kv::UNIT / kGranule);
+  plan.granule = pieces > 1 ? kGranule : 0;
+  plan.grid = (int)std::min(resident, items * pieces);
+  plan.shared = plan.grid > 6 * items;
   return plan;
 }
+// Scratch: granules in front of every row of the batch, then the parts (16-byte aligned).
+size_t attend_prefix_bytes(int32_t B) { return ((size_t)B + 2) / 2 * 2 * sizeof(long long); }
 size_t attend_part_bytes(const ad_kv_cache* c, const AttendPlan& plan, int32_t B) {
-  return plan.splits == 1 ? 0 : (size_t)B * c->n_kv_heads * plan.row_tiles * 8 * plan.nq * plan.splits * (c->head_dim + 2) * sizeof(float);
+  return plan.granule == 0 ? 0 : 2 * (size_t)plan.grid * 8 * plan.nq * (c->head_dim + 2) * sizeof(float) + attend_prefix_bytes(B);
 }
 bool attend_sizes(const ad_kv_cache* c, int32_t n_heads, int32_t max_new) {
   return n_heads >= 1 && n_heads <= 65535 && n_heads % c->n_kv_heads == 0 && (int64_t)max_new * (n_heads / c->n_kv_heads) <= (1 << 24);
 }
 
 template <typename T, typename F, int DIM, int NQ, bool TWO>
-cudaError_t launch_attention_part(const kv::AttendParams& a, int B, cudaStream_t st) {
+cudaError_t launch_attention_part(const kv::AttendParams& a, cudaStream_t st) {
   static std::atomic<uint64_t> raised{0};              // devices on which the kernel may use its shared memory
   auto kernel = kv::cache_attention_kernel<T, F, DIM, NQ, TWO>;
   constexpr int smem = kv::att_smem(DIM, NQ, sizeof(T) == 4);
@@ -142,27 +142,27 @@ cudaError_t launch_attention_part(const kv::AttendParams& a, int B, cudaStream_t
     if (e != cudaSuccess) return e;
     raised.fetch_or(bit, std::memory_order_relaxed);
   }
-  return launch_op(kernel, dim3(a.row_tiles * a.splits, a.c.heads, B), dim3(32 * kv::ATT_WARPS), dim3(), smem, st, a);
+  return launch_op(kernel, dim3(a.grid), dim3(32 * kv::ATT_WARPS), dim3(), smem, st, a);
 }
 template <typename T, typename F, int DIM, int NQ>
-cudaError_t launch_attention(const kv::AttendParams& a, int B, cudaStream_t st) {
-  cudaError_t e = a.c.block == 16 ? launch_attention_part<T, F, DIM, NQ, true>(a, B, st) : launch_attention_part<T, F, DIM, NQ, false>(a, B, st);
-  if (e == cudaSuccess && a.splits > 1) {
-    const int rows = a.row_tiles * 8 * NQ, groups = 512 / DIM;
-    if (a.splits > kv::FEW_SPLITS) e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, true>, dim3(rows, a.c.heads, B), dim3(128), dim3(), 0, st, a);
-    else e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, false>, dim3((rows + groups - 1) / groups, a.c.heads, B), dim3(128), dim3(), 0, st, a);
+cudaError_t launch_attention(const kv::AttendParams& a, const AttendPlan& plan, cudaStream_t st) {
+  cudaError_t e = a.c.block == 16 ? launch_attention_part<T, F, DIM, NQ, true>(a, st) : launch_attention_part<T, F, DIM, NQ, false>(a, st);
+  if (e == cudaSuccess && a.granule) {
+    const int rows = plan.row_tiles * 8 * NQ, groups = 512 / DIM;
+    if (plan.shared) e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, true>, dim3(rows, a.c.heads, a.B), dim3(128), dim3(), a.grid * sizeof(float), st, a);
+    else e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, false>, dim3((rows + groups - 1) / groups, a.c.heads, a.B), dim3(128), dim3(), 0, st, a);
   }
   return e;
 }
 template <typename T, typename F, int NQ>
-cudaError_t launch_attention_dim(const kv::AttendParams& a, int dim, int B, cudaStream_t st) {
-  return dim == 32 ? launch_attention<T, F, 32, NQ>(a, B, st) : dim == 64 ? launch_attention<T, F, 64, NQ>(a, B, st) : launch_attention<T, F, 128, NQ>(a, B, st);
+cudaError_t launch_attention_dim(const kv::AttendParams& a, const AttendPlan& plan, int dim, cudaStream_t st) {
+  return dim == 32 ? launch_attention<T, F, 32, NQ>(a, plan, st) : dim == 64 ? launch_attention<T, F, 64, NQ>(a, plan, st) : launch_attention<T, F, 128, NQ>(a, plan, st);
 }
 }  // namespace
 
 extern "C" size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
   if (cache_fault(c, B) || B < 1 || max_new < 1 || max_keys < 0 || !known_dtype(dtype) || !attend_sizes(c, n_heads, max_new)) return 0;
-  return attend_part_bytes(c, attend_plan(c, dtype, n_heads, B, max_new, max_keys), B);
+  return attend_part_bytes(c, attend_plan(c, n_heads, B, max_new, max_keys), B);
 }
 
 extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
@@ -179,20 +179,21 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
   if (!q || !out || !aligned(q, 16) || !aligned(out, 16)) return arg_fault(entry, "queries and result must be 16-byte aligned");
   if (q_stride < (int64_t)n_heads * c->head_dim || q_stride % (int64_t)(16 / dtype_bytes(dtype)))
     return arg_fault(entry, "queries must be a multiple of 16 bytes apart, and not overlap");
-  const AttendPlan plan = attend_plan(c, dtype, n_heads, B, max_new, max_keys);
+  const AttendPlan plan = attend_plan(c, n_heads, B, max_new, max_keys);
   const size_t need = attend_part_bytes(c, plan, B);
   if (scratch_bytes < need) return op_fail(AD_ERR_CAPACITY, entry, "scratch too small");
   if (need && (!scratch || !aligned(scratch, 256))) return arg_fault(entry, "scratch must be 256-byte aligned");
   kv::AttendParams a;
   a.c = device_cache(c); a.q = q; a.q_stride = (size_t)q_stride; a.out = out; a.n_heads = n_heads; a.M = M; a.max_new = max_new; a.off = off; a.len = len;
   a.causal = causal != 0; a.scale = scale * (float)M_LOG2E; a.status = status;
-  a.row_tiles = plan.row_tiles; a.splits = plan.splits; a.chunk = plan.chunk; a.part = static_cast<float*>(scratch);
+  a.B = B; a.grid = plan.grid; a.granule = plan.granule; a.fixed = kItemFixed;
+  a.prefix = static_cast<long long*>(scratch); a.part = reinterpret_cast<float*>(static_cast<char*>(scratch) + attend_prefix_bytes(B));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return launched(entry, by_types(dtype, c->format, [&](auto t) {
     typedef typename decltype(t)::Num T;
     typedef typename decltype(t)::Fmt F;
-    return plan.nq == 1 ? launch_attention_dim<T, F, 1>(a, c->head_dim, B, st) : plan.nq == 2 ? launch_attention_dim<T, F, 2>(a, c->head_dim, B, st)
-                                                                                           : launch_attention_dim<T, F, 4>(a, c->head_dim, B, st);
+    return plan.nq == 1 ? launch_attention_dim<T, F, 1>(a, plan, c->head_dim, st) : plan.nq == 2 ? launch_attention_dim<T, F, 2>(a, plan, c->head_dim, st)
+                                                                                                 : launch_attention_dim<T, F, 4>(a, plan, c->head_dim, st);
   }));
 }
 

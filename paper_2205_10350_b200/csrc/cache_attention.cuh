@@ -19,16 +19,16 @@ struct AttendParams {
   int causal;
   float scale;             // softmax scale times log2(e)
   int* status;
-  int row_tiles, splits;   // tiles of rows that queries may need; parts that keys may be split into
-  int chunk;               // units of a part
-  float* part;             // splits > 1: [tile rows][splits][dim] sums, then [tile rows][splits] maxima and sums of exponentials
-  // units of a part of a row with that many units
-  __host__ __device__ __forceinline__ int part_units(int units) const { const int least = (units + splits - 1) / splits; return least > chunk ? least : chunk; }
+  int B;
+  int grid;                // CTAs
+  int fixed;               // what an item takes besides its units, in units
+  int granule;             // units that one CTA works on at the least where a row's keys are split; 0: they are not
+  float* part;             // [2 grid][tile rows][dim] sums of values, then [2 grid][tile rows] maxima and sums of exponentials
+  long long* prefix;       // [B + 1] granules in front of each row of the batch
 };
 
 constexpr int UNIT = 32;               // keys that a warp works on at a time
 constexpr int ATT_WARPS = 4;
-constexpr int MAX_SPLITS = 256, FEW_SPLITS = 8;      // parts at most; parts that one thread joins
 __host__ __device__ constexpr int att_stages(int dim, int nq) { return dim == 128 ? (nq == 4 ? 3 : 2) : dim == 64 ? 3 : 4; }
 // CTAs an SM: what registers and shared memory allow.
 __host__ __device__ constexpr int att_resident(int dim, int nq) {
@@ -39,6 +39,27 @@ __host__ __device__ constexpr int att_q_bytes(int dim, int nq, bool fp32) { retu
 __host__ __device__ constexpr int att_smem(int dim, int nq, bool fp32) {
   return att_q_bytes(dim, nq, fp32) + ATT_WARPS * att_stages(dim, nq) * att_stage_bytes(dim);
 }
+
+// Work.  A row of the batch has `heads` times `tiles` (of its queries) items, each over all of the keys that the tile sees; an item is cut into `pieces`
+// granules of about the same number of units, and the CTAs share all granules evenly, in their order.  So a CTA works on a part of an item, or on
+// several, of which only the first and the last may be parts; lengths live on the device, and no batch is too ragged.
+struct RowWork {
+  int o, n, p, tiles, units, pieces;
+  long long granules;
+};
+__device__ __forceinline__ RowWork row_work(const AttendParams& a, int b, int tile_rows) {
+  RowWork w;
+  w.granules = 0;
+  if (!row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, w.o, w.n, w.p)) return w;
+  w.tiles = (w.n * (a.n_heads / a.c.heads) + tile_rows - 1) / tile_rows;
+  w.units = (w.p + (a.causal ? w.n : 0) + UNIT - 1) / UNIT;
+  w.pieces = a.granule ? (w.units + a.fixed + a.granule / 2) / a.granule : 1;
+  w.granules = (long long)a.c.heads * w.tiles * w.pieces;
+  return w;
+}
+__host__ __device__ __forceinline__ long long cta_start(long long total, long long cta, long long ctas) { return total * cta / ctas; }
+// The CTA that granule g falls to.
+__host__ __device__ __forceinline__ int cta_of(long long total, long long g, long long ctas) { return (int)(((g + 1) * ctas - 1) / total); }
 
 // 2^x to 2^-22 of itself; 0 for -inf.
 __device__ __forceinline__ float ex2(float x) {
@@ -139,7 +160,7 @@ __device__ __forceinline__ int unit_key(int nt, int n) { return 16 * (nt >> 1) +
 // keys are through; the four warps' results are joined at the end.  The 16-byte pieces lie in shared memory so that both products' operands come out
 // of it whole, in the registers where mma wants them, without a transposition: dims and keys may be summed in any order.
 // TWO: blocks of 16 tokens, two in a unit.
-// grid = (row_tiles * splits, heads, B), block = 32 * ATT_WARPS.
+// grid = as many as are resident at once, or as there are granules; block = 32 * ATT_WARPS.
 template <typename T, typename F, int DIM, int NQ, bool TWO>
 __global__ void __launch_bounds__(32 * ATT_WARPS, att_resident(DIM, NQ))
 cache_attention_kernel(AttendParams a) {
@@ -153,444 +174,525 @@ cache_attention_kernel(AttendParams a) {
   uint4* sq = reinterpret_cast<uint4*>(smem);          // [HL][MT][KSTEPS][lane]: operands as mma wants them
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
   unsigned char* ring = smem + att_q_bytes(DIM, NQ, WIDE) + warp * STAGES * STAGE;
+  __shared__ long long s_scan[ATT_WARPS], s_base;
+  __shared__ int s_row, s_vis[ROWS];
+  __shared__ struct { RowWork work; long long at, cur; int b, piece, piece_end, kvh, r0, r_last; } s_seg;
   pdl_launch();
   pdl_wait();
-  const int b = blockIdx.z, kvh = blockIdx.y, rt = blockIdx.x % a.row_tiles, split = blockIdx.x / a.row_tiles;
-  int o, n, p;
-  if (!row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, o, n, p)) return;
-  const int group = a.n_heads / a.c.heads, rows = n * group, r0 = rt * ROWS;
-  if (r0 >= rows) return;
-  const int r_last = min(r0 + ROWS, rows) - 1;
-  auto visible = [&](int r) { return a.causal ? p + min(r, r_last) / group + 1 : p; };
-  const int vis_min = visible(r0), vis_max = visible(r_last);
-  const int units = (vis_max + UNIT - 1) / UNIT, per_part = a.part_units(units);
-  const int first_unit = split * per_part, part_units = min(units - first_unit, per_part);
-  if (part_units <= 0 && split > 0) return;
-  const int u0 = first_unit + part_units * warp / ATT_WARPS, u1 = first_unit + part_units * (warp + 1) / ATT_WARPS;
-
-  // ---- the ring ----
-  const int block = a.c.block;
-  int ids[2] = {0, 0}, id_base = u0;                             // lane i: block(s) of unit id_base + i
-  auto look_up = [&](int base) {
-    id_base = base;
-    const int u = base + lane;
+  // ---- this CTA's granules ----
+  long long total = 0, mine = 0, front = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 32 * ATT_WARPS) {
+    mine = b0 + tid < a.B ? row_work(a, b0 + tid, ROWS).granules : 0;
+    long long run = mine;
 #pragma unroll
-    for (int z = 0; z < (TWO ? 2 : 1); ++z) {
-      const int pos = u * UNIT + 16 * z;
-      ids[z] = u < u1 && pos < vis_max ? a.c.find(b, pos / block) : 0;
-      if (ids[z] < 0) latch_error(a.status, AD_ERR_ARG);
+    for (int w = 1; w < 32; w <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, run, w);
+      if (lane >= w) run += y;
     }
-  };
-  // Piece i of a thread's copies: byte 512 i + 16 lane of a unit's keys or values.  In shared memory keys lie in the order of score columns, values in
-  // their own, both with their 16-byte pieces exchanged so that eight threads that read at once meet all banks.  What depends on the thread is the same for
-  // every piece (for every other one, at DIM = 128), the rest is a constant.
-  const int my_key = lane * 16 / DIM, my_x = lane * 16 % DIM / 16;
-  const int my_col = ((my_key >> 3) & 1) * 8 + ((my_key & 3) << 1) + ((my_key >> 2) & 1);
-  const uint32_t ring_s = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
-  const uint32_t k_dst = ring_s + my_col * DIM + my_x * 16, k_odd = ring_s + my_col * DIM + (DIM == 128 ? my_x ^ 4 : my_x) * 16;
-  const uint32_t v_dst = ring_s + UNIT * DIM + my_key * DIM + (DIM == 128 ? my_x ^ ((my_key & 3) << 1) : DIM == 64 ? my_x ^ (((my_key >> 1) & 1) << 1) : my_x) * 16;
-  auto issue = [&](int u, int stage) {
-    if (u >= u1) return;
-    if (u - id_base >= 32) look_up(u);
-    const int first = u * UNIT;
-    const uint32_t so = stage * STAGE;
-    size_t tile[2];
-    bool there[2];
+    if (lane == 31) s_scan[warp] = run;
+    __syncthreads();
+    front = total + run - mine;
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      const int id = z == 0 || TWO ? __shfl_sync(0xffffffffu, ids[z], u - id_base) : 0;
-      there[z] = id >= 0;
-      tile[z] = (size_t)max(id, 0) * a.c.heads + kvh;
+    for (int w = 0; w < ATT_WARPS; ++w) {
+      if (w < warp) front += s_scan[w];
+      total += s_scan[w];
     }
-    const size_t src = (tile[0] * block + (TWO ? 0 : first & (block - 1))) * DIM + lane * 16;
-    const uint8_t* ks = a.c.codes[0] + src;
-    const uint8_t* vs = a.c.codes[1] + src;
-    const ptrdiff_t second = TWO ? (ptrdiff_t)(tile[1] - tile[0]) * 16 * DIM - 16 * DIM : 0;     // from where the second half would lie to where it does
-    const bool whole = first + UNIT <= vis_max && there[0] && (!TWO || there[1]);
-#pragma unroll
-    for (int i = 0; i < COPIES; ++i) {
-      const uint32_t kd = (DIM == 128 && (i & 1) ? k_odd : k_dst) + so + (DIM == 128 ? (16 * (i >> 2) + 8 * ((i >> 1) & 1) + (i & 1)) * DIM : i * 512);
-      const uint32_t vd = v_dst + so + i * 512;
-      const ptrdiff_t at = i * 512 + (TWO && i >= COPIES / 2 ? second : 0);
-      const int z = TWO && i >= COPIES / 2 ? 1 : 0;
-      const int n = whole || (there[z] && first + my_key + i * (512 / DIM) < vis_max) ? 16 : 0;   // zeros where there is no key
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(kd), "l"(ks + at), "r"(n) : "memory");
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vd), "l"(vs + at), "r"(n) : "memory");
-    }
-    if (lane < 4) {                                               // ks0, ks1, vs0, vs1; negative: no such block
-      const int z = lane & 1;
-      float* dst = reinterpret_cast<float*>(ring + stage * STAGE + 2 * UNIT * DIM) + lane;
-      const bool need = (z == 0 || TWO) && first + 16 * z < vis_max;
-      if (need && (z ? there[1] : there[0])) cp4(dst, (lane < 2 ? a.c.scale[0] : a.c.scale[1]) + (z ? tile[1] : tile[0]));
-      else *dst = need && lane < 2 ? -1.f : 1.f;
-    }
-  };
-  look_up(u0);
-#pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s) {
-    issue(u0 + s, s);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (blockIdx.x == 0 && a.granule && b0 + tid < a.B) a.prefix[b0 + tid] = front;
+    __syncthreads();
   }
-
-  // ---- queries: the row's power of two, FP16, into operand order ----
-  // Thread's dims in step j: 64 (j / 4) + 16 c + 4 (j % 4) + 0 .. 3 (DIM = 32: 8 c + 4 j + 0 .. 3)
-  for (int r = warp; r < 16 * MT; r += ATT_WARPS) {
-    constexpr int PER = DIM / 32;
-    const int row = r0 + r;
-    float x[PER], top = 0.f;
+  if (blockIdx.x == 0 && a.granule && tid == 0) a.prefix[a.B] = total;
+  const long long ctas = min((long long)gridDim.x, total);
+  if (blockIdx.x >= ctas) return;
+  const long long g0 = cta_start(total, blockIdx.x, ctas), g1 = cta_start(total, blockIdx.x + 1, ctas);
+  if (a.B <= 32 * ATT_WARPS) {
+    if (front <= g0 && g0 < front + mine) { s_row = tid; s_base = front; }
+  } else if (warp == 0) {                     // (the same scan again, by one warp)
+    long long base = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      const long long x = b0 + lane < a.B ? row_work(a, b0 + lane, ROWS).granules : 0;
+      long long run = x;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) x[i] = 0.f;
-    if (r < ROWS && row <= r_last) {
-      const T* q = static_cast<const T*>(a.q) + (size_t)(o + row / group) * a.q_stride + ((size_t)kvh * group + row % group) * DIM + lane * PER;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) { x[i] = to_f32(q[i]); top = fmaxf(top, fabsf(x[i])); }
-    }
-    const uint32_t e = min(max(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23, 27u), 253u);     // exponent, 2^-100 .. 2^126
-    const float up = __uint_as_float((267u - e) << 23);            // 2^(13 - exponent)
-    float total = 0.f;
-#pragma unroll
-    for (int i = 0; i < PER; i += (PER > 1 ? 2 : 1)) {
-      // one number (DIM = 32) or pairs
-      const int d = lane * PER + i;
-      const int j = DIM == 32 ? (d >> 2) & 1 : (d >> 6) * 4 + ((d >> 2) & 3), cc = DIM == 32 ? d >> 3 : (d >> 4) & 3, half = (d >> 1) & 1;
-      const int mt = r >> 4, word = half * 2 + ((r >> 3) & 1), ln = (r & 7) * 4 + cc;
-      const float y0 = x[i] * up, y1 = PER > 1 ? x[PER > 1 ? i + 1 : 0] * up : 0.f;
-      const uint32_t hi = pack_f16(y0, y1), lo = rest_f16(y0, y1, hi);
-      if constexpr (KeyCodes<F>::BIAS != 0.f) {
-        const float2 h2 = unpack_f16(hi), l2 = unpack_f16(lo);
-        total += h2.x + h2.y + (WIDE ? l2.x + l2.y : 0.f);
+      for (int w = 1; w < 32; w <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, run, w);
+        if (lane >= w) run += y;
       }
-#pragma unroll
-      for (int h = 0; h < HL; ++h) {
-        unsigned char* dst = reinterpret_cast<unsigned char*>(sq + ((h * MT + mt) * KSTEPS + j) * 32 + ln) + word * 4;
-        if (PER > 1) *reinterpret_cast<uint32_t*>(dst) = h ? lo : hi;
-        else reinterpret_cast<uint16_t*>(dst)[d & 1] = (uint16_t)(h ? lo : hi);
-      }
-    }
-#pragma unroll
-    for (int w = 16; w; w >>= 1) total += __shfl_xor_sync(0xffffffffu, total, w);
-    if (lane == 0 && r < ROWS) {
-      s_rf[r] = a.scale * (1.f / up) * KeyCodes<F>::FACTOR;
-      s_start[r] = -KeyCodes<F>::BIAS / KeyCodes<F>::FACTOR * total;
+      const long long f = base + run - x;
+      if (f <= g0 && g0 < f + x) { s_row = b0 + lane; s_base = f; }
+      base += __shfl_sync(0xffffffffu, run, 31);
+      if (base > g0) break;
     }
   }
   __syncthreads();
-  // Scores: thread's row g of each eight, columns as above.  Results: dims DIM / 8 * g .. of rows 2 c and 2 c + 1 of each eight.
-  float rf[NQ], start[NQ], m[NQ], d[NQ], l[NQ], acc[NQ][ND][4];
-  bool large = false;                                 // scores whose steps in FP32 are a quarter and more
-  int vis[NQ];
-#pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    rf[q] = s_rf[q * 8 + g];
-    start[q] = s_start[q * 8 + g];
-    vis[q] = visible(r0 + q * 8 + g);
-    m[q] = d[q] = -INFINITY;
-    l[q] = 0.f;
-#pragma unroll
-    for (int i = 0; i < ND; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[q][i][j] = 0.f;
+  const int group = a.n_heads / a.c.heads;
+  if (tid == 0) {
+    s_seg.b = s_row;
+    s_seg.at = g0 - s_base;
+    s_seg.cur = g0;
+    s_seg.work = row_work(a, s_row, ROWS);
   }
-  // queries of few steps stay in registers
-  constexpr bool Q_REGS = HL * MT * KSTEPS <= 4;
-  uint4 qr[Q_REGS ? HL : 1][Q_REGS ? MT : 1][Q_REGS ? KSTEPS : 1];
-  if constexpr (Q_REGS) {
+  // What the loop over keys has no use for stays in shared memory meanwhile, for the sake of its registers.
+  for (;;) {
+    __syncthreads();
+    int kvh, r0, r_last, vis_min, vis_max, u0, u1;      // (of which this warp's units: the tile may see fewer than the row has)
+    {
+      const RowWork& work = s_seg.work;
+      const long long at = s_seg.at;
+      const int item = (int)(at / work.pieces), piece = (int)(at % work.pieces), piece_end = (int)min((long long)work.pieces, piece + (g1 - s_seg.cur));
+      kvh = item / work.tiles;
+      r0 = item % work.tiles * ROWS;
+      r_last = min(r0 + ROWS, work.n * group) - 1;
+      vis_min = a.causal ? work.p + r0 / group + 1 : work.p;
+      vis_max = a.causal ? work.p + r_last / group + 1 : work.p;
+      const int units = (vis_max + UNIT - 1) / UNIT;
+      const int f = min((int)((long long)work.units * piece / work.pieces), units), e = min((int)((long long)work.units * piece_end / work.pieces), units);
+      u0 = f + (int)((long long)(e - f) * warp / ATT_WARPS);
+      u1 = f + (int)((long long)(e - f) * (warp + 1) / ATT_WARPS);
+      if (tid < ROWS) s_vis[tid] = a.causal ? work.p + min(r0 + tid, r_last) / group + 1 : work.p;
+      if (tid == 0) { s_seg.piece = piece; s_seg.piece_end = piece_end; s_seg.kvh = kvh; s_seg.r0 = r0; s_seg.r_last = r_last; }
+    }
+    const int b = s_seg.b;
+
+    // ---- the ring ----
+    const int block = a.c.block;
+    int ids[2] = {0, 0}, id_base = u0;                             // lane i: block(s) of unit id_base + i
+    auto look_up = [&](int base) {
+      id_base = base;
+      const int u = base + lane;
 #pragma unroll
-    for (int h = 0; h < HL; ++h)
+      for (int z = 0; z < (TWO ? 2 : 1); ++z) {
+        const int pos = u * UNIT + 16 * z;
+        ids[z] = u < u1 && pos < vis_max ? a.c.find(b, pos / block) : 0;
+        if (ids[z] < 0) latch_error(a.status, AD_ERR_ARG);
+      }
+    };
+    // Piece i of a thread's copies: byte 512 i + 16 lane of a unit's keys or values.  In shared memory keys lie in the order of score columns, values in
+    // their own, both with their 16-byte pieces exchanged so that eight threads that read at once meet all banks.  What depends on the thread is the same for
+    // every piece (for every other one, at DIM = 128), the rest is a constant.
+    const int my_key = lane * 16 / DIM, my_x = lane * 16 % DIM / 16;
+    const int my_col = ((my_key >> 3) & 1) * 8 + ((my_key & 3) << 1) + ((my_key >> 2) & 1);
+    const uint32_t ring_s = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+    const uint32_t k_dst = ring_s + my_col * DIM + my_x * 16, k_odd = ring_s + my_col * DIM + (DIM == 128 ? my_x ^ 4 : my_x) * 16;
+    const uint32_t v_dst = ring_s + UNIT * DIM + my_key * DIM + (DIM == 128 ? my_x ^ ((my_key & 3) << 1) : DIM == 64 ? my_x ^ (((my_key >> 1) & 1) << 1) : my_x) * 16;
+    auto issue = [&](int u, int stage) {
+      if (u >= u1) return;
+      if (u - id_base >= 32) look_up(u);
+      const int first = u * UNIT;
+      const uint32_t so = stage * STAGE;
+      size_t tile[2];
+      bool there[2];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int id = z == 0 || TWO ? __shfl_sync(0xffffffffu, ids[z], u - id_base) : 0;
+        there[z] = id >= 0;
+        tile[z] = (size_t)max(id, 0) * a.c.heads + kvh;
+      }
+      const size_t src = (tile[0] * block + (TWO ? 0 : first & (block - 1))) * DIM + lane * 16;
+      const uint8_t* ks = a.c.codes[0] + src;
+      const uint8_t* vs = a.c.codes[1] + src;
+      const ptrdiff_t second = TWO ? (ptrdiff_t)(tile[1] - tile[0]) * 16 * DIM - 16 * DIM : 0;     // from where the second half would lie to where it does
+      const bool whole = first + UNIT <= vis_max && there[0] && (!TWO || there[1]);
+#pragma unroll
+      for (int i = 0; i < COPIES; ++i) {
+        const uint32_t kd = (DIM == 128 && (i & 1) ? k_odd : k_dst) + so + (DIM == 128 ? (16 * (i >> 2) + 8 * ((i >> 1) & 1) + (i & 1)) * DIM : i * 512);
+        const uint32_t vd = v_dst + so + i * 512;
+        const ptrdiff_t at = i * 512 + (TWO && i >= COPIES / 2 ? second : 0);
+        const int z = TWO && i >= COPIES / 2 ? 1 : 0;
+        const int n = whole || (there[z] && first + my_key + i * (512 / DIM) < vis_max) ? 16 : 0;   // zeros where there is no key
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(kd), "l"(ks + at), "r"(n) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vd), "l"(vs + at), "r"(n) : "memory");
+      }
+      if (lane < 4) {                                               // ks0, ks1, vs0, vs1; negative: no such block
+        const int z = lane & 1;
+        float* dst = reinterpret_cast<float*>(ring + stage * STAGE + 2 * UNIT * DIM) + lane;
+        const bool need = (z == 0 || TWO) && first + 16 * z < vis_max;
+        if (need && (z ? there[1] : there[0])) cp4(dst, (lane < 2 ? a.c.scale[0] : a.c.scale[1]) + (z ? tile[1] : tile[0]));
+        else *dst = need && lane < 2 ? -1.f : 1.f;
+      }
+    };
+    // ---- queries, a few rows a warp: under way first ----
+    constexpr int PER = DIM / 32, Q_ROWS = 16 * MT / ATT_WARPS;
+    T qx[Q_ROWS][PER];
+#pragma unroll
+    for (int k = 0; k < Q_ROWS; ++k) {
+      const int r = warp + k * ATT_WARPS, row = r0 + r;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) qx[k][i] = from_f32<T>(0.f);
+      if (r < ROWS && row <= r_last) {
+        const T* q = static_cast<const T*>(a.q) + (size_t)(s_seg.work.o + row / group) * a.q_stride + ((size_t)kvh * group + row % group) * DIM + lane * PER;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) qx[k][i] = q[i];
+      }
+    }
+    look_up(u0);
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+      issue(u0 + s, s);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+
+    // The row's power of two, FP16, into operand order.
+    // Thread's dims in step j: 64 (j / 4) + 16 c + 4 (j % 4) + 0 .. 3 (DIM = 32: 8 c + 4 j + 0 .. 3)
+#pragma unroll
+    for (int k = 0; k < Q_ROWS; ++k) {
+      const int r = warp + k * ATT_WARPS;
+      float x[PER], top = 0.f;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) { x[i] = to_f32(qx[k][i]); top = fmaxf(top, fabsf(x[i])); }
+      const uint32_t e = min(max(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23, 27u), 253u);     // exponent, 2^-100 .. 2^126
+      const float up = __uint_as_float((267u - e) << 23);            // 2^(13 - exponent)
+      float total = 0.f;
+#pragma unroll
+      for (int i = 0; i < PER; i += (PER > 1 ? 2 : 1)) {
+        // one number (DIM = 32) or pairs
+        const int d = lane * PER + i;
+        const int j = DIM == 32 ? (d >> 2) & 1 : (d >> 6) * 4 + ((d >> 2) & 3), cc = DIM == 32 ? d >> 3 : (d >> 4) & 3, half = (d >> 1) & 1;
+        const int mt = r >> 4, word = half * 2 + ((r >> 3) & 1), ln = (r & 7) * 4 + cc;
+        const float y0 = x[i] * up, y1 = PER > 1 ? x[PER > 1 ? i + 1 : 0] * up : 0.f;
+        const uint32_t hi = pack_f16(y0, y1), lo = rest_f16(y0, y1, hi);
+        if constexpr (KeyCodes<F>::BIAS != 0.f) {
+          const float2 h2 = unpack_f16(hi), l2 = unpack_f16(lo);
+          total += h2.x + h2.y + (WIDE ? l2.x + l2.y : 0.f);
+        }
+#pragma unroll
+        for (int h = 0; h < HL; ++h) {
+          unsigned char* dst = reinterpret_cast<unsigned char*>(sq + ((h * MT + mt) * KSTEPS + j) * 32 + ln) + word * 4;
+          if (PER > 1) *reinterpret_cast<uint32_t*>(dst) = h ? lo : hi;
+          else reinterpret_cast<uint16_t*>(dst)[d & 1] = (uint16_t)(h ? lo : hi);
+        }
+      }
+#pragma unroll
+      for (int w = 16; w; w >>= 1) total += __shfl_xor_sync(0xffffffffu, total, w);
+      if (lane == 0 && r < ROWS) {
+        s_rf[r] = a.scale * (1.f / up) * KeyCodes<F>::FACTOR;
+        s_start[r] = -KeyCodes<F>::BIAS / KeyCodes<F>::FACTOR * total;
+      }
+    }
+    __syncthreads();
+    // Scores: thread's row g of each eight, columns as above.  Results: dims DIM / 8 * g .. of rows 2 c and 2 c + 1 of each eight.
+    float rf[NQ], start[NQ], m[NQ], d[NQ], l[NQ], acc[NQ][ND][4];
+    bool large = false;                                 // scores whose steps in FP32 are a quarter and more
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      rf[q] = s_rf[q * 8 + g];
+      start[q] = s_start[q * 8 + g];
+      m[q] = d[q] = -INFINITY;
+      l[q] = 0.f;
+#pragma unroll
+      for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[q][i][j] = 0.f;
+    }
+    // queries of few steps stay in registers
+    constexpr bool Q_REGS = HL * MT * KSTEPS <= 4;
+    uint4 qr[Q_REGS ? HL : 1][Q_REGS ? MT : 1][Q_REGS ? KSTEPS : 1];
+    if constexpr (Q_REGS) {
+#pragma unroll
+      for (int h = 0; h < HL; ++h)
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int j = 0; j < KSTEPS; ++j) qr[h][t][j] = sq[((h * MT + t) * KSTEPS + j) * 32 + lane];
+    }
+
+    int stage = 0;
+    for (int u = u0; u < u1; ++u) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+      __syncwarp();
+      issue(u + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      const unsigned char* st = ring + stage * STAGE;
+      stage = stage == STAGES - 1 ? 0 : stage + 1;
+      const float4 sc = *reinterpret_cast<const float4*>(st + 2 * UNIT * DIM);
+      // ---- scores ----
+      float s[MT][4][4];
 #pragma unroll
       for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int j = 0; j < KSTEPS; ++j) qr[h][t][j] = sq[((h * MT + t) * KSTEPS + j) * 32 + lane];
-  }
-
-  int stage = 0;
-  for (int u = u0; u < u1; ++u) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
-    __syncwarp();
-    issue(u + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    const unsigned char* st = ring + stage * STAGE;
-    stage = stage == STAGES - 1 ? 0 : stage + 1;
-    const float4 sc = *reinterpret_cast<const float4*>(st + 2 * UNIT * DIM);
-    // ---- scores ----
-    float s[MT][4][4];
+        for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
+          for (int j = 0; j < 4; ++j) s[t][nt][j] = KeyCodes<F>::BIAS != 0.f && 2 * t + (j >> 1) < NQ ? start[2 * t + (j >> 1) < NQ ? 2 * t + (j >> 1) : 0] : 0.f;
+      constexpr int RAW = KSTEPS < 4 ? KSTEPS : 4;       // words of codes of one load
 #pragma unroll
-      for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[t][nt][j] = KeyCodes<F>::BIAS != 0.f && 2 * t + (j >> 1) < NQ ? start[2 * t + (j >> 1) < NQ ? 2 * t + (j >> 1) : 0] : 0.f;
-    constexpr int RAW = KSTEPS < 4 ? KSTEPS : 4;       // words of codes of one load
-#pragma unroll
-    for (int hh = 0; hh < KSTEPS / RAW; ++hh) {
-      uint32_t raw[4][RAW];
-#pragma unroll
-      for (int nt = 0; nt < 4; ++nt) {
-        const unsigned char* row = st + (nt * 8 + g) * DIM;
-        if constexpr (DIM == 32) {
-          const uint2 v = *reinterpret_cast<const uint2*>(row + c * 8);
-          raw[nt][0] = v.x; raw[nt][1] = v.y;
-        } else {
-          const int x = hh * 4 + c;
-          const uint4 v = *reinterpret_cast<const uint4*>(row + (DIM == 128 ? x ^ ((g & 1) << 2) : x) * 16);
-          raw[nt][0] = v.x; raw[nt][1] = v.y; raw[nt][RAW - 2] = v.z; raw[nt][RAW - 1] = v.w;
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < RAW; ++j) {
-        uint4 qf[HL][MT];
-#pragma unroll
-        for (int h = 0; h < HL; ++h)
-#pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            if constexpr (Q_REGS) qf[h][t] = qr[h][t][hh * RAW + j];
-            else qf[h][t] = sq[((h * MT + t) * KSTEPS + hh * RAW + j) * 32 + lane];
-          }
+      for (int hh = 0; hh < KSTEPS / RAW; ++hh) {
+        uint32_t raw[4][RAW];
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt) {
-          uint32_t b0, b1;
-          key_codes_f16(F(), raw[nt][j], b0, b1);
+          const unsigned char* row = st + (nt * 8 + g) * DIM;
+          if constexpr (DIM == 32) {
+            const uint2 v = *reinterpret_cast<const uint2*>(row + c * 8);
+            raw[nt][0] = v.x; raw[nt][1] = v.y;
+          } else {
+            const int x = hh * 4 + c;
+            const uint4 v = *reinterpret_cast<const uint4*>(row + (DIM == 128 ? x ^ ((g & 1) << 2) : x) * 16);
+            raw[nt][0] = v.x; raw[nt][1] = v.y; raw[nt][RAW - 2] = v.z; raw[nt][RAW - 1] = v.w;
+          }
+        }
 #pragma unroll
-          for (int h = HL - 1; h >= 0; --h)
+        for (int j = 0; j < RAW; ++j) {
+          uint4 qf[HL][MT];
 #pragma unroll
-            for (int t = 0; t < MT; ++t) mma_f16(s[t][nt], reinterpret_cast<const uint32_t*>(&qf[h][t]), b0, b1);
+          for (int h = 0; h < HL; ++h)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+              if constexpr (Q_REGS) qf[h][t] = qr[h][t][hh * RAW + j];
+              else qf[h][t] = sq[((h * MT + t) * KSTEPS + hh * RAW + j) * 32 + lane];
+            }
+#pragma unroll
+          for (int nt = 0; nt < 4; ++nt) {
+            uint32_t b0, b1;
+            key_codes_f16(F(), raw[nt][j], b0, b1);
+#pragma unroll
+            for (int h = HL - 1; h >= 0; --h)
+#pragma unroll
+              for (int t = 0; t < MT; ++t) mma_f16(s[t][nt], reinterpret_cast<const uint32_t*>(&qf[h][t]), b0, b1);
+          }
         }
       }
-    }
-    if (u * UNIT + UNIT > vis_min || sc.x < 0.f || sc.y < 0.f) {
+      if (u * UNIT + UNIT > vis_min || sc.x < 0.f || sc.y < 0.f) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+#pragma unroll
+          for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              if (u * UNIT + unit_key(nt, 2 * c + j) >= s_vis[q * 8 + g] || (TWO && nt >= 2 ? sc.y : sc.x) < 0.f) s[q / 2][nt][2 * (q & 1) + j] = -INFINITY;
+      }
+      // ---- probabilities ----
+      float ks[2] = {fabsf(sc.x), TWO ? fabsf(sc.y) : fabsf(sc.x)};
+      const float ve[2] = {lg2(sc.z), TWO ? lg2(sc.w) : lg2(sc.z)};
+      float ref[NQ], top[NQ], tod[NQ], tk[NQ][2];
+      bool moved = false;
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        const float(*sq4)[4] = s[q / 2];
+        const int h = 2 * (q & 1);
+        float x0 = fmaxf(max3(sq4[0][h], sq4[0][h + 1], sq4[1][h]), sq4[1][h + 1]), x1 = max3(sq4[2][h], sq4[2][h + 1], sq4[3][h]);
+        if (!TWO) x0 = max3(x0, x1, sq4[3][h + 1]);
+        else x1 = fmaxf(x1, sq4[3][h + 1]);
+        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
+        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
+        if (TWO) {
+          x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
+          x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
+        } else {
+          x1 = x0;
+        }
+        tk[q][0] = fmaxf(rf[q] * ks[0], FLT_MIN);
+        tk[q][1] = fmaxf(rf[q] * ks[1], FLT_MIN);
+        x0 = ceilf(x0 * tk[q][0]);                       // references are whole numbers: what goes from one to another is an exact power of two
+        x1 = TWO ? ceilf(x1 * tk[q][1]) : x0;
+        top[q] = fmaxf(m[q], fmaxf(x0, x1));
+        ref[q] = top[q] == -INFINITY ? 0.f : top[q];
+        tod[q] = fmaxf(d[q] + (m[q] - ref[q]), x0 - ref[q] + ve[0]);
+        if (TWO) tod[q] = fmaxf(tod[q], x1 - ref[q] + ve[1]);
+        moved |= top[q] != m[q] || tod[q] != d[q];
+      }
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+          const float less = m[q] - ref[q], keep_o = tod[q] == -INFINITY ? 0.f : ex2(less + (d[q] - tod[q]));
+          m[q] = top[q];
+          d[q] = tod[q];
+          l[q] *= ex2(less);
+          const float k0 = __shfl_sync(0xffffffffu, keep_o, 8 * c), k1 = __shfl_sync(0xffffffffu, keep_o, 8 * c + 4);
+#pragma unroll
+          for (int i = 0; i < ND; ++i) {
+            const float2 y0 = mul2(make_float2(acc[q][i][0], acc[q][i][1]), make_float2(k0, k1)), y1 = mul2(make_float2(acc[q][i][2], acc[q][i][3]), make_float2(k0, k1));
+            acc[q][i][0] = y0.x; acc[q][i][1] = y0.y; acc[q][i][2] = y1.x; acc[q][i][3] = y1.y;
+          }
+          large |= fabsf(ref[q]) > 4194304.f;
+        }
+        large = __any_sync(0xffffffffu, large);
+      }
+      if (large) {                                       // the exponent below then is a difference of rounded scores, as the maximum is one of them
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+#pragma unroll
+          for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) s[q / 2][nt][2 * (q & 1) + j] = __fsub_rn(__fmul_rn(s[q / 2][nt][2 * (q & 1) + j], tk[q][nt >> 1]), ref[q]);
+          tk[q][0] = tk[q][1] = 1.f;
+          ref[q] = 0.f;
+        }
+      }
+      uint32_t pf[HL][NQ][4];                            // [score tile]: two keys' probabilities of row g, as the second product's operand
 #pragma unroll
       for (int q = 0; q < NQ; ++q)
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
+        for (int z = 0; z < 2; ++z) {
+          // p, as a share of the softmax's maximum, times 2^(14 + e), e = log2(values' scale) - d: what goes into the second product.  Its sum is taken
+          // as it is and brought back afterwards, which the bounds on e keep inside FP32 (beyond them the values do not count, or the probability).
+          const float e = (float)P_BITS + fminf(fmaxf(ve[z] - d[q], -100.f), 100.f), less = e - ref[q];
+          const float2 t2 = make_float2(tk[q][z], tk[q][z]), r2 = make_float2(less, less);
+          float2 sum;
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            if (u * UNIT + unit_key(nt, 2 * c + j) >= vis[q] || (TWO && nt >= 2 ? sc.y : sc.x) < 0.f) s[q / 2][nt][2 * (q & 1) + j] = -INFINITY;
+          for (int nt = 2 * z; nt < 2 * z + 2; ++nt) {
+            float2 y = fma2(make_float2(s[q / 2][nt][2 * (q & 1)], s[q / 2][nt][2 * (q & 1) + 1]), t2, r2);
+            y.x = ex2(y.x);
+            y.y = ex2(y.y);
+            sum = nt == 2 * z ? y : add2(sum, y);
+            pf[0][q][nt] = pack_f16(y.x, y.y);
+            if constexpr (WIDE) pf[HL - 1][q][nt] = rest_f16(y.x, y.y, pf[0][q][nt]);
+          }
+          l[q] = fmaf(sum.x + sum.y, ex2(-e), l[q]);
+        }
+      // ---- times values ----
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        constexpr int WORDS = DIM / 32;                  // words of a key's codes that the thread reads
+        uint32_t v[4][WORDS];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = 16 * j + c + 4 * i;
+          const unsigned char* row = st + UNIT * DIM + key * DIM;
+          if constexpr (DIM == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(row + ((g ^ ((key & 3) << 1)) * 16));
+            v[i][0] = x.x; v[i][1] = x.y; v[i][WORDS - 2] = x.z; v[i][WORDS - 1] = x.w;
+          } else if constexpr (DIM == 64) {
+            const uint2 x = *reinterpret_cast<const uint2*>(row + ((g >> 1) ^ (((key >> 1) & 1) << 1)) * 16 + (g & 1) * 8);
+            v[i][0] = x.x; v[i][WORDS - 1] = x.y;
+          } else {
+            v[i][0] = *reinterpret_cast<const uint32_t*>(row + g * 4);
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < WORDS; ++x)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const uint32_t w0 = __byte_perm(v[0][x], v[1][x], y ? 0x7362 : 0x5140), w1 = __byte_perm(v[2][x], v[3][x], y ? 0x7362 : 0x5140);
+            uint32_t av[4];                              // dims DIM / 8 * g + 4 x + 2 y and the next one, four keys
+            codes_f16(F(), w0, av[0], av[1]);
+            codes_f16(F(), w1, av[2], av[3]);
+#pragma unroll
+            for (int h = HL - 1; h >= 0; --h)
+#pragma unroll
+              for (int q = 0; q < NQ; ++q) mma_f16(acc[q][2 * x + y], av, pf[h][q][2 * j], pf[h][q][2 * j + 1]);
+          }
+      }
     }
-    // ---- probabilities ----
-    float ks[2] = {fabsf(sc.x), TWO ? fabsf(sc.y) : fabsf(sc.x)};
-    const float ve[2] = {lg2(sc.z), TWO ? lg2(sc.w) : lg2(sc.z)};
-    float ref[NQ], top[NQ], tod[NQ], tk[NQ][2];
-    bool moved = false;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+
+    // ---- the warps' results together ----
+    constexpr int PITCH = DIM + 4;
+    float* so = reinterpret_cast<float*>(smem);                     // [warps][ROWS][PITCH]
+    float* sm = so + ATT_WARPS * ROWS * PITCH;                      // [warps][ROWS] maxima, sums, exponents of the results
+    float* sl = sm + ATT_WARPS * ROWS;
+    float* sd = sl + ATT_WARPS * ROWS;
+    static_assert((ATT_WARPS * ROWS * (PITCH + 3)) * 4 <= att_smem(DIM, NQ, WIDE), "results fit where the ring was");
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      const float(*sq4)[4] = s[q / 2];
-      const int h = 2 * (q & 1);
-      float x0 = fmaxf(max3(sq4[0][h], sq4[0][h + 1], sq4[1][h]), sq4[1][h + 1]), x1 = max3(sq4[2][h], sq4[2][h + 1], sq4[3][h]);
-      if (!TWO) x0 = max3(x0, x1, sq4[3][h + 1]);
-      else x1 = fmaxf(x1, sq4[3][h + 1]);
-      x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
-      x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
-      if (TWO) {
-        x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
-        x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
+      float* dst = so + (warp * ROWS + q * 8 + 2 * c) * PITCH + g * (DIM / 8);
+#pragma unroll
+      for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *reinterpret_cast<float2*>(dst + j * PITCH + 2 * i) = make_float2(acc[q][i][j], acc[q][i][2 + j]);
+      float sum = l[q];
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      if (c == 0) {
+        const int r = warp * ROWS + q * 8 + g;
+        sm[r] = m[q]; sl[r] = sum; sd[r] = d[q] - (float)P_BITS;
+      }
+    }
+    __syncthreads();
+    constexpr int LANES = DIM / 8, AT_ONCE = 32 * ATT_WARPS / LANES;      // threads a row, each eight dims
+    const int d0 = tid % LANES * 8;
+    const bool whole_item = s_seg.piece == 0 && s_seg.piece_end == s_seg.work.pieces;
+    const size_t slot = 2 * (size_t)blockIdx.x + (s_seg.cur == g0 ? 0 : 1);
+    r0 = s_seg.r0;
+    r_last = s_seg.r_last;
+    kvh = s_seg.kvh;
+    for (int r = tid / LANES; r < ROWS && r0 + r <= r_last; r += AT_ONCE) {
+      float top = -INFINITY, sum = 0.f, x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = 0.f;
+#pragma unroll
+      for (int v = 0; v < ATT_WARPS; ++v) top = fmaxf(top, sm[v * ROWS + r]);
+#pragma unroll
+      for (int v = 0; v < ATT_WARPS; ++v) {
+        const float mv = sm[v * ROWS + r], lv = sl[v * ROWS + r], f = mv == top ? 1.f : ex2(mv - top), fo = ex2(sd[v * ROWS + r]) * f;
+        if (lv == 0.f) continue;                          // (no key)
+        sum += lv * f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * fo;
+      }
+      if (!whole_item) {
+        store8(a.part + (slot * ROWS + r) * DIM + d0, x);
+        if (d0 == 0) reinterpret_cast<float2*>(a.part + 2 * (size_t)a.grid * ROWS * DIM)[slot * ROWS + r] = make_float2(top, sum);
       } else {
-        x1 = x0;
-      }
-      tk[q][0] = fmaxf(rf[q] * ks[0], FLT_MIN);
-      tk[q][1] = fmaxf(rf[q] * ks[1], FLT_MIN);
-      x0 = ceilf(x0 * tk[q][0]);                       // references are whole numbers: what goes from one to another is an exact power of two
-      x1 = TWO ? ceilf(x1 * tk[q][1]) : x0;
-      top[q] = fmaxf(m[q], fmaxf(x0, x1));
-      ref[q] = top[q] == -INFINITY ? 0.f : top[q];
-      tod[q] = fmaxf(d[q] + (m[q] - ref[q]), x0 - ref[q] + ve[0]);
-      if (TWO) tod[q] = fmaxf(tod[q], x1 - ref[q] + ve[1]);
-      moved |= top[q] != m[q] || tod[q] != d[q];
-    }
-    if (__any_sync(0xffffffffu, moved)) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        const float less = m[q] - ref[q], keep_o = tod[q] == -INFINITY ? 0.f : ex2(less + (d[q] - tod[q]));
-        m[q] = top[q];
-        d[q] = tod[q];
-        l[q] *= ex2(less);
-        const float k0 = __shfl_sync(0xffffffffu, keep_o, 8 * c), k1 = __shfl_sync(0xffffffffu, keep_o, 8 * c + 4);
-#pragma unroll
-        for (int i = 0; i < ND; ++i) {
-          const float2 y0 = mul2(make_float2(acc[q][i][0], acc[q][i][1]), make_float2(k0, k1)), y1 = mul2(make_float2(acc[q][i][2], acc[q][i][3]), make_float2(k0, k1));
-          acc[q][i][0] = y0.x; acc[q][i][1] = y0.y; acc[q][i][2] = y1.x; acc[q][i][3] = y1.y;
-        }
-        large |= fabsf(ref[q]) > 4194304.f;
-      }
-      large = __any_sync(0xffffffffu, large);
-    }
-    if (large) {                                       // the exponent below then is a difference of rounded scores, as the maximum is one of them
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-#pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) s[q / 2][nt][2 * (q & 1) + j] = __fsub_rn(__fmul_rn(s[q / 2][nt][2 * (q & 1) + j], tk[q][nt >> 1]), ref[q]);
-        tk[q][0] = tk[q][1] = 1.f;
-        ref[q] = 0.f;
+        for (int i = 0; i < 8; ++i) x[i] *= inv;
+        const int row = r0 + r;
+        store8(static_cast<T*>(a.out) + ((size_t)(s_seg.work.o + row / group) * a.n_heads + kvh * group + row % group) * DIM + d0, x);
       }
     }
-    uint32_t pf[HL][NQ][4];                            // [score tile]: two keys' probabilities of row g, as the second product's operand
-#pragma unroll
-    for (int q = 0; q < NQ; ++q)
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        // p, as a share of the softmax's maximum, times 2^(14 + e), e = log2(values' scale) - d: what goes into the second product.  Its sum is taken
-        // as it is and brought back afterwards, which the bounds on e keep inside FP32 (beyond them the values do not count, or the probability).
-        const float e = (float)P_BITS + fminf(fmaxf(ve[z] - d[q], -100.f), 100.f), less = e - ref[q];
-        const float2 t2 = make_float2(tk[q][z], tk[q][z]), r2 = make_float2(less, less);
-        float2 sum;
-#pragma unroll
-        for (int nt = 2 * z; nt < 2 * z + 2; ++nt) {
-          float2 y = fma2(make_float2(s[q / 2][nt][2 * (q & 1)], s[q / 2][nt][2 * (q & 1) + 1]), t2, r2);
-          y.x = ex2(y.x);
-          y.y = ex2(y.y);
-          sum = nt == 2 * z ? y : add2(sum, y);
-          pf[0][q][nt] = pack_f16(y.x, y.y);
-          if constexpr (WIDE) pf[HL - 1][q][nt] = rest_f16(y.x, y.y, pf[0][q][nt]);
-        }
-        l[q] = fmaf(sum.x + sum.y, ex2(-e), l[q]);
-      }
-    // ---- times values ----
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      constexpr int WORDS = DIM / 32;                  // words of a key's codes that the thread reads
-      uint32_t v[4][WORDS];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int key = 16 * j + c + 4 * i;
-        const unsigned char* row = st + UNIT * DIM + key * DIM;
-        if constexpr (DIM == 128) {
-          const uint4 x = *reinterpret_cast<const uint4*>(row + ((g ^ ((key & 3) << 1)) * 16));
-          v[i][0] = x.x; v[i][1] = x.y; v[i][WORDS - 2] = x.z; v[i][WORDS - 1] = x.w;
-        } else if constexpr (DIM == 64) {
-          const uint2 x = *reinterpret_cast<const uint2*>(row + ((g >> 1) ^ (((key >> 1) & 1) << 1)) * 16 + (g & 1) * 8);
-          v[i][0] = x.x; v[i][WORDS - 1] = x.y;
-        } else {
-          v[i][0] = *reinterpret_cast<const uint32_t*>(row + g * 4);
-        }
-      }
-#pragma unroll
-      for (int x = 0; x < WORDS; ++x)
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const uint32_t w0 = __byte_perm(v[0][x], v[1][x], y ? 0x7362 : 0x5140), w1 = __byte_perm(v[2][x], v[3][x], y ? 0x7362 : 0x5140);
-          uint32_t av[4];                              // dims DIM / 8 * g + 4 x + 2 y and the next one, four keys
-          codes_f16(F(), w0, av[0], av[1]);
-          codes_f16(F(), w1, av[2], av[3]);
-#pragma unroll
-          for (int h = HL - 1; h >= 0; --h)
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) mma_f16(acc[q][2 * x + y], av, pf[h][q][2 * j], pf[h][q][2 * j + 1]);
-        }
-    }
-  }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-  __syncthreads();
-
-  // ---- the warps' results together ----
-  constexpr int PITCH = DIM + 4;
-  float* so = reinterpret_cast<float*>(smem);                     // [warps][ROWS][PITCH]
-  float* sm = so + ATT_WARPS * ROWS * PITCH;                      // [warps][ROWS] maxima, sums, exponents of the results
-  float* sl = sm + ATT_WARPS * ROWS;
-  float* sd = sl + ATT_WARPS * ROWS;
-  static_assert((ATT_WARPS * ROWS * (PITCH + 3)) * 4 <= att_smem(DIM, NQ, WIDE), "results fit where the ring was");
-#pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    float* dst = so + (warp * ROWS + q * 8 + 2 * c) * PITCH + g * (DIM / 8);
-#pragma unroll
-    for (int i = 0; i < ND; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) *reinterpret_cast<float2*>(dst + j * PITCH + 2 * i) = make_float2(acc[q][i][j], acc[q][i][2 + j]);
-    float sum = l[q];
-    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    if (c == 0) {
-      const int r = warp * ROWS + q * 8 + g;
-      sm[r] = m[q]; sl[r] = sum; sd[r] = d[q] - (float)P_BITS;
-    }
-  }
-  __syncthreads();
-  constexpr int LANES = DIM / 8, AT_ONCE = 32 * ATT_WARPS / LANES;      // threads a row, each eight dims
-  const int d0 = tid % LANES * 8;
-  const size_t tile_row = (((size_t)b * a.c.heads + kvh) * a.row_tiles + rt) * ROWS, all_rows = (size_t)gridDim.z * gridDim.y * a.row_tiles * ROWS;
-  for (int r = tid / LANES; r < ROWS && r0 + r <= r_last; r += AT_ONCE) {
-    float top = -INFINITY, sum = 0.f, x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 0.f;
-#pragma unroll
-    for (int v = 0; v < ATT_WARPS; ++v) top = fmaxf(top, sm[v * ROWS + r]);
-#pragma unroll
-    for (int v = 0; v < ATT_WARPS; ++v) {
-      const float mv = sm[v * ROWS + r], lv = sl[v * ROWS + r], f = mv == top ? 1.f : ex2(mv - top), fo = ex2(sd[v * ROWS + r]) * f;
-      if (lv == 0.f) continue;                          // (no key)
-      sum += lv * f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * fo;
-    }
-    if (per_part < units) {
-      const size_t slot = (tile_row + r) * a.splits + split;
-      store8(a.part + slot * DIM + d0, x);
-      if (d0 == 0) reinterpret_cast<float2*>(a.part + all_rows * a.splits * DIM)[slot] = make_float2(top, sum);
-    } else {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= inv;
-      const int row = r0 + r;
-      store8(static_cast<T*>(a.out) + ((size_t)(o + row / group) * a.n_heads + kvh * group + row % group) * DIM + d0, x);
+    const int done = s_seg.piece_end - s_seg.piece;
+    if (s_seg.cur + done >= g1) break;
+    __syncthreads();                             // shared memory is the next item's
+    if (tid == 0) {
+      s_seg.cur += done;
+      s_seg.at += done;
+      while (s_seg.at == s_seg.work.granules) { s_seg.at = 0; s_seg.work = row_work(a, ++s_seg.b, ROWS); }   // (rows without work have no granules)
     }
   }
 }
 
-// Joins the parts of a row's keys, where there is more than one.  Four dims a thread, so that 128 threads are 128 / (DIM / 4) groups: SHARED, they take
-// a row's parts in turn and add up in their order, else each has a row of its own.  Bound by latency: maxima and sums of all parts are loaded at once
-// (each lane of a warp one part), results eight parts ahead.
-// grid = (rows, or rows / groups, heads, B), block = 128.
+// Joins the parts of items that more than one CTA worked on.  Four dims a thread, so that 128 threads are 128 / (DIM / 4) groups: SHARED, they take a
+// row's parts in turn, else each has a row of its own; parts are added up in their order.  Bound by latency: SHARED, maxima and sums of all parts are
+// loaded at once and results eight parts ahead.
+// grid = (rows, or rows / groups, heads, B), block = 128; dynamic shared memory (SHARED): a float per CTA of the attention.
 template <typename T, int DIM, int NQ, bool SHARED>
 __global__ void __launch_bounds__(128)
 cache_attention_join_kernel(AttendParams a) {
   constexpr int ROWS = 8 * NQ, LANES = DIM / 4, GROUPS = 128 / LANES;
+  extern __shared__ float s_w[];
   __shared__ float4 s_x[SHARED ? GROUPS - 1 : 1][LANES];
-  __shared__ float s_w[SHARED ? MAX_SPLITS : 1];
+  __shared__ float s_red[2][4];
   pdl_launch();
   pdl_wait();
-  const int tid = threadIdx.x, grp = tid / LANES, d0 = tid % LANES * 4;
+  const int tid = threadIdx.x, lane = tid & 31, grp = tid / LANES, d0 = tid % LANES * 4;
   const int b = blockIdx.z, kvh = blockIdx.y, r = SHARED ? blockIdx.x : blockIdx.x * GROUPS + grp;
-  int o, n, p;
-  if (!row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, o, n, p)) return;
+  const RowWork work = row_work(a, b, ROWS);
   const int group = a.n_heads / a.c.heads;
-  if (r >= n * group) return;
-  // as many parts as the row's tile has been split into
-  const int r_last = min(r / ROWS * ROWS + ROWS, n * group) - 1, units = ((a.causal ? p + r_last / group + 1 : p) + UNIT - 1) / UNIT;
-  const int per_part = a.part_units(units), parts = (units + per_part - 1) / per_part;
-  if (parts <= 1) return;
-  const size_t all_rows = (size_t)gridDim.z * gridDim.y * a.row_tiles * ROWS;
-  const size_t slot = (((size_t)b * a.c.heads + kvh) * a.row_tiles * ROWS + r) * a.splits;
-  const float2* ml = reinterpret_cast<const float2*>(a.part + all_rows * a.splits * DIM) + slot;
-  const float* part = a.part + slot * DIM + d0;
+  if (work.granules == 0 || r >= work.n * group || work.pieces == 1) return;
+  const long long total = __ldcg(a.prefix + a.B), ctas = min((long long)a.grid, total);
+  const long long first = __ldcg(a.prefix + b) + ((long long)kvh * work.tiles + r / ROWS) * work.pieces;
+  const int c0 = cta_of(total, first, ctas), parts = cta_of(total, first + work.pieces - 1, ctas) - c0 + 1;
+  if (parts == 1) return;
+  // the first CTA's part is its last segment unless it starts there; the others' are their first
+  const int slot0 = 2 * c0 + (cta_start(total, c0, ctas) < first ? 1 : 0);
+  const int rr = r % ROWS;
+  auto row_of = [&](int i) { return (size_t)(i == 0 ? slot0 : 2 * (c0 + i)) * ROWS + rr; };
+  const float2* ml = reinterpret_cast<const float2*>(a.part + 2 * (size_t)a.grid * ROWS * DIM);
   float sum = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](float4 y, float f) { x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w); };
   if constexpr (SHARED) {
-    // every warp for itself: maxima, weights, and their sum
-    const int lane = tid & 31;
     float top = -INFINITY;
-    float2 v[MAX_SPLITS / 32];
-#pragma unroll
-    for (int i = 0; i < MAX_SPLITS / 32; ++i) {
-      v[i] = i * 32 + lane < parts ? __ldcg(ml + i * 32 + lane) : make_float2(-INFINITY, 0.f);
-      top = fmaxf(top, v[i].x);
-    }
+    for (int i = tid; i < parts; i += 128) top = fmaxf(top, __ldcg(ml + row_of(i)).x);
 #pragma unroll
     for (int w = 16; w; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-#pragma unroll
-    for (int i = 0; i < MAX_SPLITS / 32; ++i) {
-      const float f = v[i].y == 0.f ? 0.f : v[i].x == top ? 1.f : ex2(v[i].x - top);      // (no key: nothing, whatever the maxima)
-      sum += v[i].y * f;
-      if (tid < 32 && i * 32 + lane < parts) s_w[i * 32 + lane] = f;
+    if (lane == 0) s_red[0][tid >> 5] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
+    for (int i = tid; i < parts; i += 128) {
+      const float2 v = __ldcg(ml + row_of(i));
+      const float f = v.y == 0.f ? 0.f : v.x == top ? 1.f : ex2(v.x - top);      // (no key: nothing, whatever the maxima)
+      s_w[i] = f;
+      sum += v.y * f;
     }
 #pragma unroll
     for (int w = 16; w; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+    if (lane == 0) s_red[1][tid >> 5] = sum;
     __syncthreads();
+    sum = (s_red[1][0] + s_red[1][1]) + (s_red[1][2] + s_red[1][3]);
     for (int s0 = grp; s0 < parts; s0 += 8 * GROUPS) {
       float4 y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (s0 + i * GROUPS < parts) y[i] = __ldcg(reinterpret_cast<const float4*>(part + (size_t)(s0 + i * GROUPS) * DIM));
+        if (s0 + i * GROUPS < parts) y[i] = __ldcg(reinterpret_cast<const float4*>(a.part + row_of(s0 + i * GROUPS) * DIM + d0));
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (s0 + i * GROUPS < parts) add(y[i], s_w[s0 + i * GROUPS]);
@@ -602,24 +704,19 @@ cache_attention_join_kernel(AttendParams a) {
     for (int i = 0; i < GROUPS - 1; ++i) add(s_x[i][tid], 1.f);
   } else {
     float top = -INFINITY;
-    float2 v[FEW_SPLITS];
-    float4 y[FEW_SPLITS];
-#pragma unroll
-    for (int i = 0; i < FEW_SPLITS; ++i) {
-      v[i] = i < parts ? __ldcg(ml + i) : make_float2(-INFINITY, 0.f);
-      if (i < parts) y[i] = __ldcg(reinterpret_cast<const float4*>(part + (size_t)i * DIM));
-      top = fmaxf(top, v[i].x);
-    }
-#pragma unroll
-    for (int i = 0; i < FEW_SPLITS; ++i) {
-      if (i >= parts || v[i].y == 0.f) continue;
-      const float f = v[i].x == top ? 1.f : ex2(v[i].x - top);
-      sum = fmaf(v[i].y, f, sum);
-      add(y[i], f);
+    for (int i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(ml + row_of(i)).x);
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) {
+      const float2 v = __ldcg(ml + row_of(i));
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part + row_of(i) * DIM + d0));
+      if (v.y == 0.f) continue;
+      const float f = v.x == top ? 1.f : ex2(v.x - top);
+      sum = fmaf(v.y, f, sum);
+      add(y, f);
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  T* out = static_cast<T*>(a.out) + ((size_t)(o + r / group) * a.n_heads + kvh * group + r % group) * DIM + d0;
+  T* out = static_cast<T*>(a.out) + ((size_t)(work.o + r / group) * a.n_heads + kvh * group + r % group) * DIM + d0;
   if constexpr (sizeof(T) == 4) {
     *reinterpret_cast<float4*>(out) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
   } else {

@@ -123,40 +123,65 @@ cache_append_kernel(Cache c, const T* __restrict__ k, const T* __restrict__ v, s
   if (!row_tokens(c, off, len, b, M, max_new, false, status, o, n, p)) return;
   const int i = p / c.block + blockIdx.y, base = i * c.block;
   if (base >= p + n) return;
+  const int live = max(p - base, 0), end = min(p + n - base, c.block);          // tokens in front, end of the new ones
+  const T* src = (which ? v : k) + (size_t)head * dim;
+  const int per_token = dim / 8, vecs = c.block * per_token;
+  auto place = [&](int u, int& t, int& d) {                                      // token and first number of vector u; false beyond the block
+    const int e = threadIdx.x + u * blockDim.x;
+    t = e / per_token;
+    d = (e - t * per_token) * 8;
+    return e < vecs;
+  };
+  // the new tokens do not wait for the table
+  uint4 raw[VECS][sizeof(T) / 2];
+#pragma unroll
+  for (int u = 0; u < VECS; ++u) {
+    int t, d;
+    const bool in = place(u, t, d) && t >= live && t < end;
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j)
+      raw[u][j] = in ? __ldcs(reinterpret_cast<const uint4*>(src + (size_t)(o + base + t - p) * stride + d) + j) : make_uint4(0u, 0u, 0u, 0u);
+  }
   const int id = c.find(b, i);
   if (id < 0) { latch_error(status, AD_ERR_ARG); return; }
-  const int live = max(p - base, 0), end = min(p + n - base, c.block);          // tokens in front, end of the new ones
   uint8_t* codes = (which ? c.codes[1] : c.codes[0]) + ((size_t)id * c.heads + head) * c.block * dim;
   float* scale = (which ? c.scale[1] : c.scale[0]) + (size_t)id * c.heads + head;
-  const T* src = (which ? v : k) + (size_t)head * dim;
   const float old = live ? __ldcg(scale) : 1.f;
-  const int per_token = dim / 8, vecs = c.block * per_token;
-
-  float x[VECS][8], amax = 0.f;
+  if (live) {                                                                    // those in front, as they are
+#pragma unroll
+    for (int u = 0; u < VECS; ++u) {
+      int t, d;
+      if (!place(u, t, d) || t >= live) continue;
+      const uint2 w = __ldcg(reinterpret_cast<const uint2*>(codes + t * dim + d));
+      raw[u][0].x = w.x;
+      raw[u][0].y = w.y;
+    }
+  }
+  auto numbers = [&](int u, int t, float* x) {
+    if (t < live) {
+      F::decode4(raw[u][0].x, x);
+      F::decode4(raw[u][0].y, x + 4);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= old;
+    } else {
+      load8(reinterpret_cast<const T*>(raw[u]), x);
+    }
+  };
+  float amax = 0.f;
   bool nan = false;
 #pragma unroll
   for (int u = 0; u < VECS; ++u) {
-    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 8;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[u][j] = 0.f;
-    if (e < vecs && t < live) {
-      const uint2 w = __ldcg(reinterpret_cast<const uint2*>(codes + t * dim + d));
-      F::decode4(w.x, x[u]);
-      F::decode4(w.y, x[u] + 4);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[u][j] *= old;
-    } else if (e < vecs && t < end) {
-      load8(src + (size_t)(o + base + t - p) * stride + d, x[u]);
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < VECS; ++u)
+    int t, d;
+    place(u, t, d);
+    float x[8];
+    numbers(u, t, x);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float a = fabsf(x[u][j]);
-      if (a < INFINITY) amax = fmaxf(amax, a);                                  // (infinities saturate, whatever the scale)
-      else if (a != a) { nan = true; x[u][j] = 0.f; }
+      const float a = fabsf(x[j]);
+      amax = fmaxf(amax, a < INFINITY ? a : 0.f);                                // (infinities saturate, whatever the scale)
+      nan |= a != a;
     }
+  }
   if (nan) latch_error(status, AD_ERR_ARG);
   amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
   if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = amax;
@@ -165,18 +190,21 @@ cache_append_kernel(Cache c, const T* __restrict__ k, const T* __restrict__ v, s
   const float s = block_scale<F>(amax), inv = 1.f / s;                          // (both powers of two)
 #pragma unroll
   for (int u = 0; u < VECS; ++u) {
-    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 8;
-    if (e >= vecs || t >= end || (t < live && s == old)) continue;
+    int t, d;
+    if (!place(u, t, d) || t >= end || (t < live && s == old)) continue;
+    float x[8];
+    numbers(u, t, x);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[u][j] *= inv;
-    *reinterpret_cast<uint2*>(codes + t * dim + d) = make_uint2(F::encode4(x[u]), F::encode4(x[u] + 4));
+    for (int j = 0; j < 8; ++j) x[j] = x[j] == x[j] ? x[j] * inv : 0.f;
+    *reinterpret_cast<uint2*>(codes + t * dim + d) = make_uint2(F::encode4(x), F::encode4(x + 4));
   }
   if (threadIdx.x == 0) *scale = s;
 }
 
-// Reads tokens start[b] .. of row b back into k, v [M, heads, dim].  grid and block as above.
+// Reads tokens start[b] .. of row b back into k, v [M, heads, dim].  grid as above, block = max(32, block * dim / 64).
+constexpr int READ_VECS = 4;           // vectors of sixteen codes a thread holds
 template <typename T, typename F>
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(256)
 cache_read_kernel(Cache c, T* __restrict__ k, T* __restrict__ v, int dim, const int* __restrict__ off, const int* __restrict__ start, int M, int max_tokens,
                   int* status) {
   pdl_launch();
@@ -192,23 +220,28 @@ cache_read_kernel(Cache c, T* __restrict__ k, T* __restrict__ v, int dim, const 
   const uint8_t* codes = (which ? c.codes[1] : c.codes[0]) + ((size_t)id * c.heads + head) * c.block * dim;
   const float s = __ldcg((which ? c.scale[1] : c.scale[0]) + (size_t)id * c.heads + head);
   T* dst = (which ? v : k) + (size_t)head * dim;
-  const int per_token = dim / 8, vecs = c.block * per_token;
-  uint2 w[VECS];
+  const int per_token = dim / 16, vecs = c.block * per_token;
+  uint4 w[READ_VECS];
 #pragma unroll
-  for (int u = 0; u < VECS; ++u) {
-    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 8;
-    if (e < vecs && t >= from && t < end) w[u] = __ldcg(reinterpret_cast<const uint2*>(codes + t * dim + d));
+  for (int u = 0; u < READ_VECS; ++u) {
+    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 16;
+    if (e < vecs && t >= from && t < end) w[u] = __ldcg(reinterpret_cast<const uint4*>(codes + t * dim + d));
   }
 #pragma unroll
-  for (int u = 0; u < VECS; ++u) {
-    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 8;
+  for (int u = 0; u < READ_VECS; ++u) {
+    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 16;
     if (e >= vecs || t < from || t >= end) continue;
-    float x[8];
-    F::decode4(w[u].x, x);
-    F::decode4(w[u].y, x + 4);
+    const uint32_t words[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+    T* to = dst + (size_t)(o + base + t - p) * c.heads * dim + d;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= s;
-    store8(dst + (size_t)(o + base + t - p) * c.heads * dim + d, x);
+    for (int h = 0; h < 2; ++h) {
+      float x[8];
+      F::decode4(words[2 * h], x);
+      F::decode4(words[2 * h + 1], x + 4);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= s;
+      store8(to + 8 * h, x);
+    }
   }
 }
 

@@ -131,3 +131,33 @@ int main() {
     subprocess.run([NVCC, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+@pytest.mark.skipif(not os.path.exists(NVCC), reason="no CUDA compiler")
+def test_shares_of_work_cover_it_once(tmp_path):
+    """The attention's CTAs share granules of work evenly and in order; the join finds by arithmetic which of them had a part of an item."""
+    src = tmp_path / "shares.cu"
+    src.write_text("""
+#include <stdio.h>
+#include "cache_attention.cuh"
+using namespace ad;
+#define CHECK(x) do { if (!(x)) { printf("line %d: %s (%lld granules, %lld CTAs)\\n", __LINE__, #x, total, ctas); return 1; } } while (0)
+int main() {
+  const long long totals[] = {1, 2, 3, 7, 64, 147, 148, 149, 443, 444, 445, 1000, 12501, 1ll << 33, (1ll << 40) + 17};
+  for (long long total : totals)
+    for (long long grid = 1; grid <= 900; grid += 1 + grid / 7) {
+      const long long ctas = grid < total ? grid : total;
+      CHECK(kv::cta_start(total, 0, ctas) == 0 && kv::cta_start(total, ctas, ctas) == total);
+      for (long long c = 0; c < ctas; ++c) {
+        const long long a = kv::cta_start(total, c, ctas), e = kv::cta_start(total, c + 1, ctas);
+        CHECK(a < e && e - a <= (total + ctas - 1) / ctas);
+        CHECK(kv::cta_of(total, a, ctas) == c && kv::cta_of(total, e - 1, ctas) == c && kv::cta_of(total, a + (e - a) / 2, ctas) == c);
+      }
+    }
+  return 0;
+}
+""")
+    exe = tmp_path / "shares"
+    subprocess.run([NVCC, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout
