@@ -6,7 +6,7 @@
 
 #include <type_traits>
 
-#include "kv_cache.cuh"      // load8
+#include "kv_cache.cuh"      // ex2
 
 namespace ad {
 namespace sampled {
@@ -37,7 +37,7 @@ __device__ __forceinline__ float reference(float top, float c) { return isinf(to
 
 __device__ __forceinline__ void join(Stat& a, const Stat& b, float c) {
   const float top = fmaxf(a.top, b.top), ref = reference(top, c);
-  a.sum = a.sum * exp2f(reference(a.top, c) - ref) + b.sum * exp2f(reference(b.top, c) - ref);
+  a.sum = a.sum * kv::ex2(reference(a.top, c) - ref) + b.sum * kv::ex2(reference(b.top, c) - ref);
   a.top = top;
 }
 
@@ -46,7 +46,7 @@ __device__ __forceinline__ void join(Stat& a, const Stat& b, float c) {
 template <typename T>
 __global__ void __launch_bounds__(STAT_THREADS)
 score_stats_kernel(Params p) {
-  constexpr int W = 16 / sizeof(T);                       // scores in a vector
+  constexpr int W = 16 / sizeof(T), UNDER_WAY = 4;        // scores in a vector; vectors a thread has under way
   __shared__ Stat s_part[STAT_THREADS / 32];
   pdl_launch();
   pdl_wait();
@@ -61,26 +61,34 @@ score_stats_kernel(Params p) {
 #pragma unroll
     for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
     const float ref = reference(top, p.c);
-    s.sum *= exp2f(reference(s.top, p.c) - ref);
+    s.sum *= kv::ex2(reference(s.top, p.c) - ref);
     s.top = top;
 #pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = exp2f(fmaf(x[j], p.c, -ref));
+    for (int j = 0; j < N; ++j) x[j] = kv::ex2(fmaf(x[j], p.c, -ref));
 #pragma unroll
-    for (int w = N / 2; w; w >>= 1)                       // (pairs first: a thread's sum is a chain of as many additions as it has vectors)
+    for (int w = N / 2; w; w >>= 1)                       // (pairs first: a thread's sum is a chain of as many additions as it has rounds)
 #pragma unroll
       for (int j = 0; j < w; ++j) x[j] += x[j + w];
     s.sum += x[0];
   };
   typedef std::integral_constant<int, 1> One;
-  for (int v = v0 + threadIdx.x; v < v1; v += STAT_THREADS) {
-    float x[8];
-    if constexpr (sizeof(T) == 2) {
-      kv::load8(row + head + (size_t)v * W, x);
-    } else {
-      const float4 f = *reinterpret_cast<const float4*>(row + head + (size_t)v * W);
-      x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+  for (int v = v0 + threadIdx.x; v < v1; v += UNDER_WAY * STAT_THREADS) {
+    uint4 raw[UNDER_WAY];
+#pragma unroll
+    for (int u = 0; u < UNDER_WAY; ++u)
+      if (v + u * STAT_THREADS < v1) raw[u] = __ldcg(reinterpret_cast<const uint4*>(row + head) + v + u * STAT_THREADS);
+    float x[UNDER_WAY * W];
+#pragma unroll
+    for (int u = 0; u < UNDER_WAY; ++u) {
+      const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+      const bool in = v + u * STAT_THREADS < v1;
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const uint32_t bits = sizeof(T) == 4 ? w[j % 4] : j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16;
+        x[u * W + j] = in ? __uint_as_float(bits) : -INFINITY;
+      }
     }
-    add(x, std::integral_constant<int, W>());
+    add(x, std::integral_constant<int, UNDER_WAY * W>());
   }
   if (blockIdx.y == 0) {
     const int i = threadIdx.x;
@@ -104,30 +112,58 @@ enum Decision { KEEP = 0, STOP = 1, NEAR = 2, DROP = 3 };     // STOP: kept, and
 
 namespace cg = cooperative_groups;
 
+// exp(y), y <= 0, to the last bits of FP64: y = k ln2 / 64 + f, exp(y) = 2^(k / 64) exp(f), the first from a table of 2^(j / 64) and the exponent, the
+// second from its Taylor series up to f^5 (f^6 / 720 < 4e-17), the table-driven scheme of Tang (1989).  A third of the FP64 operations of exp(), and these bound
+// the kernel.
+constexpr int EXP_TABLE = 64;
+__device__ __forceinline__ double exp_below(double y, const double* table) {
+  y = fmax(y, -746.0);
+  const double ROUND = 6755399441055744.0;                                  // 1.5 * 2^52: the sum's low word is k
+  const double kd = fma(y, 64.0 / 0.693147180559945309417, ROUND);
+  const int k = __double2loint(kd);
+  const double kr = kd - ROUND;
+  const double f = fma(kr, -2.3190468138462996e-17 / 64.0, fma(kr, -0.69314718055994530942 / 64.0, y));     // ln 2 as a double, and the rest of it
+  double e = fma(f, 1.0 / 120.0, 1.0 / 24.0);
+  e = fma(f, e, 1.0 / 6.0);
+  e = fma(f, e, 0.5);
+  e = fma(f, e, 1.0);
+  e = fma(f, e, 1.0) * table[k & (EXP_TABLE - 1)];
+  const int n = k >> 6, h = n >> 1;                                          // (in two steps: the result may be subnormal)
+  return e * __hiloint2double((h + 1023) << 20, 0) * __hiloint2double((n - h + 1023) << 20, 0);
+}
+
 // Exchange between the CTAs of a cluster, one slot per CTA.
 constexpr int MAX_CLUSTER = 8;
 struct Exchange {
-  double sum[2][MAX_CLUSTER];       // (two, taken in turn)
+  double sum[2][2][MAX_CLUSTER];    // (two sets, taken in turn)
   int pick[2][MAX_CLUSTER];         // [lowest hit, highest token with weight]
 };
+constexpr int AT_ONCE = 8;          // scores under way per thread and row
 
 // The decision for one row, by one cluster.
 //   Position i keeps its draft d while u_i q_i(d) < p_i(d).  The first one that does not gets the token at which the running sum of
 //   max(p_i - q_i, 0), in the order of ids, passes r times its total, and is the last (n = i + 1); without a draft the sum is p_i's own.
 // A token that is drawn depends on sums over the vocabulary to the last bit near a border, and a decision on a comparison; both have to come out as
 // the formula says and alike for every way of adding up.  So decisions are taken from the 32-bit sums of score_stats_kernel only where these leave no
-// doubt, and else, like the draw, from sums in 64 bits over the one position's scores, which are still in L2.
+// doubt, and else, like the draw, from sums in 64 bits over the one position's scores, which are still in L2.  With weights w = exp((score - top) / T)
+// and their sums z, p and q enter as w_p z_q and w_q z_p, multiples of the probabilities that need no division.
+// Bound by latency: decisions, one sweep over the position's scores and three exchanges in a row.  KEPT: the weights of the sweep stay in shared memory
+// for the sum and the draw, else they are computed again.
 // grid = B clusters of CTAs that share the vocabulary, block = ACCEPT_THREADS.  Every CTA of a cluster takes the same decisions from the same numbers.
-template <typename T>
+// Dynamic shared memory: KEPT, a double per score of the CTA's share, of one or two rows.
+template <typename T, bool KEPT>
 __global__ void __launch_bounds__(ACCEPT_THREADS)
 accept_sampled_kernel(Params p) {
-  __shared__ int s_first[2];
-  __shared__ double s_warp[ACCEPT_THREADS / 32];
-  __shared__ int s_pick[2];
+  constexpr int WARPS = ACCEPT_THREADS / 32;
+  extern __shared__ double s_weight[];
+  __shared__ double s_table[EXP_TABLE], s_warp[2][WARPS];
+  __shared__ int s_first[1], s_pick[2];
+  __shared__ float s_top[2];
   __shared__ Exchange s_ex;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = cluster.block_rank(), size = cluster.num_blocks(), b = blockIdx.x / size, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_launch();
+  if (tid < EXP_TABLE) s_table[tid] = exp2(tid / (double)EXP_TABLE);
   pdl_wait();
   const int o = __ldcg(p.off + b);
   const long long n_tokens = (long long)__ldcg(p.off + b + 1) - o;
@@ -142,7 +178,9 @@ accept_sampled_kernel(Params p) {
     }
     return;
   }
-  cluster.sync();                                           // (another CTA's shared memory may be written once that CTA runs)
+  cluster.barrier_arrive();                                 // (another CTA's shared memory may be written once that CTA runs)
+  bool met = false;
+  const bool two = p.score[1] != nullptr;
   const T* prow = static_cast<const T*>(p.score[0]) + (size_t)o * p.stride[0];
   const T* qrow = static_cast<const T*>(p.score[1]) + (size_t)o * p.stride[1];
   auto draft_at = [&](int i) {
@@ -150,153 +188,188 @@ accept_sampled_kernel(Params p) {
     return d < p.vocab ? d : -1;
   };
 
-  // ---- the scores' weights in 64 bits: exp((score - top) / temperature), 1 at the top (even where it is infinite), 0 for a NaN ----
+  // ---- a score's weight: 1 at the top (even where it is infinite), 0 for a NaN and where there is no top ----
   auto weight = [&](float x, float top) {
-    if (x == top) return 1.0;
-    const double e = exp(((double)x - (double)top) * p.inv_t);
-    return e >= 0.0 && !isinf(top) ? e : 0.0;
+    if (x == top) return top == -INFINITY ? 0.0 : 1.0;
+    return x < top && !isinf(top) ? exp_below(((double)x - (double)top) * p.inv_t, s_table) : 0.0;
   };
   auto row_stat = [&](int z, int i) {
+    constexpr int PARTS = 16;                               // under way at once
     Stat s = {-INFINITY, 0.f};
-    const Stat* part = p.stats + ((size_t)z * p.M + o + i) * p.parts;
-    for (int j = 0; j < p.parts; ++j) {
-      Stat t;
-      t.top = __ldcg(&part[j].top); t.sum = __ldcg(&part[j].sum);
-      join(s, t, p.c);
+    const float2* part = reinterpret_cast<const float2*>(p.stats + ((size_t)z * p.M + o + i) * p.parts);
+    for (int j0 = 0; j0 < p.parts; j0 += PARTS) {
+      float2 t[PARTS];
+#pragma unroll
+      for (int j = 0; j < PARTS; ++j) t[j] = j0 + j < p.parts ? __ldcg(part + j0 + j) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int j = 0; j < PARTS; ++j)
+        if (j0 + j < p.parts) join(s, Stat{t[j].x, t[j].y}, p.c);
     }
     return s;
   };
 
   // ---- a position's decision from the 32-bit sums ----
+  float my_top[2] = {0.f, 0.f};
   auto decide = [&](int i) -> int {
     const int d = draft_at(i);
+    const float xp = d < 0 ? 0.f : to_f32(prow[(size_t)i * p.stride[0] + d]), xq = two && d >= 0 ? to_f32(qrow[(size_t)i * p.stride[1] + d]) : 0.f;
+    const Stat sp = row_stat(0, i), sq = two ? row_stat(1, i) : Stat{0.f, 1.f};
+    my_top[0] = sp.top;
+    my_top[1] = sq.top;
     if (d < 0) return DROP;
-    const Stat sp = row_stat(0, i), sq = p.score[1] ? row_stat(1, i) : Stat{0.f, 1.f};
     if (!isfinite(sp.top) || !isfinite(sp.sum) || !isfinite(sq.top) || !isfinite(sq.sum)) return NEAR;
-    const float xp = to_f32(prow[(size_t)i * p.stride[0] + d]), xq = p.score[1] ? to_f32(qrow[(size_t)i * p.stride[1] + d]) : 0.f;
     if (xp != xp || xq != xq) return NEAR;
-    const double qd = p.score[1] ? exp2((double)xq * p.c - reference(sq.top, p.c)) : 1.0;
+    const double qd = two ? exp2((double)xq * p.c - reference(sq.top, p.c)) : 1.0;
     const double want = (double)__ldg(p.u + (size_t)b * p.kmax + i) * qd * (double)sp.sum;
     const double have = exp2((double)xp * p.c - reference(sp.top, p.c)) * (double)sq.sum;
     // How far off the two may be, relatively.  A sum: chains of at most 128 additions in all, 2^-24 each, an exponential within 2^-21 of what its
     // rounded exponent asks for; 1.6e-5 for both sums.  The exponents' factor c is off by 2^-24 of itself, which moves a probability by that share
     // of its distance from the top and of the mean distance (below 64 where it counts: what lies further off has no weight).
-    const double away = (isinf(xp) ? 0.0 : (double)(sp.top - xp)) + (p.score[1] && !isinf(xq) ? (double)(sq.top - xq) : 0.0);
+    const double away = (isinf(xp) ? 0.0 : (double)(sp.top - xp)) + (two && !isinf(xq) ? (double)(sq.top - xq) : 0.0);
     const double doubt = 3e-5 + 1.2e-7 * away * p.c;
     if (fabs(want - have) <= doubt * fmax(fabs(want), have)) return NEAR;
     return want < have ? (d == p.eos ? STOP : KEEP) : DROP;
   };
 
-  int first = -1, how = KEEP, from = 0;      // the first position that does not simply keep its draft
-  double zp = 0.0, zq = 0.0;
-  Stat sp = {0.f, 1.f}, sq = {0.f, 1.f};
+  // ---- sums over the cluster in the order of its threads: of x (in front of this thread's, and all), and of y (all) ----
   int turn = 0;
-  // sum of a value over the cluster, in the order of its threads: in front of this thread's, and all of it
-  auto cluster_sum = [&](double x, double& before, double& all) {
+  auto cluster_sums = [&](double x, double y, double& before, double& all_x, double& all_y) {
     double run = x;
 #pragma unroll
     for (int w = 1; w < 32; w <<= 1) {
-      const double y = __shfl_up_sync(0xffffffffu, run, w);
-      if (lane >= w) run += y;
+      const double v = __shfl_up_sync(0xffffffffu, run, w);
+      if (lane >= w) run += v;
+      y += __shfl_xor_sync(0xffffffffu, y, w);
     }
     __syncthreads();
-    if (lane == 31) s_warp[warp] = run;
+    if (lane == 31) { s_warp[0][warp] = run; s_warp[1][warp] = y; }
     __syncthreads();
-    double mine = 0.0, front = 0.0;
-    for (int w = 0; w < ACCEPT_THREADS / 32; ++w) {
+    double mine = 0.0, front = 0.0, mine_y = 0.0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
       if (w == warp) front = mine;
-      mine += s_warp[w];
+      mine += s_warp[0][w];
+      mine_y += s_warp[1][w];
     }
     const int slot = turn & 1;
-    if (tid < size) cluster.map_shared_rank(&s_ex, tid)->sum[slot][rank] = mine;
+    if (!met) { cluster.barrier_wait(); met = true; }
+    if (tid < 2 * size) cluster.map_shared_rank(&s_ex, tid >> 1)->sum[slot][tid & 1][rank] = tid & 1 ? mine_y : mine;
     cluster.sync();
     double ahead = 0.0;
-    all = 0.0;
+    all_x = all_y = 0.0;
     for (int j = 0; j < size; ++j) {
-      if (j == rank) ahead = all;
-      all += s_ex.sum[slot][j];
+      if (j == rank) ahead = all_x;
+      all_x += s_ex.sum[slot][0][j];
+      all_y += s_ex.sum[slot][1][j];
     }
     before = ahead + front + (run - x);
     ++turn;
   };
+  // this thread's share of the vocabulary
   const int each = (p.vocab + size * ACCEPT_THREADS - 1) / (size * ACCEPT_THREADS);
   const int v0 = min((rank * ACCEPT_THREADS + tid) * each, p.vocab), v1 = min(v0 + each, p.vocab);
-  for (;;) {
-    if (tid == 0) s_first[0] = k;
-    __syncthreads();
-    for (int i = from + tid; i < k; i += ACCEPT_THREADS)
-      if (decide(i) != KEEP) { atomicMin(&s_first[0], i); break; }              // (an integer minimum: no order in it)
-    __syncthreads();
-    first = s_first[0];
-    if (first == k) { how = KEEP; break; }
-    if (tid == 0) s_first[1] = decide(first);
-    __syncthreads();
-    how = s_first[1];
-    if (how == STOP) break;
-    // the position's sums in 64 bits
-    sp = row_stat(0, first);
-    sq = p.score[1] ? row_stat(1, first) : Stat{0.f, 1.f};
-    const T* pr = prow + (size_t)first * p.stride[0];
-    const T* qr = qrow + (size_t)first * p.stride[1];
-    double a = 0.0, c = 0.0, unused;
-    for (int v = v0; v < v1; ++v) {
-      a += weight(to_f32(pr[v]), sp.top);
-      if (p.score[1]) c += weight(to_f32(qr[v]), sq.top);
+  // calls f(v, weight of the verifier's score v, of the drafter's) over it
+  auto sweep = [&](const T* pr, const T* qr, float ptop, float qtop, auto f) {
+    for (int e0 = v0; e0 < v1; e0 += AT_ONCE) {
+      float xp[AT_ONCE], xq[AT_ONCE];
+#pragma unroll
+      for (int e = 0; e < AT_ONCE; ++e) {
+        xp[e] = e0 + e < v1 ? to_f32(pr[e0 + e]) : 0.f;
+        xq[e] = two && e0 + e < v1 ? to_f32(qr[e0 + e]) : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < AT_ONCE; ++e)
+        if (e0 + e < v1) f(e0 + e, weight(xp[e], ptop), two ? weight(xq[e], qtop) : 0.0);
     }
-    cluster_sum(a, unused, zp);
-    if (p.score[1] && sq.top > -INFINITY) cluster_sum(c, unused, zq); else zq = 1.0;
+  };
+  auto kept = [&](int z, int v) -> double& { return s_weight[(size_t)(z * each + v - v0) * ACCEPT_THREADS + tid]; };
+
+  int first = -1, how = KEEP, from = 0;      // the first position that does not simply keep its draft
+  double zp = 0.0, zq = 1.0;
+  float ptop = 0.f, qtop = 0.f;
+  const T *pr = prow, *qr = qrow;
+  for (;;) {
+    if (tid == 0) s_first[0] = INT_MAX;
+    __syncthreads();
+    int mine_first = -1;
+    for (int i = from + tid; i < k; i += ACCEPT_THREADS) {
+      const int h = decide(i);
+      if (h != KEEP) { mine_first = 4 * i + h; atomicMin(&s_first[0], mine_first); break; }              // (an integer minimum: no order in it)
+    }
+    __syncthreads();
+    if (mine_first == s_first[0]) { s_top[0] = my_top[0]; s_top[1] = my_top[1]; }
+    __syncthreads();
+    first = s_first[0] == INT_MAX ? k : s_first[0] >> 2;
+    how = s_first[0] == INT_MAX ? KEEP : s_first[0] & 3;
+    if (how == KEEP || how == STOP) break;
+    // the position's sums in 64 bits
+    ptop = s_top[0];
+    qtop = s_top[1];
+    pr = prow + (size_t)first * p.stride[0];
+    qr = qrow + (size_t)first * p.stride[1];
+    double a = 0.0, c = 0.0, unused;
+    sweep(pr, qr, ptop, qtop, [&](int v, double wp, double wq) {
+      a += wp;
+      c += wq;
+      if (KEPT) {
+        kept(0, v) = wp;
+        if (two) kept(1, v) = wq;
+      }
+    });
+    cluster_sums(a, c, unused, zp, zq);
+    if (!two || !(zq > 0.0)) zq = 1.0;                      // (no drafter, or one without a distribution: its weights are 0)
     if (how == DROP) break;
     const int d = draft_at(first);
-    const double pd = sp.top > -INFINITY ? weight(to_f32(pr[d]), sp.top) : 0.0;
-    const double qd = !p.score[1] ? 1.0 : sq.top > -INFINITY ? weight(to_f32(qr[d]), sq.top) : 0.0;
-    if ((double)__ldg(p.u + (size_t)b * p.kmax + first) * qd * zp < pd * zq) {
-      if (d == p.eos) { how = STOP; break; }
-      from = first + 1;
-      if (from == k) { first = k; how = KEEP; break; }
-    } else {
-      how = DROP;
-      break;
-    }
+    const double pd = weight(to_f32(pr[d]), ptop), qd = two ? weight(to_f32(qr[d]), qtop) : 1.0;
+    if (!((double)__ldg(p.u + (size_t)b * p.kmax + first) * qd * zp < pd * zq)) { how = DROP; break; }
+    if (d == p.eos) { how = STOP; break; }
+    from = first + 1;
+    __syncthreads();
+    if (from == k) { first = k; how = KEEP; break; }
   }
 
   // ---- the token of the first position that does not keep its draft ----
   int token = 0;
   if (how == DROP) {
-    const T* pr = prow + (size_t)first * p.stride[0];
-    const T* qr = qrow + (size_t)first * p.stride[1];
     const int d = draft_at(first);
     const double r = (double)__ldg(p.r + b);
     for (int form = d < 0 ? 1 : 0; form < 2; ++form) {      // 0: what the verifier gives beyond the drafter; 1: the verifier's own
-      auto left = [&](int v) {
-        if (sp.top == -INFINITY) return 0.0;
-        const double pv = weight(to_f32(pr[v]), sp.top) / zp;
-        if (form == 1) return pv;
-        if (!p.score[1]) return v == d ? 0.0 : pv;
-        return sq.top == -INFINITY ? pv : fmax(pv - weight(to_f32(qr[v]), sq.top) / zq, 0.0);
+      auto left = [&](int v, double wp, double wq) {
+        if (form == 1) return wp;
+        if (!two) return v == d ? 0.0 : wp;
+        return fmax(wp * zq - wq * zp, 0.0);
       };
-      double mine = 0.0, before, all;
+      auto over = [&](auto f) {                             // f(v, what is left of v)
+        if constexpr (KEPT) {
+          for (int v = v0; v < v1; ++v) f(v, left(v, kept(0, v), two ? kept(1, v) : 0.0));
+        } else {
+          sweep(pr, qr, ptop, qtop, [&](int v, double wp, double wq) { f(v, left(v, wp, wq)); });
+        }
+      };
+      double mine = 0.0, before, all, unused;
       int last = -1;
-      for (int v = v0; v < v1; ++v) {
-        const double x = left(v);
+      over([&](int v, double x) {
         mine += x;
         if (x > 0.0) last = v;
-      }
-      cluster_sum(mine, before, all);
+      });
+      if (tid == 0) { s_pick[0] = INT_MAX; s_pick[1] = -1; }
+      cluster_sums(mine, 0.0, before, all, unused);
       if (form == 0 && !(all > 0.0)) continue;              // (nothing beyond the drafter's: the verifier's own)
       int hit = INT_MAX;
       const double goal = r * all;
       if (before + mine > goal) {
         double run = before;
-        for (int v = v0; v < v1; ++v) {
-          const double x = left(v);
+        over([&](int v, double x) {
           run += x;
-          if (x > 0.0 && run > goal) { hit = v; break; }
-        }
+          if (x > 0.0 && run > goal) hit = min(hit, v);
+        });
       }
-      if (tid == 0) { s_pick[0] = INT_MAX; s_pick[1] = -1; }
-      __syncthreads();
-      atomicMin(&s_pick[0], hit);
-      atomicMax(&s_pick[1], last);
+      hit = __reduce_min_sync(0xffffffffu, hit);
+      last = __reduce_max_sync(0xffffffffu, last);
+      if (lane == 0) {
+        atomicMin(&s_pick[0], hit);
+        atomicMax(&s_pick[1], last);
+      }
       __syncthreads();
       if (tid < 2) cluster.map_shared_rank(&s_ex, 0)->pick[tid][rank] = s_pick[tid];
       cluster.sync();
@@ -308,6 +381,7 @@ accept_sampled_kernel(Params p) {
       break;
     }
   }
+  if (!met) cluster.barrier_wait();
   if (rank == 0) {
     const int n = first == k ? k : first + 1;
     if (tid == 0) p.n_acc[b] = n;

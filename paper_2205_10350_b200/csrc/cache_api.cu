@@ -209,6 +209,31 @@ int score_parts(int32_t rows, int32_t vocab) {
 }
 }  // namespace
 
+namespace {
+// Weights stay in shared memory while there is room for them: up to 53000 ids with a drafter, 106000 without (half of that in batches of many rows).
+constexpr size_t kKeptMax = 208 * 1024;
+template <typename T, bool KEPT>
+cudaError_t launch_accept_kept(const sampled::Params& p, int cluster, size_t smem, cudaStream_t st) {
+  static std::atomic<uint64_t> raised{0};
+  auto kernel = sampled::accept_sampled_kernel<T, KEPT>;
+  const uint64_t bit = 1ull << op_device();
+  if (KEPT && !(raised.load(std::memory_order_relaxed) & bit)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kKeptMax);
+    if (e != cudaSuccess) return e;
+    raised.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return launch_op(kernel, dim3(p.B * cluster), dim3(sampled::ACCEPT_THREADS), dim3(cluster), KEPT ? smem : 0, st, p);
+}
+template <typename T>
+cudaError_t launch_accept(const sampled::Params& p, cudaStream_t st) {
+  // (a CTA an SM: more rows share fewer CTAs each rather than wait for one another)
+  const int cluster = p.vocab <= 2048 ? 1 : p.B * sampled::MAX_CLUSTER <= op_num_sms() ? sampled::MAX_CLUSTER : 4;
+  const size_t each = (p.vocab + cluster * sampled::ACCEPT_THREADS - 1) / (cluster * sampled::ACCEPT_THREADS);
+  const size_t smem = each * sampled::ACCEPT_THREADS * (p.score[1] ? 2 : 1) * sizeof(double);
+  return smem <= kKeptMax ? launch_accept_kept<T, true>(p, cluster, smem, st) : launch_accept_kept<T, false>(p, cluster, smem, st);
+}
+}  // namespace
+
 extern "C" size_t ad_accept_sampled_scratch_bytes(int32_t M, int32_t vocab, int32_t with_draft) {
   if (M < 0 || M > INT_MAX / 2 || vocab < 1 || vocab > (1 << 24)) return 0;
   const int z = with_draft ? 2 : 1;
@@ -240,9 +265,6 @@ extern "C" int ad_accept_sampled(const void* target, int64_t target_stride, cons
   if (M > 0)
     e = launch_op(dtype == AD_DTYPE_BF16 ? sampled::score_stats_kernel<bf16> : sampled::score_stats_kernel<float>, dim3(M, p.parts, z),
                   dim3(sampled::STAT_THREADS), dim3(), 0, st, p);
-  const int cluster = vocab > 4096 ? sampled::MAX_CLUSTER : 1;
-  if (e == cudaSuccess)
-    e = launch_op(dtype == AD_DTYPE_BF16 ? sampled::accept_sampled_kernel<bf16> : sampled::accept_sampled_kernel<float>, dim3(B * cluster),
-                  dim3(sampled::ACCEPT_THREADS), dim3(cluster), 0, st, p);
+  if (e == cudaSuccess) e = dtype == AD_DTYPE_BF16 ? launch_accept<bf16>(p, st) : launch_accept<float>(p, st);
   return launched(entry, e);
 }

@@ -61,12 +61,6 @@ __host__ __device__ __forceinline__ long long cta_start(long long total, long lo
 // The CTA that granule g falls to.
 __host__ __device__ __forceinline__ int cta_of(long long total, long long g, long long ctas) { return (int)(((g + 1) * ctas - 1) / total); }
 
-// 2^x to 2^-22 of itself; 0 for -inf.
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // log2 x: the exponent as it is, which is all there is to a power of two, and the mantissa's to 2^-22.
 __device__ __forceinline__ float lg2(float x) {
   const uint32_t w = __float_as_uint(x);

@@ -80,6 +80,13 @@ __device__ __forceinline__ bool row_tokens(const Cache& c, const int* off, const
   return fault == AD_OK;
 }
 
+// 2^x to 2^-22 of itself; 0 for -inf.
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Eight consecutive numbers of FP32 or BF16.
 __device__ __forceinline__ void load8(const float* p, float* x) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
