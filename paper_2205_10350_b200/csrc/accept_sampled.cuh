@@ -4,8 +4,6 @@
 #include <cooperative_groups.h>
 #include <math.h>
 
-#include <type_traits>
-
 #include "kv_cache.cuh"      // ex2
 
 namespace ad {
@@ -46,65 +44,79 @@ __device__ __forceinline__ void join(Stat& a, const Stat& b, float c) {
 template <typename T>
 __global__ void __launch_bounds__(STAT_THREADS)
 score_stats_kernel(Params p) {
-  constexpr int W = 16 / sizeof(T), UNDER_WAY = 4;        // scores in a vector; vectors a thread has under way
-  __shared__ Stat s_part[STAT_THREADS / 32];
+  constexpr int W = 16 / sizeof(T), VECS = 2, N = VECS * W;      // scores in a vector; vectors of a round, the next of which is under way
+  constexpr uint32_t NOTHING = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;      // -inf
+  __shared__ float s_top[STAT_THREADS / 32], s_sum[STAT_THREADS / 32];
   pdl_launch();
   pdl_wait();
   const T* row = static_cast<const T*>(p.score[blockIdx.z]) + blockIdx.x * p.stride[blockIdx.z];
   const int head = min((int)((16 - reinterpret_cast<uintptr_t>(row) % 16) % 16 / sizeof(T)), p.vocab);
   const int vecs = (p.vocab - head) / W, tail = head + vecs * W;
   const int each = (vecs + p.parts - 1) / p.parts, v0 = min((int)blockIdx.y * each, vecs), v1 = min(v0 + each, vecs);
-  Stat s = {-INFINITY, 0.f};
-  auto add = [&](float* x, auto count) {
-    constexpr int N = decltype(count)::value;
-    float top = s.top;
-#pragma unroll
-    for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
-    const float ref = reference(top, p.c);
-    s.sum *= kv::ex2(reference(s.top, p.c) - ref);
-    s.top = top;
-#pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = kv::ex2(fmaf(x[j], p.c, -ref));
-#pragma unroll
-    for (int w = N / 2; w; w >>= 1)                       // (pairs first: a thread's sum is a chain of as many additions as it has rounds)
-#pragma unroll
-      for (int j = 0; j < w; ++j) x[j] += x[j + w];
-    s.sum += x[0];
+  const uint4* body = reinterpret_cast<const uint4*>(row + head);
+  float top = -INFINITY, sum = 0.f;
+  auto rebase = [&](float t) {                            // returns what exponents are taken against from here on
+    const float ref = reference(t, p.c);
+    sum *= kv::ex2(reference(top, p.c) - ref);
+    top = t;
+    return ref;
   };
-  typedef std::integral_constant<int, 1> One;
-  for (int v = v0 + threadIdx.x; v < v1; v += UNDER_WAY * STAT_THREADS) {
-    uint4 raw[UNDER_WAY];
+  auto load = [&](uint4* raw, int v) {
 #pragma unroll
-    for (int u = 0; u < UNDER_WAY; ++u)
-      if (v + u * STAT_THREADS < v1) raw[u] = __ldcg(reinterpret_cast<const uint4*>(row + head) + v + u * STAT_THREADS);
-    float x[UNDER_WAY * W];
+    for (int u = 0; u < VECS; ++u)
+      raw[u] = v + u * STAT_THREADS < v1 ? __ldcs(body + v + u * STAT_THREADS) : make_uint4(NOTHING, NOTHING, NOTHING, NOTHING);
+  };
+  uint4 next[VECS];
+  load(next, v0 + threadIdx.x);
+  for (int v = v0 + threadIdx.x; v < v1; v += VECS * STAT_THREADS) {
+    float x[N];
 #pragma unroll
-    for (int u = 0; u < UNDER_WAY; ++u) {
-      const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-      const bool in = v + u * STAT_THREADS < v1;
+    for (int u = 0; u < VECS; ++u) {
+      const uint32_t w[4] = {next[u].x, next[u].y, next[u].z, next[u].w};
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const uint32_t bits = sizeof(T) == 4 ? w[j % 4] : j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16;
-        x[u * W + j] = in ? __uint_as_float(bits) : -INFINITY;
-      }
+      for (int j = 0; j < W; ++j) x[u * W + j] = __uint_as_float(sizeof(T) == 4 ? w[j % 4] : j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
     }
-    add(x, std::integral_constant<int, UNDER_WAY * W>());
+    load(next, v + VECS * STAT_THREADS);
+    float t = top;
+#pragma unroll
+    for (int j = 0; j < N; j += 2) t = kv::max3(t, x[j], x[j + 1]);
+    const float ref = rebase(t);
+    float2 y[N / 2];
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) {
+      y[j] = kv::fma2(make_float2(x[2 * j], x[2 * j + 1]), make_float2(p.c, p.c), make_float2(-ref, -ref));
+      y[j] = make_float2(kv::ex2(y[j].x), kv::ex2(y[j].y));
+    }
+#pragma unroll
+    for (int w = N / 4; w; w >>= 1)                       // (pairs first: a thread's sum is a chain of as many additions as it has rounds)
+#pragma unroll
+      for (int j = 0; j < w; ++j) y[j] = kv::add2(y[j], y[j + w]);
+    sum += y[0].x + y[0].y;
   }
   if (blockIdx.y == 0) {
     const int i = threadIdx.x;
-    if (i < head) { float x = to_f32(row[i]); add(&x, One()); }
-    if (tail + i < p.vocab) { float x = to_f32(row[tail + i]); add(&x, One()); }      // (fewer than W left)
+    auto one = [&](float x) { const float ref = rebase(fmaxf(top, x)); sum += kv::ex2(fmaf(x, p.c, -ref)); };
+    if (i < head) one(to_f32(row[i]));
+    if (tail + i < p.vocab) one(to_f32(row[tail + i]));      // (fewer than W left)
   }
+  // the largest score of all threads, then their sums against it
+  float t = top;
 #pragma unroll
-  for (int w = 16; w; w >>= 1) {
-    Stat t = {__shfl_xor_sync(0xffffffffu, s.top, w), __shfl_xor_sync(0xffffffffu, s.sum, w)};
-    join(s, t, p.c);
-  }
-  if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = s;
+  for (int w = 16; w; w >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, w));
+  if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = t;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < STAT_THREADS / 32; ++w) t = fmaxf(t, s_top[w]);
+  rebase(t);
+#pragma unroll
+  for (int w = 16; w; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+  if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < STAT_THREADS / 32; ++w) join(s, s_part[w], p.c);
-    p.stats[((size_t)blockIdx.z * p.M + blockIdx.x) * p.parts + blockIdx.y] = s;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < STAT_THREADS / 32; ++w) sum += s_sum[w];
+    p.stats[((size_t)blockIdx.z * p.M + blockIdx.x) * p.parts + blockIdx.y] = Stat{top, sum};
   }
 }
 

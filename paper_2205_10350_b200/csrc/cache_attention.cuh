@@ -20,6 +20,7 @@ struct AttendParams {
   float scale;             // softmax scale times log2(e)
   int* status;
   int B;
+  int stream_once;         // more keys and values than L2 could hold for the next call
   int grid;                // CTAs
   int fixed;               // what an item takes besides its units, in units
   int granule;             // units that one CTA works on at the least where a row's keys are split; 0: they are not
@@ -67,30 +68,6 @@ __device__ __forceinline__ float lg2(float x) {
   float y;
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(__uint_as_float((w & 0x7fffffu) | 0x3f800000u)));
   return (float)((int)(w >> 23) - 127) + y;
-}
-// Two FP32 operations in one instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{ .reg .b64 a, b, c, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mov.b64 c, {%6, %7}; fma.rn.f32x2 d, a, b, c; mov.b64 {%0, %1}, d; }"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{ .reg .b64 a, b, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; add.rn.f32x2 d, a, b; mov.b64 {%0, %1}, d; }"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  float2 d;
-  asm("{ .reg .b64 a, b, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mul.rn.f32x2 d, a, b; mov.b64 {%0, %1}, d; }"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t w;
@@ -267,6 +244,9 @@ cache_attention_kernel(AttendParams a) {
     const uint32_t ring_s = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
     const uint32_t k_dst = ring_s + my_col * DIM + my_x * 16, k_odd = ring_s + my_col * DIM + (DIM == 128 ? my_x ^ 4 : my_x) * 16;
     const uint32_t v_dst = ring_s + UNIT * DIM + my_key * DIM + (DIM == 128 ? my_x ^ ((my_key & 3) << 1) : DIM == 64 ? my_x ^ (((my_key >> 1) & 1) << 1) : my_x) * 16;
+    uint64_t policy;
+    if (a.stream_once) asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+    else asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
     auto issue = [&](int u, int stage) {
       if (u >= u1) return;
       if (u - id_base >= 32) look_up(u);
@@ -292,8 +272,8 @@ cache_attention_kernel(AttendParams a) {
         const ptrdiff_t at = i * 512 + (TWO && i >= COPIES / 2 ? second : 0);
         const int z = TWO && i >= COPIES / 2 ? 1 : 0;
         const int n = whole || (there[z] && first + my_key + i * (512 / DIM) < vis_max) ? 16 : 0;   // zeros where there is no key
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(kd), "l"(ks + at), "r"(n) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vd), "l"(vs + at), "r"(n) : "memory");
+        asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(kd), "l"(ks + at), "r"(n), "l"(policy) : "memory");
+        asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(vd), "l"(vs + at), "r"(n), "l"(policy) : "memory");
       }
       if (lane < 4) {                                               // ks0, ks1, vs0, vs1; negative: no such block
         const int z = lane & 1;
@@ -648,11 +628,12 @@ cache_attention_join_kernel(AttendParams a) {
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, grp = tid / LANES, d0 = tid % LANES * 4;
   const int b = blockIdx.z, kvh = blockIdx.y, r = SHARED ? blockIdx.x : blockIdx.x * GROUPS + grp;
+  const long long total = __ldcg(a.prefix + a.B), in_front = __ldcg(a.prefix + b);
   const RowWork work = row_work(a, b, ROWS);
   const int group = a.n_heads / a.c.heads;
   if (work.granules == 0 || r >= work.n * group || work.pieces == 1) return;
-  const long long total = __ldcg(a.prefix + a.B), ctas = min((long long)a.grid, total);
-  const long long first = __ldcg(a.prefix + b) + ((long long)kvh * work.tiles + r / ROWS) * work.pieces;
+  const long long ctas = min((long long)a.grid, total);
+  const long long first = in_front + ((long long)kvh * work.tiles + r / ROWS) * work.pieces;
   const int c0 = cta_of(total, first, ctas), parts = cta_of(total, first + work.pieces - 1, ctas) - c0 + 1;
   if (parts == 1) return;
   // the first CTA's part is its last segment unless it starts there; the others' are their first
@@ -664,15 +645,24 @@ cache_attention_join_kernel(AttendParams a) {
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](float4 y, float f) { x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w); };
   if constexpr (SHARED) {
-    float top = -INFINITY;
-    for (int i = tid; i < parts; i += 128) top = fmaxf(top, __ldcg(ml + row_of(i)).x);
+    constexpr int AHEAD = 8;
+    auto load_parts = [&](float4* y, int s0) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (s0 + i * GROUPS < parts) y[i] = __ldcg(reinterpret_cast<const float4*>(a.part + row_of(s0 + i * GROUPS) * DIM + d0));
+    };
+    float4 y[AHEAD];
+    load_parts(y, grp);                          // (on their way while the weights are worked out)
+    float2 v = tid < parts ? __ldcg(ml + row_of(tid)) : make_float2(-INFINITY, 0.f);
+    float top = v.x;
+    for (int i = tid + 128; i < parts; i += 128) top = fmaxf(top, __ldcg(ml + row_of(i)).x);
 #pragma unroll
     for (int w = 16; w; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
     if (lane == 0) s_red[0][tid >> 5] = top;
     __syncthreads();
     top = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
     for (int i = tid; i < parts; i += 128) {
-      const float2 v = __ldcg(ml + row_of(i));
+      if (i > tid) v = __ldcg(ml + row_of(i));
       const float f = v.y == 0.f ? 0.f : v.x == top ? 1.f : ex2(v.x - top);      // (no key: nothing, whatever the maxima)
       s_w[i] = f;
       sum += v.y * f;
@@ -682,14 +672,11 @@ cache_attention_join_kernel(AttendParams a) {
     if (lane == 0) s_red[1][tid >> 5] = sum;
     __syncthreads();
     sum = (s_red[1][0] + s_red[1][1]) + (s_red[1][2] + s_red[1][3]);
-    for (int s0 = grp; s0 < parts; s0 += 8 * GROUPS) {
-      float4 y[8];
+    for (int s0 = grp; s0 < parts; s0 += AHEAD * GROUPS) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (s0 + i * GROUPS < parts) y[i] = __ldcg(reinterpret_cast<const float4*>(a.part + row_of(s0 + i * GROUPS) * DIM + d0));
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < AHEAD; ++i)
         if (s0 + i * GROUPS < parts) add(y[i], s_w[s0 + i * GROUPS]);
+      load_parts(y, s0 + AHEAD * GROUPS);
     }
     if (grp > 0) s_x[grp - 1][tid % LANES] = x;
     __syncthreads();
