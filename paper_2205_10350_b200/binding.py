@@ -448,48 +448,46 @@ def _refuse(entry, why):
     raise AdError(AD_ERR_ARG, f"{entry}: {why}")
 
 
-def _number_type(entry, t):
-    import torch
-    if t.dtype is torch.bfloat16:
-        return AD_DTYPE_BF16
-    if t.dtype is torch.float32:
-        return AD_DTYPE_FP32
-    _refuse(entry, f"{t.dtype} is neither float32 nor bfloat16")
+def _raise(lib, rc):
+    msg = lib.ad_last_error(None)
+    raise AdError(rc, msg.decode() if msg else "")
 
 
-def _index_arrays(entry, dev, *arrays):
+# Torch's names that a call needs, looked up once: an import statement and attribute lookups cost a call as much as its checks.
+_INT32 = _FP32 = _BF16 = _get_device = _get_stream = None
+
+
+def _names():
     import torch
-    for a, shape in arrays:
-        if a.dtype is not torch.int32 or a.device != dev or a.shape != shape or not a.is_contiguous():
-            _refuse(entry, f"offsets, lengths, tables and drafts are contiguous int32 tensors on {dev}; wanted {shape}, got {tuple(a.shape)}")
+    global _INT32, _FP32, _BF16, _get_device, _get_stream
+    _INT32, _FP32, _BF16 = torch.int32, torch.float32, torch.bfloat16
+    _get_device, _get_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _vector(t, n, dtype, dev):
+    """Whether t is a contiguous vector of n numbers of dtype on CUDA device number dev."""
+    return t.dtype is dtype and t.get_device() == dev and t.dim() == 1 and t.numel() == n and t.is_contiguous()
+
+
+def _matrix(t, shape, dtype, dev):
+    return t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous()
 
 
 def _status_pointer(entry, dev, status_t):
     if status_t is None:
         return None
-    _index_arrays(entry, dev, (status_t, (1,)))
+    if not _vector(status_t, 1, _INT32, dev):
+        _refuse(entry, f"the status is one int32 on device {dev}")
     return status_t.data_ptr()
 
 
-def _on_device(dev, call):
-    """call(raw stream) with dev current; the stream is torch's current one of dev."""
+def _call_on(dev, call, *args):
+    """call(*args, raw stream) with device number dev current; the stream is torch's current one of that device."""
+    if _get_device() == dev:
+        return call(*args, _get_stream(dev))
     import torch
-    if torch._C._cuda_getDevice() == dev.index:
-        return call(torch._C._cuda_getCurrentRawStream(dev.index))
     with torch.cuda.device(dev):
-        return call(torch._C._cuda_getCurrentRawStream(dev.index))
-
-
-def _scratch(like, nbytes):
-    """(tensor to keep, 256-byte aligned address) of nbytes of scratch."""
-    import torch
-    t = torch.empty(nbytes + 256, dtype=torch.uint8, device=like.device)
-    return t, (t.data_ptr() + 255) // 256 * 256
-
-
-def _raise(lib, rc):
-    msg = lib.ad_last_error(None)
-    raise AdError(rc, msg.decode() if msg else "")
+        return call(*args, _get_stream(dev))
 
 
 class KvCache:
@@ -501,6 +499,7 @@ class KvCache:
 
     def __init__(self, n_blocks, n_kv_heads, head_dim, block=32, fmt="e4m3", table=None, row_blocks=None, device="cuda:0", tensors=None):
         import torch
+        _names()
         entry = "KvCache"
         if fmt not in ("e4m3", "int8"):
             _refuse(entry, f"unknown format {fmt!r}")
@@ -516,46 +515,56 @@ class KvCache:
             codes = [torch.zeros(shape, dtype=torch.uint8, device=self.device).view(dt) for _ in range(2)]
             tensors = (*codes, *(torch.ones(shape[:2], dtype=torch.float32, device=self.device) for _ in range(2)))
         for t, want, s in zip(tensors, (dt, dt, torch.float32, torch.float32), (shape, shape, shape[:2], shape[:2])):
-            if t.dtype is not want or t.shape != s or t.device != self.device or not t.is_contiguous():
+            if not _matrix(t, s, want, self.device.index):
                 _refuse(entry, f"codes are contiguous {dt} {shape}, scales float32 {shape[:2]}, on {self.device}")
         self.k_codes, self.v_codes, self.k_scale, self.v_scale = tensors
         if row_blocks is None:
             row_blocks = table.shape[1] if table is not None else self.n_blocks
-        if table is not None:
-            _index_arrays(entry, self.device, (table, (table.shape[0], row_blocks)))
+        if table is not None and not _matrix(table, (table.shape[0], row_blocks), torch.int32, self.device.index):
+            _refuse(entry, f"the table is a contiguous int32 tensor [rows, {row_blocks}] on {self.device}")
         self.table, self.row_blocks = table, int(row_blocks)
         self.struct = KvCacheStruct(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
                                     table.data_ptr() if table is not None else None, self.row_blocks, self.n_blocks, self.n_kv_heads, self.block,
                                     self.head_dim, AD_CACHE_E4M3 if fmt == "e4m3" else AD_CACHE_INT8)
-        self._ref = C.byref(self.struct)
+        self._ref, self._dev = C.byref(self.struct), self.device.index
+        self._table_rows = table.shape[0] if table is not None else 1 << 30
+        self._scratch = {}              # sizes of a call -> bytes of scratch it needs
 
     def _batch(self, entry, off_t, len_t):
         """Rows of a batch: off_t [B + 1], len_t [B]."""
-        B = len_t.shape[0]
-        _index_arrays(entry, self.device, (off_t, (B + 1,)), (len_t, (B,)))
-        if self.table is not None and self.table.shape[0] < B:
-            _refuse(entry, f"the table has {self.table.shape[0]} rows, the batch {B}")
+        B = len_t.numel()
+        if not (_vector(len_t, B, _INT32, self._dev) and _vector(off_t, B + 1, _INT32, self._dev)):
+            _refuse(entry, f"offsets and lengths are contiguous int32 tensors [B + 1] and [B] on {self.device}, got {tuple(off_t.shape)} and {tuple(len_t.shape)}")
+        if self._table_rows < B:
+            _refuse(entry, f"the table has {self._table_rows} rows, the batch {B}")
         return B
 
     def _tokens(self, entry, t, heads):
-        """Numbers between tokens of t [M, heads, head_dim], whose heads lie next to each other."""
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.device != self.device:
+        """(type, tokens, numbers between them) of t [M, heads, head_dim], whose heads lie next to each other."""
+        dtype = AD_DTYPE_BF16 if t.dtype is _BF16 else AD_DTYPE_FP32
+        if dtype == AD_DTYPE_FP32 and t.dtype is not _FP32:
+            _refuse(entry, f"{t.dtype} is neither float32 nor bfloat16")
+        if t.dim() != 3 or t.get_device() != self._dev:
             _refuse(entry, f"wanted [tokens, {heads}, {self.head_dim}] on {self.device}, got {tuple(t.shape)} on {t.device}")
-        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.head_dim):
+        M, h, d = t.shape
+        if h != heads or d != self.head_dim:
+            _refuse(entry, f"wanted [tokens, {heads}, {self.head_dim}], got {tuple(t.shape)}")
+        between, per_head, one = t.stride()
+        if one != 1 or (per_head != d and heads > 1):
             _refuse(entry, "the numbers of a token must lie next to each other")
-        return t.stride(0) if t.shape[0] > 1 else heads * self.head_dim
+        return dtype, M, between if M > 1 else heads * d
 
 
 def cache_append(cache, k_t, v_t, off_t, len_t, max_new, status_t=None):
     """Writes k_t, v_t [M, n_kv_heads, head_dim] (float32 or bfloat16, views of a wider array as well) behind the len_t[b] tokens of every row."""
-    entry, lib = "ad_cache_append", load()
-    B, dtype = cache._batch(entry, off_t, len_t), _number_type(entry, k_t)
-    stride = cache._tokens(entry, k_t, cache.n_kv_heads)
-    if v_t.dtype != k_t.dtype or v_t.shape != k_t.shape or cache._tokens(entry, v_t, cache.n_kv_heads) != stride:
+    entry, lib = "ad_cache_append", _lib or load()
+    B = cache._batch(entry, off_t, len_t)
+    tokens = cache._tokens(entry, k_t, cache.n_kv_heads)
+    if cache._tokens(entry, v_t, cache.n_kv_heads) != tokens:
         _refuse(entry, "keys and values must agree in type, shape and stride")
-    status = _status_pointer(entry, cache.device, status_t)
-    rc = _on_device(cache.device, lambda stream: lib.ad_cache_append(
-        cache._ref, k_t.data_ptr(), v_t.data_ptr(), dtype, stride, off_t.data_ptr(), len_t.data_ptr(), B, k_t.shape[0], max_new, status, stream))
+    dtype, M, stride = tokens
+    rc = _call_on(cache._dev, lib.ad_cache_append, cache._ref, k_t.data_ptr(), v_t.data_ptr(), dtype, stride, off_t.data_ptr(), len_t.data_ptr(), B, M,
+                  max_new, _status_pointer(entry, cache._dev, status_t))
     if rc != AD_OK:
         _raise(lib, rc)
 
@@ -563,13 +572,15 @@ def cache_append(cache, k_t, v_t, off_t, len_t, max_new, status_t=None):
 def cache_read(cache, off_t, start_t, tokens, max_tokens, dtype=None, status_t=None):
     """Positions start_t[b] .. of every row, off_t[b + 1] - off_t[b] of them: (k, v) [tokens, n_kv_heads, head_dim] in dtype (default bfloat16).
     Tokens that no row covers are left uninitialised."""
-    import torch
-    entry, lib = "ad_cache_read", load()
+    entry, lib = "ad_cache_read", _lib or load()
     B = cache._batch(entry, off_t, start_t)
-    k, v = (torch.empty((tokens, cache.n_kv_heads, cache.head_dim), dtype=dtype or torch.bfloat16, device=cache.device) for _ in range(2))
-    code, status = _number_type(entry, k), _status_pointer(entry, cache.device, status_t)
-    rc = _on_device(cache.device, lambda stream: lib.ad_cache_read(
-        cache._ref, k.data_ptr(), v.data_ptr(), code, off_t.data_ptr(), start_t.data_ptr(), B, tokens, max_tokens, status, stream))
+    dtype = dtype or _BF16
+    if dtype is not _BF16 and dtype is not _FP32:
+        _refuse(entry, f"{dtype} is neither float32 nor bfloat16")
+    shape = (tokens, cache.n_kv_heads, cache.head_dim)
+    k, v = cache.k_scale.new_empty(shape, dtype=dtype), cache.k_scale.new_empty(shape, dtype=dtype)
+    rc = _call_on(cache._dev, lib.ad_cache_read, cache._ref, k.data_ptr(), v.data_ptr(), AD_DTYPE_BF16 if dtype is _BF16 else AD_DTYPE_FP32,
+                  off_t.data_ptr(), start_t.data_ptr(), B, tokens, max_tokens, _status_pointer(entry, cache._dev, status_t))
     if rc != AD_OK:
         _raise(lib, rc)
     return k, v
@@ -578,64 +589,73 @@ def cache_read(cache, off_t, start_t, tokens, max_tokens, dtype=None, status_t=N
 def cache_attention(cache, q_t, off_t, len_t, max_new, max_keys, causal=True, scale=None, out=None, status_t=None):
     """Attention of q_t [M, n_heads, head_dim] over the cache; returns [M, n_heads, head_dim] in q_t's type (`out`, if given).  Causal: query i of
     row b sees len_t[b] + i + 1 positions (its block has been appended), otherwise all see len_t[b].  scale: head_dim ** -0.5 unless given."""
-    import torch
-    entry, lib = "ad_cache_attention", load()
-    B, dtype = cache._batch(entry, off_t, len_t), _number_type(entry, q_t)
+    entry, lib = "ad_cache_attention", _lib or load()
+    B = cache._batch(entry, off_t, len_t)
     if q_t.dim() != 3:
         _refuse(entry, "queries are [tokens, heads, head_dim]")
-    M, H = q_t.shape[:2]
-    stride = cache._tokens(entry, q_t, H)
+    H = q_t.size(1)
+    dtype, M, stride = cache._tokens(entry, q_t, H)
     if out is None:
-        out = torch.empty((M, H, cache.head_dim), dtype=q_t.dtype, device=cache.device)
-    elif out.dtype != q_t.dtype or out.shape != q_t.shape or out.device != cache.device or not out.is_contiguous():
+        out = q_t.new_empty((M, H, cache.head_dim))
+    elif not _matrix(out, q_t.shape, q_t.dtype, cache._dev):
         _refuse(entry, "the result is a contiguous tensor like the queries")
-    status = _status_pointer(entry, cache.device, status_t)
-    scale = cache.head_dim ** -0.5 if scale is None else float(scale)
-
-    def call(stream):
-        nbytes = lib.ad_cache_attention_scratch_bytes(cache._ref, dtype, H, B, max_new, max_keys)
-        keep, scratch = _scratch(q_t, nbytes) if nbytes else (None, None)
-        return lib.ad_cache_attention(cache._ref, q_t.data_ptr(), dtype, stride, H, off_t.data_ptr(), len_t.data_ptr(), B, M, max_new, max_keys,
-                                      1 if causal else 0, scale, out.data_ptr(), scratch, nbytes, status, stream)
-
-    rc = _on_device(cache.device, call)
+    sizes = (dtype, H, B, max_new, max_keys)
+    nbytes = cache._scratch.get(sizes)
+    if nbytes is None:
+        nbytes = _call_on(cache._dev, lambda *a: lib.ad_cache_attention_scratch_bytes(*a[:-1]), cache._ref, *sizes)
+        if len(cache._scratch) < 4096:
+            cache._scratch[sizes] = nbytes
+    scratch = off_t.new_empty((nbytes + 3) // 4) if nbytes else None       # (torch's allocations are 512-byte aligned)
+    rc = _call_on(cache._dev, lib.ad_cache_attention, cache._ref, q_t.data_ptr(), dtype, stride, H, off_t.data_ptr(), len_t.data_ptr(), B, M, max_new,
+                  max_keys, 1 if causal else 0, cache.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
+                  scratch.data_ptr() if nbytes else None, nbytes, _status_pointer(entry, cache._dev, status_t))
     if rc != AD_OK:
         _raise(lib, rc)
     return out
 
 
+_accept_scratch = {}     # (device, tokens, vocabulary, drafter) -> bytes
+
+
 def accept_sampled(target_t, draft_t, drafts_t, off_t, u_t, r_t, temperature=1.0, eos=-1, status_t=None):
     """Sampled verification of drafts_t [B, kmax] against scores target_t [M, vocab] (and the drafter's, draft_t, or None for drafts that were not
     sampled) with uniform numbers u_t [B, kmax] and r_t [B].  Returns (tokens [B, kmax], n_accepted [B])."""
-    import torch
-    entry, lib = "ad_accept_sampled", load()
-    dev, dtype = target_t.device, _number_type(entry, target_t)
-    if dev.type != "cuda":
-        _refuse(entry, "scores live on a CUDA device")
-    if drafts_t.dim() != 2 or target_t.dim() != 2:
-        _refuse(entry, "drafts are [rows, kmax], scores [tokens, vocab]")
-    B, kmax = drafts_t.shape
+    entry, lib = "ad_accept_sampled", _lib or load()
+    if _INT32 is None:
+        _names()
+    dev = target_t.get_device()
+    dtype = AD_DTYPE_BF16 if target_t.dtype is _BF16 else AD_DTYPE_FP32
+    if dev < 0 or target_t.dim() != 2 or drafts_t.dim() != 2 or (dtype == AD_DTYPE_FP32 and target_t.dtype is not _FP32):
+        _refuse(entry, "scores are [tokens, vocab] on a CUDA device, in float32 or bfloat16, and drafts [rows, kmax]")
+    shape = drafts_t.shape
+    B, kmax = shape
+    if not (_matrix(drafts_t, shape, _INT32, dev) and _vector(off_t, B + 1, _INT32, dev)):
+        _refuse(entry, f"drafts and offsets are contiguous int32 tensors [B, kmax] and [B + 1] on device {dev}")
+    if not (_matrix(u_t, shape, _FP32, dev) and _vector(r_t, B, _FP32, dev)):
+        _refuse(entry, f"random numbers are contiguous float32 tensors [B, kmax] and [B] on device {dev}")
     M, V = target_t.shape
-    _index_arrays(entry, dev, (drafts_t, (B, kmax)), (off_t, (B + 1,)))
-    for x, shape in ((u_t, (B, kmax)), (r_t, (B,))):
-        if x.dtype is not torch.float32 or x.shape != shape or x.device != dev or not x.is_contiguous():
-            _refuse(entry, f"random numbers are contiguous float32 tensors on {dev}; wanted {shape}, got {tuple(x.shape)}")
-    for x in (target_t, draft_t):
-        if x is not None and (x.dtype != target_t.dtype or x.shape != target_t.shape or x.device != dev or (V > 1 and x.stride(1) != 1)):
-            _refuse(entry, "scores are [tokens, vocab], a row's next to each other, the drafter's like the verifier's")
-    strides = [V if x is None or M < 2 else x.stride(0) for x in (target_t, draft_t)]
-    status = _status_pointer(entry, dev, status_t)
-    tokens = torch.empty((B, kmax), dtype=torch.int32, device=dev)
-    count = torch.empty(B, dtype=torch.int32, device=dev)
-
-    def call(stream):
-        nbytes = lib.ad_accept_sampled_scratch_bytes(M, V, 0 if draft_t is None else 1)
-        keep, scratch = _scratch(target_t, nbytes)
-        return lib.ad_accept_sampled(target_t.data_ptr(), strides[0], None if draft_t is None else draft_t.data_ptr(), strides[1], dtype, temperature, V,
-                                     off_t.data_ptr(), drafts_t.data_ptr(), kmax, B, M, u_t.data_ptr(), r_t.data_ptr(), eos, tokens.data_ptr(),
-                                     count.data_ptr(), scratch, nbytes, status, stream)
-
-    rc = _on_device(dev, call)
+    stride, one = target_t.stride()
+    draft_stride, draft = V, None
+    if draft_t is not None:
+        if draft_t.dtype is not target_t.dtype or draft_t.shape != target_t.shape or draft_t.get_device() != dev:
+            _refuse(entry, "the drafter's scores are like the verifier's in type, shape and place")
+        draft_stride, draft_one = draft_t.stride()
+        draft = draft_t.data_ptr()
+        one = max(one, draft_one)
+    if one != 1 and V > 1:
+        _refuse(entry, "a row's scores must lie next to each other")
+    if M < 2:
+        stride = draft_stride = V
+    sizes = (dev, M, V, draft_t is not None)
+    nbytes = _accept_scratch.get(sizes)
+    if nbytes is None:
+        nbytes = _call_on(dev, lambda m, v, z, _: lib.ad_accept_sampled_scratch_bytes(m, v, 1 if z else 0), *sizes[1:])
+        if len(_accept_scratch) < 4096:
+            _accept_scratch[sizes] = nbytes
+    tokens, count, scratch = drafts_t.new_empty(shape), off_t.new_empty(B), off_t.new_empty(max(1, nbytes // 4))
+    rc = _call_on(dev, lib.ad_accept_sampled, target_t.data_ptr(), stride, draft, draft_stride, dtype, temperature, V, off_t.data_ptr(),
+                  drafts_t.data_ptr(), kmax, B, M, u_t.data_ptr(), r_t.data_ptr(), eos, tokens.data_ptr(), count.data_ptr(), scratch.data_ptr(), nbytes,
+                  _status_pointer(entry, dev, status_t))
     if rc != AD_OK:
         _raise(lib, rc)
     return tokens, count

@@ -99,15 +99,20 @@ __device__ __forceinline__ void codes_f16(Int8, uint32_t w, uint32_t& lo, uint32
   hi = *reinterpret_cast<const uint32_t*>(&y);
 }
 // The same for the first product, which takes multiples of them plus a bias: (code + BIAS) / FACTOR, with BIAS times the sum of a row's query (and
-// its sign) where the product starts from.  INT8's c + 128 alone in FP16's low byte is that many times 2^-24.
-template <typename F> struct KeyCodes { static constexpr float BIAS = 0.f, FACTOR = 1.f; };
-template <> struct KeyCodes<Int8> { static constexpr float BIAS = 128.f, FACTOR = 16777216.f; };
-__device__ __forceinline__ void key_codes_f16(E4m3 f, uint32_t w, uint32_t& lo, uint32_t& hi) { codes_f16(f, w, lo, hi); }
-__device__ __forceinline__ void key_codes_f16(Int8, uint32_t w, uint32_t& lo, uint32_t& hi) {
-  w ^= 0x80808080u;
-  lo = __byte_perm(w, 0u, 0x4140);
-  hi = __byte_perm(w, 0u, 0x4342);
-}
+// its sign) where the product starts from.  INT8's c + 128 alone in FP16's low byte is that many times 2^-24, which saves a subtraction per pair and
+// costs a bit of the sum; FP32 queries take the codes as they are (their error would double: 5e-7 to 1.2e-6).
+template <typename F, bool WIDE> struct KeyCodes {
+  static constexpr float BIAS = 0.f, FACTOR = 1.f;
+  static __device__ __forceinline__ void f16(uint32_t w, uint32_t& lo, uint32_t& hi) { codes_f16(F(), w, lo, hi); }
+};
+template <> struct KeyCodes<Int8, false> {
+  static constexpr float BIAS = 128.f, FACTOR = 16777216.f;
+  static __device__ __forceinline__ void f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    w ^= 0x80808080u;
+    lo = __byte_perm(w, 0u, 0x4140);
+    hi = __byte_perm(w, 0u, 0x4342);
+  }
+};
 __device__ __forceinline__ void cp4(void* smem_dst, const void* gmem_src) {
   const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(smem_dst));
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(s), "l"(gmem_src) : "memory");
@@ -137,6 +142,7 @@ __global__ void __launch_bounds__(32 * ATT_WARPS, att_resident(DIM, NQ))
 cache_attention_kernel(AttendParams a) {
   constexpr bool WIDE = sizeof(T) == 4;               // two FP16 numbers for each query and probability
   constexpr int HL = WIDE ? 2 : 1;
+  typedef KeyCodes<F, WIDE> Keys;
   constexpr int KSTEPS = DIM / 16, ND = DIM / 16, MT = (NQ + 1) / 2, ROWS = 8 * NQ;
   constexpr int STAGES = att_stages(DIM, NQ), STAGE = att_stage_bytes(DIM), COPIES = DIM / 16;
   constexpr int P_BITS = 14;
@@ -323,7 +329,7 @@ cache_attention_kernel(AttendParams a) {
         const int mt = r >> 4, word = half * 2 + ((r >> 3) & 1), ln = (r & 7) * 4 + cc;
         const float y0 = x[i] * up, y1 = PER > 1 ? x[PER > 1 ? i + 1 : 0] * up : 0.f;
         const uint32_t hi = pack_f16(y0, y1), lo = rest_f16(y0, y1, hi);
-        if constexpr (KeyCodes<F>::BIAS != 0.f) {
+        if constexpr (Keys::BIAS != 0.f) {
           const float2 h2 = unpack_f16(hi), l2 = unpack_f16(lo);
           total += h2.x + h2.y + (WIDE ? l2.x + l2.y : 0.f);
         }
@@ -337,8 +343,8 @@ cache_attention_kernel(AttendParams a) {
 #pragma unroll
       for (int w = 16; w; w >>= 1) total += __shfl_xor_sync(0xffffffffu, total, w);
       if (lane == 0 && r < ROWS) {
-        s_rf[r] = a.scale * (1.f / up) * KeyCodes<F>::FACTOR;
-        s_start[r] = -KeyCodes<F>::BIAS / KeyCodes<F>::FACTOR * total;
+        s_rf[r] = a.scale * (1.f / up) * Keys::FACTOR;
+        s_start[r] = -Keys::BIAS / Keys::FACTOR * total;
       }
     }
     __syncthreads();
@@ -384,7 +390,7 @@ cache_attention_kernel(AttendParams a) {
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[t][nt][j] = KeyCodes<F>::BIAS != 0.f && 2 * t + (j >> 1) < NQ ? start[2 * t + (j >> 1) < NQ ? 2 * t + (j >> 1) : 0] : 0.f;
+          for (int j = 0; j < 4; ++j) s[t][nt][j] = Keys::BIAS != 0.f && 2 * t + (j >> 1) < NQ ? start[2 * t + (j >> 1) < NQ ? 2 * t + (j >> 1) : 0] : 0.f;
       constexpr int RAW = KSTEPS < 4 ? KSTEPS : 4;       // words of codes of one load
 #pragma unroll
       for (int hh = 0; hh < KSTEPS / RAW; ++hh) {
@@ -414,7 +420,7 @@ cache_attention_kernel(AttendParams a) {
 #pragma unroll
           for (int nt = 0; nt < 4; ++nt) {
             uint32_t b0, b1;
-            key_codes_f16(F(), raw[nt][j], b0, b1);
+            Keys::f16(raw[nt][j], b0, b1);
 #pragma unroll
             for (int h = HL - 1; h >= 0; --h)
 #pragma unroll
