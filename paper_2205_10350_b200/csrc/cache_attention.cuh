@@ -85,6 +85,12 @@ __device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// The same from c0 in its first row and c1 in its second.
+__device__ __forceinline__ void mma_f16_from(float* d, const uint32_t* a, uint32_t b0, uint32_t b1, float c0, float c1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %11, %11};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
 // Four codes to FP16, exactly: lo holds the first two, hi the others.
 __device__ __forceinline__ void codes_f16(E4m3, uint32_t w, uint32_t& lo, uint32_t& hi) {
   asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(lo), "=r"(hi) : "r"(w));
@@ -127,8 +133,9 @@ __device__ __forceinline__ int unit_key(int nt, int n) { return 16 * (nt >> 1) +
 // What a number goes through.  Codes are exact in FP16, and so are queries once a power of two has brought the row's largest to 2^13 (BF16 has 8 bits;
 // FP32 goes in as two FP16 numbers, 22 bits, and so do its probabilities).  Scores are FP32: the keys' scale, the softmax scale and the query's power
 // of two come in one factor per block and row.  Probabilities meet the values' scale before they are rounded: p * vs, as a multiple of its largest
-// value so far in the row (2^d times what the softmax's own maximum m stands for), times 2^14: nothing that matters comes near FP16's subnormals,
-// however far the blocks' scales are apart.  Sums, maxima and results are FP32.
+// value so far in the row (2^d times what the softmax's own reference m stands for), times 2^15: nothing that matters comes near FP16's subnormals,
+// however far the blocks' scales are apart.  References are whole exponents, so that results go from one to another by exact powers of two, and lie up
+// to 4 above the largest score, so that few units move them (32 rows over 16 units: in nearly all of them without).  Sums and results are FP32.
 //
 // Why this shape.  What has to be read is 2 * dim bytes a key; 16 rows make 64 operations a byte of it, which mma.sync delivers several times over, so the kernel
 // is a stream of the cache with as little as possible per byte: each warp copies its own units of 32 keys through its own ring in shared memory
@@ -145,9 +152,10 @@ cache_attention_kernel(AttendParams a) {
   typedef KeyCodes<F, WIDE> Keys;
   constexpr int KSTEPS = DIM / 16, ND = DIM / 16, MT = (NQ + 1) / 2, ROWS = 8 * NQ;
   constexpr int STAGES = att_stages(DIM, NQ), STAGE = att_stage_bytes(DIM), COPIES = DIM / 16;
-  constexpr int P_BITS = 14;
+  constexpr int P_BITS = 15;
+  constexpr float SLACK = 3.f;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ float s_rf[ROWS], s_start[ROWS];
+  __shared__ float2 s_rf[ROWS];                       // factor of a row's scores, and what its first product starts from
   uint4* sq = reinterpret_cast<uint4*>(smem);          // [HL][MT][KSTEPS][lane]: operands as mma wants them
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
   unsigned char* ring = smem + att_q_bytes(DIM, NQ, WIDE) + warp * STAGES * STAGE;
@@ -270,23 +278,31 @@ cache_attention_kernel(AttendParams a) {
       const uint8_t* ks = a.c.codes[0] + src;
       const uint8_t* vs = a.c.codes[1] + src;
       const ptrdiff_t second = TWO ? (ptrdiff_t)(tile[1] - tile[0]) * 16 * DIM - 16 * DIM : 0;     // from where the second half would lie to where it does
-      const bool whole = first + UNIT <= vis_max && there[0] && (!TWO || there[1]);
+      auto k_to = [&](int i) { return (DIM == 128 && (i & 1) ? k_odd : k_dst) + so + (DIM == 128 ? (16 * (i >> 2) + 8 * ((i >> 1) & 1) + (i & 1)) * DIM : i * 512); };
+      auto from = [&](int i) { return i * 512 + (TWO && i >= COPIES / 2 ? second : 0); };
+      constexpr int SCALES = TWO ? 4 : 2;                           // ks0, ks1, vs0, vs1 (without a second block, the first of each)
+      const int slot = TWO ? lane : 2 * lane, z = TWO ? lane & 1 : 0;
+      float* scale_dst = reinterpret_cast<float*>(ring + stage * STAGE + 2 * UNIT * DIM) + slot;
+      const float* scale_src = (slot < 2 ? a.c.scale[0] : a.c.scale[1]) + (z ? tile[1] : tile[0]);
+      if (first + UNIT <= vis_max && there[0] && (!TWO || there[1])) {
 #pragma unroll
-      for (int i = 0; i < COPIES; ++i) {
-        const uint32_t kd = (DIM == 128 && (i & 1) ? k_odd : k_dst) + so + (DIM == 128 ? (16 * (i >> 2) + 8 * ((i >> 1) & 1) + (i & 1)) * DIM : i * 512);
-        const uint32_t vd = v_dst + so + i * 512;
-        const ptrdiff_t at = i * 512 + (TWO && i >= COPIES / 2 ? second : 0);
-        const int z = TWO && i >= COPIES / 2 ? 1 : 0;
-        const int n = whole || (there[z] && first + my_key + i * (512 / DIM) < vis_max) ? 16 : 0;   // zeros where there is no key
-        asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(kd), "l"(ks + at), "r"(n), "l"(policy) : "memory");
-        asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(vd), "l"(vs + at), "r"(n), "l"(policy) : "memory");
-      }
-      if (lane < 4) {                                               // ks0, ks1, vs0, vs1; negative: no such block
-        const int z = lane & 1;
-        float* dst = reinterpret_cast<float*>(ring + stage * STAGE + 2 * UNIT * DIM) + lane;
-        const bool need = (z == 0 || TWO) && first + 16 * z < vis_max;
-        if (need && (z ? there[1] : there[0])) cp4(dst, (lane < 2 ? a.c.scale[0] : a.c.scale[1]) + (z ? tile[1] : tile[0]));
-        else *dst = need && lane < 2 ? -1.f : 1.f;
+        for (int i = 0; i < COPIES; ++i) {
+          asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(k_to(i)), "l"(ks + from(i)), "l"(policy) : "memory");
+          asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(v_dst + so + i * 512), "l"(vs + from(i)), "l"(policy) : "memory");
+        }
+        if (lane < SCALES) cp4(scale_dst, scale_src);
+      } else {                                                      // zeros where there is no key; a block that is not there: a negative scale
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+          const int n = there[TWO && i >= COPIES / 2 ? 1 : 0] && first + my_key + i * (512 / DIM) < vis_max ? 16 : 0;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(k_to(i)), "l"(ks + from(i)), "r"(n) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(v_dst + so + i * 512), "l"(vs + from(i)), "r"(n) : "memory");
+        }
+        if (lane < SCALES) {
+          const bool need = first + 16 * z < vis_max;
+          if (need && (z ? there[1] : there[0])) cp4(scale_dst, scale_src);
+          else *scale_dst = need && slot < 2 ? -1.f : 1.f;
+        }
       }
     };
     // ---- queries, a few rows a warp: under way first ----
@@ -343,19 +359,21 @@ cache_attention_kernel(AttendParams a) {
 #pragma unroll
       for (int w = 16; w; w >>= 1) total += __shfl_xor_sync(0xffffffffu, total, w);
       if (lane == 0 && r < ROWS) {
-        s_rf[r] = a.scale * (1.f / up) * Keys::FACTOR;
-        s_start[r] = -Keys::BIAS / Keys::FACTOR * total;
+        s_rf[r] = make_float2(a.scale * (1.f / up) * Keys::FACTOR, -Keys::BIAS / Keys::FACTOR * total);
       }
     }
     __syncthreads();
     // Scores: thread's row g of each eight, columns as above.  Results: dims DIM / 8 * g .. of rows 2 c and 2 c + 1 of each eight.
-    float rf[NQ], start[NQ], m[NQ], d[NQ], l[NQ], acc[NQ][ND][4];
+    constexpr bool ROW_REGS = NQ < 4;                   // (with 32 rows registers are short: read again for every unit)
+    float2 row_rf[NQ];
+    float m[NQ], d[NQ], l[NQ], acc[NQ][ND][4];
+    float up[NQ][2], down[NQ][2], ve[2] = {0.f, 0.f}, vs_of[2] = {-1.f, -1.f};
     bool large = false;                                 // scores whose steps in FP32 are a quarter and more
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      rf[q] = s_rf[q * 8 + g];
-      start[q] = s_start[q * 8 + g];
+      if (ROW_REGS) row_rf[q] = s_rf[q * 8 + g];
       m[q] = d[q] = -INFINITY;
+      up[q][0] = up[q][1] = down[q][0] = down[q][1] = 0.f;
       l[q] = 0.f;
 #pragma unroll
       for (int i = 0; i < ND; ++i)
@@ -384,13 +402,14 @@ cache_attention_kernel(AttendParams a) {
       stage = stage == STAGES - 1 ? 0 : stage + 1;
       const float4 sc = *reinterpret_cast<const float4*>(st + 2 * UNIT * DIM);
       // ---- scores ----
+      float rf[NQ], start[NQ];
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        const float2 v = ROW_REGS ? row_rf[q] : s_rf[q * 8 + g];
+        rf[q] = v.x;
+        start[q] = Keys::BIAS != 0.f ? v.y : 0.f;
+      }
       float s[MT][4][4];
-#pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) s[t][nt][j] = Keys::BIAS != 0.f && 2 * t + (j >> 1) < NQ ? start[2 * t + (j >> 1) < NQ ? 2 * t + (j >> 1) : 0] : 0.f;
       constexpr int RAW = KSTEPS < 4 ? KSTEPS : 4;       // words of codes of one load
 #pragma unroll
       for (int hh = 0; hh < KSTEPS / RAW; ++hh) {
@@ -424,23 +443,40 @@ cache_attention_kernel(AttendParams a) {
 #pragma unroll
             for (int h = HL - 1; h >= 0; --h)
 #pragma unroll
-              for (int t = 0; t < MT; ++t) mma_f16(s[t][nt], reinterpret_cast<const uint32_t*>(&qf[h][t]), b0, b1);
+              for (int t = 0; t < MT; ++t) {
+                const uint32_t* qa = reinterpret_cast<const uint32_t*>(&qf[h][t]);
+                if (hh == 0 && j == 0 && h == HL - 1) mma_f16_from(s[t][nt], qa, b0, b1, start[2 * t], start[2 * t + 1 < NQ ? 2 * t + 1 : 2 * t]);
+                else mma_f16(s[t][nt], qa, b0, b1);
+              }
           }
         }
       }
-      if (u * UNIT + UNIT > vis_min || sc.x < 0.f || sc.y < 0.f) {
+      float tk[NQ][2];
 #pragma unroll
-        for (int q = 0; q < NQ; ++q)
+      for (int q = 0; q < NQ; ++q) {
+        tk[q][0] = rf[q] * fabsf(sc.x);
+        tk[q][1] = TWO ? rf[q] * fabsf(sc.y) : tk[q][0];
+      }
+      if (u * UNIT + UNIT > vis_min || sc.x < 0.f || (TWO && sc.y < 0.f)) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
 #pragma unroll
           for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
               if (u * UNIT + unit_key(nt, 2 * c + j) >= s_vis[q * 8 + g] || (TWO && nt >= 2 ? sc.y : sc.x) < 0.f) s[q / 2][nt][2 * (q & 1) + j] = -INFINITY;
+          tk[q][0] = fmaxf(tk[q][0], FLT_MIN);           // (not 0 times -inf)
+          tk[q][1] = TWO ? fmaxf(tk[q][1], FLT_MIN) : tk[q][0];
+        }
       }
-      // ---- probabilities ----
-      float ks[2] = {fabsf(sc.x), TWO ? fabsf(sc.y) : fabsf(sc.x)};
-      const float ve[2] = {lg2(sc.z), TWO ? lg2(sc.w) : lg2(sc.z)};
-      float ref[NQ], top[NQ], tod[NQ], tk[NQ][2];
+      // ---- probabilities: has any row a new maximum, or its values' scale another exponent? ----
+      const bool other_scale = sc.z != vs_of[0] || (TWO && sc.w != vs_of[1]);
+      if (other_scale) {
+        vs_of[0] = sc.z;
+        ve[0] = lg2(sc.z);
+        if (TWO) { vs_of[1] = sc.w; ve[1] = lg2(sc.w); }
+      }
+      float x[NQ][2];
       bool moved = false;
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
@@ -454,25 +490,24 @@ cache_attention_kernel(AttendParams a) {
         if (TWO) {
           x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
           x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
-        } else {
-          x1 = x0;
         }
-        tk[q][0] = fmaxf(rf[q] * ks[0], FLT_MIN);
-        tk[q][1] = fmaxf(rf[q] * ks[1], FLT_MIN);
-        x0 = ceilf(x0 * tk[q][0]);                       // references are whole numbers: what goes from one to another is an exact power of two
-        x1 = TWO ? ceilf(x1 * tk[q][1]) : x0;
-        top[q] = fmaxf(m[q], fmaxf(x0, x1));
-        ref[q] = top[q] == -INFINITY ? 0.f : top[q];
-        tod[q] = fmaxf(d[q] + (m[q] - ref[q]), x0 - ref[q] + ve[0]);
-        if (TWO) tod[q] = fmaxf(tod[q], x1 - ref[q] + ve[1]);
-        moved |= top[q] != m[q] || tod[q] != d[q];
+        x[q][0] = ceilf(x0 * tk[q][0]);                  // references are whole numbers: what goes from one to another is an exact power of two
+        x[q][1] = TWO ? ceilf(x1 * tk[q][1]) : x[q][0];
+        moved |= x[q][0] > m[q] || x[q][0] - m[q] + ve[0] > d[q];
+        if (TWO) moved |= x[q][1] > m[q] || x[q][1] - m[q] + ve[1] > d[q];
       }
-      if (__any_sync(0xffffffffu, moved)) {
+      moved = __any_sync(0xffffffffu, moved);
+      if (moved) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-          const float less = m[q] - ref[q], keep_o = tod[q] == -INFINITY ? 0.f : ex2(less + (d[q] - tod[q]));
-          m[q] = top[q];
-          d[q] = tod[q];
+          // reference m of the row's scores, and exponent d of p * scale beyond m's own
+          const float most = TWO ? fmaxf(x[q][0], x[q][1]) : x[q][0];
+          const float top = most > m[q] ? most + SLACK : m[q], ref = top == -INFINITY ? 0.f : top, less = m[q] - ref;
+          const float with = TWO ? fmaxf(x[q][0] - ref + ve[0], x[q][1] - ref + ve[1]) : x[q][0] - ref + ve[0];
+          const float tod = with > d[q] + less ? with + SLACK : d[q] + less;
+          const float keep_o = tod == -INFINITY ? 0.f : ex2(less + (d[q] - tod));
+          m[q] = top;
+          d[q] = tod;
           l[q] *= ex2(less);
           const float k0 = __shfl_sync(0xffffffffu, keep_o, 8 * c), k1 = __shfl_sync(0xffffffffu, keep_o, 8 * c + 4);
 #pragma unroll
@@ -480,19 +515,41 @@ cache_attention_kernel(AttendParams a) {
             const float2 y0 = mul2(make_float2(acc[q][i][0], acc[q][i][1]), make_float2(k0, k1)), y1 = mul2(make_float2(acc[q][i][2], acc[q][i][3]), make_float2(k0, k1));
             acc[q][i][0] = y0.x; acc[q][i][1] = y0.y; acc[q][i][2] = y1.x; acc[q][i][3] = y1.y;
           }
-          large |= fabsf(ref[q]) > 4194304.f;
+          large |= fabsf(ref) > 4194304.f;
         }
         large = __any_sync(0xffffffffu, large);
       }
-      if (large) {                                       // the exponent below then is a difference of rounded scores, as the maximum is one of them
+      if (moved || other_scale) {
+        // p, as a share of the softmax's maximum, goes into the second product times 2^(15 + e), e = log2(values' scale) - d.  Its sum is taken as it is
+        // and brought back afterwards, which the bounds on e keep inside FP32 (beyond them the values do not count, or the probability).
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+#pragma unroll
+          for (int z = 0; z < (TWO ? 2 : 1); ++z) {
+            const float e = (float)P_BITS + fminf(fmaxf(ve[z] - d[q], -100.f), 100.f);
+            up[q][z] = m[q] == -INFINITY ? e : e - m[q];
+            down[q][z] = ex2(-e);
+          }
+      }
+      float from[NQ][TWO ? 2 : 1];
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int z = 0; z < (TWO ? 2 : 1); ++z) from[q][z] = up[q][z];
+      if (large) {                                       // scores in steps of a quarter and more: a difference of rounded ones, as the maximum is one of them
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
+          const float ref = m[q] == -INFINITY ? 0.f : m[q];
 #pragma unroll
           for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) s[q / 2][nt][2 * (q & 1) + j] = __fsub_rn(__fmul_rn(s[q / 2][nt][2 * (q & 1) + j], tk[q][nt >> 1]), ref[q]);
+            for (int j = 0; j < 2; ++j) {
+              float& v = s[q / 2][nt][2 * (q & 1) + j];
+              v = __fsub_rn(__fmul_rn(v, tk[q][nt >> 1]), ref);
+            }
           tk[q][0] = tk[q][1] = 1.f;
-          ref[q] = 0.f;
+#pragma unroll
+          for (int z = 0; z < (TWO ? 2 : 1); ++z) from[q][z] = -log2f(down[q][z]);
         }
       }
       uint32_t pf[HL][NQ][4];                            // [score tile]: two keys' probabilities of row g, as the second product's operand
@@ -500,10 +557,8 @@ cache_attention_kernel(AttendParams a) {
       for (int q = 0; q < NQ; ++q)
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
-          // p, as a share of the softmax's maximum, times 2^(14 + e), e = log2(values' scale) - d: what goes into the second product.  Its sum is taken
-          // as it is and brought back afterwards, which the bounds on e keep inside FP32 (beyond them the values do not count, or the probability).
-          const float e = (float)P_BITS + fminf(fmaxf(ve[z] - d[q], -100.f), 100.f), less = e - ref[q];
-          const float2 t2 = make_float2(tk[q][z], tk[q][z]), r2 = make_float2(less, less);
+          const int zz = TWO ? z : 0;
+          const float2 t2 = make_float2(tk[q][zz], tk[q][zz]), r2 = make_float2(from[q][zz], from[q][zz]);
           float2 sum;
 #pragma unroll
           for (int nt = 2 * z; nt < 2 * z + 2; ++nt) {
@@ -514,7 +569,7 @@ cache_attention_kernel(AttendParams a) {
             pf[0][q][nt] = pack_f16(y.x, y.y);
             if constexpr (WIDE) pf[HL - 1][q][nt] = rest_f16(y.x, y.y, pf[0][q][nt]);
           }
-          l[q] = fmaf(sum.x + sum.y, ex2(-e), l[q]);
+          l[q] = fmaf(sum.x + sum.y, down[q][zz], l[q]);
         }
       // ---- times values ----
 #pragma unroll
