@@ -131,7 +131,7 @@ size_t attend_part_bytes(const ad_kv_cache* c, const AttendPlan& plan, int32_t B
   return plan.granule == 0 ? 0 : 2 * (size_t)plan.grid * 8 * plan.nq * (c->head_dim + 2) * sizeof(float) + attend_prefix_bytes(B);
 }
 bool attend_sizes(const ad_kv_cache* c, int32_t n_heads, int32_t max_new) {
-  return n_heads >= 1 && n_heads <= 65535 && n_heads % c->n_kv_heads == 0 && (int64_t)max_new * (n_heads / c->n_kv_heads) <= (1 << 24);
+  return n_heads >= 1 && n_heads <= 65535 && n_heads % c->n_kv_heads == 0 && (int64_t)max_new * (n_heads / c->n_kv_heads) <= (1 << 24) && (int64_t)max_new * n_heads <= (1 << 30);
 }
 
 template <typename T, typename F, int DIM, int NQ, bool TWO>
@@ -175,7 +175,7 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
   if (const char* why = batch_fault(off, len, B, M, max_new)) return arg_fault(entry, why);
   if (const char* why = cache_fault(c, B)) return arg_fault(entry, why);
   if (!known_dtype(dtype)) return arg_fault(entry, "unknown dtype");
-  if (!attend_sizes(c, n_heads, max_new)) return arg_fault(entry, "query heads must be a multiple of the cache's, at most 65535, and max_new times their ratio at most 2^24");
+  if (!attend_sizes(c, n_heads, max_new)) return arg_fault(entry, "query heads must be a multiple of the cache's, at most 65535, and max_new times their ratio at most 2^24 (times them, 2^30)");
   if (max_keys < 0) return arg_fault(entry, "negative number of keys");
   if (!(scale > 0.f) || !(scale < INFINITY)) return arg_fault(entry, "the scale must be positive and finite");
   if (M == 0) return AD_OK;

@@ -59,7 +59,8 @@ def test_append_refusals(lib, bad):
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(q=P + 2), dict(out=None), dict(out=P + 4), dict(dtype=7), dict(stride=255), dict(stride=260), dict(heads=3),
                                  dict(heads=0), dict(off=None), dict(len=None), dict(B=0), dict(M=-5), dict(max_new=0), dict(max_keys=-1), dict(scale=0.0),
-                                 dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))])
+                                 dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(heads=65534, stride=65534 * 64, max_new=600),
+                                 dict(max_new=1 << 20)])
 def test_attention_refusals(lib, bad):
     _refused(lib, lib.ad_cache_attention(C.byref(_cache()), *{**ATTEND, **bad}.values(), None, None))
 

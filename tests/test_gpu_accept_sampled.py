@@ -102,6 +102,17 @@ def test_ragged_batches(dtype, drafter, V):
     assert n[new.index(0)] == 0
 
 
+@pytest.mark.parametrize("dtype,drafter,V", [("bf16", True, 120001), ("fp32", False, 230000)])
+def test_vocabularies_whose_weights_do_not_stay_in_shared_memory(dtype, drafter, V):
+    check(*problem([3, 1, 2], V, dtype, 51, drafter))
+
+
+def test_more_rows_than_clusters_of_eight():
+    """Clusters of four CTAs, and of one where the vocabulary is small."""
+    for V in (7000, 900):
+        check(*problem([2, 1, 3, 0] * 12, V, "bf16", 53, True, 0.9), temperature=0.9)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("V", [31, 5003])
 def test_plain_sampling_follows_the_inverse_distribution(dtype, V):

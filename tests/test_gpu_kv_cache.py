@@ -423,6 +423,31 @@ def test_addresses_beyond_32_bits():
     attend_and_check(cache, small, q, [3], [147], True, "bf16")
 
 
+@pytest.mark.parametrize("dtype,heads,group,dim,block", [("bf16", 2, 1, 64, 32), ("bf16", 1, 4, 128, 16), ("fp32", 1, 2, 32, 64)])
+def test_more_rows_than_a_thread_block(dtype, heads, group, dim, block):
+    """200 rows, most of them short or without queries, a few long ones whose keys are shared out over many CTAs."""
+    g = np.random.default_rng(dim)
+    new = [int(x) for x in g.integers(0, 4, 200)]
+    lens = [int(x) for x in g.integers(0, 40, 200)]
+    for b, n in ((0, 900), (57, 1500), (130, 2900), (199, 700)):
+        lens[b], new[b] = n, 3
+    cache, model = filled([p + n for p, n in zip(lens, new)], heads, dim, block, "int8", dtype, 8)
+    q = numbers((sum(new), heads * group, dim), dtype, 6, 0.3).to(DEV)
+    attend_and_check(cache, model, q, new, lens, True, dtype)
+    attend_and_check(cache, model, q, new, lens, False, dtype)
+
+
+def test_batches_without_any_query():
+    cache, _ = filled([40, 70], 2, 64, 32, "e4m3", "bf16", 4)
+    q = numbers((3, 2, 64), "bf16", 6, 0.3).to(DEV)
+    out = torch.full((3, 2, 64), 9.0, dtype=torch.bfloat16, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for max_keys in (70, 4000):                              # (with and without a second kernel that joins parts)
+        binding.cache_attention(cache, q, ints([1, 1, 1]), ints([40, 70]), 3, max_keys, causal=False, out=out, status_t=status)
+        binding.cache_append(cache, q, q, ints([3, 3, 3]), ints([40, 70]), 3, status_t=status)
+    assert bool((out == 9.0).all()) and int(status.item()) == 0
+
+
 def test_calls_on_another_stream_and_in_a_graph():
     """The current stream is the one that counts; a captured step reads lengths that change between replays."""
     lens, heads, dim = [40, 70], 2, 64
