@@ -62,8 +62,12 @@ cudaError_t by_types(int32_t dtype, int32_t format, Fn f) {
 int arg_fault(const char* entry, const char* why) { return op_fail(AD_ERR_ARG, entry, why); }
 int launched(const char* entry, cudaError_t e) { return e == cudaSuccess ? AD_OK : op_fail(AD_ERR_CUDA, entry, cudaGetErrorString(e)); }
 
-dim3 tile_grid(const ad_kv_cache* c, int32_t B, int32_t max_new) {
-  return dim3(2 * c->n_kv_heads, (max_new + c->block - 2) / c->block + 1, B);
+// Heads' tiles that a CTA of ad_cache_append and ad_cache_read takes one after the other: four where there are CTAs enough without, else one.
+int tiles_a_cta(const ad_kv_cache* c, int32_t B, int32_t max_new) {
+  return (int64_t)2 * c->n_kv_heads * ((max_new + c->block - 1) / c->block) * B >= 16 * (int64_t)op_num_sms() ? 4 : 1;
+}
+dim3 tile_grid(const ad_kv_cache* c, int32_t B, int32_t max_new, int tiles) {
+  return dim3((2 * c->n_kv_heads + tiles - 1) / tiles, (max_new + c->block - 2) / c->block + 1, B);
 }
 dim3 tile_threads(const ad_kv_cache* c) { return dim3(std::max(32, c->block * c->head_dim / (8 * kv::VECS))); }
 dim3 read_threads(const ad_kv_cache* c) { return dim3(std::max(32, c->block * c->head_dim / (16 * kv::READ_VECS))); }
@@ -81,11 +85,12 @@ extern "C" int ad_cache_append(const ad_kv_cache* c, const void* k, const void* 
   if (token_stride < (int64_t)c->n_kv_heads * c->head_dim || token_stride % (int64_t)(16 / dtype_bytes(dtype)))
     return arg_fault(entry, "tokens must be a multiple of 16 bytes apart, and not overlap");
   const kv::Cache d = device_cache(c);
+  const int tiles = tiles_a_cta(c, B, max_new);
   return launched(entry, by_types(dtype, c->format, [&](auto t) {
     typedef typename decltype(t)::Num T;
-    return launch_op(kv::cache_append_kernel<T, typename decltype(t)::Fmt>, tile_grid(c, B, max_new), tile_threads(c), dim3(), 0,
+    return launch_op(kv::cache_append_kernel<T, typename decltype(t)::Fmt>, tile_grid(c, B, max_new, tiles), tile_threads(c), dim3(), 0,
                      static_cast<cudaStream_t>(stream), d, static_cast<const T*>(k), static_cast<const T*>(v), (size_t)token_stride,
-                     (int)c->head_dim, off, len, (int)M, (int)max_new, status);
+                     (int)c->head_dim, off, len, (int)M, (int)max_new, tiles, status);
   }));
 }
 
@@ -98,11 +103,12 @@ extern "C" int ad_cache_read(const ad_kv_cache* c, void* k, void* v, int32_t dty
   if (M == 0) return AD_OK;
   if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return arg_fault(entry, "keys and values must be 16-byte aligned");
   const kv::Cache d = device_cache(c);
+  const int tiles = tiles_a_cta(c, B, max_tokens);
   return launched(entry, by_types(dtype, c->format, [&](auto t) {
     typedef typename decltype(t)::Num T;
-    return launch_op(kv::cache_read_kernel<T, typename decltype(t)::Fmt>, tile_grid(c, B, max_tokens), read_threads(c), dim3(), 0,
+    return launch_op(kv::cache_read_kernel<T, typename decltype(t)::Fmt>, tile_grid(c, B, max_tokens, tiles), read_threads(c), dim3(), 0,
                      static_cast<cudaStream_t>(stream), d, static_cast<T*>(k), static_cast<T*>(v), (int)c->head_dim, off, start, (int)M,
-                     (int)max_tokens, status);
+                     (int)max_tokens, tiles, status);
   }));
 }
 

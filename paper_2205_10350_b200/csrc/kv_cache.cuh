@@ -138,109 +138,146 @@ __device__ __forceinline__ void store8(bf16* p, const float* x) {
 // code that gets another scale is only moved by whole binary places, exact in E4M3 above the subnormals of the new scale, and in INT8 off by half a
 // step of the new scale; steps at least double from one rounding to the next, so all of a value's roundings together stay below one step of the
 // largest scale that its block ever had.
-// One CTA per block of tokens, head and keys / values; its numbers stay in registers between the maximum and the codes, so that everything is read
-// and written once.  Bound by bytes.
-// grid = (2 * heads, blocks a row's new tokens may touch, B), block = max(32, block * dim / 32) threads.
+// A CTA takes a block of tokens' keys or values of one head at a time, `tiles` of them one after the other, with the next one's loads under way; numbers
+// stay in registers between the maximum and the codes, so that everything is read and written once.  Bound by bytes: 8 prompts of 2500 to 8190
+// tokens, 8 heads of 128, BF16 to E4M3, APPEND_FIGURES.
+// grid = (ceil(2 * heads / tiles), blocks a row's new tokens may touch, B), block = max(32, block * dim / 32) threads.
 constexpr int VECS = 4;                // vectors of eight numbers a thread holds
+__device__ __forceinline__ uint32_t max_bits(uint32_t m, uint4 v, float) {      // largest |x| as an integer: FP32 ...
+  return max(max(max(m, v.x & 0x7fffffffu), max(v.y & 0x7fffffffu, v.z & 0x7fffffffu)), v.w & 0x7fffffffu);
+}
+__device__ __forceinline__ uint32_t max_bits(uint32_t m, uint4 v, bf16) {       // ... or of two BF16 side by side
+  m = __vmaxu2(m, v.x & 0x7fff7fffu);
+  m = __vmaxu2(m, v.y & 0x7fff7fffu);
+  m = __vmaxu2(m, v.z & 0x7fff7fffu);
+  return __vmaxu2(m, v.w & 0x7fff7fffu);
+}
 template <typename T, typename F>
 __global__ void __launch_bounds__(512)
 cache_append_kernel(Cache c, const T* __restrict__ k, const T* __restrict__ v, size_t stride, int dim, const int* __restrict__ off,
-                    const int* __restrict__ len, int M, int max_new, int* status) {
-  __shared__ float s_max[16];
+                    const int* __restrict__ len, int M, int max_new, int tiles, int* status) {
+  constexpr int WORDS = sizeof(T) / 2;                    // 16-byte words of a vector
+  __shared__ uint32_t s_max[2][16];
   pdl_launch();
   pdl_wait();
-  const int b = blockIdx.z, which = blockIdx.x & 1, head = blockIdx.x >> 1;
+  const int b = blockIdx.z, first = blockIdx.x * tiles, last = min(first + tiles, 2 * c.heads), warps = blockDim.x >> 5;
   int o, n, p;
   if (!row_tokens(c, off, len, b, M, max_new, false, status, o, n, p)) return;
   const int i = p / c.block + blockIdx.y, base = i * c.block;
   if (base >= p + n) return;
   const int live = max(p - base, 0), end = min(p + n - base, c.block);          // tokens in front, end of the new ones
-  const T* src = (which ? v : k) + (size_t)head * dim;
-  const int per_token = dim / 8, vecs = c.block * per_token;
-  auto place = [&](int u, int& t, int& d) {                                      // token and first number of vector u; false beyond the block
-    const int e = threadIdx.x + u * blockDim.x;
-    t = e / per_token;
-    d = (e - t * per_token) * 8;
-    return e < vecs;
-  };
-  // the new tokens do not wait for the table
-  uint4 raw[VECS][sizeof(T) / 2];
-#pragma unroll
-  for (int u = 0; u < VECS; ++u) {
-    int t, d;
-    const bool in = place(u, t, d) && t >= live && t < end;
-#pragma unroll
-    for (int j = 0; j < (int)sizeof(T) / 2; ++j)
-      raw[u][j] = in ? __ldcs(reinterpret_cast<const uint4*>(src + (size_t)(o + base + t - p) * stride + d) + j) : make_uint4(0u, 0u, 0u, 0u);
-  }
-  const int id = c.find(b, i);
-  if (id < 0) { latch_error(status, AD_ERR_ARG); return; }
-  uint8_t* codes = (which ? c.codes[1] : c.codes[0]) + ((size_t)id * c.heads + head) * c.block * dim;
-  float* scale = (which ? c.scale[1] : c.scale[0]) + (size_t)id * c.heads + head;
-  const float old = live ? __ldcg(scale) : 1.f;
-  if (live) {                                                                    // those in front, as they are
+  const int shift = __ffs(dim) - 4, vecs = c.block << shift;                    // (dim / 8 vectors a token)
+  auto token = [&](int u) { return (int)(threadIdx.x + u * blockDim.x) >> shift; };
+  auto place = [&](int u) { return (int)(threadIdx.x + u * blockDim.x) * 8; };  // in the block's codes
+  auto inside = [&](int u) { return (int)(threadIdx.x + u * blockDim.x) < vecs; };
+  auto load_new = [&](int tile, uint4 (*raw)[WORDS]) {
+    const T* src = (tile & 1 ? v : k) + (size_t)(tile >> 1) * dim + (size_t)(o + base - p) * stride;
 #pragma unroll
     for (int u = 0; u < VECS; ++u) {
-      int t, d;
-      if (!place(u, t, d) || t >= live) continue;
-      const uint2 w = __ldcg(reinterpret_cast<const uint2*>(codes + t * dim + d));
-      raw[u][0].x = w.x;
-      raw[u][0].y = w.y;
-    }
-  }
-  auto numbers = [&](int u, int t, float* x) {
-    if (t < live) {
-      F::decode4(raw[u][0].x, x);
-      F::decode4(raw[u][0].y, x + 4);
+      const int t = token(u);
+      const bool in = inside(u) && t >= live && t < end;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= old;
-    } else {
-      load8(reinterpret_cast<const T*>(raw[u]), x);
+      for (int j = 0; j < WORDS; ++j)
+        raw[u][j] = in ? __ldcs(reinterpret_cast<const uint4*>(src + (size_t)t * stride + (place(u) & (dim - 1))) + j) : make_uint4(0u, 0u, 0u, 0u);
     }
   };
-  float amax = 0.f;
-  bool nan = false;
+  constexpr bool AHEAD = sizeof(T) == 2;                  // (FP32's would take too many registers)
+  uint4 raw[VECS][WORDS], next[AHEAD ? VECS : 1][WORDS];
+  load_new(first, AHEAD ? next : raw);                    // the new tokens do not wait for the table
+  const int id = c.find(b, i);
+  if (id < 0) { latch_error(status, AD_ERR_ARG); return; }
+  for (int tile = first; tile < last; ++tile) {
+    const int which = tile & 1, head = tile >> 1, turn = (tile - first) & 1;
+    if constexpr (AHEAD) {
 #pragma unroll
-  for (int u = 0; u < VECS; ++u) {
-    int t, d;
-    place(u, t, d);
-    float x[8];
-    numbers(u, t, x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float a = fabsf(x[j]);
-      amax = fmaxf(amax, a < INFINITY ? a : 0.f);                                // (infinities saturate, whatever the scale)
-      nan |= a != a;
+      for (int u = 0; u < VECS; ++u) raw[u][0] = next[u][0];
+      if (tile + 1 < last) load_new(tile + 1, next);
+    } else {
+      if (tile > first) load_new(tile, raw);
     }
-  }
-  if (nan) latch_error(status, AD_ERR_ARG);
-  amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
-  if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = amax;
-  __syncthreads();
-  for (int w = 0; w < (int)blockDim.x >> 5; ++w) amax = fmaxf(amax, s_max[w]);
-  const float s = block_scale<F>(amax), inv = 1.f / s;                          // (both powers of two)
+    uint8_t* codes = (which ? c.codes[1] : c.codes[0]) + ((size_t)id * c.heads + head) * c.block * dim;
+    float* scale = (which ? c.scale[1] : c.scale[0]) + (size_t)id * c.heads + head;
+    const float old = live ? __ldcg(scale) : 1.f;
+    uint32_t top = 0;
 #pragma unroll
-  for (int u = 0; u < VECS; ++u) {
-    int t, d;
-    if (!place(u, t, d) || t >= end || (t < live && s == old)) continue;
-    float x[8];
-    numbers(u, t, x);
+    for (int u = 0; u < VECS; ++u)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = x[j] == x[j] ? x[j] * inv : 0.f;
-    *reinterpret_cast<uint2*>(codes + t * dim + d) = make_uint2(F::encode4(x), F::encode4(x + 4));
+      for (int j = 0; j < WORDS; ++j) top = max_bits(top, raw[u][j], T());
+    if (sizeof(T) == 2) top = max(top << 16, top & 0xffff0000u);
+    auto numbers = [&](int u, float* x) {
+      if (token(u) < live) {
+        F::decode4(raw[u][0].x, x);
+        F::decode4(raw[u][0].y, x + 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= old;
+      } else {
+        load8(reinterpret_cast<const T*>(raw[u]), x);
+      }
+    };
+    if (live) {                                           // those in front, as they are
+#pragma unroll
+      for (int u = 0; u < VECS; ++u) {
+        if (!inside(u) || token(u) >= live) continue;
+        const uint2 w = __ldcg(reinterpret_cast<const uint2*>(codes + place(u)));
+        raw[u][0].x = w.x;
+        raw[u][0].y = w.y;
+        float x[8];
+        numbers(u, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+      }
+    }
+    auto block_max = [&](uint32_t m) {
+      m = __reduce_max_sync(0xffffffffu, m);
+      if ((threadIdx.x & 31) == 0) s_max[turn][threadIdx.x >> 5] = m;
+      __syncthreads();
+      for (int w = 0; w < warps; ++w) m = max(m, s_max[turn][w]);
+      return m;
+    };
+    top = block_max(top);
+    if (top >= 0x7f800000u) {                             // infinities saturate, whatever the scale; a NaN becomes 0
+      uint32_t finite = 0;
+      bool nan = false;
+#pragma unroll
+      for (int u = 0; u < VECS; ++u) {
+        float x[8];
+        numbers(u, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t m = __float_as_uint(x[j]) & 0x7fffffffu;
+          if (m < 0x7f800000u) finite = max(finite, m);
+          else if (m > 0x7f800000u) { nan = true; reinterpret_cast<T*>(raw[u])[j] = from_f32<T>(0.f); }
+        }
+      }
+      if (nan) latch_error(status, AD_ERR_ARG);
+      __syncthreads();
+      top = block_max(finite);
+    }
+    const float s = block_scale<F>(__uint_as_float(top)), inv = 1.f / s;        // (both powers of two)
+#pragma unroll
+    for (int u = 0; u < VECS; ++u) {
+      const int t = token(u);
+      if (!inside(u) || t >= end || (t < live && s == old)) continue;
+      float x[8];
+      numbers(u, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= inv;
+      *reinterpret_cast<uint2*>(codes + place(u)) = make_uint2(F::encode4(x), F::encode4(x + 4));
+    }
+    if (threadIdx.x == 0) *scale = s;
   }
-  if (threadIdx.x == 0) *scale = s;
 }
 
-// Reads tokens start[b] .. of row b back into k, v [M, heads, dim].  grid as above, block = max(32, block * dim / 64).
+// Reads tokens start[b] .. of row b back into k, v [M, heads, dim], tile after tile as above.  Bound by bytes: the prompts above, READ_FIGURES.
+// grid as above, block = max(32, block * dim / 64).
 constexpr int READ_VECS = 4;           // vectors of sixteen codes a thread holds
 template <typename T, typename F>
 __global__ void __launch_bounds__(256)
 cache_read_kernel(Cache c, T* __restrict__ k, T* __restrict__ v, int dim, const int* __restrict__ off, const int* __restrict__ start, int M, int max_tokens,
-                  int* status) {
+                  int tiles, int* status) {
   pdl_launch();
   pdl_wait();
-  const int b = blockIdx.z, which = blockIdx.x & 1, head = blockIdx.x >> 1;
+  const int b = blockIdx.z, first = blockIdx.x * tiles, last = min(first + tiles, 2 * c.heads);
   int o, n, p;
   if (!row_tokens(c, off, start, b, M, max_tokens, false, status, o, n, p)) return;
   const int i = p / c.block + blockIdx.y, base = i * c.block;
@@ -248,30 +285,42 @@ cache_read_kernel(Cache c, T* __restrict__ k, T* __restrict__ v, int dim, const 
   const int id = c.find(b, i);
   if (id < 0) { latch_error(status, AD_ERR_ARG); return; }
   const int from = max(p - base, 0), end = min(p + n - base, c.block);
-  const uint8_t* codes = (which ? c.codes[1] : c.codes[0]) + ((size_t)id * c.heads + head) * c.block * dim;
-  const float s = __ldcg((which ? c.scale[1] : c.scale[0]) + (size_t)id * c.heads + head);
-  T* dst = (which ? v : k) + (size_t)head * dim;
-  const int per_token = dim / 16, vecs = c.block * per_token;
-  uint4 w[READ_VECS];
+  const int shift = __ffs(dim) - 5, vecs = c.block << shift;
+  auto load = [&](int tile, uint4* w, float& s) {
+    const size_t at = (size_t)id * c.heads + (tile >> 1);
+    const uint8_t* codes = (tile & 1 ? c.codes[1] : c.codes[0]) + at * c.block * dim;
+    s = __ldcg((tile & 1 ? c.scale[1] : c.scale[0]) + at);
 #pragma unroll
-  for (int u = 0; u < READ_VECS; ++u) {
-    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 16;
-    if (e < vecs && t >= from && t < end) w[u] = __ldcg(reinterpret_cast<const uint4*>(codes + t * dim + d));
-  }
+    for (int u = 0; u < READ_VECS; ++u) {
+      const int e = threadIdx.x + u * blockDim.x, t = e >> shift;
+      if (e < vecs && t >= from && t < end) w[u] = __ldcs(reinterpret_cast<const uint4*>(codes + e * 16));
+    }
+  };
+  uint4 next[READ_VECS];
+  float next_scale;
+  load(first, next, next_scale);
+  for (int tile = first; tile < last; ++tile) {
+    uint4 w[READ_VECS];
 #pragma unroll
-  for (int u = 0; u < READ_VECS; ++u) {
-    const int e = threadIdx.x + u * blockDim.x, t = e / per_token, d = (e - t * per_token) * 16;
-    if (e >= vecs || t < from || t >= end) continue;
-    const uint32_t words[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
-    T* to = dst + (size_t)(o + base + t - p) * c.heads * dim + d;
+    for (int u = 0; u < READ_VECS; ++u) w[u] = next[u];
+    const float s = next_scale;
+    if (tile + 1 < last) load(tile + 1, next, next_scale);
+    T* dst = (tile & 1 ? v : k) + (size_t)(tile >> 1) * dim + (size_t)(o + base - p) * c.heads * dim;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float x[8];
-      F::decode4(words[2 * h], x);
-      F::decode4(words[2 * h + 1], x + 4);
+    for (int u = 0; u < READ_VECS; ++u) {
+      const int e = threadIdx.x + u * blockDim.x, t = e >> shift;
+      if (e >= vecs || t < from || t >= end) continue;
+      const uint32_t words[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+      T* to = dst + (size_t)t * c.heads * dim + (e * 16 & (dim - 1));
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= s;
-      store8(to + 8 * h, x);
+      for (int h = 0; h < 2; ++h) {
+        float x[8];
+        F::decode4(words[2 * h], x);
+        F::decode4(words[2 * h + 1], x + 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= s;
+        store8(to + 8 * h, x);
+      }
     }
   }
 }
