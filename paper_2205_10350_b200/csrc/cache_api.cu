@@ -153,19 +153,21 @@ cudaError_t launch_attention_part(const kv::AttendParams& a, cudaStream_t st) {
   }
   return launch_op(kernel, dim3(a.grid), dim3(32 * kv::ATT_WARPS), dim3(), smem, st, a);
 }
+template <typename T, int DIM, int NQ>
+cudaError_t launch_join(const kv::AttendParams& a, const AttendPlan& plan, cudaStream_t st) {
+  if (!a.granule) return cudaSuccess;
+  const int rows = plan.row_tiles * 8 * NQ, groups = 512 / DIM;
+  return plan.shared ? launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, true>, dim3(rows, a.c.heads, a.B), dim3(128), dim3(), a.grid * sizeof(float), st, a)
+                     : launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, false>, dim3((rows + groups - 1) / groups, a.c.heads, a.B), dim3(128), dim3(), 0, st, a);
+}
 template <typename T, typename F, int DIM, int NQ>
 cudaError_t launch_attention(const kv::AttendParams& a, const AttendPlan& plan, cudaStream_t st) {
-  cudaError_t e = a.c.block == 16 ? launch_attention_part<T, F, DIM, NQ, true>(a, st) : launch_attention_part<T, F, DIM, NQ, false>(a, st);
-  if (e == cudaSuccess && a.granule) {
-    const int rows = plan.row_tiles * 8 * NQ, groups = 512 / DIM;
-    if (plan.shared) e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, true>, dim3(rows, a.c.heads, a.B), dim3(128), dim3(), a.grid * sizeof(float), st, a);
-    else e = launch_op(kv::cache_attention_join_kernel<T, DIM, NQ, false>, dim3((rows + groups - 1) / groups, a.c.heads, a.B), dim3(128), dim3(), 0, st, a);
-  }
-  return e;
+  const cudaError_t e = a.c.block == 16 ? launch_attention_part<T, F, DIM, NQ, true>(a, st) : launch_attention_part<T, F, DIM, NQ, false>(a, st);
+  return e == cudaSuccess ? launch_join<T, DIM, NQ>(a, plan, st) : e;
 }
-template <typename T, typename F, int NQ>
-cudaError_t launch_attention_dim(const kv::AttendParams& a, const AttendPlan& plan, int dim, cudaStream_t st) {
-  return dim == 32 ? launch_attention<T, F, 32, NQ>(a, plan, st) : dim == 64 ? launch_attention<T, F, 64, NQ>(a, plan, st) : launch_attention<T, F, 128, NQ>(a, plan, st);
+template <typename T, typename F, int DIM>
+cudaError_t launch_attention_dim(const kv::AttendParams& a, const AttendPlan& plan, cudaStream_t st) {
+  return plan.nq == 1 ? launch_attention<T, F, DIM, 1>(a, plan, st) : plan.nq == 2 ? launch_attention<T, F, DIM, 2>(a, plan, st) : launch_attention<T, F, DIM, 4>(a, plan, st);
 }
 }  // namespace
 
@@ -204,8 +206,8 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
   return launched(entry, by_types(dtype, c->format, [&](auto t) {
     typedef typename decltype(t)::Num T;
     typedef typename decltype(t)::Fmt F;
-    return plan.nq == 1 ? launch_attention_dim<T, F, 1>(a, plan, c->head_dim, st) : plan.nq == 2 ? launch_attention_dim<T, F, 2>(a, plan, c->head_dim, st)
-                                                                                                 : launch_attention_dim<T, F, 4>(a, plan, c->head_dim, st);
+    return c->head_dim == 32 ? launch_attention_dim<T, F, 32>(a, plan, st) : c->head_dim == 64 ? launch_attention_dim<T, F, 64>(a, plan, st)
+                                                                                              : launch_attention_dim<T, F, 128>(a, plan, st);
   }));
 }
 

@@ -62,6 +62,137 @@ __host__ __device__ __forceinline__ long long cta_start(long long total, long lo
 // The CTA that granule g falls to.
 __host__ __device__ __forceinline__ int cta_of(long long total, long long g, long long ctas) { return (int)(((g + 1) * ctas - 1) / total); }
 
+// A CTA's place in its share of the work, kept in shared memory: the loop over keys has no use for it, and every use for its registers.
+struct Segment {
+  RowWork work;
+  long long at, cur;                   // granule of the row of the batch, and of all
+  int b, piece, piece_end, kvh, r0, r_last;
+  long long scan[ATT_WARPS], base;
+  int row;
+};
+// Granules g0 .. g1 - 1 are this CTA's; the first of them is where seg starts.  False: none.  CTA 0 leaves the granules in front of each row for the join.
+__device__ __forceinline__ bool find_share(const AttendParams& a, int rows, Segment& seg, long long& g0, long long& g1) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  long long total = 0, mine = 0, front = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 32 * ATT_WARPS) {
+    mine = b0 + tid < a.B ? row_work(a, b0 + tid, rows).granules : 0;
+    long long run = mine;
+#pragma unroll
+    for (int w = 1; w < 32; w <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, run, w);
+      if (lane >= w) run += y;
+    }
+    if (lane == 31) seg.scan[warp] = run;
+    __syncthreads();
+    front = total + run - mine;
+#pragma unroll
+    for (int w = 0; w < ATT_WARPS; ++w) {
+      if (w < warp) front += seg.scan[w];
+      total += seg.scan[w];
+    }
+    if (blockIdx.x == 0 && a.granule && b0 + tid < a.B) a.prefix[b0 + tid] = front;
+    __syncthreads();
+  }
+  if (blockIdx.x == 0 && a.granule && tid == 0) a.prefix[a.B] = total;
+  const long long ctas = min((long long)gridDim.x, total);
+  if (blockIdx.x >= ctas) return false;
+  g0 = cta_start(total, blockIdx.x, ctas);
+  g1 = cta_start(total, blockIdx.x + 1, ctas);
+  if (a.B <= 32 * ATT_WARPS) {
+    if (front <= g0 && g0 < front + mine) { seg.row = tid; seg.base = front; }
+  } else if (warp == 0) {                     // (the same scan again, by one warp)
+    long long base = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      const long long x = b0 + lane < a.B ? row_work(a, b0 + lane, rows).granules : 0;
+      long long run = x;
+#pragma unroll
+      for (int w = 1; w < 32; w <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, run, w);
+        if (lane >= w) run += y;
+      }
+      const long long f = base + run - x;
+      if (f <= g0 && g0 < f + x) { seg.row = b0 + lane; seg.base = f; }
+      base += __shfl_sync(0xffffffffu, run, 31);
+      if (base > g0) break;
+    }
+  }
+  __syncthreads();
+  if (tid == 0) {
+    seg.b = seg.row;
+    seg.at = g0 - seg.base;
+    seg.cur = g0;
+    seg.work = row_work(a, seg.row, rows);
+  }
+  return true;
+}
+struct SegmentKeys { int kvh, r0, r_last, vis_min, vis_max, u0, u1; };      // positions that the first and the last row see; units (the tile may see fewer than the row has)
+// Opens the segment that seg has come to; s_vis: positions that each row of the tile sees.
+__device__ __forceinline__ SegmentKeys open_segment(const AttendParams& a, int rows, Segment& seg, int* s_vis, long long g1) {
+  const RowWork& work = seg.work;
+  const int tid = threadIdx.x, group = a.n_heads / a.c.heads;
+  const int item = (int)(seg.at / work.pieces), piece = (int)(seg.at % work.pieces), piece_end = (int)min((long long)work.pieces, piece + (g1 - seg.cur));
+  SegmentKeys v;
+  v.kvh = item / work.tiles;
+  v.r0 = item % work.tiles * rows;
+  v.r_last = min(v.r0 + rows, work.n * group) - 1;
+  v.vis_min = a.causal ? work.p + v.r0 / group + 1 : work.p;
+  v.vis_max = a.causal ? work.p + v.r_last / group + 1 : work.p;
+  const int units = (v.vis_max + UNIT - 1) / UNIT;
+  v.u0 = min((int)((long long)work.units * piece / work.pieces), units);
+  v.u1 = min((int)((long long)work.units * piece_end / work.pieces), units);
+  if (tid < rows) s_vis[tid] = a.causal ? work.p + min(v.r0 + tid, v.r_last) / group + 1 : work.p;
+  if (tid == 0) { seg.piece = piece; seg.piece_end = piece_end; seg.kvh = v.kvh; seg.r0 = v.r0; seg.r_last = v.r_last; }
+  return v;
+}
+// On to the next segment (all threads, behind the last use of shared memory's segment); false: that was all.
+__device__ __forceinline__ bool next_segment(const AttendParams& a, int rows, Segment& seg, long long g1) {
+  const int done = seg.piece_end - seg.piece;
+  if (seg.cur + done >= g1) return false;
+  __syncthreads();                             // shared memory is the next item's
+  if (threadIdx.x == 0) {
+    seg.cur += done;
+    seg.at += done;
+    while (seg.at == seg.work.granules) { seg.at = 0; seg.work = row_work(a, ++seg.b, rows); }   // (rows without work have no granules)
+  }
+  return true;
+}
+// Joins what PARTS warps found for the same rows over their keys (so [PARTS][ROWS][PITCH] results, sm, sl, sd [PARTS][ROWS] references, sums, exponents of
+// the results) and writes it out, or as this CTA's part of the item.
+template <typename T, int DIM, int ROWS, int PARTS, int PITCH>
+__device__ __forceinline__ void store_results(const AttendParams& a, const Segment& seg, long long g0, const float* so, const float* sm, const float* sl,
+                                              const float* sd) {
+  constexpr int LANES = DIM / 8, AT_ONCE = 32 * ATT_WARPS / LANES;      // threads a row, each eight dims
+  const int tid = threadIdx.x, d0 = tid % LANES * 8, group = a.n_heads / a.c.heads;
+  const bool whole_item = seg.piece == 0 && seg.piece_end == seg.work.pieces;
+  const size_t slot = 2 * (size_t)blockIdx.x + (seg.cur == g0 ? 0 : 1);
+  const int r0 = seg.r0, r_last = seg.r_last, kvh = seg.kvh;
+  for (int r = tid / LANES; r < ROWS && r0 + r <= r_last; r += AT_ONCE) {
+    float top = -INFINITY, sum = 0.f, x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = 0.f;
+#pragma unroll
+    for (int v = 0; v < PARTS; ++v) top = fmaxf(top, sm[v * ROWS + r]);
+#pragma unroll
+    for (int v = 0; v < PARTS; ++v) {
+      const float mv = sm[v * ROWS + r], lv = sl[v * ROWS + r], f = mv == top ? 1.f : ex2(mv - top), fo = ex2(sd[v * ROWS + r]) * f;
+      if (lv == 0.f) continue;                          // (no key)
+      sum += lv * f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * fo;
+    }
+    if (!whole_item) {
+      store8(a.part + (slot * ROWS + r) * DIM + d0, x);
+      if (d0 == 0) reinterpret_cast<float2*>(a.part + 2 * (size_t)a.grid * ROWS * DIM)[slot * ROWS + r] = make_float2(top, sum);
+    } else {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= inv;
+      const int row = r0 + r;
+      store8(static_cast<T*>(a.out) + ((size_t)(seg.work.o + row / group) * a.n_heads + kvh * group + row % group) * DIM + d0, x);
+    }
+  }
+}
+
 // log2 x: the exponent as it is, which is all there is to a power of two, and the mantissa's to 2^-22.
 __device__ __forceinline__ float lg2(float x) {
   const uint32_t w = __float_as_uint(x);
@@ -128,6 +259,134 @@ __device__ __forceinline__ void cp4(void* smem_dst, const void* gmem_src) {
 // part of the probabilities' operand of the second product; this order makes them keys 16 j + c + {0, 4, 8, 12}, which reads values without bank conflicts.
 __device__ __forceinline__ int unit_key(int nt, int n) { return 16 * (nt >> 1) + (n >> 1) + 4 * ((nt & 1) * 2 + (n & 1)); }
 
+// What a warp keeps of its rows (thread's row g of each eight) between units.
+template <int NQ>
+struct Softmax {
+  float m[NQ], d[NQ], l[NQ];           // reference of the scores, exponent of probability * scale beyond it, sum of probabilities
+  float up[NQ][2], down[NQ][2];        // what goes on a score, and the power of two that a sum of what comes out is multiplied by
+  float ve[2], vs_of[2];               // log2 of the values' scales of the last unit, and these
+  bool large;                          // scores whose steps in FP32 are a quarter and more
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      m[q] = d[q] = -INFINITY;
+      l[q] = up[q][0] = up[q][1] = down[q][0] = down[q][1] = 0.f;
+    }
+    ve[0] = ve[1] = 0.f;
+    vs_of[0] = vs_of[1] = -1.f;
+    large = false;
+  }
+};
+constexpr int P_BITS = 15;
+constexpr float SLACK = 8.f;
+// A unit's probabilities from its scores s (times tk: exponents), masked ones -inf: pf [score tile] holds two keys' of row g, times their values' scale
+// vs0 (TWO: the second half's vs1) as described below, ready to be the second product's operand.  Results acc move along when a reference does.
+template <int NQ, int ND, bool TWO, bool WIDE>
+__device__ __forceinline__ void probabilities(Softmax<NQ>& st, float (&s)[(NQ + 1) / 2][4][4], float (&tk)[NQ][2], float vs0, float vs1, float (&acc)[NQ][ND][4],
+                                              uint32_t (&pf)[WIDE ? 2 : 1][NQ][4], int c) {
+  // has any row a new maximum, or its values' scale another exponent?
+  const bool other_scale = vs0 != st.vs_of[0] || (TWO && vs1 != st.vs_of[1]);
+  if (other_scale) {
+    st.vs_of[0] = vs0;
+    st.ve[0] = lg2(vs0);
+    if (TWO) { st.vs_of[1] = vs1; st.ve[1] = lg2(vs1); }
+  }
+  float x[NQ][2];
+  bool moved = false;
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    const float(*sq4)[4] = s[q / 2];
+    const int h = 2 * (q & 1);
+    float x0 = fmaxf(max3(sq4[0][h], sq4[0][h + 1], sq4[1][h]), sq4[1][h + 1]), x1 = max3(sq4[2][h], sq4[2][h + 1], sq4[3][h]);
+    if (!TWO) x0 = max3(x0, x1, sq4[3][h + 1]);
+    else x1 = fmaxf(x1, sq4[3][h + 1]);
+    x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
+    x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
+    if (TWO) {
+      x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
+      x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
+    }
+    x[q][0] = ceilf(x0 * tk[q][0]);                  // references are whole numbers: what goes from one to another is an exact power of two
+    x[q][1] = TWO ? ceilf(x1 * tk[q][1]) : x[q][0];
+    moved |= x[q][0] > st.m[q] || x[q][0] - st.m[q] + st.ve[0] > st.d[q];
+    if (TWO) moved |= x[q][1] > st.m[q] || x[q][1] - st.m[q] + st.ve[1] > st.d[q];
+  }
+  moved = __any_sync(0xffffffffu, moved);
+  if (moved) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      // reference st.m of the row's scores, and exponent st.d of p * scale beyond st.m's own
+      const float most = TWO ? fmaxf(x[q][0], x[q][1]) : x[q][0];
+      const float top = most > st.m[q] ? most + SLACK : st.m[q], ref = top == -INFINITY ? 0.f : top, less = st.m[q] - ref;
+      const float with = TWO ? fmaxf(x[q][0] - ref + st.ve[0], x[q][1] - ref + st.ve[1]) : x[q][0] - ref + st.ve[0];
+      const float tod = with > st.d[q] + less ? with + SLACK : st.d[q] + less;
+      const float keep_o = tod == -INFINITY ? 0.f : ex2(less + (st.d[q] - tod));
+      st.m[q] = top;
+      st.d[q] = tod;
+      st.l[q] *= ex2(less);
+      const float k0 = __shfl_sync(0xffffffffu, keep_o, 8 * c), k1 = __shfl_sync(0xffffffffu, keep_o, 8 * c + 4);
+#pragma unroll
+      for (int i = 0; i < ND; ++i) {
+        const float2 y0 = mul2(make_float2(acc[q][i][0], acc[q][i][1]), make_float2(k0, k1)), y1 = mul2(make_float2(acc[q][i][2], acc[q][i][3]), make_float2(k0, k1));
+        acc[q][i][0] = y0.x; acc[q][i][1] = y0.y; acc[q][i][2] = y1.x; acc[q][i][3] = y1.y;
+      }
+      st.large |= fabsf(ref) > 4194304.f;
+    }
+    st.large = __any_sync(0xffffffffu, st.large);
+  }
+  if (moved || other_scale) {
+    // p, as a share of the softmax's maximum, goes into the second product times 2^(15 + e), e = log2(values' scale) - st.d.  Its sum is taken as it is
+    // and brought back afterwards, which the bounds on e keep inside FP32 (beyond them the values do not count, or the probability).
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int z = 0; z < (TWO ? 2 : 1); ++z) {
+        const float e = (float)P_BITS + fminf(fmaxf(st.ve[z] - st.d[q], -100.f), 100.f);
+        st.up[q][z] = st.m[q] == -INFINITY ? e : e - st.m[q];
+        st.down[q][z] = ex2(-e);
+      }
+  }
+  float from[NQ][TWO ? 2 : 1];
+#pragma unroll
+  for (int q = 0; q < NQ; ++q)
+#pragma unroll
+    for (int z = 0; z < (TWO ? 2 : 1); ++z) from[q][z] = st.up[q][z];
+  if (st.large) {                                       // scores in steps of a quarter and more: a difference of rounded ones, as the maximum is one of them
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const float ref = st.m[q] == -INFINITY ? 0.f : st.m[q];
+#pragma unroll
+      for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float& v = s[q / 2][nt][2 * (q & 1) + j];
+          v = __fsub_rn(__fmul_rn(v, tk[q][nt >> 1]), ref);
+        }
+      tk[q][0] = tk[q][1] = 1.f;
+#pragma unroll
+      for (int z = 0; z < (TWO ? 2 : 1); ++z) from[q][z] = -log2f(st.down[q][z]);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < NQ; ++q)
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const int zz = TWO ? z : 0;
+      const float2 t2 = make_float2(tk[q][zz], tk[q][zz]), r2 = make_float2(from[q][zz], from[q][zz]);
+      float2 sum;
+#pragma unroll
+      for (int nt = 2 * z; nt < 2 * z + 2; ++nt) {
+        float2 y = fma2(make_float2(s[q / 2][nt][2 * (q & 1)], s[q / 2][nt][2 * (q & 1) + 1]), t2, r2);
+        y.x = ex2(y.x);
+        y.y = ex2(y.y);
+        sum = nt == 2 * z ? y : add2(sum, y);
+        pf[0][q][nt] = pack_f16(y.x, y.y);
+        if constexpr (WIDE) pf[WIDE ? 1 : 0][q][nt] = rest_f16(y.x, y.y, pf[0][q][nt]);
+      }
+      st.l[q] = fmaf(sum.x + sum.y, st.down[q][zz], st.l[q]);
+    }
+}
+
 // Attention of 8 NQ rows (queries of one row of the batch times the query heads that share a key/value head) over a part of the row's keys.
 //
 // What a number goes through.  Codes are exact in FP16, and so are queries once a power of two has brought the row's largest to 2^13 (BF16 has 8 bits;
@@ -135,7 +394,8 @@ __device__ __forceinline__ int unit_key(int nt, int n) { return 16 * (nt >> 1) +
 // of two come in one factor per block and row.  Probabilities meet the values' scale before they are rounded: p * vs, as a multiple of its largest
 // value so far in the row (2^d times what the softmax's own reference m stands for), times 2^15: nothing that matters comes near FP16's subnormals,
 // however far the blocks' scales are apart.  References are whole exponents, so that results go from one to another by exact powers of two, and lie up
-// to 4 above the largest score, so that few units move them (32 rows over 16 units: in nearly all of them without).  Sums and results are FP32.
+// to 9 above the largest score, so that few units move them (without, one of 32 rows does in nearly every unit; 32 x 64 queries 126 -> 117 us with 8
+// rather than 3 to spare).  Sums and results are FP32.
 //
 // Why this shape.  What has to be read is 2 * dim bytes a key; 16 rows make 64 operations a byte of it, which mma.sync delivers several times over, so the kernel
 // is a stream of the cache with as little as possible per byte: each warp copies its own units of 32 keys through its own ring in shared memory
@@ -152,89 +412,24 @@ cache_attention_kernel(AttendParams a) {
   typedef KeyCodes<F, WIDE> Keys;
   constexpr int KSTEPS = DIM / 16, ND = DIM / 16, MT = (NQ + 1) / 2, ROWS = 8 * NQ;
   constexpr int STAGES = att_stages(DIM, NQ), STAGE = att_stage_bytes(DIM), COPIES = DIM / 16;
-  constexpr int P_BITS = 15;
-  constexpr float SLACK = 3.f;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ float2 s_rf[ROWS];                       // factor of a row's scores, and what its first product starts from
   uint4* sq = reinterpret_cast<uint4*>(smem);          // [HL][MT][KSTEPS][lane]: operands as mma wants them
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
   unsigned char* ring = smem + att_q_bytes(DIM, NQ, WIDE) + warp * STAGES * STAGE;
-  __shared__ long long s_scan[ATT_WARPS], s_base;
-  __shared__ int s_row, s_vis[ROWS];
-  __shared__ struct { RowWork work; long long at, cur; int b, piece, piece_end, kvh, r0, r_last; } s_seg;
+  __shared__ int s_vis[ROWS];
+  __shared__ Segment s_seg;
   pdl_launch();
   pdl_wait();
-  // ---- this CTA's granules ----
-  long long total = 0, mine = 0, front = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 32 * ATT_WARPS) {
-    mine = b0 + tid < a.B ? row_work(a, b0 + tid, ROWS).granules : 0;
-    long long run = mine;
-#pragma unroll
-    for (int w = 1; w < 32; w <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, run, w);
-      if (lane >= w) run += y;
-    }
-    if (lane == 31) s_scan[warp] = run;
-    __syncthreads();
-    front = total + run - mine;
-#pragma unroll
-    for (int w = 0; w < ATT_WARPS; ++w) {
-      if (w < warp) front += s_scan[w];
-      total += s_scan[w];
-    }
-    if (blockIdx.x == 0 && a.granule && b0 + tid < a.B) a.prefix[b0 + tid] = front;
-    __syncthreads();
-  }
-  if (blockIdx.x == 0 && a.granule && tid == 0) a.prefix[a.B] = total;
-  const long long ctas = min((long long)gridDim.x, total);
-  if (blockIdx.x >= ctas) return;
-  const long long g0 = cta_start(total, blockIdx.x, ctas), g1 = cta_start(total, blockIdx.x + 1, ctas);
-  if (a.B <= 32 * ATT_WARPS) {
-    if (front <= g0 && g0 < front + mine) { s_row = tid; s_base = front; }
-  } else if (warp == 0) {                     // (the same scan again, by one warp)
-    long long base = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 32) {
-      const long long x = b0 + lane < a.B ? row_work(a, b0 + lane, ROWS).granules : 0;
-      long long run = x;
-#pragma unroll
-      for (int w = 1; w < 32; w <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, run, w);
-        if (lane >= w) run += y;
-      }
-      const long long f = base + run - x;
-      if (f <= g0 && g0 < f + x) { s_row = b0 + lane; s_base = f; }
-      base += __shfl_sync(0xffffffffu, run, 31);
-      if (base > g0) break;
-    }
-  }
-  __syncthreads();
+  long long g0, g1;
+  if (!find_share(a, ROWS, s_seg, g0, g1)) return;
   const int group = a.n_heads / a.c.heads;
-  if (tid == 0) {
-    s_seg.b = s_row;
-    s_seg.at = g0 - s_base;
-    s_seg.cur = g0;
-    s_seg.work = row_work(a, s_row, ROWS);
-  }
   // What the loop over keys has no use for stays in shared memory meanwhile, for the sake of its registers.
   for (;;) {
     __syncthreads();
-    int kvh, r0, r_last, vis_min, vis_max, u0, u1;      // (of which this warp's units: the tile may see fewer than the row has)
-    {
-      const RowWork& work = s_seg.work;
-      const long long at = s_seg.at;
-      const int item = (int)(at / work.pieces), piece = (int)(at % work.pieces), piece_end = (int)min((long long)work.pieces, piece + (g1 - s_seg.cur));
-      kvh = item / work.tiles;
-      r0 = item % work.tiles * ROWS;
-      r_last = min(r0 + ROWS, work.n * group) - 1;
-      vis_min = a.causal ? work.p + r0 / group + 1 : work.p;
-      vis_max = a.causal ? work.p + r_last / group + 1 : work.p;
-      const int units = (vis_max + UNIT - 1) / UNIT;
-      const int f = min((int)((long long)work.units * piece / work.pieces), units), e = min((int)((long long)work.units * piece_end / work.pieces), units);
-      u0 = f + (int)((long long)(e - f) * warp / ATT_WARPS);
-      u1 = f + (int)((long long)(e - f) * (warp + 1) / ATT_WARPS);
-      if (tid < ROWS) s_vis[tid] = a.causal ? work.p + min(r0 + tid, r_last) / group + 1 : work.p;
-      if (tid == 0) { s_seg.piece = piece; s_seg.piece_end = piece_end; s_seg.kvh = kvh; s_seg.r0 = r0; s_seg.r_last = r_last; }
-    }
+    const SegmentKeys view = open_segment(a, ROWS, s_seg, s_vis, g1);
+    const int kvh = view.kvh, r0 = view.r0, r_last = view.r_last, vis_min = view.vis_min, vis_max = view.vis_max, n_units = view.u1 - view.u0;
+    const int u0 = view.u0 + (int)((long long)n_units * warp / ATT_WARPS), u1 = view.u0 + (int)((long long)n_units * (warp + 1) / ATT_WARPS);      // this warp's
     const int b = s_seg.b;
 
     // ---- the ring ----
@@ -366,15 +561,12 @@ cache_attention_kernel(AttendParams a) {
     // Scores: thread's row g of each eight, columns as above.  Results: dims DIM / 8 * g .. of rows 2 c and 2 c + 1 of each eight.
     constexpr bool ROW_REGS = NQ < 4;                   // (with 32 rows registers are short: read again for every unit)
     float2 row_rf[NQ];
-    float m[NQ], d[NQ], l[NQ], acc[NQ][ND][4];
-    float up[NQ][2], down[NQ][2], ve[2] = {0.f, 0.f}, vs_of[2] = {-1.f, -1.f};
-    bool large = false;                                 // scores whose steps in FP32 are a quarter and more
+    float acc[NQ][ND][4];
+    Softmax<NQ> soft;
+    soft.clear();
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       if (ROW_REGS) row_rf[q] = s_rf[q * 8 + g];
-      m[q] = d[q] = -INFINITY;
-      up[q][0] = up[q][1] = down[q][0] = down[q][1] = 0.f;
-      l[q] = 0.f;
 #pragma unroll
       for (int i = 0; i < ND; ++i)
 #pragma unroll
@@ -469,108 +661,9 @@ cache_attention_kernel(AttendParams a) {
           tk[q][1] = TWO ? fmaxf(tk[q][1], FLT_MIN) : tk[q][0];
         }
       }
-      // ---- probabilities: has any row a new maximum, or its values' scale another exponent? ----
-      const bool other_scale = sc.z != vs_of[0] || (TWO && sc.w != vs_of[1]);
-      if (other_scale) {
-        vs_of[0] = sc.z;
-        ve[0] = lg2(sc.z);
-        if (TWO) { vs_of[1] = sc.w; ve[1] = lg2(sc.w); }
-      }
-      float x[NQ][2];
-      bool moved = false;
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        const float(*sq4)[4] = s[q / 2];
-        const int h = 2 * (q & 1);
-        float x0 = fmaxf(max3(sq4[0][h], sq4[0][h + 1], sq4[1][h]), sq4[1][h + 1]), x1 = max3(sq4[2][h], sq4[2][h + 1], sq4[3][h]);
-        if (!TWO) x0 = max3(x0, x1, sq4[3][h + 1]);
-        else x1 = fmaxf(x1, sq4[3][h + 1]);
-        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
-        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
-        if (TWO) {
-          x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
-          x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
-        }
-        x[q][0] = ceilf(x0 * tk[q][0]);                  // references are whole numbers: what goes from one to another is an exact power of two
-        x[q][1] = TWO ? ceilf(x1 * tk[q][1]) : x[q][0];
-        moved |= x[q][0] > m[q] || x[q][0] - m[q] + ve[0] > d[q];
-        if (TWO) moved |= x[q][1] > m[q] || x[q][1] - m[q] + ve[1] > d[q];
-      }
-      moved = __any_sync(0xffffffffu, moved);
-      if (moved) {
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-          // reference m of the row's scores, and exponent d of p * scale beyond m's own
-          const float most = TWO ? fmaxf(x[q][0], x[q][1]) : x[q][0];
-          const float top = most > m[q] ? most + SLACK : m[q], ref = top == -INFINITY ? 0.f : top, less = m[q] - ref;
-          const float with = TWO ? fmaxf(x[q][0] - ref + ve[0], x[q][1] - ref + ve[1]) : x[q][0] - ref + ve[0];
-          const float tod = with > d[q] + less ? with + SLACK : d[q] + less;
-          const float keep_o = tod == -INFINITY ? 0.f : ex2(less + (d[q] - tod));
-          m[q] = top;
-          d[q] = tod;
-          l[q] *= ex2(less);
-          const float k0 = __shfl_sync(0xffffffffu, keep_o, 8 * c), k1 = __shfl_sync(0xffffffffu, keep_o, 8 * c + 4);
-#pragma unroll
-          for (int i = 0; i < ND; ++i) {
-            const float2 y0 = mul2(make_float2(acc[q][i][0], acc[q][i][1]), make_float2(k0, k1)), y1 = mul2(make_float2(acc[q][i][2], acc[q][i][3]), make_float2(k0, k1));
-            acc[q][i][0] = y0.x; acc[q][i][1] = y0.y; acc[q][i][2] = y1.x; acc[q][i][3] = y1.y;
-          }
-          large |= fabsf(ref) > 4194304.f;
-        }
-        large = __any_sync(0xffffffffu, large);
-      }
-      if (moved || other_scale) {
-        // p, as a share of the softmax's maximum, goes into the second product times 2^(15 + e), e = log2(values' scale) - d.  Its sum is taken as it is
-        // and brought back afterwards, which the bounds on e keep inside FP32 (beyond them the values do not count, or the probability).
-#pragma unroll
-        for (int q = 0; q < NQ; ++q)
-#pragma unroll
-          for (int z = 0; z < (TWO ? 2 : 1); ++z) {
-            const float e = (float)P_BITS + fminf(fmaxf(ve[z] - d[q], -100.f), 100.f);
-            up[q][z] = m[q] == -INFINITY ? e : e - m[q];
-            down[q][z] = ex2(-e);
-          }
-      }
-      float from[NQ][TWO ? 2 : 1];
-#pragma unroll
-      for (int q = 0; q < NQ; ++q)
-#pragma unroll
-        for (int z = 0; z < (TWO ? 2 : 1); ++z) from[q][z] = up[q][z];
-      if (large) {                                       // scores in steps of a quarter and more: a difference of rounded ones, as the maximum is one of them
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-          const float ref = m[q] == -INFINITY ? 0.f : m[q];
-#pragma unroll
-          for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              float& v = s[q / 2][nt][2 * (q & 1) + j];
-              v = __fsub_rn(__fmul_rn(v, tk[q][nt >> 1]), ref);
-            }
-          tk[q][0] = tk[q][1] = 1.f;
-#pragma unroll
-          for (int z = 0; z < (TWO ? 2 : 1); ++z) from[q][z] = -log2f(down[q][z]);
-        }
-      }
-      uint32_t pf[HL][NQ][4];                            // [score tile]: two keys' probabilities of row g, as the second product's operand
-#pragma unroll
-      for (int q = 0; q < NQ; ++q)
-#pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const int zz = TWO ? z : 0;
-          const float2 t2 = make_float2(tk[q][zz], tk[q][zz]), r2 = make_float2(from[q][zz], from[q][zz]);
-          float2 sum;
-#pragma unroll
-          for (int nt = 2 * z; nt < 2 * z + 2; ++nt) {
-            float2 y = fma2(make_float2(s[q / 2][nt][2 * (q & 1)], s[q / 2][nt][2 * (q & 1) + 1]), t2, r2);
-            y.x = ex2(y.x);
-            y.y = ex2(y.y);
-            sum = nt == 2 * z ? y : add2(sum, y);
-            pf[0][q][nt] = pack_f16(y.x, y.y);
-            if constexpr (WIDE) pf[HL - 1][q][nt] = rest_f16(y.x, y.y, pf[0][q][nt]);
-          }
-          l[q] = fmaf(sum.x + sum.y, down[q][zz], l[q]);
-        }
+      // ---- probabilities ----
+      uint32_t pf[HL][NQ][4];
+      probabilities<NQ, ND, TWO, WIDE>(soft, s, tk, sc.z, sc.w, acc, pf, c);
       // ---- times values ----
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -622,55 +715,17 @@ cache_attention_kernel(AttendParams a) {
       for (int i = 0; i < ND; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j) *reinterpret_cast<float2*>(dst + j * PITCH + 2 * i) = make_float2(acc[q][i][j], acc[q][i][2 + j]);
-      float sum = l[q];
+      float sum = soft.l[q];
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
       if (c == 0) {
         const int r = warp * ROWS + q * 8 + g;
-        sm[r] = m[q]; sl[r] = sum; sd[r] = d[q] - (float)P_BITS;
+        sm[r] = soft.m[q]; sl[r] = sum; sd[r] = soft.d[q] - (float)P_BITS;
       }
     }
     __syncthreads();
-    constexpr int LANES = DIM / 8, AT_ONCE = 32 * ATT_WARPS / LANES;      // threads a row, each eight dims
-    const int d0 = tid % LANES * 8;
-    const bool whole_item = s_seg.piece == 0 && s_seg.piece_end == s_seg.work.pieces;
-    const size_t slot = 2 * (size_t)blockIdx.x + (s_seg.cur == g0 ? 0 : 1);
-    r0 = s_seg.r0;
-    r_last = s_seg.r_last;
-    kvh = s_seg.kvh;
-    for (int r = tid / LANES; r < ROWS && r0 + r <= r_last; r += AT_ONCE) {
-      float top = -INFINITY, sum = 0.f, x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = 0.f;
-#pragma unroll
-      for (int v = 0; v < ATT_WARPS; ++v) top = fmaxf(top, sm[v * ROWS + r]);
-#pragma unroll
-      for (int v = 0; v < ATT_WARPS; ++v) {
-        const float mv = sm[v * ROWS + r], lv = sl[v * ROWS + r], f = mv == top ? 1.f : ex2(mv - top), fo = ex2(sd[v * ROWS + r]) * f;
-        if (lv == 0.f) continue;                          // (no key)
-        sum += lv * f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * fo;
-      }
-      if (!whole_item) {
-        store8(a.part + (slot * ROWS + r) * DIM + d0, x);
-        if (d0 == 0) reinterpret_cast<float2*>(a.part + 2 * (size_t)a.grid * ROWS * DIM)[slot * ROWS + r] = make_float2(top, sum);
-      } else {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= inv;
-        const int row = r0 + r;
-        store8(static_cast<T*>(a.out) + ((size_t)(s_seg.work.o + row / group) * a.n_heads + kvh * group + row % group) * DIM + d0, x);
-      }
-    }
-    const int done = s_seg.piece_end - s_seg.piece;
-    if (s_seg.cur + done >= g1) break;
-    __syncthreads();                             // shared memory is the next item's
-    if (tid == 0) {
-      s_seg.cur += done;
-      s_seg.at += done;
-      while (s_seg.at == s_seg.work.granules) { s_seg.at = 0; s_seg.work = row_work(a, ++s_seg.b, ROWS); }   // (rows without work have no granules)
-    }
+    store_results<T, DIM, ROWS, ATT_WARPS, PITCH>(a, s_seg, g0, so, sm, sl, sd);
+    if (!next_segment(a, ROWS, s_seg, g1)) break;
   }
 }
 

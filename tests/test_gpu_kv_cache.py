@@ -274,14 +274,14 @@ def test_rows_that_cannot_be_done_are_latched_and_the_others_done(what, code):
 def bound(dtype, want, weight, size, floor, keys, dim):
     """How far a result may be off.  A score: dim products and their sum, the scales and the query's 22 bits (2^-24 and 2^-22 of sum |q k|, as
     exponents); an exponential 2^-21; sums over keys 2^-24 each addition; both numerator and denominator.  BF16 besides: probabilities of 11 bits,
-    and the result's own half step.  A probability times its block's scale goes into the product as an FP16 number that is 2^11
-    to 2^15 for the largest so far in the row (whose reference is a whole exponent, up to 4 above it); FP16's steps are 2^-24 at the least, so one that
-    is too small for 11 bits is off by at most 2^-25 there, 2^-36 of the largest, times its code."""
+    and the result's own half step.  A probability times its block's scale goes into the product as an FP16 number that is 2^6
+    to 2^15 for the largest so far in the row (whose reference is a whole exponent, up to 9 above it); FP16's steps are 2^-24 at the least, so one that
+    is too small for 11 bits is off by at most 2^-25 there, 2^-31 of the largest, times its code."""
     e = (dim + 8) * 2.0 ** -24 + 2.0 ** -22
     rel = 2 * (e * size[..., None] + 2.0 ** -21 + keys * 2.0 ** -24) + 2.0 ** -22
-    tol = rel * weight + 2.0 ** -36 * floor + 1e-37
+    tol = rel * weight + 2.0 ** -31 * floor + 1e-37
     if dtype == "bf16":
-        tol = (rel + 2.0 ** -11) * weight + 2.0 ** -36 * floor + 2.0 ** -8 * np.abs(want) * 1.01 + 1e-37
+        tol = (rel + 2.0 ** -11) * weight + 2.0 ** -31 * floor + 2.0 ** -8 * np.abs(want) * 1.01 + 1e-37
     return tol
 
 
