@@ -140,7 +140,8 @@ __device__ __forceinline__ void store8(bf16* p, const float* x) {
 // largest scale that its block ever had.
 // A CTA takes a block of tokens' keys or values of one head at a time, `tiles` of them one after the other, with the next one's loads under way; numbers
 // stay in registers between the maximum and the codes, so that everything is read and written once.  Bound by bytes: 8 prompts of 2500 to 8190
-// tokens, 8 heads of 128, BF16 to E4M3, APPEND_FIGURES.
+// tokens, 8 heads of 128, BF16 to E4M3, 59 us, 4.5 TB/s (a tile a CTA 100 us, two 76, four 64, eight 64 in a build before); a third of the time the
+// issue slots are idle, in the barrier of each tile and its round trips.
 // grid = (ceil(2 * heads / tiles), blocks a row's new tokens may touch, B), block = max(32, block * dim / 32) threads.
 constexpr int VECS = 4;                // vectors of eight numbers a thread holds
 __device__ __forceinline__ uint32_t max_bits(uint32_t m, uint4 v, float) {      // largest |x| as an integer: FP32 ...
@@ -268,7 +269,8 @@ cache_append_kernel(Cache c, const T* __restrict__ k, const T* __restrict__ v, s
   }
 }
 
-// Reads tokens start[b] .. of row b back into k, v [M, heads, dim], tile after tile as above.  Bound by bytes: the prompts above, READ_FIGURES.
+// Reads tokens start[b] .. of row b back into k, v [M, heads, dim], tile after tile as above.  Bound by bytes, two thirds of them written: the prompts
+// above, E4M3 to BF16, 53 us, 5.0 TB/s (a tile a CTA 72 us).
 // grid as above, block = max(32, block * dim / 64).
 constexpr int READ_VECS = 4;           // vectors of sixteen codes a thread holds
 template <typename T, typename F>
