@@ -367,8 +367,8 @@ int ad_cache_read(const ad_kv_cache* cache, void* k, void* v, int32_t dtype, con
  * Positions beyond are never looked at.  max_keys: longest row to plan for; longer ones are computed as well, only slower.
  * Probabilities and sums are held in FP32.  In front of the product with the values, probabilities (times the scale of the
  * values' block) are rounded to 11 bits with BF16 queries, to 22 with FP32 ones, and no finer than 2^-30 of a query's largest.
- * scratch: ad_cache_attention_scratch_bytes() of device memory, 256-byte aligned (NULL when that is 0); calls that may overlap
- * need scratch of their own. */
+ * scale: positive, 1e30 at most.  scratch: ad_cache_attention_scratch_bytes() of device memory, 256-byte aligned (NULL when
+ * that is 0); calls that may overlap need scratch of their own. */
 size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* cache, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new,
                                         int32_t max_keys);
 int ad_cache_attention(const ad_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads,
@@ -386,10 +386,10 @@ int ad_cache_attention(const ad_kv_cache* cache, const void* q, int32_t dtype, i
  * r [B] are uniform in [0, 1).  Comparisons are decided as in 64-bit arithmetic.
  * tokens [B, kmax] receives the verified tokens and -1 behind them, n_accepted [B] their count: 1 .. k_b, cut at the first
  * accepted `eos` (negative: none); 0 for idle rows.  ad_force_commit takes both as they are.
- * Scores of -inf are probability 0, +inf share all of it; a NaN counts as -inf.  A position without any score above -inf takes id 0.
- * A draft >= vocab counts as a negative slot and latches AD_ERR_ARG; so does a row outside of 0 .. M or longer than kmax,
- * which comes back as idle.  scratch: device memory, 256-byte aligned, ad_accept_sampled_scratch_bytes() of it; calls that may
- * overlap need scratch of their own. */
+ * Scores of -inf are probability 0, +inf share all of it; a NaN counts as -inf.  A position without any score above -inf takes
+ * id 0.  vocab is at most 2^20, temperature at least 1e-30.  A draft >= vocab counts as a negative slot and latches AD_ERR_ARG;
+ * so does a row outside of 0 .. M or longer than kmax, which comes back as idle.  scratch: device memory, 256-byte aligned,
+ * ad_accept_sampled_scratch_bytes() of it; calls that may overlap need scratch of their own. */
 size_t ad_accept_sampled_scratch_bytes(int32_t M, int32_t vocab, int32_t with_draft);
 int ad_accept_sampled(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int32_t dtype,
                       float temperature, int32_t vocab, const int32_t* off, const int32_t* drafts, int32_t kmax, int32_t B,

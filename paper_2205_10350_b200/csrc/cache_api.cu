@@ -185,7 +185,7 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
   if (!known_dtype(dtype)) return arg_fault(entry, "unknown dtype");
   if (!attend_sizes(c, n_heads, max_new)) return arg_fault(entry, "query heads must be a multiple of the cache's, at most 65535, and max_new times their ratio at most 2^24 (times them, 2^30)");
   if (max_keys < 0) return arg_fault(entry, "negative number of keys");
-  if (!(scale > 0.f) || !(scale < INFINITY)) return arg_fault(entry, "the scale must be positive and finite");
+  if (!(scale > 0.f) || !(scale <= 1e30f)) return arg_fault(entry, "the scale must be positive, and 1e30 at most");
   if (M == 0) return AD_OK;
   if (!q || !out || !aligned(q, 16) || !aligned(out, 16)) return arg_fault(entry, "queries and result must be 16-byte aligned");
   if (q_stride < (int64_t)n_heads * c->head_dim || q_stride % (int64_t)(16 / dtype_bytes(dtype)))
@@ -213,13 +213,14 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
 
 namespace {
 // Parts a row's scores are split into: four CTAs an SM where there are few rows, as long as every thread has a vector; at least so many that no
-// thread adds up more than 32 vectors.
+// thread adds up more than 32 vectors.  64 parts at most: the accept kernel's bound on the sums' errors counts on it.
+constexpr int kMaxVocab = 1 << 20;
 int score_parts(int32_t rows, int32_t vocab) {
   const int vecs = (vocab + 3) / 4;                                  // (FP32's; BF16 has half as many)
   const int least = (vecs + 32 * sampled::STAT_THREADS - 1) / (32 * sampled::STAT_THREADS);
   const int most = std::max(1, vecs / (2 * sampled::STAT_THREADS));
   const int fill = (4 * op_num_sms() + std::max(rows, 1) - 1) / std::max(rows, 1);
-  return std::max(least, std::min(most, fill));
+  return std::max(least, std::min({most, fill, 64}));
 }
 }  // namespace
 
@@ -249,7 +250,7 @@ cudaError_t launch_accept(const sampled::Params& p, cudaStream_t st) {
 }  // namespace
 
 extern "C" size_t ad_accept_sampled_scratch_bytes(int32_t M, int32_t vocab, int32_t with_draft) {
-  if (M < 0 || M > INT_MAX / 2 || vocab < 1 || vocab > (1 << 24)) return 0;
+  if (M < 0 || M > INT_MAX / 2 || vocab < 1 || vocab > kMaxVocab) return 0;
   const int z = with_draft ? 2 : 1;
   return (size_t)std::max(M, 1) * z * score_parts(M * z, vocab) * sizeof(sampled::Stat);
 }
@@ -261,7 +262,7 @@ extern "C" int ad_accept_sampled(const void* target, int64_t target_stride, cons
   const char* entry = "ad_accept_sampled";
   if (!off || !drafts || !u || !r || !tokens || !n_accepted) return arg_fault(entry, "null argument");
   if (!known_dtype(dtype)) return arg_fault(entry, "unknown dtype");
-  if (B < 1 || B > kMaxRows || kmax < 1 || kmax > kMaxNew || M < 0 || M > INT_MAX / 2 || vocab < 1 || vocab > (1 << 24)) return arg_fault(entry, "size out of range");
+  if (B < 1 || B > kMaxRows || kmax < 1 || kmax > kMaxNew || M < 0 || M > INT_MAX / 2 || vocab < 1 || vocab > kMaxVocab) return arg_fault(entry, "size out of range");
   if (!(temperature >= 1e-30f) || !(temperature < INFINITY)) return arg_fault(entry, "the temperature must be positive (1e-30 at least) and finite");
   if (M > 0 && !target) return arg_fault(entry, "null scores");
   if (!aligned(target, dtype_bytes(dtype)) || !aligned(draft, dtype_bytes(dtype))) return arg_fault(entry, "misaligned scores");

@@ -247,7 +247,7 @@ cache_append_kernel(Cache c, const T* __restrict__ k, const T* __restrict__ v, s
         for (int j = 0; j < 8; ++j) {
           const uint32_t m = __float_as_uint(x[j]) & 0x7fffffffu;
           if (m < 0x7f800000u) finite = max(finite, m);
-          else if (m > 0x7f800000u) { nan = true; reinterpret_cast<T*>(raw[u])[j] = from_f32<T>(0.f); }
+          else if (m > 0x7f800000u && token(u) >= live) { nan = true; reinterpret_cast<T*>(raw[u])[j] = from_f32<T>(0.f); }
         }
       }
       if (nan) latch_error(status, AD_ERR_ARG);

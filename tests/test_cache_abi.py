@@ -59,14 +59,14 @@ def test_append_refusals(lib, bad):
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(q=P + 2), dict(out=None), dict(out=P + 4), dict(dtype=7), dict(stride=255), dict(stride=260), dict(heads=3),
                                  dict(heads=0), dict(off=None), dict(len=None), dict(B=0), dict(M=-5), dict(max_new=0), dict(max_keys=-1), dict(scale=0.0),
-                                 dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(heads=65534, stride=65534 * 64, max_new=600),
+                                 dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38), dict(heads=65534, stride=65534 * 64, max_new=600),
                                  dict(max_new=1 << 20)])
 def test_attention_refusals(lib, bad):
     _refused(lib, lib.ad_cache_attention(C.byref(_cache()), *{**ATTEND, **bad}.values(), None, None))
 
 
 @pytest.mark.parametrize("bad", [dict(target=None), dict(target=P + 2), dict(draft=P + 1), dict(ts=999), dict(ds=999), dict(dtype=3), dict(t=0.0), dict(t=-1.0),
-                                 dict(t=float("nan")), dict(t=float("inf")), dict(t=1e-35), dict(vocab=0), dict(vocab=1 << 25), dict(off=None), dict(drafts=None),
+                                 dict(t=float("nan")), dict(t=float("inf")), dict(t=1e-35), dict(vocab=0), dict(vocab=(1 << 20) + 1, ts=1 << 21, ds=1 << 21), dict(off=None), dict(drafts=None),
                                  dict(kmax=0), dict(B=0), dict(M=-1), dict(u=None), dict(r=None), dict(tokens=None), dict(n=None), dict(scratch=None),
                                  dict(scratch=P + 128)])
 def test_sampled_verification_refusals(lib, bad):

@@ -266,6 +266,18 @@ def test_tokens_are_distributed_as_the_verifier_says(drafter):
     assert (n == 1).all() and (np.abs(share - p) <= 6 * np.sqrt(p * (1 - p) / B)).all()
 
 
+def test_batches_without_any_draft():
+    none = np.zeros((3, 4), np.int32)
+    for M in (0, 5):
+        tokens, n = run(torch.zeros((M, 100)), torch.zeros((M, 100)), none, [0, 0, 0, 0], np.zeros((3, 4)), np.zeros(3))
+        assert (tokens == -1).all() and (n == 0).all()
+
+
+def test_one_row_of_the_largest_vocabulary():
+    target, _, drafts, off, u, r = problem([2], 1 << 20, "fp32", 61, False)
+    check(target, None, drafts, off, u, r)
+
+
 def test_captured_calls_and_other_streams():
     target, draft, drafts, off, u, r = problem([5, 9, 2], 7001, "bf16", 37)
     dev = [x.to(DEV) for x in (target, draft)] + [torch.tensor(np.asarray(x), dtype=dt, device=DEV) for x, dt in
