@@ -62,9 +62,13 @@ cudaError_t by_types(int32_t dtype, int32_t format, Fn f) {
 int arg_fault(const char* entry, const char* why) { return op_fail(AD_ERR_ARG, entry, why); }
 int launched(const char* entry, cudaError_t e) { return e == cudaSuccess ? AD_OK : op_fail(AD_ERR_CUDA, entry, cudaGetErrorString(e)); }
 
-// Heads' tiles that a CTA of ad_cache_append and ad_cache_read takes one after the other: four where there are CTAs enough without, else one.
+// Heads' tiles that a CTA of ad_cache_append and ad_cache_read takes one after the other, by how often one tile a CTA would fill the GPU (768 threads an
+// SM, what registers allow): four beyond eight times, two beyond two and a half, else one.  Appending, one / two / four: 1.7 times (32 rows x 9-64 tokens, 64 wide)
+// 6.9 / 7.9 / 11.1 us, 3.4 times (128 wide) 12.6 / 12.1 / 13.3, 4.9 times (8 rows x 100-1000) 23.9 / 19.8 / 19.6, 37 times (8 prompts) 100 / 76 / 64.
 int tiles_a_cta(const ad_kv_cache* c, int32_t B, int32_t max_new) {
-  return (int64_t)2 * c->n_kv_heads * ((max_new + c->block - 1) / c->block) * B >= 16 * (int64_t)op_num_sms() ? 4 : 1;
+  const int64_t threads = (int64_t)2 * c->n_kv_heads * ((max_new + c->block - 1) / c->block) * B * std::max(32, c->block * c->head_dim / (8 * kv::VECS));
+  const int64_t filled = 768 * (int64_t)op_num_sms();
+  return threads >= 8 * filled ? 4 : 2 * threads >= 5 * filled ? 2 : 1;
 }
 dim3 tile_grid(const ad_kv_cache* c, int32_t B, int32_t max_new, int tiles) {
   return dim3((2 * c->n_kv_heads + tiles - 1) / tiles, (max_new + c->block - 2) / c->block + 1, B);
