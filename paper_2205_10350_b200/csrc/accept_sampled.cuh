@@ -33,9 +33,13 @@ struct Params {
 // What exponents are taken against: finite whatever the maximum is.
 __device__ __forceinline__ float reference(float top, float c) { return isinf(top) ? 0.f : top * c; }
 
+// What brings a sum from one maximum's reference to a larger one's; nothing where there was no score yet (an empty sum has no reference: with the new one far
+// below zero the factor would be infinite, and zero times it no number).
+__device__ __forceinline__ float rescale(float top, float ref, float c) { return top == -INFINITY ? 0.f : kv::ex2(reference(top, c) - ref); }
+
 __device__ __forceinline__ void join(Stat& a, const Stat& b, float c) {
   const float top = fmaxf(a.top, b.top), ref = reference(top, c);
-  a.sum = a.sum * kv::ex2(reference(a.top, c) - ref) + b.sum * kv::ex2(reference(b.top, c) - ref);
+  a.sum = a.sum * rescale(a.top, ref, c) + b.sum * rescale(b.top, ref, c);
   a.top = top;
 }
 
@@ -58,7 +62,7 @@ score_stats_kernel(Params p) {
   float top = -INFINITY, sum = 0.f;
   auto rebase = [&](float t) {                            // returns what exponents are taken against from here on
     const float ref = reference(t, p.c);
-    sum *= kv::ex2(reference(top, p.c) - ref);
+    sum *= rescale(top, ref, p.c);
     top = t;
     return ref;
   };

@@ -312,3 +312,77 @@ def test_calls_that_are_refused():
                 dict(temperature=0.0), dict(temperature=float("nan")), dict(target_t=a["target_t"].t()), dict(status_t=a["off_t"])):
         with pytest.raises(binding.AdError):
             binding.accept_sampled(**{**a, **bad})
+
+
+# ---------------------------------------------------------------------------------------------------------
+# ranges of scores and temperatures
+# ---------------------------------------------------------------------------------------------------------
+def sums_of_parts(target, draft, temperature):
+    """(largest score, sum of exponentials) that a call leaves in its scratch for every part of every row of scores, [scores, M, parts, 2]."""
+    lib = binding.load()
+    M, V = target.shape
+    z = 1 if draft is None else 2
+    nbytes = lib.ad_accept_sampled_scratch_bytes(M, V, z - 1)
+    dev = [None if x is None else x.to(DEV) for x in (target, draft)]
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device=DEV)
+    scratch = torch.full((nbytes // 4,), float("nan"), device=DEV)
+    one, tokens, count = torch.zeros((1, M), device=DEV), i32(*[0] * M), i32(0)
+    rc = lib.ad_accept_sampled(dev[0].data_ptr(), V, dev[1].data_ptr() if z == 2 else None, V, 1 if target.dtype is torch.bfloat16 else 0, temperature, V,
+                               i32(0, M).data_ptr(), i32(*[0] * M).data_ptr(), M, 1, M, one.data_ptr(), one.data_ptr(), -1, tokens.data_ptr(),
+                               count.data_ptr(), scratch.data_ptr(), nbytes, None, torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    torch.cuda.synchronize()
+    return scratch.view(z, M, -1, 2).cpu().double().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [3, 1000, 32000])
+@pytest.mark.parametrize("shift,temperature", [(0.0, 1.0), (-100.0, 1.0), (-200.0, 0.7), (-3e4, 1.0), (-20.0, 0.01), (100.0, 0.05), (3e4, 1.0)])
+def test_sums_are_finite_wherever_the_scores_lie(dtype, V, shift, temperature):
+    """A row's maximum may lie anywhere: sums that are no numbers cost every position a sweep of its own."""
+    g = torch.Generator().manual_seed(V)
+    target, draft = ((torch.randn((3, V), generator=g) * 2 + shift).to(TORCH[dtype]) for _ in range(2))
+    target[1, : V // 2] = -float("inf")
+    stats = sums_of_parts(target, draft, temperature)
+    assert np.isfinite(stats[..., 1]).all() and (stats[..., 1] >= 0).all()
+    assert np.array_equal(stats[..., 0].max(2), torch.stack([target, draft]).double().amax(2).numpy())
+    assert (stats[..., 1].max(2) > 0.1).all()
+    check(*_drawn(target, draft, temperature, [3], V), temperature=temperature)
+
+
+def _drawn(target, draft, temperature, new, seed):
+    """The arguments of a call on these scores, with drafts drawn from the drafter (or the verifier)."""
+    g = np.random.default_rng(seed)
+    drafts, off = np.full((len(new), max(new)), -1), offsets_of(new)
+    for b, n in enumerate(new):
+        for i in range(n):
+            drafts[b, i] = g.choice(target.shape[1], p=probabilities((target if draft is None else draft)[off[b] + i].double().numpy(), temperature))
+    return target, draft, drafts, off, g.random(drafts.shape, dtype=np.float32), g.random(len(new), dtype=np.float32)
+
+
+def offsets_of(new):
+    return [0] + [int(x) for x in np.cumsum(new)]
+
+
+def test_scores_far_below_zero_cost_no_more_than_others():
+    """64 drafts that are all kept, where every one that 32 bits leave open would take a sweep over the vocabulary: scores around -200 within three
+    times the time of scores around zero (sweeps one after the other would be twenty times it)."""
+    V, n = 32000, 64
+    target = problem([n], V, "fp32", 71, True)[0]
+    args = [torch.tensor(np.asarray(a), dtype=dt, device=DEV) for a, dt in ((target.argmax(1)[None], torch.int32), ([0, n], torch.int32), (np.full((1, n), 0.1), torch.float32),
+                                                                            ([0.5], torch.float32))]
+    times = []
+    for shift in (0.0, -200.0):
+        t = (target + shift).to(DEV)
+        best = 1e9
+        for _ in range(8):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda._sleep(1000000)
+            start.record()
+            tokens, count = binding.accept_sampled(t, t, *args)
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, start.elapsed_time(end))
+        assert int(count[0]) == n
+        times.append(best)
+    assert times[1] <= 3 * times[0], times
