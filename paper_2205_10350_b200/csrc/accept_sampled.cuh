@@ -30,16 +30,20 @@ struct Params {
   int* status;
 };
 
-// What exponents are taken against: finite whatever the maximum is.
-__device__ __forceinline__ float reference(float top, float c) { return isinf(top) ? 0.f : top * c; }
-
-// What brings a sum from one maximum's reference to a larger one's; nothing where there was no score yet (an empty sum has no reference: with the new one far
-// below zero the factor would be infinite, and zero times it no number).
-__device__ __forceinline__ float rescale(float top, float ref, float c) { return top == -INFINITY ? 0.f : kv::ex2(reference(top, c) - ref); }
+// What exponents are taken against: a whole number, finite whatever the maximum is; at or above the maximum's own while that is below 2^22, next to it beyond.
+// (Roundings by additions: conversions would go through the pipe of the exponentials, which is the one that is full.)
+constexpr float WHOLE = 12582912.f;                                  // 1.5 * 2^23
+__device__ __forceinline__ float reference(float top, float c) { return isinf(top) ? 0.f : __fadd_ru(__fmul_rn(top, c), WHOLE) - WHOLE; }
+// What brings a sum from one reference to that of a larger maximum.  Both are whole, so this is a power of two, put together from its exponent: however often
+// the maximum moves, sums are not rounded for it.  At most one: from an empty sum, which has no reference (0), nothing is scaled up.
+__device__ __forceinline__ float rescale(float from, float to) {
+  const float k = fmaxf(fminf(from - to, 0.f), -127.f);
+  return __int_as_float(__float_as_int(k + (WHOLE + 127.f)) << 23);     // (the sum's last nine bits are k + 127: the exponent, or 0)
+}
 
 __device__ __forceinline__ void join(Stat& a, const Stat& b, float c) {
   const float top = fmaxf(a.top, b.top), ref = reference(top, c);
-  a.sum = a.sum * rescale(a.top, ref, c) + b.sum * rescale(b.top, ref, c);
+  a.sum = a.sum * rescale(reference(a.top, c), ref) + b.sum * rescale(reference(b.top, c), ref);
   a.top = top;
 }
 
@@ -59,12 +63,12 @@ score_stats_kernel(Params p) {
   const int vecs = (p.vocab - head) / W, tail = head + vecs * W;
   const int each = (vecs + p.parts - 1) / p.parts, v0 = min((int)blockIdx.y * each, vecs), v1 = min(v0 + each, vecs);
   const uint4* body = reinterpret_cast<const uint4*>(row + head);
-  float top = -INFINITY, sum = 0.f;
-  auto rebase = [&](float t) {                            // returns what exponents are taken against from here on
-    const float ref = reference(t, p.c);
-    sum *= rescale(top, ref, p.c);
+  float top = -INFINITY, sum = 0.f, ref = 0.f;
+  auto rebase = [&](float t) {                            // to the reference of maximum t
+    const float to = reference(t, p.c);
+    sum *= rescale(ref, to);
+    ref = to;
     top = t;
-    return ref;
   };
   auto load = [&](uint4* raw, int v) {
 #pragma unroll
@@ -85,7 +89,7 @@ score_stats_kernel(Params p) {
     float t = top;
 #pragma unroll
     for (int j = 0; j < N; j += 2) t = kv::max3(t, x[j], x[j + 1]);
-    const float ref = rebase(t);
+    rebase(t);
     float2 y[N / 2];
 #pragma unroll
     for (int j = 0; j < N / 2; ++j) {
@@ -100,7 +104,7 @@ score_stats_kernel(Params p) {
   }
   if (blockIdx.y == 0) {
     const int i = threadIdx.x;
-    auto one = [&](float x) { const float ref = rebase(fmaxf(top, x)); sum += kv::ex2(fmaf(x, p.c, -ref)); };
+    auto one = [&](float x) { rebase(fmaxf(top, x)); sum += kv::ex2(fmaf(x, p.c, -ref)); };
     if (i < head) one(to_f32(row[i]));
     if (tail + i < p.vocab) one(to_f32(row[tail + i]));      // (fewer than W left)
   }
@@ -239,9 +243,9 @@ accept_sampled_kernel(Params p) {
     const double qd = two ? exp2((double)xq * p.c - reference(sq.top, p.c)) : 1.0;
     const double want = (double)__ldg(p.u + (size_t)b * p.kmax + i) * qd * (double)sp.sum;
     const double have = exp2((double)xp * p.c - reference(sp.top, p.c)) * (double)sq.sum;
-    // How far off the two may be, relatively.  A sum: chains of at most 128 additions in all, 2^-24 each, an exponential within 2^-21 of what its
-    // rounded exponent asks for; 1.6e-5 for both sums.  The exponents' factor c is off by 2^-24 of itself, which moves a probability by that share
-    // of its distance from the top and of the mean distance (below 64 where it counts: what lies further off has no weight).
+    // How far off the two may be, relatively.  A sum: chains of at most 128 additions in all, 2^-24 each, and an exponential within 2^-21; 1.6e-5 for both
+    // sums.  Moving maxima round nothing.  An exponent is rounded to 2^-24 of itself and the factor c is off by as much, which moves a sum by these shares of
+    // the mean distance from the top (20 exponents at most, with 2^20 scores) and an exponential by one of its own distance; 4e-6 and the last term.
     const double away = (isinf(xp) ? 0.0 : (double)(sp.top - xp)) + (two && !isinf(xq) ? (double)(sq.top - xq) : 0.0);
     const double doubt = 3e-5 + 1.2e-7 * away * p.c;
     if (fabs(want - have) <= doubt * fmax(fabs(want), have)) return NEAR;

@@ -386,3 +386,22 @@ def test_scores_far_below_zero_cost_no_more_than_others():
         assert int(count[0]) == n
         times.append(best)
     assert times[1] <= 3 * times[0], times
+
+
+def test_scores_that_rise_over_a_large_vocabulary():
+    """Every round and every part of a row moves the maximum, and random numbers lie next to the borders of decisions."""
+    V, n = 1 << 20, 6
+    g = np.random.default_rng(3)
+    rise = torch.linspace(0, 9, V, dtype=torch.float64)
+    target, draft = ((rise + 0.3 * torch.tensor(g.standard_normal((2 * n, V)))).float() for _ in range(2))
+    drafts, u = g.integers(V - 2000, V, (2, n)), np.zeros((2, n), np.float32)
+    for b in range(2):
+        for i in range(n):
+            p, q = (probabilities(x[b * n + i].double().numpy(), 1.0)[drafts[b, i]] for x in (target, draft))
+            if p >= 0.999 * q:
+                draft[b * n + i, drafts[b, i]] += float(np.log(p / q) + 0.5)
+                q = probabilities(draft[b * n + i].double().numpy(), 1.0)[drafts[b, i]]
+            edge = p / q * (1 + (-1e-5 if i < n - 1 else 1e-5))
+            u[b, i] = edge
+    tokens, count = check(target, draft, drafts, [0, n, 2 * n], u, g.random(2, dtype=np.float32))
+    assert (count == n).all()
