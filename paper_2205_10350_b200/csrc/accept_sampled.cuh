@@ -30,7 +30,7 @@ struct Params {
   int* status;
 };
 
-// What exponents are taken against: a whole number, finite whatever the maximum is; at or above the maximum's own while that is below 2^22, next to it beyond.
+// What exponents are taken against: a whole number, finite whatever the maximum is; at or above the maximum's own while that is below 2^22, within a step of FP32 beyond.
 // (Roundings by additions: conversions would go through the pipe of the exponentials, which is the one that is full.)
 constexpr float WHOLE = 12582912.f;                                  // 1.5 * 2^23
 __device__ __forceinline__ float reference(float top, float c) { return isinf(top) ? 0.f : __fadd_ru(__fmul_rn(top, c), WHOLE) - WHOLE; }
@@ -238,11 +238,14 @@ accept_sampled_kernel(Params p) {
     my_top[0] = sp.top;
     my_top[1] = sq.top;
     if (d < 0) return DROP;
+    const float rp = reference(sp.top, p.c), rq = reference(sq.top, p.c);
     if (!isfinite(sp.top) || !isfinite(sp.sum) || !isfinite(sq.top) || !isfinite(sq.sum)) return NEAR;
+    // Scores over T beyond 2^26: FP32's steps put the reference so far from the maximum (10 exponents there, 128 and more from 2^30 on) that sums vanish.
+    if (!(fabsf(rp) <= 67108864.f) || !(fabsf(rq) <= 67108864.f)) return NEAR;
     if (xp != xp || xq != xq) return NEAR;
-    const double qd = two ? exp2((double)xq * p.c - reference(sq.top, p.c)) : 1.0;
+    const double qd = two ? exp2((double)xq * p.c - rq) : 1.0;
     const double want = (double)__ldg(p.u + (size_t)b * p.kmax + i) * qd * (double)sp.sum;
-    const double have = exp2((double)xp * p.c - reference(sp.top, p.c)) * (double)sq.sum;
+    const double have = exp2((double)xp * p.c - rp) * (double)sq.sum;
     // How far off the two may be, relatively.  A sum: chains of at most 128 additions in all, 2^-24 each, and an exponential within 2^-21; 1.6e-5 for both
     // sums.  Moving maxima round nothing.  An exponent is rounded to 2^-24 of itself and the factor c is off by as much, which moves a sum by these shares of
     // the mean distance from the top (20 exponents at most, with 2^20 scores) and an exponential by one of its own distance; 4e-6 and the last term.

@@ -405,3 +405,30 @@ def test_scores_that_rise_over_a_large_vocabulary():
             u[b, i] = edge
     tokens, count = check(target, draft, drafts, [0, n, 2 * n], u, g.random(2, dtype=np.float32))
     assert (count == n).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("drafter", [True, False])
+@pytest.mark.parametrize("temperature", [1e-6, 1e-8, 1e-9, 1e-10, 1e-20, 1e-30])
+def test_temperatures_that_leave_next_to_one_token(dtype, drafter, temperature):
+    """Scores over such a temperature lie beyond 2^24, 2^31 and FP32's range.  Tied best tokens, a step of the type between best and second, drafts on
+    either, random numbers on both sides of the shares that ties leave."""
+    V, n, B = 700, 3, 16
+    g = np.random.default_rng(9)
+    target = torch.tensor(g.standard_normal((B * n, V)), dtype=torch.float32).to(TORCH[dtype])
+    drafts = np.zeros((B, n), np.int64)
+    step = float(torch.finfo(TORCH[dtype]).eps)
+    for b in range(B):
+        for i in range(n):
+            m, ids = b * n + i, g.permutation(V)[:3]
+            top = float(torch.tensor(8 * (1 + g.random())).to(TORCH[dtype]))           # between 8 and 16: steps of 8 eps
+            target[m, ids[0]] = top
+            target[m, ids[1]] = top if b % 2 else top - 8 * step
+            target[m, ids[2]] = top - 8 * step
+            drafts[b, i] = ids[b // 2 % 3]
+    draft = None
+    if drafter:
+        draft = target[:, torch.randperm(V, generator=torch.Generator().manual_seed(1))].clone()
+        draft[::2] = target[::2]
+    u = np.where(g.random((B, n)) < 0.5, 0.3, 0.7).astype(np.float32)
+    check(target, draft, drafts, offsets_of([n] * B), u, g.random(B, dtype=np.float32), temperature=temperature)
