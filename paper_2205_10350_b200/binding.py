@@ -641,7 +641,8 @@ def accept_sampled(target_t, draft_t, drafts_t, off_t, u_t, r_t, temperature=1.0
             _refuse(entry, "the drafter's scores are like the verifier's in type, shape and place")
         draft_stride, draft_one = draft_t.stride()
         draft = draft_t.data_ptr()
-        one = max(one, draft_one)
+        if draft_one != 1:
+            one = draft_one
     if one != 1 and V > 1:
         _refuse(entry, "a row's scores must lie next to each other")
     if M < 2:

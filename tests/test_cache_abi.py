@@ -162,3 +162,51 @@ int main() {
     subprocess.run([NVCC, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+class _OnDevice:
+    """A tensor of the CPU that says it lies on device 0; what would be launched on it is looked at instead."""
+
+    def __init__(self, t):
+        self.t = t
+
+    def get_device(self):
+        return 0
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    @property
+    def shape(self):
+        return self.t.shape
+
+
+class _NoLaunch:
+    def ad_accept_sampled_scratch_bytes(self, *_):
+        return 4096
+
+    def ad_accept_sampled(self, *a):
+        raise AssertionError("reached the library")
+
+
+def _accept(monkeypatch, target, draft, B=1, kmax=2):
+    import torch
+    monkeypatch.setattr(binding, "_lib", _NoLaunch())
+    monkeypatch.setattr(binding, "_call_on", lambda dev, call, *a: call(*a, None))
+    i32 = lambda *s: _OnDevice(torch.zeros(s, dtype=torch.int32))
+    f32 = lambda *s: _OnDevice(torch.zeros(s))
+    return binding.accept_sampled(_OnDevice(target), None if draft is None else _OnDevice(draft), i32(B, kmax), i32(B + 1), f32(B, kmax), f32(B))
+
+
+@pytest.mark.parametrize("M", [1, 2])
+def test_scores_that_do_not_lie_next_to_each_other_are_refused(monkeypatch, M):
+    """One score for a whole row (a stride of zero) is not a row of scores: kernels would read behind it."""
+    import torch
+    full, column, spread = torch.zeros(M, 40), torch.zeros(M, 1).expand(M, 40), torch.zeros(M, 80)[:, ::2]
+    wide = torch.zeros(M * 100).as_strided((M, 40), (100, 0))
+    for t, d in ((column, None), (spread, None), (wide, None), (column, full), (full, column), (wide, full), (full, wide), (full, spread), (spread, full), (wide, wide)):
+        with pytest.raises(binding.AdError, match="next to each other|overlap"):
+            _accept(monkeypatch, t, d)
+    for t, d in ((full, None), (full, full), (torch.zeros(M, 60)[:, 7:47], full)):
+        with pytest.raises(AssertionError, match="reached"):
+            _accept(monkeypatch, t, d)
