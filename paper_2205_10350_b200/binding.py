@@ -453,6 +453,9 @@ def _raise(lib, rc):
     raise AdError(rc, msg.decode() if msg else "")
 
 
+_TOO_LARGE = "sizes must lie between 0 and 2^31 - 1"
+
+
 # Torch's names that a call needs, looked up once: an import statement and attribute lookups cost a call as much as its checks.
 _INT32 = _FP32 = _BF16 = _get_device = _get_stream = None
 
@@ -558,6 +561,8 @@ class KvCache:
 def cache_append(cache, k_t, v_t, off_t, len_t, max_new, status_t=None):
     """Writes k_t, v_t [M, n_kv_heads, head_dim] (float32 or bfloat16, views of a wider array as well) behind the len_t[b] tokens of every row."""
     entry, lib = "ad_cache_append", _lib or load()
+    if max_new >> 31:
+        _refuse(entry, _TOO_LARGE)
     B = cache._batch(entry, off_t, len_t)
     tokens = cache._tokens(entry, k_t, cache.n_kv_heads)
     if cache._tokens(entry, v_t, cache.n_kv_heads) != tokens:
@@ -573,6 +578,8 @@ def cache_read(cache, off_t, start_t, tokens, max_tokens, dtype=None, status_t=N
     """Positions start_t[b] .. of every row, off_t[b + 1] - off_t[b] of them: (k, v) [tokens, n_kv_heads, head_dim] in dtype (default bfloat16).
     Tokens that no row covers are left uninitialised."""
     entry, lib = "ad_cache_read", _lib or load()
+    if (tokens | max_tokens) >> 31:
+        _refuse(entry, _TOO_LARGE)
     B = cache._batch(entry, off_t, start_t)
     dtype = dtype or _BF16
     if dtype is not _BF16 and dtype is not _FP32:
@@ -590,6 +597,8 @@ def cache_attention(cache, q_t, off_t, len_t, max_new, max_keys, causal=True, sc
     """Attention of q_t [M, n_heads, head_dim] over the cache; returns [M, n_heads, head_dim] in q_t's type (`out`, if given).  Causal: query i of
     row b sees len_t[b] + i + 1 positions (its block has been appended), otherwise all see len_t[b].  scale: head_dim ** -0.5 unless given."""
     entry, lib = "ad_cache_attention", _lib or load()
+    if (max_new | max_keys) >> 31:
+        _refuse(entry, _TOO_LARGE)
     B = cache._batch(entry, off_t, len_t)
     if q_t.dim() != 3:
         _refuse(entry, "queries are [tokens, heads, head_dim]")
@@ -634,6 +643,8 @@ def accept_sampled(target_t, draft_t, drafts_t, off_t, u_t, r_t, temperature=1.0
     if not (_matrix(u_t, shape, _FP32, dev) and _vector(r_t, B, _FP32, dev)):
         _refuse(entry, f"random numbers are contiguous float32 tensors [B, kmax] and [B] on device {dev}")
     M, V = target_t.shape
+    if (M | V | B | kmax) >> 31:
+        _refuse(entry, _TOO_LARGE)
     stride, one = target_t.stride()
     draft_stride, draft = V, None
     if draft_t is not None:

@@ -210,3 +210,27 @@ def test_scores_that_do_not_lie_next_to_each_other_are_refused(monkeypatch, M):
     for t, d in ((full, None), (full, full), (torch.zeros(M, 60)[:, 7:47], full)):
         with pytest.raises(AssertionError, match="reached"):
             _accept(monkeypatch, t, d)
+
+
+def test_sizes_that_32_bits_do_not_hold_are_refused(monkeypatch):
+    """The library's sizes are 32-bit; a larger one would arrive as another number, a vocabulary of 2^32 + 5 as one of five."""
+    import torch
+    big = (1 << 32) + 5
+    for M, V in ((1, big), (big, 1), (1, 1 << 31)):
+        scores = torch.empty((M, V), device="meta")
+        for draft in (None, scores):
+            with pytest.raises(binding.AdError, match="2\\^31"):
+                _accept(monkeypatch, scores, draft)
+    # a cache's calls, up to where they would reach the library
+    cache = object.__new__(binding.KvCache)
+    cache._dev, cache.device, cache._table_rows, cache.n_kv_heads, cache.head_dim, cache._scratch, cache._ref = 0, "cuda:0", 4, 2, 64, {}, None
+    i32 = lambda n: _OnDevice(torch.zeros(n, dtype=torch.int32))
+    x = _OnDevice(torch.zeros(3, 2, 64, dtype=torch.bfloat16))
+    monkeypatch.setattr(binding, "_BF16", torch.bfloat16)
+    monkeypatch.setattr(binding, "_INT32", torch.int32)
+    for bad in (big, 1 << 31, -1):
+        for call in (lambda: binding.cache_append(cache, x, x, i32(2), i32(1), bad), lambda: binding.cache_attention(cache, x, i32(2), i32(1), bad, 10),
+                     lambda: binding.cache_attention(cache, x, i32(2), i32(1), 3, bad), lambda: binding.cache_read(cache, i32(2), i32(1), 3, bad),
+                     lambda: binding.cache_read(cache, i32(2), i32(1), bad, 3)):
+            with pytest.raises(binding.AdError, match="2\\^31"):
+                call()
