@@ -367,7 +367,7 @@ int ad_cache_read(const ad_kv_cache* cache, void* k, void* v, int32_t dtype, con
  * Positions beyond are never looked at.  max_keys: longest row to plan for; longer ones are computed as well, only slower.
  * Probabilities and sums are held in FP32.  In front of the product with the values, probabilities (times the scale of the
  * values' block) are rounded to 11 bits with BF16 queries, to 22 with FP32 ones, and no finer than 2^-30 of a query's largest.
- * scale: positive, 1e30 at most.  scratch: ad_cache_attention_scratch_bytes() of device memory, 256-byte aligned (NULL when
+ * scale: positive, 1e30 at most; a query with a score (the scale in it) beyond FP32's range may come out as NaN.  scratch: ad_cache_attention_scratch_bytes() of device memory, 256-byte aligned (NULL when
  * that is 0); calls that may overlap need scratch of their own. */
 size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* cache, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new,
                                         int32_t max_keys);

@@ -235,15 +235,17 @@ __device__ __forceinline__ void codes_f16(Int8, uint32_t w, uint32_t& lo, uint32
   lo = *reinterpret_cast<const uint32_t*>(&x);
   hi = *reinterpret_cast<const uint32_t*>(&y);
 }
-// The same for the first product, which takes multiples of them plus a bias: (code + BIAS) / FACTOR, with BIAS times the sum of a row's query (and
+// The same for the first product, which takes multiples of them plus a bias: (code + BIAS) / 2^FACTOR_BITS, with BIAS times the sum of a row's query (and
 // its sign) where the product starts from.  INT8's c + 128 alone in FP16's low byte is that many times 2^-24, which saves a subtraction per pair and
 // costs a bit of the sum; FP32 queries take the codes as they are (their error would double: 5e-7 to 1.2e-6).
 template <typename F, bool WIDE> struct KeyCodes {
-  static constexpr float BIAS = 0.f, FACTOR = 1.f;
+  static constexpr float BIAS = 0.f;
+  static constexpr int FACTOR_BITS = 0;
   static __device__ __forceinline__ void f16(uint32_t w, uint32_t& lo, uint32_t& hi) { codes_f16(F(), w, lo, hi); }
 };
 template <> struct KeyCodes<Int8, false> {
-  static constexpr float BIAS = 128.f, FACTOR = 16777216.f;
+  static constexpr float BIAS = 128.f;
+  static constexpr int FACTOR_BITS = 24;
   static __device__ __forceinline__ void f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
     w ^= 0x80808080u;
     lo = __byte_perm(w, 0u, 0x4140);
@@ -420,6 +422,7 @@ cache_attention_kernel(AttendParams a) {
   constexpr int STAGES = att_stages(DIM, NQ), STAGE = att_stage_bytes(DIM), COPIES = DIM / 16;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ float2 s_rf[ROWS];                       // factor of a row's scores, and what its first product starts from
+  __shared__ float s_rest[ROWS];                      // power of two that the factor has no room for; one in all but the oddest of rows
   uint4* sq = reinterpret_cast<uint4*>(smem);          // [HL][MT][KSTEPS][lane]: operands as mma wants them
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
   unsigned char* ring = smem + att_q_bytes(DIM, NQ, WIDE) + warp * STAGES * STAGE;
@@ -559,11 +562,20 @@ cache_attention_kernel(AttendParams a) {
       }
 #pragma unroll
       for (int w = 16; w; w >>= 1) total += __shfl_xor_sync(0xffffffffu, total, w);
-      if (lane == 0 && r < ROWS) {
-        s_rf[r] = make_float2(a.scale * (1.f / up) * Keys::FACTOR, -Keys::BIAS / Keys::FACTOR * total);
-      }
+      if (lane == 0 && r < ROWS) s_rf[r] = make_float2(__int_as_float((int)e), total);
     }
     __syncthreads();
+    int odd = 0;                                        // whether any row of the tile has a rest
+    if (tid < ROWS) {
+      // scale / up * 2^FACTOR_BITS: the part within 2^-120 .. 2^121 meets the keys' scale first, what is left of the powers of two their product
+      const float2 v = s_rf[tid];
+      const int power = __float_as_int(v.x) - 140 + Keys::FACTOR_BITS, room = 247 - (int)(__float_as_uint(a.scale) >> 23), first = min(max(power, room - 240), room);
+      s_rf[tid] = make_float2(ldexpf(a.scale, first), -Keys::BIAS / (float)(1 << Keys::FACTOR_BITS) * v.y);
+      s_rest[tid] = ldexpf(1.f, power - first);
+      odd = power != first;
+    }
+    // The loop's branch for units that some row does not see whole is the one for tiles with a rest, too.
+    const int whole_until = __syncthreads_or(odd) ? 0 : vis_min;
     // Scores: thread's row g of each eight, columns as above.  Results: dims DIM / 8 * g .. of rows 2 c and 2 c + 1 of each eight.
     constexpr bool ROW_REGS = NQ < 4;                   // (with 32 rows registers are short: read again for every unit)
     float2 row_rf[NQ];
@@ -655,7 +667,7 @@ cache_attention_kernel(AttendParams a) {
         tk[q][0] = rf[q] * fabsf(sc.x);
         tk[q][1] = TWO ? rf[q] * fabsf(sc.y) : tk[q][0];
       }
-      if (u * UNIT + UNIT > vis_min || sc.x < 0.f || (TWO && sc.y < 0.f)) {
+      if (u * UNIT + UNIT > whole_until || sc.x < 0.f || (TWO && sc.y < 0.f)) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
 #pragma unroll
@@ -663,8 +675,9 @@ cache_attention_kernel(AttendParams a) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
               if (u * UNIT + unit_key(nt, 2 * c + j) >= s_vis[q * 8 + g] || (TWO && nt >= 2 ? sc.y : sc.x) < 0.f) s[q / 2][nt][2 * (q & 1) + j] = -INFINITY;
-          tk[q][0] = fmaxf(tk[q][0], FLT_MIN);           // (not 0 times -inf)
-          tk[q][1] = TWO ? fmaxf(tk[q][1], FLT_MIN) : tk[q][0];
+          const float rest = s_rest[q * 8 + g];
+          tk[q][0] = fmaxf(tk[q][0] * rest, FLT_MIN);    // (not 0 times -inf)
+          tk[q][1] = TWO ? fmaxf(tk[q][1] * rest, FLT_MIN) : tk[q][0];
         }
       }
       // ---- probabilities ----

@@ -503,3 +503,32 @@ def test_calls_that_are_refused():
     # queries whose heads the cache's do not divide
     with pytest.raises(binding.AdError, match="multiple"):
         binding.cache_attention(cache, numbers((4, 3, 64), "bf16", 1).to(DEV), off, ln, 4, 4)
+
+
+# ---------------------------------------------------------------------------------------------------------
+# ends of the range
+# ---------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+@pytest.mark.parametrize("q_bits,k_bits,scale", [(0, 0, 1e30), (20, 0, 1e30), (60, -70, 1e30), (100, -100, 1e20), (120, 0, 0.125), (126, -120, 1e30), (-100, 80, 1e30), (-90, 110, 1.0)])
+def test_scores_are_finite_wherever_their_factors_lie(fmt, dtype, dim, q_bits, k_bits, scale):
+    """Scale, queries and keys at the ends of their ranges, scores inside of FP32's and far apart: each query gets its best key's value."""
+    n = 40
+    g = torch.Generator().manual_seed(dim)
+    k, v = torch.randn((n, 1, dim), generator=g), torch.randn((n, 1, dim), generator=g)
+    q = torch.randn((5, 1, dim), generator=g)
+    q /= q.abs().amax(2, keepdim=True)
+    k, q, v = ((x * 2.0 ** e).to(TORCH[dtype]) for x, e in ((k, k_bits), (q, q_bits), (v, 0)))
+    cache, model = both(2, 1, dim, 32, fmt)
+    binding.cache_append(cache, k.to(DEV), v.to(DEV), ints([0, n]), ints([0]), max_new=n)
+    model.append(k.double().numpy(), v.double().numpy(), [0, n], [0])
+    got = binding.cache_attention(cache, q.to(DEV), ints([0, 5]), ints([n]), 5, n, causal=False, scale=scale).double().cpu().numpy()[:, 0]
+    kk, vv = model.values(0, 0, n)[:, 0], model.values(1, 0, n)[:, 0]
+    scores = q.double().numpy()[:, 0] @ kk.T * float(np.float32(scale))
+    assert np.abs(scores).max() < 2.0 ** 125
+    rest = np.sort(scores, 1)
+    assert (rest[:, -1] - rest[:, -2]).min() > 200            # (one key has all of it)
+    assert (np.abs(got - vv[scores.argmax(1)]) <= 2.0 ** -8 * np.abs(vv[scores.argmax(1)])).all()
