@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda_fp16.h>
+#include <float.h>
 #include <limits.h>
 
 #include "ad_common.cuh"
@@ -210,7 +211,10 @@ cache_append_kernel(Cache c, const T* __restrict__ k, const T* __restrict__ v, s
         F::decode4(raw[u][0].x, x);
         F::decode4(raw[u][0].y, x + 4);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= old;
+        for (int j = 0; j < 8; ++j) {
+          x[j] *= old;
+          if (isinf(x[j])) x[j] = copysignf(FLT_MAX, x[j]);      // (FP32's largest had been rounded up to 2^128: FLT_MAX has the same code)
+        }
       } else {
         load8(reinterpret_cast<const T*>(raw[u]), x);
       }

@@ -532,3 +532,19 @@ def test_scores_are_finite_wherever_their_factors_lie(fmt, dtype, dim, q_bits, k
     rest = np.sort(scores, 1)
     assert (rest[:, -1] - rest[:, -2]).min() > 200            # (one key has all of it)
     assert (np.abs(got - vv[scores.argmax(1)]) <= 2.0 ** -8 * np.abs(vv[scores.argmax(1)])).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_live_codes_that_stand_for_more_than_fp32_holds(dtype, fmt):
+    """The type's largest numbers round up to 2^128.  Tokens that come to them later leave them what they are."""
+    block, heads, dim = 16, 2, 32
+    cache, model = both(1, heads, dim, block, fmt)
+    x = numbers((3, heads, dim), dtype, 5)
+    x[0, 0, 3], x[0, 1, 4] = torch.finfo(TORCH[dtype]).max, torch.finfo(TORCH[dtype]).min
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for p in range(3):
+        binding.cache_append(cache, x[p: p + 1].to(DEV), x[p: p + 1].to(DEV), ints([0, 1]), ints([p]), max_new=1, status_t=status)
+        model.append(x[p: p + 1].double().numpy(), x[p: p + 1].double().numpy(), [0, 1], [p])
+        same(cache, model)
+    assert int(status.item()) == 0
