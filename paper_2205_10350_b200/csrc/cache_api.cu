@@ -119,11 +119,14 @@ extern "C" int ad_cache_read(const ad_kv_cache* c, void* k, void* v, int32_t dty
 namespace {
 constexpr int kGranule = 8, kItemFixed = 16;
 struct AttendPlan { int nq, row_tiles, grid, granule; bool shared; };
+// max_keys, but no more than a row can hold (which leaves room for roundings below 2^31).
+int32_t longest_row(const ad_kv_cache* c, int32_t max_keys) { return std::min(max_keys, c->table_stride * c->block); }
 // Rows of queries a CTA takes: 8 or 16 where that is all there are, else 32, which make the most of a key's codes once they are FP16.  Keys that are
 // too few to be split leave the GPU to as many CTAs as there are tiles of rows: then tiles are made smaller while all are resident at once
 // (8 x 25 queries in FP32 over 400 keys, 8 heads: 20.7 -> 14.1 us).
 AttendPlan attend_plan(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
   AttendPlan plan;
+  max_keys = longest_row(c, max_keys);
   const int rows = max_new * (n_heads / c->n_kv_heads), pieces = std::max(1, (max_keys + kv::UNIT - 1) / kv::UNIT / kGranule);
   auto items = [&](int nq) { return (int64_t)B * c->n_kv_heads * ((rows + 8 * nq - 1) / (8 * nq)); };
   auto resident = [&](int nq) { return (int64_t)op_num_sms() * kv::att_resident(c->head_dim, nq); };
@@ -131,7 +134,7 @@ AttendPlan attend_plan(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t
   while (pieces == 1 && plan.nq > 1 && items(plan.nq / 2) <= resident(plan.nq / 2)) plan.nq /= 2;
   plan.row_tiles = (rows + 8 * plan.nq - 1) / (8 * plan.nq);
   plan.granule = pieces > 1 ? kGranule : 0;
-  plan.grid = (int)std::min(resident(plan.nq), items(plan.nq) * pieces);
+  plan.grid = (int)std::min(resident(plan.nq), std::min(resident(plan.nq), items(plan.nq)) * pieces);     // (items times pieces alone may pass 64 bits)
   plan.shared = plan.grid > 6 * items(plan.nq);
   return plan;
 }
@@ -203,7 +206,7 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
   a.causal = causal != 0; a.scale = scale * (float)M_LOG2E; a.status = status;
   // More than half of L2 would not be there any more for the next call, and drives out what others keep there (1 x 200001 keys 104 -> 91 us); tiles of
   // the same row read one another's keys from L2.
-  a.stream_once = plan.row_tiles == 1 && (int64_t)B * max_keys * c->n_kv_heads * c->head_dim * 2 > (64 << 20);
+  a.stream_once = plan.row_tiles == 1 && (double)B * longest_row(c, max_keys) * c->n_kv_heads * c->head_dim * 2 > (64 << 20);
   a.B = B; a.grid = plan.grid; a.granule = plan.granule; a.fixed = kItemFixed;
   a.prefix = static_cast<long long*>(scratch); a.part = reinterpret_cast<float*>(static_cast<char*>(scratch) + attend_prefix_bytes(B));
   cudaStream_t st = static_cast<cudaStream_t>(stream);

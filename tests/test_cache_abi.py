@@ -234,3 +234,16 @@ def test_sizes_that_32_bits_do_not_hold_are_refused(monkeypatch):
                      lambda: binding.cache_read(cache, i32(2), i32(1), bad, 3)):
             with pytest.raises(binding.AdError, match="2\\^31"):
                 call()
+
+
+@pytest.mark.parametrize("heads,max_new", [(4, 3), (2, 1 << 19), (64, 1 << 10)])
+def test_longer_rows_than_there_can_be_are_planned_as_the_longest(lib, heads, max_new):
+    """max_keys up to INT_MAX ("no bound") plans like the capacity of a row, for a single row and for the most that a batch can have."""
+    for table_stride, B in ((300, 1), (300, 65535), ((2 ** 31 - 2 ** 19 - 1) // 32, 1), ((2 ** 31 - 2 ** 19 - 1) // 32, 65535)):
+        c = C.byref(_cache(table_stride=table_stride))
+        need = [lib.ad_cache_attention_scratch_bytes(c, 1, heads, B, max_new, n) for n in (table_stride * 32, 2 ** 31 - 1, 2 ** 31 - 31, 2 ** 31 - 32)]
+        assert need[0] > 0 and len(set(need)) == 1, need
+        # as many parts at the most as twice the CTAs that an SM and 4096 SMs could hold, and a place per row
+        assert need[0] <= 2 * 5 * 4096 * 32 * (64 + 2) * 4 + 8 * (B + 2)
+        _refused(lib, lib.ad_cache_attention(c, *{**ATTEND, "heads": heads, "stride": heads * 64, "B": B, "max_new": max_new, "max_keys": 2 ** 31 - 1,
+                                                  "nbytes": need[0] - 1}.values(), None, None), binding.AD_ERR_CAPACITY)
