@@ -365,8 +365,9 @@ int ad_cache_read(const ad_kv_cache* cache, void* k, void* v, int32_t dtype, con
  * causal != 0 (self-attention of a block, appended before): query i of row b sees the row's first len[b] + i + 1 positions;
  * causal == 0 (keys of an encoder): all queries of the row see its first len[b].  A query that sees nothing gets zeros.
  * Positions beyond are never looked at.  max_keys: longest row to plan for; longer ones are computed as well, only slower.
- * Probabilities and sums are held in FP32.  In front of the product with the values, probabilities (times the scale of the
- * values' block) are rounded to 11 bits with BF16 queries, to 22 with FP32 ones, and no finer than 2^-30 of a query's largest.
+ * Scores, probabilities and sums are held in FP32.  In front of their products, queries are rounded to 22 bits (BF16: as they are), no finer than 2^-38 of
+ * a query's largest number, and probabilities (times the scale of the values' block) to 11 bits with BF16 queries, no finer than 2^-37 of a query's
+ * largest, and to 22 bits with FP32 ones, no finer than 2^-50 of it.
  * scale: positive, 1e30 at most; a query with a score (the scale in it) beyond FP32's range may come out as NaN.  scratch: ad_cache_attention_scratch_bytes() of device memory, 256-byte aligned (NULL when
  * that is 0); calls that may overlap need scratch of their own. */
 size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* cache, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new,

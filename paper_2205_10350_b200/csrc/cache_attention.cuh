@@ -206,10 +206,15 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   return w;
 }
 __device__ __forceinline__ float2 unpack_f16(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
-// What rounding a pair to FP16 leaves over, in FP16.
+// What rounding a pair to FP16 leaves over, in FP16, 2^UP times as much.
+template <int UP = 0>
 __device__ __forceinline__ uint32_t rest_f16(float lo, float hi, uint32_t w) {
   const float2 f = unpack_f16(w);
-  return pack_f16(lo - f.x, hi - f.y);
+  return pack_f16((lo - f.x) * (float)(1 << UP), (hi - f.y) * (float)(1 << UP));
+}
+__device__ __forceinline__ uint32_t times_f16(uint32_t w, float f) {
+  const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(f));
+  return *reinterpret_cast<const uint32_t*>(&x);
 }
 __device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -280,12 +285,16 @@ struct Softmax {
   }
 };
 constexpr int P_BITS = 15;
-constexpr float SLACK = 8.f;
+constexpr int REST_UP = 11;             // FP32's second operands are taken this many binary places up, and meet values that far down: steps of 2^-35
+// How far above a new largest score references are put, so that fewer units move them: each place is one that small probabilities lose at FP16's lower end.
+// BF16: 2, which keeps keys that another one leads by 20 nats to BF16's half step (32 x 64 queries: none 137 us, 2 or 3 134, 8 130); FP32: none (161 us, 8 157).
+__host__ __device__ constexpr float att_slack(bool fp32) { return fp32 ? 0.f : 2.f; }
 // A unit's probabilities from its scores s (times tk: exponents), masked ones -inf: pf [score tile] holds two keys' of row g, times their values' scale
 // vs0 (TWO: the second half's vs1) as described below, ready to be the second product's operand.  Results acc move along when a reference does.
 template <int NQ, int ND, bool TWO, bool WIDE>
 __device__ __forceinline__ void probabilities(Softmax<NQ>& st, float (&s)[(NQ + 1) / 2][4][4], float (&tk)[NQ][2], float vs0, float vs1, float (&acc)[NQ][ND][4],
                                               uint32_t (&pf)[WIDE ? 2 : 1][NQ][4], int c) {
+  constexpr float SLACK = att_slack(WIDE);
   // has any row a new maximum, or its values' scale another exponent?
   const bool other_scale = vs0 != st.vs_of[0] || (TWO && vs1 != st.vs_of[1]);
   if (other_scale) {
@@ -383,7 +392,7 @@ __device__ __forceinline__ void probabilities(Softmax<NQ>& st, float (&s)[(NQ + 
         y.y = ex2(y.y);
         sum = nt == 2 * z ? y : add2(sum, y);
         pf[0][q][nt] = pack_f16(y.x, y.y);
-        if constexpr (WIDE) pf[WIDE ? 1 : 0][q][nt] = rest_f16(y.x, y.y, pf[0][q][nt]);
+        if constexpr (WIDE) pf[WIDE ? 1 : 0][q][nt] = rest_f16<REST_UP>(y.x, y.y, pf[0][q][nt]);
       }
       st.l[q] = fmaf(sum.x + sum.y, st.down[q][zz], st.l[q]);
     }
@@ -391,13 +400,13 @@ __device__ __forceinline__ void probabilities(Softmax<NQ>& st, float (&s)[(NQ + 
 
 // Attention of 8 NQ rows (queries of one row of the batch times the query heads that share a key/value head) over a part of the row's keys.
 //
-// What a number goes through.  Codes are exact in FP16, and so are queries once a power of two has brought the row's largest to 2^13 (BF16 has 8 bits;
-// FP32 goes in as two FP16 numbers, 22 bits, and so do its probabilities).  Scores are FP32: the keys' scale, the softmax scale and the query's power
+// What a number goes through.  Codes are exact in FP16.  Queries are brought to 2^13 by a power of two of their row: BF16 is exact then, and FP32 goes in as two
+// FP16 numbers, 22 bits, both down to 2^-38 of the row's largest number.  Scores are FP32: the keys' scale, the softmax scale and the query's power
 // of two come in one factor per block and row.  Probabilities meet the values' scale before they are rounded: p * vs, as a multiple of its largest
-// value so far in the row (2^d times what the softmax's own reference m stands for), times 2^15: nothing that matters comes near FP16's subnormals,
-// however far the blocks' scales are apart.  References are whole exponents, so that results go from one to another by exact powers of two, and lie up
-// to 9 above the largest score, so that few units move them (without, one of 32 rows does in nearly every unit; 32 x 64 queries 126 -> 117 us with 8
-// rather than 3 to spare).  Sums and results are FP32.
+// value so far in the row (2^d times what the softmax's own reference m stands for), times 2^15, so that blocks' scales may be far apart.  FP16's steps
+// end at 2^-24, and with them what is left of small ones: BF16's have 11 bits down to 2^-26 of the largest in their row and steps of 2^-36 of it below, FP32's, whose second
+// number is taken 2^11 times and meets values of 2^-11 for it, 22 bits down to 2^-27 and steps of 2^-49.  References are whole exponents, so that results
+// go from one to another by exact powers of two.  Sums and results are FP32.
 //
 // Why this shape.  What has to be read is 2 * dim bytes a key; 16 rows make 64 operations a byte of it, which mma.sync delivers several times over, so the kernel
 // is a stream of the cache with as little as possible per byte: each warp copies its own units of 32 keys through its own ring in shared memory
@@ -710,10 +719,15 @@ cache_attention_kernel(AttendParams a) {
             uint32_t av[4];                              // dims DIM / 8 * g + 4 x + 2 y and the next one, four keys
             codes_f16(F(), w0, av[0], av[1]);
             codes_f16(F(), w1, av[2], av[3]);
+            if constexpr (WIDE) {
+              uint32_t down[4];                          // (E4M3's smallest is 2^-9, so that these are exact)
 #pragma unroll
-            for (int h = HL - 1; h >= 0; --h)
+              for (int i = 0; i < 4; ++i) down[i] = times_f16(av[i], 1.f / (1 << REST_UP));
 #pragma unroll
-              for (int q = 0; q < NQ; ++q) mma_f16(acc[q][2 * x + y], av, pf[h][q][2 * j], pf[h][q][2 * j + 1]);
+              for (int q = 0; q < NQ; ++q) mma_f16(acc[q][2 * x + y], down, pf[HL - 1][q][2 * j], pf[HL - 1][q][2 * j + 1]);
+            }
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) mma_f16(acc[q][2 * x + y], av, pf[0][q][2 * j], pf[0][q][2 * j + 1]);
           }
       }
     }

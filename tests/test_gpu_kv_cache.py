@@ -548,3 +548,59 @@ def test_live_codes_that_stand_for_more_than_fp32_holds(dtype, fmt):
         model.append(x[p: p + 1].double().numpy(), x[p: p + 1].double().numpy(), [0, 1], [p])
         same(cache, model)
     assert int(status.item()) == 0
+
+
+def close_bound(dtype, want, weight, size, floor, keys, dim):
+    """`bound` with the end to what small probabilities lose that the header gives: the product's steps are 2^-24, a largest operand is at least 2^12
+    with BF16 queries, and 2^14 with FP32 ones, whose second number has steps of 2^-35: half of that over it, times the codes."""
+    return bound(dtype, want, weight, size, 0.0 * floor, keys, dim) + (2.0 ** -37 if dtype == "bf16" else 2.0 ** -50) * floor
+
+
+def leading_key(dtype, fmt, lead, n, heads, dim, block, value, seed):
+    """A cache whose first key leads all others by about `lead` nats for every query, and whose value is `value` times the others'."""
+    cache, model = both((n + block - 1) // block, heads, dim, block, fmt)
+    k, v, q = numbers((n, heads, dim), dtype, seed, 0.0), numbers((n, heads, dim), dtype, seed + 1, 0.0), numbers((6, heads, dim), dtype, seed + 2, 0.0)
+    k[:, :, 0], q[:, :, 0] = 0, 4.0
+    k[0] = 0
+    others = (torch.einsum("qhd,khd->qhk", q.double(), k.double()) * dim ** -0.5).amax((0, 1, 2)).item()
+    k[0, :, 0] = (others + lead) * dim ** 0.5 / 4
+    v[0] *= value
+    binding.cache_append(cache, k.to(DEV), v.to(DEV), ints([0, n]), ints([0]), max_new=n)
+    model.append(k.double().numpy(), v.double().numpy(), [0, n], [0])
+    return cache, model, q
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("n,heads,dim,block", [(30, 1, 64, 32), (90, 2, 128, 16), (2000, 2, 64, 64), (2000, 1, 32, 16), (2000, 1, 128, 128)])
+@pytest.mark.parametrize("lead", [10, 12, 14, 16, 18, 20])
+def test_keys_that_another_one_outweighs(dtype, fmt, n, heads, dim, block, lead):
+    """A first key that leads by many nats and has a value of zero or next to it, as a decoder's first token often does: what the others say is all there is to the result, and
+    is as exact as it is for keys that lead."""
+    for value in (0.0, 1e-3):
+        cache, model, q = leading_key(dtype, fmt, lead, n, heads, dim, block, value, lead + dim)
+        for causal in (False, True):
+            off, lens = [0, 6], [n - 6 if causal else n]
+            got = binding.cache_attention(cache, q.to(DEV), ints(off), ints(lens), 6, n, causal=causal)
+            want, weight, size, floor = model.attend(q.double().numpy(), off, lens, causal, dim ** -0.5)
+            tol = close_bound(dtype, want, weight, size, floor, n, dim)
+            err = np.abs(got.double().cpu().numpy() - want)
+            assert (err <= tol).all(), (value, causal, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("heads,group,dim,block", [(2, 1, 32, 16), (2, 2, 64, 32), (1, 4, 128, 64), (2, 1, 128, 16)])
+@pytest.mark.parametrize("spread", [0.3, 2.0])
+def test_blocks_of_queries_within_the_close_bound(fmt, dtype, heads, group, dim, block, spread):
+    """Ragged rows, scores close together and (where queries are large) tens of nats apart."""
+    new, lens = [1, 7, 33, 20], [0, 3 * block + 5, 129, 700]
+    cache, model = filled([p + n for p, n in zip(lens, new)], heads, dim, block, fmt, dtype, dim + block)
+    q = numbers((sum(new), heads * group, dim), dtype, 5, spread).to(DEV)
+    off = offsets(new)
+    for causal in (True, False):
+        got = binding.cache_attention(cache, q, ints(off), ints(lens), max(new), 720, causal=causal)
+        want, weight, size, floor = model.attend(q.cpu().double().numpy(), off, lens, causal, dim ** -0.5)
+        err = np.abs(got.double().cpu().numpy() - want)
+        tol = close_bound(dtype, want, weight, size, floor, 720, dim)
+        assert (err <= tol).all(), float((err / tol).max())
