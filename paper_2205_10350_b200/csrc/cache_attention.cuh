@@ -156,6 +156,8 @@ __device__ __forceinline__ bool next_segment(const AttendParams& a, int rows, Se
   }
   return true;
 }
+constexpr int P_BITS = 15;                     // results lie this many binary places above p * scale's reference
+constexpr float P_ONE = 1.f / (1 << P_BITS);
 // Joins what PARTS warps found for the same rows over their keys (so [PARTS][ROWS][PITCH] results, sm, sl, sd [PARTS][ROWS] references, sums, exponents of
 // the results) and writes it out, or as this CTA's part of the item.
 template <typename T, int DIM, int ROWS, int PARTS, int PITCH>
@@ -174,11 +176,11 @@ __device__ __forceinline__ void store_results(const AttendParams& a, const Segme
     for (int v = 0; v < PARTS; ++v) top = fmaxf(top, sm[v * ROWS + r]);
 #pragma unroll
     for (int v = 0; v < PARTS; ++v) {
-      const float mv = sm[v * ROWS + r], lv = sl[v * ROWS + r], f = mv == top ? 1.f : ex2(mv - top), fo = ex2(sd[v * ROWS + r]) * f;
+      const float mv = sm[v * ROWS + r], lv = sl[v * ROWS + r], f = mv == top ? 1.f : ex2(mv - top), fo = ex2(sd[v * ROWS + r]);
       if (lv == 0.f) continue;                          // (no key)
       sum += lv * f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * fo;
+      for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * P_ONE * fo * f;        // (one after the other: together they may be too small)
     }
     if (!whole_item) {
       store8(a.part + (slot * ROWS + r) * DIM + d0, x);
@@ -193,12 +195,16 @@ __device__ __forceinline__ void store_results(const AttendParams& a, const Segme
   }
 }
 
-// log2 x: the exponent as it is, which is all there is to a power of two, and the mantissa's to 2^-22.
-__device__ __forceinline__ float lg2(float x) {
-  const uint32_t w = __float_as_uint(x);
-  float y;
-  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(__uint_as_float((w & 0x7fffffu) | 0x3f800000u)));
-  return (float)((int)(w >> 23) - 127) + y;
+// log2 x of a positive normal number, rounded up to a whole one; and its own value, which is the same for a power of two, else to 2^-22.
+__device__ __forceinline__ float whole_lg2(float x) { return __int_as_float(0x4b400000 + (int)((__float_as_uint(x) + 0x7fffffu) >> 23) - 127) - 12582912.f; }
+__device__ __forceinline__ float lg2(float x, float whole) {
+  const uint32_t m = __float_as_uint(x) & 0x7fffffu;
+  if (m) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(__uint_as_float(m | 0x3f800000u)));
+    whole += y - 1.f;
+  }
+  return whole;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t w;
@@ -271,7 +277,7 @@ template <int NQ>
 struct Softmax {
   float m[NQ], d[NQ], l[NQ];           // reference of the scores, exponent of probability * scale beyond it, sum of probabilities
   float up[NQ][2], down[NQ][2];        // what goes on a score, and the power of two that a sum of what comes out is multiplied by
-  float ve[2], vs_of[2];               // log2 of the values' scales of the last unit, and these
+  float ve[2], vs_of[2];               // log2 of the values' scales of the last unit, rounded up, and these
   bool large;                          // scores whose steps in FP32 are a quarter and more
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -284,7 +290,7 @@ struct Softmax {
     large = false;
   }
 };
-constexpr int P_BITS = 15;
+constexpr float SPAN = 100.f;           // exponents that values' scales may be apart from p * scale's reference: 2^(15 + SPAN) and its inverse are FP32 numbers
 constexpr int REST_UP = 11;             // FP32's second operands are taken this many binary places up, and meet values that far down: steps of 2^-35
 // How far above a new largest score references are put, so that fewer units move them: each place is one that small probabilities lose at FP16's lower end.
 // BF16: 2, which keeps keys that another one leads by 20 nats to BF16's half step (32 x 64 queries: none 137 us, 2 or 3 134, 8 130); FP32: none (161 us, 8 157).
@@ -297,13 +303,16 @@ __device__ __forceinline__ void probabilities(Softmax<NQ>& st, float (&s)[(NQ + 
   constexpr float SLACK = att_slack(WIDE);
   // has any row a new maximum, or its values' scale another exponent?
   const bool other_scale = vs0 != st.vs_of[0] || (TWO && vs1 != st.vs_of[1]);
+  bool moved = false;
   if (other_scale) {
     st.vs_of[0] = vs0;
-    st.ve[0] = lg2(vs0);
-    if (TWO) { st.vs_of[1] = vs1; st.ve[1] = lg2(vs1); }
+    st.ve[0] = whole_lg2(vs0);
+    if (TWO) { st.vs_of[1] = vs1; st.ve[1] = whole_lg2(vs1); }
+    const float least = (TWO ? fmaxf(st.ve[0], st.ve[1]) : st.ve[0]) - SPAN;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) moved |= least > st.d[q];
   }
   float x[NQ][2];
-  bool moved = false;
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
     const float(*sq4)[4] = s[q / 2];
@@ -330,7 +339,7 @@ __device__ __forceinline__ void probabilities(Softmax<NQ>& st, float (&s)[(NQ + 
       const float most = TWO ? fmaxf(x[q][0], x[q][1]) : x[q][0];
       const float top = most > st.m[q] ? most + SLACK : st.m[q], ref = top == -INFINITY ? 0.f : top, less = st.m[q] - ref;
       const float with = TWO ? fmaxf(x[q][0] - ref + st.ve[0], x[q][1] - ref + st.ve[1]) : x[q][0] - ref + st.ve[0];
-      const float tod = with > st.d[q] + less ? with + SLACK : st.d[q] + less;
+      const float tod = fmaxf(with > st.d[q] + less ? with + SLACK : st.d[q] + less, (TWO ? fmaxf(st.ve[0], st.ve[1]) : st.ve[0]) - SPAN);
       const float keep_o = tod == -INFINITY ? 0.f : ex2(less + (st.d[q] - tod));
       st.m[q] = top;
       st.d[q] = tod;
@@ -347,15 +356,17 @@ __device__ __forceinline__ void probabilities(Softmax<NQ>& st, float (&s)[(NQ + 
   }
   if (moved || other_scale) {
     // p, as a share of the softmax's maximum, goes into the second product times 2^(15 + e), e = log2(values' scale) - st.d.  Its sum is taken as it is
-    // and brought back afterwards, which the bounds on e keep inside FP32 (beyond them the values do not count, or the probability).
+    // and brought back afterwards, which the bounds on e keep inside FP32: at -SPAN values do not count, and SPAN is as far as the reference lets them go.
 #pragma unroll
-    for (int q = 0; q < NQ; ++q)
+    for (int z = 0; z < (TWO ? 2 : 1); ++z) {
+      const float ve = lg2(st.vs_of[z], st.ve[z]);
 #pragma unroll
-      for (int z = 0; z < (TWO ? 2 : 1); ++z) {
-        const float e = (float)P_BITS + fminf(fmaxf(st.ve[z] - st.d[q], -100.f), 100.f);
+      for (int q = 0; q < NQ; ++q) {
+        const float e = (float)P_BITS + fminf(fmaxf(ve - st.d[q], -SPAN), SPAN);
         st.up[q][z] = st.m[q] == -INFINITY ? e : e - st.m[q];
         st.down[q][z] = ex2(-e);
       }
+    }
   }
   float from[NQ][TWO ? 2 : 1];
 #pragma unroll
@@ -753,7 +764,7 @@ cache_attention_kernel(AttendParams a) {
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
       if (c == 0) {
         const int r = warp * ROWS + q * 8 + g;
-        sm[r] = soft.m[q]; sl[r] = sum; sd[r] = soft.d[q] - (float)P_BITS;
+        sm[r] = soft.m[q]; sl[r] = sum; sd[r] = soft.d[q];
       }
     }
     __syncthreads();

@@ -604,3 +604,24 @@ def test_blocks_of_queries_within_the_close_bound(fmt, dtype, heads, group, dim,
         err = np.abs(got.double().cpu().numpy() - want)
         tol = close_bound(dtype, want, weight, size, floor, 720, dim)
         assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("gap", [60, 90, 99, 104, 112, 118])
+def test_small_probabilities_of_large_values(dtype, block, gap):
+    """Keys of probability 2^-gap whose values are 2^(gap + 7) times as large as those of the keys that lead: they are nearly all of the result."""
+    dim, n = 64, 5 * block
+    cache, model = both(5, 1, dim, block, "e4m3")
+    k, v = torch.zeros((n, 1, dim)), numbers((n, 1, dim), "fp32", gap, 0.0)
+    small = torch.arange(n) // block % 2 == 1                 # the second and the fourth block
+    q = torch.zeros((2, 1, dim))
+    q[:, :, 0], q[:, :, 1] = 1.0, 0.25
+    k[:, 0, 1] = torch.linspace(0, 1, n)
+    k[small, 0, 0] = -gap * float(np.log(2))
+    v[small] *= 2.0 ** 10
+    v[~small] *= 2.0 ** (3 - gap)
+    k, v, q = (x.to(TORCH[dtype]) for x in (k, v, q))
+    binding.cache_append(cache, k.to(DEV), v.to(DEV), ints([0, n]), ints([0]), max_new=n)
+    model.append(k.double().numpy(), v.double().numpy(), [0, n], [0])
+    attend_and_check(cache, model, q.to(DEV), [2], [n - 2], True, dtype, scale=1.0)
