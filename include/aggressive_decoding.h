@@ -334,13 +334,14 @@ int ad_linear(const void* x, const void* W, const float* bias, int32_t dtype, in
  * that the table sends to a block which does not exist (only blocks with tokens in them are looked up), latches AD_ERR_ARG in
  * *status; one whose tokens do not fit table_stride blocks latches AD_ERR_CAPACITY.  What concerns such a row or block is left
  * out, the rest is done.  status: optional device int, 0 before; the first error stays.
- * Different rows may share blocks that are full (a common prefix).  A block that a call writes must belong to one row. */
+ * Different rows may share blocks that are full (a common prefix).  A block that a call writes must belong to one row, and stand in it once.
+ * M = 0: nothing is done, and offsets and lengths are not looked at. */
 enum { AD_CACHE_E4M3 = 0,     /* sign, 4 bits of exponent, 3 of mantissa; largest code 448.  No code written is a NaN. */
        AD_CACHE_INT8 = 1 };   /* -127 .. 127 */
 typedef struct ad_kv_cache {
   void* k_codes;             /* [n_blocks, n_kv_heads, block, head_dim] bytes, 16-byte aligned */
   void* v_codes;
-  float* k_scale;            /* [n_blocks, n_kv_heads] */
+  float* k_scale;            /* [n_blocks, n_kv_heads]; adopted ones may be any positive normal numbers */
   float* v_scale;
   const int32_t* table;      /* [B, table_stride]: block i of row b; NULL: block b * table_stride + i */
   int32_t table_stride;      /* blocks of a row */

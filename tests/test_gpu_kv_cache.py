@@ -625,3 +625,36 @@ def test_small_probabilities_of_large_values(dtype, block, gap):
     binding.cache_append(cache, k.to(DEV), v.to(DEV), ints([0, n]), ints([0]), max_new=n)
     model.append(k.double().numpy(), v.double().numpy(), [0, n], [0])
     attend_and_check(cache, model, q.to(DEV), [2], [n - 2], True, dtype, scale=1.0)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("block", [16, 64])
+def test_scales_that_are_no_powers_of_two(dtype, fmt, block):
+    """Memory that is adopted may come with any scales; blocks that grow by one part in fifty move the results' reference again and again."""
+    heads, dim, n_blocks = 2, 64, 60
+    g = torch.Generator().manual_seed(block)
+    codes = [(torch.randn((n_blocks, heads, block, dim), generator=g) * (60 if fmt == "e4m3" else 30)).clamp(-127, 127) for _ in range(2)]
+    codes = [x.to(torch.float8_e4m3fn) if fmt == "e4m3" else x.round().to(torch.int8) for x in codes]
+    k_scale = 0.01 * (1 + torch.rand((n_blocks, heads), generator=g))
+    v_scale = 0.3 * 1.02 ** torch.arange(n_blocks)[:, None] * (1 + 0.1 * torch.rand((n_blocks, heads), generator=g))
+    v_scale[n_blocks // 2:] = v_scale[n_blocks // 2:].flip(0)
+    held = [x.to(DEV) for x in (*codes, k_scale, v_scale)]
+    cache = binding.KvCache(n_blocks, heads, dim, block, fmt, device=DEV, tensors=tuple(held))
+    model = Model(n_blocks, heads, dim, block, fmt)
+    model.codes = [x.double().numpy() for x in codes]
+    model.scale = [k_scale.double().numpy(), v_scale.double().numpy()]
+    n = n_blocks * block
+    for new in (3, 20):
+        q = numbers((new, 2 * heads, dim), dtype, new, 0.3).to(DEV)
+        off = [0, new]
+        got = binding.cache_attention(cache, q, ints(off), ints([n - new]), new, n)
+        want, weight, size, floor = model.attend(q.cpu().double().numpy(), off, [n - new], True, dim ** -0.5)
+        # (besides `close_bound`: the values' scale enters a probability through an exponent of 2^-22)
+        err, tol = np.abs(got.double().cpu().numpy() - want), close_bound(dtype, want, weight, size, floor, n, dim) + 2.0 ** -22 * weight
+        assert (err <= tol).all(), float((err / tol).max())
+    # and tokens that come to such blocks
+    x = numbers((5, heads, dim), dtype, 9)
+    binding.cache_append(cache, x.to(DEV), x.to(DEV), ints([0, 5]), ints([n - 9]), max_new=5)
+    model.append(x.double().numpy(), x.double().numpy(), [0, 5], [n - 9])
+    assert np.array_equal(cache.v_scale.cpu().double().numpy()[-1], model.scale[1][-1])
