@@ -432,3 +432,9 @@ def test_temperatures_that_leave_next_to_one_token(dtype, drafter, temperature):
         draft[::2] = target[::2]
     u = np.where(g.random((B, n)) < 0.5, 0.3, 0.7).astype(np.float32)
     check(target, draft, drafts, offsets_of([n] * B), u, g.random(B, dtype=np.float32), temperature=temperature)
+
+
+@pytest.mark.parametrize("dtype,drafter,V", [("bf16", True, 60000), ("fp32", True, 60000), ("fp32", False, 110000)])
+def test_many_rows_whose_weights_do_not_stay_in_shared_memory(dtype, drafter, V):
+    """Clusters of four CTAs, which keep weights of half as many ids."""
+    check(*problem([1] * 24, V, dtype, 57, drafter))

@@ -658,3 +658,25 @@ def test_scales_that_are_no_powers_of_two(dtype, fmt, block):
     binding.cache_append(cache, x.to(DEV), x.to(DEV), ints([0, 5]), ints([n - 9]), max_new=5)
     model.append(x.double().numpy(), x.double().numpy(), [0, 5], [n - 9])
     assert np.array_equal(cache.v_scale.cpu().double().numpy()[-1], model.scale[1][-1])
+
+
+# ---------------------------------------------------------------------------------------------------------
+# larger calls
+# ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("new,lens,heads,group,dim,block", [([300, 65, 129], [0, 700, 31], 2, 1, 64, 32), ([513], [1000], 1, 2, 128, 16), ([70, 1, 200], [5, 400, 0], 1, 4, 32, 128)])
+def test_prompts_of_hundreds_of_queries(dtype, new, lens, heads, group, dim, block):
+    """Tiles of queries far beyond a block's 64, within rows and across them."""
+    cache, model = filled([p + n for p, n in zip(lens, new)], heads, dim, block, "e4m3", dtype, 31)
+    q = numbers((sum(new), heads * group, dim), dtype, 6, 0.3).to(DEV)
+    attend_and_check(cache, model, q, new, lens, True, dtype)
+    attend_and_check(cache, model, q, new, lens, False, dtype, max_keys=10 ** 6)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("heads,group,dim,block", [(2, 4, 128, 64), (4, 1, 64, 16)])
+def test_long_rows_under_fp32_queries(fmt, heads, group, dim, block):
+    lens, new = [20011, 6000, 3001], [1, 5, 9]
+    cache, model = filled([p + n for p, n in zip(lens, new)], heads, dim, block, fmt, "fp32", 13)
+    q = numbers((sum(new), heads * group, dim), "fp32", 6, 0.3).to(DEV)
+    attend_and_check(cache, model, q, new, lens, True, "fp32")
