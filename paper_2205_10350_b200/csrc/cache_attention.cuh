@@ -24,7 +24,7 @@ struct AttendParams {
   int grid;                // CTAs
   int fixed;               // what an item takes besides its units, in units
   int granule;             // units that one CTA works on at the least where a row's keys are split; 0: they are not
-  float* part;             // [2 grid][tile rows][dim] sums of values, then [2 grid][tile rows] maxima and sums of exponentials
+  float* part;             // [2 grid][tile rows][dim] means of values, then [2 grid][tile rows] maxima and sums of exponentials
   long long* prefix;       // [B + 1] granules in front of each row of the batch
 };
 
@@ -169,26 +169,30 @@ __device__ __forceinline__ void store_results(const AttendParams& a, const Segme
   const size_t slot = 2 * (size_t)blockIdx.x + (seg.cur == g0 ? 0 : 1);
   const int r0 = seg.r0, r_last = seg.r_last, kvh = seg.kvh;
   for (int r = tid / LANES; r < ROWS && r0 + r <= r_last; r += AT_ONCE) {
-    float top = -INFINITY, sum = 0.f, x[8];
+    float top = -INFINITY, sum = 0.f, f[PARTS], x[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = 0.f;
 #pragma unroll
     for (int v = 0; v < PARTS; ++v) top = fmaxf(top, sm[v * ROWS + r]);
 #pragma unroll
     for (int v = 0; v < PARTS; ++v) {
-      const float mv = sm[v * ROWS + r], lv = sl[v * ROWS + r], f = mv == top ? 1.f : ex2(mv - top), fo = ex2(sd[v * ROWS + r]);
-      if (lv == 0.f) continue;                          // (no key)
-      sum += lv * f;
+      const float mv = sm[v * ROWS + r], lv = sl[v * ROWS + r];
+      f[v] = mv == top ? 1.f : ex2(mv - top);
+      if (lv != 0.f) sum += lv * f[v];                  // (else: no key)
+    }
+    // Means, not sums, which FP32 may have no room for; factor after factor, as they may have none together.
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * P_ONE * fo * f;        // (one after the other: together they may be too small)
+    for (int v = 0; v < PARTS; ++v) {
+      if (sl[v * ROWS + r] == 0.f) continue;
+      const float share = f[v] * inv * P_ONE, unit = ex2(sd[v * ROWS + r]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] += so[(v * ROWS + r) * PITCH + d0 + i] * share * unit;
     }
     if (!whole_item) {
       store8(a.part + (slot * ROWS + r) * DIM + d0, x);
       if (d0 == 0) reinterpret_cast<float2*>(a.part + 2 * (size_t)a.grid * ROWS * DIM)[slot * ROWS + r] = make_float2(top, sum);
     } else {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= inv;
       const int row = r0 + r;
       store8(static_cast<T*>(a.out) + ((size_t)(seg.work.o + row / group) * a.n_heads + kvh * group + row % group) * DIM + d0, x);
     }
@@ -823,19 +827,20 @@ cache_attention_join_kernel(AttendParams a) {
     top = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
     for (int i = tid; i < parts; i += 128) {
       if (i > tid) v = __ldcg(ml + row_of(i));
-      const float f = v.y == 0.f ? 0.f : v.x == top ? 1.f : ex2(v.x - top);      // (no key: nothing, whatever the maxima)
+      const float f = v.y == 0.f ? 0.f : v.x == top ? v.y : v.y * ex2(v.x - top);      // (no key: nothing, whatever the maxima)
       s_w[i] = f;
-      sum += v.y * f;
+      sum += f;
     }
 #pragma unroll
     for (int w = 16; w; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
     if (lane == 0) s_red[1][tid >> 5] = sum;
     __syncthreads();
     sum = (s_red[1][0] + s_red[1][1]) + (s_red[1][2] + s_red[1][3]);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     for (int s0 = grp; s0 < parts; s0 += AHEAD * GROUPS) {
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i)
-        if (s0 + i * GROUPS < parts) add(y[i], s_w[s0 + i * GROUPS]);
+        if (s0 + i * GROUPS < parts) add(y[i], s_w[s0 + i * GROUPS] * inv);
       load_parts(y, s0 + AHEAD * GROUPS);
     }
     if (grp > 0) s_x[grp - 1][tid % LANES] = x;
@@ -845,23 +850,27 @@ cache_attention_join_kernel(AttendParams a) {
     for (int i = 0; i < GROUPS - 1; ++i) add(s_x[i][tid], 1.f);
   } else {
     float top = -INFINITY;
-    for (int i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(ml + row_of(i)).x);
+    for (int i = 0; i < parts; ++i) {
+      const float2 v = __ldcg(ml + row_of(i));
+      if (v.y == 0.f) continue;                  // (no key: nothing, whatever the maxima)
+      const float most = fmaxf(top, v.x);
+      sum = v.x == top ? sum + v.y : fmaf(sum, ex2(top - most), v.x == most ? v.y : v.y * ex2(v.x - most));
+      top = most;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 4
     for (int i = 0; i < parts; ++i) {
       const float2 v = __ldcg(ml + row_of(i));
       const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part + row_of(i) * DIM + d0));
       if (v.y == 0.f) continue;
-      const float f = v.x == top ? 1.f : ex2(v.x - top);
-      sum = fmaf(v.y, f, sum);
-      add(y, f);
+      add(y, (v.x == top ? v.y : v.y * ex2(v.x - top)) * inv);
     }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = static_cast<T*>(a.out) + ((size_t)(work.o + r / group) * a.n_heads + kvh * group + r % group) * DIM + d0;
   if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(out) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+    *reinterpret_cast<float4*>(out) = x;
   } else {
-    __nv_bfloat162 w[2] = {__floats2bfloat162_rn(x.x * inv, x.y * inv), __floats2bfloat162_rn(x.z * inv, x.w * inv)};
+    __nv_bfloat162 w[2] = {__floats2bfloat162_rn(x.x, x.y), __floats2bfloat162_rn(x.z, x.w)};
     *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(w);
   }
 }

@@ -680,3 +680,18 @@ def test_long_rows_under_fp32_queries(fmt, heads, group, dim, block):
     cache, model = filled([p + n for p, n in zip(lens, new)], heads, dim, block, fmt, "fp32", 13)
     q = numbers((sum(new), heads * group, dim), "fp32", 6, 0.3).to(DEV)
     attend_and_check(cache, model, q, new, lens, True, "fp32")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("n,new,heads,group", [(400, 1, 1, 1), (3000, 2, 1, 4), (9000, 1, 1, 8), (9000, 30, 4, 1)])
+def test_values_whose_sums_pass_fp32(dtype, fmt, n, new, heads, group):
+    """Results are means of values: thousands of 2^120 and more have one, though no sum."""
+    dim, block = 64, 64
+    cache, model = both((n + block - 1) // block, heads, dim, block, fmt)
+    k, v = numbers((n, heads, dim), dtype, 1, 0.0), numbers((n, heads, dim), dtype, 2, 0.0)
+    v = (v.float().abs() * 2.0 ** 122).to(TORCH[dtype])
+    binding.cache_append(cache, k.to(DEV), v.to(DEV), ints([0, n]), ints([0]), max_new=n)
+    model.append(k.double().numpy(), v.double().numpy(), [0, n], [0])
+    q = numbers((new, heads * group, dim), dtype, 3, 0.0).to(DEV)
+    attend_and_check(cache, model, q, [new], [n - new], True, dtype)
