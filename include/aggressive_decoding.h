@@ -215,7 +215,8 @@ int ad_sync(ad_handle* h);
 
 /* Debug: scores of the last ad_verify_block (or, with which = 1, of the last ad_draft_block) written out as
  * FP32 [M, vocab] (device pointer), M = sum of k_b, rows packed in row order.  This materialises what the
- * fused projection+argmax kernel never writes; for parity tests only. */
+ * fused projection+argmax kernel never writes: for parity tests, and where a decision needs the scores themselves
+ * (ad_accept_sampled).  Waits for the handle's stream before it writes. */
 int ad_debug_logits(ad_handle* h, int32_t which, float* logits, size_t capacity_elems);
 
 /* Debug: FP32 copy of the verifier's encoder memory of row b, [src_len_b, d_model] (device pointer). */

@@ -49,7 +49,7 @@ __device__ __forceinline__ void join(Stat& a, const Stat& b, float c) {
 
 // Largest score and sum of exponentials of part blockIdx.y of row blockIdx.x, of the verifier's scores or (blockIdx.z) the drafter's.  Scores are
 // read once, 16 bytes at a time behind a ragged beginning; bound by bytes: 1970 rows of 200000 FP32 scores, verifier's and drafter's, 449 us, 7.0 TB/s;
-// of BF16 264 us, 6.0 TB/s, with the exponentials' pipe as busy (71 %); 1656 rows of 32000, 43 us.  grid = (M, parts, 1 or 2), block = STAT_THREADS.
+// of BF16 264 us, 6.0 TB/s; 1656 rows of 32000 in BF16, 44 us, 4.9 TB/s, with the exponentials' pipe at 66 %.  grid = (M, parts, 1 or 2), block = STAT_THREADS.
 template <typename T>
 __global__ void __launch_bounds__(STAT_THREADS)
 score_stats_kernel(Params p) {
@@ -168,7 +168,7 @@ constexpr int AT_ONCE = 8;          // scores under way per thread and row
 // the formula says and alike for every way of adding up.  So decisions are taken from the 32-bit sums of score_stats_kernel only where these leave no
 // doubt, and else, like the draw, from sums in 64 bits over the one position's scores, which are still in L2.  With weights w = exp((score - top) / T)
 // and their sums z, p and q enter as w_p z_q and w_q z_p, multiples of the probabilities that need no division.
-// Bound by latency: decisions, one sweep over the position's scores and three exchanges in a row (18 us from a cold start, one row or 32).  KEPT: the weights of the sweep stay in shared memory
+// Bound by latency: decisions, one sweep over the position's scores and three exchanges in a row (from a cold start 20 us for one row, 25 for 32).  KEPT: the weights of the sweep stay in shared memory
 // for the sum and the draw, else they are computed again.
 // grid = B clusters of CTAs that share the vocabulary, block = ACCEPT_THREADS.  Every CTA of a cluster takes the same decisions from the same numbers.
 // Dynamic shared memory: KEPT, a double per score of the CTA's share, of one or two rows.

@@ -117,13 +117,16 @@ extern "C" int ad_cache_read(const ad_kv_cache* c, void* k, void* v, int32_t dty
 }
 
 namespace {
+// Units of 32 keys that one piece of a row's keys has, and what a tile of rows costs besides its keys, in units.  Measured, with another kernel between the
+// calls: pieces of 4 / 8 / 16, one query on 2000 keys 10.4 / 12.4 / 17.3 us, two rows of 25 queries on 4000 24.6 / 20.6 / 20.6, 24 rows of one on 20000
+// 129 / 129 / 134; 0 / 16 / 32 for the tile, 32 rows x 17-64 queries 178 / 122 / 125, two rows of 25 on 4000 20.7 / 20.6 / 24.7.
 constexpr int kGranule = 8, kItemFixed = 16;
 struct AttendPlan { int nq, row_tiles, grid, granule; bool shared; };
 // max_keys, but no more than a row can hold (which leaves room for roundings below 2^31).
 int32_t longest_row(const ad_kv_cache* c, int32_t max_keys) { return std::min(max_keys, c->table_stride * c->block); }
 // Rows of queries a CTA takes: 8 or 16 where that is all there are, else 32, which make the most of a key's codes once they are FP16.  Keys that are
 // too few to be split leave the GPU to as many CTAs as there are tiles of rows: then tiles are made smaller while all are resident at once
-// (8 x 25 queries in FP32 over 400 keys, 8 heads: 20.7 -> 14.1 us).
+// (8 x 25 queries in FP32 over 400 keys, 8 heads: 14.4 -> 10.3 us).
 AttendPlan attend_plan(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
   AttendPlan plan;
   max_keys = longest_row(c, max_keys);
@@ -135,6 +138,8 @@ AttendPlan attend_plan(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t
   plan.row_tiles = (rows + 8 * plan.nq - 1) / (8 * plan.nq);
   plan.granule = pieces > 1 ? kGranule : 0;
   plan.grid = (int)std::min(resident(plan.nq), std::min(resident(plan.nq), items(plan.nq)) * pieces);     // (items times pieces alone may pass 64 bits)
+  // Whether the threads of a CTA of the join share a row's parts: from six CTAs a tile of rows on (single queries on 20000 keys, four rows, 14 CTAs a tile: 41.1 -> 34.8 us,
+  // eight, 7: 53.4 -> 50.5); at two to five both take the same time, and with many rows shared ones are too many CTAs (32 x 17-64 queries 122 against 191).
   plan.shared = plan.grid > 6 * items(plan.nq);
   return plan;
 }
@@ -232,7 +237,7 @@ int score_parts(int32_t rows, int32_t vocab) {
 }  // namespace
 
 namespace {
-// Weights stay in shared memory while there is room for them: up to 53000 ids with a drafter, 106000 without (half of that in batches of many rows).
+// Weights stay in shared memory while there is room for them: up to 106496 ids with a drafter and 212992 without in clusters of eight CTAs, half of that in clusters of four.
 constexpr size_t kKeptMax = 208 * 1024;
 template <typename T, bool KEPT>
 cudaError_t launch_accept_kept(const sampled::Params& p, int cluster, size_t smem, cudaStream_t st) {

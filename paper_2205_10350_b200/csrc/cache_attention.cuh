@@ -428,10 +428,11 @@ __device__ __forceinline__ void probabilities(Softmax<NQ>& st, float (&s)[(NQ + 
 // (16-byte asynchronous copies, zeros where no key is), nothing but __syncwarp between them, and keeps maximum, sum and result in registers until its
 // keys are through; the four warps' results are joined at the end.  The 16-byte pieces lie in shared memory so that both products' operands come out
 // of it whole, in the registers where mma wants them, without a transposition: dims and keys may be summed in any order.
-// What it measured (BF16 queries, whole call): one query on 200001 keys, 32 query heads on 8 of 128, INT8, 86 us, 4.7 TB/s, 79 of them this kernel at
-// 5.2 TB/s, bound by DRAM and the ends; 16 rows of 3 to 8 queries on 6000 to 32000 keys, the same heads, E4M3, 169 us, 3.7 TB/s at 51 % of mma.sync's
-// rate: 32 rows take 255 registers, two warps a scheduler that wait for their own instructions more than for anything else, so that neither pipe is
-// full; 32 rows of 17 to 64 queries on 200 to 4000 keys, 16 heads of 64, INT8, 144 us, of which the same 107 here, two tiles of rows reading the keys.
+// What it measured (BF16 queries, whole calls one after the other): one query on 200001 keys, 32 query heads on 8 of 128, INT8, 84 to 100 us by GPU, 4.1 to
+// 4.9 TB/s, 81 of them this kernel at 5.1 TB/s, bound by DRAM and the ends; 16 rows of 3 to 8 queries on 6000 to 32000 keys, the same heads, E4M3, 166 to 176 us, 3.7 TB/s
+// at 49 % of mma.sync's rate: 32 rows take 255 registers, two warps a scheduler that wait for their own instructions more than for anything else, so that neither pipe is
+// full; 32 rows of 17 to 64 queries on 200 to 4000 keys, 16 heads of 64, INT8, 138 us (120 with another kernel between the calls), of which 115 here, two tiles of rows
+// reading the keys.  FP32 queries: 161, 246 and 93 us.
 // Tried and slower: codes turned into FP16 in shared memory once for 64 rows by the whole CTA (ldmatrix, a barrier every 64 keys), 117 -> 147 us;
 // 16 rows a CTA at three CTAs an SM, 127 -> 136 and 178 -> 200; 32 rows at two CTAs an SM without spills (64 wide), 127 -> 137.
 // TWO: blocks of 16 tokens, two in a unit.
