@@ -361,7 +361,7 @@ accept_sampled_kernel(Params p) {
       auto left = [&](int v, double wp, double wq) {
         if (form == 1) return wp;
         if (!two) return v == d ? 0.0 : wp;
-        return fmax(wp * zq - wq * zp, 0.0);
+        return fmax(__dmul_rn(wp, zq) - __dmul_rn(wq, zp), 0.0);     // (each rounded: equal distributions leave nothing, not one product's rounding)
       };
       auto over = [&](auto f) {                             // f(v, what is left of v)
         if constexpr (KEPT) {

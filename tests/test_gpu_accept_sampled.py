@@ -438,3 +438,15 @@ def test_temperatures_that_leave_next_to_one_token(dtype, drafter, temperature):
 def test_many_rows_whose_weights_do_not_stay_in_shared_memory(dtype, drafter, V):
     """Clusters of four CTAs, which keep weights of half as many ids."""
     check(*problem([1] * 24, V, dtype, 57, drafter))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [5, 700, 60000])
+def test_equal_distributions_leave_nothing_beyond_the_drafter(dtype, V):
+    """A draft that a random number of one rejects all the same: the drafter has all of the verifier's probability, so that the draw is from the verifier's own."""
+    B = 30
+    target, _, drafts, off, u, r = problem([1] * B, V, dtype, 47, True, 1.7)
+    u[:] = 1.0
+    shifted = (target.float().round() - 64.0).to(TORCH[dtype])           # (the same distances from the top)
+    check(target, target.clone(), drafts, off, u, r, temperature=1.7)
+    check(target.float().round().to(TORCH[dtype]), shifted, drafts, off, u, r, temperature=1.7)
