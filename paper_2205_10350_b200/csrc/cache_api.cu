@@ -231,7 +231,7 @@ int score_parts(int32_t rows, int32_t vocab) {
   const int vecs = (vocab + 3) / 4;                                  // (FP32's; BF16 has half as many)
   const int least = (vecs + 32 * sampled::STAT_THREADS - 1) / (32 * sampled::STAT_THREADS);
   const int most = std::max(1, vecs / (2 * sampled::STAT_THREADS));
-  const int fill = (4 * op_num_sms() + std::max(rows, 1) - 1) / std::max(rows, 1);
+  const int fill = (4 * op_num_sms() - 1) / std::max(rows, 1) + 1;
   return std::max(least, std::min({most, fill, 64}));
 }
 }  // namespace

@@ -247,3 +247,11 @@ def test_longer_rows_than_there_can_be_are_planned_as_the_longest(lib, heads, ma
         assert need[0] <= 2 * 5 * 4096 * 32 * (64 + 2) * 4 + 8 * (B + 2)
         _refused(lib, lib.ad_cache_attention(c, *{**ATTEND, "heads": heads, "stride": heads * 64, "B": B, "max_new": max_new, "max_keys": 2 ** 31 - 1,
                                                   "nbytes": need[0] - 1}.values(), None, None), binding.AD_ERR_CAPACITY)
+
+
+def test_scratch_of_as_many_tokens_as_there_can_be(lib):
+    """Rows of scores counted in 32 bits: a part for each, 8 bytes, and no sum on the way that passes them."""
+    most = (2 ** 31 - 1) // 2
+    assert lib.ad_accept_sampled_scratch_bytes(most, 8, 1) == most * 2 * 8
+    assert lib.ad_accept_sampled_scratch_bytes(most, 8, 0) == most * 8
+    assert lib.ad_accept_sampled_scratch_bytes(most + 1, 8, 0) == 0
