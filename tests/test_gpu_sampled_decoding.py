@@ -100,3 +100,34 @@ def test_sampling_through_a_handle_follows_greedy_decoding_as_the_temperature_fa
         else:
             assert len(out) >= 1 and all(0 <= x < V for x in out)
     dec.close()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_calls_that_overlap_on_two_streams(dtype):
+    """Attention over one cache and sampled verification, on two streams at once and again and again: what each gives alone."""
+    heads, dim, block, n = 4, 64, 32, 3000
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator().manual_seed(3)
+    cache = binding.KvCache(2 * (n // block + 1), heads, dim, block, "int8", row_blocks=n // block + 1, device=DEV)
+    k = torch.randn((2 * n, heads, dim), generator=g).to(dt).to(DEV)
+    binding.cache_append(cache, k, k.flip(0), ints([0, n, 2 * n]), ints([0, 0]), n)
+    work = []
+    for new in (1, 9):
+        q = torch.randn((2 * new, heads * 2, dim), generator=g).to(dt).to(DEV)
+        scores = (torch.randn((2 * new, 9000), generator=g) * 3).to(dt).to(DEV)
+        drafts = scores.argmax(1).view(2, new).int()
+        u, r = torch.rand((2, new), generator=g).to(DEV), torch.rand(2, generator=g).to(DEV)
+        off, lens = ints([0, new, 2 * new]), ints([n - new, n - 40 * new])
+        work.append(lambda q=q, s=scores, d=drafts, u=u, r=r, o=off, l=lens, m=new: (binding.cache_attention(cache, q, o, l, m, n),
+                                                                                     *binding.accept_sampled(s, s.flip(0).contiguous(), d, o, u, r)))
+    alone = [f() for f in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    got = [[], []]
+    for _ in range(20):
+        for i, (f, s) in enumerate(zip(work, streams)):
+            with torch.cuda.stream(s):
+                got[i].append(f())
+    torch.cuda.synchronize()
+    for want, results in zip(alone, got):
+        assert all(torch.equal(a, b) for res in results for a, b in zip(want, res))
