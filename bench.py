@@ -80,19 +80,32 @@ def reduce_max_sum(dist, dev, seconds_or_ms, count):
 # DRAM counters of one verification step (dram__bytes_read.sum + dram__bytes_write.sum summed over the step's
 # kernels, ncu, caches flushed before every kernel) with the digest of the kernel sources they were taken on:
 # the figures are reported only while the sources still have that digest.
-NCU_COUNTERS = dict(sources_sha256="c216cf0249969fb925acd873e37ad3e6636032a2dc8321bcc0510fa5401777c5",
-                    step_block40_bytes=104946176, projection_bytes=32872960,
+NCU_COUNTERS = dict(sources_sha256="4176717b07e516bcdb8abe5f086510439e72d50ad7714151bef600c495a050da",
+                    step_block40_bytes=104930816, projection_bytes=32864768,
                     summary="profiles/verify_step_base_b1_k40_dram_traffic.txt")
 
 
+def kernel_sources():
+    """Sources that a verification step's kernels come from: the handle's and what it includes (not those of other operator-level calls)."""
+    import re
+    csrc = os.path.join(ROOT, "paper_2205_10350_b200", "csrc")
+    todo, found = ["ad_api.cu"], {}
+    while todo:
+        name = todo.pop()
+        if name in found or not os.path.exists(os.path.join(csrc, name)):
+            continue
+        with open(os.path.join(csrc, name), "rb") as f:
+            found[name] = f.read()
+        todo += re.findall(r'^#include "([^"/]+)"', found[name].decode(), re.M)
+    return dict(sorted(found.items()))
+
+
 def kernel_sources_digest():
-    import glob
     import hashlib
     h = hashlib.sha256()
-    for path in sorted(glob.glob(os.path.join(ROOT, "paper_2205_10350_b200", "csrc", "*"))):
-        h.update(os.path.basename(path).encode())
-        with open(path, "rb") as f:
-            h.update(f.read())
+    for name, text in kernel_sources().items():
+        h.update(name.encode())
+        h.update(text)
     return h.hexdigest()
 
 

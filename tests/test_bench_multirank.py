@@ -79,3 +79,23 @@ def test_stored_profiler_counters_expire_with_the_kernel_sources(monkeypatch):
         __import__("paper_2205_10350_b200.synth", fromlist=["BASE"]).BASE)
     monkeypatch.setitem(bench.NCU_COUNTERS, "sources_sha256", "0" * 64)
     assert bench.ncu_counter("step_block40_bytes") is None and bench.ncu_counter("projection_bytes") is None
+
+
+def test_counters_of_a_step_go_by_the_sources_of_its_kernels(monkeypatch, tmp_path):
+    """Sources of other operator-level calls neither belong to them nor take the figures away; a change of the step's own does."""
+    import shutil
+    sys.path.insert(0, ROOT)
+    import bench
+    names = set(bench.kernel_sources())
+    assert {"ad_api.cu", "gemm_few.cuh", "attention_few.cuh", "ffn_few.cuh", "gemm_tc.cuh", "accept.cuh", "steps.cuh", "ad_common.cuh"} <= names
+    assert not names & {"cache_api.cu", "kv_cache.cuh", "cache_attention.cuh", "accept_sampled.cuh"}
+    digest = bench.kernel_sources_digest()
+    csrc = tmp_path / "paper_2205_10350_b200" / "csrc"
+    shutil.copytree(os.path.join(bench.ROOT, "paper_2205_10350_b200", "csrc"), csrc)
+    monkeypatch.setattr(bench, "ROOT", str(tmp_path))
+    (csrc / "another_call.cu").write_text("// another call\n")
+    (csrc / "kv_cache.cuh").write_text("// changed\n")
+    assert bench.kernel_sources_digest() == digest
+    with open(csrc / "steps.cuh", "a") as f:
+        f.write("\n")
+    assert bench.kernel_sources_digest() != digest
