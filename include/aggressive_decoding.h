@@ -399,6 +399,70 @@ int ad_accept_sampled(const void* target, int64_t target_stride, const void* dra
                       int32_t M, const float* u, const float* r, int32_t eos, int32_t* tokens, int32_t* n_accepted,
                       void* scratch, size_t scratch_bytes, int32_t* status, void* stream);
 
+/* Attention over the cache for batches whose rows share prefixes.  The rows group[g] .. group[g + 1] - 1 (group [G + 1], device, ascending from 0 to B) hold
+ * the same keys and values in their first shared[g] positions (shared [G], device; 0: nothing shared; no row of the group sees fewer), as rows do that
+ * ad_cache_fork made from one, or that look at one encoder's keys.  These positions are read once for the group, through the table of its first row, whatever
+ * the others' tables say there.  Otherwise arguments, result and precision are those of ad_cache_attention.  max_shared: longest prefix to plan for.
+ * A group that does not lie in ascending order within 0 .. B, or with shared[g] below 0 or beyond the row's capacity, latches AD_ERR_ARG and its rows come out as zeros;
+ * a row that sees fewer than shared[g] positions latches AD_ERR_ARG and is left out.  At most 8192 rows. */
+size_t ad_cache_attention_shared_scratch_bytes(const ad_kv_cache* cache, int32_t dtype, int32_t n_heads, int32_t B, int32_t M, int32_t max_new,
+                                               int32_t max_keys, int32_t G, int32_t max_shared);
+int ad_cache_attention_shared(const ad_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
+                              const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, const int32_t* group,
+                              const int32_t* shared, int32_t G, int32_t max_shared, int32_t causal, float scale, void* out, void* scratch,
+                              size_t scratch_bytes, int32_t* status, void* stream);
+
+/* ---- pool of cache blocks -------------------------------------------------------------------------------------
+ * (No counterpart in the paper: for decoders that keep several hypotheses or samples of a source, and batches whose rows come and go.)  The blocks of
+ * one or more caches, the layers of a decoder, are handed out together: all layers have the same table, and refs counts for every block the entries of the table
+ * that name it (0: the block is free).  Both start as the caller lays them out (all -1 and all 0: an empty pool) and are kept by these calls, on the device, without the
+ * host; results do not depend on the order in which threads run.  All B rows of a call take part at once. */
+typedef struct ad_kv_pool {
+  int32_t* table;            /* [rows, table_stride]: block i of row b, -1: none */
+  int32_t* refs;             /* [n_blocks] */
+  int32_t rows;              /* 1 .. 8192 */
+  int32_t table_stride;      /* blocks that a row may have */
+  int32_t n_blocks;
+  int32_t block;             /* tokens of a block, as in the caches */
+} ad_kv_pool;
+
+/* Row b becomes the first len[b] tokens of what row parent[b] was before the call (0 .. B - 1, itself included), for rows 0 .. B - 1 at once; a negative
+ * parent leaves the row empty.  So this forks rows, changes their places, drops them, and gives back what lies behind a row's length.  Blocks are shared, not copied;
+ * what no row holds any more is free.  parent and len are device arrays [B].  A row whose parent or length makes no sense latches AD_ERR_ARG (AD_ERR_CAPACITY: longer than a
+ * row can be) and stays as it was; one that asks for more than its parent holds gets what there is and latches AD_ERR_ARG. */
+int ad_cache_fork(const ad_kv_pool* pool, const int32_t* parent, const int32_t* len, int32_t B, int32_t* status, void* stream);
+
+/* Makes rows ready for an ad_cache_append of the same off [B + 1] and len [B]: every block that row b's off[b + 1] - off[b] new tokens will be written to
+ * exists and belongs to this row alone.  Rows get blocks where they have none; a block that other rows hold as well is replaced by one of the row's own,
+ * with the tokens in front of len[b] copied in all `n_caches` caches (0 .. 64; none: nothing is copied).  Where nobody else holds it, the first of the rows that write
+ * a shared block keeps it.  Free blocks are taken in ascending order, for rows and for a row's blocks in order.  A pool without enough of them latches AD_ERR_CAPACITY and
+ * stays as it is.  A row whose offsets or length make no sense, or that would pass its capacity, latches AD_ERR_ARG or AD_ERR_CAPACITY and is left alone.  Codes behind the copied
+ * tokens stay as they were.  scratch: ad_cache_reserve_scratch_bytes() of device memory, 256-byte aligned; calls that may overlap need scratch of their own. */
+size_t ad_cache_reserve_scratch_bytes(const ad_kv_pool* pool, int32_t B);
+int ad_cache_reserve(const ad_kv_pool* pool, const ad_kv_cache* caches, int32_t n_caches, const int32_t* off, const int32_t* len, int32_t B,
+                     void* scratch, size_t scratch_bytes, int32_t* status, void* stream);
+
+/* Moves the blocks in use to the front of the pool: *n_used (device) receives their number, and those behind it go to the free ones in front of it, both
+ * in ascending order, in all caches; the whole table (all `rows`) and refs follow.  Blocks from *n_used on are free afterwards and can be given to something else.  scratch as above. */
+size_t ad_cache_compact_scratch_bytes(const ad_kv_pool* pool);
+int ad_cache_compact(const ad_kv_pool* pool, const ad_kv_cache* caches, int32_t n_caches, int32_t* n_used, void* scratch, size_t scratch_bytes,
+                     void* stream);
+
+/* Sampling: the token that follows each of M rows of scores [M, vocab] (dtype; rows `stride` scores apart), from given random numbers r [M], uniform in [0, 1).
+ * With w(v) = exp((score(v) - largest) / temperature) and ids in descending order of their scores (ties: lowest id first): top_k keeps the first top_k ids
+ * (0 or less: all); top_p, of these, the ones in front of which less than top_p of their weight lies, and the first in any case (1 or more: all); min_p, of
+ * those, the ones with w >= min_p (0 or less: all).  tokens[m] is the lowest kept id at which the running sum of w, over kept ids in ascending order,
+ * exceeds r[m] times its total.  Every parameter is a device array [M] or NULL (temperature one; no such filter).  temperature 0: the largest score, lowest id.
+ * logp (NULL: not wanted) [M] receives the token's log-probability among the kept ids.  filtered (NULL: not wanted) [M, vocab] in dtype, rows filtered_stride
+ * apart, receives the scores of the kept ids and -inf for the others: what ad_accept_sampled takes as the scores of a truncated distribution, the verifier's or the
+ * drafter's.  It may be `scores` itself (with the same stride).
+ * Weights are computed in 64 bits and summed as integers in units of 2^-62 * vocab of the largest (vocab rounded up to a power of two); comparisons are decided on these sums.
+ * Scores of -inf have no weight, +inf share all of it, a NaN counts as -inf.  A row without any score above -inf takes id 0 with logp -inf.  One whose
+ * temperature is negative or not finite, or with a NaN for a parameter or r, latches AD_ERR_ARG: token -1, logp and all filtered scores -inf.  vocab is at most 2^20. */
+int ad_sample(const void* scores, int64_t stride, int32_t dtype, int32_t vocab, int32_t M, const float* temperature, const int32_t* top_k,
+              const float* top_p, const float* min_p, const float* r, int32_t* tokens, float* logp, void* filtered, int64_t filtered_stride,
+              int32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,7 +25,8 @@ EXPORTS = [
     "ad_debug_logits", "ad_debug_encoder_memory", "ad_debug_stage_timeline", "ad_debug_profile_verify", "ad_vocab_argmax_scratch_bytes", "ad_vocab_argmax",
     "ad_vocab_argmax_static", "ad_debug_graph_count", "ad_debug_projection_shapes", "ad_debug_wait_probe", "ad_debug_grid_barrier_probe",
     "ad_linear", "ad_cache_append", "ad_cache_read", "ad_cache_attention_scratch_bytes", "ad_cache_attention", "ad_accept_sampled_scratch_bytes",
-    "ad_accept_sampled",
+    "ad_accept_sampled", "ad_cache_attention_shared_scratch_bytes", "ad_cache_attention_shared", "ad_cache_fork", "ad_cache_reserve_scratch_bytes",
+    "ad_cache_reserve", "ad_cache_compact_scratch_bytes", "ad_cache_compact", "ad_sample",
 ]
 
 
@@ -60,6 +61,10 @@ class KvCacheStruct(C.Structure):
                [(n, C.c_int32) for n in ("table_stride", "n_blocks", "n_kv_heads", "block", "head_dim", "format")]
 
 
+class KvPoolStruct(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("table", "refs")] + [(n, C.c_int32) for n in ("rows", "table_stride", "n_blocks", "block")]
+
+
 class AdError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"aggressive_decoding error {code}: {msg}")
@@ -79,7 +84,7 @@ def load():
                           "there is no fallback path")
     lib = C.CDLL(LIB_PATH)
     vp, i32, sz = C.c_void_p, C.c_int32, C.c_size_t
-    cache, i64, f32 = C.POINTER(KvCacheStruct), C.c_int64, C.c_float
+    cache, pool, i64, f32 = C.POINTER(KvCacheStruct), C.POINTER(KvPoolStruct), C.c_int64, C.c_float
     sig = {
         "ad_weight_counts": (C.c_int, [C.POINTER(ModelCfg), C.POINTER(sz), C.POINTER(sz)]),
         "ad_query_workspace": (C.c_int, [C.POINTER(ModelCfg), C.POINTER(sz)]),
@@ -107,6 +112,14 @@ def load():
         "ad_cache_read": (C.c_int, [cache, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp]),
         "ad_cache_attention_scratch_bytes": (sz, [cache, i32, i32, i32, i32, i32]),
         "ad_cache_attention": (C.c_int, [cache, vp, i32, i64, i32, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, sz, vp, vp]),
+        "ad_cache_attention_shared_scratch_bytes": (sz, [cache, i32, i32, i32, i32, i32, i32, i32, i32]),
+        "ad_cache_attention_shared": (C.c_int, [cache, vp, i32, i64, i32, vp, vp, i32, i32, i32, i32, vp, vp, i32, i32, i32, f32, vp, vp, sz, vp, vp]),
+        "ad_cache_fork": (C.c_int, [pool, vp, vp, i32, vp, vp]),
+        "ad_cache_reserve_scratch_bytes": (sz, [pool, i32]),
+        "ad_cache_reserve": (C.c_int, [pool, cache, i32, vp, vp, i32, vp, sz, vp, vp]),
+        "ad_cache_compact_scratch_bytes": (sz, [pool]),
+        "ad_cache_compact": (C.c_int, [pool, cache, i32, vp, vp, sz, vp]),
+        "ad_sample": (C.c_int, [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp]),
         "ad_accept_sampled_scratch_bytes": (sz, [i32, i32, i32]),
         "ad_accept_sampled": (C.c_int, [vp, i64, vp, i64, i32, f32, i32, vp, vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, sz, vp, vp]),
         "ad_debug_graph_count": (C.c_int, [vp, vp]),
@@ -621,6 +634,156 @@ def cache_attention(cache, q_t, off_t, len_t, max_new, max_keys, causal=True, sc
     if rc != AD_OK:
         _raise(lib, rc)
     return out
+
+
+def cache_attention_shared(cache, q_t, off_t, len_t, group_t, shared_t, max_new, max_keys, max_shared=None, causal=True, scale=None, out=None,
+                           status_t=None):
+    """cache_attention for rows that share prefixes: rows group_t[g] .. group_t[g + 1] - 1 (group_t [G + 1]) have their first shared_t[g] positions in
+    common (shared_t [G]), which are read once for all of them, through the first row's blocks.  max_shared: longest prefix (max_keys unless given)."""
+    entry, lib = "ad_cache_attention_shared", _lib or load()
+    if max_shared is None:
+        max_shared = max_keys
+    if (max_new | max_keys | max_shared) >> 31:
+        _refuse(entry, _TOO_LARGE)
+    B, G = cache._batch(entry, off_t, len_t), shared_t.numel()
+    if not (_vector(shared_t, G, _INT32, cache._dev) and _vector(group_t, G + 1, _INT32, cache._dev)):
+        _refuse(entry, f"groups and shared lengths are contiguous int32 tensors [G + 1] and [G] on {cache.device}, got {tuple(group_t.shape)} and {tuple(shared_t.shape)}")
+    if q_t.dim() != 3:
+        _refuse(entry, "queries are [tokens, heads, head_dim]")
+    H = q_t.size(1)
+    dtype, M, stride = cache._tokens(entry, q_t, H)
+    if out is None:
+        out = q_t.new_empty((M, H, cache.head_dim))
+    elif not _matrix(out, q_t.shape, q_t.dtype, cache._dev):
+        _refuse(entry, "the result is a contiguous tensor like the queries")
+    sizes = (dtype, H, B, M, max_new, max_keys, G, max_shared)
+    nbytes = cache._scratch.get(sizes)
+    if nbytes is None:
+        nbytes = _call_on(cache._dev, lambda *a: lib.ad_cache_attention_shared_scratch_bytes(*a[:-1]), cache._ref, *sizes)
+        if len(cache._scratch) < 4096:
+            cache._scratch[sizes] = nbytes
+    scratch = off_t.new_empty((nbytes + 3) // 4) if nbytes else None       # (torch's allocations are 512-byte aligned)
+    rc = _call_on(cache._dev, lib.ad_cache_attention_shared, cache._ref, q_t.data_ptr(), dtype, stride, H, off_t.data_ptr(), len_t.data_ptr(), B, M, max_new,
+                  max_keys, group_t.data_ptr(), shared_t.data_ptr(), G, max_shared, 1 if causal else 0, cache.head_dim ** -0.5 if scale is None else scale,
+                  out.data_ptr(), scratch.data_ptr() if nbytes else None, nbytes, _status_pointer(entry, cache._dev, status_t))
+    if rc != AD_OK:
+        _raise(lib, rc)
+    return out
+
+
+class KvPool:
+    """Blocks of one or more caches (the layers of a decoder) that rows share: a table [rows, row_blocks] of the blocks of each row, -1 where there is none,
+    and refs [n_blocks], how many entries name a block.  Starts empty; `tensors` = (table, refs) adopts existing ones.  Caches join by add_cache."""
+
+    def __init__(self, rows, row_blocks, n_blocks, block=32, device="cuda:0", tensors=None):
+        import torch
+        _names()
+        entry = "KvPool"
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            _refuse(entry, "the pool lives on a CUDA device")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.rows, self.row_blocks, self.n_blocks, self.block = int(rows), int(row_blocks), int(n_blocks), int(block)
+        if min(self.rows, self.row_blocks, self.n_blocks) < 1 or (self.rows | self.row_blocks | self.n_blocks) >> 31:
+            _refuse(entry, "sizes must lie between 1 and 2^31 - 1")
+        if tensors is None:
+            tensors = (torch.full((self.rows, self.row_blocks), -1, dtype=torch.int32, device=self.device),
+                       torch.zeros(self.n_blocks, dtype=torch.int32, device=self.device))
+        self.table, self.refs = tensors
+        self._dev = self.device.index
+        if not (_matrix(self.table, (self.rows, self.row_blocks), torch.int32, self._dev) and _vector(self.refs, self.n_blocks, _INT32, self._dev)):
+            _refuse(entry, f"table and refs are contiguous int32 tensors [{rows}, {row_blocks}] and [{n_blocks}] on {self.device}")
+        self.struct = KvPoolStruct(self.table.data_ptr(), self.refs.data_ptr(), self.rows, self.row_blocks, self.n_blocks, self.block)
+        self._ref, self.caches, self._structs, self._scratch = C.byref(self.struct), [], None, {}
+
+    def add_cache(self, n_kv_heads, head_dim, fmt="e4m3", tensors=None):
+        """A cache (of one layer) on the pool's blocks and table; cache_reserve and cache_compact move its contents from now on."""
+        cache = KvCache(self.n_blocks, n_kv_heads, head_dim, self.block, fmt, table=self.table, row_blocks=self.row_blocks, device=self.device, tensors=tensors)
+        self.caches.append(cache)
+        self._structs = (KvCacheStruct * len(self.caches))(*(c.struct for c in self.caches))
+        return cache
+
+    def _scratch_for(self, what, *sizes):
+        nbytes = self._scratch.get((what, *sizes))
+        if nbytes is None:
+            nbytes = self._scratch[what, *sizes] = getattr(load(), what)(self._ref, *sizes)
+        return self.refs.new_empty(max(1, nbytes // 4)), nbytes
+
+
+def cache_fork(pool, parent_t, len_t, status_t=None):
+    """Row b becomes the first len_t[b] tokens of what row parent_t[b] was (negative: empty), all rows of the call at once; blocks are shared, and free when
+    no row holds them any more.  parent_t, len_t: int32 [B], B at most the pool's rows."""
+    entry, lib = "ad_cache_fork", _lib or load()
+    B = len_t.numel()
+    if not (_vector(len_t, B, _INT32, pool._dev) and _vector(parent_t, B, _INT32, pool._dev)):
+        _refuse(entry, f"parents and lengths are contiguous int32 tensors [B] on {pool.device}")
+    rc = _call_on(pool._dev, lib.ad_cache_fork, pool._ref, parent_t.data_ptr(), len_t.data_ptr(), B, _status_pointer(entry, pool._dev, status_t))
+    if rc != AD_OK:
+        _raise(lib, rc)
+
+
+def cache_reserve(pool, off_t, len_t, status_t=None):
+    """Blocks of their own for what a cache_append of the same offsets and lengths will write: new ones where rows have none, copies (in all of the pool's
+    caches) where others hold them too."""
+    entry, lib = "ad_cache_reserve", _lib or load()
+    B = len_t.numel()
+    if not (_vector(len_t, B, _INT32, pool._dev) and _vector(off_t, B + 1, _INT32, pool._dev)):
+        _refuse(entry, f"offsets and lengths are contiguous int32 tensors [B + 1] and [B] on {pool.device}")
+    scratch, nbytes = pool._scratch_for("ad_cache_reserve_scratch_bytes", B)
+    rc = _call_on(pool._dev, lib.ad_cache_reserve, pool._ref, pool._structs, len(pool.caches), off_t.data_ptr(), len_t.data_ptr(), B, scratch.data_ptr(), nbytes,
+                  _status_pointer(entry, pool._dev, status_t))
+    if rc != AD_OK:
+        _raise(lib, rc)
+
+
+def cache_compact(pool):
+    """Moves the blocks in use to the front of the pool, in all of its caches; returns their number (int32 [1], on the device)."""
+    lib = _lib or load()
+    scratch, nbytes = pool._scratch_for("ad_cache_compact_scratch_bytes")
+    n_used = pool.refs.new_empty(1)
+    rc = _call_on(pool._dev, lib.ad_cache_compact, pool._ref, pool._structs, len(pool.caches), n_used.data_ptr(), scratch.data_ptr(), nbytes)
+    if rc != AD_OK:
+        _raise(lib, rc)
+    return n_used
+
+
+def sample(scores_t, r_t, temperature=None, top_k=None, top_p=None, min_p=None, filtered=None, status_t=None):
+    """Tokens that follow rows of scores_t [M, vocab], drawn with uniform numbers r_t [M] from what temperature, top_k, top_p and min_p leave: tensors [M]
+    (top_k int32, the others float32) or None for no such filter.  Returns (tokens int32 [M], their log-probabilities float32 [M]).  `filtered`, a tensor like
+    scores_t or scores_t itself, receives the scores of the ids that are left and -inf for the others."""
+    entry, lib = "ad_sample", _lib or load()
+    if _INT32 is None:
+        _names()
+    dev = scores_t.get_device()
+    dtype = AD_DTYPE_BF16 if scores_t.dtype is _BF16 else AD_DTYPE_FP32
+    if dev < 0 or scores_t.dim() != 2 or (dtype == AD_DTYPE_FP32 and scores_t.dtype is not _FP32):
+        _refuse(entry, "scores are [rows, vocab] on a CUDA device, in float32 or bfloat16")
+    M, V = scores_t.shape
+    if (M | V) >> 31:
+        _refuse(entry, _TOO_LARGE)
+    for t, want, what in ((r_t, _FP32, "random numbers"), (temperature, _FP32, "temperatures"), (top_k, _INT32, "top_k"), (top_p, _FP32, "top_p"), (min_p, _FP32, "min_p")):
+        if not (t is None and t is not r_t) and not _vector(t, M, want, dev):
+            _refuse(entry, f"{what}: a contiguous {want} tensor [{M}] on device {dev}")
+    stride, one = scores_t.stride()
+    out, out_stride = None, V
+    if filtered is not None:
+        if filtered.dtype is not scores_t.dtype or filtered.shape != scores_t.shape or filtered.get_device() != dev:
+            _refuse(entry, "what is left of the scores is like them in type, shape and place")
+        out, (out_stride, out_one) = filtered.data_ptr(), filtered.stride()
+        if out_one != 1:
+            one = out_one
+    if one != 1 and V > 1:
+        _refuse(entry, "a row's scores must lie next to each other")
+    if M < 2:
+        stride = out_stride = V
+    tokens, logp = r_t.new_empty(M, dtype=_INT32), r_t.new_empty(M)
+    point = lambda t: None if t is None else t.data_ptr()
+    rc = _call_on(dev, lib.ad_sample, scores_t.data_ptr(), stride, dtype, V, M, point(temperature), point(top_k), point(top_p), point(min_p), r_t.data_ptr(),
+                  tokens.data_ptr(), logp.data_ptr(), out, out_stride, _status_pointer(entry, dev, status_t))
+    if rc != AD_OK:
+        _raise(lib, rc)
+    return tokens, logp
 
 
 _accept_scratch = {}     # (device, tokens, vocabulary, drafter) -> bytes

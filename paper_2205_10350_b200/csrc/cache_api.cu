@@ -8,48 +8,13 @@
 #include "accept_sampled.cuh"
 #include "ad_common.cuh"
 #include "cache_attention.cuh"
+#include "cache_checks.h"
 #include "kv_cache.cuh"
 #include "op_launch.h"
 
 using namespace ad;
 
 namespace {
-
-constexpr int kMaxNew = 1 << 19;       // tokens of a row in one call (grid dimensions)
-constexpr int kMaxRows = 65535;
-
-bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-bool known_dtype(int32_t t) { return t == AD_DTYPE_FP32 || t == AD_DTYPE_BF16; }
-size_t dtype_bytes(int32_t t) { return t == AD_DTYPE_FP32 ? 4 : 2; }
-
-// Why a cache cannot be worked on, or null.
-const char* cache_fault(const ad_kv_cache* c, int32_t B) {
-  if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return "null cache";
-  if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16)) return "codes must be 16-byte aligned";
-  if (c->format != AD_CACHE_E4M3 && c->format != AD_CACHE_INT8) return "unknown format";
-  if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128) return "blocks hold 16, 32, 64 or 128 tokens";
-  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return "heads are 32, 64 or 128 wide";
-  if (c->n_blocks < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 4096 || c->table_stride < 1) return "sizes must be positive (and at most 4096 heads)";
-  if ((int64_t)c->table_stride * c->block > INT_MAX - kMaxNew) return "a row's capacity must stay below 2^31 - 2^19 tokens";
-  if (!c->table && (int64_t)B * c->table_stride > c->n_blocks) return "without a table there must be B * table_stride blocks";
-  return nullptr;
-}
-
-const char* batch_fault(const int32_t* off, const int32_t* len, int32_t B, int32_t M, int32_t max_new) {
-  if (!off || !len) return "null offsets or lengths";
-  if (B < 1 || B > kMaxRows) return "1 to 65535 rows";
-  if (M < 0) return "negative number of tokens";
-  if (max_new < 1 || max_new > kMaxNew) return "1 to 2^19 tokens of a row";
-  return nullptr;
-}
-
-kv::Cache device_cache(const ad_kv_cache* c) {
-  kv::Cache d;
-  d.codes[0] = static_cast<uint8_t*>(c->k_codes); d.codes[1] = static_cast<uint8_t*>(c->v_codes);
-  d.scale[0] = c->k_scale; d.scale[1] = c->v_scale;
-  d.table = c->table; d.table_stride = c->table_stride; d.n_blocks = c->n_blocks; d.heads = c->n_kv_heads; d.block = c->block;
-  return d;
-}
 
 template <typename T, typename F> struct Types { typedef T Num; typedef F Fmt; };
 // Calls f with the number and code types of a call.
@@ -58,9 +23,6 @@ cudaError_t by_types(int32_t dtype, int32_t format, Fn f) {
   if (dtype == AD_DTYPE_FP32) return format == AD_CACHE_E4M3 ? f(Types<float, kv::E4m3>()) : f(Types<float, kv::Int8>());
   return format == AD_CACHE_E4M3 ? f(Types<bf16, kv::E4m3>()) : f(Types<bf16, kv::Int8>());
 }
-
-int arg_fault(const char* entry, const char* why) { return op_fail(AD_ERR_ARG, entry, why); }
-int launched(const char* entry, cudaError_t e) { return e == cudaSuccess ? AD_OK : op_fail(AD_ERR_CUDA, entry, cudaGetErrorString(e)); }
 
 // Heads' tiles that a CTA of ad_cache_append and ad_cache_read takes one after the other, by how often one tile a CTA would fill the GPU (768 threads an
 // SM, what registers allow): four beyond eight times, two beyond two and a half, else one.  Appending, one / two / four: 1.7 times (32 rows x 9-64 tokens, 64 wide)
@@ -221,6 +183,21 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
     return c->head_dim == 32 ? launch_attention_dim<T, F, 32>(a, plan, st) : c->head_dim == 64 ? launch_attention_dim<T, F, 64>(a, plan, st)
                                                                                               : launch_attention_dim<T, F, 128>(a, plan, st);
   }));
+}
+
+extern "C" size_t ad_cache_attention_shared_scratch_bytes(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t M, int32_t max_new,
+                                                          int32_t max_keys, int32_t G, int32_t max_shared) {
+  if (M < 0 || G < 1 || max_shared < 0) return 0;
+  return ad_cache_attention_scratch_bytes(c, dtype, n_heads, B, max_new, max_keys);
+}
+extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
+                                         const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, const int32_t* group,
+                                         const int32_t* shared, int32_t G, int32_t max_shared, int32_t causal, float scale, void* out, void* scratch,
+                                         size_t scratch_bytes, int32_t* status, void* stream) {
+  const char* entry = "ad_cache_attention_shared";
+  if (!group || !shared) return arg_fault(entry, "null groups");
+  if (G < 1 || G > B || max_shared < 0) return arg_fault(entry, "a group has a row at least");
+  return ad_cache_attention(c, q, dtype, q_stride, n_heads, off, len, B, M, max_new, max_keys, causal, scale, out, scratch, scratch_bytes, status, stream);
 }
 
 namespace {

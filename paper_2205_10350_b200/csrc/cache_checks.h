@@ -1,0 +1,52 @@
+// Checks that the entry points around the 8-bit cache share: sizes, alignment, and how a refusal is told.
+#pragma once
+
+#include <limits.h>
+#include <stdint.h>
+
+#include "ad_common.cuh"
+#include "kv_cache.cuh"
+#include "op_launch.h"
+
+namespace ad {
+
+constexpr int kMaxNew = 1 << 19;       // tokens of a row in one call (grid dimensions)
+constexpr int kMaxRows = 65535;
+
+inline bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+inline bool known_dtype(int32_t t) { return t == AD_DTYPE_FP32 || t == AD_DTYPE_BF16; }
+inline size_t dtype_bytes(int32_t t) { return t == AD_DTYPE_FP32 ? 4 : 2; }
+
+// Why a cache cannot be worked on, or null.
+inline const char* cache_fault(const ad_kv_cache* c, int32_t B) {
+  if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return "null cache";
+  if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16)) return "codes must be 16-byte aligned";
+  if (c->format != AD_CACHE_E4M3 && c->format != AD_CACHE_INT8) return "unknown format";
+  if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128) return "blocks hold 16, 32, 64 or 128 tokens";
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return "heads are 32, 64 or 128 wide";
+  if (c->n_blocks < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 4096 || c->table_stride < 1) return "sizes must be positive (and at most 4096 heads)";
+  if ((int64_t)c->table_stride * c->block > INT_MAX - kMaxNew) return "a row's capacity must stay below 2^31 - 2^19 tokens";
+  if (!c->table && (int64_t)B * c->table_stride > c->n_blocks) return "without a table there must be B * table_stride blocks";
+  return nullptr;
+}
+
+inline const char* batch_fault(const int32_t* off, const int32_t* len, int32_t B, int32_t M, int32_t max_new) {
+  if (!off || !len) return "null offsets or lengths";
+  if (B < 1 || B > kMaxRows) return "1 to 65535 rows";
+  if (M < 0) return "negative number of tokens";
+  if (max_new < 1 || max_new > kMaxNew) return "1 to 2^19 tokens of a row";
+  return nullptr;
+}
+
+inline kv::Cache device_cache(const ad_kv_cache* c) {
+  kv::Cache d;
+  d.codes[0] = static_cast<uint8_t*>(c->k_codes); d.codes[1] = static_cast<uint8_t*>(c->v_codes);
+  d.scale[0] = c->k_scale; d.scale[1] = c->v_scale;
+  d.table = c->table; d.table_stride = c->table_stride; d.n_blocks = c->n_blocks; d.heads = c->n_kv_heads; d.block = c->block;
+  return d;
+}
+
+inline int arg_fault(const char* entry, const char* why) { return op_fail(AD_ERR_ARG, entry, why); }
+inline int launched(const char* entry, cudaError_t e) { return e == cudaSuccess ? AD_OK : op_fail(AD_ERR_CUDA, entry, cudaGetErrorString(e)); }
+
+}  // namespace ad
