@@ -7,8 +7,8 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libad_b200.so")
-SOURCES = ["ad_api.cu", "cache_api.cu", "pool_api.cu"]
-HEADERS = ["ad_common.cuh", "gemm_tc.cuh", "gemm_tc_pair.cuh", "gemm_simt.cuh", "gemm_few.cuh", "attention.cuh", "attention_few.cuh", "attention_mma.cuh", "ffn_few.cuh", "sublayer_f32.cuh", "steps.cuh", "accept.cuh", "grid_sync.cuh", "mega.cuh", "kv_cache.cuh", "cache_attention.cuh", "accept_sampled.cuh", "block_pool.cuh", "sample.cuh", "cache_checks.h", "op_launch.h"]
+SOURCES = ["ad_api.cu", "cache_api.cu", "pool_api.cu", "shared_api.cu"]
+HEADERS = ["ad_common.cuh", "gemm_tc.cuh", "gemm_tc_pair.cuh", "gemm_simt.cuh", "gemm_few.cuh", "attention.cuh", "attention_few.cuh", "attention_mma.cuh", "ffn_few.cuh", "sublayer_f32.cuh", "steps.cuh", "accept.cuh", "grid_sync.cuh", "mega.cuh", "kv_cache.cuh", "cache_attention.cuh", "accept_sampled.cuh", "shared_attention.cuh", "block_pool.cuh", "sample.cuh", "cache_checks.h", "op_launch.h"]
 
 
 def _stale() -> bool:

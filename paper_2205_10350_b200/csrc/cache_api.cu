@@ -185,21 +185,6 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
   }));
 }
 
-extern "C" size_t ad_cache_attention_shared_scratch_bytes(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t M, int32_t max_new,
-                                                          int32_t max_keys, int32_t G, int32_t max_shared) {
-  if (M < 0 || G < 1 || max_shared < 0) return 0;
-  return ad_cache_attention_scratch_bytes(c, dtype, n_heads, B, max_new, max_keys);
-}
-extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
-                                         const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, const int32_t* group,
-                                         const int32_t* shared, int32_t G, int32_t max_shared, int32_t causal, float scale, void* out, void* scratch,
-                                         size_t scratch_bytes, int32_t* status, void* stream) {
-  const char* entry = "ad_cache_attention_shared";
-  if (!group || !shared) return arg_fault(entry, "null groups");
-  if (G < 1 || G > B || max_shared < 0) return arg_fault(entry, "a group has a row at least");
-  return ad_cache_attention(c, q, dtype, q_stride, n_heads, off, len, B, M, max_new, max_keys, causal, scale, out, scratch, scratch_bytes, status, stream);
-}
-
 namespace {
 // Parts a row's scores are split into: four CTAs an SM where there are few rows, as long as every thread has a vector; at least so many that no
 // thread adds up more than 32 vectors.  64 parts at most: the accept kernel's bound on the sums' errors counts on it.
