@@ -1,6 +1,8 @@
 // Attention over the 8-bit key/value cache for rows that share prefixes: the shared positions once for all rows of a group, on the tensor cores' own memory.
 #pragma once
 
+#include <type_traits>
+
 #include "cache_attention.cuh"
 #include "gemm_tc.cuh"
 
@@ -247,7 +249,9 @@ template <int DIM, bool WIDE>
 __host__ __device__ constexpr int smem_bytes() { return 1023 + Layout<DIM, WIDE>::BYTES + (int)sizeof(Small<DIM, WIDE>); }
 
 constexpr int SOFTMAX_WARPS = 8, CONVERT_WARPS = 4;
-constexpr int W_CONVERT = SOFTMAX_WARPS, W_MMA = W_CONVERT + CONVERT_WARPS, W_LOAD = W_MMA + 1, THREADS = 32 * (W_LOAD + 1);
+constexpr int W_CONVERT = SOFTMAX_WARPS, W_MMA = W_CONVERT + CONVERT_WARPS, W_LOAD = W_MMA + 1, THREADS = 512;      // (four warpgroups, for the sake of their registers)
+// Registers of a thread by warpgroup, from the 128 of the launch: 2 * 144 + 2 * 112 = 4 * 128.
+constexpr int SOFTMAX_REGS = 144, OTHER_REGS = 112;
 
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -358,6 +362,10 @@ shared_attention_kernel(const __grid_constant__ Params a) {
   Walk walk;
   const bool work = walk.begin(a);
 
+  if (work) {
+    if (warp < SOFTMAX_WARPS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+  }
   if (work && warp == W_LOAD) {
     // ================= codes and scales: table -> scales -> copies, each a tile ahead of the next =================
     struct Tile { int row, kvh, pos, lo, hi; bool there; };
@@ -701,7 +709,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
       l = 0.f;
       const int n = s.t1 - s.t0, row = s.r0 + (s.two ? half * M_ROWS : 0) + r, last_row = s.r0 + s.rows - 1;
       const int sees = s.causal ? s.p + min(row, last_row) / per_kv + 1 : s.p;
-      const bool busy = __any_sync(0xffffffffu, row <= last_row);
+      const bool mine = row <= last_row, busy = __any_sync(0xffffffffu, mine);      // (rows that there are none of hold anything, and decide on nothing)
       for (int i = s.two ? 0 : half; i < n && ok; i += s.two ? 1 : 2) {
         ok = wait_warp(sm.s[half], s_phase);
         if (!ok) break;
@@ -714,110 +722,119 @@ shared_attention_kernel(const __grid_constant__ Params a) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) whole = whole && info.ks[j] >= 0.f;
           whole = __all_sync(0xffffffffu, whole);
-          auto masked = [&](int j, int c) {                     // key c of 16 keys j
-            const int at = pos + 16 * j + c;
-            return at < s.lo || at >= sees || info.ks[j] < 0.f;
-          };
-          auto factor_of = [&](int j) { return fmaxf(factor * fabsf(info.ks[j]) * rest, FLT_MIN); };      // (not 0 times -inf)
-          // ---- the largest score of every 16 keys ----
-          float most = -INFINITY, ve_max = info.ve[0];
-          float x[8];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t y[2][32];
-            tmem_issue32(col_s(half) + 64 * h + quad, y[0]);
-            tmem_issue32(col_s(half) + 64 * h + 32 + quad, y[1]);
-            tmem_wait_ld();
-            tmem_landed32(y[0]);
-            tmem_landed32(y[1]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int j = 4 * h + k;
-              float v[16];
-#pragma unroll
-              for (int c = 0; c < 16; ++c) v[c] = __uint_as_float(y[k >> 1][(k & 1) * 16 + c]);
-              if (!whole) {
-#pragma unroll
-                for (int c = 0; c < 16; ++c)
-                  if (masked(j, c)) v[c] = -INFINITY;
-              }
-              float top = kv::max3(v[0], v[1], v[2]);
-#pragma unroll
-              for (int c = 3; c < 15; c += 2) top = kv::max3(top, v[c], v[c + 1]);
-              top = fmaxf(top, v[15]);
-              x[j] = ceilf(top * factor_of(j));                  // references are whole numbers: what goes from one to another is an exact power of two
-              most = fmaxf(most, x[j]);
-              ve_max = fmaxf(ve_max, info.ve[j]);
-            }
-          }
           const bool first_tile = i < 2 && (s.two ? i == 0 : true);
-          bool moves = most > m || ve_max - kv::SPAN > d;
+          const int lo = s.lo - pos, hi = sees - pos;
+          // MASKED: some of the keys are not there, or not seen by some row of the warp
+          auto tile = [&](auto masked_keys) {
+            constexpr bool MASKED = decltype(masked_keys)::value;
+            // ---- the largest score of every 16 keys ----
+            float most = -INFINITY, ve_max = info.ve[0], x[8], tk[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) moves = moves || x[j] - m + info.ve[j] > d;
-          float keep_o = 1.f;
-          if (moves) {
-            // reference m of the row's scores, and exponent d of p * scale beyond m's own
-            const float top = most > m ? most + SLACK : m, ref = top == -INFINITY ? 0.f : top, less = m - ref;
-            float beyond = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) beyond = fmaxf(beyond, x[j] - ref + info.ve[j]);
-            const float tod = fmaxf(beyond > d + less ? beyond + SLACK : d + less, ve_max - kv::SPAN);
-            keep_o = tod == -INFINITY ? 0.f : kv::ex2(less + (d - tod));
-            m = top;
-            d = tod;
-            l *= kv::ex2(less);
-          }
-          if (!first_tile && __any_sync(0xffffffffu, moves)) {
-#pragma unroll 1
-            for (int c0 = 0; c0 < DP; c0 += 32) {
-              uint32_t y[32];
-              tmem_issue32(col_o(half) + c0 + quad, y);
+            for (int h = 0; h < 2; ++h) {
+              uint32_t y[2][32];
+              tmem_issue32(col_s(half) + 64 * h + quad, y[0]);
+              tmem_issue32(col_s(half) + 64 * h + 32 + quad, y[1]);
               tmem_wait_ld();
-              tmem_landed32(y);
+              tmem_landed32(y[0]);
+              tmem_landed32(y[1]);
 #pragma unroll
-              for (int c = 0; c < 32; ++c) y[c] = __float_as_uint(__uint_as_float(y[c]) * keep_o);
+              for (int k = 0; k < 4; ++k) {
+                const int j = 4 * h + k;
+                float v[16];
 #pragma unroll
-              for (int c = 0; c < 32; c += 8) tmem_store8(col_o(half) + c0 + c + quad, y + c);
-            }
-          }
-          const float ref = m == -INFINITY ? 0.f : m;
-          const bool large = __any_sync(0xffffffffu, fabsf(ref) > 4194304.f);      // scores in steps of a quarter and more: a difference of rounded ones
-          // ---- probabilities times their values' scale, as shares of 2^15 at the references ----
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t y[2][32];
-            tmem_issue32(col_s(half) + 64 * h + quad, y[0]);
-            tmem_issue32(col_s(half) + 64 * h + 32 + quad, y[1]);
-            tmem_wait_ld();
-            tmem_landed32(y[0]);
-            tmem_landed32(y[1]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int j = 4 * h + k;
-              const float e = (float)kv::P_BITS + fminf(fmaxf(info.lv[j] - d, -kv::SPAN), kv::SPAN), tk = factor_of(j), from = large ? e : e - ref;
-              const float2 t2 = make_float2(large ? 1.f : tk, large ? 1.f : tk), f2 = make_float2(from, from);
-              float2 sum = make_float2(0.f, 0.f);
-              uint32_t hi[8], lo[8];
-#pragma unroll
-              for (int c = 0; c < 16; c += 2) {
-                float2 v = make_float2(__uint_as_float(y[k >> 1][(k & 1) * 16 + c]), __uint_as_float(y[k >> 1][(k & 1) * 16 + c + 1]));
-                if (!whole) {
-                  if (masked(j, c)) v.x = -INFINITY;
-                  if (masked(j, c + 1)) v.y = -INFINITY;
+                for (int c = 0; c < 16; ++c) {
+                  v[c] = __uint_as_float(y[k >> 1][(k & 1) * 16 + c]);
+                  if (MASKED && (16 * j + c < lo || 16 * j + c >= hi || info.ks[j] < 0.f)) v[c] = -INFINITY;
                 }
-                if (large) v = make_float2(__fsub_rn(__fmul_rn(v.x, tk), ref), __fsub_rn(__fmul_rn(v.y, tk), ref));
-                v = kv::fma2(v, t2, f2);
-                v.x = kv::ex2(v.x);
-                v.y = kv::ex2(v.y);
-                sum = kv::add2(sum, v);
-                hi[c / 2] = kv::pack_f16(v.x, v.y);
-                if (WIDE) lo[c / 2] = kv::rest_f16(v.x, v.y, hi[c / 2]);
+                float t0 = kv::max3(v[0], v[1], v[2]), t1 = kv::max3(v[3], v[4], v[5]);
+                t0 = kv::max3(t0, v[6], v[7]); t1 = kv::max3(t1, v[8], v[9]);
+                t0 = kv::max3(t0, v[10], v[11]); t1 = kv::max3(t1, v[12], v[13]);
+                t0 = kv::max3(t0, v[14], v[15]);
+                tk[j] = fmaxf(factor * fabsf(info.ks[j]) * rest, FLT_MIN);          // (not 0 times -inf)
+                x[j] = ceilf(fmaxf(t0, t1) * tk[j]);         // references are whole numbers: what goes from one to another is an exact power of two
+                most = fmaxf(most, x[j]);
+                ve_max = fmaxf(ve_max, info.ve[j]);
               }
-              l = fmaf(sum.x + sum.y, kv::ex2(-e), l);
-              tmem_store8(col_s(half) + 16 * j + quad, hi);
-              if (WIDE) tmem_store8(col_s(half) + 16 * j + 8 + quad, lo);
             }
-          }
+            bool moves = most > m || ve_max - kv::SPAN > d;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) moves = moves || x[j] - m + info.ve[j] > d;
+            moves = moves && mine;
+            if (__any_sync(0xffffffffu, moves)) {
+              float keep_o = 1.f;
+              if (moves) {
+                // reference m of the row's scores, and exponent d of p * scale beyond m's own
+                const float top = most > m ? most + SLACK : m, to = top == -INFINITY ? 0.f : top, less = m - to;
+                float beyond = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) beyond = fmaxf(beyond, x[j] - to + info.ve[j]);
+                const float tod = fmaxf(beyond > d + less ? beyond + SLACK : d + less, ve_max - kv::SPAN);
+                keep_o = tod == -INFINITY ? 0.f : kv::ex2(less + (d - tod));
+                m = top;
+                d = tod;
+                l *= kv::ex2(less);
+              }
+              if (!first_tile) {
+#pragma unroll 1
+                for (int c0 = 0; c0 < DP; c0 += 32) {
+                  uint32_t y[32];
+                  tmem_issue32(col_o(half) + c0 + quad, y);
+                  tmem_wait_ld();
+                  tmem_landed32(y);
+#pragma unroll
+                  for (int c = 0; c < 32; ++c) y[c] = __float_as_uint(__uint_as_float(y[c]) * keep_o);
+#pragma unroll
+                  for (int c = 0; c < 32; c += 8) tmem_store8(col_o(half) + c0 + c + quad, y + c);
+                }
+              }
+            }
+            // ---- probabilities times their values' scale, as shares of 2^15 at the references ----
+            const float ref = m == -INFINITY ? 0.f : m;
+            // Scores in steps of a quarter and more: a difference of rounded ones.  (Along with masks, in a form of its own.)
+            const bool large = __any_sync(0xffffffffu, mine && fabsf(ref) > 4194304.f);
+            auto second = [&](auto any_scores) {
+              constexpr bool ANY = decltype(any_scores)::value;
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                uint32_t y[2][32];
+                tmem_issue32(col_s(half) + 64 * h + quad, y[0]);
+                tmem_issue32(col_s(half) + 64 * h + 32 + quad, y[1]);
+                tmem_wait_ld();
+                tmem_landed32(y[0]);
+                tmem_landed32(y[1]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const int j = 4 * h + k;
+                  const float e = (float)kv::P_BITS + fminf(fmaxf(info.lv[j] - d, -kv::SPAN), kv::SPAN), from = ANY && large ? e : e - ref;
+                  const float t = ANY && large ? 1.f : tk[j];
+                  float2 sum;
+                  uint32_t hi16[8], lo16[8];
+#pragma unroll
+                  for (int c = 0; c < 16; c += 2) {
+                    float2 v = make_float2(__uint_as_float(y[k >> 1][(k & 1) * 16 + c]), __uint_as_float(y[k >> 1][(k & 1) * 16 + c + 1]));
+                    if (ANY) {
+                      if (large) v = make_float2(__fsub_rn(__fmul_rn(v.x, tk[j]), ref), __fsub_rn(__fmul_rn(v.y, tk[j]), ref));
+                      if (16 * j + c < lo || 16 * j + c >= hi || info.ks[j] < 0.f) v.x = -INFINITY;
+                      if (16 * j + c + 1 < lo || 16 * j + c + 1 >= hi || info.ks[j] < 0.f) v.y = -INFINITY;
+                    }
+                    v = kv::fma2(v, make_float2(t, t), make_float2(from, from));
+                    v.x = kv::ex2(v.x);
+                    v.y = kv::ex2(v.y);
+                    sum = c == 0 ? v : kv::add2(sum, v);
+                    hi16[c / 2] = kv::pack_f16(v.x, v.y);
+                    if (WIDE) lo16[c / 2] = kv::rest_f16(v.x, v.y, hi16[c / 2]);
+                  }
+                  l = fmaf(sum.x + sum.y, kv::ex2(-e), l);
+                  tmem_store8(col_s(half) + 16 * j + quad, hi16);
+                  if (WIDE) tmem_store8(col_s(half) + 16 * j + 8 + quad, lo16);
+                }
+              }
+            };
+            if (MASKED || large) second(std::true_type());
+            else second(std::false_type());
+          };
+          if (whole) tile(std::false_type());
+          else tile(std::true_type());
           tmem_wait_st();
         }
         before_sync();
