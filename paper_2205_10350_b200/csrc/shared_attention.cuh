@@ -1,8 +1,6 @@
 // Attention over the 8-bit key/value cache for rows that share prefixes: the shared positions once for all rows of a group, on the tensor cores' own memory.
 #pragma once
 
-#include <type_traits>
-
 #include "cache_attention.cuh"
 #include "gemm_tc.cuh"
 
@@ -238,7 +236,7 @@ struct Info { float ks[8], ve[8], lv[8]; };                   // scales of the k
 template <int DIM, bool WIDE>
 struct Small {
   typedef Layout<DIM, WIDE> L;
-  uint64_t raw_full[L::N_RAW], raw_empty[L::N_RAW], full[L::N_TILES], empty[L::N_TILES], s[2], p[2], o[2], q, seg, drain;
+  uint64_t raw_full[L::N_RAW], raw_empty[L::N_RAW], full[L::N_TILES], empty[L::N_TILES], s[2], p[2][2], o[2], q, seg, drain;
   Info info[L::N_INFO];
   Segment segment[2];                  // for the softmax's warps, whose registers are short; two: the one in front is stored late
   int exponent[M_ROWS];                // of the rows' largest numbers, where both halves of the keys want them
@@ -332,7 +330,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
   if (threadIdx.x == 0) {
     for (int i = 0; i < L::N_RAW; ++i) { tc::mbar_init(bar(sm.raw_full[i]), 1); tc::mbar_init(bar(sm.raw_empty[i]), CONVERT_WARPS); }
     for (int i = 0; i < L::N_TILES; ++i) { tc::mbar_init(bar(sm.full[i]), CONVERT_WARPS); tc::mbar_init(bar(sm.empty[i]), 1); }
-    for (int i = 0; i < 2; ++i) { tc::mbar_init(bar(sm.s[i]), 1); tc::mbar_init(bar(sm.p[i]), 4); tc::mbar_init(bar(sm.o[i]), 1); }
+    for (int i = 0; i < 2; ++i) { tc::mbar_init(bar(sm.s[i]), 1); tc::mbar_init(bar(sm.p[i][0]), 4); tc::mbar_init(bar(sm.p[i][1]), 4); tc::mbar_init(bar(sm.o[i]), 1); }
     tc::mbar_init(bar(sm.q), SOFTMAX_WARPS);
     tc::mbar_init(bar(sm.seg), 1);
     tc::mbar_init(bar(sm.drain), 1);
@@ -351,11 +349,12 @@ shared_attention_kernel(const __grid_constant__ Params a) {
   after_sync();
   pdl_launch();
   pdl_wait();
-  const uint32_t tmem = sm.tmem;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sm.tmem, 0);
   auto col_s = [&](int t) { return tmem + t * 128; };          // scores, and over them probabilities
   auto col_o = [&](int t) { return tmem + 256 + t * DP; };
   auto aborted = [&]() { return *reinterpret_cast<volatile int*>(&sm.abort) != 0; };
   auto wait_warp = [&](uint64_t& b, uint32_t parity) {
+    if (__all_sync(0xffffffffu, tc::mbar_try_wait(bar(b), parity))) return true;
     if (__any_sync(0xffffffffu, aborted()) || !tc::mbar_wait_warp(bar(b), parity, a.status)) { sm.abort = 1; return false; }
     return true;
   };
@@ -533,21 +532,27 @@ shared_attention_kernel(const __grid_constant__ Params a) {
     };
     auto values = [&](int t, int fill, bool first, bool last, bool end) {
       const int slot = slot_of(fill);
-      if (!wait_warp(sm.full[slot], phase_of(fill)) || !wait_warp(sm.p[t], p_phase[t])) return false;
-      p_phase[t] ^= 1u;
-      after_sync();
-      if (tc::elect_one()) {
-        const uint32_t v = smem + L::F16 + slot * L::TILE;
+      if (!wait_warp(sm.full[slot], phase_of(fill))) return false;
+      const uint32_t v = smem + L::F16 + slot * L::TILE;
 #pragma unroll
-        for (int j = 0; j < KEYS / 16; ++j) {
+      for (int part = 0; part < 2; ++part) {                   // (probabilities come in two halves)
+        if (!wait_warp(sm.p[t][part], p_phase[t])) return false;
+        after_sync();
+        if (tc::elect_one()) {
 #pragma unroll
-          for (int h = WIDE ? 1 : 0; h >= 0; --h)
-            umma_f16_ts(col_o(t), col_s(t) + 16 * j + 8 * h, value_desc(v + j * 2048), idesc_o, (!first || j > 0 || (WIDE && h == 0)) ? 1u : 0u);
+          for (int j = part * KEYS / 32; j < (part + 1) * KEYS / 32; ++j) {
+#pragma unroll
+            for (int h = WIDE ? 1 : 0; h >= 0; --h)
+              umma_f16_ts(col_o(t), col_s(t) + 16 * j + 8 * h, value_desc(v + j * 2048), idesc_o, (!first || j > 0 || (WIDE && h == 0)) ? 1u : 0u);
+          }
+          if (part == 1) {
+            if (last) tc::umma_commit(bar(sm.empty[slot]));
+            if (end) tc::umma_commit(bar(sm.o[t]));
+          }
         }
-        if (last) tc::umma_commit(bar(sm.empty[slot]));
-        if (end) tc::umma_commit(bar(sm.o[t]));
+        __syncwarp();
       }
-      __syncwarp();
+      p_phase[t] ^= 1u;
       return true;
     };
     int turn = 0;
@@ -566,8 +571,9 @@ shared_attention_kernel(const __grid_constant__ Params a) {
       ok = wait_warp(sm.q, q_phase);
       q_phase ^= 1u;
       after_sync();
-      const int n = s.t1 - s.t0;
-      if (s.two) {
+      const int n = __shfl_sync(0xffffffffu, s.t1 - s.t0, 0);      // (so that the compiler knows it to be the same in all lanes)
+      const bool two = __shfl_sync(0xffffffffu, (int)s.two, 0) != 0;
+      if (two) {
         // two tiles of rows take turns: while one's scores become probabilities, the other's are multiplied
         ok = ok && scores(0, 0, next_k, false) && scores(1, 1, next_k, true);
         for (int i = 0; i < n && ok; ++i) {
@@ -715,131 +721,148 @@ shared_attention_kernel(const __grid_constant__ Params a) {
         if (!ok) break;
         s_phase ^= 1u;
         after_sync();
+        auto hand_over = [&](int part) {
+          tmem_wait_st();
+          before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(sm.p[half][part]));
+        };
         if (busy) {
           const Info& info = sm.info[(info0 + i) & (L::N_INFO - 1)];
           const int pos = key_base(s.lo) + (s.t0 + i) * KEYS;
           bool whole = pos >= s.lo && pos + KEYS <= sees;
 #pragma unroll
           for (int j = 0; j < 8; ++j) whole = whole && info.ks[j] >= 0.f;
-          whole = __all_sync(0xffffffffu, whole);
-          const bool first_tile = i < 2 && (s.two ? i == 0 : true);
-          const int lo = s.lo - pos, hi = sees - pos;
-          // MASKED: some of the keys are not there, or not seen by some row of the warp
-          auto tile = [&](auto masked_keys) {
-            constexpr bool MASKED = decltype(masked_keys)::value;
-            // ---- the largest score of every 16 keys ----
-            float most = -INFINITY, ve_max = info.ve[0], x[8], tk[8];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint32_t y[2][32];
-              tmem_issue32(col_s(half) + 64 * h + quad, y[0]);
-              tmem_issue32(col_s(half) + 64 * h + 32 + quad, y[1]);
-              tmem_wait_ld();
-              tmem_landed32(y[0]);
-              tmem_landed32(y[1]);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const int j = 4 * h + k;
-                float v[16];
-#pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                  v[c] = __uint_as_float(y[k >> 1][(k & 1) * 16 + c]);
-                  if (MASKED && (16 * j + c < lo || 16 * j + c >= hi || info.ks[j] < 0.f)) v[c] = -INFINITY;
-                }
-                float t0 = kv::max3(v[0], v[1], v[2]), t1 = kv::max3(v[3], v[4], v[5]);
-                t0 = kv::max3(t0, v[6], v[7]); t1 = kv::max3(t1, v[8], v[9]);
-                t0 = kv::max3(t0, v[10], v[11]); t1 = kv::max3(t1, v[12], v[13]);
-                t0 = kv::max3(t0, v[14], v[15]);
-                tk[j] = fmaxf(factor * fabsf(info.ks[j]) * rest, FLT_MIN);          // (not 0 times -inf)
-                x[j] = ceilf(fmaxf(t0, t1) * tk[j]);         // references are whole numbers: what goes from one to another is an exact power of two
-                most = fmaxf(most, x[j]);
-                ve_max = fmaxf(ve_max, info.ve[j]);
-              }
-            }
-            bool moves = most > m || ve_max - kv::SPAN > d;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) moves = moves || x[j] - m + info.ve[j] > d;
-            moves = moves && mine;
-            if (__any_sync(0xffffffffu, moves)) {
-              float keep_o = 1.f;
-              if (moves) {
-                // reference m of the row's scores, and exponent d of p * scale beyond m's own
-                const float top = most > m ? most + SLACK : m, to = top == -INFINITY ? 0.f : top, less = m - to;
-                float beyond = -INFINITY;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) beyond = fmaxf(beyond, x[j] - to + info.ve[j]);
-                const float tod = fmaxf(beyond > d + less ? beyond + SLACK : d + less, ve_max - kv::SPAN);
-                keep_o = tod == -INFINITY ? 0.f : kv::ex2(less + (d - tod));
-                m = top;
-                d = tod;
-                l *= kv::ex2(less);
-              }
-              if (!first_tile) {
+          // Scores are changed where they lie, in short loops of their own, before they are looked at: one form of the rest for all tiles, as instructions that are
+          // not in the SM's cache cost more than any of these loops.
+          if (!__all_sync(0xffffffffu, whole)) {                // keys that are not there, or not seen by some row of the warp
+            const int lo = s.lo - pos, hi = sees - pos;
 #pragma unroll 1
-                for (int c0 = 0; c0 < DP; c0 += 32) {
-                  uint32_t y[32];
-                  tmem_issue32(col_o(half) + c0 + quad, y);
-                  tmem_wait_ld();
-                  tmem_landed32(y);
+            for (int j = 0; j < 8; ++j) {
+              uint32_t y[16];
+              tc::tmem_issue16(col_s(half) + 16 * j + quad, y);
+              const bool gone = info.ks[j] < 0.f;
+              tmem_wait_ld();
+              tc::tmem_landed16(y);
 #pragma unroll
-                  for (int c = 0; c < 32; ++c) y[c] = __float_as_uint(__uint_as_float(y[c]) * keep_o);
+              for (int c = 0; c < 16; ++c)
+                if (gone || 16 * j + c < lo || 16 * j + c >= hi) y[c] = 0xff800000u;
+              tmem_store8(col_s(half) + 16 * j + quad, y);
+              tmem_store8(col_s(half) + 16 * j + 8 + quad, y + 8);
+            }
+            tmem_wait_st();
+          }
+          // ---- the largest score of every 16 keys: do references move? ----
+          auto factor_of = [&](int j) { return fmaxf(factor * fabsf(info.ks[j]) * rest, FLT_MIN); };      // (not 0 times -inf)
+          auto over_maxima = [&](auto f) {                      // f(x, log2 of the values' scale): references are whole numbers, so that what goes from
+#pragma unroll 1                                                // one to another is an exact power of two
+            for (int g = 0; g < 4; ++g) {
+              uint32_t y[32];
+              tmem_issue32(col_s(half) + 32 * g + quad, y);
+              const float tk[2] = {factor_of(2 * g), factor_of(2 * g + 1)};
+              tmem_wait_ld();
+              tmem_landed32(y);
 #pragma unroll
-                  for (int c = 0; c < 32; c += 8) tmem_store8(col_o(half) + c0 + c + quad, y + c);
-                }
+              for (int k = 0; k < 2; ++k) {
+                auto v = [&](int c) { return __uint_as_float(y[16 * k + c]); };
+                float t0 = kv::max3(v(0), v(1), v(2)), t1 = kv::max3(v(3), v(4), v(5));
+                t0 = kv::max3(t0, v(6), v(7)); t1 = kv::max3(t1, v(8), v(9));
+                t0 = kv::max3(t0, v(10), v(11)); t1 = kv::max3(t1, v(12), v(13));
+                t0 = kv::max3(t0, v(14), v(15));
+                f(ceilf(fmaxf(t0, t1) * tk[k]), info.ve[2 * g + k]);
               }
             }
-            // ---- probabilities times their values' scale, as shares of 2^15 at the references ----
-            const float ref = m == -INFINITY ? 0.f : m;
-            // Scores in steps of a quarter and more: a difference of rounded ones.  (Along with masks, in a form of its own.)
-            const bool large = __any_sync(0xffffffffu, mine && fabsf(ref) > 4194304.f);
-            auto second = [&](auto any_scores) {
-              constexpr bool ANY = decltype(any_scores)::value;
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                uint32_t y[2][32];
-                tmem_issue32(col_s(half) + 64 * h + quad, y[0]);
-                tmem_issue32(col_s(half) + 64 * h + 32 + quad, y[1]);
-                tmem_wait_ld();
-                tmem_landed32(y[0]);
-                tmem_landed32(y[1]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  const int j = 4 * h + k;
-                  const float e = (float)kv::P_BITS + fminf(fmaxf(info.lv[j] - d, -kv::SPAN), kv::SPAN), from = ANY && large ? e : e - ref;
-                  const float t = ANY && large ? 1.f : tk[j];
-                  float2 sum;
-                  uint32_t hi16[8], lo16[8];
-#pragma unroll
-                  for (int c = 0; c < 16; c += 2) {
-                    float2 v = make_float2(__uint_as_float(y[k >> 1][(k & 1) * 16 + c]), __uint_as_float(y[k >> 1][(k & 1) * 16 + c + 1]));
-                    if (ANY) {
-                      if (large) v = make_float2(__fsub_rn(__fmul_rn(v.x, tk[j]), ref), __fsub_rn(__fmul_rn(v.y, tk[j]), ref));
-                      if (16 * j + c < lo || 16 * j + c >= hi || info.ks[j] < 0.f) v.x = -INFINITY;
-                      if (16 * j + c + 1 < lo || 16 * j + c + 1 >= hi || info.ks[j] < 0.f) v.y = -INFINITY;
-                    }
-                    v = kv::fma2(v, make_float2(t, t), make_float2(from, from));
-                    v.x = kv::ex2(v.x);
-                    v.y = kv::ex2(v.y);
-                    sum = c == 0 ? v : kv::add2(sum, v);
-                    hi16[c / 2] = kv::pack_f16(v.x, v.y);
-                    if (WIDE) lo16[c / 2] = kv::rest_f16(v.x, v.y, hi16[c / 2]);
-                  }
-                  l = fmaf(sum.x + sum.y, kv::ex2(-e), l);
-                  tmem_store8(col_s(half) + 16 * j + quad, hi16);
-                  if (WIDE) tmem_store8(col_s(half) + 16 * j + 8 + quad, lo16);
-                }
-              }
-            };
-            if (MASKED || large) second(std::true_type());
-            else second(std::false_type());
           };
-          if (whole) tile(std::false_type());
-          else tile(std::true_type());
-          tmem_wait_st();
+          float most = -INFINITY, ve_max = -INFINITY;
+          bool moves = false;
+          over_maxima([&](float x, float ve) {
+            most = fmaxf(most, x);
+            ve_max = fmaxf(ve_max, ve);
+            moves = moves || x - m + ve > d;
+          });
+          moves = mine && (moves || most > m || ve_max - kv::SPAN > d);
+          if (__any_sync(0xffffffffu, moves)) {
+            // reference m of the row's scores, and exponent d of p * scale beyond m's own
+            const float top = most > m ? most + SLACK : m, to = top == -INFINITY ? 0.f : top, less = m - to;
+            float beyond = -INFINITY, keep_o = 1.f;
+            over_maxima([&](float x, float ve) { beyond = fmaxf(beyond, x - to + ve); });
+            if (moves) {
+              const float tod = fmaxf(beyond > d + less ? beyond + SLACK : d + less, ve_max - kv::SPAN);
+              keep_o = tod == -INFINITY ? 0.f : kv::ex2(less + (d - tod));
+              m = top;
+              d = tod;
+              l *= kv::ex2(less);
+            }
+            if (i > (s.two ? 0 : 1)) {                          // (the half's first tile has no results in front)
+#pragma unroll 1
+              for (int c0 = 0; c0 < DP; c0 += 16) {
+                uint32_t y[16];
+                tc::tmem_issue16(col_o(half) + c0 + quad, y);
+                tmem_wait_ld();
+                tc::tmem_landed16(y);
+#pragma unroll
+                for (int c = 0; c < 16; ++c) y[c] = __float_as_uint(__uint_as_float(y[c]) * keep_o);
+                tmem_store8(col_o(half) + c0 + quad, y);
+                tmem_store8(col_o(half) + c0 + 8 + quad, y + 8);
+              }
+            }
+          }
+          float ref = m == -INFINITY ? 0.f : m;
+          const bool large = __any_sync(0xffffffffu, mine && fabsf(ref) > 4194304.f);
+          if (large) {                                          // scores in steps of a quarter and more: a difference of rounded ones
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+              uint32_t y[16];
+              tc::tmem_issue16(col_s(half) + 16 * j + quad, y);
+              const float t = factor_of(j);
+              tmem_wait_ld();
+              tc::tmem_landed16(y);
+#pragma unroll
+              for (int c = 0; c < 16; ++c) y[c] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(y[c]), t), ref));
+              tmem_store8(col_s(half) + 16 * j + quad, y);
+              tmem_store8(col_s(half) + 16 * j + 8 + quad, y + 8);
+            }
+            tmem_wait_st();
+            ref = 0.f;
+          }
+          // ---- probabilities times their values' scale, as shares of 2^15 at the references ----
+#pragma unroll 1
+          for (int g = 0; g < 4; ++g) {
+            uint32_t y[32];
+            tmem_issue32(col_s(half) + 32 * g + quad, y);
+            float e[2], t[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              e[k] = (float)kv::P_BITS + fminf(fmaxf(info.lv[2 * g + k] - d, -kv::SPAN), kv::SPAN);
+              t[k] = large ? 1.f : factor_of(2 * g + k);
+            }
+            tmem_wait_ld();
+            tmem_landed32(y);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float from = e[k] - ref;
+              float2 sum;
+              uint32_t hi[8], lo[8];
+#pragma unroll
+              for (int c = 0; c < 16; c += 2) {
+                float2 v = make_float2(__uint_as_float(y[16 * k + c]), __uint_as_float(y[16 * k + c + 1]));
+                v = kv::fma2(v, make_float2(t[k], t[k]), make_float2(from, from));
+                v.x = kv::ex2(v.x);
+                v.y = kv::ex2(v.y);
+                sum = c == 0 ? v : kv::add2(sum, v);
+                hi[c / 2] = kv::pack_f16(v.x, v.y);
+                if (WIDE) lo[c / 2] = kv::rest_f16(v.x, v.y, hi[c / 2]);
+              }
+              l = fmaf(sum.x + sum.y, kv::ex2(-e[k]), l);
+              tmem_store8(col_s(half) + 32 * g + 16 * k + quad, hi);
+              if (WIDE) tmem_store8(col_s(half) + 32 * g + 16 * k + 8 + quad, lo);
+            }
+            if (g == 1) hand_over(0);                            // (the second product begins with the first half)
+          }
+        } else {
+          hand_over(0);
         }
-        before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(sm.p[half]));
+        hand_over(1);
       }
       info0 += n;
       pending = true;
