@@ -314,6 +314,15 @@ struct Turn {
   }
 };
 
+// The rest of a wait by a whole warp whose first look found nothing.  (Out of line: the kernel's roles compete for the SM's instruction cache.)
+__device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort, int* status) {
+  if (__any_sync(0xffffffffu, *abort != 0) || !tc::mbar_wait_warp(bar, parity, status)) {
+    *abort = 1;
+    return false;
+  }
+  return true;
+}
+
 template <typename T, typename F, int DIM>
 __global__ void __launch_bounds__(THREADS, 1)
 shared_attention_kernel(const __grid_constant__ Params a) {
@@ -355,8 +364,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
   auto aborted = [&]() { return *reinterpret_cast<volatile int*>(&sm.abort) != 0; };
   auto wait_warp = [&](uint64_t& b, uint32_t parity) {
     if (__all_sync(0xffffffffu, tc::mbar_try_wait(bar(b), parity))) return true;
-    if (__any_sync(0xffffffffu, aborted()) || !tc::mbar_wait_warp(bar(b), parity, a.status)) { sm.abort = 1; return false; }
-    return true;
+    return wait_on(bar(b), parity, &sm.abort, a.status);
   };
   Walk walk;
   const bool work = walk.begin(a);
@@ -465,8 +473,8 @@ shared_attention_kernel(const __grid_constant__ Params a) {
           bool whole = pos >= s.lo && pos + KEYS <= s.hi;
 #pragma unroll
           for (int j = 0; j < 8; ++j) whole = whole && sm.info[info].ks[j] >= 0.f;
-          constexpr int AT_ONCE = N < 8 ? N : 8;
-#pragma unroll
+          constexpr int AT_ONCE = 4;
+#pragma unroll 1
           for (int i0 = 0; i0 < N; i0 += AT_ONCE) {
             uint2 w[AT_ONCE];
 #pragma unroll
@@ -573,25 +581,13 @@ shared_attention_kernel(const __grid_constant__ Params a) {
       after_sync();
       const int n = __shfl_sync(0xffffffffu, s.t1 - s.t0, 0);      // (so that the compiler knows it to be the same in all lanes)
       const bool two = __shfl_sync(0xffffffffu, (int)s.two, 0) != 0;
-      if (two) {
-        // two tiles of rows take turns: while one's scores become probabilities, the other's are multiplied
-        ok = ok && scores(0, 0, next_k, false) && scores(1, 1, next_k, true);
-        for (int i = 0; i < n && ok; ++i) {
-          const int k = next_k + 2 * (i + 1), v = next_k + 2 * i + 1;
-          ok = values(0, v, i == 0, false, i + 1 == n);
-          if (ok && i + 1 < n) ok = scores(0, 0, k, false);
-          if (ok) ok = values(1, v, i == 0, true, i + 1 == n);
-          if (ok && i + 1 < n) ok = scores(1, 1, k, true);
-        }
-      } else {
-        // one tile of rows: two halves of the keys do
-        ok = ok && scores(0, 0, next_k, true);
-        if (n > 1) ok = ok && scores(1, 0, next_k + 2, true);
-        for (int i = 0; i < n && ok; ++i) {
-          const int v = next_k + 2 * i + 1;
-          ok = values(i & 1, v, i < 2, true, i + 2 >= n);
-          if (ok && i + 2 < n) ok = scores(i & 1, 0, next_k + 2 * (i + 2), true);
-        }
+      // The halves take turns: while one's scores become probabilities, the other's are multiplied.  Each is a tile of rows over all tiles of keys (two), or
+      // every other tile of keys for the same rows.
+      const int last = two ? 2 * n : n;
+      for (int u = 0; u < last + 2 && ok; ++u) {
+        const int t = u & 1;
+        if (u >= 2) ok = values(t, next_k + 2 * (two ? (u - 2) >> 1 : u - 2) + 1, u < 4, !two || t == 1, u >= last);
+        if (u < last && ok) ok = scores(t, two ? t : 0, next_k + 2 * (two ? u >> 1 : u), !two || t == 1);
       }
       next_k += 2 * n;
       more = walk.next(a, s);
@@ -754,39 +750,41 @@ shared_attention_kernel(const __grid_constant__ Params a) {
           }
           // ---- the largest score of every 16 keys: do references move? ----
           auto factor_of = [&](int j) { return fmaxf(factor * fabsf(info.ks[j]) * rest, FLT_MIN); };      // (not 0 times -inf)
-          auto over_maxima = [&](auto f) {                      // f(x, log2 of the values' scale): references are whole numbers, so that what goes from
-#pragma unroll 1                                                // one to another is an exact power of two
+          // (references are whole numbers, so that what goes from one to another is an exact power of two)
+          float keep_o = 1.f;
+          bool moved = false;
+          for (float to = m == -INFINITY ? 0.f : m;;) {
+            float most = -INFINITY, ve_max = -INFINITY, beyond = -INFINITY;
+            uint32_t y[2][16];
+            tc::tmem_issue16(col_s(half) + quad, y[0]);
+#pragma unroll 1
             for (int g = 0; g < 4; ++g) {
-              uint32_t y[32];
-              tmem_issue32(col_s(half) + 32 * g + quad, y);
-              const float tk[2] = {factor_of(2 * g), factor_of(2 * g + 1)};
-              tmem_wait_ld();
-              tmem_landed32(y);
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                auto v = [&](int c) { return __uint_as_float(y[16 * k + c]); };
+                tmem_wait_ld();
+                tc::tmem_landed16(y[k]);
+                if (k == 0 || g < 3) tc::tmem_issue16(col_s(half) + 32 * g + 16 * (k + 1) + quad, y[k ^ 1]);
+                auto v = [&](int c) { return __uint_as_float(y[k][c]); };
                 float t0 = kv::max3(v(0), v(1), v(2)), t1 = kv::max3(v(3), v(4), v(5));
                 t0 = kv::max3(t0, v(6), v(7)); t1 = kv::max3(t1, v(8), v(9));
                 t0 = kv::max3(t0, v(10), v(11)); t1 = kv::max3(t1, v(12), v(13));
                 t0 = kv::max3(t0, v(14), v(15));
-                f(ceilf(fmaxf(t0, t1) * tk[k]), info.ve[2 * g + k]);
+                const float x = ceilf(fmaxf(t0, t1) * factor_of(2 * g + k)), ve = info.ve[2 * g + k];
+                most = fmaxf(most, x);
+                ve_max = fmaxf(ve_max, ve);
+                beyond = fmaxf(beyond, x - to + ve);
               }
             }
-          };
-          float most = -INFINITY, ve_max = -INFINITY;
-          bool moves = false;
-          over_maxima([&](float x, float ve) {
-            most = fmaxf(most, x);
-            ve_max = fmaxf(ve_max, ve);
-            moves = moves || x - m + ve > d;
-          });
-          moves = mine && (moves || most > m || ve_max - kv::SPAN > d);
-          if (__any_sync(0xffffffffu, moves)) {
+            if (!moved) {
+              moved = mine && (most > m || beyond > d || ve_max - kv::SPAN > d);
+              if (!__any_sync(0xffffffffu, moved)) break;
+              if (moved && most > m) to = most + SLACK;         // ... and how far p * scale goes beyond that: the same again
+              moved = true;
+              continue;
+            }
             // reference m of the row's scores, and exponent d of p * scale beyond m's own
-            const float top = most > m ? most + SLACK : m, to = top == -INFINITY ? 0.f : top, less = m - to;
-            float beyond = -INFINITY, keep_o = 1.f;
-            over_maxima([&](float x, float ve) { beyond = fmaxf(beyond, x - to + ve); });
-            if (moves) {
+            if (mine && (most > m || beyond > d || ve_max - kv::SPAN > d)) {
+              const float top = most > m ? to : m, less = m - to;
               const float tod = fmaxf(beyond > d + less ? beyond + SLACK : d + less, ve_max - kv::SPAN);
               keep_o = tod == -INFINITY ? 0.f : kv::ex2(less + (d - tod));
               m = top;
@@ -806,6 +804,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
                 tmem_store8(col_o(half) + c0 + 8 + quad, y + 8);
               }
             }
+            break;
           }
           float ref = m == -INFINITY ? 0.f : m;
           const bool large = __any_sync(0xffffffffu, mine && fabsf(ref) > 4194304.f);
@@ -826,34 +825,29 @@ shared_attention_kernel(const __grid_constant__ Params a) {
             ref = 0.f;
           }
           // ---- probabilities times their values' scale, as shares of 2^15 at the references ----
+          uint32_t y[2][16];
+          tc::tmem_issue16(col_s(half) + quad, y[0]);
 #pragma unroll 1
           for (int g = 0; g < 4; ++g) {
-            uint32_t y[32];
-            tmem_issue32(col_s(half) + 32 * g + quad, y);
-            float e[2], t[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              e[k] = (float)kv::P_BITS + fminf(fmaxf(info.lv[2 * g + k] - d, -kv::SPAN), kv::SPAN);
-              t[k] = large ? 1.f : factor_of(2 * g + k);
-            }
-            tmem_wait_ld();
-            tmem_landed32(y);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const float from = e[k] - ref;
+              const float e = (float)kv::P_BITS + fminf(fmaxf(info.lv[2 * g + k] - d, -kv::SPAN), kv::SPAN), from = e - ref, t = large ? 1.f : factor_of(2 * g + k);
+              tmem_wait_ld();
+              tc::tmem_landed16(y[k]);
+              if (k == 0 || g < 3) tc::tmem_issue16(col_s(half) + 32 * g + 16 * (k + 1) + quad, y[k ^ 1]);
               float2 sum;
               uint32_t hi[8], lo[8];
 #pragma unroll
               for (int c = 0; c < 16; c += 2) {
-                float2 v = make_float2(__uint_as_float(y[16 * k + c]), __uint_as_float(y[16 * k + c + 1]));
-                v = kv::fma2(v, make_float2(t[k], t[k]), make_float2(from, from));
+                float2 v = make_float2(__uint_as_float(y[k][c]), __uint_as_float(y[k][c + 1]));
+                v = kv::fma2(v, make_float2(t, t), make_float2(from, from));
                 v.x = kv::ex2(v.x);
                 v.y = kv::ex2(v.y);
                 sum = c == 0 ? v : kv::add2(sum, v);
                 hi[c / 2] = kv::pack_f16(v.x, v.y);
                 if (WIDE) lo[c / 2] = kv::rest_f16(v.x, v.y, hi[c / 2]);
               }
-              l = fmaf(sum.x + sum.y, kv::ex2(-e[k]), l);
+              l = fmaf(sum.x + sum.y, kv::ex2(-e), l);
               tmem_store8(col_s(half) + 32 * g + 16 * k + quad, hi);
               if (WIDE) tmem_store8(col_s(half) + 32 * g + 16 * k + 8 + quad, lo);
             }
