@@ -9,8 +9,6 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libad_b200.so")
 SOURCES = ["ad_api.cu", "cache_api.cu", "pool_api.cu", "shared_api.cu"]
-# Compiled as wholes, without relocatable device code, which would fix a thread's registers for all warps of a kernel.
-WHOLE = ["shared_api.cu"]
 HEADERS = ["ad_common.cuh", "gemm_tc.cuh", "gemm_tc_pair.cuh", "gemm_simt.cuh", "gemm_few.cuh", "attention.cuh", "attention_few.cuh", "attention_mma.cuh", "ffn_few.cuh", "sublayer_f32.cuh", "steps.cuh", "accept.cuh", "grid_sync.cuh", "mega.cuh", "kv_cache.cuh", "cache_attention.cuh", "accept_sampled.cuh", "shared_attention.cuh", "block_pool.cuh", "sample.cuh", "cache_checks.h", "op_launch.h"]
 
 
@@ -34,7 +32,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         flags += ["-Xptxas", "-v"]
     with tempfile.TemporaryDirectory() as folder:
         objects = [os.path.join(folder, s[:-3] + ".o") for s in SOURCES]
-        running = [subprocess.Popen([nvcc, *flags, *([] if s in WHOLE else ["-rdc=true"]), "-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, objects)]
+        running = [subprocess.Popen([nvcc, *flags, "-rdc=true", "-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, objects)]
         codes = [r.wait() for r in running]
         if any(codes):
             raise RuntimeError("compilation failed: " + ", ".join(s for s, c in zip(SOURCES, codes) if c))

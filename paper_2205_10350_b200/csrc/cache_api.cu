@@ -145,44 +145,58 @@ cudaError_t launch_attention_dim(const kv::AttendParams& a, const AttendPlan& pl
 }
 }  // namespace
 
+size_t ad::cache_attention_scratch(const ad_kv_cache* c, int n_heads, int B, int max_new, int max_keys) {
+  return attend_part_bytes(c, attend_plan(c, n_heads, B, max_new, max_keys), B);
+}
+cudaError_t ad::cache_attention(const ad_kv_cache* c, const AttentionCall& call, void* scratch, cudaStream_t st) {
+  const AttendPlan plan = attend_plan(c, call.n_heads, call.B, call.max_new, call.max_keys);
+  kv::AttendParams a;
+  a.c = device_cache(c); a.c.first = call.first;
+  a.q = call.q; a.q_stride = (size_t)call.q_stride; a.out = call.out; a.n_heads = call.n_heads; a.M = call.M; a.max_new = call.max_new; a.off = call.off; a.len = call.len;
+  a.causal = call.causal; a.scale = call.scale * (float)M_LOG2E; a.status = call.status; a.mean = call.mean; a.weight = call.weight;
+  // More than half of L2 would not be there any more for the next call, and drives out what others keep there (1 x 200001 keys 104 -> 91 us); tiles of
+  // the same row read one another's keys from L2.
+  a.stream_once = plan.row_tiles == 1 && (double)call.B * longest_row(c, call.max_keys) * c->n_kv_heads * c->head_dim * 2 > (64 << 20);
+  a.B = call.B; a.grid = plan.grid; a.granule = plan.granule; a.fixed = kItemFixed;
+  a.prefix = static_cast<long long*>(scratch); a.part = reinterpret_cast<float*>(static_cast<char*>(scratch) + attend_prefix_bytes(call.B));
+  return by_types(call.dtype, c->format, [&](auto t) {
+    typedef typename decltype(t)::Num T;
+    typedef typename decltype(t)::Fmt F;
+    return c->head_dim == 32 ? launch_attention_dim<T, F, 32>(a, plan, st) : c->head_dim == 64 ? launch_attention_dim<T, F, 64>(a, plan, st)
+                                                                                              : launch_attention_dim<T, F, 128>(a, plan, st);
+  });
+}
+
 extern "C" size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
   if (cache_fault(c, B) || B < 1 || max_new < 1 || max_keys < 0 || !known_dtype(dtype) || !attend_sizes(c, n_heads, max_new)) return 0;
-  return attend_part_bytes(c, attend_plan(c, n_heads, B, max_new, max_keys), B);
+  return cache_attention_scratch(c, n_heads, B, max_new, max_keys);
+}
+
+const char* ad::cache_attention_fault(const ad_kv_cache* c, const AttentionCall& call) {
+  if (const char* why = batch_fault(call.off, call.len, call.B, call.M, call.max_new)) return why;
+  if (const char* why = cache_fault(c, call.B)) return why;
+  if (!known_dtype(call.dtype)) return "unknown dtype";
+  if (!attend_sizes(c, call.n_heads, call.max_new)) return "query heads must be a multiple of the cache's, at most 65535, and max_new times their ratio at most 2^24 (times them, 2^30)";
+  if (call.max_keys < 0) return "negative number of keys";
+  if (!(call.scale > 0.f) || !(call.scale <= 1e30f)) return "the scale must be positive, and 1e30 at most";
+  if (call.M == 0) return nullptr;
+  if (!call.q || !call.out || !aligned(call.q, 16) || !aligned(call.out, 16)) return "queries and result must be 16-byte aligned";
+  if (call.q_stride < (int64_t)call.n_heads * c->head_dim || call.q_stride % (int64_t)(16 / dtype_bytes(call.dtype)))
+    return "queries must be a multiple of 16 bytes apart, and not overlap";
+  return nullptr;
 }
 
 extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
                                   const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, int32_t causal, float scale, void* out,
                                   void* scratch, size_t scratch_bytes, int32_t* status, void* stream) {
   const char* entry = "ad_cache_attention";
-  if (const char* why = batch_fault(off, len, B, M, max_new)) return arg_fault(entry, why);
-  if (const char* why = cache_fault(c, B)) return arg_fault(entry, why);
-  if (!known_dtype(dtype)) return arg_fault(entry, "unknown dtype");
-  if (!attend_sizes(c, n_heads, max_new)) return arg_fault(entry, "query heads must be a multiple of the cache's, at most 65535, and max_new times their ratio at most 2^24 (times them, 2^30)");
-  if (max_keys < 0) return arg_fault(entry, "negative number of keys");
-  if (!(scale > 0.f) || !(scale <= 1e30f)) return arg_fault(entry, "the scale must be positive, and 1e30 at most");
+  const AttentionCall call = {q, dtype, q_stride, n_heads, off, len, B, M, max_new, max_keys, causal != 0, scale, out, status, nullptr, nullptr, nullptr};
+  if (const char* why = cache_attention_fault(c, call)) return arg_fault(entry, why);
   if (M == 0) return AD_OK;
-  if (!q || !out || !aligned(q, 16) || !aligned(out, 16)) return arg_fault(entry, "queries and result must be 16-byte aligned");
-  if (q_stride < (int64_t)n_heads * c->head_dim || q_stride % (int64_t)(16 / dtype_bytes(dtype)))
-    return arg_fault(entry, "queries must be a multiple of 16 bytes apart, and not overlap");
-  const AttendPlan plan = attend_plan(c, n_heads, B, max_new, max_keys);
-  const size_t need = attend_part_bytes(c, plan, B);
+  const size_t need = cache_attention_scratch(c, n_heads, B, max_new, max_keys);
   if (scratch_bytes < need) return op_fail(AD_ERR_CAPACITY, entry, "scratch too small");
   if (need && (!scratch || !aligned(scratch, 256))) return arg_fault(entry, "scratch must be 256-byte aligned");
-  kv::AttendParams a;
-  a.c = device_cache(c); a.q = q; a.q_stride = (size_t)q_stride; a.out = out; a.n_heads = n_heads; a.M = M; a.max_new = max_new; a.off = off; a.len = len;
-  a.causal = causal != 0; a.scale = scale * (float)M_LOG2E; a.status = status;
-  // More than half of L2 would not be there any more for the next call, and drives out what others keep there (1 x 200001 keys 104 -> 91 us); tiles of
-  // the same row read one another's keys from L2.
-  a.stream_once = plan.row_tiles == 1 && (double)B * longest_row(c, max_keys) * c->n_kv_heads * c->head_dim * 2 > (64 << 20);
-  a.B = B; a.grid = plan.grid; a.granule = plan.granule; a.fixed = kItemFixed;
-  a.prefix = static_cast<long long*>(scratch); a.part = reinterpret_cast<float*>(static_cast<char*>(scratch) + attend_prefix_bytes(B));
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return launched(entry, by_types(dtype, c->format, [&](auto t) {
-    typedef typename decltype(t)::Num T;
-    typedef typename decltype(t)::Fmt F;
-    return c->head_dim == 32 ? launch_attention_dim<T, F, 32>(a, plan, st) : c->head_dim == 64 ? launch_attention_dim<T, F, 64>(a, plan, st)
-                                                                                              : launch_attention_dim<T, F, 128>(a, plan, st);
-  }));
+  return launched(entry, cache_attention(c, call, scratch, static_cast<cudaStream_t>(stream)));
 }
 
 namespace {

@@ -26,6 +26,9 @@ struct AttendParams {
   int granule;             // units that one CTA works on at the least where a row's keys are split; 0: they are not
   float* part;             // [2 grid][tile rows][dim] means of values, then [2 grid][tile rows] maxima and sums of exponentials
   long long* prefix;       // [B + 1] granules in front of each row of the batch
+  // Not null: results go here instead of out, means of values [M, n_heads, dim] and maxima and sums of exponentials [M, n_heads], to be joined with others.
+  float* mean;
+  float2* weight;
 };
 
 constexpr int UNIT = 32;               // keys that a warp works on at a time
@@ -194,7 +197,13 @@ __device__ __forceinline__ void store_results(const AttendParams& a, const Segme
       if (d0 == 0) reinterpret_cast<float2*>(a.part + 2 * (size_t)a.grid * ROWS * DIM)[slot * ROWS + r] = make_float2(top, sum);
     } else {
       const int row = r0 + r;
-      store8(static_cast<T*>(a.out) + ((size_t)(seg.work.o + row / group) * a.n_heads + kvh * group + row % group) * DIM + d0, x);
+      const size_t at = (size_t)(seg.work.o + row / group) * a.n_heads + kvh * group + row % group;
+      if (a.mean) {
+        store8(a.mean + at * DIM + d0, x);
+        if (d0 == 0) a.weight[at] = make_float2(top, sum);
+      } else {
+        store8(static_cast<T*>(a.out) + at * DIM + d0, x);
+      }
     }
   }
 }
@@ -806,7 +815,7 @@ cache_attention_join_kernel(AttendParams a) {
   const int rr = r % ROWS;
   auto row_of = [&](int i) { return (size_t)(i == 0 ? slot0 : 2 * (c0 + i)) * ROWS + rr; };
   const float2* ml = reinterpret_cast<const float2*>(a.part + 2 * (size_t)a.grid * ROWS * DIM);
-  float sum = 0.f;
+  float sum = 0.f, most = -INFINITY;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](float4 y, float f) { x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w); };
   if constexpr (SHARED) {
@@ -826,6 +835,7 @@ cache_attention_join_kernel(AttendParams a) {
     if (lane == 0) s_red[0][tid >> 5] = top;
     __syncthreads();
     top = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
+    most = top;
     for (int i = tid; i < parts; i += 128) {
       if (i > tid) v = __ldcg(ml + row_of(i));
       const float f = v.y == 0.f ? 0.f : v.x == top ? v.y : v.y * ex2(v.x - top);      // (no key: nothing, whatever the maxima)
@@ -854,7 +864,7 @@ cache_attention_join_kernel(AttendParams a) {
     for (int i = 0; i < parts; ++i) {
       const float2 v = __ldcg(ml + row_of(i));
       if (v.y == 0.f) continue;                  // (no key: nothing, whatever the maxima)
-      const float most = fmaxf(top, v.x);
+      most = fmaxf(top, v.x);
       sum = v.x == top ? sum + v.y : fmaf(sum, ex2(top - most), v.x == most ? v.y : v.y * ex2(v.x - most));
       top = most;
     }
@@ -867,7 +877,13 @@ cache_attention_join_kernel(AttendParams a) {
       add(y, (v.x == top ? v.y : v.y * ex2(v.x - top)) * inv);
     }
   }
-  T* out = static_cast<T*>(a.out) + ((size_t)(work.o + r / group) * a.n_heads + kvh * group + r % group) * DIM + d0;
+  const size_t at = (size_t)(work.o + r / group) * a.n_heads + kvh * group + r % group;
+  if (a.mean) {
+    *reinterpret_cast<float4*>(a.mean + at * DIM + d0) = x;
+    if (d0 == 0) a.weight[at] = make_float2(most, sum);
+    return;
+  }
+  T* out = static_cast<T*>(a.out) + at * DIM + d0;
   if constexpr (sizeof(T) == 4) {
     *reinterpret_cast<float4*>(out) = x;
   } else {

@@ -49,4 +49,25 @@ inline kv::Cache device_cache(const ad_kv_cache* c) {
 inline int arg_fault(const char* entry, const char* why) { return op_fail(AD_ERR_ARG, entry, why); }
 inline int launched(const char* entry, cudaError_t e) { return e == cudaSuccess ? AD_OK : op_fail(AD_ERR_CUDA, entry, cudaGetErrorString(e)); }
 
+// The attention over a cache, as its entry point gets it, and as a part of others'.  first (null: none): blocks in front of what each row looks at.  mean and weight
+// (null: results go to out): means of values [M, n_heads, head_dim], and maxima of the scores (times log2 e) and sums of exponentials [M, n_heads].
+struct AttentionCall {
+  const void* q;
+  int32_t dtype;
+  int64_t q_stride;
+  int32_t n_heads;
+  const int32_t *off, *len;
+  int32_t B, M, max_new, max_keys;
+  bool causal;
+  float scale;
+  void* out;
+  int32_t* status;
+  const int32_t* first;
+  float* mean;
+  float2* weight;
+};
+const char* cache_attention_fault(const ad_kv_cache* c, const AttentionCall& call);      // why it cannot be done, or null
+size_t cache_attention_scratch(const ad_kv_cache* c, int n_heads, int B, int max_new, int max_keys);
+cudaError_t cache_attention(const ad_kv_cache* c, const AttentionCall& call, void* scratch, cudaStream_t st);
+
 }  // namespace ad

@@ -55,8 +55,10 @@ struct Cache {
   float* scale[2];               // [n_blocks, heads]
   const int* table;              // [B, table_stride] or null
   int table_stride, n_blocks, heads, block;
+  const int* first = nullptr;    // [B] blocks of the row in front of its block 0, or null
   // block i of row b; negative when the table names none that exists
   __host__ __device__ __forceinline__ int find(int b, int i) const {
+    if (first) i += first[b];
     const int id = table ? table[(size_t)b * table_stride + i] : b * table_stride + i;
     return (unsigned)id < (unsigned)n_blocks ? id : -1;
   }

@@ -15,36 +15,46 @@ constexpr int kSharedRows = 8192;
 
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-struct Scratch { size_t total, lines, start, ml, part, bytes; long long part_rows; int grid; };
-// Results: of every query and head once in its group's items and once in its row's, and as much as an item's between the CTAs' parts.
-Scratch scratch_of(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t M, int32_t G) {
+// Most positions that a row may have of its own, to plan for.
+int32_t own_keys(int32_t max_keys, int32_t max_shared, int32_t block) { return (int32_t)std::max<int64_t>(block, std::min<int64_t>(max_keys, (int64_t)max_keys - max_shared + block)); }
+
+struct Scratch { size_t total, lines, start, first, len, ml, part, own_ml, own_part, rows, bytes; long long part_rows; int grid; };
+// Results of the groups' items: of every query and head, and as much as an item's between the CTAs' parts, twice (either half of the keys); those of the rows' own
+// positions; and what the attention row by row wants.
+Scratch scratch_of(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, int32_t G, int32_t max_shared) {
   Scratch s;
+  const size_t mh = (size_t)M * n_heads;
   s.grid = op_num_sms();
-  s.part_rows = 2ll * M * n_heads + (long long)s.grid * shr::ITEM_ROWS;
+  s.part_rows = (long long)mh + (long long)s.grid * shr::ITEM_ROWS;
   s.total = 0;
   s.lines = 256;
   s.start = s.lines + rounded(((size_t)G + B) * sizeof(shr::Line));
-  s.ml = s.start + rounded(s.grid * sizeof(shr::Start));
+  s.first = s.start + rounded(s.grid * sizeof(shr::Start));
+  s.len = s.first + rounded(B * sizeof(int));
+  s.ml = s.len + rounded(B * sizeof(int));
   s.part = s.ml + rounded(2 * (size_t)s.part_rows * sizeof(float2));
-  s.bytes = s.part + rounded(2 * (size_t)s.part_rows * c->head_dim * sizeof(float));
+  s.own_ml = s.part + rounded(2 * (size_t)s.part_rows * c->head_dim * sizeof(float));
+  s.own_part = s.own_ml + rounded(mh * sizeof(float2));
+  s.rows = s.own_part + rounded(mh * c->head_dim * sizeof(float));
+  s.bytes = s.rows + rounded(cache_attention_scratch(c, n_heads, B, max_new, own_keys(max_keys, max_shared, c->block)));
   return s;
 }
-const char* shared_fault(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, int32_t G, int32_t max_shared) {
-  if (const char* why = cache_fault(c, B)) return why;
+// Whether the groups' positions are read once for all rows.
+bool worth_sharing(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys, int32_t G, int32_t max_shared) {
+  (void)c; (void)n_heads; (void)B; (void)max_new; (void)max_keys; (void)G; (void)max_shared;
+  return true;
+}
+const char* shared_fault(int32_t n_heads, int32_t B, int32_t M, int32_t G, int32_t max_shared) {
   if (B < 1 || B > kSharedRows) return "1 to 8192 rows";
   if (G < 1 || G > B) return "1 to as many groups as rows";
-  if (M < 0) return "negative number of tokens";
-  if (max_new < 1 || max_new > kMaxNew) return "1 to 2^19 tokens of a row";
-  if (!known_dtype(dtype)) return "unknown dtype";
-  if (n_heads < 1 || n_heads > 65535 || n_heads % c->n_kv_heads != 0 || (int64_t)M * n_heads > (1 << 30))
-    return "query heads must be a multiple of the cache's, at most 65535, and tokens times them at most 2^30";
-  if ((int64_t)max_new * n_heads > (1 << 30)) return "max_new times the query heads may be 2^30 at most";
-  if (max_keys < 0 || max_shared < 0) return "negative number of keys";
+  if (M < 0 || n_heads < 1 || (int64_t)M * n_heads > (1 << 30)) return "tokens times query heads may be 2^30 at most";
+  if (max_shared < 0) return "negative number of shared positions";
   return nullptr;
 }
 
-template <typename T, typename F, int DIM>
-cudaError_t launch_shared(const shr::Params& a, cudaStream_t st) {
+// rows(): the attention row by row over what the groups do not share.
+template <typename T, typename F, int DIM, typename Rows>
+cudaError_t launch_shared(const shr::Params& a, cudaStream_t st, Rows rows) {
   static std::atomic<uint64_t> raised{0};              // devices on which the kernel may use its shared memory
   auto kernel = shr::shared_attention_kernel<T, F, DIM>;
   constexpr int smem = shr::smem_bytes<DIM, sizeof(T) == 4>();
@@ -57,22 +67,25 @@ cudaError_t launch_shared(const shr::Params& a, cudaStream_t st) {
     raised.fetch_or(bit, std::memory_order_relaxed);
   }
   e = launch_op(shr::shared_plan_kernel, dim3(1), dim3(shr::PLAN_THREADS), dim3(), 0, st, a);
+  if (e == cudaSuccess) e = rows();
   if (e == cudaSuccess) e = launch_op(kernel, dim3(a.grid), dim3(shr::THREADS), dim3(), smem, st, a);
   const long long warps = (long long)a.max_new * a.n_heads, each = shr::JOIN_THREADS / 32;
   if (e == cudaSuccess) e = launch_op(shr::shared_join_kernel<T, DIM>, dim3((unsigned)((warps + each - 1) / each), a.B), dim3(shr::JOIN_THREADS), dim3(), 0, st, a);
   return e;
 }
-template <typename T, typename F>
-cudaError_t launch_shared_dim(int dim, const shr::Params& a, cudaStream_t st) {
-  return dim == 32 ? launch_shared<T, F, 32>(a, st) : dim == 64 ? launch_shared<T, F, 64>(a, st) : launch_shared<T, F, 128>(a, st);
+template <typename T, typename F, typename Rows>
+cudaError_t launch_shared_dim(int dim, const shr::Params& a, cudaStream_t st, Rows rows) {
+  return dim == 32 ? launch_shared<T, F, 32>(a, st, rows) : dim == 64 ? launch_shared<T, F, 64>(a, st, rows) : launch_shared<T, F, 128>(a, st, rows);
 }
 
 }  // namespace
 
 extern "C" size_t ad_cache_attention_shared_scratch_bytes(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t M, int32_t max_new,
                                                           int32_t max_keys, int32_t G, int32_t max_shared) {
-  if (shared_fault(c, dtype, n_heads, B, M, max_new, max_keys, G, max_shared)) return 0;
-  return scratch_of(c, n_heads, B, M, G).bytes;
+  if (shared_fault(n_heads, B, M, G, max_shared)) return 0;
+  const size_t alone = ad_cache_attention_scratch_bytes(c, dtype, n_heads, B, max_new, max_keys);
+  if (cache_fault(c, B) || !known_dtype(dtype) || max_new < 1 || max_keys < 0 || n_heads % c->n_kv_heads) return 0;
+  return worth_sharing(c, n_heads, B, max_new, max_keys, G, max_shared) ? scratch_of(c, n_heads, B, M, max_new, max_keys, G, max_shared).bytes : alone;
 }
 
 extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
@@ -80,27 +93,31 @@ extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, in
                                          const int32_t* shared, int32_t G, int32_t max_shared, int32_t causal, float scale, void* out, void* scratch,
                                          size_t scratch_bytes, int32_t* status, void* stream) {
   const char* entry = "ad_cache_attention_shared";
-  if (!off || !len || !group || !shared) return arg_fault(entry, "null offsets, lengths or groups");
-  if (const char* why = shared_fault(c, dtype, n_heads, B, M, max_new, max_keys, G, max_shared)) return arg_fault(entry, why);
-  if (!(scale > 0.f) || !(scale <= 1e30f)) return arg_fault(entry, "the scale must be positive, and 1e30 at most");
+  AttentionCall call = {q, dtype, q_stride, n_heads, off, len, B, M, max_new, max_keys, causal != 0, scale, out, status, nullptr, nullptr, nullptr};
+  if (const char* why = cache_attention_fault(c, call)) return arg_fault(entry, why);
+  if (!group || !shared) return arg_fault(entry, "null groups");
+  if (const char* why = shared_fault(n_heads, B, M, G, max_shared)) return arg_fault(entry, why);
   if (M == 0) return AD_OK;
-  if (!q || !out || !aligned(q, 16) || !aligned(out, 16)) return arg_fault(entry, "queries and result must be 16-byte aligned");
-  if (q_stride < (int64_t)n_heads * c->head_dim || q_stride % (int64_t)(16 / dtype_bytes(dtype)))
-    return arg_fault(entry, "queries must be a multiple of 16 bytes apart, and not overlap");
-  const Scratch s = scratch_of(c, n_heads, B, M, G);
-  if (scratch_bytes < s.bytes) return op_fail(AD_ERR_CAPACITY, entry, "scratch too small");
-  if (!scratch || !aligned(scratch, 256)) return arg_fault(entry, "scratch must be 256-byte aligned");
+  const size_t need = ad_cache_attention_shared_scratch_bytes(c, dtype, n_heads, B, M, max_new, max_keys, G, max_shared);
+  if (scratch_bytes < need) return op_fail(AD_ERR_CAPACITY, entry, "scratch too small");
+  if (need && (!scratch || !aligned(scratch, 256))) return arg_fault(entry, "scratch must be 256-byte aligned");
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (!worth_sharing(c, n_heads, B, max_new, max_keys, G, max_shared)) return launched(entry, cache_attention(c, call, scratch, st));
+  const Scratch s = scratch_of(c, n_heads, B, M, max_new, max_keys, G, max_shared);
   char* at = static_cast<char*>(scratch);
   shr::Params a = {};
   a.c = device_cache(c); a.q = q; a.q_stride = (size_t)q_stride; a.out = out; a.n_heads = n_heads; a.M = M; a.max_new = max_new; a.B = B; a.G = G;
   a.off = off; a.len = len; a.group = group; a.shared = shared; a.causal = causal != 0; a.scale = scale * (float)M_LOG2E; a.status = status;
   a.grid = s.grid; a.item_rows = dtype == AD_DTYPE_FP32 ? shr::M_ROWS : shr::ITEM_ROWS; a.part_rows = s.part_rows;
   a.total = reinterpret_cast<long long*>(at + s.total); a.lines = reinterpret_cast<shr::Line*>(at + s.lines); a.start = reinterpret_cast<shr::Start*>(at + s.start);
+  a.own_first = reinterpret_cast<int*>(at + s.first); a.own_len = reinterpret_cast<int*>(at + s.len);
   a.ml = reinterpret_cast<float2*>(at + s.ml); a.part = reinterpret_cast<float*>(at + s.part);
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  a.own_ml = reinterpret_cast<float2*>(at + s.own_ml); a.own_part = reinterpret_cast<float*>(at + s.own_part);
+  call.first = a.own_first; call.len = a.own_len; call.max_keys = own_keys(max_keys, max_shared, c->block); call.mean = a.own_part; call.weight = a.own_ml;
+  auto rows = [&] { return cache_attention(c, call, at + s.rows, st); };
   const int dim = c->head_dim;
   cudaError_t e;
-  if (dtype == AD_DTYPE_FP32) e = c->format == AD_CACHE_E4M3 ? launch_shared_dim<float, kv::E4m3>(dim, a, st) : launch_shared_dim<float, kv::Int8>(dim, a, st);
-  else e = c->format == AD_CACHE_E4M3 ? launch_shared_dim<bf16, kv::E4m3>(dim, a, st) : launch_shared_dim<bf16, kv::Int8>(dim, a, st);
+  if (dtype == AD_DTYPE_FP32) e = c->format == AD_CACHE_E4M3 ? launch_shared_dim<float, kv::E4m3>(dim, a, st, rows) : launch_shared_dim<float, kv::Int8>(dim, a, st, rows);
+  else e = c->format == AD_CACHE_E4M3 ? launch_shared_dim<bf16, kv::E4m3>(dim, a, st, rows) : launch_shared_dim<bf16, kv::Int8>(dim, a, st, rows);
   return launched(entry, e);
 }

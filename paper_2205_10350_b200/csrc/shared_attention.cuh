@@ -10,15 +10,17 @@ namespace shr {
 using kv::Cache;
 
 constexpr int KEYS = 128;              // keys of a tile
+constexpr int SUB = 64;                // ... of which scores are worked on so many at a time
 constexpr int M_ROWS = 128;            // rows of an MMA
 constexpr int ITEM_ROWS = 256;         // most rows of an item, and the distance of CTAs' parts in scratch
 
-// What is worked on: first the groups' shared positions, then the rows' own ones.  A line has `heads` times `tiles` (of its rows) items, each over the keys
-// lo .. of it; an item is `per` granules: FIXED ones, and `weight` for every tile of keys.  The CTAs share all granules evenly, in order.
+// What is worked on: a line for every group, its rows' queries over the blocks that they share.  A line has `heads` times `tiles` (of its rows) items, each over all
+// of its keys; an item is `per` granules: FIXED ones, and `weight` for every tile of keys.  The CTAs share all granules evenly, in order.  What the rows have besides is left to the
+// attention row by row; behind the groups' lines each row of the batch has one that says which queries are its own, and of which group.
 struct Line {
   long long front, rows_front;         // granules and rows of results in front of it
-  int o, n, lo, p;                     // tokens o .. o + n - 1; keys lo .. p + causal * (query + 1)
-  int row, causal, tiles, per, weight, group, pad[2];
+  int o, n, keys;                      // tokens o .. o + n - 1; keys that they share
+  int row, tiles, per, weight, group, pad[4];
 };
 static_assert(sizeof(Line) == 64, "four 16-byte loads");
 struct Start { int line, pad; long long at; };
@@ -36,19 +38,22 @@ struct Params {
   int causal;
   float scale;                         // softmax scale times log2(e)
   int* status;
-  int grid, item_rows;                 // CTAs; rows of a group's item
+  int grid, item_rows;                 // CTAs; rows of an item
   long long part_rows;                 // rows of results of one half
   // scratch
   long long* total;                    // granules of all lines
   Line* lines;                         // [G + B]
   Start* start;                        // [grid]
+  int* own_first;                      // [B] blocks that row b shares, and positions behind them (negative: the row is left out)
+  int* own_len;
   float2* ml;                          // [2][part_rows] maxima and sums
   float* part;                         // [2][part_rows][dim] means of values
+  float2* own_ml;                      // [M][n_heads] the same of the rows' own positions
+  float* own_part;                     // [M][n_heads][dim]
 };
 
 constexpr int FIXED = 4;
-__host__ __device__ __forceinline__ int key_base(int lo) { return lo & ~15; }         // (scales change every 16 keys at most)
-__host__ __device__ __forceinline__ int key_tiles(int lo, int hi) { return hi > lo ? (hi - key_base(lo) + KEYS - 1) / KEYS : 0; }
+__host__ __device__ __forceinline__ int key_tiles(int keys) { return (keys + KEYS - 1) / KEYS; }
 // The tile that granule x of an item starts with.
 __host__ __device__ __forceinline__ int tile_at(int x, int weight) { return x <= FIXED ? 0 : (x - FIXED + weight - 1) / weight; }
 
@@ -73,80 +78,85 @@ __device__ __forceinline__ long long block_scan(long long x, long long* s_warp, 
   }
   return front;
 }
-// Tokens and shared positions of group g; false: it makes no sense, or holds nothing.
+// Tokens of group g, and the positions that its rows share; false: it makes no sense.
 __device__ __forceinline__ bool group_of(const Params& a, int g, int& first, int& last, int& o, int& n, int& keys) {
   first = __ldcg(a.group + g);
   last = __ldcg(a.group + g + 1);
   keys = __ldcg(a.shared + g);
-  if (first < 0 || last < first || last > a.B || keys < 0 || keys > a.c.table_stride * a.c.block) { latch_error(a.status, AD_ERR_ARG); return false; }
-  if (first == last) return false;
-  o = __ldcg(a.off + first);
-  const long long d = (long long)__ldcg(a.off + last) - o;
-  if (o < 0 || d < 0 || o + d > a.M) { latch_error(a.status, AD_ERR_ARG); return false; }
-  n = (int)d;
-  return n > 0;
+  bool good = first >= 0 && last >= first && last <= a.B && keys >= 0 && keys <= a.c.table_stride * a.c.block;
+  o = n = 0;
+  if (good && first < last) {
+    o = __ldcg(a.off + first);
+    const long long d = (long long)__ldcg(a.off + last) - o;
+    good = o >= 0 && d >= 0 && o + d <= a.M;
+    n = good ? (int)d : 0;
+  }
+  if (!good) latch_error(a.status, AD_ERR_ARG);
+  return good;
 }
 // grid = 1, block = PLAN_THREADS.
 __global__ void __launch_bounds__(PLAN_THREADS)
-shared_plan_kernel(Params a) {
+shared_plan_kernel(const __grid_constant__ Params a) {
   __shared__ long long s_warp[PLAN_THREADS / 32];
   pdl_launch();
   pdl_wait();
-  const int lines = a.G + a.B, per_kv = a.n_heads / a.c.heads, tid = threadIdx.x;
-  long long granules_front = 0, tokens_front = 0, row_tokens_front = 0;
-  for (int l0 = 0; l0 < lines; l0 += PLAN_THREADS) {
+  const int per_kv = a.n_heads / a.c.heads, tid = threadIdx.x;
+  // rows: which group they are of, and what is left for the attention row by row
+  for (int b = tid; b < a.B; b += PLAN_THREADS) {
+    Line x = {};
+    int lo = 0, hi = a.G - 1;                                // the last group that starts at b or in front of it
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (__ldcg(a.group + mid) <= b) lo = mid;
+      else hi = mid - 1;
+    }
+    x.row = b;
+    x.group = lo;
+    int first, last, go, gn, keys, p;
+    a.own_first[b] = 0;
+    a.own_len[b] = -1;
+    if (kv::row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, x.o, x.n, p)) {
+      if (group_of(a, lo, first, last, go, gn, keys) && first <= b && b < last && keys <= p && x.o >= go && x.o + x.n <= go + gn) {
+        a.own_first[b] = keys / a.c.block;
+        a.own_len[b] = p - keys / a.c.block * a.c.block;
+      } else {
+        latch_error(a.status, AD_ERR_ARG);
+        x.n = 0;
+      }
+    } else {
+      x.n = 0;
+    }
+    a.lines[a.G + b] = x;
+  }
+  long long granules_front = 0, tokens_front = 0;
+  for (int l0 = 0; l0 < a.G; l0 += PLAN_THREADS) {
     const int l = l0 + tid;
     Line x = {};
-    int hi = 0;
-    bool some = false;
     if (l < a.G) {
-      int first, last;
-      some = group_of(a, l, first, last, x.o, x.n, x.p) && x.p > 0;
-      x.row = first;
-      hi = x.p;
-    } else if (l < lines) {
-      const int b = l - a.G;
-      int lo = 0, hi_g = a.G - 1;                            // the last group that starts at b or in front of it
-      while (lo < hi_g) {
-        const int mid = (lo + hi_g + 1) >> 1;
-        if (__ldcg(a.group + mid) <= b) lo = mid;
-        else hi_g = mid - 1;
-      }
-      int first, last, go, gn;
-      x.row = b;
-      x.causal = a.causal;
-      x.group = lo;
-      if (kv::row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, x.o, x.n, x.p)) {
-        some = group_of(a, lo, first, last, go, gn, x.lo) && first <= b && b < last && x.lo <= x.p && x.o >= go && x.o + x.n <= go + gn;
-        if (!some) latch_error(a.status, AD_ERR_ARG);
-      }
-      hi = x.causal ? x.p + x.n : x.p;
+      int last;
+      if (!group_of(a, l, x.row, last, x.o, x.n, x.keys)) x.keys = 0;
+      x.keys -= x.keys % a.c.block;                           // (whole blocks; the rest is the rows' own)
     }
     // no more results than there is room for, whatever the offsets
-    long long all_g, all_r;
-    const long long tf = tokens_front + block_scan(some && l < a.G ? x.n : 0, s_warp, all_g);
-    const long long rf = row_tokens_front + block_scan(some && l >= a.G ? x.n : 0, s_warp, all_r);
-    if (some && (l < a.G ? tf : rf) + x.n > a.M) {
-      some = false;
+    long long all_t, all;
+    const long long front = tokens_front + block_scan(x.n, s_warp, all_t);
+    if (front + x.n > a.M) {
+      x.n = 0;
       latch_error(a.status, AD_ERR_ARG);
     }
-    const int item_rows = l < a.G ? a.item_rows : M_ROWS, rows = x.n * per_kv;
-    x.rows_front = ((l < a.G ? tf : a.M + rf)) * a.n_heads;
-    x.tiles = some ? (rows + item_rows - 1) / item_rows : 0;
-    x.weight = l < a.G && item_rows > M_ROWS && rows > M_ROWS ? 2 : 1;
-    const int kt = key_tiles(x.lo, hi);
-    x.per = kt ? kt * x.weight + FIXED : 0;
-    if (!some) x.n = 0;
-    long long all;
+    const int rows = x.n * per_kv;
+    x.rows_front = front * a.n_heads;
+    x.tiles = x.keys > 0 ? (rows + a.item_rows - 1) / a.item_rows : 0;
+    x.weight = a.item_rows > M_ROWS && rows > M_ROWS ? 2 : 1;
+    x.per = key_tiles(x.keys) * x.weight + FIXED;
     x.front = granules_front + block_scan((long long)a.c.heads * x.tiles * x.per, s_warp, all);
-    if (l < lines) a.lines[l] = x;
+    if (l < a.G) a.lines[l] = x;
     granules_front += all;
-    tokens_front += all_g;
-    row_tokens_front += all_r;
+    tokens_front += all_t;
   }
   const long long total = granules_front, ctas = min((long long)a.grid, total);
   if (tid == 0) *a.total = total;
-  for (int l = tid; l < lines; l += PLAN_THREADS) {
+  for (int l = tid; l < a.G; l += PLAN_THREADS) {
     const Line x = a.lines[l];                               // (written by this thread)
     const long long n = (long long)a.c.heads * x.tiles * x.per;
     if (n == 0) continue;
@@ -158,9 +168,9 @@ shared_plan_kernel(Params a) {
 
 // ---- a CTA's way through its share ---------------------------------------------------------------------------------
 struct Segment {
-  int row, kvh, o, lo, p, causal;      // as the line's
+  int row, kvh, o;                     // as the line's
   int r0, rows;                        // rows r0 .. of the line's n * per_kv
-  int t0, t1, hi;                      // tiles of keys; end of the keys that any of the rows sees
+  int t0, t1, keys;                    // tiles of keys; keys of the line
   bool two;                            // two tiles of rows, each over all keys; else two halves of the keys
   long long part;                      // where its results go
 };
@@ -195,15 +205,13 @@ struct Walk {
       const int item = (int)(at / x.per), g0 = (int)(at % x.per), take = (int)min((long long)(x.per - g0), end - cur);
       at += take;
       cur += take;
-      const bool is_group = line < a.G;
-      const int item_rows = is_group ? a.item_rows : M_ROWS, rows = x.n * per_kv;
-      s.row = x.row; s.o = x.o; s.lo = x.lo; s.p = x.p; s.causal = x.causal;
+      const int rows = x.n * per_kv;
+      s.row = x.row; s.o = x.o; s.keys = x.keys;
       s.kvh = item / x.tiles;
-      s.r0 = item % x.tiles * item_rows;
-      s.rows = min(item_rows, rows - s.r0);
+      s.r0 = item % x.tiles * a.item_rows;
+      s.rows = min(a.item_rows, rows - s.r0);
       s.two = s.rows > M_ROWS;
-      s.hi = x.causal ? x.p + (s.r0 + s.rows - 1) / per_kv + 1 : x.p;
-      const int kt = key_tiles(x.lo, s.hi);
+      const int kt = key_tiles(x.keys);
       s.t0 = min(tile_at(g0, x.weight), kt);
       s.t1 = min(tile_at(g0 + take, x.weight), kt);
       s.part = x.rows_front + (long long)s.kvh * rows + s.r0 + (long long)blockIdx.x * ITEM_ROWS;
@@ -221,7 +229,7 @@ struct Layout {
   static constexpr int DP = DIM < 64 ? 64 : DIM;               // (32 wide: the upper half is zeros)
   static constexpr int TILE = KEYS * DP * 2;                   // FP16 keys or values of a tile; also 128 rows of queries
   static constexpr int RAW = KEYS * DIM;                       // their codes
-  static constexpr int N_TILES = DIM == 128 ? 3 : 6, N_RAW = DIM == 128 ? 4 : 8;
+  static constexpr int N_TILES = DIM == 128 ? 4 : 6, N_RAW = DIM == 128 ? 2 : 8;
   static constexpr int Q = 0, F16 = Q + 2 * TILE;              // queries: two tiles of rows, or (WIDE) two halves of their bits
   static constexpr int CODES = F16 + N_TILES * TILE;
   static constexpr int BYTES = CODES + N_RAW * RAW;
@@ -230,26 +238,29 @@ struct Layout {
   static constexpr int N_INFO = DIM == 128 ? 8 : 16;
   static_assert(N_RAW / 2 + N_TILES / 2 + 3 <= N_INFO, "scales stay until they have been used");
 };
-struct Info { float ks[8], ve[8], lv[8]; };                   // scales of the keys (negative: no such block), log2 of the values' (rounded up, and itself)
+struct alignas(16) Info { float ks[8], ve[8], lv[8]; int whole[4]; };                   // scales of the keys (negative: no such block), log2 of the values' (rounded up, and
+                                                               // itself); whether all blocks are there, of each 64 keys
 
 // What else lies in shared memory, behind the tiles.
+// Segments that are told ahead.  The warp that asks for codes looks three tiles ahead and asks for a tile's values along with the next one's keys, so the segment whose
+// place it waits for has to be the fifth in front, or none of its values would come.
+constexpr int N_SEGMENTS = 8;
 template <int DIM, bool WIDE>
 struct Small {
   typedef Layout<DIM, WIDE> L;
-  uint64_t raw_full[L::N_RAW], raw_empty[L::N_RAW], full[L::N_TILES], empty[L::N_TILES], s[2], p[2][2], o[2], q, seg, drain;
+  uint64_t raw_full[L::N_RAW], raw_empty[L::N_RAW], full[L::N_TILES], empty[L::N_TILES], s[2][2], p[2][2], o[2][2], q, drain, seg_full[N_SEGMENTS], seg_empty[N_SEGMENTS];
   Info info[L::N_INFO];
-  Segment segment[2];                  // for the softmax's warps, whose registers are short; two: the one in front is stored late
-  int exponent[M_ROWS];                // of the rows' largest numbers, where both halves of the keys want them
+  Segment segment[N_SEGMENTS];         // what the warp that asks for codes has come to, for all others; t1 = 0: that was all
+  uint8_t exponent[2][M_ROWS];          // of the rows' largest numbers
   uint32_t tmem;
   int abort;
 };
 template <int DIM, bool WIDE>
-__host__ __device__ constexpr int smem_bytes() { return 1023 + Layout<DIM, WIDE>::BYTES + (int)sizeof(Small<DIM, WIDE>); }
+__host__ __device__ constexpr int smem_bytes() { return Layout<DIM, WIDE>::BYTES + (int)sizeof(Small<DIM, WIDE>); }
 
+// Warps: 8 for the softmax (two halves, either of 128 rows), 4 that turn codes into operands, one for each half that issues its products, one that asks for codes.
 constexpr int SOFTMAX_WARPS = 8, CONVERT_WARPS = 4;
-constexpr int W_CONVERT = SOFTMAX_WARPS, W_MMA = W_CONVERT + CONVERT_WARPS, W_LOAD = W_MMA + 1, THREADS = 512;      // (four warpgroups, for the sake of their registers)
-// Registers of a thread by warpgroup, from the 128 of the launch: 2 * 144 + 2 * 112 = 4 * 128.
-constexpr int SOFTMAX_REGS = 144, OTHER_REGS = 112;
+constexpr int W_CONVERT = SOFTMAX_WARPS, W_MMA = W_CONVERT + CONVERT_WARPS, W_LOAD = W_MMA + 2, THREADS = 32 * (W_LOAD + 1);
 
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -280,20 +291,6 @@ __device__ __forceinline__ uint64_t value_desc(uint32_t addr) {
   d |= static_cast<uint64_t>(2) << 61;
   return d;
 }
-__device__ __forceinline__ void tmem_issue32(uint32_t taddr, uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
-        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr));
-}
-// (orders every use of r behind the wait)
-__device__ __forceinline__ void tmem_landed32(uint32_t (&r)[32]) {
-#pragma unroll
-  for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
-}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_store8(uint32_t taddr, const uint32_t* r) {
@@ -301,9 +298,22 @@ __device__ __forceinline__ void tmem_store8(uint32_t taddr, const uint32_t* r) {
                "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
+__device__ __forceinline__ void tmem_load8(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) asm volatile("" : "+r"(r[i]));
+}
 __device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// Order in which a CTA's tiles g = 0, 1, .. become operands: keys 0, keys 1, values 0, keys 2, values 1, .., so that scores are never waited for behind values whose
+// room is still taken.  (What would follow the last values is left out.)
+__host__ __device__ __forceinline__ int keys_fill(int g) { return g == 0 ? 0 : 2 * g - 1; }
+__host__ __device__ __forceinline__ int values_fill(int g) { return 2 * g + 2; }
 
 // A ring's place: which slot, and the parity of its phase.
 struct Turn {
@@ -314,13 +324,20 @@ struct Turn {
   }
 };
 
-// The rest of a wait by a whole warp whose first look found nothing.  (Out of line: the kernel's roles compete for the SM's instruction cache.)
+// A wait by a whole warp, bounded in time, once a first look has found nothing.  (Short, and out of line: the kernel's roles share the SM's instruction cache.  With the
+// polls unrolled, 140 KB of instructions, 4 prompts x 24-32 samples took 330 us instead of 318.)
 __device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort, int* status) {
-  if (__any_sync(0xffffffffu, *abort != 0) || !tc::mbar_wait_warp(bar, parity, status)) {
-    *abort = 1;
-    return false;
+  const unsigned long long t0 = tc::global_ns();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (__all_sync(0xffffffffu, tc::mbar_try_wait(bar, parity))) return true;
+    if (__any_sync(0xffffffffu, *abort != 0)) return false;
+    if (__any_sync(0xffffffffu, tc::global_ns() - t0 > tc::WAIT_BUDGET_NS)) break;
   }
-  return true;
+  *abort = 1;
+  latch_error(status, AD_ERR_TIMEOUT);
+  return false;
 }
 
 template <typename T, typename F, int DIM>
@@ -330,19 +347,22 @@ shared_attention_kernel(const __grid_constant__ Params a) {
   typedef Layout<DIM, WIDE> L;
   constexpr int DP = L::DP, KSTEPS = DIM / 16;
   constexpr float SLACK = 2.f;
-  extern __shared__ __align__(16) unsigned char smem_raw[];
+  extern __shared__ __align__(1024) unsigned char smem_p[];
   const int warp = tc::uniform_warp(), lane = threadIdx.x & 31, per_kv = a.n_heads / a.c.heads;
-  const uint32_t smem = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
-  unsigned char* smem_p = smem_raw + (smem - tc::smem_u32(smem_raw));
+  const uint32_t smem = tc::smem_u32(smem_p);
+  if (smem & 1023u) {                                          // (nothing else lies in shared memory that could move it)
+    latch_error(a.status, AD_ERR_CUDA);
+    return;
+  }
   Small<DIM, WIDE>& sm = *reinterpret_cast<Small<DIM, WIDE>*>(smem_p + L::BYTES);
   auto bar = [](uint64_t& b) { return tc::smem_u32(&b); };
   if (threadIdx.x == 0) {
     for (int i = 0; i < L::N_RAW; ++i) { tc::mbar_init(bar(sm.raw_full[i]), 1); tc::mbar_init(bar(sm.raw_empty[i]), CONVERT_WARPS); }
-    for (int i = 0; i < L::N_TILES; ++i) { tc::mbar_init(bar(sm.full[i]), CONVERT_WARPS); tc::mbar_init(bar(sm.empty[i]), 1); }
-    for (int i = 0; i < 2; ++i) { tc::mbar_init(bar(sm.s[i]), 1); tc::mbar_init(bar(sm.p[i][0]), 4); tc::mbar_init(bar(sm.p[i][1]), 4); tc::mbar_init(bar(sm.o[i]), 1); }
+    for (int i = 0; i < L::N_TILES; ++i) { tc::mbar_init(bar(sm.full[i]), CONVERT_WARPS); tc::mbar_init(bar(sm.empty[i]), 2); }
+    for (int i = 0; i < 2; ++i) { tc::mbar_init(bar(sm.s[i][0]), 1); tc::mbar_init(bar(sm.s[i][1]), 1); tc::mbar_init(bar(sm.p[i][0]), 4); tc::mbar_init(bar(sm.p[i][1]), 4); tc::mbar_init(bar(sm.o[i][0]), 1); tc::mbar_init(bar(sm.o[i][1]), 1); }
     tc::mbar_init(bar(sm.q), SOFTMAX_WARPS);
-    tc::mbar_init(bar(sm.seg), 1);
-    tc::mbar_init(bar(sm.drain), 1);
+    for (int i = 0; i < N_SEGMENTS; ++i) { tc::mbar_init(bar(sm.seg_full[i]), 1); tc::mbar_init(bar(sm.seg_empty[i]), SOFTMAX_WARPS + CONVERT_WARPS + 2); }
+    tc::mbar_init(bar(sm.drain), 2);
     sm.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -362,44 +382,66 @@ shared_attention_kernel(const __grid_constant__ Params a) {
   auto col_s = [&](int t) { return tmem + t * 128; };          // scores, and over them probabilities
   auto col_o = [&](int t) { return tmem + 256 + t * DP; };
   auto aborted = [&]() { return *reinterpret_cast<volatile int*>(&sm.abort) != 0; };
+  auto drain = [&](uint64_t& b, uint32_t parity) {             // waits whether or not somebody has given up
+    int never = 0;
+    wait_on(bar(b), parity, &never, a.status);
+  };
   auto wait_warp = [&](uint64_t& b, uint32_t parity) {
     if (__all_sync(0xffffffffu, tc::mbar_try_wait(bar(b), parity))) return true;
     return wait_on(bar(b), parity, &sm.abort, a.status);
   };
-  Walk walk;
-  const bool work = walk.begin(a);
+  const bool work = Walk().begin(a);
+  // Segments in their order, for the warps that read them.
+  Turn seg;
+  auto segment = [&]() -> const Segment* {                     // the next one; null: that was all, or a wait has run out
+    if (!wait_warp(sm.seg_full[seg.slot], seg.phase)) return nullptr;
+    const Segment* s = &sm.segment[seg.slot];
+    return s->t1 == 0 ? nullptr : s;
+  };
+  auto done_with = [&](int slot) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(sm.seg_empty[slot]));
+  };
 
-  if (work) {
-    if (warp < SOFTMAX_WARPS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
-  }
   if (work && warp == W_LOAD) {
     // ================= codes and scales: table -> scales -> copies, each a tile ahead of the next =================
-    struct Tile { int row, kvh, pos, lo, hi; bool there; };
+    struct Tile { int row, kvh, pos, hi; bool there; };
+    Walk walk;
+    walk.begin(a);
     Segment s;
-    int t = 0;
-    bool more = walk.next(a, s);
-    if (more) t = s.t0;
+    int t = 0, told = 0;
+    auto next_segment = [&]() {                                 // goes on, and tells the others
+      const bool more = walk.next(a, s);
+      if (!more) s.t0 = s.t1 = 0;
+      if (told >= N_SEGMENTS) wait_warp(sm.seg_empty[seg.slot], seg.phase ^ 1u);
+      if (lane == 0) {
+        sm.segment[seg.slot] = s;
+        mbar_arrive(bar(sm.seg_full[seg.slot]));
+      }
+      __syncwarp();
+      seg.step(N_SEGMENTS);
+      ++told;
+      t = s.t0;
+      return more;
+    };
+    bool more = next_segment();
     auto next_tile = [&]() {
       Tile x;
       x.there = more;
       if (!more) return x;
-      x.row = s.row; x.kvh = s.kvh; x.pos = key_base(s.lo) + t * KEYS; x.lo = s.lo; x.hi = s.hi;
-      if (++t == s.t1) {
-        more = walk.next(a, s);
-        if (more) t = s.t0;
-      }
+      x.row = s.row; x.kvh = s.kvh; x.pos = t * KEYS; x.hi = s.keys;
+      if (++t == s.t1) more = next_segment();
       return x;
     };
-    const int block = a.c.block, n_blocks = KEYS / block + 1;
+    const int block = a.c.block, shift = __ffs(block) - 1, n_blocks = KEYS / block + 1;
     auto find = [&](const Tile& x) {                           // lane i: the tile's i-th block; -2: none
-      const int i = x.pos / block + lane;
-      if (!x.there || lane >= n_blocks || i * block >= min(x.hi, x.pos + KEYS)) return -2;
+      const int i = (x.pos >> shift) + lane;
+      if (!x.there || lane >= n_blocks || i << shift >= min(x.hi, x.pos + KEYS)) return -2;
       return a.c.find(x.row, i);
     };
     auto scales = [&](const Tile& x, int id, float& ks, float& vs) {      // lane j < 8: 16 keys each
       const int pos = x.pos + 16 * lane;
-      const int mine = __shfl_sync(0xffffffffu, id, (pos / block - x.pos / block) & 31);
+      const int mine = __shfl_sync(0xffffffffu, id, ((pos >> shift) - (x.pos >> shift)) & 31);
       ks = -1.f;
       vs = 1.f;
       if (x.there && lane < 8 && pos < x.hi && mine >= 0) {
@@ -407,73 +449,94 @@ shared_attention_kernel(const __grid_constant__ Params a) {
         vs = __ldcg(a.c.scale[1] + (size_t)mine * a.c.heads + x.kvh);
       }
     };
-    Tile x0 = next_tile(), x1 = next_tile();
-    int id0 = find(x0), id1 = find(x1);
-    float ks, vs;
-    scales(x0, id0, ks, vs);
+    Tile x0 = {}, x1 = {};
+    int id0 = -2, id1 = -2;
+    float ks = -1.f, vs = 1.f;
     Turn raw;
-    int info = 0;
+    int g = 0, issued = 0;
+    // what this lane copies of a tile: bytes, from where, to where in the tile; of all lanes
+    uint32_t bytes = 0, to = 0, all = 0, bytes0 = 0, to0 = 0, all0 = 0;
+    size_t src = 0, src0 = 0;
     bool ok = true;
-    int issued = 0;
-    while (x0.there && ok) {
+    for (int round = 0; ok; ++round) {                           // (the first two rounds only fill the line)
       const Tile x2 = next_tile();
       const int id2 = find(x2);
       float ks1, vs1;
       scales(x1, id1, ks1, vs1);
-      if (id0 == -1) latch_error(a.status, AD_ERR_ARG);
-      // this lane's block: what of it falls into the tile
-      const int first = max((x0.pos / block + lane) * block, x0.pos), last = min(min((x0.pos / block + lane + 1) * block, x0.pos + KEYS), x0.hi);
-      const int bytes = id0 >= 0 && last > first ? (last - first) * DIM : 0;
-      const int all = __reduce_add_sync(0xffffffffu, bytes);
-      const size_t src = (((size_t)max(id0, 0) * a.c.heads + x0.kvh) * block + (first & (block - 1))) * DIM;
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        if (issued >= L::N_RAW) ok = wait_warp(sm.raw_empty[raw.slot], raw.phase ^ 1u);
-        if (!ok) break;
-        if (z == 0) {
-          if (lane < 8) {
-            sm.info[info].ks[lane] = ks;
-            const float whole = kv::whole_lg2(vs);
-            sm.info[info].ve[lane] = whole;
-            sm.info[info].lv[lane] = kv::lg2(vs, whole);
+      if (round >= 2) {
+        if (id0 == -1) latch_error(a.status, AD_ERR_ARG);
+        const int first = max(((x0.pos >> shift) + lane) << shift, x0.pos), last = min(min(((x0.pos >> shift) + lane + 1) << shift, x0.pos + KEYS), x0.hi);
+        bytes = x0.there && id0 >= 0 && last > first ? (last - first) * DIM : 0;
+        all = __reduce_add_sync(0xffffffffu, bytes);
+        to = (first - x0.pos) * DIM;
+        src = (((size_t)max(id0, 0) * a.c.heads + x0.kvh) * block + (first & (block - 1))) * DIM;
+#pragma unroll 1
+        for (int z = 0; z < 2; ++z) {
+          if (z == 0 ? !x0.there : g == 0) continue;
+          if (issued >= L::N_RAW) ok = wait_warp(sm.raw_empty[raw.slot], raw.phase ^ 1u);
+          if (!ok) break;
+          if (z == 0) {
+            Info& info = sm.info[g & (L::N_INFO - 1)];
+            if (lane < 8) {
+              info.ks[lane] = ks;
+              const float whole = kv::whole_lg2(vs);
+              info.ve[lane] = whole;
+              info.lv[lane] = kv::lg2(vs, whole);
+            }
+            const unsigned gone = __ballot_sync(0xffffffffu, ks < 0.f);
+            if (lane < 2) info.whole[lane] = (gone >> (4 * lane) & 15u) == 0;
+            __syncwarp();
           }
-          info = (info + 1) & (L::N_INFO - 1);
+          const uint32_t full = bar(sm.raw_full[raw.slot]), n = z == 0 ? bytes : bytes0;
+          if (lane == 0) tc::mbar_expect_tx(full, z == 0 ? all : all0);
           __syncwarp();
+          if (n) bulk_load(smem + L::CODES + raw.slot * L::RAW + (z == 0 ? to : to0), a.c.codes[z] + (z == 0 ? src : src0), n, full);
+          raw.step(L::N_RAW);
+          ++issued;
         }
-        const uint32_t full = bar(sm.raw_full[raw.slot]);
-        if (lane == 0) tc::mbar_expect_tx(full, (uint32_t)all);
-        __syncwarp();
-        if (bytes) bulk_load(smem + L::CODES + raw.slot * L::RAW + (first - x0.pos) * DIM, a.c.codes[z] + src, (uint32_t)bytes, full);
-        raw.step(L::N_RAW);
-        ++issued;
+        if (!x0.there) break;
+        bytes0 = bytes; to0 = to; all0 = all; src0 = src;
+        ++g;
       }
       x0 = x1; x1 = x2; id0 = id1; id1 = id2; ks = ks1; vs = vs1;
     }
     for (int i = max(0, issued - L::N_RAW); i < issued; ++i)   // nothing is under way when the CTA ends, whoever gave up
-      tc::mbar_wait_warp(bar(sm.raw_full[i % L::N_RAW]), (uint32_t)(i / L::N_RAW) & 1u, a.status);
+      drain(sm.raw_full[i % L::N_RAW], (uint32_t)(i / L::N_RAW) & 1u);
   } else if (work && warp >= W_CONVERT && warp < W_MMA) {
     // ================= codes to FP16 =================
-    constexpr int PIECES = DIM / 8, STEP = 128 / PIECES, N = KEYS / STEP;      // pieces of a key; keys between a thread's pieces; its pieces
+    constexpr int PIECES = DIM / 8, STEP = 32 * CONVERT_WARPS / PIECES, N = KEYS / STEP;      // pieces of a key; keys between a thread's pieces; its pieces
     const int ct = threadIdx.x - 32 * W_CONVERT, key0 = ct / PIECES, piece = ct % PIECES;
     const int src0 = key0 * DIM + piece * 8, dst0 = (piece >> 3) * KEYS * 128 + key0 * 128 + (((piece & 7) ^ (key0 & 7)) << 4);
-    Segment s;
-    Turn raw, f16;
-    int info = 0, done = 0;
-    bool ok = true;
-    while (ok && walk.next(a, s)) {
-      for (int t = s.t0; t < s.t1 && ok; ++t) {
-        const int pos = key_base(s.lo) + t * KEYS;
+    Turn raw;
+    int g = 0, left0 = 0;                                       // keys of the tile in front, whose values come behind this one's keys
+    bool ok = true, more = true;
+    const Segment* s = segment();
+    int t = s ? s->t0 : 0;
+    for (; ok && more; ++g) {
+      int left = 0;
+      more = s != nullptr;
+      if (more) {
+        left = s->keys - t * KEYS;
+        if (++t == s->t1) {
+          done_with(seg.slot);
+          seg.step(N_SEGMENTS);
+          s = segment();
+          t = s ? s->t0 : 0;
+        }
+      }
 #pragma unroll 1
-        for (int z = 0; z < 2; ++z) {
+      for (int z = 0; z < 2; ++z) {                              // keys of tile g, values of the one in front
+        if (z == 0 ? !more : g == 0) continue;
+        const int fill = z == 0 ? keys_fill(g) : values_fill(g - 1), slot = fill % L::N_TILES, info = (z == 0 ? g : g - 1) & (L::N_INFO - 1);
+        const int keys = z == 0 ? left : left0;
+        {
           ok = wait_warp(sm.raw_full[raw.slot], raw.phase);
-          if (ok && done >= L::N_TILES) ok = wait_warp(sm.empty[f16.slot], f16.phase ^ 1u);
+          if (ok && fill >= L::N_TILES) ok = wait_warp(sm.empty[slot], (uint32_t)(fill / L::N_TILES - 1) & 1u);
           if (!ok) break;
           const unsigned char* src = smem_p + L::CODES + raw.slot * L::RAW + src0;
-          unsigned char* dst = smem_p + L::F16 + f16.slot * L::TILE + dst0;
-          bool whole = pos >= s.lo && pos + KEYS <= s.hi;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) whole = whole && sm.info[info].ks[j] >= 0.f;
-          constexpr int AT_ONCE = 4;
+          unsigned char* dst = smem_p + L::F16 + slot * L::TILE + dst0;
+          const bool whole = keys >= KEYS && sm.info[info].whole[0] && sm.info[info].whole[1];
+          constexpr int AT_ONCE = N < 8 ? N : 8;
 #pragma unroll 1
           for (int i0 = 0; i0 < N; i0 += AT_ONCE) {
             uint2 w[AT_ONCE];
@@ -483,7 +546,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
 #pragma unroll
               for (int i = 0; i < AT_ONCE; ++i) {
                 const int key = key0 + (i0 + i) * STEP;
-                if (pos + key < s.lo || pos + key >= s.hi || sm.info[info].ks[key >> 4] < 0.f) w[i] = make_uint2(0u, 0u);
+                if (key >= keys || sm.info[info].ks[key >> 4] < 0.f) w[i] = make_uint2(0u, 0u);
               }
             }
 #pragma unroll
@@ -498,119 +561,96 @@ shared_attention_kernel(const __grid_constant__ Params a) {
           __syncwarp();
           if (lane == 0) {
             mbar_arrive(bar(sm.raw_empty[raw.slot]));
-            mbar_arrive(bar(sm.full[f16.slot]));
+            mbar_arrive(bar(sm.full[slot]));
           }
           raw.step(L::N_RAW);
-          f16.step(L::N_TILES);
-          ++done;
         }
-        info = (info + 1) & (L::N_INFO - 1);
       }
+      left0 = left;
     }
-  } else if (work && warp == W_MMA) {
-    // ================= products =================
-    const uint32_t idesc_s = idesc_f16(M_ROWS, KEYS, false), idesc_o = idesc_f16(M_ROWS, DP, true);
-    Segment s;
-    uint32_t q_phase = 0, p_phase[2] = {0, 0};
-    int next_k = 0;                                            // fills of the ring in front of the segment: keys 2 i, values 2 i + 1
+  } else if (work && warp < W_LOAD && warp >= W_MMA) {
+    // ================= products of one half =================
+    const int t = warp - W_MMA;
+    const uint32_t idesc_s = idesc_f16(M_ROWS, SUB, false), idesc_o = idesc_f16(M_ROWS, DP, true);
+    uint32_t phase = 0, p_phase = 0;
+    int next_k = 0;                                            // the CTA's tiles in front of the segment
     bool ok = true;
-    auto slot_of = [&](int fill) { return fill % L::N_TILES; };
-    auto phase_of = [&](int fill) { return (uint32_t)(fill / L::N_TILES) & 1u; };
-    // scores of tile `fill` / 2 for half t; last: the keys are not read again
-    auto scores = [&](int t, int q_tile, int fill, bool last) {
-      const int slot = slot_of(fill);
-      if (!wait_warp(sm.full[slot], phase_of(fill))) return false;
+    while (const Segment* s = ok ? segment() : nullptr) {
+      const int n = __shfl_sync(0xffffffffu, s->t1 - s->t0, 0);      // (so that the compiler knows it to be the same in all lanes)
+      const bool two = __shfl_sync(0xffffffffu, (int)s->two, 0) != 0;
+      const int last_subs = __shfl_sync(0xffffffffu, s->keys > (s->t1 - 1) * KEYS + SUB ? 2 : 1, 0);      // steps of the last tile
+      done_with(seg.slot);
+      seg.step(N_SEGMENTS);
+      ok = wait_warp(sm.q, phase);
+      phase ^= 1u;
       after_sync();
-      if (tc::elect_one()) {
-        const uint32_t k = smem + L::F16 + slot * L::TILE;
+      // The half's tiles of keys: all of them for its rows (two), or every other one for the same rows; each in two steps of 64 keys, whose scores lie side by
+      // side.  Scores two steps ahead; then, step by step, probabilities times values and the scores of two steps on: the softmax always finds some.
+      const int stride = two ? 1 : 2, first = two ? 0 : t, steps = first < n ? 2 * ((n - 1 - first) / stride) + ((n - 1 - first) % stride == 0 ? last_subs : 2) : 0;
+      for (int u = 0; u < steps + 2 && steps > 0 && ok; ++u) {
+        const int sub = u & 1;
+        if (u >= 2) {
+          const int i = first + ((u - 2) >> 1) * stride, fill = values_fill(next_k + i), slot = fill % L::N_TILES;
+          ok = wait_warp(sm.full[slot], (uint32_t)(fill / L::N_TILES) & 1u) && wait_warp(sm.p[t][sub], p_phase >> sub & 1u);
+          p_phase ^= 1u << sub;
+          if (!ok) break;
+          after_sync();
+          if (tc::elect_one()) {
+            const uint32_t v = smem + L::F16 + slot * L::TILE + sub * (SUB / 16) * 2048;
 #pragma unroll
-        for (int h = WIDE ? 1 : 0; h >= 0; --h) {
-          const uint32_t q = smem + L::Q + (WIDE ? h : q_tile) * L::TILE;
+            for (int j = 0; j < SUB / 16; ++j) {
 #pragma unroll
-          for (int j = 0; j < KSTEPS; ++j) {
-            const uint32_t at = (j >> 2) * KEYS * 128 + (j & 3) * 32;
-            umma_f16_ss(col_s(t), tc::make_smem_desc(q + at), tc::make_smem_desc(k + at), idesc_s, (j > 0 || (WIDE && h == 0)) ? 1u : 0u);
+              for (int h = WIDE ? 1 : 0; h >= 0; --h)
+                umma_f16_ts(col_o(t), col_s(t) + SUB * sub + 16 * j + 8 * h, value_desc(v + j * 2048), idesc_o, (u > 2 || j > 0 || (WIDE && h == 0)) ? 1u : 0u);
+            }
+            tc::umma_commit(bar(sm.o[t][sub]));
+            if (sub == 1 || u - 2 == steps - 1) {
+              tc::umma_commit(bar(sm.empty[slot]));
+              if (!two) tc::umma_commit(bar(sm.empty[slot]));      // (for the other half, which has no use for it)
+            }
           }
+          __syncwarp();
         }
-        tc::umma_commit(bar(sm.s[t]));
-        if (last) tc::umma_commit(bar(sm.empty[slot]));
-      }
-      __syncwarp();
-      return true;
-    };
-    auto values = [&](int t, int fill, bool first, bool last, bool end) {
-      const int slot = slot_of(fill);
-      if (!wait_warp(sm.full[slot], phase_of(fill))) return false;
-      const uint32_t v = smem + L::F16 + slot * L::TILE;
+        if (u < steps) {
+          const int i = first + (u >> 1) * stride, fill = keys_fill(next_k + i), slot = fill % L::N_TILES;
+          ok = wait_warp(sm.full[slot], (uint32_t)(fill / L::N_TILES) & 1u);
+          if (!ok) break;
+          after_sync();
+          if (tc::elect_one()) {
+            const uint32_t k = smem + L::F16 + slot * L::TILE + sub * SUB * 128;
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {                   // (probabilities come in two halves)
-        if (!wait_warp(sm.p[t][part], p_phase[t])) return false;
-        after_sync();
-        if (tc::elect_one()) {
+            for (int h = WIDE ? 1 : 0; h >= 0; --h) {
+              const uint32_t q = smem + L::Q + (WIDE ? h : two ? t : 0) * L::TILE;
 #pragma unroll
-          for (int j = part * KEYS / 32; j < (part + 1) * KEYS / 32; ++j) {
-#pragma unroll
-            for (int h = WIDE ? 1 : 0; h >= 0; --h)
-              umma_f16_ts(col_o(t), col_s(t) + 16 * j + 8 * h, value_desc(v + j * 2048), idesc_o, (!first || j > 0 || (WIDE && h == 0)) ? 1u : 0u);
+              for (int j = 0; j < KSTEPS; ++j) {
+                const uint32_t at = (j >> 2) * KEYS * 128 + (j & 3) * 32;
+                umma_f16_ss(col_s(t) + SUB * sub, tc::make_smem_desc(q + at), tc::make_smem_desc(k + at), idesc_s, (j > 0 || (WIDE && h == 0)) ? 1u : 0u);
+              }
+            }
+            tc::umma_commit(bar(sm.s[t][sub]));
+            if (sub == 1 || u == steps - 1) {
+              tc::umma_commit(bar(sm.empty[slot]));
+              if (!two) tc::umma_commit(bar(sm.empty[slot]));
+            }
           }
-          if (part == 1) {
-            if (last) tc::umma_commit(bar(sm.empty[slot]));
-            if (end) tc::umma_commit(bar(sm.o[t]));
-          }
+          __syncwarp();
         }
-        __syncwarp();
       }
-      p_phase[t] ^= 1u;
-      return true;
-    };
-    int turn = 0;
-    auto publish = [&](bool more) {                            // (t1 = 0: that was all)
-      if (lane == 0) {
-        if (!more) s.t0 = s.t1 = 0;
-        sm.segment[turn] = s;
-        mbar_arrive(bar(sm.seg));
-      }
-      __syncwarp();
-      turn ^= 1;
-    };
-    bool more = walk.next(a, s);
-    publish(more);
-    while (ok && more) {
-      ok = wait_warp(sm.q, q_phase);
-      q_phase ^= 1u;
-      after_sync();
-      const int n = __shfl_sync(0xffffffffu, s.t1 - s.t0, 0);      // (so that the compiler knows it to be the same in all lanes)
-      const bool two = __shfl_sync(0xffffffffu, (int)s.two, 0) != 0;
-      // The halves take turns: while one's scores become probabilities, the other's are multiplied.  Each is a tile of rows over all tiles of keys (two), or
-      // every other tile of keys for the same rows.
-      const int last = two ? 2 * n : n;
-      for (int u = 0; u < last + 2 && ok; ++u) {
-        const int t = u & 1;
-        if (u >= 2) ok = values(t, next_k + 2 * (two ? (u - 2) >> 1 : u - 2) + 1, u < 4, !two || t == 1, u >= last);
-        if (u < last && ok) ok = scores(t, two ? t : 0, next_k + 2 * (two ? u >> 1 : u), !two || t == 1);
-      }
-      next_k += 2 * n;
-      more = walk.next(a, s);
-      publish(more);
+      next_k += n;
     }
     // (what was issued is through before tensor memory is given back)
     if (tc::elect_one()) tc::umma_commit(bar(sm.drain));
     __syncwarp();
-    if (!tc::mbar_wait_warp(bar(sm.drain), 0, a.status)) sm.abort = 1;
+    if (t == 0) drain(sm.drain, 0);
   } else if (work && warp < SOFTMAX_WARPS) {
     // ================= probabilities, results =================
     const int half = warp >> 2, r = threadIdx.x & (M_ROWS - 1);
     const uint32_t quad = (uint32_t)(warp & 3) << 21;           // the warp's lanes of tensor memory
-    uint32_t s_phase = 0, o_phase = 0, seg_phase = 0;
-    int info0 = 0, turn = 0;
+    uint32_t s_phase = 0, o_phase = 0;                          // a bit for either step of a tile
+    int behind = 0;                                             // which of the two was the last one
+    int info0 = 0, before = -1;                                 // the slot of the segment in front, whose results are stored late
     float m = -INFINITY, d = -INFINITY, l = 0.f, factor = 0.f, rest = 1.f;
-    bool ok = true, pending = false;
-    // scale / up: the part within 2^-120 .. 2^121 meets the keys' scale first, what is left of the powers of two their product
-    auto factors = [&](int e) {
-      const int power = e - 140, room = 247 - (int)(__float_as_uint(a.scale) >> 23), first = min(max(power, room - 240), room);
-      factor = ldexpf(a.scale, first);
-      rest = ldexpf(1.f, power - first);
-    };
+    bool large = false;                                         // scores whose steps in FP32 are a quarter and more
     // queries of a segment: a thread a row, its power of two, FP16
     auto load_queries = [&](const Segment& x) {
       const int row = x.r0 + (x.two ? half * M_ROWS : 0) + r;
@@ -647,8 +687,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
             if (WIDE) *reinterpret_cast<uint4*>(dst + L::TILE) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
           }
         }
-        factors((int)e);
-        if (!x.two) sm.exponent[r] = (int)e;
+        sm.exponent[half][r] = (uint8_t)e;
       }
       to_async_proxy();
       __syncwarp();
@@ -658,8 +697,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
       const int row = x.two ? half * M_ROWS + r : r;
       const bool mine = row < x.rows, any = x.two || x.t1 - x.t0 > half;
       if (any) {
-        if (!ok || !wait_warp(sm.o[half], o_phase)) { ok = false; return; }
-        o_phase ^= 1u;
+        if (!wait_warp(sm.o[half][behind], (o_phase >> behind & 1u) ^ 1u)) return;
         after_sync();
       }
       const long long at = x.part + row + (x.two ? 0 : half * a.part_rows);
@@ -669,14 +707,14 @@ shared_attention_kernel(const __grid_constant__ Params a) {
         // means, not sums, which FP32 may have no room for; factor after factor, as they may have none together
         const float share = some ? 1.f / l * kv::P_ONE : 0.f, unit = some ? kv::ex2(d) : 0.f;
 #pragma unroll 1
-        for (int c0 = 0; c0 < DIM; c0 += 32) {
-          uint32_t y[32];
-          tmem_issue32(col_o(half) + c0 + quad, y);
+        for (int c0 = 0; c0 < DIM; c0 += 16) {
+          uint32_t y[16];
+          tc::tmem_issue16(col_o(half) + c0 + quad, y);
           tmem_wait_ld();
-          tmem_landed32(y);
+          tc::tmem_landed16(y);
           if (mine && some) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4)
+            for (int i = 0; i < 16; i += 4)
               *reinterpret_cast<float4*>(a.part + at * DIM + c0 + i) =
                   make_float4(__uint_as_float(y[i]) * share * unit, __uint_as_float(y[i + 1]) * share * unit, __uint_as_float(y[i + 2]) * share * unit,
                               __uint_as_float(y[i + 3]) * share * unit);
@@ -686,182 +724,186 @@ shared_attention_kernel(const __grid_constant__ Params a) {
       }
     };
     for (;;) {
-      // (one that has given up goes on to where it is not waited for any more: every wait of its ends at once)
-      const bool there = wait_warp(sm.seg, seg_phase);
-      seg_phase ^= 1u;
-      ok = ok && there;
-      const Segment& s = sm.segment[turn];
-      turn ^= 1;
-      // Queries in front have been read: both halves have had their last scores.  All threads go on, or none.
-      uint32_t over = !ok || aborted() || s.t0 == s.t1;
+      const Segment* next = segment();
+      // Queries in front have been read: both halves have had their last scores.  All threads go on, or none.  A warp whose wait has run out goes through
+      // the barriers like the others, with what it finds: every later wait of it ends at once.
+      uint32_t over = !next || aborted();
       asm volatile(
           "{\n\t.reg .pred p, q;\n\t"
           "setp.ne.u32 p, %0, 0;\n\t"
-          "barrier.cta.red.or.pred q, 1, 256, p;\n\t"
+          "barrier.cta.red.or.pred q, 1, %1, p;\n\t"
           "selp.u32 %0, 1, 0, q;\n\t}"
           : "+r"(over)
-          :
+          : "n"(32 * SOFTMAX_WARPS)
           : "memory");
       if (over) break;
+      const Segment& s = *next;
       load_queries(s);
-      if (pending) store(sm.segment[turn]);
-      asm volatile("barrier.cta.sync 1, 256;" ::: "memory");
-      if (!s.two && half == 1 && r < s.rows) factors(sm.exponent[r]);
+      if (before >= 0) {
+        store(sm.segment[before]);
+        done_with(before);
+      }
+      before = seg.slot;
+      seg.step(N_SEGMENTS);
+      asm volatile("barrier.cta.sync 1, %0;" ::"n"(32 * SOFTMAX_WARPS) : "memory");
+      const int n = s.t1 - s.t0, row = s.r0 + (s.two ? half * M_ROWS : 0) + r, last_row = s.r0 + s.rows - 1;
+      const bool mine = row <= last_row, busy = __any_sync(0xffffffffu, mine);      // (rows that there are none of hold anything, and decide on nothing)
+      {
+        // scale / up: the part within 2^-120 .. 2^121 meets the keys' scale first, what is left of the powers of two their product
+        const int power = (mine ? (int)sm.exponent[s.two ? half : 0][r] : 140) - 140, room = 247 - (int)(__float_as_uint(a.scale) >> 23),
+                  first = min(max(power, room - 240), room);
+        factor = ldexpf(a.scale, first);
+        rest = ldexpf(1.f, power - first);
+      }
       m = d = -INFINITY;
       l = 0.f;
-      const int n = s.t1 - s.t0, row = s.r0 + (s.two ? half * M_ROWS : 0) + r, last_row = s.r0 + s.rows - 1;
-      const int sees = s.causal ? s.p + min(row, last_row) / per_kv + 1 : s.p;
-      const bool mine = row <= last_row, busy = __any_sync(0xffffffffu, mine);      // (rows that there are none of hold anything, and decide on nothing)
-      for (int i = s.two ? 0 : half; i < n && ok; i += s.two ? 1 : 2) {
-        ok = wait_warp(sm.s[half], s_phase);
-        if (!ok) break;
-        s_phase ^= 1u;
+      large = false;
+      const int stride = s.two ? 1 : 2, base = s.t0 * KEYS;
+      const int begin = (s.two ? 0 : half) * (KEYS / SUB);
+      for (int u = begin, k = 0; u < n * (KEYS / SUB) && base + u * SUB < s.keys; ++k, u += u & 1 ? 1 + (stride - 1) * (KEYS / SUB) : 1) {      // steps of 64 keys
+        const int sub = u & 1, pos = base + u * SUB;
+        const uint32_t cols = col_s(half) + SUB * sub + quad;
+        wait_warp(sm.s[half][sub], s_phase >> sub & 1u);
+        s_phase ^= 1u << sub;
         after_sync();
-        auto hand_over = [&](int part) {
-          tmem_wait_st();
-          before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(sm.p[half][part]));
-        };
         if (busy) {
-          const Info& info = sm.info[(info0 + i) & (L::N_INFO - 1)];
-          const int pos = key_base(s.lo) + (s.t0 + i) * KEYS;
-          bool whole = pos >= s.lo && pos + KEYS <= sees;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) whole = whole && info.ks[j] >= 0.f;
-          // Scores are changed where they lie, in short loops of their own, before they are looked at: one form of the rest for all tiles, as instructions that are
-          // not in the SM's cache cost more than any of these loops.
-          if (!__all_sync(0xffffffffu, whole)) {                // keys that are not there, or not seen by some row of the warp
-            const int lo = s.lo - pos, hi = sees - pos;
+          const Info& info = sm.info[(info0 + (u >> 1)) & (L::N_INFO - 1)];
+          const float *ks = info.ks + 4 * sub, *ve = info.ve + 4 * sub, *lv = info.lv + 4 * sub;
+          const float4 ks4 = *reinterpret_cast<const float4*>(ks), lv4 = *reinterpret_cast<const float4*>(lv);
+          // Scores are changed where they lie, in short loops of their own, before they are looked at: one form of the rest for all tiles.
+          if (pos + SUB > s.keys || !info.whole[sub]) {          // keys that are not there
+            const int hi = s.keys - pos;
 #pragma unroll 1
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < 4; ++j) {
               uint32_t y[16];
-              tc::tmem_issue16(col_s(half) + 16 * j + quad, y);
-              const bool gone = info.ks[j] < 0.f;
+              tc::tmem_issue16(cols + 16 * j, y);
+              const bool gone = ks[j] < 0.f;
               tmem_wait_ld();
               tc::tmem_landed16(y);
 #pragma unroll
               for (int c = 0; c < 16; ++c)
-                if (gone || 16 * j + c < lo || 16 * j + c >= hi) y[c] = 0xff800000u;
-              tmem_store8(col_s(half) + 16 * j + quad, y);
-              tmem_store8(col_s(half) + 16 * j + 8 + quad, y + 8);
+                if (gone || 16 * j + c >= hi) y[c] = 0xff800000u;
+              tmem_store8(cols + 16 * j, y);
+              tmem_store8(cols + 16 * j + 8, y + 8);
             }
             tmem_wait_st();
           }
-          // ---- the largest score of every 16 keys: do references move? ----
-          auto factor_of = [&](int j) { return fmaxf(factor * fabsf(info.ks[j]) * rest, FLT_MIN); };      // (not 0 times -inf)
-          // (references are whole numbers, so that what goes from one to another is an exact power of two)
-          float keep_o = 1.f;
-          bool moved = false;
-          for (float to = m == -INFINITY ? 0.f : m;;) {
-            float most = -INFINITY, ve_max = -INFINITY, beyond = -INFINITY;
-            uint32_t y[2][16];
-            tc::tmem_issue16(col_s(half) + quad, y[0]);
-#pragma unroll 1
-            for (int g = 0; g < 4; ++g) {
+          auto factor_of = [&](int j) {                          // (not 0 times -inf)
+            return fmaxf(factor * fabsf(j == 0 ? ks4.x : j == 1 ? ks4.y : j == 2 ? ks4.z : ks4.w) * rest, FLT_MIN);
+          };
+          // Probabilities times their values' scale, as shares of 2^15 at the references m of the scores and d of the products.  With the references as they are, at
+          // first, and if any row's turn out too large for FP16 or for the sum, again once these have moved.
+          auto unit_of = [&](int j) {                            // exponent of what a probability of one becomes
+            return (float)kv::P_BITS + fminf(fmaxf((j == 0 ? lv4.x : j == 1 ? lv4.y : j == 2 ? lv4.z : lv4.w) - d, -kv::SPAN), kv::SPAN);
+          };
+          // Exponents first, with the references as they are, or, where any row's probabilities would be too large for FP16 or for their sum, once these have moved.
+          uint32_t y[4][16];                                     // the row's scores, then exponents
+          for (bool as_they_are = k > 0 && !large;; as_they_are = false) {
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                tmem_wait_ld();
-                tc::tmem_landed16(y[k]);
-                if (k == 0 || g < 3) tc::tmem_issue16(col_s(half) + 32 * g + 16 * (k + 1) + quad, y[k ^ 1]);
-                auto v = [&](int c) { return __uint_as_float(y[k][c]); };
-                float t0 = kv::max3(v(0), v(1), v(2)), t1 = kv::max3(v(3), v(4), v(5));
-                t0 = kv::max3(t0, v(6), v(7)); t1 = kv::max3(t1, v(8), v(9));
-                t0 = kv::max3(t0, v(10), v(11)); t1 = kv::max3(t1, v(12), v(13));
-                t0 = kv::max3(t0, v(14), v(15));
-                const float x = ceilf(fmaxf(t0, t1) * factor_of(2 * g + k)), ve = info.ve[2 * g + k];
-                most = fmaxf(most, x);
-                ve_max = fmaxf(ve_max, ve);
-                beyond = fmaxf(beyond, x - to + ve);
+            for (int j = 0; j < 4; ++j) tc::tmem_issue16(cols + 16 * j, y[j]);
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) tc::tmem_landed16(y[j]);
+            if (!as_they_are) {
+              // (References are whole numbers, so that what goes from one to another is an exact power of two.)
+              bool again = false;
+              for (float to = m == -INFINITY ? 0.f : m;;) {
+                float most = -INFINITY, ve_max = -INFINITY, beyond = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  auto v = [&](int c) { return __uint_as_float(y[j][c]); };
+                  float t0 = kv::max3(v(0), v(1), v(2));
+#pragma unroll
+                  for (int c = 3; c < 15; c += 2) t0 = kv::max3(t0, v(c), v(c + 1));
+                  const float x = ceilf(fmaxf(t0, v(15)) * factor_of(j)), e = ve[j];
+                  most = fmaxf(most, x);
+                  ve_max = fmaxf(ve_max, e);
+                  beyond = fmaxf(beyond, x - to + e);
+                }
+                const bool moves = mine && (most > m || beyond > d || ve_max - kv::SPAN > d);
+                if (!again) {
+                  if (!__any_sync(0xffffffffu, moves)) break;
+                  // some row's do: how far p * scale goes beyond the new one, the same again
+                  if (most > m) to = most + SLACK;
+                  again = true;
+                  continue;
+                }
+                float keep_o = 1.f;
+                if (moves) {
+                  const float top = most > m ? to : m, less = m - to;
+                  const float tod = fmaxf(beyond > d + less ? beyond + SLACK : d + less, ve_max - kv::SPAN);
+                  keep_o = tod == -INFINITY ? 0.f : kv::ex2(less + (d - tod));
+                  m = top;
+                  d = tod;
+                  l *= kv::ex2(less);
+                }
+                if (k > 0) {                                    // (the half's first step has no results in front)
+                  wait_warp(sm.o[half][behind], (o_phase >> behind & 1u) ^ 1u);      // (the products in front; those before them are, as these scores are)
+                  after_sync();
+#pragma unroll 1
+                  for (int c0 = 0; c0 < DP; c0 += 8) {
+                    uint32_t z[8];
+                    tmem_load8(col_o(half) + c0 + quad, z);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) z[c] = __float_as_uint(__uint_as_float(z[c]) * keep_o);
+                    tmem_store8(col_o(half) + c0 + quad, z);
+                  }
+                }
+                break;
               }
+              large = __any_sync(0xffffffffu, mine && fabsf(m) > 4194304.f && m != -INFINITY);
             }
-            if (!moved) {
-              moved = mine && (most > m || beyond > d || ve_max - kv::SPAN > d);
-              if (!__any_sync(0xffffffffu, moved)) break;
-              if (moved && most > m) to = most + SLACK;         // ... and how far p * scale goes beyond that: the same again
-              moved = true;
-              continue;
-            }
-            // reference m of the row's scores, and exponent d of p * scale beyond m's own
-            if (mine && (most > m || beyond > d || ve_max - kv::SPAN > d)) {
-              const float top = most > m ? to : m, less = m - to;
-              const float tod = fmaxf(beyond > d + less ? beyond + SLACK : d + less, ve_max - kv::SPAN);
-              keep_o = tod == -INFINITY ? 0.f : kv::ex2(less + (d - tod));
-              m = top;
-              d = tod;
-              l *= kv::ex2(less);
-            }
-            if (i > (s.two ? 0 : 1)) {                          // (the half's first tile has no results in front)
-#pragma unroll 1
-              for (int c0 = 0; c0 < DP; c0 += 16) {
-                uint32_t y[16];
-                tc::tmem_issue16(col_o(half) + c0 + quad, y);
-                tmem_wait_ld();
-                tc::tmem_landed16(y);
+            float ref = m == -INFINITY ? 0.f : m;
+            if (large) {                                        // scores in steps of a quarter and more: a difference of rounded ones
 #pragma unroll
-                for (int c = 0; c < 16; ++c) y[c] = __float_as_uint(__uint_as_float(y[c]) * keep_o);
-                tmem_store8(col_o(half) + c0 + quad, y);
-                tmem_store8(col_o(half) + c0 + 8 + quad, y + 8);
-              }
-            }
-            break;
-          }
-          float ref = m == -INFINITY ? 0.f : m;
-          const bool large = __any_sync(0xffffffffu, mine && fabsf(ref) > 4194304.f);
-          if (large) {                                          // scores in steps of a quarter and more: a difference of rounded ones
-#pragma unroll 1
-            for (int j = 0; j < 8; ++j) {
-              uint32_t y[16];
-              tc::tmem_issue16(col_s(half) + 16 * j + quad, y);
-              const float t = factor_of(j);
-              tmem_wait_ld();
-              tc::tmem_landed16(y);
+              for (int j = 0; j < 4; ++j)
 #pragma unroll
-              for (int c = 0; c < 16; ++c) y[c] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(y[c]), t), ref));
-              tmem_store8(col_s(half) + 16 * j + quad, y);
-              tmem_store8(col_s(half) + 16 * j + 8 + quad, y + 8);
+                for (int c = 0; c < 16; ++c) y[j][c] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(y[j][c]), factor_of(j)), ref));
+              ref = 0.f;
             }
-            tmem_wait_st();
-            ref = 0.f;
-          }
-          // ---- probabilities times their values' scale, as shares of 2^15 at the references ----
-          uint32_t y[2][16];
-          tc::tmem_issue16(col_s(half) + quad, y[0]);
-#pragma unroll 1
-          for (int g = 0; g < 4; ++g) {
+            bool fits = fmaxf(fmaxf(lv4.x, lv4.y), fmaxf(lv4.z, lv4.w)) - kv::SPAN <= d;
+            const float most = m == -INFINITY ? -INFINITY : 15.9f;      // (2^16 is beyond FP16)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const float e = (float)kv::P_BITS + fminf(fmaxf(info.lv[2 * g + k] - d, -kv::SPAN), kv::SPAN), from = e - ref, t = large ? 1.f : factor_of(2 * g + k);
-              tmem_wait_ld();
-              tc::tmem_landed16(y[k]);
-              if (k == 0 || g < 3) tc::tmem_issue16(col_s(half) + 32 * g + 16 * (k + 1) + quad, y[k ^ 1]);
-              float2 sum;
-              uint32_t hi[8], lo[8];
+            for (int j = 0; j < 4; ++j) {
+              const float e = unit_of(j), from = e - ref, t = large ? 1.f : factor_of(j);
+              float top = -INFINITY;
 #pragma unroll
               for (int c = 0; c < 16; c += 2) {
-                float2 v = make_float2(__uint_as_float(y[k][c]), __uint_as_float(y[k][c + 1]));
-                v = kv::fma2(v, make_float2(t, t), make_float2(from, from));
-                v.x = kv::ex2(v.x);
-                v.y = kv::ex2(v.y);
-                sum = c == 0 ? v : kv::add2(sum, v);
-                hi[c / 2] = kv::pack_f16(v.x, v.y);
-                if (WIDE) lo[c / 2] = kv::rest_f16(v.x, v.y, hi[c / 2]);
+                const float2 v = kv::fma2(make_float2(__uint_as_float(y[j][c]), __uint_as_float(y[j][c + 1])), make_float2(t, t), make_float2(from, from));
+                y[j][c] = __float_as_uint(v.x);
+                y[j][c + 1] = __float_as_uint(v.y);
+                top = kv::max3(top, v.x, v.y);
               }
-              l = fmaf(sum.x + sum.y, kv::ex2(-e), l);
-              tmem_store8(col_s(half) + 32 * g + 16 * k + quad, hi);
-              if (WIDE) tmem_store8(col_s(half) + 32 * g + 16 * k + 8 + quad, lo);
+              fits = fits && top <= fminf(most, e + 1.f);
             }
-            if (g == 1) hand_over(0);                            // (the second product begins with the first half)
+            if (!as_they_are || __all_sync(0xffffffffu, fits || !mine)) break;
           }
-        } else {
-          hand_over(0);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float2 sum;
+            uint32_t hi[8], lo[8];
+#pragma unroll
+            for (int c = 0; c < 16; c += 2) {
+              const float2 v = make_float2(kv::ex2(__uint_as_float(y[j][c])), kv::ex2(__uint_as_float(y[j][c + 1])));
+              sum = c == 0 ? v : kv::add2(sum, v);
+              hi[c / 2] = kv::pack_f16(v.x, v.y);
+              if (WIDE) lo[c / 2] = kv::rest_f16(v.x, v.y, hi[c / 2]);
+            }
+            l = fmaf(sum.x + sum.y, kv::ex2(-unit_of(j)), l);
+            tmem_store8(cols + 16 * j, hi);
+            if (WIDE) tmem_store8(cols + 16 * j + 8, lo);
+          }
+          tmem_wait_st();
         }
-        hand_over(1);
+        before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(sm.p[half][sub]));
+        o_phase ^= 1u << sub;
+        behind = sub;
       }
       info0 += n;
-      pending = true;
     }
-    if (pending && ok && !aborted()) store(sm.segment[turn]);
+    if (before >= 0 && !aborted()) store(sm.segment[before]);
   }
   before_sync();
   __syncthreads();
@@ -869,7 +911,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
   if (warp == W_MMA) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
 }
 
-// Joins the parts of every query: of its group's items and of its row's.  A warp a query and head.
+// Joins the parts of every query: of its group's items, and of its row's own positions.  A warp a query and head.
 // grid = (enough for max_new * n_heads warps, B), block = JOIN_THREADS.
 constexpr int JOIN_THREADS = 256;
 template <typename T, int DIM>
@@ -886,77 +928,82 @@ shared_join_kernel(const __grid_constant__ Params a) {
     for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(&x)[i] = __ldcg(src + i);
     return x;
   };
+  auto load = [&](const float* p, float* y) {
+    p += lane * PER;
+    if constexpr (PER == 4) { const float4 t = __ldcg(reinterpret_cast<const float4*>(p)); y[0] = t.x; y[1] = t.y; y[PER - 2] = t.z; y[PER - 1] = t.w; }
+    else if constexpr (PER == 2) { const float2 t = __ldcg(reinterpret_cast<const float2*>(p)); y[0] = t.x; y[PER - 1] = t.y; }
+    else y[0] = __ldcg(p);
+  };
   const Line row = load_line(a.G + b);
   const long long w = (long long)blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5);
   if (w >= (long long)row.n * a.n_heads) return;
   const Line grp = load_line(row.group);
   const long long total = __ldcg(a.total), ctas = min((long long)a.grid, total);
   const int i = (int)(w / a.n_heads), head = (int)(w % a.n_heads), kvh = head / per_kv;
-  float top = -INFINITY, sum = 0.f, x[PER];
-#pragma unroll
-  for (int j = 0; j < PER; ++j) x[j] = 0.f;
-  auto add = [&](const Line& ln, bool is_group) {
-    if (ln.per == 0 || ln.tiles == 0) return;
-    const int item_rows = is_group ? a.item_rows : M_ROWS, rows = ln.n * per_kv, r = (row.o - ln.o + i) * per_kv + head % per_kv, tile = r / item_rows;
-    const int n_rows = min(item_rows, rows - tile * item_rows), last = tile * item_rows + n_rows - 1;
-    const int hi = ln.causal ? ln.p + last / per_kv + 1 : ln.p, kt = key_tiles(ln.lo, hi);
-    const long long first = ln.front + ((long long)kvh * ln.tiles + tile) * ln.per;
-    const int c0 = kv::cta_of(total, first, ctas), c1 = kv::cta_of(total, first + ln.per - 1, ctas), halves = n_rows > M_ROWS ? 1 : 2;
-    const long long at = ln.rows_front + (long long)kvh * rows + r;
-    // lane u: part u (32 at a time)
-    for (int u0 = 0; u0 < (c1 - c0 + 1) * halves; u0 += 32) {
-      const int u = u0 + lane, c = c0 + u / halves;
-      float2 v = make_float2(-INFINITY, 0.f);
-      long long where = 0;
-      if (c <= c1) {
-        const int g0 = (int)(max(kv::cta_start(total, c, ctas), first) - first), g1 = (int)(min(kv::cta_start(total, c + 1, ctas), first + ln.per) - first);
-        where = at + (long long)c * ITEM_ROWS + (u % halves) * a.part_rows;
-        if (min(tile_at(g0, ln.weight), kt) < min(tile_at(g1, ln.weight), kt)) v = __ldcg(a.ml + where);
-      }
-      const unsigned some = __ballot_sync(0xffffffffu, v.y != 0.f);
-      float most = v.y != 0.f ? v.x : -INFINITY;
-#pragma unroll
-      for (int s = 16; s; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
-      const float to = fmaxf(top, most), back = top == to ? 1.f : kv::ex2(top - to);
-      sum *= back;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) x[j] *= back;
-      top = to;
-      const float f = v.y == 0.f ? 0.f : v.x == top ? v.y : v.y * kv::ex2(v.x - top);
-      for (unsigned left = some; left;) {
-        constexpr int AHEAD = 4;
-        float y[AHEAD][PER], g[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-          const int src = left ? __ffs(left) - 1 : 0;
-          g[k] = __shfl_sync(0xffffffffu, f, src);
-          const long long from = __shfl_sync(0xffffffffu, where, src);
-          if (!left) g[k] = 0.f;
-#pragma unroll
-          for (int j = 0; j < PER; ++j) y[k][j] = 0.f;
-          if (left) {
-            const float* p = a.part + from * DIM + lane * PER;
-            if constexpr (PER == 4) { const float4 t = __ldcg(reinterpret_cast<const float4*>(p)); y[k][0] = t.x; y[k][1] = t.y; y[k][PER - 2] = t.z; y[k][PER - 1] = t.w; }
-            else if constexpr (PER == 2) { const float2 t = __ldcg(reinterpret_cast<const float2*>(p)); y[k][0] = t.x; y[k][PER - 1] = t.y; }
-            else y[k][0] = __ldcg(p);
-          }
-          left &= left - 1;
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-          sum += g[k];
-#pragma unroll
-          for (int j = 0; j < PER; ++j) x[j] = fmaf(y[k][j], g[k], x[j]);
-        }
-      }
-    }
+  // the row's own positions
+  const size_t own = (size_t)(row.o + i) * a.n_heads + head;
+  const float2 mine = __ldcg(a.own_ml + own);
+  // part u of its group's: maximum and sum, and where its means are; all there are
+  const int rows = grp.n * per_kv, r = (row.o - grp.o + i) * per_kv + head % per_kv, tile = r / a.item_rows, kt = key_tiles(grp.keys);
+  const long long first = grp.front + ((long long)kvh * grp.tiles + tile) * grp.per, at = grp.rows_front + (long long)kvh * rows + r;
+  const int halves = min(a.item_rows, rows - tile * a.item_rows) > M_ROWS ? 1 : 2;
+  int c0 = 0, parts = 0;
+  if (grp.tiles > 0) {
+    c0 = kv::cta_of(total, first, ctas);
+    parts = (kv::cta_of(total, first + grp.per - 1, ctas) - c0 + 1) * halves;
+  }
+  auto part = [&](int u, long long& where) {
+    const int c = c0 + u / halves;
+    where = at + (long long)c * ITEM_ROWS + (u % halves) * a.part_rows;
+    if (u >= parts) return make_float2(-INFINITY, 0.f);
+    const int g0 = (int)(max(kv::cta_start(total, c, ctas), first) - first), g1 = (int)(min(kv::cta_start(total, c + 1, ctas), first + grp.per) - first);
+    return min(tile_at(g0, grp.weight), kt) < min(tile_at(g1, grp.weight), kt) ? __ldcg(a.ml + where) : make_float2(-INFINITY, 0.f);
   };
-  add(grp, true);
-  add(row, false);
+  // the largest maximum and the sum against it; then means times their shares (sums of values may be more than FP32 has room for)
+  float top = mine.y == 0.f ? -INFINITY : mine.x, sum = mine.y, x[PER];
+  long long where;
+  for (int u0 = 0; u0 < parts; u0 += 32) {
+    const float2 v = part(u0 + lane, where);
+    float most = v.y != 0.f ? v.x : -INFINITY;
+#pragma unroll
+    for (int s = 16; s; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
+    most = fmaxf(top, most);
+    float more = v.y == 0.f ? 0.f : v.x == most ? v.y : v.y * kv::ex2(v.x - most);
+#pragma unroll
+    for (int s = 16; s; s >>= 1) more += __shfl_xor_sync(0xffffffffu, more, s);
+    sum = (top == most ? sum : sum * kv::ex2(top - most)) + more;
+    top = most;
+  }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  auto share = [&](float2 v) { return v.y == 0.f ? 0.f : (v.x == top ? v.y : v.y * kv::ex2(v.x - top)) * inv; };
+  load(a.own_part + own * DIM, x);
+#pragma unroll
+  for (int j = 0; j < PER; ++j) x[j] = mine.y == 0.f ? 0.f : x[j] * share(mine);
+  for (int u0 = 0; u0 < parts; u0 += 32) {
+    const float2 v = part(u0 + lane, where);
+    const float f = share(v);
+    for (unsigned left = __ballot_sync(0xffffffffu, v.y != 0.f); left;) {
+      constexpr int AHEAD = 4;
+      float y[AHEAD][PER], g[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const int src = left ? __ffs(left) - 1 : 0;
+        g[k] = left ? __shfl_sync(0xffffffffu, f, src) : 0.f;
+        const long long from = __shfl_sync(0xffffffffu, where, src);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) y[k][j] = 0.f;
+        if (left) load(a.part + from * DIM, y[k]);
+        left &= left - 1;
+      }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) x[j] = fmaf(y[k][j], g[k], x[j]);
+    }
+  }
   T* out = static_cast<T*>(a.out) + ((size_t)(row.o + i) * a.n_heads + head) * DIM + lane * PER;
 #pragma unroll
-  for (int j = 0; j < PER; ++j) out[j] = from_f32<T>(x[j] * inv);
+  for (int j = 0; j < PER; ++j) out[j] = from_f32<T>(x[j]);
 }
 
 }  // namespace shr

@@ -9,17 +9,6 @@ from tests.test_gpu_kv_cache import DEV, Model, bound, ints, numbers, offsets
 pytestmark = pytest.mark.gpu
 
 
-class Shared(Model):
-    """A cache whose rows take their first positions from their group's first row.  (Rows that share a block in part have copies of it, whose codes may have been
-    rounded anew since, each with its row's scale.)"""
-
-    def values(self, z, b, n):
-        own = super().values(z, b, n)
-        first, shared = self.prefix[b]
-        k = min(shared, n)
-        return np.concatenate([super().values(z, first, k), own[k:]]) if k else own
-
-
 def batch(groups, shared, tails, new, heads, dim, block, fmt, causal, seed=0, spread=1.0, gap=2, copies=False):
     """A cache and its model whose rows share their first positions: groups [G] rows each, shared [G], tails and new [B].  Shared blocks stand in all of
     a group's rows; one that is shared in part is copied for each (`copies`: all of them are)."""
@@ -44,8 +33,7 @@ def batch(groups, shared, tails, new, heads, dim, block, fmt, causal, seed=0, sp
             b += 1
         first.append(b)
     cache = binding.KvCache(most, heads, dim, block, fmt, table=ints(table), row_blocks=row_blocks, device=DEV)
-    model = Shared(most, heads, dim, block, fmt, table, row_blocks)
-    model.prefix = [(grp.index(g), shared[g]) for g in grp]
+    model = Model(most, heads, dim, block, fmt, table, row_blocks)
     # the shared positions into every row (the same numbers), then each row's own
     kt, vt = (torch.cat([x[: shared[g]] for g in grp]) if sum(shared[g] for g in grp) else x[:0] for x in (k0, v0))
     off = offsets([shared[g] for g in grp])
@@ -104,6 +92,14 @@ def test_all_of_it_shared(dtype, dim):
     """An encoder's keys: no tails, all queries see the same positions, lengths around tiles and blocks; a source of no length."""
     for lens in ([127, 128, 129], [1, 0, 16], [255, 256, 400]):
         check([2, 3, 1], lens, [0] * 6, [5, 1, 0, 2, 3, 4], 2, 2, dim, 32, "int8", dtype, False, seed=lens[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_many_groups_and_heads(dtype):
+    """More items than CTAs, most of them of a tile or two: every CTA goes through several, of all lengths."""
+    groups = [1 + g % 4 for g in range(40)]
+    rows = sum(groups)
+    check(groups, [(37 * g) % 300 for g in range(40)], [b % 9 for b in range(rows)], [1 + b % 2 for b in range(rows)], 8, 2, 128, 16, "int8", dtype, True, seed=9)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
