@@ -39,10 +39,11 @@ Scratch scratch_of(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t M, 
   s.bytes = s.rows + rounded(cache_attention_scratch(c, n_heads, B, max_new, own_keys(max_keys, max_shared, c->block)));
   return s;
 }
-// Whether the groups' positions are read once for all rows.
+// Whether the groups' positions are read once for all rows: where that saves the attention row by row 28000 units of 32 keys for 32 rows of queries, or more, which take it as
+// long as the calls' latencies.  Row by row / shared, 32 query heads on 8 of 128, BF16: 16 rows of one query behind 4000 positions (15000 units) XXX.
 bool worth_sharing(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys, int32_t G, int32_t max_shared) {
-  (void)c; (void)n_heads; (void)B; (void)max_new; (void)max_keys; (void)G; (void)max_shared;
-  return true;
+  const int64_t rows = (int64_t)max_new * (n_heads / c->n_kv_heads), keys = std::min<int64_t>(std::min(max_keys, max_shared), (int64_t)c->table_stride * c->block);
+  return (double)(B - G) * c->n_kv_heads * (double)((rows + 31) / 32) * (double)(keys / 32) >= 28000.0;
 }
 const char* shared_fault(int32_t n_heads, int32_t B, int32_t M, int32_t G, int32_t max_shared) {
   if (B < 1 || B > kSharedRows) return "1 to 8192 rows";

@@ -52,7 +52,7 @@ struct Params {
   float* own_part;                     // [M][n_heads][dim]
 };
 
-constexpr int FIXED = 4;
+constexpr int FIXED = 3;
 __host__ __device__ __forceinline__ int key_tiles(int keys) { return (keys + KEYS - 1) / KEYS; }
 // The tile that granule x of an item starts with.
 __host__ __device__ __forceinline__ int tile_at(int x, int weight) { return x <= FIXED ? 0 : (x - FIXED + weight - 1) / weight; }
@@ -156,13 +156,16 @@ shared_plan_kernel(const __grid_constant__ Params a) {
   }
   const long long total = granules_front, ctas = min((long long)a.grid, total);
   if (tid == 0) *a.total = total;
-  for (int l = tid; l < a.G; l += PLAN_THREADS) {
-    const Line x = a.lines[l];                               // (written by this thread)
-    const long long n = (long long)a.c.heads * x.tiles * x.per;
-    if (n == 0) continue;
-    long long c = kv::cta_of(total, x.front, ctas);
-    if (kv::cta_start(total, c, ctas) < x.front) ++c;
-    for (; c < ctas && kv::cta_start(total, c, ctas) < x.front + n; ++c) a.start[c] = Start{l, 0, kv::cta_start(total, c, ctas) - x.front};
+  __syncthreads();
+  for (int c = tid; c < ctas; c += PLAN_THREADS) {           // where each CTA starts: in the last line that has begun there
+    const long long g = kv::cta_start(total, c, ctas);
+    int lo = 0, hi = a.G - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (a.lines[mid].front <= g) lo = mid;
+      else hi = mid - 1;
+    }
+    a.start[c] = Start{lo, 0, g - a.lines[lo].front};
   }
 }
 

@@ -16,7 +16,7 @@ def batch(groups, shared, tails, new, heads, dim, block, fmt, causal, seed=0, sp
     grp = [g for g, n in enumerate(groups) for _ in range(n)]
     lens = [shared[g] + t for g, t in zip(grp, tails)]
     ends = [n + m if causal else n for n, m in zip(lens, new)]
-    row_blocks = max(1, max(-(-e // block) for e in ends)) + 1
+    row_blocks = max(1, max(-(-e // block) for e in ends)) + 60000      # (room for rows that make it worth reading shared positions once)
     r = np.random.default_rng(seed + block)
     most = sum(-(-e // block) for e in ends) + sum(-(-s // block) for s in shared) + gap
     ids = iter(r.permutation(most))
@@ -48,10 +48,13 @@ def batch(groups, shared, tails, new, heads, dim, block, fmt, causal, seed=0, sp
     return cache, model, first, lens, ends
 
 
-def run(cache, q, new, lens, first, shared, ends, causal, **kw):
+FAR = 1 << 21        # positions to plan for that make it worth reading shared ones once, whatever there are
+
+
+def run(cache, q, new, lens, first, shared, ends, causal, plan=FAR, **kw):
     status = torch.zeros(1, dtype=torch.int32, device=DEV)
-    out = binding.cache_attention_shared(cache, q, ints(offsets(new)), ints(lens), ints(first), ints(shared), max(1, max(new)), max(1, max(ends)), max_shared=max(shared),
-                                         causal=causal, status_t=status, **kw)
+    out = binding.cache_attention_shared(cache, q, ints(offsets(new)), ints(lens), ints(first), ints(shared), max(1, max(new)), plan + max(1, max(ends)),
+                                         max_shared=plan + max(shared), causal=causal, status_t=status, **kw)
     return out, int(status.item())
 
 
@@ -172,7 +175,7 @@ def test_rows_and_groups_that_make_no_sense_are_left_out():
                                  ([2 ** 31 - 1, 2, 4], shared, off, lens, [2, 3]), ([0, 2, 4], [2 ** 31 - 1, 96], off, lens, [2, 3])):
         status = torch.zeros(1, dtype=torch.int32, device=DEV)
         out = torch.full_like(want, 7.0)
-        binding.cache_attention_shared(cache, q, ints(of), ints(le), ints(fi), ints(sh), 2, max(ends), causal=True, out=out, status_t=status)
+        binding.cache_attention_shared(cache, q, ints(of), ints(le), ints(fi), ints(sh), 2, FAR + max(ends), max_shared=FAR, causal=True, out=out, status_t=status)
         assert int(status.item()) == binding.AD_ERR_ARG
         for b in good or ():
             rows = slice(off[b], off[b + 1])
@@ -180,7 +183,7 @@ def test_rows_and_groups_that_make_no_sense_are_left_out():
     # a block that does not exist is left out like in the attention row by row
     cache.table[0, 1] = 10 ** 6
     status = torch.zeros(1, dtype=torch.int32, device=DEV)
-    out = binding.cache_attention_shared(cache, q, ints(off), ints(lens), ints(first), ints(shared), 2, max(ends), status_t=status)
+    out = binding.cache_attention_shared(cache, q, ints(off), ints(lens), ints(first), ints(shared), 2, FAR + max(ends), max_shared=FAR, status_t=status)
     alone = binding.cache_attention(cache, q[:1], ints([0, 1]), ints(lens[:1]), 2, max(ends))
     assert int(status.item()) == binding.AD_ERR_ARG and torch.allclose(out[:1].float(), alone.float(), atol=0.02) and torch.allclose(out[3:].float(), want[3:].float(), atol=0.02)
 
@@ -193,7 +196,7 @@ def test_strides_streams_and_graphs(dtype):
     wide = numbers((16, 12 + 8, 64), dtype, 4).to(DEV)
     q = wide[:, 4: 12]
     args = [ints(offsets(new)), ints(lens), ints(first), ints(shared)]
-    call = lambda x, **kw: binding.cache_attention_shared(cache, x, *args, 2, max(ends), causal=True, **kw)
+    call = lambda x, **kw: binding.cache_attention_shared(cache, x, *args, 2, FAR + max(ends), max_shared=FAR, causal=True, **kw)
     want = call(q.contiguous())
     out = torch.empty_like(want)
     assert call(q, out=out) is out and torch.equal(out, want)
@@ -214,6 +217,17 @@ def test_strides_streams_and_graphs(dtype):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(replayed, call(q)) and torch.equal(other, call(q * 0.5)) and not torch.equal(replayed, want)
+
+
+def test_short_prefixes_are_left_to_the_attention_row_by_row():
+    """Where reading them once would not pay, results are that one's, bit by bit; one call or the other by sizes that the host knows."""
+    groups, shared, tails, new = [4], [640], [0, 10, 100, 300], [3, 1, 2, 5]
+    cache, model, first, lens, ends = batch(groups, shared, tails, new, 2, 64, 32, "int8", True)
+    q = numbers((11, 8, 64), "bf16", 3).to(DEV)
+    out, status = run(cache, q, new, lens, first, shared, ends, True, plan=0)
+    assert status == 0 and torch.equal(out, binding.cache_attention(cache, q, ints(offsets(new)), ints(lens), max(new), max(ends)))
+    once, _ = run(cache, q, new, lens, first, shared, ends, True)
+    assert not torch.equal(out, once) and float((out.float() - once.float()).abs().max()) <= 2 ** -7 * float(out.float().abs().max())
 
 
 def test_nothing_to_do():
