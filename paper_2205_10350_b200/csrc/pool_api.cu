@@ -140,10 +140,11 @@ extern "C" int ad_cache_compact(const ad_kv_pool* p, const ad_kv_cache* caches, 
 
 namespace {
 constexpr int kSampleVocab = 1 << 20;
-constexpr size_t kScoresKept = 192 * 1024;       // (beside the histograms)
-size_t kept_bytes(int32_t vocab, int cluster, size_t element) {
-  const size_t warps = (size_t)cluster * sample::WARPS;
-  return ((vocab + warps - 1) / warps + 31) / 32 * 32 * sample::WARPS * element;
+constexpr size_t kScoresKept = 188 * 1024;       // (beside the histogram and the list)
+// Scores of a warp: vectors for all of its lanes, and room for one that begins in front of the row.
+int scores_each(int32_t vocab, int cluster, size_t element) {
+  const int64_t round = 32 * 16 / (int64_t)element, warps = (int64_t)cluster * sample::WARPS;
+  return (int)((vocab + 16 / (int64_t)element + warps * round - 1) / (warps * round) * round);
 }
 template <typename T, bool KEPT>
 cudaError_t launch_sample_kept(const sample::Params& p, int cluster, size_t smem, cudaStream_t st) {
@@ -158,9 +159,10 @@ cudaError_t launch_sample_kept(const sample::Params& p, int cluster, size_t smem
   return launch_op(kernel, dim3(p.M * cluster), dim3(sample::THREADS), dim3(cluster), KEPT ? smem : 0, st, p);
 }
 template <typename T>
-cudaError_t launch_sample(const sample::Params& p, cudaStream_t st) {
+cudaError_t launch_sample(sample::Params p, cudaStream_t st) {
   const int cluster = p.vocab <= 2048 ? 1 : p.M * (int64_t)sample::MAX_CLUSTER <= 2 * op_num_sms() ? sample::MAX_CLUSTER : 4;
-  const size_t smem = kept_bytes(p.vocab, cluster, sizeof(T));
+  p.each = scores_each(p.vocab, cluster, sizeof(T));
+  const size_t smem = (size_t)p.each * sample::WARPS * sizeof(T);
   return smem <= kScoresKept ? launch_sample_kept<T, true>(p, cluster, smem, st) : launch_sample_kept<T, false>(p, cluster, smem, st);
 }
 }  // namespace

@@ -13,7 +13,8 @@ namespace sample {
 namespace cg = cooperative_groups;
 
 constexpr int THREADS = 512, WARPS = THREADS / 32, MAX_CLUSTER = 8;
-constexpr int DIGIT = 11, BINS = 1 << DIGIT, PER = BINS / THREADS;      // bins of a level, and of a thread
+constexpr int DIGIT = 11, BINS = 1 << DIGIT, PER = BINS / THREADS;      // bins of a histogram, and of a thread
+constexpr int LIST = 4096;             // scores of one bin that are put in order
 typedef unsigned long long u64;
 
 struct Params {
@@ -30,6 +31,7 @@ struct Params {
   void* out;                     // [M, vocab] or null
   size_t out_stride;
   int scale_bits;                // weights are counted in units of 2^-scale_bits
+  int each;                      // scores of a warp, a multiple of 32 vectors
   int* status;
 };
 
@@ -47,10 +49,16 @@ template <> struct Key<bf16> {
   static __device__ __forceinline__ uint32_t of(float x) { return Key<float>::of(x) >> 16; }
 };
 template <typename T> __device__ __forceinline__ T clean(T x) { return to_f32(x) == to_f32(x) ? x : from_f32<T>(-INFINITY); }     // a NaN counts as -inf
+// A key's score.
+template <typename T> __device__ __forceinline__ float score_of(uint32_t key) {
+  const uint32_t wide = Key<T>::BITS == 16 ? key << 16 | (key & 0x8000u ? 0u : 0xffffu) : key;
+  return __uint_as_float(wide & 0x80000000u ? wide & 0x7fffffffu : ~wide);
+}
 
-// What a level of the search has counted: scores, and their weights in two halves.
+// What has been counted: scores, and their weights in two halves.
 struct Histogram { uint32_t n[BINS], lo[BINS], hi[BINS]; };
-struct Found { uint32_t bin, n; u64 in_front_n, in_front, mass; };
+struct Found { int bin; uint32_t n; u64 in_front_n, in_front, mass; };
+struct Border { uint32_t key, kept, ties; };      // scores above this key stay, and of those that have it, `ties`, the first `kept`
 
 // 64-bit sums from 32-bit atomic additions: exact, so that their order does not matter.
 __device__ __forceinline__ void add_mass(Histogram& h, uint32_t bin, u64 w) {
@@ -58,28 +66,36 @@ __device__ __forceinline__ void add_mass(Histogram& h, uint32_t bin, u64 w) {
   const uint32_t up = (uint32_t)(w >> 32) + carry;
   if (up) atomicAdd(&h.hi[bin], up);
 }
+// Bin of a score that lies y below the largest: 128 to the octave of y, from 2^-7 to 2^9.
+__device__ __forceinline__ int bin_of(float y) { return min(max((int)(__float_as_uint(y) >> 16) - (120 << 7), 0), BINS - 1); }
 
 // One row by a cluster of CTAs that share the vocabulary, every warp a run of ids.
 //   w(v) = exp((score(v) - largest) / T); tokens are ordered by score, ties by id.  Top-k keeps the first k; top-p, of these, the ones in front of
 //   which less than top_p of their weight lies (and the first); min-p, of those, the ones with w >= min_p.  All three keep a beginning of the order, so that what
 //   is kept is told by one score and the number of ids that are kept of those that have just this score.  The token is the lowest kept id at which
 //   the running sum of weights, over kept ids in order, exceeds r times their total.
-// The k-th largest score, and the one at which the weight in front reaches top_p of the whole, are found digit by digit of its key: a histogram of the digit
-// among the scores that share the digits so far, summed over the cluster, and the bin in which the border lies.  Weights are worked out in FP64 and
-// summed as integers in units of 2^-scale_bits (vocab * 2^scale_bits <= 2^62): the largest is 1, so a sum is off by vocab * 2^-(scale_bits + 1) of itself at
-// most, 2^-43 with 1000 ids and 2^-23 with 2^20 (roundings of either sign: their root, a 2^-10th of that, in fact), and comes out the same in any order.
+// The k-th largest score, and the one at which the weight in front reaches top_p of the whole: a histogram over the distance from the largest (in shared memory, summed
+// over the cluster), the bin in which the border lies, and that bin's scores put in order by one CTA; where these are too many (ties, as a rule), digit
+// by digit of their keys.  Weights are worked out in FP64 and summed as integers in units of 2^-scale_bits (vocab * 2^scale_bits <= 2^62): the largest is 1, so a
+// sum is off by vocab * 2^-(scale_bits + 1) of itself at most, 2^-43 with 1000 ids and 2^-23 with 2^20 (roundings of either sign: their root, a 2^-10th
+// of that, in fact), and comes out the same in any order.
+// Scores are taken 16 bytes at a time: places g = id + shift, shift such that a place that is a multiple of a vector's lies on a vector's boundary.
 // grid = M clusters, block = THREADS.  Dynamic shared memory: KEPT, the CTA's scores.
 template <typename T, bool KEPT>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 2)
 sample_kernel(Params p) {
+  constexpr int VEC = 16 / sizeof(T);
   extern __shared__ __align__(16) unsigned char s_raw[];
-  __shared__ Histogram s_h;
+  __shared__ __align__(16) union { Histogram h; u64 list[LIST]; } s_u;
   __shared__ double s_table[sampled::EXP_TABLE];
   __shared__ float s_top[MAX_CLUSTER];
-  __shared__ u64 s_warp[WARPS], s_cta[2];
+  __shared__ u64 s_warp[WARPS], s_scan[WARPS], s_cta[1];
   __shared__ uint32_t s_scan_n[WARPS];
-  __shared__ u64 s_scan[WARPS];
-  __shared__ Found s_found;
+  __shared__ Found s_found, s_best[MAX_CLUSTER];
+  __shared__ u64 s_chunk[2][MAX_CLUSTER];
+  __shared__ Border s_border;
+  __shared__ int s_n;
+  Histogram& s_h = s_u.h;
   T* s_x = reinterpret_cast<T*>(s_raw);
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = cluster.block_rank(), size = cluster.num_blocks(), m = blockIdx.x / size, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -96,29 +112,59 @@ sample_kernel(Params p) {
   if (greedy) top_k = 1;
   const double inv_t = greedy ? 1.0 : 1.0 / (double)temperature;
 
-  // ---- scores: warp's ids v0 .. v1 - 1, of the CTA's c0 .. ----
-  const int each = ((p.vocab + size * WARPS - 1) / (size * WARPS) + 31) / 32 * 32;
-  const int c0 = min(rank * WARPS * each, p.vocab), v0 = min(c0 + warp * each, p.vocab), v1 = min(v0 + each, p.vocab);
-  auto score = [&](int v) { return KEPT ? s_x[v - c0] : clean(row[v]); };
+  // ---- places: the warp's g0 .. g1 - 1, of the CTA's c0 ..; scores at shift .. end - 1 ----
+  const int shift = (int)(reinterpret_cast<uintptr_t>(row) / sizeof(T) % VEC), end = p.vocab + shift;
+  const int each = p.each, c0 = rank * WARPS * each, g0 = c0 + warp * each, g1 = min(g0 + each, (end + VEC - 1) / VEC * VEC);
+  auto fetch = [&](int g, T (&x)[VEC]) {                       // VEC scores from memory, -inf where there are none
+    if (g >= shift && g + VEC <= end) {
+      const uint4 v = *reinterpret_cast<const uint4*>(row + (g - shift));
+      *reinterpret_cast<uint4*>(x) = v;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[j] = clean(x[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[j] = g + j >= shift && g + j < end ? clean(row[g + j - shift]) : from_f32<T>(-INFINITY);
+    }
+  };
+  // calls f(place of the first, VEC scores) by all lanes of the warp alike: lanes beyond the end get -inf
+  auto sweep = [&](auto f) {
+    for (int i0 = g0; i0 < g1; i0 += 32 * VEC) {
+      const int g = i0 + lane * VEC;
+      T x[VEC];
+      if (g >= g1) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[j] = from_f32<T>(-INFINITY);
+      } else if (KEPT) {
+        *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(s_x + (g - c0));
+      } else {
+        fetch(g, x);
+      }
+      f(g, x);
+    }
+  };
   float top = -INFINITY;
-  for (int v = v0 + lane; v < v1; v += 32) {
-    const T x = clean(row[v]);
-    if (KEPT) s_x[v - c0] = x;
-    top = fmaxf(top, to_f32(x));
+#pragma unroll 4
+  for (int g = g0 + lane * VEC; g < g1; g += 32 * VEC) {
+    T x[VEC];
+    fetch(g, x);
+    if (KEPT) *reinterpret_cast<uint4*>(s_x + (g - c0)) = *reinterpret_cast<const uint4*>(x);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) top = fmaxf(top, to_f32(x[j]));
   }
 #pragma unroll
   for (int w = 16; w; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
   if (lane == 0) s_warp[warp] = __float_as_uint(top);
-  __syncthreads();
-  for (int w = 0; w < WARPS; ++w) top = fmaxf(top, __uint_as_float((uint32_t)s_warp[w]));
   cluster.sync();                                            // (all CTAs run: their shared memory may be written)
-  if (tid < size) cluster.map_shared_rank(s_top, tid)[rank] = top;
-  cluster.sync();
-  for (int j = 0; j < size; ++j) top = fmaxf(top, s_top[j]);
+  for (int w = 0; w < WARPS; ++w) top = fmaxf(top, __uint_as_float((uint32_t)s_warp[w]));
+  if (size > 1) {
+    if (tid < size) cluster.map_shared_rank(s_top, tid)[rank] = top;
+    cluster.sync();
+    for (int j = 0; j < size; ++j) top = fmaxf(top, s_top[j]);
+  }
 
   if (bad || top == -INFINITY) {                              // (all CTAs alike)
     if (out)
-      for (int v = v0 + lane; v < v1; v += 32) out[v] = from_f32<T>(-INFINITY);
+      for (int g = max(c0, shift) + tid; g < min(c0 + WARPS * each, end); g += THREADS) out[g - shift] = from_f32<T>(-INFINITY);
     if (rank == 0 && tid == 0) {
       if (bad) latch_error(p.status, AD_ERR_ARG);
       p.tokens[m] = bad ? -1 : 0;
@@ -131,6 +177,7 @@ sample_kernel(Params p) {
   };
   const double unit = ldexp(1.0, p.scale_bits);
   auto weight = [&](float x) { return __double2ull_rn(exact(x) * unit); };
+  auto below = [&](float x) { return x == top ? 0.f : top - x; };
 
   // ---- sums over the cluster in the order of its warps: of x (alike in all lanes of a warp), in front of this warp, and all ----
   auto cluster_sum = [&](u64 x, u64& before) {
@@ -143,6 +190,7 @@ sample_kernel(Params p) {
       if (w < warp) before += s_warp[w];
       mine += s_warp[w];
     }
+    if (size == 1) return mine;
     if (tid == 0) s_cta[0] = mine;
     cluster.sync();
     for (int j = 0; j < size; ++j) {
@@ -158,46 +206,72 @@ sample_kernel(Params p) {
     for (int w = 16; w; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
     return x;
   };
+  // sums over the CTA in the order of its threads, in front of this one, and all
+  auto cta_scan = [&](uint32_t n, u64 x, u64& front_n, u64& front, u64& all_n, u64& all) {
+    u64 run_n = n, run = x;
+#pragma unroll
+    for (int w = 1; w < 32; w <<= 1) {
+      const u64 a = __shfl_up_sync(0xffffffffu, run_n, w), b = __shfl_up_sync(0xffffffffu, run, w);
+      if (lane >= w) { run_n += a; run += b; }
+    }
+    __syncthreads();
+    if (lane == 31) { s_scan_n[warp] = (uint32_t)run_n; s_scan[warp] = run; }
+    __syncthreads();
+    front_n = run_n - n;
+    front = run - x;
+    all_n = all = 0;
+    for (int w = 0; w < WARPS; ++w) {
+      if (w < warp) { front_n += s_scan_n[w]; front += s_scan[w]; }
+      all_n += s_scan_n[w];
+      all += s_scan[w];
+    }
+  };
 
-  // ---- the border: of those with keys from `from` on (of those at `from` itself only the first `from_n`), the key at which `passes` ends ----
-  // BY_MASS: goal is what the weight in front has to be below; else the number in front.
-  uint32_t border = 0, border_n = 0xffffffffu;                // kept: keys above border, and the first border_n that have it
-  uint32_t from = 0, from_n = 0xffffffffu;
-  auto search = [&](bool by_mass, double share, u64 k) {
+  // ---- borders: of the scores above `from`, and the first from_n of those that have it (0: of all), where top-k's count or top-p's share of the weight ends ----
+  uint32_t from = 0, from_n = 0;
+  const bool by_k = top_k > 0 && top_k < p.vocab, by_p = top_p < 1.f;
+  // Of n ties of weight w, those with front + j w below the goal, the very first in any case.
+  auto ties_below = [&](u64 n, u64 w, u64 front, double goal) {
+    if (w == 0) return n;
+    const double want = (goal - (double)front) / (double)w;
+    u64 t = want < 1.0 ? 1 : want >= (double)n ? n : (u64)want;
+    while (t > 1 && !((double)(front + (t - 1) * w) < goal)) --t;
+    while (t < n && (double)(front + t * w) < goal) ++t;
+    return t;
+  };
+  // Digit by digit of the key: any number of ties, and as many rounds as digits.
+  auto search_digits = [&](bool by_mass, double share, u64 k) {
     uint32_t prefix = 0;
     int above = Key<T>::BITS;                                  // bits below which the digit lies
     u64 in_front_n = 0, in_front = 0;
     double goal = 0.0;
     Found f;
     while (above > 0) {
-      const int bits = min(DIGIT, above), shift = above - bits;
+      const int bits = min(DIGIT, above), shr = above - bits;
       for (int i = tid; i < BINS; i += THREADS) s_h.n[i] = s_h.lo[i] = s_h.hi[i] = 0;
       __syncthreads();
       const bool first_level = above == Key<T>::BITS;
-      for (int v = v0 + lane; v < v1; v += 32) {
-        const float x = to_f32(score(v));
-        const uint32_t key = Key<T>::of(x);
-        if ((first_level || key >> above == prefix) && (key > from || from == 0)) {
-          const uint32_t bin = key >> shift & ((1u << bits) - 1u);
-          atomicAdd(&s_h.n[bin], 1u);
-          if (by_mass) add_mass(s_h, bin, weight(x));
+      sweep([&](int g, const T (&x)[VEC]) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const float xf = to_f32(x[j]);
+          const uint32_t key = Key<T>::of(xf);
+          if (g + j >= shift && g + j < end && (first_level || key >> above == prefix) && key > from) {
+            const uint32_t bin = key >> shr & ((1u << bits) - 1u);
+            atomicAdd(&s_h.n[bin], 1u);
+            if (by_mass) add_mass(s_h, bin, weight(xf));
+          }
         }
-      }
+      });
       if (from != 0 && rank == 0 && tid == 0 && (first_level || from >> above == prefix)) {     // ties at the border found before: as many as were kept
-        const uint32_t bin = from >> shift & ((1u << bits) - 1u);
-        // (a key's score)
-        const uint32_t wide = Key<T>::BITS == 16 ? from << 16 | (from & 0x8000u ? 0u : 0xffffu) : from;
-        const float x = __uint_as_float(wide & 0x80000000u ? wide & 0x7fffffffu : ~wide);
+        const uint32_t bin = from >> shr & ((1u << bits) - 1u);
         atomicAdd(&s_h.n[bin], from_n);
-        if (by_mass) {
-          const u64 w = weight(x) * from_n;
-          add_mass(s_h, bin, w);
-        }
+        if (by_mass) add_mass(s_h, bin, weight(score_of<T>(from)) * from_n);
       }
       cluster.sync();
       // a thread's bins, from the last one on
-      uint32_t n[PER];
-      u64 mass[PER], sum_n = 0, sum = 0;
+      uint32_t n[PER], sum_n = 0;
+      u64 mass[PER], sum = 0;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int bin = BINS - 1 - (tid * PER + i);
@@ -211,29 +285,19 @@ sample_kernel(Params p) {
         sum_n += n[i];
         sum += mass[i];
       }
-      // in front of them
-      u64 run_n = sum_n, run = sum;
-#pragma unroll
-      for (int w = 1; w < 32; w <<= 1) {
-        const u64 a = __shfl_up_sync(0xffffffffu, run_n, w), b = __shfl_up_sync(0xffffffffu, run, w);
-        if (lane >= w) { run_n += a; run += b; }
-      }
-      if (lane == 31) { s_scan_n[warp] = (uint32_t)run_n; s_scan[warp] = run; }
-      __syncthreads();
-      u64 front_n = in_front_n + run_n - sum_n, front = in_front + run - sum, total = in_front;
-      for (int w = 0; w < WARPS; ++w) {
-        if (w < warp) { front_n += s_scan_n[w]; front += s_scan[w]; }
-        total += s_scan[w];
-      }
-      if (first_level) goal = share * (double)total;
+      u64 front_n, front, all_n, all;
+      cta_scan(sum_n, sum, front_n, front, all_n, all);
+      front_n += in_front_n;
+      front += in_front;
+      if (first_level) goal = share * (double)all;
       // the last bin that has any, and in front of which there is less than the goal (the first one in any case)
       if (tid == 0) s_found.bin = BINS;
       __syncthreads();
-      uint32_t best = BINS;
+      int best = BINS;
       Found mine = {};
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const uint32_t bin = BINS - 1 - (tid * PER + i);
+        const int bin = BINS - 1 - (tid * PER + i);
         if (n[i] > 0 && (by_mass ? front_n == 0 || (double)front < goal : front_n < k)) {
           best = bin;
           mine = Found{bin, n[i], front_n, front, mass[i]};
@@ -248,71 +312,247 @@ sample_kernel(Params p) {
       f = s_found;
       in_front_n = f.in_front_n;
       in_front = f.in_front;
-      prefix = prefix << bits | f.bin;
-      above = shift;
+      prefix = prefix << bits | (uint32_t)f.bin;
+      above = shr;
       cluster.sync();                                          // (histograms have been read)
     }
-    border = prefix;
-    if (by_mass) {
-      // of n ties of weight w, those with in_front + j w below the goal (the very first in any case)
-      const u64 w = f.mass / f.n;
-      u64 t = f.n;
-      if (w > 0) {
-        const double want = (goal - (double)in_front) / (double)w;
-        t = want < 1.0 ? 1 : want >= (double)f.n ? f.n : (u64)want;
-        while (t > 1 && !((double)(in_front + (t - 1) * w) < goal)) --t;
-        while (t < f.n && (double)(in_front + t * w) < goal) ++t;
-      }
-      border_n = (uint32_t)t;
-    } else {
-      border_n = (uint32_t)min((u64)f.n, k - in_front_n);
-    }
-    return f.n;
+    const u64 t = by_mass ? ties_below(f.n, f.mass / f.n, in_front, goal) : min((u64)f.n, k - in_front_n);
+    return Border{prefix, (uint32_t)t, f.n};
   };
-  uint32_t ties = 0;                                           // that have the border's key
-  const bool by_k = top_k > 0 && top_k < p.vocab, by_p = top_p < 1.f;
+  auto search = [&](bool by_mass, double share, u64 k) {
+    for (int i = tid; i < BINS; i += THREADS) s_h.n[i] = s_h.lo[i] = s_h.hi[i] = 0;
+    __syncthreads();
+    sweep([&](int g, const T (&x)[VEC]) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float xf = to_f32(x[j]);
+        if (Key<T>::of(xf) > from && g + j >= shift && g + j < end) {
+          const int bin = bin_of(below(xf));
+          atomicAdd(&s_h.n[bin], 1u);
+          if (by_mass) add_mass(s_h, bin, weight(xf));
+        }
+      }
+    });
+    const float from_x = from != 0 ? score_of<T>(from) : 0.f;
+    const u64 from_w = from != 0 && by_mass ? weight(from_x) : 0;
+    const int from_bin = from != 0 ? bin_of(below(from_x)) : -1;
+    if (from != 0 && rank == 0 && tid == 0) {                  // ties at the border found before: as many as were kept
+      atomicAdd(&s_h.n[from_bin], from_n);
+      if (by_mass) add_mass(s_h, from_bin, from_w * from_n);
+    }
+    cluster.sync();
+    // every CTA adds up its part of the bins, a few a thread
+    const int chunk = BINS / size, per = max(1, chunk / THREADS), b0 = rank * chunk + tid * per;
+    uint32_t n[PER], sum_n = 0;
+    u64 mass[PER], sum = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      n[i] = 0;
+      mass[i] = 0;
+      if (i < per && tid * per < chunk)
+        for (int j = 0; j < size; ++j) {
+          const Histogram* h = cluster.map_shared_rank(&s_h, j);
+          n[i] += h->n[b0 + i];
+          if (by_mass) mass[i] += ((u64)h->hi[b0 + i] << 32) + h->lo[b0 + i];
+        }
+      sum_n += n[i];
+      sum += mass[i];
+    }
+    u64 front_n, front, all_n, all;
+    cta_scan(sum_n, sum, front_n, front, all_n, all);
+    if (size > 1) {
+      if (tid < size) {
+        cluster.map_shared_rank(&s_chunk[0][0], tid)[rank] = all_n;
+        cluster.map_shared_rank(&s_chunk[1][0], tid)[rank] = all;
+      }
+      cluster.sync();
+      all = 0;
+      for (int j = 0; j < size; ++j) {
+        if (j < rank) { front_n += s_chunk[0][j]; front += s_chunk[1][j]; }
+        all += s_chunk[1][j];
+      }
+    }
+    const double goal = share * (double)all;
+    // the last bin that has any, and in front of which there is less than the goal (the first one in any case)
+    if (tid == 0) s_found.bin = -1;
+    __syncthreads();
+    int best = -1;
+    Found mine = {};
+    mine.bin = -1;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (n[i] > 0 && (by_mass ? front_n == 0 || (double)front < goal : front_n < k)) {
+        best = b0 + i;
+        mine = Found{best, n[i], front_n, front, mass[i]};
+      }
+      front_n += n[i];
+      front += mass[i];
+    }
+    if (best >= 0) atomicMax(&s_found.bin, best);
+    __syncthreads();
+    if (best >= 0 && s_found.bin == best) s_found = mine;
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    Found f = s_found;
+    if (size > 1) {
+      if (tid < size) cluster.map_shared_rank(s_best, tid)[rank] = f;
+      cluster.sync();
+      for (int j = 0; j < size; ++j)
+        if (s_best[j].bin >= f.bin) f = s_best[j];
+    }
+    if (f.n > LIST) {
+      cluster.sync();                                          // (histograms and what was found have been read)
+      return search_digits(by_mass, share, k);
+    }
+    // the bin's scores, with their ids, to the first CTA: in ascending order of (keys from the largest on, ids)
+    int* counter = cluster.map_shared_rank(&s_n, 0);
+    u64* list = cluster.map_shared_rank(s_u.list, 0);
+    sweep([&](int g, const T (&x)[VEC]) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float xf = to_f32(x[j]);
+        const uint32_t key = Key<T>::of(xf);
+        if (key > from && g + j >= shift && g + j < end && bin_of(below(xf)) == f.bin) list[atomicAdd(counter, 1)] = (u64)~key << 32 | (uint32_t)(g + j - shift);
+      }
+    });
+    cluster.sync();
+    if (rank == 0) {
+      const int have = s_n;
+      int n2 = 2;
+      while (n2 < have) n2 <<= 1;
+      for (int i = have + tid; i < n2; i += THREADS) s_u.list[i] = ~0ull;
+      __syncthreads();
+      for (int a = 2; a <= n2; a <<= 1)
+        for (int b = a >> 1; b; b >>= 1) {
+          for (int i = tid; i < n2 / 2; i += THREADS) {
+            const int lo = (i & (b - 1)) | (i & ~(b - 1)) << 1, hi = lo | b;
+            const u64 x = s_u.list[lo], y = s_u.list[hi];
+            if ((x > y) == ((lo & a) == 0)) { s_u.list[lo] = y; s_u.list[hi] = x; }
+          }
+          __syncthreads();
+        }
+      auto key_at = [&](int i) { return ~(uint32_t)(s_u.list[i] >> 32); };
+      // how many of them, in order, are kept
+      int kept;
+      u64 inside = 0;                                          // weight of all of them
+      if (by_mass) {
+        const int per_thread = (n2 + THREADS - 1) / THREADS, i0 = tid * per_thread;
+        u64 w = 0, unused_n, before, unused;
+        for (int i = i0; i < min(i0 + per_thread, have); ++i) w += weight(score_of<T>(key_at(i)));
+        cta_scan(0, w, unused_n, before, unused, inside);
+        uint32_t below_goal = 0;
+        u64 run = f.in_front + before;
+        for (int i = i0; i < min(i0 + per_thread, have); ++i) {
+          below_goal += (i == 0 && f.in_front_n == 0) || (double)run < goal;
+          run += weight(score_of<T>(key_at(i)));
+        }
+        u64 a, b, total;
+        cta_scan(below_goal, 0, a, b, total, unused);
+        kept = (int)total;
+      } else {
+        kept = (int)min((u64)have, k - f.in_front_n);
+      }
+      if (tid == 0) {
+        Border x;
+        const u64 virtual_ties = f.bin == from_bin ? from_n : 0;       // (of the border before: behind all others)
+        const bool into = by_mass && virtual_ties > 0 && kept == have && (have == 0 || (double)(f.in_front + inside) < goal);
+        if (into || have == 0) {
+          x.key = from;
+          x.kept = (uint32_t)ties_below(virtual_ties, from_w, f.in_front + inside, goal);
+          x.ties = 0xffffffffu;                                // (as many as were found before)
+        } else {
+          x.key = key_at(kept - 1);
+          int lo = kept - 1, hi = kept;
+          while (lo > 0 && key_at(lo - 1) == x.key) --lo;
+          while (hi < have && key_at(hi) == x.key) ++hi;
+          x.kept = kept - lo;
+          x.ties = hi - lo;
+        }
+        s_border = x;
+        for (int j = 1; j < size; ++j) *cluster.map_shared_rank(&s_border, j) = x;
+      }
+    }
+    cluster.sync();
+    return s_border;
+  };
+  Border border = {0, 0xffffffffu, 0};
   if (by_k) {
-    ties = search(false, 0.0, (u64)top_k);
-    from = border;
-    from_n = border_n;
+    border = search(false, 0.0, (u64)top_k);
+    from = border.key;
+    from_n = border.kept;
   }
   if (by_p) {
-    const uint32_t all = search(true, (double)top_p, 0);
-    if (border != from) ties = all;                            // (else: of those at the border before, some more go)
+    const uint32_t ties = border.ties;
+    border = search(true, (double)top_p, 0);
+    if (by_k && border.key == from) border.ties = ties;        // (of those at the border before, some more go)
   }
 
   // ---- what is kept, in the order of ids ----
-  const bool some_ties = (by_k || by_p) && border_n < ties;
+  const bool some_ties = (by_k || by_p) && border.kept < border.ties;
   u64 tie_rank = 0;
   if (some_ties) {
     u64 mine = 0;
-    for (int v = v0 + lane; v < v1; v += 32) mine += Key<T>::of(to_f32(score(v))) == border;
+    sweep([&](int g, const T (&x)[VEC]) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) mine += g + j >= shift && g + j < end && Key<T>::of(to_f32(x[j])) == border.key;
+    });
     cluster_sum(warp_sum(mine), tie_rank);
   }
   const double least = min_p > 0.f ? (double)min_p : 0.0;
-  // f(v, score, whether it is kept, its weight) for the warp's ids, 32 at a time by all lanes
-  auto over = [&](auto f) {
-    u64 at = tie_rank;
-    for (int i0 = v0; i0 < v1; i0 += 32) {
-      const int v = i0 + lane;
-      const T x = v < v1 ? score(v) : from_f32<T>(-INFINITY);
-      const float xf = to_f32(x);
-      const uint32_t key = Key<T>::of(xf);
-      bool keep = v < v1 && key >= border;
-      if (some_ties) {
-        const unsigned tie = __ballot_sync(0xffffffffu, v < v1 && key == border);
-        if (key == border) keep = keep && at + __popc(tie & ((1u << lane) - 1u)) < border_n;
-        at += __popc(tie);
-      }
-      const double w = keep ? exact(xf) : 0.0;
-      keep = keep && w >= least;
-      f(v, x, keep, keep ? __double2ull_rn(w * unit) : 0ull);
+  // Weights of VEC scores, 0 where they go, and which stay; `at`: ties in front of the warp's first.
+  auto keep = [&](int g, const T (&x)[VEC], u64& at, u64 (&w)[VEC]) {
+    uint32_t stay = 0, tie = 0;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const uint32_t key = Key<T>::of(to_f32(x[j]));
+      const bool in = g + j >= shift && g + j < end;
+      if (in && key >= border.key) stay |= 1u << j;
+      if (in && key == border.key) tie |= 1u << j;
     }
+    if (some_ties) {
+      int before = __popc(tie), all;
+#pragma unroll
+      for (int s = 1; s < 32; s <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, before, s);
+        if (lane >= s) before += y;
+      }
+      all = __shfl_sync(0xffffffffu, before, 31);
+      before -= __popc(tie);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+        if (tie >> j & 1u && at + before + __popc(tie & ((1u << j) - 1u)) >= border.kept) stay &= ~(1u << j);
+      at += all;
+    }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      w[j] = 0;
+      if (stay >> j & 1u) {
+        const double e = exact(to_f32(x[j]));
+        if (e >= least) w[j] = __double2ull_rn(e * unit);
+        else stay &= ~(1u << j);
+      }
+    }
+    return stay;
   };
-  u64 mine = 0, before;
-  over([&](int v, T x, bool keep, u64 w) {
-    mine += w;
-    if (out && v < v1) out[v] = keep ? x : from_f32<T>(-INFINITY);
+  const bool aligned_out = out && reinterpret_cast<uintptr_t>(out) / sizeof(T) % VEC == (unsigned)shift;
+  u64 mine = 0, before, at = tie_rank;
+  sweep([&](int g, const T (&x)[VEC]) {
+    u64 w[VEC];
+    const uint32_t stay = keep(g, x, at, w);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) mine += w[j];
+    if (out && g < g1) {
+      T y[VEC];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) y[j] = stay >> j & 1u ? x[j] : from_f32<T>(-INFINITY);
+      if (aligned_out && g >= shift && g + VEC <= end) {
+        __stcs(reinterpret_cast<uint4*>(out + (g - shift)), *reinterpret_cast<const uint4*>(y));
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          if (g + j >= shift && g + j < end) out[g + j - shift] = y[j];
+      }
+    }
   });
   mine = warp_sum(mine);
   const u64 all = cluster_sum(mine, before);
@@ -322,42 +562,45 @@ sample_kernel(Params p) {
   const bool hit = mine > 0 && (past ? before + mine == all : !((double)before > goal) && (double)(before + mine) > goal);
   if (hit) {
     u64 run = before;
-    int token = -1;
-    float x_of = 0.f;
-    // (scores may have been overwritten by what is left of them: the token's is among those)
-    u64 at = tie_rank;
-    (void)at;
-    for (int i0 = v0; i0 < v1 && token < 0; i0 += 32) {
-      const int v = i0 + lane;
-      const float xf = v < v1 ? to_f32(out && !KEPT ? clean(out[v]) : score(v)) : -INFINITY;
-      const uint32_t key = Key<T>::of(xf);
-      bool keep = v < v1 && key >= border;
-      if (some_ties && !(out && !KEPT)) {
-        const unsigned tie = __ballot_sync(0xffffffffu, v < v1 && key == border);
-        if (key == border) keep = keep && at + __popc(tie & ((1u << lane) - 1u)) < border_n;
-        at += __popc(tie);
+    at = tie_rank;
+    bool done = false;
+    // (without KEPT, scores may have been overwritten by what is left of them: those that went are -inf, and the others, ties among them, all stay)
+    sweep([&](int g, const T (&x)[VEC]) {
+      if (done) return;
+      u64 w[VEC], sum = 0;
+      if (!KEPT && out == row) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) w[j] = to_f32(x[j]) == -INFINITY ? 0 : weight(to_f32(x[j]));
+      } else {
+        keep(g, x, at, w);
       }
-      const double w = keep ? exact(xf) : 0.0;
-      const u64 x = keep && w >= least ? __double2ull_rn(w * unit) : 0ull;
-      u64 sum = x;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) sum += w[j];
+      u64 upto = sum;
 #pragma unroll
       for (int s = 1; s < 32; s <<= 1) {
-        const u64 y = __shfl_up_sync(0xffffffffu, sum, s);
-        if (lane >= s) sum += y;
+        const u64 y = __shfl_up_sync(0xffffffffu, upto, s);
+        if (lane >= s) upto += y;
       }
-      const bool is = x > 0 && (past ? run + sum == all : (double)(run + sum) > goal);
-      const unsigned who = __ballot_sync(0xffffffffu, is);
+      auto passes = [&](u64 x) { return past ? x == all : (double)x > goal; };
+      const unsigned who = __ballot_sync(0xffffffffu, sum > 0 && passes(run + upto));
       if (who) {
-        const int l = __ffs(who) - 1;
-        token = i0 + l;
-        x_of = __shfl_sync(0xffffffffu, xf, l);
+        done = true;
+        if (lane == __ffs(who) - 1) {
+          u64 y = run + upto - sum;
+          int token = -1;
+          float x_of = 0.f;
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) {
+            y += w[j];
+            if (token < 0 && w[j] > 0 && passes(y)) { token = g + j - shift; x_of = to_f32(x[j]); }
+          }
+          p.tokens[m] = token;
+          if (p.logp) p.logp[m] = (float)((x_of == top ? 0.0 : ((double)x_of - (double)top) * inv_t) - log((double)all / unit));
+        }
       }
-      run += __shfl_sync(0xffffffffu, sum, 31);
-    }
-    if (lane == 0) {
-      p.tokens[m] = token;
-      if (p.logp) p.logp[m] = (float)((x_of == top ? 0.0 : ((double)x_of - (double)top) * inv_t) - log((double)all / unit));
-    }
+      run += __shfl_sync(0xffffffffu, upto, 31);
+    });
   }
 }
 
