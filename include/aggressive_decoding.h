@@ -451,12 +451,13 @@ int ad_cache_compact(const ad_kv_pool* pool, const ad_kv_cache* caches, int32_t 
 /* Sampling: the token that follows each of M rows of scores [M, vocab] (dtype; rows `stride` scores apart), from given random numbers r [M], uniform in [0, 1).
  * With w(v) = exp((score(v) - largest) / temperature) and ids in descending order of their scores (ties: lowest id first): top_k keeps the first top_k ids
  * (0 or less: all); top_p, of these, the ones in front of which less than top_p of their weight lies, and the first in any case (1 or more: all); min_p, of
- * those, the ones with w >= min_p (0 or less: all).  tokens[m] is the lowest kept id at which the running sum of w, over kept ids in ascending order,
+ * those, the ones with w >= min_p (0 or less: all; 1 or more: those that tie with the largest).  tokens[m] is the lowest kept id at which the running sum of w, over kept ids in ascending order,
  * exceeds r[m] times its total.  Every parameter is a device array [M] or NULL (temperature one; no such filter).  temperature 0: the largest score, lowest id.
  * logp (NULL: not wanted) [M] receives the token's log-probability among the kept ids.  filtered (NULL: not wanted) [M, vocab] in dtype, rows filtered_stride
  * apart, receives the scores of the kept ids and -inf for the others: what ad_accept_sampled takes as the scores of a truncated distribution, the verifier's or the
  * drafter's.  It may be `scores` itself (with the same stride).
- * Weights are computed in 64 bits and summed as integers in units of 2^-62 * vocab of the largest (vocab rounded up to a power of two); comparisons are decided on these sums.
+ * Weights are computed in 64 bits and summed as integers in units of 2^-62 * vocab of the largest (vocab rounded up to a power of two, 2048 at least); comparisons are decided on
+ * these sums, and the ones of min_p on the weights.
  * Scores of -inf have no weight, +inf share all of it, a NaN counts as -inf.  A row without any score above -inf takes id 0 with logp -inf.  One whose
  * temperature is negative or not finite, or with a NaN for a parameter or r, latches AD_ERR_ARG: token -1, logp and all filtered scores -inf.  vocab is at most 2^20. */
 int ad_sample(const void* scores, int64_t stride, int32_t dtype, int32_t vocab, int32_t M, const float* temperature, const int32_t* top_k,

@@ -186,7 +186,7 @@ extern "C" int ad_sample(const void* scores, int64_t stride, int32_t dtype, int3
   sample::Params p = {};
   p.scores = scores; p.stride = (size_t)stride; p.vocab = vocab; p.M = M; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p; p.r = r;
   p.tokens = tokens; p.logp = logp; p.out = filtered; p.out_stride = (size_t)filtered_stride; p.status = status;
-  p.scale_bits = 62;
+  p.scale_bits = 51;                               // (a weight in the bits of a double, and sums below 2^62)
   while ((1ll << (62 - p.scale_bits)) < vocab) --p.scale_bits;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return launched(entry, dtype == AD_DTYPE_BF16 ? launch_sample<bf16>(p, st) : launch_sample<float>(p, st));

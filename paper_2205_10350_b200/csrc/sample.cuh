@@ -4,7 +4,6 @@
 #include <cooperative_groups.h>
 #include <math.h>
 
-#include "accept_sampled.cuh"      // exp_below
 #include "kv_cache.cuh"
 
 namespace ad {
@@ -66,8 +65,46 @@ __device__ __forceinline__ void add_mass(Histogram& h, uint32_t bin, u64 w) {
   const uint32_t up = (uint32_t)(w >> 32) + carry;
   if (up) atomicAdd(&h.hi[bin], up);
 }
-// Bin of a score that lies y below the largest: 128 to the octave of y, from 2^-7 to 2^9.
-__device__ __forceinline__ int bin_of(float y) { return min(max((int)(__float_as_uint(y) >> 16) - (120 << 7), 0), BINS - 1); }
+// Bin of a score x: by how far it lies below the largest, 128 to the octave, from 2^-7 to 2^9.  (Two infinities are no distance apart.)
+__device__ __forceinline__ int bin_of(float top, float x) { return min(max((int)(__float_as_uint(fmaxf(top - x, 0.f)) >> 16) - (120 << 7), 0), BINS - 1); }
+
+// Weights in units of 2^-bits, bits <= 51, to the last bits of FP64: w = 2^(k / 256) exp(f), k / 256 and f the whole 256ths and the rest of the exponent to the base of 2,
+// the first from a table of 2^(j / 256) and the exponent, the second from its Taylor series up to f^4 (f^5 / 120 < 5e-17); the table-driven scheme of Tang (1989).
+constexpr int EXP_TABLE = 256;
+struct Weights {
+  const double* table;
+  double top, scale;             // largest score; 256 log2(e) / T
+  float topf, half_top, twice;   // largest score, half of it; 2 / T
+  int bits;
+  __device__ __forceinline__ double fraction(float x, int& n) const {      // of 2^n
+    const double ROUND = 6755399441055744.0;                                  // 1.5 * 2^52: the sum's low word is k
+    const double z = ((double)x - top) * scale, kd = z + ROUND;
+    const int k = __double2loint(kd);
+    const double f = (z - (kd - ROUND)) * (0.693147180559945309417 / 256.0);
+    double e = fma(f, 1.0 / 24.0, 1.0 / 6.0);
+    e = fma(f, e, 0.5);
+    e = fma(f, e, 1.0);
+    const double t = table[k & (EXP_TABLE - 1)];
+    n = k >> 8;
+    return fma(t * f, e, t);
+  }
+  // Whether x has any weight to speak of: 2^-54 and less is none in these units.  (An infinite largest score takes all of it.)
+  __device__ __forceinline__ bool any(float x) const { return fmaf(-0.5f, x, half_top) * twice < 38.f; }
+  __device__ __forceinline__ u64 operator()(float x) const {
+    if (x == topf) return 1ull << bits;
+    if (!any(x)) return 0;
+    int n;
+    const double e = fraction(x, n);
+    const double w = __hiloint2double(__double2hiint(e) + ((n + bits) << 20), __double2loint(e)) + 4503599627370496.0;      // (2^52: the sum's low bits are w, rounded)
+    return (u64)__double_as_longlong(w) & 0xfffffffffffffull;
+  }
+  // w(x) >= least, in FP64
+  __device__ __forceinline__ bool reaches(float x, double least) const {
+    if (x == topf) return 1.0 >= least;
+    if (isinf(topf) || x == -INFINITY) return 0.0 >= least;
+    return exp(((double)x - top) * (scale * (0.693147180559945309417 / 256.0))) >= least;
+  }
+};
 
 // One row by a cluster of CTAs that share the vocabulary, every warp a run of ids.
 //   w(v) = exp((score(v) - largest) / T); tokens are ordered by score, ties by id.  Top-k keeps the first k; top-p, of these, the ones in front of
@@ -77,7 +114,7 @@ __device__ __forceinline__ int bin_of(float y) { return min(max((int)(__float_as
 // The k-th largest score, and the one at which the weight in front reaches top_p of the whole: a histogram over the distance from the largest (in shared memory, summed
 // over the cluster), the bin in which the border lies, and that bin's scores put in order by one CTA; where these are too many (ties, as a rule), digit
 // by digit of their keys.  Weights are worked out in FP64 and summed as integers in units of 2^-scale_bits (vocab * 2^scale_bits <= 2^62): the largest is 1, so a
-// sum is off by vocab * 2^-(scale_bits + 1) of itself at most, 2^-43 with 1000 ids and 2^-23 with 2^20 (roundings of either sign: their root, a 2^-10th
+// sum is off by vocab * 2^-(scale_bits + 1) of itself at most, 2^-42 with 1000 ids and 2^-23 with 2^20 (roundings of either sign: their root, a 2^-10th
 // of that, in fact), and comes out the same in any order.
 // Scores are taken 16 bytes at a time: places g = id + shift, shift such that a place that is a multiple of a vector's lies on a vector's boundary.
 // grid = M clusters, block = THREADS.  Dynamic shared memory: KEPT, the CTA's scores.
@@ -87,7 +124,7 @@ sample_kernel(Params p) {
   constexpr int VEC = 16 / sizeof(T);
   extern __shared__ __align__(16) unsigned char s_raw[];
   __shared__ __align__(16) union { Histogram h; u64 list[LIST]; } s_u;
-  __shared__ double s_table[sampled::EXP_TABLE];
+  __shared__ double s_table[EXP_TABLE];
   __shared__ float s_top[MAX_CLUSTER];
   __shared__ u64 s_warp[WARPS], s_scan[WARPS], s_cta[1];
   __shared__ uint32_t s_scan_n[WARPS];
@@ -100,7 +137,7 @@ sample_kernel(Params p) {
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = cluster.block_rank(), size = cluster.num_blocks(), m = blockIdx.x / size, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_launch();
-  if (tid < sampled::EXP_TABLE) s_table[tid] = exp2(tid / (double)sampled::EXP_TABLE);
+  if (tid < EXP_TABLE) s_table[tid] = exp2(tid / (double)EXP_TABLE);
   pdl_wait();
   const T* row = static_cast<const T*>(p.scores) + (size_t)m * p.stride;
   T* out = p.out ? static_cast<T*>(p.out) + (size_t)m * p.out_stride : nullptr;
@@ -172,12 +209,8 @@ sample_kernel(Params p) {
     }
     return;
   }
-  auto exact = [&](float x) {                                 // weight; 1 at the top even where that is infinite
-    return x == top ? 1.0 : isinf(top) || x == -INFINITY ? 0.0 : sampled::exp_below(((double)x - (double)top) * inv_t, s_table);
-  };
+  const Weights weight = {s_table, (double)top, inv_t * (256.0 / 0.693147180559945309417), top, 0.5f * top, (float)(2.0 * inv_t), p.scale_bits};
   const double unit = ldexp(1.0, p.scale_bits);
-  auto weight = [&](float x) { return __double2ull_rn(exact(x) * unit); };
-  auto below = [&](float x) { return x == top ? 0.f : top - x; };
 
   // ---- sums over the cluster in the order of its warps: of x (alike in all lanes of a warp), in front of this warp, and all ----
   auto cluster_sum = [&](u64 x, u64& before) {
@@ -228,7 +261,9 @@ sample_kernel(Params p) {
   };
 
   // ---- borders: of the scores above `from`, and the first from_n of those that have it (0: of all), where top-k's count or top-p's share of the weight ends ----
-  uint32_t from = 0, from_n = 0;
+  // (Scores of -inf have no weight and are never among those; places that there are no scores for hold -inf.)
+  uint32_t from = Key<T>::of(-INFINITY), from_n = 0;
+  float from_x = -INFINITY;
   const bool by_k = top_k > 0 && top_k < p.vocab, by_p = top_p < 1.f;
   // Of n ties of weight w, those with front + j w below the goal, the very first in any case.
   auto ties_below = [&](u64 n, u64 w, u64 front, double goal) {
@@ -256,17 +291,17 @@ sample_kernel(Params p) {
         for (int j = 0; j < VEC; ++j) {
           const float xf = to_f32(x[j]);
           const uint32_t key = Key<T>::of(xf);
-          if (g + j >= shift && g + j < end && (first_level || key >> above == prefix) && key > from) {
+          if ((first_level || key >> above == prefix) && xf > from_x) {
             const uint32_t bin = key >> shr & ((1u << bits) - 1u);
             atomicAdd(&s_h.n[bin], 1u);
             if (by_mass) add_mass(s_h, bin, weight(xf));
           }
         }
       });
-      if (from != 0 && rank == 0 && tid == 0 && (first_level || from >> above == prefix)) {     // ties at the border found before: as many as were kept
+      if (from_n != 0 && rank == 0 && tid == 0 && (first_level || from >> above == prefix)) {     // ties at the border found before: as many as were kept
         const uint32_t bin = from >> shr & ((1u << bits) - 1u);
         atomicAdd(&s_h.n[bin], from_n);
-        if (by_mass) add_mass(s_h, bin, weight(score_of<T>(from)) * from_n);
+        if (by_mass) add_mass(s_h, bin, weight(from_x) * from_n);
       }
       cluster.sync();
       // a thread's bins, from the last one on
@@ -326,17 +361,16 @@ sample_kernel(Params p) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float xf = to_f32(x[j]);
-        if (Key<T>::of(xf) > from && g + j >= shift && g + j < end) {
-          const int bin = bin_of(below(xf));
+        if (xf > from_x) {
+          const int bin = bin_of(top, xf);
           atomicAdd(&s_h.n[bin], 1u);
           if (by_mass) add_mass(s_h, bin, weight(xf));
         }
       }
     });
-    const float from_x = from != 0 ? score_of<T>(from) : 0.f;
-    const u64 from_w = from != 0 && by_mass ? weight(from_x) : 0;
-    const int from_bin = from != 0 ? bin_of(below(from_x)) : -1;
-    if (from != 0 && rank == 0 && tid == 0) {                  // ties at the border found before: as many as were kept
+    const u64 from_w = from_n != 0 && by_mass ? weight(from_x) : 0;
+    const int from_bin = from_n != 0 ? bin_of(top, from_x) : -1;
+    if (from_n != 0 && rank == 0 && tid == 0) {                  // ties at the border found before: as many as were kept
       atomicAdd(&s_h.n[from_bin], from_n);
       if (by_mass) add_mass(s_h, from_bin, from_w * from_n);
     }
@@ -411,8 +445,7 @@ sample_kernel(Params p) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float xf = to_f32(x[j]);
-        const uint32_t key = Key<T>::of(xf);
-        if (key > from && g + j >= shift && g + j < end && bin_of(below(xf)) == f.bin) list[atomicAdd(counter, 1)] = (u64)~key << 32 | (uint32_t)(g + j - shift);
+        if (xf > from_x && bin_of(top, xf) == f.bin) list[atomicAdd(counter, 1)] = (u64)~Key<T>::of(xf) << 32 | (uint32_t)(g + j - shift);
       }
     });
     cluster.sync();
@@ -475,11 +508,12 @@ sample_kernel(Params p) {
     cluster.sync();
     return s_border;
   };
-  Border border = {0, 0xffffffffu, 0};
+  Border border = {from, 0, 0};                               // (all above -inf)
   if (by_k) {
     border = search(false, 0.0, (u64)top_k);
     from = border.key;
     from_n = border.kept;
+    from_x = score_of<T>(from);
   }
   if (by_p) {
     const uint32_t ties = border.ties;
@@ -489,26 +523,34 @@ sample_kernel(Params p) {
 
   // ---- what is kept, in the order of ids ----
   const bool some_ties = (by_k || by_p) && border.kept < border.ties;
+  const float border_x = score_of<T>(border.key);
   u64 tie_rank = 0;
   if (some_ties) {
     u64 mine = 0;
     sweep([&](int g, const T (&x)[VEC]) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) mine += g + j >= shift && g + j < end && Key<T>::of(to_f32(x[j])) == border.key;
+      for (int j = 0; j < VEC; ++j) mine += to_f32(x[j]) == border_x;
     });
     cluster_sum(warp_sum(mine), tie_rank);
   }
-  const double least = min_p > 0.f ? (double)min_p : 0.0;
+  const double least = min_p > 0.f ? fmin((double)min_p, 1.0) : 0.0;
+  // min-p: scores above `sure` reach it, those below `never` do not (a hundred thousandth of the distance, and some steps of FP32, to either side of the border)
+  float sure = INFINITY, never = -INFINITY;
+  if (least > 0.0 && !isinf(top)) {
+    const double away = fmax(-log(least) / inv_t, 0.0), slack = away * 1e-5 + (fabs((double)top) + away) * 1e-6;
+    sure = (float)((double)top - away + slack);
+    never = (float)((double)top - away - slack);
+  }
   // Weights of VEC scores, 0 where they go, and which stay; `at`: ties in front of the warp's first.
   auto keep = [&](int g, const T (&x)[VEC], u64& at, u64 (&w)[VEC]) {
     uint32_t stay = 0, tie = 0;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
-      const uint32_t key = Key<T>::of(to_f32(x[j]));
-      const bool in = g + j >= shift && g + j < end;
-      if (in && key >= border.key) stay |= 1u << j;
-      if (in && key == border.key) tie |= 1u << j;
+      const float xf = to_f32(x[j]);
+      if (xf > border_x) stay |= 1u << j;
+      if (xf == border_x) tie |= 1u << j;
     }
+    if (by_k || by_p) stay |= tie;                              // (else the border is -inf)
     if (some_ties) {
       int before = __popc(tie), all;
 #pragma unroll
@@ -523,15 +565,16 @@ sample_kernel(Params p) {
         if (tie >> j & 1u && at + before + __popc(tie & ((1u << j) - 1u)) >= border.kept) stay &= ~(1u << j);
       at += all;
     }
+    if (least > 0.0) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      w[j] = 0;
-      if (stay >> j & 1u) {
-        const double e = exact(to_f32(x[j]));
-        if (e >= least) w[j] = __double2ull_rn(e * unit);
-        else stay &= ~(1u << j);
+      for (int j = 0; j < VEC; ++j) {
+        const float xf = to_f32(x[j]);
+        // clear of the border by far, or worked out
+        if ((stay >> j & 1u) && !(xf > sure) && (xf < never || !weight.reaches(xf, least))) stay &= ~(1u << j);
       }
     }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) w[j] = stay >> j & 1u ? weight(to_f32(x[j])) : 0;
     return stay;
   };
   const bool aligned_out = out && reinterpret_cast<uintptr_t>(out) / sizeof(T) % VEC == (unsigned)shift;
@@ -570,7 +613,7 @@ sample_kernel(Params p) {
       u64 w[VEC], sum = 0;
       if (!KEPT && out == row) {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) w[j] = to_f32(x[j]) == -INFINITY ? 0 : weight(to_f32(x[j]));
+        for (int j = 0; j < VEC; ++j) w[j] = weight(to_f32(x[j]));
       } else {
         keep(g, x, at, w);
       }

@@ -31,7 +31,7 @@ def draw(x, r, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         c = np.concatenate([[0.0], np.cumsum(w[:n])[:-1]])
         kept = int((c < top_p * total).sum())
         n = min(n, max(kept, 1))
-    n = int((w[:n] >= min_p).sum()) if min_p > 0 else n
+    n = int((w[:n] >= min(min_p, 1.0)).sum()) if min_p > 0 else n
     ids = np.sort(order[:n])
     rank = np.empty(len(w), dtype=int)
     rank[order] = np.arange(len(w))
@@ -83,7 +83,7 @@ def test_all_filters_at_all_sizes(dtype, V):
     r = np.random.default_rng(V).random(M).astype(np.float32)
     pick = lambda values, shift=0: [values[(m + shift) % len(values)] for m in range(M)]
     params = dict(temperature=pick([1.0, 0.7, 1.9, 0.3, 5.0]), top_k=pick([0, 50, 1, 7, V, V - 1, V + 5, -3, 1000]), top_p=pick([1.0, 0.9, 0.5, 0.99, 0.0, 0.2, 2.0]),
-                  min_p=pick([0.0, 0.05, 0.0, 0.001, 1.0, -1.0, 0.3, 0.0], 2))
+                  min_p=pick([0.0, 0.05, 0.0, 0.001, 1.0, -1.0, 0.3, 7.0], 2))
     check(logits(M, V, dtype, V), r, **params)
     check(logits(M, V, dtype, V + 1, peaks=False), r, filtered=False, **{n: params[n] for n in ("temperature", "top_p")})
     check(logits(M, V, dtype, V + 2), r, **{n: params[n] for n in ("top_k",)})
@@ -140,10 +140,12 @@ def test_infinities_and_nans(dtype):
     x[8] = torch.finfo(x.dtype).max
     x[8, 5] = torch.finfo(x.dtype).min
     x[9] = x[9] * 1e30
+    x[11] = torch.linspace(-1, 1, V) * 0.99 * torch.finfo(x.dtype).max
     x[10] = x[10] * 1e-38
     r = np.random.default_rng(1).random(12).astype(np.float32)
     for params in ({}, dict(top_k=[3] * 12), dict(top_k=[650] * 12, top_p=[0.8] * 12), dict(top_p=[0.5] * 12), dict(min_p=[0.5] * 12), dict(temperature=[0.0] * 12),
-                   dict(temperature=[1e-30] * 12), dict(temperature=[1e30] * 12, top_p=[0.5] * 12), dict(temperature=[3e38] * 12, top_k=[5] * 12)):
+                   dict(temperature=[1e-30] * 12), dict(temperature=[1e30] * 12, top_p=[0.5] * 12), dict(temperature=[3e38] * 12, top_k=[5] * 12), dict(temperature=[3e38] * 12, top_p=[0.7] * 12),
+                   dict(temperature=[3e38] * 12, min_p=[0.3] * 12), dict(temperature=[1e-42] * 12, top_p=[0.7] * 12)):
         check(x, r, **params)
 
 
