@@ -48,19 +48,41 @@ template <> struct Key<bf16> {
   static __device__ __forceinline__ uint32_t of(float x) { return Key<float>::of(x) >> 16; }
 };
 template <typename T> __device__ __forceinline__ T clean(T x) { return to_f32(x) == to_f32(x) ? x : from_f32<T>(-INFINITY); }     // a NaN counts as -inf
+// Vectors of 16 bytes: as FP32 numbers, their largest, and whether a NaN is among them.
+__device__ __forceinline__ void unpack(uint4 v, float (&x)[4]) { x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w); }
+__device__ __forceinline__ void unpack(uint4 v, float (&x)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ float largest(uint4 v, float) {
+  return fmaxf(kv::max3(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z)), __uint_as_float(v.w));
+}
+__device__ __forceinline__ float largest(uint4 v, bf16) {
+  const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
+  const __nv_bfloat162 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ bool has_nan(uint4 v, float) {
+  return max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu)) > 0x7f800000u;
+}
+__device__ __forceinline__ bool has_nan(uint4 v, bf16) {
+  const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+  return max(m & 0xffffu, m >> 16) > 0x7f80u;
+}
 // A key's score.
 template <typename T> __device__ __forceinline__ float score_of(uint32_t key) {
   const uint32_t wide = Key<T>::BITS == 16 ? key << 16 | (key & 0x8000u ? 0u : 0xffffu) : key;
   return __uint_as_float(wide & 0x80000000u ? wide & 0x7fffffffu : ~wide);
 }
 
-// What has been counted: scores, and their weights in two halves.
-struct Histogram { uint32_t n[BINS], lo[BINS], hi[BINS]; };
-struct Found { int bin; uint32_t n; u64 in_front_n, in_front, mass; };
+// What has been counted: scores, or their weights in two halves.
+struct Histogram { uint32_t lo[BINS], hi[BINS]; };
+struct Found { int bin; u64 in_front, amount; };       // of scores, or of weight
 struct Border { uint32_t key, kept, ties; };      // scores above this key stay, and of those that have it, `ties`, the first `kept`
 
-// 64-bit sums from 32-bit atomic additions: exact, so that their order does not matter.
-__device__ __forceinline__ void add_mass(Histogram& h, uint32_t bin, u64 w) {
+// 64-bit sums from 32-bit atomic additions: exact, so that their order does not matter.  (Additions of 64 bits in shared memory are loops: 256 rows of 128000, top-p 384 -> 505 us.)
+__device__ __forceinline__ void add_to(Histogram& h, uint32_t bin, u64 w) {
   const uint32_t l = (uint32_t)w, old = atomicAdd(&h.lo[bin], l), carry = old + l < old;
   const uint32_t up = (uint32_t)(w >> 32) + carry;
   if (up) atomicAdd(&h.hi[bin], up);
@@ -74,34 +96,29 @@ constexpr int EXP_TABLE = 256;
 struct Weights {
   const double* table;
   double top, scale;             // largest score; 256 log2(e) / T
-  float topf, half_top, twice;   // largest score, half of it; 2 / T
+  float topf, half_top, far;     // largest score, half of it; half a distance that leaves no weight to speak of
   int bits;
-  __device__ __forceinline__ double fraction(float x, int& n) const {      // of 2^n
+  bool infinite;
+  // Whether x has any weight to speak of: 2^-54 and less is none in these units.
+  __device__ __forceinline__ bool any(float x) const { return fmaf(-0.5f, x, half_top) < far; }
+  // Without branches, so that a vector's are worked out side by side.  (An infinite largest score takes all of it.)
+  __device__ __forceinline__ u64 operator()(float x) const {
     const double ROUND = 6755399441055744.0;                                  // 1.5 * 2^52: the sum's low word is k
     const double z = ((double)x - top) * scale, kd = z + ROUND;
     const int k = __double2loint(kd);
-    const double f = (z - (kd - ROUND)) * (0.693147180559945309417 / 256.0);
+    const double f = (z - (kd - ROUND)) * (0.693147180559945309417 / 256.0), t = table[k & (EXP_TABLE - 1)];
     double e = fma(f, 1.0 / 24.0, 1.0 / 6.0);
     e = fma(f, e, 0.5);
     e = fma(f, e, 1.0);
-    const double t = table[k & (EXP_TABLE - 1)];
-    n = k >> 8;
-    return fma(t * f, e, t);
-  }
-  // Whether x has any weight to speak of: 2^-54 and less is none in these units.  (An infinite largest score takes all of it.)
-  __device__ __forceinline__ bool any(float x) const { return fmaf(-0.5f, x, half_top) * twice < 38.f; }
-  __device__ __forceinline__ u64 operator()(float x) const {
-    if (x == topf) return 1ull << bits;
-    if (!any(x)) return 0;
-    int n;
-    const double e = fraction(x, n);
-    const double w = __hiloint2double(__double2hiint(e) + ((n + bits) << 20), __double2loint(e)) + 4503599627370496.0;      // (2^52: the sum's low bits are w, rounded)
-    return (u64)__double_as_longlong(w) & 0xfffffffffffffull;
+    e = fma(t * f, e, t);
+    const double w = __hiloint2double(__double2hiint(e) + (((k >> 8) + bits) << 20), __double2loint(e)) + 4503599627370496.0;      // (2^52: the sum's low bits are w, rounded)
+    const u64 u = (u64)__double_as_longlong(w) & 0xfffffffffffffull;
+    return infinite ? (x == topf ? 1ull << bits : 0ull) : any(x) ? u : 0ull;
   }
   // w(x) >= least, in FP64
   __device__ __forceinline__ bool reaches(float x, double least) const {
     if (x == topf) return 1.0 >= least;
-    if (isinf(topf) || x == -INFINITY) return 0.0 >= least;
+    if (infinite || x == -INFINITY) return 0.0 >= least;
     return exp(((double)x - top) * (scale * (0.693147180559945309417 / 256.0))) >= least;
   }
 };
@@ -127,9 +144,8 @@ sample_kernel(Params p) {
   __shared__ double s_table[EXP_TABLE];
   __shared__ float s_top[MAX_CLUSTER];
   __shared__ u64 s_warp[WARPS], s_scan[WARPS], s_cta[1];
-  __shared__ uint32_t s_scan_n[WARPS];
   __shared__ Found s_found, s_best[MAX_CLUSTER];
-  __shared__ u64 s_chunk[2][MAX_CLUSTER];
+  __shared__ u64 s_chunk[MAX_CLUSTER];
   __shared__ Border s_border;
   __shared__ int s_n;
   Histogram& s_h = s_u.h;
@@ -152,42 +168,34 @@ sample_kernel(Params p) {
   // ---- places: the warp's g0 .. g1 - 1, of the CTA's c0 ..; scores at shift .. end - 1 ----
   const int shift = (int)(reinterpret_cast<uintptr_t>(row) / sizeof(T) % VEC), end = p.vocab + shift;
   const int each = p.each, c0 = rank * WARPS * each, g0 = c0 + warp * each, g1 = min(g0 + each, (end + VEC - 1) / VEC * VEC);
-  auto fetch = [&](int g, T (&x)[VEC]) {                       // VEC scores from memory, -inf where there are none
-    if (g >= shift && g + VEC <= end) {
-      const uint4 v = *reinterpret_cast<const uint4*>(row + (g - shift));
-      *reinterpret_cast<uint4*>(x) = v;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) x[j] = clean(x[j]);
-    } else {
+  const uint32_t nothing = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;      // -inf
+  auto fetch = [&](int g) {                                    // VEC scores from memory, -inf where there are none
+    uint4 v;
+    const bool inside = g >= shift && g + VEC <= end;
+    if (inside) v = *reinterpret_cast<const uint4*>(row + (g - shift));
+    if (!inside || has_nan(v, T())) {
+      T x[VEC];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) x[j] = g + j >= shift && g + j < end ? clean(row[g + j - shift]) : from_f32<T>(-INFINITY);
+      v = *reinterpret_cast<const uint4*>(x);
     }
+    return v;
   };
   // calls f(place of the first, VEC scores) by all lanes of the warp alike: lanes beyond the end get -inf
   auto sweep = [&](auto f) {
     for (int i0 = g0; i0 < g1; i0 += 32 * VEC) {
       const int g = i0 + lane * VEC;
-      T x[VEC];
-      if (g >= g1) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) x[j] = from_f32<T>(-INFINITY);
-      } else if (KEPT) {
-        *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(s_x + (g - c0));
-      } else {
-        fetch(g, x);
-      }
-      f(g, x);
+      f(g, g >= g1 ? make_uint4(nothing, nothing, nothing, nothing) : KEPT ? *reinterpret_cast<const uint4*>(s_x + (g - c0)) : fetch(g));
     }
   };
   float top = -INFINITY;
 #pragma unroll 4
   for (int g = g0 + lane * VEC; g < g1; g += 32 * VEC) {
-    T x[VEC];
-    fetch(g, x);
-    if (KEPT) *reinterpret_cast<uint4*>(s_x + (g - c0)) = *reinterpret_cast<const uint4*>(x);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) top = fmaxf(top, to_f32(x[j]));
+    const uint4 v = fetch(g);
+    if (KEPT) *reinterpret_cast<uint4*>(s_x + (g - c0)) = v;
+    top = fmaxf(top, largest(v, T()));
   }
+  const float my_top = top;                                    // the thread's own
 #pragma unroll
   for (int w = 16; w; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
   if (lane == 0) s_warp[warp] = __float_as_uint(top);
@@ -209,7 +217,7 @@ sample_kernel(Params p) {
     }
     return;
   }
-  const Weights weight = {s_table, (double)top, inv_t * (256.0 / 0.693147180559945309417), top, 0.5f * top, (float)(2.0 * inv_t), p.scale_bits};
+  const Weights weight = {s_table, (double)top, inv_t * (256.0 / 0.693147180559945309417), top, 0.5f * top, (float)(19.0 / inv_t), p.scale_bits, isinf(top) != 0};
   const double unit = ldexp(1.0, p.scale_bits);
 
   // ---- sums over the cluster in the order of its warps: of x (alike in all lanes of a warp), in front of this warp, and all ----
@@ -240,22 +248,20 @@ sample_kernel(Params p) {
     return x;
   };
   // sums over the CTA in the order of its threads, in front of this one, and all
-  auto cta_scan = [&](uint32_t n, u64 x, u64& front_n, u64& front, u64& all_n, u64& all) {
-    u64 run_n = n, run = x;
+  auto cta_scan = [&](u64 x, u64& front, u64& all) {
+    u64 run = x;
 #pragma unroll
     for (int w = 1; w < 32; w <<= 1) {
-      const u64 a = __shfl_up_sync(0xffffffffu, run_n, w), b = __shfl_up_sync(0xffffffffu, run, w);
-      if (lane >= w) { run_n += a; run += b; }
+      const u64 y = __shfl_up_sync(0xffffffffu, run, w);
+      if (lane >= w) run += y;
     }
     __syncthreads();
-    if (lane == 31) { s_scan_n[warp] = (uint32_t)run_n; s_scan[warp] = run; }
+    if (lane == 31) s_scan[warp] = run;
     __syncthreads();
-    front_n = run_n - n;
     front = run - x;
-    all_n = all = 0;
+    all = 0;
     for (int w = 0; w < WARPS; ++w) {
-      if (w < warp) { front_n += s_scan_n[w]; front += s_scan[w]; }
-      all_n += s_scan_n[w];
+      if (w < warp) front += s_scan[w];
       all += s_scan[w];
     }
   };
@@ -274,57 +280,46 @@ sample_kernel(Params p) {
     while (t < n && (double)(front + t * w) < goal) ++t;
     return t;
   };
-  // Digit by digit of the key: any number of ties, and as many rounds as digits.
+  // Digit by digit of the key: any number of ties, and as many rounds as digits.  Counts scores, or (by_mass) their weight.
   auto search_digits = [&](bool by_mass, double share, u64 k) {
     uint32_t prefix = 0;
     int above = Key<T>::BITS;                                  // bits below which the digit lies
-    u64 in_front_n = 0, in_front = 0;
+    u64 in_front = 0;
     double goal = 0.0;
     Found f;
     while (above > 0) {
       const int bits = min(DIGIT, above), shr = above - bits;
-      for (int i = tid; i < BINS; i += THREADS) s_h.n[i] = s_h.lo[i] = s_h.hi[i] = 0;
+      for (int i = tid; i < BINS; i += THREADS) s_h.lo[i] = s_h.hi[i] = 0;
       __syncthreads();
       const bool first_level = above == Key<T>::BITS;
-      sweep([&](int g, const T (&x)[VEC]) {
+      sweep([&](int g, uint4 v) {
+        float x[VEC];
+        unpack(v, x);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          const float xf = to_f32(x[j]);
-          const uint32_t key = Key<T>::of(xf);
-          if ((first_level || key >> above == prefix) && xf > from_x) {
-            const uint32_t bin = key >> shr & ((1u << bits) - 1u);
-            atomicAdd(&s_h.n[bin], 1u);
-            if (by_mass) add_mass(s_h, bin, weight(xf));
-          }
+          const uint32_t key = Key<T>::of(x[j]);
+          if ((first_level || key >> above == prefix) && x[j] > from_x) add_to(s_h, key >> shr & ((1u << bits) - 1u), by_mass ? weight(x[j]) : 1ull);
         }
       });
-      if (from_n != 0 && rank == 0 && tid == 0 && (first_level || from >> above == prefix)) {     // ties at the border found before: as many as were kept
-        const uint32_t bin = from >> shr & ((1u << bits) - 1u);
-        atomicAdd(&s_h.n[bin], from_n);
-        if (by_mass) add_mass(s_h, bin, weight(from_x) * from_n);
-      }
+      if (from_n != 0 && rank == 0 && tid == 0 && (first_level || from >> above == prefix))      // ties at the border found before: as many as were kept
+        add_to(s_h, from >> shr & ((1u << bits) - 1u), by_mass ? weight(from_x) * from_n : from_n);
       cluster.sync();
       // a thread's bins, from the last one on
-      uint32_t n[PER], sum_n = 0;
-      u64 mass[PER], sum = 0;
+      u64 amount[PER], sum = 0;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int bin = BINS - 1 - (tid * PER + i);
-        n[i] = 0;
-        mass[i] = 0;
+        amount[i] = 0;
         for (int j = 0; j < size; ++j) {
           const Histogram* h = cluster.map_shared_rank(&s_h, j);
-          n[i] += h->n[bin];
-          if (by_mass) mass[i] += ((u64)h->hi[bin] << 32) + h->lo[bin];
+          amount[i] += ((u64)h->hi[bin] << 32) + h->lo[bin];
         }
-        sum_n += n[i];
-        sum += mass[i];
+        sum += amount[i];
       }
-      u64 front_n, front, all_n, all;
-      cta_scan(sum_n, sum, front_n, front, all_n, all);
-      front_n += in_front_n;
+      u64 front, all;
+      cta_scan(sum, front, all);
       front += in_front;
-      if (first_level) goal = share * (double)all;
+      if (first_level) goal = by_mass ? share * (double)all : (double)k;
       // the last bin that has any, and in front of which there is less than the goal (the first one in any case)
       if (tid == 0) s_found.bin = BINS;
       __syncthreads();
@@ -333,80 +328,83 @@ sample_kernel(Params p) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int bin = BINS - 1 - (tid * PER + i);
-        if (n[i] > 0 && (by_mass ? front_n == 0 || (double)front < goal : front_n < k)) {
+        if (amount[i] > 0 && (front == 0 || (double)front < goal)) {
           best = bin;
-          mine = Found{bin, n[i], front_n, front, mass[i]};
+          mine = Found{bin, front, amount[i]};
         }
-        front_n += n[i];
-        front += mass[i];
+        front += amount[i];
       }
       if (best < BINS) atomicMin(&s_found.bin, best);
       __syncthreads();
       if (best < BINS && s_found.bin == best) s_found = mine;
       __syncthreads();
       f = s_found;
-      in_front_n = f.in_front_n;
       in_front = f.in_front;
       prefix = prefix << bits | (uint32_t)f.bin;
       above = shr;
       cluster.sync();                                          // (histograms have been read)
     }
-    const u64 t = by_mass ? ties_below(f.n, f.mass / f.n, in_front, goal) : min((u64)f.n, k - in_front_n);
-    return Border{prefix, (uint32_t)t, f.n};
+    const u64 w = by_mass ? weight(score_of<T>(prefix)) : 1, n = w ? f.amount / w : f.amount;
+    return Border{prefix, (uint32_t)(by_mass ? ties_below(n, w, in_front, goal) : min(n, k - in_front)), (uint32_t)n};
   };
-  auto search = [&](bool by_mass, double share, u64 k) {
-    for (int i = tid; i < BINS; i += THREADS) s_h.n[i] = s_h.lo[i] = s_h.hi[i] = 0;
+  // few: of the threads' own largest scores instead of all, whose k-th lies no higher than the k-th of all; what is in its bin and in front of it is put in order.
+  auto search = [&](bool by_mass, double share, u64 k, bool few) {
+    for (int i = tid; i < BINS; i += THREADS) s_h.lo[i] = s_h.hi[i] = 0;
     __syncthreads();
-    sweep([&](int g, const T (&x)[VEC]) {
+    if (few) {
+      if (my_top > from_x) atomicAdd(&s_h.lo[bin_of(top, my_top)], 1u);
+    } else if (__any_sync(0xffffffffu, my_top > from_x)) {
+      sweep([&](int g, uint4 v) {
+        if (!__any_sync(0xffffffffu, largest(v, T()) > from_x)) return;
+        float x[VEC];
+        unpack(v, x);
+        if (by_mass) {
+          u64 w[VEC];
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float xf = to_f32(x[j]);
-        if (xf > from_x) {
-          const int bin = bin_of(top, xf);
-          atomicAdd(&s_h.n[bin], 1u);
-          if (by_mass) add_mass(s_h, bin, weight(xf));
+          for (int j = 0; j < VEC; ++j) w[j] = weight(x[j]);
+#pragma unroll
+          for (int j = 0; j < VEC; ++j)
+            if (x[j] > from_x) add_to(s_h, bin_of(top, x[j]), w[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < VEC; ++j)
+            if (x[j] > from_x) atomicAdd(&s_h.lo[bin_of(top, x[j])], 1u);
         }
-      }
-    });
+      });
+    }
     const u64 from_w = from_n != 0 && by_mass ? weight(from_x) : 0;
     const int from_bin = from_n != 0 ? bin_of(top, from_x) : -1;
-    if (from_n != 0 && rank == 0 && tid == 0) {                  // ties at the border found before: as many as were kept
-      atomicAdd(&s_h.n[from_bin], from_n);
-      if (by_mass) add_mass(s_h, from_bin, from_w * from_n);
-    }
+    if (from_n != 0 && rank == 0 && tid == 0) add_to(s_h, from_bin, by_mass ? from_w * from_n : from_n);      // ties at the border found before: as many as were kept
     cluster.sync();
     // every CTA adds up its part of the bins, a few a thread
     const int chunk = BINS / size, per = max(1, chunk / THREADS), b0 = rank * chunk + tid * per;
-    uint32_t n[PER], sum_n = 0;
-    u64 mass[PER], sum = 0;
+    u64 amount[PER], sum = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      n[i] = 0;
-      mass[i] = 0;
+      amount[i] = 0;
       if (i < per && tid * per < chunk)
         for (int j = 0; j < size; ++j) {
           const Histogram* h = cluster.map_shared_rank(&s_h, j);
-          n[i] += h->n[b0 + i];
-          if (by_mass) mass[i] += ((u64)h->hi[b0 + i] << 32) + h->lo[b0 + i];
+          amount[i] += ((u64)h->hi[b0 + i] << 32) + h->lo[b0 + i];
         }
-      sum_n += n[i];
-      sum += mass[i];
+      sum += amount[i];
     }
-    u64 front_n, front, all_n, all;
-    cta_scan(sum_n, sum, front_n, front, all_n, all);
+    u64 front, all;
+    cta_scan(sum, front, all);
     if (size > 1) {
-      if (tid < size) {
-        cluster.map_shared_rank(&s_chunk[0][0], tid)[rank] = all_n;
-        cluster.map_shared_rank(&s_chunk[1][0], tid)[rank] = all;
-      }
+      if (tid < size) cluster.map_shared_rank(s_chunk, tid)[rank] = all;
       cluster.sync();
       all = 0;
       for (int j = 0; j < size; ++j) {
-        if (j < rank) { front_n += s_chunk[0][j]; front += s_chunk[1][j]; }
-        all += s_chunk[1][j];
+        if (j < rank) front += s_chunk[j];
+        all += s_chunk[j];
       }
     }
-    const double goal = share * (double)all;
+    if (few && all < k) {                                      // (not so many threads have scores)
+      cluster.sync();
+      return Border{0, 0, 0};
+    }
+    const double goal = by_mass ? share * (double)all : (double)k;
     // the last bin that has any, and in front of which there is less than the goal (the first one in any case)
     if (tid == 0) s_found.bin = -1;
     __syncthreads();
@@ -415,12 +413,11 @@ sample_kernel(Params p) {
     mine.bin = -1;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if (n[i] > 0 && (by_mass ? front_n == 0 || (double)front < goal : front_n < k)) {
+      if (amount[i] > 0 && (front == 0 || (double)front < goal)) {
         best = b0 + i;
-        mine = Found{best, n[i], front_n, front, mass[i]};
+        mine = Found{best, front, amount[i]};
       }
-      front_n += n[i];
-      front += mass[i];
+      front += amount[i];
     }
     if (best >= 0) atomicMax(&s_found.bin, best);
     __syncthreads();
@@ -434,56 +431,74 @@ sample_kernel(Params p) {
       for (int j = 0; j < size; ++j)
         if (s_best[j].bin >= f.bin) f = s_best[j];
     }
-    if (f.n > LIST) {
-      cluster.sync();                                          // (histograms and what was found have been read)
-      return search_digits(by_mass, share, k);
-    }
+    if (few) f.in_front = 0;
     // the bin's scores, with their ids, to the first CTA: in ascending order of (keys from the largest on, ids)
     int* counter = cluster.map_shared_rank(&s_n, 0);
     u64* list = cluster.map_shared_rank(s_u.list, 0);
-    sweep([&](int g, const T (&x)[VEC]) {
+    if (__any_sync(0xffffffffu, my_top > from_x && bin_of(top, my_top) <= f.bin)) {
+      sweep([&](int g, uint4 v) {
+        const float most = largest(v, T());
+        if (!(most > from_x) || bin_of(top, most) > f.bin) return;
+        float x[VEC];
+        unpack(v, x);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float xf = to_f32(x[j]);
-        if (xf > from_x && bin_of(top, xf) == f.bin) list[atomicAdd(counter, 1)] = (u64)~Key<T>::of(xf) << 32 | (uint32_t)(g + j - shift);
-      }
-    });
+        for (int j = 0; j < VEC; ++j) {
+          const int bin = bin_of(top, x[j]);
+          if (x[j] > from_x && (few ? bin <= f.bin : bin == f.bin)) {
+            const int at = atomicAdd(counter, 1);
+            if (at < LIST) list[at] = (u64)~Key<T>::of(x[j]) << 32 | (uint32_t)(g + j - shift);
+          }
+        }
+      });
+    }
     cluster.sync();
+    if (*counter > LIST) {
+      cluster.sync();                                          // (has been read)
+      return few ? Border{0, 0, 0} : search_digits(by_mass, share, k);
+    }
     if (rank == 0) {
       const int have = s_n;
       int n2 = 2;
       while (n2 < have) n2 <<= 1;
-      for (int i = have + tid; i < n2; i += THREADS) s_u.list[i] = ~0ull;
-      __syncthreads();
-      for (int a = 2; a <= n2; a <<= 1)
-        for (int b = a >> 1; b; b >>= 1) {
-          for (int i = tid; i < n2 / 2; i += THREADS) {
-            const int lo = (i & (b - 1)) | (i & ~(b - 1)) << 1, hi = lo | b;
-            const u64 x = s_u.list[lo], y = s_u.list[hi];
-            if ((x > y) == ((lo & a) == 0)) { s_u.list[lo] = y; s_u.list[hi] = x; }
+      if (have <= THREADS) {                                   // a thread an entry: its place is the number of those in front of it
+        const u64 x = tid < have ? s_u.list[tid] : 0;
+        int place = 0;
+#pragma unroll 4
+        for (int i = 0; i < have; ++i) place += s_u.list[i] < x;
+        __syncthreads();
+        if (tid < have) s_u.list[place] = x;
+        __syncthreads();
+      } else {
+        for (int i = have + tid; i < n2; i += THREADS) s_u.list[i] = ~0ull;
+        __syncthreads();
+        for (int a = 2; a <= n2; a <<= 1)
+          for (int b = a >> 1; b; b >>= 1) {
+            for (int i = tid; i < n2 / 2; i += THREADS) {
+              const int lo = (i & (b - 1)) | (i & ~(b - 1)) << 1, hi = lo | b;
+              const u64 x = s_u.list[lo], y = s_u.list[hi];
+              if ((x > y) == ((lo & a) == 0)) { s_u.list[lo] = y; s_u.list[hi] = x; }
+            }
+            __syncthreads();
           }
-          __syncthreads();
-        }
+      }
       auto key_at = [&](int i) { return ~(uint32_t)(s_u.list[i] >> 32); };
       // how many of them, in order, are kept
       int kept;
       u64 inside = 0;                                          // weight of all of them
       if (by_mass) {
         const int per_thread = (n2 + THREADS - 1) / THREADS, i0 = tid * per_thread;
-        u64 w = 0, unused_n, before, unused;
+        u64 w = 0, before, unused;
         for (int i = i0; i < min(i0 + per_thread, have); ++i) w += weight(score_of<T>(key_at(i)));
-        cta_scan(0, w, unused_n, before, unused, inside);
-        uint32_t below_goal = 0;
-        u64 run = f.in_front + before;
+        cta_scan(w, before, inside);
+        u64 below_goal = 0, run = f.in_front + before, total;
         for (int i = i0; i < min(i0 + per_thread, have); ++i) {
-          below_goal += (i == 0 && f.in_front_n == 0) || (double)run < goal;
+          below_goal += (i == 0 && f.in_front == 0) || (double)run < goal;
           run += weight(score_of<T>(key_at(i)));
         }
-        u64 a, b, total;
-        cta_scan(below_goal, 0, a, b, total, unused);
+        cta_scan(below_goal, unused, total);
         kept = (int)total;
       } else {
-        kept = (int)min((u64)have, k - f.in_front_n);
+        kept = (int)min((u64)have, k - f.in_front);
       }
       if (tid == 0) {
         Border x;
@@ -509,15 +524,18 @@ sample_kernel(Params p) {
     return s_border;
   };
   Border border = {from, 0, 0};                               // (all above -inf)
+  const bool few = top_k <= min(size * THREADS / 2, LIST / 4);
   if (by_k) {
-    border = search(false, 0.0, (u64)top_k);
+    // (half of the threads at most: their largest scores must be enough of them, and not all)
+    border = search(false, 0.0, (u64)top_k, few);
+    if (border.ties == 0) border = search(false, 0.0, (u64)top_k, false);
     from = border.key;
     from_n = border.kept;
     from_x = score_of<T>(from);
   }
   if (by_p) {
     const uint32_t ties = border.ties;
-    border = search(true, (double)top_p, 0);
+    border = search(true, (double)top_p, 0, false);
     if (by_k && border.key == from) border.ties = ties;        // (of those at the border before, some more go)
   }
 
@@ -527,9 +545,11 @@ sample_kernel(Params p) {
   u64 tie_rank = 0;
   if (some_ties) {
     u64 mine = 0;
-    sweep([&](int g, const T (&x)[VEC]) {
+    sweep([&](int g, uint4 v) {
+      float x[VEC];
+      unpack(v, x);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) mine += to_f32(x[j]) == border_x;
+      for (int j = 0; j < VEC; ++j) mine += x[j] == border_x;
     });
     cluster_sum(warp_sum(mine), tie_rank);
   }
@@ -542,13 +562,19 @@ sample_kernel(Params p) {
     never = (float)((double)top - away - slack);
   }
   // Weights of VEC scores, 0 where they go, and which stay; `at`: ties in front of the warp's first.
-  auto keep = [&](int g, const T (&x)[VEC], u64& at, u64 (&w)[VEC]) {
+  const float low = fmaxf(border_x, never);                    // below it nothing stays
+  auto keep = [&](uint4 v, u64& at, u64 (&w)[VEC]) {
     uint32_t stay = 0, tie = 0;
 #pragma unroll
+    for (int j = 0; j < VEC; ++j) w[j] = 0;
+    const float most = largest(v, T());
+    if (!__any_sync(0xffffffffu, most >= low && most > -INFINITY)) return stay;
+    float x[VEC];
+    unpack(v, x);
+#pragma unroll
     for (int j = 0; j < VEC; ++j) {
-      const float xf = to_f32(x[j]);
-      if (xf > border_x) stay |= 1u << j;
-      if (xf == border_x) tie |= 1u << j;
+      if (x[j] > border_x) stay |= 1u << j;
+      if (x[j] == border_x) tie |= 1u << j;
     }
     if (by_k || by_p) stay |= tie;                              // (else the border is -inf)
     if (some_ties) {
@@ -568,35 +594,45 @@ sample_kernel(Params p) {
     if (least > 0.0) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float xf = to_f32(x[j]);
         // clear of the border by far, or worked out
-        if ((stay >> j & 1u) && !(xf > sure) && (xf < never || !weight.reaches(xf, least))) stay &= ~(1u << j);
+        if ((stay >> j & 1u) && !(x[j] > sure) && (x[j] < never || !weight.reaches(x[j], least))) stay &= ~(1u << j);
       }
     }
+    if (__any_sync(0xffffffffu, stay != 0)) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) w[j] = stay >> j & 1u ? weight(to_f32(x[j])) : 0;
+      for (int j = 0; j < VEC; ++j) {
+        const u64 u = weight(x[j]);
+        w[j] = stay >> j & 1u ? u : 0;
+      }
+    }
     return stay;
   };
   const bool aligned_out = out && reinterpret_cast<uintptr_t>(out) / sizeof(T) % VEC == (unsigned)shift;
   u64 mine = 0, before, at = tie_rank;
-  sweep([&](int g, const T (&x)[VEC]) {
-    u64 w[VEC];
-    const uint32_t stay = keep(g, x, at, w);
+  if (out || __any_sync(0xffffffffu, my_top >= low))
+    sweep([&](int g, uint4 v) {
+      u64 w[VEC];
+      const uint32_t stay = keep(v, at, w);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) mine += w[j];
-    if (out && g < g1) {
-      T y[VEC];
+      for (int j = 0; j < VEC; ++j) mine += w[j];
+      if (out && g < g1) {
+        uint4 y = make_uint4(nothing, nothing, nothing, nothing);
+        if (stay) {
+          const T* x = reinterpret_cast<const T*>(&v);
+          T z[VEC];
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) y[j] = stay >> j & 1u ? x[j] : from_f32<T>(-INFINITY);
-      if (aligned_out && g >= shift && g + VEC <= end) {
-        __stcs(reinterpret_cast<uint4*>(out + (g - shift)), *reinterpret_cast<const uint4*>(y));
-      } else {
+          for (int j = 0; j < VEC; ++j) z[j] = stay >> j & 1u ? x[j] : from_f32<T>(-INFINITY);
+          y = *reinterpret_cast<const uint4*>(z);
+        }
+        if (aligned_out && g >= shift && g + VEC <= end) {
+          __stcs(reinterpret_cast<uint4*>(out + (g - shift)), y);
+        } else {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j)
-          if (g + j >= shift && g + j < end) out[g + j - shift] = y[j];
+          for (int j = 0; j < VEC; ++j)
+            if (g + j >= shift && g + j < end) out[g + j - shift] = reinterpret_cast<const T*>(&y)[j];
+        }
       }
-    }
-  });
+    });
   mine = warp_sum(mine);
   const u64 all = cluster_sum(mine, before);
   const double goal = fmax((double)r, 0.0) * (double)all;
@@ -608,14 +644,16 @@ sample_kernel(Params p) {
     at = tie_rank;
     bool done = false;
     // (without KEPT, scores may have been overwritten by what is left of them: those that went are -inf, and the others, ties among them, all stay)
-    sweep([&](int g, const T (&x)[VEC]) {
+    sweep([&](int g, uint4 v) {
       if (done) return;
+      float x[VEC];
+      unpack(v, x);
       u64 w[VEC], sum = 0;
       if (!KEPT && out == row) {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) w[j] = weight(to_f32(x[j]));
+        for (int j = 0; j < VEC; ++j) w[j] = weight(x[j]);
       } else {
-        keep(g, x, at, w);
+        keep(v, at, w);
       }
 #pragma unroll
       for (int j = 0; j < VEC; ++j) sum += w[j];
@@ -636,7 +674,7 @@ sample_kernel(Params p) {
 #pragma unroll
           for (int j = 0; j < VEC; ++j) {
             y += w[j];
-            if (token < 0 && w[j] > 0 && passes(y)) { token = g + j - shift; x_of = to_f32(x[j]); }
+            if (token < 0 && w[j] > 0 && passes(y)) { token = g + j - shift; x_of = x[j]; }
           }
           p.tokens[m] = token;
           if (p.logp) p.logp[m] = (float)((x_of == top ? 0.0 : ((double)x_of - (double)top) * inv_t) - log((double)all / unit));
