@@ -400,11 +400,13 @@ int ad_accept_sampled(const void* target, int64_t target_stride, const void* dra
                       void* scratch, size_t scratch_bytes, int32_t* status, void* stream);
 
 /* Attention over the cache for batches whose rows share prefixes.  The rows group[g] .. group[g + 1] - 1 (group [G + 1], device, ascending from 0 to B) hold
- * the same keys and values in their first shared[g] positions (shared [G], device; 0: nothing shared; no row of the group sees fewer), as rows do that
- * ad_cache_fork made from one, or that look at one encoder's keys.  These positions are read once for the group, through the table of its first row, whatever
- * the others' tables say there.  Otherwise arguments, result and precision are those of ad_cache_attention.  max_shared: longest prefix to plan for.
- * A group that does not lie in ascending order within 0 .. B, or with shared[g] below 0 or beyond the row's capacity, latches AD_ERR_ARG and its rows come out as zeros;
- * a row that sees fewer than shared[g] positions latches AD_ERR_ARG and is left out.  At most 8192 rows. */
+ * the same keys and values in their first shared[g] positions (shared [G], device; 0: nothing shared; at most len[b] of every row that brings tokens), as rows do
+ * that ad_cache_fork made from one, or that look at one encoder's keys.  The whole blocks among these positions may be read once for the group, through the table of its
+ * first row (which then must name them, whether or not that row brings tokens); the rest is read through each row's own table, which must be in order
+ * throughout.  Whether they are is decided by the sizes that the host gives, by what it saves; the result differs by roundings alone.  Otherwise arguments, result and
+ * precision are those of ad_cache_attention.  max_shared: longest prefix to plan for; longer ones are computed as well, only slower.  Where positions are read once,
+ * rows of a group that does not lie in ascending order within 0 .. B, or with shared[g] below 0 or beyond a row's capacity, and rows with fewer than shared[g]
+ * positions latch AD_ERR_ARG and are left out; where they are not, groups are not looked at.  At most 8192 rows, and M * n_heads at most 2^30. */
 size_t ad_cache_attention_shared_scratch_bytes(const ad_kv_cache* cache, int32_t dtype, int32_t n_heads, int32_t B, int32_t M, int32_t max_new,
                                                int32_t max_keys, int32_t G, int32_t max_shared);
 int ad_cache_attention_shared(const ad_kv_cache* cache, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
