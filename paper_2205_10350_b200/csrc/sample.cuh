@@ -81,16 +81,26 @@ template <typename T> __device__ __forceinline__ float score_of(uint32_t key) {
 struct Histogram { uint32_t lo[BINS], hi[BINS]; };
 struct Found { int bin; u64 in_front, amount; };       // of scores, or of weight
 // BF16 numbers from the largest on, one to a bin: the 16 octaves up to the largest magnitude that has any weight, 128 numbers each, of either sign.  The first bin of either
-// sign holds all smaller magnitudes as well.
+// sign holds all smaller magnitudes instead.  In shared memory a number that has a bin lies at its bits' distance from `first`, those of either sign in a half of their own; the last
+// place of either half belongs to the first number without weight.
 struct Values {
-  int base;                      // bits of the smallest magnitude
-  // 0 and less: shares its bin; HALF and more: has no weight
-  __device__ __forceinline__ int place(float x) const { return (int)(__float_as_uint(x) >> 16 & 0x7fffu) - base; }
-  __device__ __forceinline__ int bin(float x, int place) const { return x < 0.f ? HALF + place : HALF - 1 - place; }
-  __device__ __forceinline__ int bin(float x) const { return bin(x, min(max(place(x), 0), HALF - 1)); }
-  __device__ __forceinline__ bool shared(int b) const { return b == HALF || b == HALF - 1; }
-  __device__ __forceinline__ float value(int b) const { return __uint_as_float((uint32_t)(base + (b < HALF ? HALF - 1 - b : b - HALF)) << 16 | (b < HALF ? 0u : 0x80000000u)); }
+  int first;                     // bits of the smallest magnitude that has a bin
+  __device__ __forceinline__ int distance(uint32_t bits) const { return (int)bits - first; }                   // of a score's 16 bits
+  static __device__ __forceinline__ bool outside(int distance) { return (distance & 0x7800) != 0; }            // (of several at once, too: their bits together)
+  static __device__ __forceinline__ int at(int distance) { return (distance & 0x7ff) | (distance >> 4 & 0x800); }
+  __device__ __forceinline__ float value(int at) const { return __uint_as_float((uint32_t)((at & (HALF - 1)) + first + (at >= HALF ? 0x8000 : 0)) << 16); }
+  // bins, and where they lie
+  __device__ __forceinline__ int bin(float x) const {
+    const int place = min(max((int)(__float_as_uint(x) >> 16 & 0x7fffu) - first + 1, 0), HALF - 1);
+    return x < 0.f ? HALF + place : HALF - 1 - place;
+  }
+  static __device__ __forceinline__ bool small(int bin) { return bin == HALF || bin == HALF - 1; }
+  static __device__ __forceinline__ int at_bin(int bin) { return bin < HALF ? HALF - 2 - bin : bin - 1; }
 };
+__device__ __forceinline__ uint32_t score_bits(uint4 v, int j) {      // BF16's
+  const uint32_t w = j < 2 ? v.x : j < 4 ? v.y : j < 6 ? v.z : v.w;
+  return j & 1 ? w >> 16 : w & 0xffffu;
+}
 struct Border { uint32_t key, kept, ties; };      // scores above this key stay, and of those that have it, `ties`, the first `kept`
 
 // 64-bit sums from 32-bit atomic additions: exact, so that their order does not matter.  (Additions of 64 bits in shared memory are loops: 256 rows of 128000, top-p 384 -> 505 us.)
@@ -156,7 +166,7 @@ sample_kernel(Params p) {
   __shared__ uint32_t s_small[2][2];                         // weight of small magnitudes of either sign, in halves
   __shared__ double s_table[EXP_TABLE];
   __shared__ float s_top[MAX_CLUSTER];
-  __shared__ u64 s_warp[WARPS], s_scan[WARPS], s_cta[1];
+  __shared__ u64 s_warp[WARPS], s_scan[WARPS], s_sum[2][MAX_CLUSTER];
   __shared__ Found s_found, s_best[MAX_CLUSTER];
   __shared__ u64 s_chunk[MAX_CLUSTER];
   __shared__ Border s_border;
@@ -165,6 +175,7 @@ sample_kernel(Params p) {
   T* s_x = reinterpret_cast<T*>(s_raw);
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = cluster.block_rank(), size = cluster.num_blocks(), m = blockIdx.x / size, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // (waited for before any other CTA's shared memory is written)
   pdl_launch();
   if (tid < EXP_TABLE) s_table[tid] = exp2(tid / (double)EXP_TABLE);
   pdl_wait();
@@ -212,8 +223,12 @@ sample_kernel(Params p) {
 #pragma unroll
   for (int w = 16; w; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
   if (lane == 0) s_warp[warp] = __float_as_uint(top);
-  cluster.sync();                                            // (all CTAs run: their shared memory may be written)
-  for (int w = 0; w < WARPS; ++w) top = fmaxf(top, __uint_as_float((uint32_t)s_warp[w]));
+  __syncthreads();
+  top = lane < WARPS ? __uint_as_float((uint32_t)s_warp[lane]) : -INFINITY;
+#pragma unroll
+  for (int w = WARPS / 2; w; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+  top = __shfl_sync(0xffffffffu, top, 0);
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   if (size > 1) {
     if (tid < size) cluster.map_shared_rank(s_top, tid)[rank] = top;
     cluster.sync();
@@ -234,7 +249,7 @@ sample_kernel(Params p) {
   const double unit = ldexp(1.0, p.scale_bits);
 
   // ---- sums over the cluster in the order of its warps: of x (alike in all lanes of a warp), in front of this warp, and all ----
-  auto cluster_sum = [&](u64 x, u64& before) {
+  auto cluster_sum = [&](u64 x, u64& before, int which) {
     __syncthreads();
     if (lane == 0) s_warp[warp] = x;
     __syncthreads();
@@ -248,14 +263,13 @@ sample_kernel(Params p) {
     before = __shfl_sync(0xffffffffu, sum, (warp + 31) & 31);
     if (warp == 0) before = 0;
     if (size == 1) return mine;
-    if (tid == 0) s_cta[0] = mine;
+    if (tid < size) *cluster.map_shared_rank(&s_sum[which][rank], tid) = mine;
     cluster.sync();
     for (int j = 0; j < size; ++j) {
-      const u64 y = *cluster.map_shared_rank(&s_cta[0], j);
+      const u64 y = s_sum[which][j];
       if (j < rank) before += y;
       all += y;
     }
-    cluster.sync();
     return all;
   };
   auto warp_sum = [&](u64 x) {
@@ -292,7 +306,7 @@ sample_kernel(Params p) {
   Values values = {0};
   if (by_values) {
     const float bottom = fmaxf(top - 2.1f * weight.far, -FLT_MAX);
-    values.base = (max((int)(__float_as_uint(fmaxf(fabsf(top), fabsf(bottom))) >> 23), 15) - 15) << 7;
+    values.first = ((max((int)(__float_as_uint(fmaxf(fabsf(top), fabsf(bottom))) >> 23), 15) - 15) << 7) + 1;
   }
   uint32_t from = Key<T>::of(-INFINITY), from_n = 0;
   float from_x = -INFINITY;
@@ -393,13 +407,23 @@ sample_kernel(Params p) {
         float x[VEC];
         unpack(v, x);
         if (by_value) {
+          int d[VEC], any = 0;
 #pragma unroll
           for (int j = 0; j < VEC; ++j) {
-            const int at = values.place(x[j]);
-            if (x[j] > from_x && at < HALF) {
-              if (at > 0) atomicAdd(&s_u.count[values.bin(x[j], at)], 1u);
-              else small(x[j], 1);
-            }
+            d[j] = values.distance(score_bits(v, j));
+            any |= d[j];
+          }
+          if (!__any_sync(0xffffffffu, Values::outside(any))) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+              if (x[j] > from_x) atomicAdd(&s_u.count[Values::at(d[j])], 1u);
+          } else {
+#pragma unroll 1
+            for (int j = 0; j < VEC; ++j)
+              if (x[j] > from_x) {
+                if (!Values::outside(d[j])) atomicAdd(&s_u.count[Values::at(d[j])], 1u);
+                else if (weight.any(x[j])) small(x[j], 1);
+              }
           }
         } else if (by_mass) {
           u64 w[VEC];
@@ -419,8 +443,8 @@ sample_kernel(Params p) {
     const int from_bin = from_n == 0 ? -1 : by_value ? values.bin(from_x) : bin_of(top, from_x);
     if (from_n != 0 && rank == 0 && tid == 0) {                // ties at the border found before: as many as were kept
       if (!by_value) add_to(s_h, from_bin, by_mass ? from_w * from_n : from_n);
-      else if (values.shared(from_bin)) small(from_x, from_n);
-      else if (values.place(from_x) < HALF) atomicAdd(&s_u.count[from_bin], from_n);
+      else if (Values::small(from_bin)) small(from_x, from_n);
+      else if (const int d = values.distance(__float_as_uint(from_x) >> 16); !Values::outside(d)) atomicAdd(&s_u.count[Values::at(d)], from_n);
     }
     cluster.sync();
     // every CTA adds up its part of the bins, a few a thread
@@ -432,12 +456,12 @@ sample_kernel(Params p) {
       amount[i] = 0;
       if (i < per && tid * per < chunk) {
         if (by_value) {
-          const bool small_ones = values.shared(b0 + i);
+          const bool small_ones = Values::small(b0 + i);
           for (int j = 0; j < size; ++j) {
             const uint32_t* h = cluster.map_shared_rank(&s_small[b0 + i == HALF][0], j);
-            amount[i] += small_ones ? ((u64)h[1] << 32) + h[0] : cluster.map_shared_rank(s_u.count, j)[b0 + i];
+            amount[i] += small_ones ? ((u64)h[1] << 32) + h[0] : cluster.map_shared_rank(s_u.count, j)[Values::at_bin(b0 + i)];
           }
-          if (amount[i] && !small_ones) amount[i] *= weight(values.value(b0 + i));
+          if (amount[i] && !small_ones) amount[i] *= weight(values.value(Values::at_bin(b0 + i)));
         } else {
           for (int j = 0; j < size; ++j) {
             const Histogram* h = cluster.map_shared_rank(&s_h, j);
@@ -490,9 +514,9 @@ sample_kernel(Params p) {
         if (s_best[j].bin >= f.bin) f = s_best[j];
     }
     if (few) f.in_front = 0;
-    if (by_value && !values.shared(f.bin)) {                   // ties, all of them
+    if (by_value && !Values::small(f.bin)) {                   // ties, all of them
       if (tid == 0) {
-        const float x = values.value(f.bin);
+        const float x = values.value(Values::at_bin(f.bin));
         const u64 w = weight(x), n = f.amount / w;
         s_border = Border{Key<T>::of(x), (uint32_t)ties_below(n, w, f.in_front, goal), f.bin == from_bin ? 0xffffffffu : (uint32_t)n};      // (as many as were found before)
       }
@@ -619,7 +643,7 @@ sample_kernel(Params p) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) mine += x[j] == border_x;
     });
-    cluster_sum(warp_sum(mine), tie_rank);
+    cluster_sum(warp_sum(mine), tie_rank, 0);
   }
   const double least = min_p > 0.f ? fmin((double)min_p, 1.0) : 0.0;
   // min-p: scores above `sure` reach it, those below `never` do not (a hundred thousandth of the distance, and some steps of FP32, to either side of the border)
@@ -629,25 +653,45 @@ sample_kernel(Params p) {
     sure = (float)((double)top - away + slack);
     never = (float)((double)top - away - slack);
   }
-  // Weights of VEC scores, 0 where they go, and which stay; `at`: ties in front of the warp's first.
+  const uint32_t border_bits = __float_as_uint(border_x) >> 16;
   const float low = fmaxf(border_x, never);                    // below it nothing stays
+  // BF16 rows with many scores: every number's weight where it stays, and the highest bit.  (Border ties of which some go are looked at one by one.)
+  constexpr u64 STAYS = 1ull << 63;
   if (by_values) {
-    const int first = values.bin(top), last = min(values.bin(low) + 1, VALUES - 1);
-    for (int b = first + tid; b <= last; b += THREADS) s_u.value[b] = weight(values.value(b));
+    for (int i = tid; i < VALUES; i += THREADS) {
+      const float x = values.value(i);
+      bool stays = x <= top && (x > border_x || (x == border_x && (by_k || by_p)));
+      if (stays && least > 0.0 && !(x > sure)) stays = !(x < never) && weight.reaches(x, least);
+      s_u.value[i] = stays ? STAYS | weight(x) : 0;
+    }
     __syncthreads();
   }
-  auto weight_of = [&](float x) {
-    if (!by_values) return weight(x);
-    const int at = values.place(x);
-    if (at <= 0) return weight(x);
-    return at < HALF ? s_u.value[values.bin(x, at)] : 0ull;
-  };
+  // Weights of VEC scores, 0 where they go, and which stay; `at`: ties in front of the warp's first.
   auto keep = [&](uint4 v, u64& at, u64 (&w)[VEC]) {
     uint32_t stay = 0, tie = 0;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) w[j] = 0;
     const float most = largest(v, T());
     if (!__any_sync(0xffffffffu, most >= low && most > -INFINITY)) return stay;
+    if (by_values) {
+      int d[VEC], any = 0;
+      bool odd = false;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        d[j] = values.distance(score_bits(v, j));
+        any |= d[j];
+        if (some_ties) odd = odd || score_bits(v, j) == border_bits;
+      }
+      if (!__any_sync(0xffffffffu, odd || Values::outside(any))) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const u64 y = s_u.value[Values::at(d[j])];
+          stay |= (uint32_t)(y >> 63) << j;
+          w[j] = y & ~STAYS;
+        }
+        return stay;
+      }
+    }
     float x[VEC];
     unpack(v, x);
 #pragma unroll
@@ -680,7 +724,7 @@ sample_kernel(Params p) {
     if (__any_sync(0xffffffffu, stay != 0)) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const u64 u = weight_of(x[j]);
+        const u64 u = weight(x[j]);
         w[j] = stay >> j & 1u ? u : 0;
       }
     }
@@ -713,7 +757,7 @@ sample_kernel(Params p) {
       }
     });
   mine = warp_sum(mine);
-  const u64 all = cluster_sum(mine, before);
+  const u64 all = cluster_sum(mine, before, 1);
   const double goal = fmax((double)r, 0.0) * (double)all;
   // the warp in which the running sum passes the goal; beyond all of them (r not below one), the last that has any weight
   const bool past = !((double)all > goal);
