@@ -64,6 +64,16 @@ __device__ __forceinline__ float largest(uint4 v, bf16) {
   const __nv_bfloat162 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
   return fmaxf(__low2float(m), __high2float(m));
 }
+// Which of a vector's are x, a bit each.
+__device__ __forceinline__ uint32_t equal(uint4 v, float x, float) {
+  return (__uint_as_float(v.x) == x ? 1u : 0u) | (__uint_as_float(v.y) == x ? 2u : 0u) | (__uint_as_float(v.z) == x ? 4u : 0u) | (__uint_as_float(v.w) == x ? 8u : 0u);
+}
+__device__ __forceinline__ uint32_t equal(uint4 v, float x, bf16) {
+  const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
+  const __nv_bfloat162 y = __float2bfloat162_rn(x);
+  const uint32_t m = (__heq2_mask(p[0], y) & 0x00020001u) | (__heq2_mask(p[1], y) & 0x00080004u) | (__heq2_mask(p[2], y) & 0x00200010u) | (__heq2_mask(p[3], y) & 0x00800040u);
+  return (m | m >> 16) & 0xffu;
+}
 __device__ __forceinline__ bool has_nan(uint4 v, float) {
   return max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu)) > 0x7f800000u;
 }
@@ -637,12 +647,7 @@ sample_kernel(Params p) {
   u64 tie_rank = 0;
   if (some_ties) {
     u64 mine = 0;
-    sweep([&](int g, uint4 v) {
-      float x[VEC];
-      unpack(v, x);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) mine += x[j] == border_x;
-    });
+    sweep([&](int, uint4 v) { mine += __popc(equal(v, border_x, T())); });
     cluster_sum(warp_sum(mine), tie_rank, 0);
   }
   const double least = min_p > 0.f ? fmin((double)min_p, 1.0) : 0.0;
@@ -653,14 +658,33 @@ sample_kernel(Params p) {
     sure = (float)((double)top - away + slack);
     never = (float)((double)top - away - slack);
   }
-  const uint32_t border_bits = __float_as_uint(border_x) >> 16;
+  // Of the ties at the border, the first border.kept: all lanes' bits; `at` ties lie in front of the warp's, and it goes on.
+  auto ties_that_stay = [&](uint32_t tie, u64& at) {
+    if (!__any_sync(0xffffffffu, tie)) return 0u;
+    int before = __popc(tie);
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, before, s);
+      if (lane >= s) before += y;
+    }
+    const int all = __shfl_sync(0xffffffffu, before, 31);
+    before -= __popc(tie);
+    uint32_t stay = 0;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+      if (tie >> j & 1u && at + before + __popc(tie & ((1u << j) - 1u)) < border.kept) stay |= 1u << j;
+    at += all;
+    return stay;
+  };
   const float low = fmaxf(border_x, never);                    // below it nothing stays
   // BF16 rows with many scores: every number's weight where it stays, and the highest bit.  (Border ties of which some go are looked at one by one.)
   constexpr u64 STAYS = 1ull << 63;
+  const bool border_stays = some_ties && (least == 0.0 || weight.reaches(border_x, least));
+  const u64 border_w = border_stays ? weight(border_x) : 0;
   if (by_values) {
     for (int i = tid; i < VALUES; i += THREADS) {
       const float x = values.value(i);
-      bool stays = x <= top && (x > border_x || (x == border_x && (by_k || by_p)));
+      bool stays = x <= top && (x > border_x || (x == border_x && (by_k || by_p) && !some_ties));
       if (stays && least > 0.0 && !(x > sure)) stays = !(x < never) && weight.reaches(x, least);
       s_u.value[i] = stays ? STAYS | weight(x) : 0;
     }
@@ -668,26 +692,31 @@ sample_kernel(Params p) {
   }
   // Weights of VEC scores, 0 where they go, and which stay; `at`: ties in front of the warp's first.
   auto keep = [&](uint4 v, u64& at, u64 (&w)[VEC]) {
-    uint32_t stay = 0, tie = 0;
+    uint32_t stay = 0;
 #pragma unroll
     for (int j = 0; j < VEC; ++j) w[j] = 0;
     const float most = largest(v, T());
     if (!__any_sync(0xffffffffu, most >= low && most > -INFINITY)) return stay;
     if (by_values) {
       int d[VEC], any = 0;
-      bool odd = false;
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         d[j] = values.distance(score_bits(v, j));
         any |= d[j];
-        if (some_ties) odd = odd || score_bits(v, j) == border_bits;
       }
-      if (!__any_sync(0xffffffffu, odd || Values::outside(any))) {
+      if (!__any_sync(0xffffffffu, Values::outside(any))) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
           const u64 y = s_u.value[Values::at(d[j])];
           stay |= (uint32_t)(y >> 63) << j;
           w[j] = y & ~STAYS;
+        }
+        if (border_stays) {
+          const uint32_t ties = ties_that_stay(equal(v, border_x, T()), at);
+#pragma unroll
+          for (int j = 0; j < VEC; ++j)
+            if (ties >> j & 1u) w[j] = border_w;
+          stay |= ties;
         }
         return stay;
       }
@@ -695,24 +724,11 @@ sample_kernel(Params p) {
     float x[VEC];
     unpack(v, x);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
+    for (int j = 0; j < VEC; ++j)
       if (x[j] > border_x) stay |= 1u << j;
-      if (x[j] == border_x) tie |= 1u << j;
-    }
-    if (by_k || by_p) stay |= tie;                              // (else the border is -inf)
-    if (some_ties) {
-      int before = __popc(tie), all;
-#pragma unroll
-      for (int s = 1; s < 32; s <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, before, s);
-        if (lane >= s) before += y;
-      }
-      all = __shfl_sync(0xffffffffu, before, 31);
-      before -= __popc(tie);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j)
-        if (tie >> j & 1u && at + before + __popc(tie & ((1u << j) - 1u)) >= border.kept) stay &= ~(1u << j);
-      at += all;
+    if (by_k || by_p) {                                        // (else the border is -inf)
+      const uint32_t tie = equal(v, border_x, T());
+      stay |= some_ties ? ties_that_stay(tie, at) : tie;
     }
     if (least > 0.0) {
 #pragma unroll
