@@ -110,7 +110,7 @@ extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, in
   a.c = device_cache(c); a.q = q; a.q_stride = (size_t)q_stride; a.out = out; a.n_heads = n_heads; a.M = M; a.max_new = max_new; a.B = B; a.G = G;
   a.off = off; a.len = len; a.group = group; a.shared = shared; a.causal = causal != 0; a.scale = scale * (float)M_LOG2E; a.status = status;
   a.grid = s.grid; a.item_rows = dtype == AD_DTYPE_FP32 ? shr::M_ROWS : shr::ITEM_ROWS; a.part_rows = s.part_rows;
-  a.total = reinterpret_cast<long long*>(at + s.total); a.lines = reinterpret_cast<shr::Line*>(at + s.lines); a.start = reinterpret_cast<shr::Start*>(at + s.start);
+  a.total = reinterpret_cast<shr::Total*>(at + s.total); a.lines = reinterpret_cast<shr::Line*>(at + s.lines); a.start = reinterpret_cast<shr::Start*>(at + s.start);
   a.own_first = reinterpret_cast<int*>(at + s.first); a.own_len = reinterpret_cast<int*>(at + s.len);
   a.ml = reinterpret_cast<float2*>(at + s.ml); a.part = reinterpret_cast<float*>(at + s.part);
   a.own_ml = reinterpret_cast<float2*>(at + s.own_ml); a.own_part = reinterpret_cast<float*>(at + s.own_part);

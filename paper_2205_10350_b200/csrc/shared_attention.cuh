@@ -15,7 +15,7 @@ constexpr int M_ROWS = 128;            // rows of an MMA
 constexpr int ITEM_ROWS = 256;         // most rows of an item, and the distance of CTAs' parts in scratch
 
 // What is worked on: a line for every group, its rows' queries over the blocks that they share.  A line has `heads` times `tiles` (of its rows) items, each over all
-// of its keys; an item is `per` granules: FIXED ones, and `weight` for every tile of keys.  The CTAs share all granules evenly, in order.  What the rows have besides is left to the
+// of its keys; an item is `per` granules: FIXED ones, and `weight`, one or two, for every tile of keys.  The CTAs share all granules evenly, in order.  What the rows have besides is left to the
 // attention row by row; behind the groups' lines each row of the batch has one that says which queries are its own, and of which group.
 struct Line {
   long long front, rows_front;         // granules and rows of results in front of it
@@ -24,6 +24,7 @@ struct Line {
 };
 static_assert(sizeof(Line) == 64, "four 16-byte loads");
 struct Start { int line, pad; long long at; };
+struct Total { long long all, each; };  // granules of all lines; of a CTA, in order (the last ones may get fewer, or none)
 
 struct Params {
   Cache c;
@@ -41,7 +42,7 @@ struct Params {
   int grid, item_rows;                 // CTAs; rows of an item
   long long part_rows;                 // rows of results of one half
   // scratch
-  long long* total;                    // granules of all lines
+  Total* total;
   Line* lines;                         // [G + B]
   Start* start;                        // [grid]
   int* own_first;                      // [B] blocks that row b shares, and positions behind them (negative: the row is left out)
@@ -55,7 +56,7 @@ struct Params {
 constexpr int FIXED = 3;
 __host__ __device__ __forceinline__ int key_tiles(int keys) { return (keys + KEYS - 1) / KEYS; }
 // The tile that granule x of an item starts with.
-__host__ __device__ __forceinline__ int tile_at(int x, int weight) { return x <= FIXED ? 0 : (x - FIXED + weight - 1) / weight; }
+__host__ __device__ __forceinline__ int tile_at(int x, int weight) { return x <= FIXED ? 0 : (x - FIXED + weight - 1) >> (weight - 1); }
 
 // ---- plan ----------------------------------------------------------------------------------------------------------
 constexpr int PLAN_THREADS = 1024;
@@ -154,11 +155,11 @@ shared_plan_kernel(const __grid_constant__ Params a) {
     granules_front += all;
     tokens_front += all_t;
   }
-  const long long total = granules_front, ctas = min((long long)a.grid, total);
-  if (tid == 0) *a.total = total;
+  const long long total = granules_front, each = (total + a.grid - 1) / a.grid;
+  if (tid == 0) *a.total = Total{total, each};
   __syncthreads();
-  for (int c = tid; c < ctas; c += PLAN_THREADS) {           // where each CTA starts: in the last line that has begun there
-    const long long g = kv::cta_start(total, c, ctas);
+  for (int c = tid; c * each < total; c += PLAN_THREADS) {   // where each CTA starts: in the last line that has begun there
+    const long long g = c * each;
     int lo = 0, hi = a.G - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -189,10 +190,10 @@ struct Walk {
     loaded = line;
   }
   __device__ __forceinline__ bool begin(const Params& a) {
-    const long long total = __ldcg(a.total), ctas = min((long long)a.grid, total);
-    if (blockIdx.x >= ctas) return false;
-    cur = kv::cta_start(total, blockIdx.x, ctas);
-    end = kv::cta_start(total, blockIdx.x + 1, ctas);
+    const long long total = __ldcg(&a.total->all), each = __ldcg(&a.total->each);
+    cur = blockIdx.x * each;
+    end = min(cur + each, total);
+    if (cur >= end) return false;
     const Start* s = a.start + blockIdx.x;
     line = __ldcg(&s->line);
     at = __ldcg(&s->at);
@@ -938,35 +939,38 @@ shared_join_kernel(const __grid_constant__ Params a) {
     else y[0] = __ldcg(p);
   };
   const Line row = load_line(a.G + b);
-  const long long w = (long long)blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5);
-  if (w >= (long long)row.n * a.n_heads) return;
-  const Line grp = load_line(row.group);
-  const long long total = __ldcg(a.total), ctas = min((long long)a.grid, total);
-  const int i = (int)(w / a.n_heads), head = (int)(w % a.n_heads), kvh = head / per_kv;
+  if ((long long)blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5) >= (long long)row.n * a.n_heads) return;      // (below 2^30)
+  const int w = blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5), i = w / a.n_heads, head = w - i * a.n_heads, kvh = head / per_kv;
   // the row's own positions
   const size_t own = (size_t)(row.o + i) * a.n_heads + head;
   const float2 mine = __ldcg(a.own_ml + own);
+  float x[PER];
+  load(a.own_part + own * DIM, x);
+  const Line grp = load_line(row.group);
+  const long long each = __ldcg(&a.total->each);
   // part u of its group's: maximum and sum, and where its means are; all there are
   const int rows = grp.n * per_kv, r = (row.o - grp.o + i) * per_kv + head % per_kv, tile = r / a.item_rows, kt = key_tiles(grp.keys);
   const long long first = grp.front + ((long long)kvh * grp.tiles + tile) * grp.per, at = grp.rows_front + (long long)kvh * rows + r;
   const int halves = min(a.item_rows, rows - tile * a.item_rows) > M_ROWS ? 1 : 2;
+  auto cta_of = [&](long long g) { return (int)((g | each) >> 32 ? g / each : (unsigned)g / (unsigned)each); };
   int c0 = 0, parts = 0;
   if (grp.tiles > 0) {
-    c0 = kv::cta_of(total, first, ctas);
-    parts = (kv::cta_of(total, first + grp.per - 1, ctas) - c0 + 1) * halves;
+    c0 = cta_of(first);
+    parts = (cta_of(first + grp.per - 1) - c0 + 1) * halves;
   }
   auto part = [&](int u, long long& where) {
-    const int c = c0 + u / halves;
-    where = at + (long long)c * ITEM_ROWS + (u % halves) * a.part_rows;
+    const int c = c0 + (halves == 2 ? u >> 1 : u);
+    where = at + (long long)c * ITEM_ROWS + (halves == 2 && (u & 1) ? a.part_rows : 0);
     if (u >= parts) return make_float2(-INFINITY, 0.f);
-    const int g0 = (int)(max(kv::cta_start(total, c, ctas), first) - first), g1 = (int)(min(kv::cta_start(total, c + 1, ctas), first + grp.per) - first);
+    const int g0 = (int)(max(c * each, first) - first), g1 = (int)(min((c + 1) * each, first + grp.per) - first);
     return min(tile_at(g0, grp.weight), kt) < min(tile_at(g1, grp.weight), kt) ? __ldcg(a.ml + where) : make_float2(-INFINITY, 0.f);
   };
   // the largest maximum and the sum against it; then means times their shares (sums of values may be more than FP32 has room for)
-  float top = mine.y == 0.f ? -INFINITY : mine.x, sum = mine.y, x[PER];
+  float top = mine.y == 0.f ? -INFINITY : mine.x, sum = mine.y;
   long long where;
+  float2 v = make_float2(-INFINITY, 0.f);
   for (int u0 = 0; u0 < parts; u0 += 32) {
-    const float2 v = part(u0 + lane, where);
+    v = part(u0 + lane, where);
     float most = v.y != 0.f ? v.x : -INFINITY;
 #pragma unroll
     for (int s = 16; s; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
@@ -979,14 +983,13 @@ shared_join_kernel(const __grid_constant__ Params a) {
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   auto share = [&](float2 v) { return v.y == 0.f ? 0.f : (v.x == top ? v.y : v.y * kv::ex2(v.x - top)) * inv; };
-  load(a.own_part + own * DIM, x);
 #pragma unroll
   for (int j = 0; j < PER; ++j) x[j] = mine.y == 0.f ? 0.f : x[j] * share(mine);
   for (int u0 = 0; u0 < parts; u0 += 32) {
-    const float2 v = part(u0 + lane, where);
+    if (parts > 32) v = part(u0 + lane, where);
     const float f = share(v);
     for (unsigned left = __ballot_sync(0xffffffffu, v.y != 0.f); left;) {
-      constexpr int AHEAD = 4;
+      constexpr int AHEAD = 8;
       float y[AHEAD][PER], g[AHEAD];
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {
