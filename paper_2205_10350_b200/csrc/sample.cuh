@@ -165,6 +165,10 @@ struct Weights {
 // by digit of their keys.  Weights are worked out in FP64 and summed as integers in units of 2^-scale_bits (vocab * 2^scale_bits <= 2^62): the largest is 1, so a
 // sum is off by vocab * 2^-(scale_bits + 1) of itself at most, 2^-42 with 1000 ids and 2^-23 with 2^20 (roundings of either sign: their root, a 2^-10th
 // of that, in fact), and comes out the same in any order.
+// A row of FP32, or a short one, has every score's weight worked out, about 45 instructions; a long one of BF16 the weights of the 4096 numbers that lie within 16 octaves of the
+// largest magnitude with any weight, once a CTA: top-p's histogram counts numbers then, its border is one of them, and what is kept is looked up.
+// Bound by instructions and the cluster's barriers, about 0.7 us each: 256 rows of 128000 in BF16 (1024 CTAs, two an SM, four turns) take 89 us without a filter, 54 with min-p 0.05, 111 with
+// top-k 50, 189 with top-p 0.9, 140 with both; reading them takes 10.  One row of 32000 in FP32: 13, 13, 16, 21 and 24 us.
 // Scores are taken 16 bytes at a time: places g = id + shift, shift such that a place that is a multiple of a vector's lies on a vector's boundary.
 // grid = M clusters, block = THREADS.  Dynamic shared memory: KEPT, the CTA's scores.
 template <typename T, bool KEPT>
@@ -311,7 +315,8 @@ sample_kernel(Params p) {
 
   // ---- borders: of the scores above `from`, and the first from_n of those that have it (0: of all), where top-k's count or top-p's share of the weight ends ----
   // (Scores of -inf have no weight and are never among those; places that there are no scores for hold -inf.)
-  // BF16 rows with more scores than there are bins: weights are worked out by bin.  (256 rows of 128000, top-p: 370 -> 213 us; without a filter 133 -> 118.)
+  // BF16 rows with more scores a CTA than there are bins: weights are worked out number by number, not score by score.  (256 rows of 128000, top-p: 189 us instead of 370; without
+  // a filter 89 instead of 133.)
   const bool by_values = sizeof(T) == 2 && WARPS * each > VALUES;
   Values values = {0};
   if (by_values) {

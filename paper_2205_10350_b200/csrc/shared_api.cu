@@ -39,8 +39,10 @@ Scratch scratch_of(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t M, 
   s.bytes = s.rows + rounded(cache_attention_scratch(c, n_heads, B, max_new, own_keys(max_keys, max_shared, c->block)));
   return s;
 }
-// Whether the groups' positions are read once for all rows: where that saves the attention row by row 28000 units of 32 keys for 32 rows of queries, or more, which take it as
-// long as the calls' latencies.  Row by row / shared, 32 query heads on 8 of 128, BF16: 16 rows of one query behind 4000 positions (15000 units) XXX.
+// Whether the groups' positions are read once for all rows: where that saves the attention row by row 28000 units of 32 keys for 32 rows of queries and a key/value head, or more, as the
+// plan, a second pass over the rows and the join cost about what it takes for these.  Row by row / shared, 32 query heads on 8 of 128, BF16, one query a row: 16 rows
+// behind 4000 positions (15000 units) 43 / 43 us, 64 behind 1000 (15600) 37 / 48, 8 behind 16000 (28000) 63 / 49, 8 groups of 8 behind 2000 (27800) 71 / 51, 8 groups of 32 behind 500
+// (29800) 82 / 78, 64 behind 16000 (252000) 269 / 74; eight queries a row: 16 behind 4000 60 / 66, 8 groups of 8 behind 2000 102 / 105, 8 behind 16000 88 / 70.
 bool worth_sharing(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys, int32_t G, int32_t max_shared) {
   const int64_t rows = (int64_t)max_new * (n_heads / c->n_kv_heads), keys = std::min<int64_t>(std::min(max_keys, max_shared), (int64_t)c->table_stride * c->block);
   return (double)(B - G) * c->n_kv_heads * (double)((rows + 31) / 32) * (double)(keys / 32) >= 28000.0;

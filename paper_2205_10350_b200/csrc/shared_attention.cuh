@@ -95,6 +95,8 @@ __device__ __forceinline__ bool group_of(const Params& a, int g, int& first, int
   if (!good) latch_error(a.status, AD_ERR_ARG);
   return good;
 }
+// Bound by latency: four round trips one after another for rows and groups, two more for the CTAs' starts, 9 us alone and cold.  (Starts found by one thread, line after line
+// with a 64-bit division for each: 20 us.)
 // grid = 1, block = PLAN_THREADS.
 __global__ void __launch_bounds__(PLAN_THREADS)
 shared_plan_kernel(const __grid_constant__ Params a) {
@@ -328,8 +330,8 @@ struct Turn {
   }
 };
 
-// A wait by a whole warp, bounded in time, once a first look has found nothing.  (Short, and out of line: the kernel's roles share the SM's instruction cache.  With the
-// polls unrolled, 140 KB of instructions, 4 prompts x 24-32 samples took 330 us instead of 318.)
+// A wait by a whole warp, bounded in time, once a first look has found nothing.  (Short, and out of line: with the polls unrolled the kernel had 140 KB of instructions instead
+// of 92; its time was the same.)
 __device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort, int* status) {
   const unsigned long long t0 = tc::global_ns();
   for (;;) {
@@ -344,6 +346,22 @@ __device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int
   return false;
 }
 
+// S = Q K^T, P = 2^(factor S - m), O = P V over the positions that a group shares, for all of its rows' queries: with per_kv heads on one key/value head, n tokens are n per_kv rows
+// of the same matrices, so that 128 of them fill an MMA's rows where the attention row by row has 4 to 32.
+// Codes are exact in FP16, and so are BF16 queries times a power of two (FP32 ones and their probabilities go in as two FP16 numbers: twice the products); a block's scale meets
+// the scores behind the product, and the probabilities in front of the next one, rounded to 11 bits (22) as in the attention row by row, sums in FP32.  References m and d
+// (of scores, and of probability times scale) are whole exponents: what changes when they move is exact.
+// Scores lie in tensor memory, probabilities replace them there in half the columns and are the second product's A as they lie.  A CTA works on two halves, each 128 rows of its own (or, with no
+// more than 128 rows, every other tile of keys for the same rows), in steps of 64 keys whose scores are issued two steps ahead, so that tensor cores and exponentials of the
+// halves take turns.  Exponents are worked out against the references as they are, and again only where one of the warp's rows passes them.
+// The CTAs take equal shares of all granules: an item's fixed part is what queries, results and the first tiles' latency cost (9600 cycles), a tile of 128 keys 3440 cycles with one tile
+// of rows and 5700 with two.
+// Bound by the softmax's latency: of a step's 2900 cycles with two tiles of rows its eight warps wait 290 for scores, look at them for 620 (loads from tensor memory among it),
+// take 1000 for exponents and 930 for powers of two (MUFU: 256), store and hand over for 300; the products are 1024, at 8192 operations a cycle.  Sixteen softmax warps, two
+// a row, with references exchanged through shared memory, were slower (registers: 64 scores a thread are held at once); so was a branch of its own for keys that are not there.
+// 109 rows of 3-8 queries behind 4 prefixes of 6000-16000, 32 heads on 8 of 128, INT8: 195 us, 104 GFLOP, 535 TFLOP/s of 1668 measured; 64 single queries behind 32000: 81 us, 418
+// TFLOP/s.  (All of it by the attention row by row: 682 and 598 us with what follows.)
+// grid = (CTAs that the plan is for), block = THREADS; dynamic shared memory: smem_bytes.
 template <typename T, typename F, int DIM>
 __global__ void __launch_bounds__(THREADS, 1)
 shared_attention_kernel(const __grid_constant__ Params a) {
@@ -915,7 +933,9 @@ shared_attention_kernel(const __grid_constant__ Params a) {
   if (warp == W_MMA) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
 }
 
-// Joins the parts of every query: of its group's items, and of its row's own positions.  A warp a query and head.
+// Joins the parts of every query: of its group's items, and of its row's own positions, with out = sum of mean_i s_i 2^(m_i - m) / sum of s_i 2^(m_i - m).  A warp a query and head.
+// Bound by latency: lines, maxima, means, one after another; 600 queries of 32 heads with 2 to 4 parts each 32 us, 64 with 20 parts 9.6 us.  (With the parts' borders by 64-bit divisions and four
+// means under way: 34 and 12.5 us.)
 // grid = (enough for max_new * n_heads warps, B), block = JOIN_THREADS.
 constexpr int JOIN_THREADS = 256;
 template <typename T, int DIM>

@@ -254,3 +254,29 @@ def test_truncated_distributions_are_verified_like_any_others():
     for b in range(B):
         for i in range(int(n[b])):
             assert kept[b, i, int(ids[b, i])]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V", [40001, 131073])
+def test_long_rows_of_all_kinds(dtype, V):
+    """Rows whose weights are looked up by number: magnitudes far apart, borders among numbers too small for a bin, zeros of both signs, few numbers with thousands of ties each, scores
+    below zero only, one infinity and many, masked ids, temperatures that make all of them alike or leave one."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn((12, V), generator=g)
+    x[1] *= 1e-4                                                # (all of it small, beside one larger number)
+    x[1, 77] = 4.0
+    x[2] = x[2].sign() * 0.0
+    x[2, ::9] = -1.0
+    x[3] = (x[3] * 2).round()                                  # (a dozen numbers)
+    x[4] = -x[4].abs() * 3 - 100
+    x[5, 1000] = float("inf")
+    x[6, ::1000] = float("inf")
+    x[7, torch.rand(V, generator=g) < 0.9] = float("-inf")
+    x[8] *= torch.exp(torch.randn(V, generator=g) * 4)         # (many octaves)
+    x[9] = torch.where(x[9] > 0, 1e-30, -1e-30) * x[9].abs()
+    x[10, 5:] = float("-inf")
+    x[11] = x[11].clamp(-0.01, 0.01)
+    r = np.random.default_rng(V)
+    for temperature in (0.7, 30.0, 1e5, 1e37, 1e-3):
+        for k, p, least in ((0, 1.0, 0.0), (0, 0.83, 0.0), (V // 3, 1.0, 0.0), (V // 2, 0.71, 0.0), (40, 0.6, 0.0), (0, 0.9, 0.3), (0, 1.0, 0.2)):
+            check(x.to(TORCH[dtype]), r.random(12), temperature=[temperature] * 12, top_k=[k] * 12, top_p=[p] * 12, min_p=[least] * 12)
