@@ -111,6 +111,8 @@ __device__ __forceinline__ uint32_t score_bits(uint4 v, int j) {      // BF16's
   const uint32_t w = j < 2 ? v.x : j < 4 ? v.y : j < 6 ? v.z : v.w;
   return j & 1 ? w >> 16 : w & 0xffffu;
 }
+struct Counts { static constexpr bool MASS = false; };      // what a search goes by
+struct Mass { static constexpr bool MASS = true; };
 struct Border { uint32_t key, kept, ties; };      // scores above this key stay, and of those that have it, `ties`, the first `kept`
 
 // 64-bit sums from 32-bit atomic additions: exact, so that their order does not matter.  (Additions of 64 bits in shared memory are loops: 256 rows of 128000, top-p 384 -> 505 us.)
@@ -167,8 +169,8 @@ struct Weights {
 // of that, in fact), and comes out the same in any order.
 // A row of FP32, or a short one, has every score's weight worked out, about 45 instructions; a long one of BF16 the weights of the 4096 numbers that lie within 16 octaves of the
 // largest magnitude with any weight, once a CTA: top-p's histogram counts numbers then, its border is one of them, and what is kept is looked up.
-// Bound by instructions and the cluster's barriers, about 0.7 us each: 256 rows of 128000 in BF16 (1024 CTAs, two an SM, four turns) take 89 us without a filter, 54 with min-p 0.05, 111 with
-// top-k 50, 189 with top-p 0.9, 140 with both; reading them takes 10.  One row of 32000 in FP32: 13, 13, 16, 21 and 24 us.
+// Bound by instructions and the cluster's barriers, about 0.7 us each: 256 rows of 128000 in BF16 (1024 CTAs, two an SM, four turns) take 90 us without a filter, 54 with min-p 0.05, 111 with
+// top-k 50, 190 with top-p 0.9, 104 with both (one search; two: 140); reading them takes 10.  One row of 32000 in FP32: 14, 14, 15, 20 and 16 us.
 // Scores are taken 16 bytes at a time: places g = id + shift, shift such that a place that is a multiple of a vector's lies on a vector's boundary.
 // grid = M clusters, block = THREADS.  Dynamic shared memory: KEPT, the CTA's scores.
 template <typename T, bool KEPT>
@@ -403,7 +405,8 @@ sample_kernel(Params p) {
     return Border{prefix, (uint32_t)(by_mass ? ties_below(n, w, in_front, goal) : min(n, k - in_front)), (uint32_t)n};
   };
   // few: of the threads' own largest scores instead of all, whose k-th lies no higher than the k-th of all; what is in its bin and in front of it is put in order.
-  auto search = [&](bool by_mass, double share, u64 k, bool few) {
+  auto search = [&](auto what, double share, u64 k, bool few) {
+    constexpr bool by_mass = decltype(what)::MASS;
     const bool by_value = by_mass && by_values;
     auto small = [&](float x, u64 n) {                         // n of a score whose magnitude is small
       const u64 w = weight(x) * n;
@@ -463,7 +466,7 @@ sample_kernel(Params p) {
     }
     cluster.sync();
     // every CTA adds up its part of the bins, a few a thread
-    constexpr int MOST = sizeof(T) == 2 ? VALUES / THREADS : PER;
+    constexpr int MOST = by_mass && sizeof(T) == 2 ? VALUES / THREADS : PER;
     const int chunk = (by_value ? VALUES : BINS) / size, per = max(1, chunk / THREADS), b0 = rank * chunk + tid * per;
     u64 amount[MOST], sum = 0;
 #pragma unroll
@@ -590,10 +593,20 @@ sample_kernel(Params p) {
       }
       auto key_at = [&](int i) { return ~(uint32_t)(s_u.list[i] >> 32); };
       // how many of them, in order, are kept
-      int kept;
+      int kept = (int)min((u64)have, k - f.in_front);
       u64 inside = 0;                                          // weight of all of them
-      if (by_mass) {
-        const int per_thread = (n2 + THREADS - 1) / THREADS, i0 = tid * per_thread;
+      const int per_thread = (n2 + THREADS - 1) / THREADS, i0 = tid * per_thread;
+      if (few && share < 1.0) {                                // all that top-k keeps is here: what top-p leaves of it
+        u64 w = 0, below_goal = 0, run, all, unused;
+        for (int i = i0; i < min(i0 + per_thread, kept); ++i) w += weight(score_of<T>(key_at(i)));
+        cta_scan(w, run, all);
+        for (int i = i0; i < min(i0 + per_thread, kept); ++i) {
+          below_goal += i == 0 || (double)run < share * (double)all;
+          run += weight(score_of<T>(key_at(i)));
+        }
+        cta_scan(below_goal, unused, all);
+        kept = (int)all;
+      } else if (by_mass) {
         u64 w = 0, before, unused;
         for (int i = i0; i < min(i0 + per_thread, have); ++i) w += weight(score_of<T>(key_at(i)));
         cta_scan(w, before, inside);
@@ -604,8 +617,6 @@ sample_kernel(Params p) {
         }
         cta_scan(below_goal, unused, total);
         kept = (int)total;
-      } else {
-        kept = (int)min((u64)have, k - f.in_front);
       }
       if (tid == 0) {
         Border x;
@@ -632,18 +643,23 @@ sample_kernel(Params p) {
   };
   Border border = {from, 0, 0};                               // (all above -inf)
   const bool few = top_k <= min(size * THREADS / 2, LIST / 4);
-  if (by_k) {
-    // (half of the threads at most: their largest scores must be enough of them, and not all)
-    border = search(false, 0.0, (u64)top_k, few);
-    if (border.ties == 0) border = search(false, 0.0, (u64)top_k, false);
+  // (Either form is called at one place only, so that its code is there once and in line: a third call took one row of FP32 from 21 us to 38.)
+  bool both = false;                                           // top-k's search has found top-p's border
+  uint32_t ties_before = 0;
+#pragma unroll 1
+  for (bool among_few = few; by_k; among_few = false) {
+    border = search(Counts(), by_p ? (double)top_p : 1.0, (u64)top_k, among_few);
+    if (border.ties == 0 && among_few) continue;               // (not enough threads, or too many scores)
+    both = among_few && by_p;
     from = border.key;
     from_n = border.kept;
     from_x = score_of<T>(from);
+    ties_before = border.ties;
+    break;
   }
-  if (by_p) {
-    const uint32_t ties = border.ties;
-    border = search(true, (double)top_p, 0, false);
-    if (by_k && border.key == from) border.ties = ties;        // (of those at the border before, some more go)
+  if (by_p && !both) {
+    border = search(Mass(), (double)top_p, 0, false);
+    if (by_k && border.key == from) border.ties = ties_before;      // (of those at the border before, some more go)
   }
 
   // ---- what is kept, in the order of ids ----
