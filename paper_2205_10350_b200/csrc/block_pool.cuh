@@ -71,7 +71,7 @@ cache_fork_kernel(Pool p, const int* __restrict__ parent, const int* __restrict_
 // ---- planning kernels: one cluster ---------------------------------------------------------------------------------
 // Whatever is numbered in order (free blocks, rows' needs) is counted by ranges, one per warp of the cluster: a count, the ranges' counts added up in front of
 // each, then the same walk again with its number at hand.
-constexpr int PLAN_THREADS = 1024, PLAN_WARPS = PLAN_THREADS / 32, MAX_CLUSTER = 8, COUNTS = 3;
+constexpr int PLAN_THREADS = 1024, PLAN_WARPS = PLAN_THREADS / 32, MAX_CLUSTER = 8, COUNTS = 3;      // at most (warps of a CTA: a power of two)
 struct Move { int src, dst, live; };       // `live` tokens of block src go to block dst
 struct Plan {
   Pool p;
@@ -97,7 +97,7 @@ __device__ __forceinline__ void cluster_counts(cg::cluster_group& cluster, Count
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int x = s.warp[i][lane];
+    const int x = lane < (int)blockDim.x / 32 ? s.warp[i][lane] : 0;
     front[i] = __reduce_add_sync(0xffffffffu, lane < warp ? x : 0);
     const int sum = __reduce_add_sync(0xffffffffu, x);
     if (threadIdx.x == 0) s.cta[i] = sum;
@@ -115,7 +115,7 @@ __device__ __forceinline__ void cluster_counts(cg::cluster_group& cluster, Count
 }
 // A warp's part of n things that lie in order.
 __device__ __forceinline__ void warp_range(cg::cluster_group& cluster, int n, int& lo, int& hi) {
-  const int warps = cluster.num_blocks() * PLAN_WARPS, w = cluster.block_rank() * PLAN_WARPS + (threadIdx.x >> 5);
+  const int each = blockDim.x >> 5, warps = cluster.num_blocks() * each, w = cluster.block_rank() * each + (threadIdx.x >> 5);
   lo = (int)((long long)n * w / warps);
   hi = (int)((long long)n * (w + 1) / warps);
 }
@@ -154,10 +154,10 @@ __host__ __device__ __forceinline__ bool span_of(const Pool& p, int off0, int of
 // too.  Of the rows that write the same block the first keeps it where nobody else holds it; all others leave it.  Fresh blocks are the free ones
 // in ascending order, handed out in the order of rows and of blocks within a row: nothing here depends on the order in which threads run.  A pool with too few
 // of them latches AD_ERR_CAPACITY and stays as it is.  moves[b]: what the copy kernel is to do for row b.
-// Bound by latency: eight barriers, as many round trips, and its own instructions, which come from memory when others have run in between (8 rows: 11 us alone and cold, of
+// Bound by latency: eight barriers, as many round trips, and its own instructions, which come from memory when others have run in between (8 rows: 10 us alone and cold, of
 // which 3 are spent on loops that have nothing to do).  256 rows of 1678 blocks, a cluster: 15 us.  (Claims and lists of a single CTA in shared memory, with barriers of
 // its own: the same.)
-// grid = one cluster, block = PLAN_THREADS.
+// grid = one cluster, block = PLAN_THREADS or less.
 __global__ void __launch_bounds__(PLAN_THREADS)
 cache_reserve_kernel(Plan a, const int* __restrict__ off, const int* __restrict__ len, int B, int* status) {
   __shared__ Counting s_count;
@@ -253,7 +253,7 @@ cache_reserve_kernel(Plan a, const int* __restrict__ off, const int* __restrict_
 
 // ---- moving what is in use to the front --------------------------------------------------------------------------
 // With U blocks in use, those from U on go to the free ones in front of U, both in ascending order.  Bound by latency, as above: 6.5 us alone and cold.
-// grid = one cluster, block = PLAN_THREADS.
+// grid = one cluster, block = PLAN_THREADS or less.
 __global__ void __launch_bounds__(PLAN_THREADS)
 cache_compact_kernel(Plan a, int* n_used) {
   __shared__ Counting s_count;
@@ -282,7 +282,7 @@ cache_compact_kernel(Plan a, int* n_used) {
   });
   cluster_counts(cluster, s_count, {movers}, unused, all);
   const int H = all[0];                                                   // (as many holes in front of U as blocks in use behind it)
-  for (int j = cluster.block_rank() * PLAN_THREADS + threadIdx.x; j < H; j += cluster.num_blocks() * PLAN_THREADS) {
+  for (int j = cluster.block_rank() * blockDim.x + threadIdx.x; j < H; j += cluster.num_blocks() * blockDim.x) {
     const int dst = __ldcg(a.list + j), src = __ldcg(a.list + p.n_blocks + H - 1 - j);
     a.moves[j] = Move{src, dst, p.block};
     a.map[src] = dst;

@@ -59,7 +59,7 @@ __host__ __device__ __forceinline__ int key_tiles(int keys) { return (keys + KEY
 __host__ __device__ __forceinline__ int tile_at(int x, int weight) { return x <= FIXED ? 0 : (x - FIXED + weight - 1) >> (weight - 1); }
 
 // ---- plan ----------------------------------------------------------------------------------------------------------
-constexpr int PLAN_THREADS = 1024;
+constexpr int PLAN_THREADS = 256;
 __device__ __forceinline__ long long block_scan(long long x, long long* s_warp, long long& all) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   long long run = x;
@@ -95,8 +95,8 @@ __device__ __forceinline__ bool group_of(const Params& a, int g, int& first, int
   if (!good) latch_error(a.status, AD_ERR_ARG);
   return good;
 }
-// Bound by latency: four round trips one after another for rows and groups, two more for the CTAs' starts, 9 us alone and cold.  (Starts found by one thread, line after line
-// with a 64-bit division for each: 20 us.)
+// Bound by latency: four round trips one after another for rows and groups, two more for the CTAs' starts, 6 us alone and cold.  (With 1024 threads 9.5 us.  Starts found by one thread, line after
+// line with a 64-bit division for each: 10 more.)
 // grid = 1, block = PLAN_THREADS.
 __global__ void __launch_bounds__(PLAN_THREADS)
 shared_plan_kernel(const __grid_constant__ Params a) {
