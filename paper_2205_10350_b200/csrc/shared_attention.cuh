@@ -934,12 +934,12 @@ shared_attention_kernel(const __grid_constant__ Params a) {
 }
 
 // Joins the parts of every query: of its group's items, and of its row's own positions, with out = sum of mean_i s_i 2^(m_i - m) / sum of s_i 2^(m_i - m).  A warp a query and head.
-// Bound by latency: lines, maxima, means, one after another; 600 queries of 32 heads with 2 to 4 parts each 32 us, 64 with 20 parts 9.6 us.  (With the parts' borders by 64-bit divisions and four
-// means under way: 34 and 12.5 us.)
+// Bound by latency: lines, maxima, means, one after another; five means under way and four CTAs an SM: 600 queries of 32 heads with 2 to 4 parts each 23 us, 64 with 20 parts 11 us.  (Eight
+// means and three CTAs: 33 and 9.7; with the parts' borders by 64-bit divisions besides: 34 and 12.5.)
 // grid = (enough for max_new * n_heads warps, B), block = JOIN_THREADS.
 constexpr int JOIN_THREADS = 256;
 template <typename T, int DIM>
-__global__ void __launch_bounds__(JOIN_THREADS)
+__global__ void __launch_bounds__(JOIN_THREADS, 4)
 shared_join_kernel(const __grid_constant__ Params a) {
   constexpr int PER = DIM / 32;
   pdl_launch();
@@ -1009,7 +1009,7 @@ shared_join_kernel(const __grid_constant__ Params a) {
     if (parts > 32) v = part(u0 + lane, where);
     const float f = share(v);
     for (unsigned left = __ballot_sync(0xffffffffu, v.y != 0.f); left;) {
-      constexpr int AHEAD = 8;
+      constexpr int AHEAD = 5;
       float y[AHEAD][PER], g[AHEAD];
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {
