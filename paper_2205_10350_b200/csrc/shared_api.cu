@@ -39,13 +39,18 @@ Scratch scratch_of(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t M, 
   s.bytes = s.rows + rounded(cache_attention_scratch(c, n_heads, B, max_new, own_keys(max_keys, max_shared, c->block)));
   return s;
 }
-// Whether the groups' positions are read once for all rows: where that saves the attention row by row 28000 units of 32 keys for 32 rows of queries and a key/value head, or more, as the
-// plan, a second pass over the rows and the join cost about what it takes for these.  Row by row / shared, 32 query heads on 8 of 128, BF16, one query a row: 16 rows
-// behind 4000 positions (15000 units) 43 / 43 us, 64 behind 1000 (15600) 37 / 48, 8 behind 16000 (28000) 63 / 49, 8 groups of 8 behind 2000 (27800) 71 / 51, 8 groups of 32 behind 500
-// (29800) 82 / 78, 64 behind 16000 (252000) 269 / 74; eight queries a row: 16 behind 4000 60 / 66, 8 groups of 8 behind 2000 102 / 105, 8 behind 16000 88 / 70.
-bool worth_sharing(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys, int32_t G, int32_t max_shared) {
+// Whether the groups' positions are read once for all rows.  That saves units of 32 keys for 32 rows of queries and a key/value head, and costs the plan, a second pass over the rows and the join:
+// about as much as 13000 units (16000 of 128 wide BF16, which the attention row by row takes less long for), one for every row and key/value head, and 0.4 for
+// every query and head, whose parts are written and read again.
+// Row by row / shared in us, 8 key/value heads:
+//   128 wide, 4 query heads each, BF16: 16 rows of a query behind 4000 positions (15000 units) 46 / 39, 64 behind 1000 (15600) 39 / 44, 8 behind 16000 (28000) 63 / 49, 64 behind 16000 (252000)
+//   269 / 74; 16 rows of 8 behind 4000 (15000) 60 / 62, 8 groups of 16 of 8 behind 1000 (29800, 32800 queries) 131 / 129, 8 of 16 of 15 behind 330 (19200, 61400 queries) 107 / 185;
+//   64 wide, a query head each: 64 rows of a query behind 1000 (15600) 36 / 28, in FP32 41 / 29; 8 groups of 8 of 8 behind 1000 (13900) 38 / 36, in FP32 43 / 37; 16 behind 4000
+//   (15000) 33 / 32, in FP32 37 / 32; 8 of 32 of a query behind 250 (13900) 36 / 47, in FP32 41 / 49; 8 of 16 of 15 behind 330 (9600, 15400 queries) 28 / 54, in FP32 34 / 54.
+bool worth_sharing(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, int32_t G, int32_t max_shared) {
   const int64_t rows = (int64_t)max_new * (n_heads / c->n_kv_heads), keys = std::min<int64_t>(std::min(max_keys, max_shared), (int64_t)c->table_stride * c->block);
-  return (double)(B - G) * c->n_kv_heads * (double)((rows + 31) / 32) * (double)(keys / 32) >= 28000.0;
+  const double saved = (double)(B - G) * c->n_kv_heads * (double)((rows + 31) / 32) * (double)(keys / 32);
+  return saved >= (dtype == AD_DTYPE_BF16 && c->head_dim == 128 ? 16000.0 : 13000.0) + (double)B * c->n_kv_heads + 0.4 * M * (double)n_heads;
 }
 const char* shared_fault(int32_t n_heads, int32_t B, int32_t M, int32_t G, int32_t max_shared) {
   if (B < 1 || B > kSharedRows) return "1 to 8192 rows";
@@ -88,7 +93,7 @@ extern "C" size_t ad_cache_attention_shared_scratch_bytes(const ad_kv_cache* c, 
   if (shared_fault(n_heads, B, M, G, max_shared)) return 0;
   const size_t alone = ad_cache_attention_scratch_bytes(c, dtype, n_heads, B, max_new, max_keys);
   if (cache_fault(c, B) || !known_dtype(dtype) || max_new < 1 || max_keys < 0 || n_heads % c->n_kv_heads) return 0;
-  return worth_sharing(c, n_heads, B, max_new, max_keys, G, max_shared) ? scratch_of(c, n_heads, B, M, max_new, max_keys, G, max_shared).bytes : alone;
+  return worth_sharing(c, dtype, n_heads, B, M, max_new, max_keys, G, max_shared) ? scratch_of(c, n_heads, B, M, max_new, max_keys, G, max_shared).bytes : alone;
 }
 
 extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
@@ -105,7 +110,7 @@ extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, in
   if (scratch_bytes < need) return op_fail(AD_ERR_CAPACITY, entry, "scratch too small");
   if (need && (!scratch || !aligned(scratch, 256))) return arg_fault(entry, "scratch must be 256-byte aligned");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (!worth_sharing(c, n_heads, B, max_new, max_keys, G, max_shared)) return launched(entry, cache_attention(c, call, scratch, st));
+  if (!worth_sharing(c, dtype, n_heads, B, M, max_new, max_keys, G, max_shared)) return launched(entry, cache_attention(c, call, scratch, st));
   const Scratch s = scratch_of(c, n_heads, B, M, max_new, max_keys, G, max_shared);
   char* at = static_cast<char*>(scratch);
   shr::Params a = {};

@@ -357,7 +357,7 @@ __device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int
 // The CTAs take equal shares of all granules: an item's fixed part is what queries, results and the first tiles' latency cost (9600 cycles), a tile of 128 keys 3440 cycles with one tile
 // of rows and 5700 with two.
 // Bound by the softmax's latency: of a step's 2900 cycles with two tiles of rows its eight warps wait 290 for scores, look at them for 620 (loads from tensor memory among it),
-// take 1000 for exponents and 930 for powers of two (MUFU: 256), store and hand over for 300; the products are 1024, at 8192 operations a cycle.  Sixteen softmax warps, two
+// take 1000 for exponents and 930 for powers of two, store and hand over for 300, while products and powers of two of both halves need 1024 each.  Sixteen softmax warps, two
 // a row, with references exchanged through shared memory, were slower (registers: 64 scores a thread are held at once); so was a branch of its own for keys that are not there.
 // 109 rows of 3-8 queries behind 4 prefixes of 6000-16000, 32 heads on 8 of 128, INT8: 195 us, 104 GFLOP, 535 TFLOP/s of 1668 measured; 64 single queries behind 32000: 81 us, 418
 // TFLOP/s.  (All of it by the attention row by row: 682 and 598 us with what follows.)
