@@ -402,7 +402,7 @@ int ad_accept_sampled(const void* target, int64_t target_stride, const void* dra
 /* Attention over the cache for batches whose rows share prefixes.  The rows group[g] .. group[g + 1] - 1 (group [G + 1], device, ascending from 0 to B) hold
  * the same keys and values in their first shared[g] positions (shared [G], device; 0: nothing shared; at most len[b] of every row that brings tokens), as rows do
  * that ad_cache_fork made from one, or that look at one encoder's keys.  The whole blocks among these positions may be read once for the group, through the table of its
- * first row (which then must name them, whether or not that row brings tokens); the rest is read through each row's own table, which must be in order
+ * first row that brings tokens; the rest is read through each row's own table, which must be in order
  * throughout.  Whether they are is decided by the sizes that the host gives, by what it saves; the result differs by roundings alone.  Otherwise arguments, result and
  * precision are those of ad_cache_attention.  max_shared: longest prefix to plan for; longer ones are computed as well, only slower.  Where positions are read once,
  * rows of a group that does not lie in ascending order within 0 .. B, or with shared[g] below 0 or beyond a row's capacity, and rows with fewer than shared[g]

@@ -17,6 +17,7 @@ constexpr int ITEM_ROWS = 256;         // most rows of an item, and the distance
 // What is worked on: a line for every group, its rows' queries over the blocks that they share.  A line has `heads` times `tiles` (of its rows) items, each over all
 // of its keys; an item is `per` granules: FIXED ones, and `weight`, one or two, for every tile of keys.  The CTAs share all granules evenly, in order.  What the rows have besides is left to the
 // attention row by row; behind the groups' lines each row of the batch has one that says which queries are its own, and of which group.
+// `row`: the one whose table names the group's blocks.
 struct Line {
   long long front, rows_front;         // granules and rows of results in front of it
   int o, n, keys;                      // tokens o .. o + n - 1; keys that they share
@@ -138,6 +139,14 @@ shared_plan_kernel(const __grid_constant__ Params a) {
     if (l < a.G) {
       int last;
       if (!group_of(a, l, x.row, last, x.o, x.n, x.keys)) x.keys = 0;
+      if (x.n > 0 && __ldcg(a.off + x.row + 1) <= x.o) {      // the first row that brings tokens: others may have been given up
+        int hi = last - 1;
+        while (x.row < hi) {
+          const int mid = (x.row + hi) >> 1;
+          if (__ldcg(a.off + mid + 1) > x.o) hi = mid;
+          else x.row = mid + 1;
+        }
+      }
       x.keys -= x.keys % a.c.block;                           // (whole blocks; the rest is the rows' own)
     }
     // no more results than there is room for, whatever the offsets

@@ -236,3 +236,22 @@ def test_nothing_to_do():
     assert binding.cache_attention_shared(cache, empty, ints([0, 0, 0]), ints(lens), ints(first), ints([64]), 1, 65).shape == (0, 2, 64)
     out, status = run(cache, numbers((2, 1, 64), "bf16", 1).to(DEV), [2, 0], [0, 0], first, [0], [0], False)
     assert status == 0 and bool((out == 0).all())
+
+
+@pytest.mark.parametrize("idle", [[0], [0, 1, 2], [0, 1, 2, 4], [1, 3], [0, 5, 6], [5, 6, 7, 8]])
+def test_rows_that_were_given_up(idle):
+    """Rows without tokens need no blocks, wherever they stand in their group, and none at all in a group: the others' results are what they were."""
+    groups, shared = [5, 4], [300, 129]
+    tails, new = [10, 0, 70, 5, 1, 33, 2, 0, 64], [0 if b in idle else 1 + b % 4 for b in range(9)]
+    cache, model, first, lens, ends = batch(groups, shared, tails, new, 2, 64, 32, "e4m3", True)
+    q = numbers((sum(new), 4, 64), "bf16", 3, 0.3).to(DEV)
+    want, status = run(cache, q, new, lens, first, shared, ends, True)
+    assert status == 0
+    table = cache.table
+    for b in idle:
+        table[b] = -1
+        lens[b] = -5 if b % 2 else 0
+    got, status = run(cache, q, new, lens, first, shared, ends, True)
+    assert status == 0 and torch.equal(got, want)
+    exact = model.attend(q.double().cpu().numpy(), offsets(new), [max(n, 0) for n in lens], True, 64 ** -0.5)
+    assert (np.abs(got.double().cpu().numpy() - exact[0]) <= bound("bf16", *exact, max(ends), 64)).all()
