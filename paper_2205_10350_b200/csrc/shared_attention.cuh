@@ -263,7 +263,8 @@ constexpr int N_SEGMENTS = 8;
 template <int DIM, bool WIDE>
 struct Small {
   typedef Layout<DIM, WIDE> L;
-  uint64_t raw_full[L::N_RAW], raw_empty[L::N_RAW], full[L::N_TILES], empty[L::N_TILES], s[2][2], p[2][2], o[2][2], q, drain, seg_full[N_SEGMENTS], seg_empty[N_SEGMENTS];
+  uint64_t raw_full[L::N_RAW], raw_empty[L::N_RAW], full[L::N_TILES], empty[L::N_TILES], s[2][2], p[2][2], o[2][2], drain, seg_full[N_SEGMENTS], seg_empty[N_SEGMENTS];
+  uint64_t q[N_SEGMENTS];              // queries of the segment in that place.  (The place is not told again before both halves' products have waited for them: none gets two phases behind.)
   Info info[L::N_INFO];
   Segment segment[N_SEGMENTS];         // what the warp that asks for codes has come to, for all others; t1 = 0: that was all
   uint8_t exponent[2][M_ROWS];          // of the rows' largest numbers
@@ -391,8 +392,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
     for (int i = 0; i < L::N_RAW; ++i) { tc::mbar_init(bar(sm.raw_full[i]), 1); tc::mbar_init(bar(sm.raw_empty[i]), CONVERT_WARPS); }
     for (int i = 0; i < L::N_TILES; ++i) { tc::mbar_init(bar(sm.full[i]), CONVERT_WARPS); tc::mbar_init(bar(sm.empty[i]), 2); }
     for (int i = 0; i < 2; ++i) { tc::mbar_init(bar(sm.s[i][0]), 1); tc::mbar_init(bar(sm.s[i][1]), 1); tc::mbar_init(bar(sm.p[i][0]), 4); tc::mbar_init(bar(sm.p[i][1]), 4); tc::mbar_init(bar(sm.o[i][0]), 1); tc::mbar_init(bar(sm.o[i][1]), 1); }
-    tc::mbar_init(bar(sm.q), SOFTMAX_WARPS);
-    for (int i = 0; i < N_SEGMENTS; ++i) { tc::mbar_init(bar(sm.seg_full[i]), 1); tc::mbar_init(bar(sm.seg_empty[i]), SOFTMAX_WARPS + CONVERT_WARPS + 2); }
+    for (int i = 0; i < N_SEGMENTS; ++i) { tc::mbar_init(bar(sm.q[i]), SOFTMAX_WARPS); tc::mbar_init(bar(sm.seg_full[i]), 1); tc::mbar_init(bar(sm.seg_empty[i]), SOFTMAX_WARPS + CONVERT_WARPS + 2); }
     tc::mbar_init(bar(sm.drain), 2);
     sm.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -603,17 +603,17 @@ shared_attention_kernel(const __grid_constant__ Params a) {
     // ================= products of one half =================
     const int t = warp - W_MMA;
     const uint32_t idesc_s = idesc_f16(M_ROWS, SUB, false), idesc_o = idesc_f16(M_ROWS, DP, true);
-    uint32_t phase = 0, p_phase = 0;
+    uint32_t p_phase = 0;
     int next_k = 0;                                            // the CTA's tiles in front of the segment
     bool ok = true;
     while (const Segment* s = ok ? segment() : nullptr) {
       const int n = __shfl_sync(0xffffffffu, s->t1 - s->t0, 0);      // (so that the compiler knows it to be the same in all lanes)
       const bool two = __shfl_sync(0xffffffffu, (int)s->two, 0) != 0;
       const int last_subs = __shfl_sync(0xffffffffu, s->keys > (s->t1 - 1) * KEYS + SUB ? 2 : 1, 0);      // steps of the last tile
+      // (A half without steps waits as well: nothing else would keep it from falling behind.)
+      ok = wait_warp(sm.q[seg.slot], seg.phase);
       done_with(seg.slot);
       seg.step(N_SEGMENTS);
-      ok = wait_warp(sm.q, phase);
-      phase ^= 1u;
       after_sync();
       // The half's tiles of keys: all of them for its rows (two), or every other one for the same rows; each in two steps of 64 keys, whose scores lie side by
       // side.  Scores two steps ahead; then, step by step, probabilities times values and the scores of two steps on: the softmax always finds some.
@@ -722,7 +722,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
       }
       to_async_proxy();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(sm.q));
+      if (lane == 0) mbar_arrive(bar(sm.q[seg.slot]));
     };
     auto store = [&](const Segment& x) {                        // results of the segment that has come to its end
       const int row = x.two ? half * M_ROWS + r : r;

@@ -255,3 +255,13 @@ def test_rows_that_were_given_up(idle):
     assert status == 0 and torch.equal(got, want)
     exact = model.attend(q.double().cpu().numpy(), offsets(new), [max(n, 0) for n in lens], True, 64 ** -0.5)
     assert (np.abs(got.double().cpu().numpy() - exact[0]) <= bound("bf16", *exact, max(ends), 64)).all()
+
+
+@pytest.mark.parametrize("dtype,dim,block", [("bf16", 64, 32), ("bf16", 128, 128), ("fp32", 32, 16)])
+def test_many_prefixes_of_one_tile(dtype, dim, block):
+    """One tile of keys after another, of as many groups: a half of a CTA that none of them gives any work keeps step with the other, call after call."""
+    G, heads = 150, 8
+    cache, q, out, (new, lens, first, shared, ends, causal) = check([2] * G, [128] * G, [b % 3 for b in range(2 * G)], [1] * (2 * G), heads, 1, dim, block, "int8", dtype, True, seed=11)
+    for _ in range(20):
+        again, status = run(cache, q.to(DEV), new, lens, first, shared, ends, causal)
+        assert status == 0 and torch.equal(again, out)
