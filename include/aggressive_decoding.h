@@ -434,15 +434,22 @@ typedef struct ad_kv_pool {
  * row can be) and stays as it was; one that asks for more than its parent holds gets what there is and latches AD_ERR_ARG. */
 int ad_cache_fork(const ad_kv_pool* pool, const int32_t* parent, const int32_t* len, int32_t B, int32_t* status, void* stream);
 
-/* Makes rows ready for an ad_cache_append of the same off [B + 1] and len [B]: every block that row b's off[b + 1] - off[b] new tokens will be written to
+/* Makes rows ready for an ad_cache_append_pooled of the same off [B + 1] and len [B]: every block that row b's off[b + 1] - off[b] new tokens will be written to
  * exists and belongs to this row alone.  Rows get blocks where they have none; a block that other rows hold as well is replaced by one of the row's own,
  * with the tokens in front of len[b] copied in all `n_caches` caches (0 .. 64; none: nothing is copied).  Where nobody else holds it, the first of the rows that write
  * a shared block keeps it.  Free blocks are taken in ascending order, for rows and for a row's blocks in order.  A pool without enough of them latches AD_ERR_CAPACITY and
- * stays as it is.  A row whose offsets or length make no sense, or that would pass its capacity, latches AD_ERR_ARG or AD_ERR_CAPACITY and is left alone.  Codes behind the copied
+ * stays as it is: rows go on sharing what they shared, which ad_cache_append_pooled respects without the host's doing, so that the sequence can be captured and *status read
+ * behind it.  (ad_cache_append knows nothing of counts and must not follow a refusal: rows would write the same block at once.)  A row whose offsets or length make no sense, or that
+ * would pass its capacity, latches AD_ERR_ARG or AD_ERR_CAPACITY and is left alone.  Codes behind the copied
  * tokens stay as they were.  scratch: ad_cache_reserve_scratch_bytes() of device memory, 256-byte aligned; calls that may overlap need scratch of their own. */
 size_t ad_cache_reserve_scratch_bytes(const ad_kv_pool* pool, int32_t B);
 int ad_cache_reserve(const ad_kv_pool* pool, const ad_kv_cache* caches, int32_t n_caches, const int32_t* off, const int32_t* len, int32_t B,
                      void* scratch, size_t scratch_bytes, int32_t* status, void* stream);
+
+/* ad_cache_append to one of the pool's caches.  A row that lacks a block for one of its new tokens, or that would write a block which other entries of the table name as
+ * well, latches AD_ERR_ARG and is left out as a whole; the others are written. */
+int ad_cache_append_pooled(const ad_kv_pool* pool, const ad_kv_cache* cache, const void* k, const void* v, int32_t dtype, int64_t token_stride, const int32_t* off,
+                           const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t* status, void* stream);
 
 /* Moves the blocks in use to the front of the pool: *n_used (device) receives their number, and those behind it go to the free ones in front of it, both
  * in ascending order, in all caches; the whole table (all `rows`) and refs follow.  Blocks from *n_used on are free afterwards and can be given to something else.  scratch as above. */

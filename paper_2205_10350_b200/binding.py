@@ -26,7 +26,7 @@ EXPORTS = [
     "ad_vocab_argmax_static", "ad_debug_graph_count", "ad_debug_projection_shapes", "ad_debug_wait_probe", "ad_debug_grid_barrier_probe",
     "ad_linear", "ad_cache_append", "ad_cache_read", "ad_cache_attention_scratch_bytes", "ad_cache_attention", "ad_accept_sampled_scratch_bytes",
     "ad_accept_sampled", "ad_cache_attention_shared_scratch_bytes", "ad_cache_attention_shared", "ad_cache_fork", "ad_cache_reserve_scratch_bytes",
-    "ad_cache_reserve", "ad_cache_compact_scratch_bytes", "ad_cache_compact", "ad_sample",
+    "ad_cache_reserve", "ad_cache_append_pooled", "ad_cache_compact_scratch_bytes", "ad_cache_compact", "ad_sample",
 ]
 
 
@@ -117,6 +117,7 @@ def load():
         "ad_cache_fork": (C.c_int, [pool, vp, vp, i32, vp, vp]),
         "ad_cache_reserve_scratch_bytes": (sz, [pool, i32]),
         "ad_cache_reserve": (C.c_int, [pool, cache, i32, vp, vp, i32, vp, sz, vp, vp]),
+        "ad_cache_append_pooled": (C.c_int, [pool, cache, vp, vp, i32, i64, vp, vp, i32, i32, i32, vp, vp]),
         "ad_cache_compact_scratch_bytes": (sz, [pool]),
         "ad_cache_compact": (C.c_int, [pool, cache, i32, vp, vp, sz, vp]),
         "ad_sample": (C.c_int, [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp]),
@@ -513,6 +514,8 @@ class KvCache:
     b * row_blocks .. (b + 1) * row_blocks - 1.  `tensors` = (k_codes, v_codes, k_scale, v_scale) adopts existing memory; otherwise
     the cache is allocated here."""
 
+    pool = None                         # the KvPool whose blocks it has
+
     def __init__(self, n_blocks, n_kv_heads, head_dim, block=32, fmt="e4m3", table=None, row_blocks=None, device="cuda:0", tensors=None):
         import torch
         _names()
@@ -572,7 +575,8 @@ class KvCache:
 
 
 def cache_append(cache, k_t, v_t, off_t, len_t, max_new, status_t=None):
-    """Writes k_t, v_t [M, n_kv_heads, head_dim] (float32 or bfloat16, views of a wider array as well) behind the len_t[b] tokens of every row."""
+    """Writes k_t, v_t [M, n_kv_heads, head_dim] (float32 or bfloat16, views of a wider array as well) behind the len_t[b] tokens of every row.
+    In a cache of a pool, rows that lack blocks for them, or would write blocks that other rows hold too (cache_reserve was refused or left out), are left as they are."""
     entry, lib = "ad_cache_append", _lib or load()
     if max_new >> 31:
         _refuse(entry, _TOO_LARGE)
@@ -581,8 +585,11 @@ def cache_append(cache, k_t, v_t, off_t, len_t, max_new, status_t=None):
     if cache._tokens(entry, v_t, cache.n_kv_heads) != tokens:
         _refuse(entry, "keys and values must agree in type, shape and stride")
     dtype, M, stride = tokens
-    rc = _call_on(cache._dev, lib.ad_cache_append, cache._ref, k_t.data_ptr(), v_t.data_ptr(), dtype, stride, off_t.data_ptr(), len_t.data_ptr(), B, M,
-                  max_new, _status_pointer(entry, cache._dev, status_t))
+    args = (k_t.data_ptr(), v_t.data_ptr(), dtype, stride, off_t.data_ptr(), len_t.data_ptr(), B, M, max_new, _status_pointer(entry, cache._dev, status_t))
+    if cache.pool is None:
+        rc = _call_on(cache._dev, lib.ad_cache_append, cache._ref, *args)
+    else:
+        rc = _call_on(cache._dev, lib.ad_cache_append_pooled, cache.pool._ref, cache._ref, *args)
     if rc != AD_OK:
         _raise(lib, rc)
 
@@ -701,6 +708,7 @@ class KvPool:
     def add_cache(self, n_kv_heads, head_dim, fmt="e4m3", tensors=None):
         """A cache (of one layer) on the pool's blocks and table; cache_reserve and cache_compact move its contents from now on."""
         cache = KvCache(self.n_blocks, n_kv_heads, head_dim, self.block, fmt, table=self.table, row_blocks=self.row_blocks, device=self.device, tensors=tensors)
+        cache.pool = self
         self.caches.append(cache)
         self._structs = (KvCacheStruct * len(self.caches))(*(c.struct for c in self.caches))
         return cache

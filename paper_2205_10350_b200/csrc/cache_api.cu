@@ -40,9 +40,8 @@ dim3 read_threads(const ad_kv_cache* c) { return dim3(std::max(32, c->block * c-
 
 }  // namespace
 
-extern "C" int ad_cache_append(const ad_kv_cache* c, const void* k, const void* v, int32_t dtype, int64_t token_stride, const int32_t* off,
-                               const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t* status, void* stream) {
-  const char* entry = "ad_cache_append";
+int ad::cache_append(const char* entry, const ad_kv_cache* c, const int32_t* refs, const void* k, const void* v, int32_t dtype, int64_t token_stride, const int32_t* off,
+                     const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t* status, void* stream) {
   if (const char* why = batch_fault(off, len, B, M, max_new)) return arg_fault(entry, why);
   if (const char* why = cache_fault(c, B)) return arg_fault(entry, why);
   if (!known_dtype(dtype)) return arg_fault(entry, "unknown dtype");
@@ -54,10 +53,16 @@ extern "C" int ad_cache_append(const ad_kv_cache* c, const void* k, const void* 
   const int tiles = tiles_a_cta(c, B, max_new);
   return launched(entry, by_types(dtype, c->format, [&](auto t) {
     typedef typename decltype(t)::Num T;
-    return launch_op(kv::cache_append_kernel<T, typename decltype(t)::Fmt>, tile_grid(c, B, max_new, tiles), tile_threads(c), dim3(), 0,
-                     static_cast<cudaStream_t>(stream), d, static_cast<const T*>(k), static_cast<const T*>(v), (size_t)token_stride,
+    auto kernel = refs ? kv::cache_append_kernel<T, typename decltype(t)::Fmt, true> : kv::cache_append_kernel<T, typename decltype(t)::Fmt, false>;
+    return launch_op(kernel, tile_grid(c, B, max_new, tiles), tile_threads(c), dim3(), 0,
+                     static_cast<cudaStream_t>(stream), d, refs, static_cast<const T*>(k), static_cast<const T*>(v), (size_t)token_stride,
                      (int)c->head_dim, off, len, (int)M, (int)max_new, tiles, status);
   }));
+}
+
+extern "C" int ad_cache_append(const ad_kv_cache* c, const void* k, const void* v, int32_t dtype, int64_t token_stride, const int32_t* off,
+                               const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t* status, void* stream) {
+  return cache_append("ad_cache_append", c, nullptr, k, v, dtype, token_stride, off, len, B, M, max_new, status, stream);
 }
 
 extern "C" int ad_cache_read(const ad_kv_cache* c, void* k, void* v, int32_t dtype, const int32_t* off, const int32_t* start, int32_t B, int32_t M,

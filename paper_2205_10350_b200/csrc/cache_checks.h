@@ -66,6 +66,9 @@ struct AttentionCall {
   float* mean;
   float2* weight;
 };
+// ad_cache_append for `entry`; refs: null, or counts by which rows that do not own what they would write are left out.
+int cache_append(const char* entry, const ad_kv_cache* c, const int32_t* refs, const void* k, const void* v, int32_t dtype, int64_t token_stride, const int32_t* off,
+                 const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t* status, void* stream);
 const char* cache_attention_fault(const ad_kv_cache* c, const AttentionCall& call);      // why it cannot be done, or null
 size_t cache_attention_scratch(const ad_kv_cache* c, int n_heads, int B, int max_new, int max_keys);
 cudaError_t cache_attention(const ad_kv_cache* c, const AttentionCall& call, void* scratch, cudaStream_t st);

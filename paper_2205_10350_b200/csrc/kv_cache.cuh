@@ -145,6 +145,8 @@ __device__ __forceinline__ void store8(bf16* p, const float* x) {
 // stay in registers between the maximum and the codes, so that everything is read and written once.  Bound by bytes: 8 prompts of 2500 to 8190
 // tokens, 8 heads of 128, BF16 to E4M3, 59 us, 4.5 TB/s (a tile a CTA 100 us, two 76, four 64, eight 64 in a build before); a third of the time the
 // issue slots are idle, in the barrier of each tile and its round trips.
+// POOLED: refs counts the entries of the table that name a block, and a row that lacks a block or would write one that others hold too is left out by all of its CTAs (one more
+// round trip: 32 rows of a token 6.6 -> 7.7 us, 32 of 32 7.3 -> 8.0, 8 of 4000 in blocks of 64 40 -> 42 and of 16 38 -> 45).
 // grid = (ceil(2 * heads / tiles), blocks a row's new tokens may touch, B), block = max(32, block * dim / 32) threads.
 constexpr int VECS = 4;                // vectors of eight numbers a thread holds
 __device__ __forceinline__ uint32_t max_bits(uint32_t m, uint4 v, float) {      // largest |x| as an integer: FP32 ...
@@ -156,9 +158,9 @@ __device__ __forceinline__ uint32_t max_bits(uint32_t m, uint4 v, bf16) {       
   m = __vmaxu2(m, v.z & 0x7fff7fffu);
   return __vmaxu2(m, v.w & 0x7fff7fffu);
 }
-template <typename T, typename F>
+template <typename T, typename F, bool POOLED>
 __global__ void __launch_bounds__(512)
-cache_append_kernel(Cache c, const T* __restrict__ k, const T* __restrict__ v, size_t stride, int dim, const int* __restrict__ off,
+cache_append_kernel(Cache c, const int* __restrict__ refs, const T* __restrict__ k, const T* __restrict__ v, size_t stride, int dim, const int* __restrict__ off,
                     const int* __restrict__ len, int M, int max_new, int tiles, int* status) {
   constexpr int WORDS = sizeof(T) / 2;                    // 16-byte words of a vector
   __shared__ uint32_t s_max[2][16];
@@ -189,6 +191,14 @@ cache_append_kernel(Cache c, const T* __restrict__ k, const T* __restrict__ v, s
   uint4 raw[VECS][WORDS], next[AHEAD ? VECS : 1][WORDS];
   load_new(first, AHEAD ? next : raw);                    // the new tokens do not wait for the table
   const int id = c.find(b, i);
+  if constexpr (POOLED) {
+    bool own = true;
+    for (int j = p / c.block + (int)threadIdx.x; j <= (p + n - 1) / c.block; j += blockDim.x) {
+      const int e = c.find(b, j);
+      own = own && e >= 0 && __ldcg(refs + e) <= 1;
+    }
+    if (!__syncthreads_and(own)) { latch_error(status, AD_ERR_ARG); return; }
+  }
   if (id < 0) { latch_error(status, AD_ERR_ARG); return; }
   for (int tile = first; tile < last; ++tile) {
     const int which = tile & 1, head = tile >> 1, turn = (tile - first) & 1;

@@ -107,6 +107,14 @@ extern "C" int ad_cache_reserve(const ad_kv_pool* p, const ad_kv_cache* caches, 
   return launched(entry, e);
 }
 
+extern "C" int ad_cache_append_pooled(const ad_kv_pool* p, const ad_kv_cache* c, const void* k, const void* v, int32_t dtype, int64_t token_stride,
+                                      const int32_t* off, const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t* status, void* stream) {
+  const char* entry = "ad_cache_append_pooled";
+  if (const char* why = pool_fault(p, B)) return arg_fault(entry, why);
+  if (const char* why = layers_fault(p, c, 1)) return arg_fault(entry, why);
+  return cache_append(entry, c, p->refs, k, v, dtype, token_stride, off, len, B, M, max_new, status, stream);
+}
+
 extern "C" size_t ad_cache_compact_scratch_bytes(const ad_kv_pool* p) {
   if (pool_fault(p, 1)) return 0;
   return rounded(2 * (size_t)p->n_blocks * sizeof(int)) + rounded((size_t)p->n_blocks * sizeof(int)) + rounded(sizeof(int)) +

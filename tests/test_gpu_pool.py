@@ -296,3 +296,58 @@ def test_empty_and_adopted_pools():
     assert int(binding.cache_compact(adopted).item()) == 2
     assert table.tolist() == [[0, 1], [0, -1]] or table.tolist() == [[1, 0], [1, -1]]
     assert refs.tolist()[:2] in ([2, 1], [1, 2]) and refs.tolist()[2:] == [0, 0, 0]
+
+
+def contents(pool):
+    return [x.clone() for c in pool.caches for x in (c.k_codes.view(torch.uint8), c.v_codes.view(torch.uint8), c.k_scale, c.v_scale)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("captured", [False, True])
+def test_what_follows_a_refused_reservation_writes_nothing(captured, dtype):
+    """Rows that share a partly filled block, and one that lacks its next, go on in a pool that is too small: reserve and append of all layers, one after the other as a program that
+    does not look in between runs them, leave every row's tokens as they were.  Once there is room the same calls write what the plain append writes."""
+    pool, model = both(5, 4, 4, 16, [(2, 64, "e4m3"), (1, 32, "int8"), (3, 128, "e4m3")])
+    st, g = status(), torch.Generator().manual_seed(3)
+    numbers = {c: [torch.randn((64, c.n_kv_heads, c.head_dim), generator=g).to(dtype).to(DEV) for _ in range(2)] for c in pool.caches}
+    appended = lambda new, lens: [binding.cache_append(c, *(x[: sum(new)] * 50 for x in numbers[c]), ints(offsets(new)), ints(lens), max(new), st) for c in pool.caches]
+    for new, lens in (([21, 0, 0, 0, 0], [0] * 5), ([0, 0, 0, 0, 16], [21, 0, 0, 0, 0])):
+        binding.cache_reserve(pool, ints(offsets(new)), ints(lens), st)
+        appended(new, lens)
+    parent, lens = [0, 0, 0, 0, 4], [21] * 4 + [16]
+    binding.cache_fork(pool, ints(parent), ints(lens), st)
+    assert int(st.item()) == 0 and pool.refs.tolist() == [4, 4, 1, 0]
+    before, off_t, len_t, new = contents(pool), ints(offsets([1] * 5)), ints(lens), [1] * 5
+
+    def step():
+        binding.cache_reserve(pool, off_t, len_t, st)
+        for c in pool.caches:
+            binding.cache_append(c, *(x[:5] for x in numbers[c]), off_t, len_t, 1, st)
+    call = step
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        call = graph.replay
+    for _ in range(2):
+        call()
+        assert int(st.item()) == binding.AD_ERR_CAPACITY
+        assert all(torch.equal(a, b) for a, b in zip(contents(pool), before))
+    # without a reservation at all, and a row that owns the first block it would write but lacks the next
+    for new, at in (([1] * 5, lens), ([0, 0, 0, 0, 20], [21] * 4 + [10]), ([3, 1, 0, 0, 0], lens)):
+        st.zero_()
+        appended(new, at)
+        assert int(st.item()) == binding.AD_ERR_ARG and all(torch.equal(a, b) for a, b in zip(contents(pool), before))
+    # room for all that is left: what the plain append makes of the same blocks
+    st.zero_()
+    binding.cache_fork(pool, ints([0, -1, -1, -1, 4]), ints([21, 0, 0, 0, 16]), st)
+    off_t.copy_(ints(offsets([1, 0, 0, 0, 1])))
+    len_t.copy_(ints([21, 0, 0, 0, 16]))
+    plain = [binding.KvCache(4, c.n_kv_heads, c.head_dim, 16, c.fmt, row_blocks=4, table=ints([[0, 1, -1, -1]] + [[-1] * 4] * 3 + [[2, 3, -1, -1]]), device=DEV,
+                             tensors=[x.clone() for x in (c.k_codes, c.v_codes, c.k_scale, c.v_scale)]) for c in pool.caches]
+    call()
+    for c, p in zip(pool.caches, plain):
+        binding.cache_append(p, *(x[:5] for x in numbers[c]), off_t, len_t, 1)
+        assert torch.equal(pool.table, p.table)
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip((c.k_codes, c.v_codes, c.k_scale, c.v_scale), (p.k_codes, p.v_codes, p.k_scale, p.v_scale)))
+    assert int(st.item()) == 0 and not all(torch.equal(a, b) for a, b in zip(contents(pool), before))

@@ -220,3 +220,22 @@ def test_what_kernels_decide_by(tmp_path):
     subprocess.run([NVCC, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+APPEND_POOLED = dict(k=P, v=P, dtype=1, stride=128, off=P, len=P, B=3, M=5, max_new=3)
+
+
+@pytest.mark.parametrize("bad", [dict(off=None), dict(len=None), dict(B=0), dict(B=7), dict(M=-1), dict(max_new=0), dict(max_new=1 << 20), dict(dtype=2), dict(k=None), dict(v=P + 8),
+                                 dict(stride=120), dict(stride=130)])
+def test_pooled_append_refusals(lib, bad):
+    _refused(lib, lib.ad_cache_append_pooled(_pool(), C.byref(_cache()), *{**APPEND_POOLED, **bad}.values(), None, None))
+
+
+def test_pooled_append_of_pools_and_caches_that_do_not_belong_together(lib):
+    for bad in BAD_POOL:
+        _refused(lib, lib.ad_cache_append_pooled(_pool(**bad), C.byref(_cache()), *APPEND_POOLED.values(), None, None))
+    for bad in [b for b in BAD_CACHE if "table" not in b] + [dict(table=None), dict(table=P + 4), dict(table_stride=5), dict(n_blocks=9), dict(block=64)]:
+        _refused(lib, lib.ad_cache_append_pooled(_pool(), C.byref(_cache(**bad)), *APPEND_POOLED.values(), None, None))
+    _refused(lib, lib.ad_cache_append_pooled(None, C.byref(_cache()), *APPEND_POOLED.values(), None, None))
+    _refused(lib, lib.ad_cache_append_pooled(_pool(), None, *APPEND_POOLED.values(), None, None))
+    assert lib.ad_cache_append_pooled(_pool(), C.byref(_cache()), *{**APPEND_POOLED, "M": 0, "k": None, "v": None}.values(), None, None) == binding.AD_OK
