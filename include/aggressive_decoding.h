@@ -404,7 +404,8 @@ int ad_accept_sampled(const void* target, int64_t target_stride, const void* dra
  * that ad_cache_fork made from one, or that look at one encoder's keys.  The whole blocks among these positions may be read once for the group, through the table of its
  * first row that brings tokens; the rest is read through each row's own table, which must be in order
  * throughout.  Whether they are is decided by the sizes that the host gives, by what it saves; the result differs by roundings alone.  Otherwise arguments, result and
- * precision are those of ad_cache_attention.  max_shared: longest prefix to plan for; longer ones are computed as well, only slower.  Where positions are read once,
+ * precision are those of ad_cache_attention.  max_shared: longest prefix, by which the decision goes (0: rows one by one); longer ones are computed as well, and groups may share less,
+ * or nothing: every row is planned to have up to max_keys positions of its own.  Where positions are read once,
  * rows of a group that does not lie in ascending order within 0 .. B, or with shared[g] below 0 or beyond a row's capacity, and rows with fewer than shared[g]
  * positions latch AD_ERR_ARG and are left out; where they are not, groups are not looked at.  At most 8192 rows, and M * n_heads at most 2^30. */
 size_t ad_cache_attention_shared_scratch_bytes(const ad_kv_cache* cache, int32_t dtype, int32_t n_heads, int32_t B, int32_t M, int32_t max_new,

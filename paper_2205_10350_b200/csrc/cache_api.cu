@@ -93,15 +93,16 @@ struct AttendPlan { int nq, row_tiles, grid, granule; bool shared; };
 int32_t longest_row(const ad_kv_cache* c, int32_t max_keys) { return std::min(max_keys, c->table_stride * c->block); }
 // Rows of queries a CTA takes: 8 or 16 where that is all there are, else 32, which make the most of a key's codes once they are FP16.  Keys that are
 // too few to be split leave the GPU to as many CTAs as there are tiles of rows: then tiles are made smaller while all are resident at once
-// (8 x 25 queries in FP32 over 400 keys, 8 heads: 14.4 -> 10.3 us).
-AttendPlan attend_plan(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
+// (8 x 25 queries in FP32 over 400 keys, 8 heads: 14.4 -> 10.3 us).  So they are where rows may be long but are likely to be short (`own`: what is left of them behind a prefix that
+// others share: 2 x 8 rows of 5 queries, 32 heads on 8, of 300 keys beside the prefix's work 87 -> 83 us; with one of 16000 among them 107 both ways).
+AttendPlan attend_plan(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys, bool own) {
   AttendPlan plan;
   max_keys = longest_row(c, max_keys);
   const int rows = max_new * (n_heads / c->n_kv_heads), pieces = std::max(1, (max_keys + kv::UNIT - 1) / kv::UNIT / kGranule);
   auto items = [&](int nq) { return (int64_t)B * c->n_kv_heads * ((rows + 8 * nq - 1) / (8 * nq)); };
   auto resident = [&](int nq) { return (int64_t)op_num_sms() * kv::att_resident(c->head_dim, nq); };
   plan.nq = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
-  while (pieces == 1 && plan.nq > 1 && items(plan.nq / 2) <= resident(plan.nq / 2)) plan.nq /= 2;
+  while ((own || pieces == 1) && plan.nq > 1 && items(plan.nq / 2) <= resident(plan.nq / 2)) plan.nq /= 2;
   plan.row_tiles = (rows + 8 * plan.nq - 1) / (8 * plan.nq);
   plan.granule = pieces > 1 ? kGranule : 0;
   plan.grid = (int)std::min(resident(plan.nq), std::min(resident(plan.nq), items(plan.nq)) * pieces);     // (items times pieces alone may pass 64 bits)
@@ -142,7 +143,7 @@ cudaError_t launch_join(const kv::AttendParams& a, const AttendPlan& plan, cudaS
 template <typename T, typename F, int DIM, int NQ>
 cudaError_t launch_attention(const kv::AttendParams& a, const AttendPlan& plan, cudaStream_t st) {
   const cudaError_t e = a.c.block == 16 ? launch_attention_part<T, F, DIM, NQ, true>(a, st) : launch_attention_part<T, F, DIM, NQ, false>(a, st);
-  return e == cudaSuccess ? launch_join<T, DIM, NQ>(a, plan, st) : e;
+  return e == cudaSuccess && !a.mean ? launch_join<T, DIM, NQ>(a, plan, st) : e;
 }
 template <typename T, typename F, int DIM>
 cudaError_t launch_attention_dim(const kv::AttendParams& a, const AttendPlan& plan, cudaStream_t st) {
@@ -150,20 +151,24 @@ cudaError_t launch_attention_dim(const kv::AttendParams& a, const AttendPlan& pl
 }
 }  // namespace
 
-size_t ad::cache_attention_scratch(const ad_kv_cache* c, int n_heads, int B, int max_new, int max_keys) {
-  return attend_part_bytes(c, attend_plan(c, n_heads, B, max_new, max_keys), B);
+size_t ad::cache_attention_scratch(const ad_kv_cache* c, int n_heads, int B, int max_new, int max_keys, bool own) {
+  return attend_part_bytes(c, attend_plan(c, n_heads, B, max_new, max_keys, own), B);
+}
+kv::Parts ad::cache_attention_parts(const ad_kv_cache* c, const AttentionCall& call, void* scratch) {
+  const AttendPlan plan = attend_plan(c, call.n_heads, call.B, call.max_new, call.max_keys, call.mean);
+  return kv::Parts{reinterpret_cast<float*>(static_cast<char*>(scratch) + attend_prefix_bytes(call.B)), static_cast<long long*>(scratch), plan.grid, 8 * plan.nq, kItemFixed, plan.granule};
 }
 cudaError_t ad::cache_attention(const ad_kv_cache* c, const AttentionCall& call, void* scratch, cudaStream_t st) {
-  const AttendPlan plan = attend_plan(c, call.n_heads, call.B, call.max_new, call.max_keys);
+  const AttendPlan plan = attend_plan(c, call.n_heads, call.B, call.max_new, call.max_keys, call.mean);
   kv::AttendParams a;
   a.c = device_cache(c); a.c.first = call.first;
   a.q = call.q; a.q_stride = (size_t)call.q_stride; a.out = call.out; a.n_heads = call.n_heads; a.M = call.M; a.max_new = call.max_new; a.off = call.off; a.len = call.len;
-  a.causal = call.causal; a.scale = call.scale * (float)M_LOG2E; a.status = call.status; a.mean = call.mean; a.weight = call.weight;
+  a.causal = call.causal; a.scale = call.scale * (float)M_LOG2E; a.status = call.status; a.mean = call.mean; a.weight = call.weight; a.whole = call.whole;
   // More than half of L2 would not be there any more for the next call, and drives out what others keep there (1 x 200001 keys 104 -> 91 us); tiles of
   // the same row read one another's keys from L2.
   a.stream_once = plan.row_tiles == 1 && (double)call.B * longest_row(c, call.max_keys) * c->n_kv_heads * c->head_dim * 2 > (64 << 20);
-  a.B = call.B; a.grid = plan.grid; a.granule = plan.granule; a.fixed = kItemFixed;
-  a.prefix = static_cast<long long*>(scratch); a.part = reinterpret_cast<float*>(static_cast<char*>(scratch) + attend_prefix_bytes(call.B));
+  const kv::Parts parts = cache_attention_parts(c, call, scratch);
+  a.B = call.B; a.grid = plan.grid; a.granule = plan.granule; a.fixed = kItemFixed; a.prefix = const_cast<long long*>(parts.prefix); a.part = const_cast<float*>(parts.part);
   return by_types(call.dtype, c->format, [&](auto t) {
     typedef typename decltype(t)::Num T;
     typedef typename decltype(t)::Fmt F;
@@ -174,7 +179,7 @@ cudaError_t ad::cache_attention(const ad_kv_cache* c, const AttentionCall& call,
 
 extern "C" size_t ad_cache_attention_scratch_bytes(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t max_new, int32_t max_keys) {
   if (cache_fault(c, B) || B < 1 || max_new < 1 || max_keys < 0 || !known_dtype(dtype) || !attend_sizes(c, n_heads, max_new)) return 0;
-  return cache_attention_scratch(c, n_heads, B, max_new, max_keys);
+  return cache_attention_scratch(c, n_heads, B, max_new, max_keys, false);
 }
 
 const char* ad::cache_attention_fault(const ad_kv_cache* c, const AttentionCall& call) {
@@ -195,10 +200,10 @@ extern "C" int ad_cache_attention(const ad_kv_cache* c, const void* q, int32_t d
                                   const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, int32_t causal, float scale, void* out,
                                   void* scratch, size_t scratch_bytes, int32_t* status, void* stream) {
   const char* entry = "ad_cache_attention";
-  const AttentionCall call = {q, dtype, q_stride, n_heads, off, len, B, M, max_new, max_keys, causal != 0, scale, out, status, nullptr, nullptr, nullptr};
+  const AttentionCall call = {q, dtype, q_stride, n_heads, off, len, B, M, max_new, max_keys, causal != 0, scale, out, status, nullptr, nullptr, nullptr, nullptr};
   if (const char* why = cache_attention_fault(c, call)) return arg_fault(entry, why);
   if (M == 0) return AD_OK;
-  const size_t need = cache_attention_scratch(c, n_heads, B, max_new, max_keys);
+  const size_t need = cache_attention_scratch(c, n_heads, B, max_new, max_keys, false);
   if (scratch_bytes < need) return op_fail(AD_ERR_CAPACITY, entry, "scratch too small");
   if (need && (!scratch || !aligned(scratch, 256))) return arg_fault(entry, "scratch must be 256-byte aligned");
   return launched(entry, cache_attention(c, call, scratch, static_cast<cudaStream_t>(stream)));

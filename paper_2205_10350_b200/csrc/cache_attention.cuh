@@ -26,9 +26,10 @@ struct AttendParams {
   int granule;             // units that one CTA works on at the least where a row's keys are split; 0: they are not
   float* part;             // [2 grid][tile rows][dim] means of values, then [2 grid][tile rows] maxima and sums of exponentials
   long long* prefix;       // [B + 1] granules in front of each row of the batch
-  // Not null: results go here instead of out, means of values [M, n_heads, dim] and maxima and sums of exponentials [M, n_heads], to be joined with others.
+  // Not null: results of whole items go here instead of out, means of values [M, n_heads, dim] and maxima and sums of exponentials [M, n_heads], and parts stay where they are, to be joined with others.
   float* mean;
   float2* weight;
+  const int* whole;        // not null and not zero there: no row's keys are split after all
 };
 
 constexpr int UNIT = 32;               // keys that a warp works on at a time
@@ -54,10 +55,11 @@ struct RowWork {
 __device__ __forceinline__ RowWork row_work(const AttendParams& a, int b, int tile_rows) {
   RowWork w;
   w.granules = 0;
+  const bool split = a.granule && !(a.whole && __ldcg(a.whole));      // (loaded along with the offsets)
   if (!row_tokens(a.c, a.off, a.len, b, a.M, a.max_new, !a.causal, a.status, w.o, w.n, w.p)) return w;
   w.tiles = (w.n * (a.n_heads / a.c.heads) + tile_rows - 1) / tile_rows;
   w.units = (w.p + (a.causal ? w.n : 0) + UNIT - 1) / UNIT;
-  w.pieces = a.granule ? (w.units + a.fixed + a.granule / 2) / a.granule : 1;
+  w.pieces = split ? (w.units + a.fixed + a.granule / 2) / a.granule : 1;
   w.granules = (long long)a.c.heads * w.tiles * w.pieces;
   return w;
 }
@@ -815,7 +817,7 @@ cache_attention_join_kernel(AttendParams a) {
   const int rr = r % ROWS;
   auto row_of = [&](int i) { return (size_t)(i == 0 ? slot0 : 2 * (c0 + i)) * ROWS + rr; };
   const float2* ml = reinterpret_cast<const float2*>(a.part + 2 * (size_t)a.grid * ROWS * DIM);
-  float sum = 0.f, most = -INFINITY;
+  float sum = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](float4 y, float f) { x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w); };
   if constexpr (SHARED) {
@@ -835,7 +837,6 @@ cache_attention_join_kernel(AttendParams a) {
     if (lane == 0) s_red[0][tid >> 5] = top;
     __syncthreads();
     top = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
-    most = top;
     for (int i = tid; i < parts; i += 128) {
       if (i > tid) v = __ldcg(ml + row_of(i));
       const float f = v.y == 0.f ? 0.f : v.x == top ? v.y : v.y * ex2(v.x - top);      // (no key: nothing, whatever the maxima)
@@ -864,7 +865,7 @@ cache_attention_join_kernel(AttendParams a) {
     for (int i = 0; i < parts; ++i) {
       const float2 v = __ldcg(ml + row_of(i));
       if (v.y == 0.f) continue;                  // (no key: nothing, whatever the maxima)
-      most = fmaxf(top, v.x);
+      const float most = fmaxf(top, v.x);
       sum = v.x == top ? sum + v.y : fmaf(sum, ex2(top - most), v.x == most ? v.y : v.y * ex2(v.x - most));
       top = most;
     }
@@ -877,13 +878,7 @@ cache_attention_join_kernel(AttendParams a) {
       add(y, (v.x == top ? v.y : v.y * ex2(v.x - top)) * inv);
     }
   }
-  const size_t at = (size_t)(work.o + r / group) * a.n_heads + kvh * group + r % group;
-  if (a.mean) {
-    *reinterpret_cast<float4*>(a.mean + at * DIM + d0) = x;
-    if (d0 == 0) a.weight[at] = make_float2(most, sum);
-    return;
-  }
-  T* out = static_cast<T*>(a.out) + at * DIM + d0;
+  T* out = static_cast<T*>(a.out) + ((size_t)(work.o + r / group) * a.n_heads + kvh * group + r % group) * DIM + d0;
   if constexpr (sizeof(T) == 4) {
     *reinterpret_cast<float4*>(out) = x;
   } else {

@@ -50,7 +50,8 @@ inline int arg_fault(const char* entry, const char* why) { return op_fail(AD_ERR
 inline int launched(const char* entry, cudaError_t e) { return e == cudaSuccess ? AD_OK : op_fail(AD_ERR_CUDA, entry, cudaGetErrorString(e)); }
 
 // The attention over a cache, as its entry point gets it, and as a part of others'.  first (null: none): blocks in front of what each row looks at.  mean and weight
-// (null: results go to out): means of values [M, n_heads, head_dim], and maxima of the scores (times log2 e) and sums of exponentials [M, n_heads].
+// (null: results go to out): means of values [M, n_heads, head_dim], and maxima of the scores (times log2 e) and sums of exponentials [M, n_heads], of items that one CTA worked on; the
+// others' parts are where cache_attention_parts says.  whole (null: no such word): not zero on the device, rows are not split, although max_keys would have it.
 struct AttentionCall {
   const void* q;
   int32_t dtype;
@@ -65,12 +66,14 @@ struct AttentionCall {
   const int32_t* first;
   float* mean;
   float2* weight;
+  const int32_t* whole;
 };
 // ad_cache_append for `entry`; refs: null, or counts by which rows that do not own what they would write are left out.
 int cache_append(const char* entry, const ad_kv_cache* c, const int32_t* refs, const void* k, const void* v, int32_t dtype, int64_t token_stride, const int32_t* off,
                  const int32_t* len, int32_t B, int32_t M, int32_t max_new, int32_t* status, void* stream);
 const char* cache_attention_fault(const ad_kv_cache* c, const AttentionCall& call);      // why it cannot be done, or null
-size_t cache_attention_scratch(const ad_kv_cache* c, int n_heads, int B, int max_new, int max_keys);
+size_t cache_attention_scratch(const ad_kv_cache* c, int n_heads, int B, int max_new, int max_keys, bool own);      // own: with call.mean
+kv::Parts cache_attention_parts(const ad_kv_cache* c, const AttentionCall& call, void* scratch);
 cudaError_t cache_attention(const ad_kv_cache* c, const AttentionCall& call, void* scratch, cudaStream_t st);
 
 }  // namespace ad

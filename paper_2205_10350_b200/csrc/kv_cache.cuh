@@ -64,6 +64,13 @@ struct Cache {
   }
 };
 
+// Where the attention leaves parts of items that more than one CTA worked on.
+struct Parts {
+  const float* part;             // [2 grid][tile rows][dim] means of values, then [2 grid][tile rows] maxima and sums of exponentials
+  const long long* prefix;       // [B + 1] granules in front of each row of the batch
+  int grid, tile_rows, fixed, granule;
+};
+
 // Whether a row's n tokens o .. o + n - 1 of M can go to positions p .. of it (in_row = n), or look at its first p (in_row = 0): AD_OK or what is wrong.
 __host__ __device__ __forceinline__ int row_fault(const Cache& c, int o, int n, int p, int M, int max_new, int in_row) {
   if (o < 0 || n < 0 || n > max_new || o > M - n || p < 0) return AD_ERR_ARG;

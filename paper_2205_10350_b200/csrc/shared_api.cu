@@ -15,13 +15,12 @@ constexpr int kSharedRows = 8192;
 
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Most positions that a row may have of its own, to plan for.
-int32_t own_keys(int32_t max_keys, int32_t max_shared, int32_t block) { return (int32_t)std::max<int64_t>(block, std::min<int64_t>(max_keys, (int64_t)max_keys - max_shared + block)); }
-
 struct Scratch { size_t total, lines, start, first, len, ml, part, own_ml, own_part, rows, bytes; long long part_rows; int grid; };
 // Results of the groups' items: of every query and head, and as much as an item's between the CTAs' parts, twice (either half of the keys); those of the rows' own
-// positions; and what the attention row by row wants.
-Scratch scratch_of(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, int32_t G, int32_t max_shared) {
+// positions; and what the attention row by row wants, which is planned for rows of max_keys of their own: groups need not share max_shared positions, nor any.  (Planned for max_keys - max_shared, a
+// row of 32000 that shared nothing was not split beside 64 rows behind 32000: 729 us instead of 114, row by row 525.)  That no row is long after all is found out on the device, and nothing
+// is split then.
+Scratch scratch_of(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, int32_t G) {
   Scratch s;
   const size_t mh = (size_t)M * n_heads;
   s.grid = op_num_sms();
@@ -36,7 +35,7 @@ Scratch scratch_of(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t M, 
   s.own_ml = s.part + rounded(2 * (size_t)s.part_rows * c->head_dim * sizeof(float));
   s.own_part = s.own_ml + rounded(mh * sizeof(float2));
   s.rows = s.own_part + rounded(mh * c->head_dim * sizeof(float));
-  s.bytes = s.rows + rounded(cache_attention_scratch(c, n_heads, B, max_new, own_keys(max_keys, max_shared, c->block)));
+  s.bytes = s.rows + rounded(cache_attention_scratch(c, n_heads, B, max_new, max_keys, true));
   return s;
 }
 // Whether the groups' positions are read once for all rows.  That saves units of 32 keys for 32 rows of queries and a key/value head, and costs the plan, a second pass over the rows and the join:
@@ -93,7 +92,7 @@ extern "C" size_t ad_cache_attention_shared_scratch_bytes(const ad_kv_cache* c, 
   if (shared_fault(n_heads, B, M, G, max_shared)) return 0;
   const size_t alone = ad_cache_attention_scratch_bytes(c, dtype, n_heads, B, max_new, max_keys);
   if (cache_fault(c, B) || !known_dtype(dtype) || max_new < 1 || max_keys < 0 || n_heads % c->n_kv_heads) return 0;
-  return worth_sharing(c, dtype, n_heads, B, M, max_new, max_keys, G, max_shared) ? scratch_of(c, n_heads, B, M, max_new, max_keys, G, max_shared).bytes : alone;
+  return worth_sharing(c, dtype, n_heads, B, M, max_new, max_keys, G, max_shared) ? scratch_of(c, n_heads, B, M, max_new, max_keys, G).bytes : alone;
 }
 
 extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads, const int32_t* off,
@@ -101,7 +100,7 @@ extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, in
                                          const int32_t* shared, int32_t G, int32_t max_shared, int32_t causal, float scale, void* out, void* scratch,
                                          size_t scratch_bytes, int32_t* status, void* stream) {
   const char* entry = "ad_cache_attention_shared";
-  AttentionCall call = {q, dtype, q_stride, n_heads, off, len, B, M, max_new, max_keys, causal != 0, scale, out, status, nullptr, nullptr, nullptr};
+  AttentionCall call = {q, dtype, q_stride, n_heads, off, len, B, M, max_new, max_keys, causal != 0, scale, out, status, nullptr, nullptr, nullptr, nullptr};
   if (const char* why = cache_attention_fault(c, call)) return arg_fault(entry, why);
   if (!group || !shared) return arg_fault(entry, "null groups");
   if (const char* why = shared_fault(n_heads, B, M, G, max_shared)) return arg_fault(entry, why);
@@ -111,7 +110,7 @@ extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, in
   if (need && (!scratch || !aligned(scratch, 256))) return arg_fault(entry, "scratch must be 256-byte aligned");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (!worth_sharing(c, dtype, n_heads, B, M, max_new, max_keys, G, max_shared)) return launched(entry, cache_attention(c, call, scratch, st));
-  const Scratch s = scratch_of(c, n_heads, B, M, max_new, max_keys, G, max_shared);
+  const Scratch s = scratch_of(c, n_heads, B, M, max_new, max_keys, G);
   char* at = static_cast<char*>(scratch);
   shr::Params a = {};
   a.c = device_cache(c); a.q = q; a.q_stride = (size_t)q_stride; a.out = out; a.n_heads = n_heads; a.M = M; a.max_new = max_new; a.B = B; a.G = G;
@@ -121,7 +120,8 @@ extern "C" int ad_cache_attention_shared(const ad_kv_cache* c, const void* q, in
   a.own_first = reinterpret_cast<int*>(at + s.first); a.own_len = reinterpret_cast<int*>(at + s.len);
   a.ml = reinterpret_cast<float2*>(at + s.ml); a.part = reinterpret_cast<float*>(at + s.part);
   a.own_ml = reinterpret_cast<float2*>(at + s.own_ml); a.own_part = reinterpret_cast<float*>(at + s.own_part);
-  call.first = a.own_first; call.len = a.own_len; call.max_keys = own_keys(max_keys, max_shared, c->block); call.mean = a.own_part; call.weight = a.own_ml;
+  call.first = a.own_first; call.len = a.own_len; call.mean = a.own_part; call.weight = a.own_ml; call.whole = &a.total->own_whole;
+  a.own = cache_attention_parts(c, call, at + s.rows);
   auto rows = [&] { return cache_attention(c, call, at + s.rows, st); };
   const int dim = c->head_dim;
   cudaError_t e;

@@ -25,7 +25,10 @@ struct Line {
 };
 static_assert(sizeof(Line) == 64, "four 16-byte loads");
 struct Start { int line, pad; long long at; };
-struct Total { long long all, each; };  // granules of all lines; of a CTA, in order (the last ones may get fewer, or none)
+struct Total {
+  long long all, each;                 // granules of all lines; of a CTA, in order (the last ones may get fewer, or none)
+  int own_whole;                       // no row has so many positions of its own that they are split
+};
 
 struct Params {
   Cache c;
@@ -50,14 +53,18 @@ struct Params {
   int* own_len;
   float2* ml;                          // [2][part_rows] maxima and sums
   float* part;                         // [2][part_rows][dim] means of values
-  float2* own_ml;                      // [M][n_heads] the same of the rows' own positions
+  float2* own_ml;                      // [M][n_heads] the same of the rows' own positions, where one CTA worked on them
   float* own_part;                     // [M][n_heads][dim]
+  kv::Parts own;                       // ... and where several did
 };
 
 constexpr int FIXED = 3;
 __host__ __device__ __forceinline__ int key_tiles(int keys) { return (keys + KEYS - 1) / KEYS; }
 // The tile that granule x of an item starts with.
 __host__ __device__ __forceinline__ int tile_at(int x, int weight) { return x <= FIXED ? 0 : (x - FIXED + weight - 1) >> (weight - 1); }
+
+// Units of keys that a row has of its own.
+__device__ __forceinline__ int own_units(const Params& a, int len, int n) { return (len + (a.causal ? n : 0) + kv::UNIT - 1) / kv::UNIT; }
 
 // ---- plan ----------------------------------------------------------------------------------------------------------
 constexpr int PLAN_THREADS = 256;
@@ -106,6 +113,7 @@ shared_plan_kernel(const __grid_constant__ Params a) {
   pdl_wait();
   const int per_kv = a.n_heads / a.c.heads, tid = threadIdx.x;
   // rows: which group they are of, and what is left for the attention row by row
+  bool own_long = false;
   for (int b = tid; b < a.B; b += PLAN_THREADS) {
     Line x = {};
     int lo = 0, hi = a.G - 1;                                // the last group that starts at b or in front of it
@@ -123,6 +131,7 @@ shared_plan_kernel(const __grid_constant__ Params a) {
       if (group_of(a, lo, first, last, go, gn, keys) && first <= b && b < last && keys <= p && x.o >= go && x.o + x.n <= go + gn) {
         a.own_first[b] = keys / a.c.block;
         a.own_len[b] = p - keys / a.c.block * a.c.block;
+        own_long = own_long || own_units(a, a.own_len[b], x.n) >= 2 * a.own.granule;
       } else {
         latch_error(a.status, AD_ERR_ARG);
         x.n = 0;
@@ -132,6 +141,7 @@ shared_plan_kernel(const __grid_constant__ Params a) {
     }
     a.lines[a.G + b] = x;
   }
+  own_long = __syncthreads_or(own_long);
   long long granules_front = 0, tokens_front = 0;
   for (int l0 = 0; l0 < a.G; l0 += PLAN_THREADS) {
     const int l = l0 + tid;
@@ -167,7 +177,7 @@ shared_plan_kernel(const __grid_constant__ Params a) {
     tokens_front += all_t;
   }
   const long long total = granules_front, each = (total + a.grid - 1) / a.grid;
-  if (tid == 0) *a.total = Total{total, each};
+  if (tid == 0) *a.total = Total{total, each, !own_long};
   __syncthreads();
   for (int c = tid; c * each < total; c += PLAN_THREADS) {   // where each CTA starts: in the last line that has begun there
     const long long g = c * each;
@@ -942,7 +952,7 @@ shared_attention_kernel(const __grid_constant__ Params a) {
   if (warp == W_MMA) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
 }
 
-// Joins the parts of every query: of its group's items, and of its row's own positions, with out = sum of mean_i s_i 2^(m_i - m) / sum of s_i 2^(m_i - m).  A warp a query and head.
+// Joins the parts of every query: of its group's items, and of its row's own positions (one, or what several CTAs of the attention row by row left), with out = sum of mean_i s_i 2^(m_i - m) / sum of s_i 2^(m_i - m).  A warp a query and head.
 // Bound by latency: lines, maxima, means, one after another; five means under way and four CTAs an SM: 600 queries of 32 heads with 2 to 4 parts each 23 us, 64 with 20 parts 11 us.  (Eight
 // means and three CTAs: 33 and 9.7; with the parts' borders by 64-bit divisions besides: 34 and 12.5.)
 // grid = (enough for max_new * n_heads warps, B), block = JOIN_THREADS.
@@ -968,38 +978,53 @@ shared_join_kernel(const __grid_constant__ Params a) {
     else y[0] = __ldcg(p);
   };
   const Line row = load_line(a.G + b);
+  const int own_len = __ldcg(a.own_len + b), own_whole = __ldcg(&a.total->own_whole);
   if ((long long)blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5) >= (long long)row.n * a.n_heads) return;      // (below 2^30)
   const int w = blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5), i = w / a.n_heads, head = w - i * a.n_heads, kvh = head / per_kv;
-  // the row's own positions
-  const size_t own = (size_t)(row.o + i) * a.n_heads + head;
-  const float2 mine = __ldcg(a.own_ml + own);
-  float x[PER];
-  load(a.own_part + own * DIM, x);
   const Line grp = load_line(row.group);
+  // the row's own positions, by one CTA or several
+  const size_t own = (size_t)(row.o + i) * a.n_heads + head;
+  const int r_own = i * per_kv + head % per_kv, pieces = a.own.granule && !own_whole ? (own_units(a, own_len, row.n) + a.own.fixed + a.own.granule / 2) / a.own.granule : 1;
+  int own0 = 0, slot0 = 0, own_parts = 1;
+  if (pieces > 1) {
+    const long long total = __ldcg(a.own.prefix + a.B), ctas = min((long long)a.own.grid, total);
+    const long long first = __ldcg(a.own.prefix + b) + ((long long)kvh * ((row.n * per_kv + a.own.tile_rows - 1) / a.own.tile_rows) + r_own / a.own.tile_rows) * pieces;
+    auto cta = [&](long long g) { return total * ctas >> 32 ? kv::cta_of(total, g, ctas) : (int)((unsigned)((g + 1) * ctas - 1) / (unsigned)total); };
+    own0 = cta(first);
+    own_parts = cta(first + pieces - 1) - own0 + 1;
+    slot0 = 2 * own0 + (total * own0 < first * ctas ? 1 : 0);   // (its last segment, unless it starts there)
+  }
   const long long each = __ldcg(&a.total->each);
-  // part u of its group's: maximum and sum, and where its means are; all there are
+  // part u, of its own or its group's: maximum and sum, and where its means are; all there are
   const int rows = grp.n * per_kv, r = (row.o - grp.o + i) * per_kv + head % per_kv, tile = r / a.item_rows, kt = key_tiles(grp.keys);
   const long long first = grp.front + ((long long)kvh * grp.tiles + tile) * grp.per, at = grp.rows_front + (long long)kvh * rows + r;
   const int halves = min(a.item_rows, rows - tile * a.item_rows) > M_ROWS ? 1 : 2;
   auto cta_of = [&](long long g) { return (int)((g | each) >> 32 ? g / each : (unsigned)g / (unsigned)each); };
-  int c0 = 0, parts = 0;
+  int c0 = 0, parts = own_parts;
   if (grp.tiles > 0) {
     c0 = cta_of(first);
-    parts = (cta_of(first + grp.per - 1) - c0 + 1) * halves;
+    parts += (cta_of(first + grp.per - 1) - c0 + 1) * halves;
   }
-  auto part = [&](int u, long long& where) {
-    const int c = c0 + (halves == 2 ? u >> 1 : u);
-    where = at + (long long)c * ITEM_ROWS + (halves == 2 && (u & 1) ? a.part_rows : 0);
+  auto part = [&](int u, const float*& means) {
+    if (u < own_parts) {
+      const size_t slot = (size_t)(u == 0 ? slot0 : 2 * (own0 + u)) * a.own.tile_rows + r_own % a.own.tile_rows;
+      means = own_parts == 1 ? a.own_part + own * DIM : a.own.part + slot * DIM;
+      return __ldcg(own_parts == 1 ? a.own_ml + own : reinterpret_cast<const float2*>(a.own.part + 2 * (size_t)a.own.grid * a.own.tile_rows * DIM) + slot);
+    }
     if (u >= parts) return make_float2(-INFINITY, 0.f);
+    u -= own_parts;
+    const int c = c0 + (halves == 2 ? u >> 1 : u);
+    const long long where = at + (long long)c * ITEM_ROWS + (halves == 2 && (u & 1) ? a.part_rows : 0);
+    means = a.part + where * DIM;
     const int g0 = (int)(max(c * each, first) - first), g1 = (int)(min((c + 1) * each, first + grp.per) - first);
     return min(tile_at(g0, grp.weight), kt) < min(tile_at(g1, grp.weight), kt) ? __ldcg(a.ml + where) : make_float2(-INFINITY, 0.f);
   };
   // the largest maximum and the sum against it; then means times their shares (sums of values may be more than FP32 has room for)
-  float top = mine.y == 0.f ? -INFINITY : mine.x, sum = mine.y;
-  long long where;
+  float top = -INFINITY, sum = 0.f, x[PER];
+  const float* means = a.part;
   float2 v = make_float2(-INFINITY, 0.f);
   for (int u0 = 0; u0 < parts; u0 += 32) {
-    v = part(u0 + lane, where);
+    v = part(u0 + lane, means);
     float most = v.y != 0.f ? v.x : -INFINITY;
 #pragma unroll
     for (int s = 16; s; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
@@ -1013,9 +1038,9 @@ shared_join_kernel(const __grid_constant__ Params a) {
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   auto share = [&](float2 v) { return v.y == 0.f ? 0.f : (v.x == top ? v.y : v.y * kv::ex2(v.x - top)) * inv; };
 #pragma unroll
-  for (int j = 0; j < PER; ++j) x[j] = mine.y == 0.f ? 0.f : x[j] * share(mine);
+  for (int j = 0; j < PER; ++j) x[j] = 0.f;
   for (int u0 = 0; u0 < parts; u0 += 32) {
-    if (parts > 32) v = part(u0 + lane, where);
+    if (parts > 32) v = part(u0 + lane, means);
     const float f = share(v);
     for (unsigned left = __ballot_sync(0xffffffffu, v.y != 0.f); left;) {
       constexpr int AHEAD = 5;
@@ -1024,10 +1049,10 @@ shared_join_kernel(const __grid_constant__ Params a) {
       for (int k = 0; k < AHEAD; ++k) {
         const int src = left ? __ffs(left) - 1 : 0;
         g[k] = left ? __shfl_sync(0xffffffffu, f, src) : 0.f;
-        const long long from = __shfl_sync(0xffffffffu, where, src);
+        const float* from = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(means), src));
 #pragma unroll
         for (int j = 0; j < PER; ++j) y[k][j] = 0.f;
-        if (left) load(a.part + from * DIM, y[k]);
+        if (left) load(from, y[k]);
         left &= left - 1;
       }
 #pragma unroll

@@ -265,3 +265,42 @@ def test_many_prefixes_of_one_tile(dtype, dim, block):
     for _ in range(20):
         again, status = run(cache, q.to(DEV), new, lens, first, shared, ends, causal)
         assert status == 0 and torch.equal(again, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,per_kv,dim,block", [(2, 4, 128, 64), (1, 1, 32, 16), (8, 2, 64, 32)])
+def test_long_rows_beside_long_prefixes(dtype, heads, per_kv, dim, block):
+    """A newcomer that shares nothing and is as long as a group's prefix, rows whose own positions are many behind a short prefix, and short ones among them: own positions in one
+    part, in several, and in many."""
+    check([4, 1, 2], [3000, 0, 100], [5, 0, 60, 511, 5000, 2000, 480], [1, 2, 1, 3, 2, 1, 4], heads, per_kv, dim, block, "int8", dtype, True, seed=21)
+    check([3, 1], [1000, 0], [0, 700, 3, 9000], [2, 9, 1, 20], heads, per_kv, dim, block, "e4m3", dtype, False, seed=22)
+
+
+def test_own_positions_around_where_they_are_split():
+    """Longest own positions just below and from 512 on, where parts begin; calls in turn on the same scratch sizes."""
+    for own in (495, 496, 511, 512, 513, 600):
+        check([3, 2], [200, 64], [own, 3, 100, 0, 17], [1] * 5, 2, 2, 64, 32, "int8", "bf16", True, seed=own)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_planned_for_one_length_and_replayed_for_others(dtype):
+    """A captured call whose rows grow from short own positions to long ones and back: what is split is decided anew by every replay."""
+    shared, grow = [640, 0], ([3, 50, 1, 20], [3, 50, 1, 4000], [900, 50, 1, 4000], [3, 0, 400, 20])
+    most = [max(t) for t in zip(*grow)]
+    cache, model, first, lens, ends = batch([3, 1], shared, most, [2] * 4, 2, 64, 32, "int8", True)
+    q = numbers((8, 4, 64), dtype, 5, 0.3)
+    len_t, qd = ints(lens), q.to(DEV)
+    call = lambda: binding.cache_attention_shared(cache, qd, ints_off, len_t, first_t, shared_t, 2, FAR + 5000, max_shared=FAR)
+    ints_off, first_t, shared_t = ints(offsets([2] * 4)), ints(first), ints(shared)
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for tails in grow:
+        now = [s + t for s, t in zip([640] * 3 + [0], tails)]
+        len_t.copy_(ints(now))
+        graph.replay()
+        torch.cuda.synchronize()
+        want, weight, size, floor = model.attend(q.double().numpy(), offsets([2] * 4), now, True, 64 ** -0.5)
+        assert (np.abs(out.double().cpu().numpy() - want) <= bound(dtype, want, weight, size, floor, max(now) + 2, 64)).all()
+        assert torch.equal(out, call())

@@ -239,3 +239,13 @@ def test_pooled_append_of_pools_and_caches_that_do_not_belong_together(lib):
     _refused(lib, lib.ad_cache_append_pooled(None, C.byref(_cache()), *APPEND_POOLED.values(), None, None))
     _refused(lib, lib.ad_cache_append_pooled(_pool(), None, *APPEND_POOLED.values(), None, None))
     assert lib.ad_cache_append_pooled(_pool(), C.byref(_cache()), *{**APPEND_POOLED, "M": 0, "k": None, "v": None}.values(), None, None) == binding.AD_OK
+
+
+@pytest.mark.parametrize("heads,B,max_new", [(4, 17, 1), (2, 65, 8), (8, 3, 64)])
+def test_rows_own_positions_are_planned_for_whatever_others_share(lib, heads, B, max_new):
+    """A row may share nothing and be as long as any (max_keys): the attention over its own positions is planned, and given scratch, as cache_attention's would be, whatever the longest
+    prefix is."""
+    c, M, keys = C.byref(_cache(table_stride=1 << 20)), B * max_new, 1 << 24
+    need = {n: lib.ad_cache_attention_shared_scratch_bytes(c, 1, heads, B, M, max_new, keys, 2, n) for n in (keys, keys - 300, keys - 5000, keys // 2)}
+    own = lib.ad_cache_attention_scratch_bytes(c, 1, heads, B, max_new, keys)
+    assert own > 0 and len(set(need.values())) == 1 and need[keys] > own, (need, own)
