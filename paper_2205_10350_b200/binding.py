@@ -646,11 +646,11 @@ def cache_attention(cache, q_t, off_t, len_t, max_new, max_keys, causal=True, sc
 def cache_attention_shared(cache, q_t, off_t, len_t, group_t, shared_t, max_new, max_keys, max_shared=None, causal=True, scale=None, out=None,
                            status_t=None):
     """cache_attention for rows that share prefixes: rows group_t[g] .. group_t[g + 1] - 1 (group_t [G + 1]) have their first shared_t[g] positions in
-    common (shared_t [G]); whole blocks of these are read once for all of them, through the first row with tokens, where that saves time.  max_shared: longest prefix
-    (max_keys unless given)."""
+    common (shared_t [G]); whole blocks of these are read once for all of them, through the first row with tokens, where that saves time.  max_shared: longest prefix, which
+    decides it; unless it is given nothing is known of the prefixes, which only the device has, and every row reads its own positions as in cache_attention."""
     entry, lib = "ad_cache_attention_shared", _lib or load()
     if max_shared is None:
-        max_shared = max_keys
+        max_shared = 0
     if (max_new | max_keys | max_shared) >> 31:
         _refuse(entry, _TOO_LARGE)
     B, G = cache._batch(entry, off_t, len_t), shared_t.numel()

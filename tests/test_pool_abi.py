@@ -249,3 +249,29 @@ def test_rows_own_positions_are_planned_for_whatever_others_share(lib, heads, B,
     need = {n: lib.ad_cache_attention_shared_scratch_bytes(c, 1, heads, B, M, max_new, keys, 2, n) for n in (keys, keys - 300, keys - 5000, keys // 2)}
     own = lib.ad_cache_attention_scratch_bytes(c, 1, heads, B, max_new, keys)
     assert own > 0 and len(set(need.values())) == 1 and need[keys] > own, (need, own)
+
+
+def test_a_prefix_that_nobody_named_is_not_planned_for(monkeypatch):
+    """Without max_shared the call does not take max_keys for the longest prefix: rows of many positions of their own would go the way that pays for long prefixes."""
+    seen = []
+
+    class Lib:
+        def ad_cache_attention_shared_scratch_bytes(self, *a):
+            return 0
+
+        def ad_cache_attention_shared(self, *a):
+            seen.append(a)
+            return binding.AD_OK
+    monkeypatch.setattr(binding, "_lib", Lib())
+    monkeypatch.setattr(binding, "_call_on", lambda dev, call, *a: call(*a, None))
+    monkeypatch.setattr(binding, "_BF16", torch.bfloat16)
+    monkeypatch.setattr(binding, "_FP32", torch.float32)
+    monkeypatch.setattr(binding, "_INT32", torch.int32)
+    cache = object.__new__(binding.KvCache)
+    cache._dev, cache.device, cache._table_rows, cache.n_kv_heads, cache.head_dim, cache._scratch, cache._ref = 0, "cuda:0", 4, 2, 64, {}, None
+    i32 = lambda n: _OnDevice(torch.zeros(n, dtype=torch.int32))
+    q, out = (_OnDevice(torch.zeros(3, 4, 64, dtype=torch.bfloat16)) for _ in range(2))
+    for kw, want in (({}, 0), (dict(max_shared=None), 0), (dict(max_shared=0), 0), (dict(max_shared=4000), 4000), (dict(max_shared=20000), 20000)):
+        binding.cache_attention_shared(cache, q, i32(3), i32(2), i32(2), i32(1), 3, 20000, out=out, **kw)
+        args = dict(zip("cache q dtype stride heads off len B M max_new max_keys group shared G max_shared".split(), seen.pop()))
+        assert (args["max_keys"], args["G"], args["max_shared"]) == (20000, 1, want)
