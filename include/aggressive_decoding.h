@@ -425,7 +425,7 @@ typedef struct ad_kv_pool {
   int32_t* refs;             /* [n_blocks] */
   int32_t rows;              /* 1 .. 8192 */
   int32_t table_stride;      /* blocks that a row may have */
-  int32_t n_blocks;
+  int32_t n_blocks;          /* 1 .. 2^30 - 512 */
   int32_t block;             /* tokens of a block, as in the caches */
 } ad_kv_pool;
 

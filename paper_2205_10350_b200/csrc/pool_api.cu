@@ -11,11 +11,13 @@ using namespace ad;
 namespace {
 
 constexpr int kPoolRows = 8192;        // (a column of the table, all rows, lies in a CTA's shared memory)
+constexpr int kPoolBlocks = (1 << 30) - 512;      // (the planning kernels look up to 256 blocks beyond the last one, and keep as many holes and movers behind one another, in 32 bits)
 
 const char* pool_fault(const ad_kv_pool* p, int32_t B) {
   if (!p || !p->table || !p->refs) return "null pool";
   if (p->block != 16 && p->block != 32 && p->block != 64 && p->block != 128) return "blocks hold 16, 32, 64 or 128 tokens";
   if (p->n_blocks < 1 || p->table_stride < 1 || p->rows < 1 || p->rows > kPoolRows) return "sizes must be positive (and at most 8192 rows)";
+  if (p->n_blocks > kPoolBlocks) return "a pool has 2^30 - 512 blocks at most";
   if ((int64_t)p->table_stride * p->block > INT_MAX - kMaxNew) return "a row's capacity must stay below 2^31 - 2^19 tokens";
   if ((int64_t)p->table_stride * p->rows > INT_MAX) return "the table must have fewer than 2^31 entries";
   if (B < 1 || B > p->rows) return "a batch has 1 row to as many as the pool";

@@ -275,3 +275,19 @@ def test_a_prefix_that_nobody_named_is_not_planned_for(monkeypatch):
         binding.cache_attention_shared(cache, q, i32(3), i32(2), i32(2), i32(1), 3, 20000, out=out, **kw)
         args = dict(zip("cache q dtype stride heads off len B M max_new max_keys group shared G max_shared".split(), seen.pop()))
         assert (args["max_keys"], args["G"], args["max_shared"]) == (20000, 1, want)
+
+
+def test_pools_of_more_blocks_than_32_bits_can_number(lib):
+    """The planning kernels count holes and movers behind one another, and walk the counts some way beyond the last one."""
+    for n in ((1 << 30) - 511, 1 << 30, (1 << 31) - 257, (1 << 31) - 1):
+        pool = _pool(n_blocks=n)
+        _refused(lib, lib.ad_cache_fork(pool, P, P, 3, None, None))
+        _refused(lib, lib.ad_cache_reserve(pool, None, 0, P, P, 3, P, HUGE, None, None))
+        _refused(lib, lib.ad_cache_append_pooled(pool, C.byref(_cache(n_blocks=n)), *APPEND_POOLED.values(), None, None))
+        _refused(lib, lib.ad_cache_compact(pool, None, 0, P, P, HUGE, None))
+        assert lib.ad_cache_reserve_scratch_bytes(pool, 3) == 0 and lib.ad_cache_compact_scratch_bytes(pool) == 0
+    most = (1 << 30) - 512
+    # claims, lists and moves of as many blocks as there may be, counted in 64 bits
+    assert lib.ad_cache_reserve_scratch_bytes(_pool(n_blocks=most), 3) > 12 * most and lib.ad_cache_compact_scratch_bytes(_pool(n_blocks=most)) > 18 * most - 4096
+    # the last index of either list, and the last step of a walk
+    assert 2 * most - 1 < 2 ** 31 and most + 2 * 256 < 2 ** 31
