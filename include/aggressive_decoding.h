@@ -465,7 +465,7 @@ int ad_cache_compact(const ad_kv_pool* pool, const ad_kv_cache* caches, int32_t 
  * exceeds r[m] times its total.  Every parameter is a device array [M] or NULL (temperature one; no such filter).  temperature 0: the largest score, lowest id.
  * logp (NULL: not wanted) [M] receives the token's log-probability among the kept ids.  filtered (NULL: not wanted) [M, vocab] in dtype, rows filtered_stride
  * apart, receives the scores of the kept ids and -inf for the others: what ad_accept_sampled takes as the scores of a truncated distribution, the verifier's or the
- * drafter's.  It may be `scores` itself (with the same stride).
+ * drafter's.  It may be `scores` itself, or lie between its rows, with the same stride; otherwise it lies apart from it.
  * Weights are computed in 64 bits and summed as integers in units of 2^-62 * vocab of the largest (vocab rounded up to a power of two, 2048 at least); comparisons are decided on
  * these sums, and the ones of min_p on the weights.
  * Scores of -inf have no weight, +inf share all of it, a NaN counts as -inf.  A row without any score above -inf takes id 0 with logp -inf.  One whose

@@ -46,6 +46,16 @@ inline kv::Cache device_cache(const ad_kv_cache* c) {
   return d;
 }
 
+// Whether what is left would be written over other scores than its own: M rows of `vocab` elements at a and at b.  It may take the place of the scores themselves, lie apart from them, or, with
+// the same stride, between them: then b lies the same distance behind some row of a's in all rows, and overlaps neither that row nor the next.
+inline bool rows_overlap(uintptr_t a, size_t stride_a, uintptr_t b, size_t stride_b, size_t vocab, size_t M, size_t element) {
+  if (a >= b + ((M - 1) * stride_b + vocab) * element || b >= a + ((M - 1) * stride_a + vocab) * element) return false;
+  if (M == 1 || stride_a != stride_b) return a != b || (M > 1 && stride_a != stride_b);
+  if (a == b) return false;
+  const size_t stride = stride_a * element, behind = b > a ? (b - a) % stride : (stride - (a - b) % stride) % stride;
+  return behind < vocab * element || behind > stride - vocab * element;
+}
+
 inline int arg_fault(const char* entry, const char* why) { return op_fail(AD_ERR_ARG, entry, why); }
 inline int launched(const char* entry, cudaError_t e) { return e == cudaSuccess ? AD_OK : op_fail(AD_ERR_CUDA, entry, cudaGetErrorString(e)); }
 

@@ -192,11 +192,8 @@ extern "C" int ad_sample(const void* scores, int64_t stride, int32_t dtype, int3
   const size_t element = dtype_bytes(dtype);
   if (!aligned(scores, element) || !aligned(filtered, element)) return arg_fault(entry, "misaligned scores");
   if (stride < vocab || (filtered && filtered_stride < vocab)) return arg_fault(entry, "rows of scores overlap");
-  if (filtered) {                                  // either the scores themselves or apart from them
-    const uintptr_t a = reinterpret_cast<uintptr_t>(scores), b = reinterpret_cast<uintptr_t>(filtered);
-    const uintptr_t a1 = a + ((size_t)(M - 1) * stride + vocab) * element, b1 = b + ((size_t)(M - 1) * filtered_stride + vocab) * element;
-    if (a < b1 && b < a1 && (a != b || (stride != filtered_stride && M > 1))) return arg_fault(entry, "scores and what is left of them overlap");
-  }
+  if (filtered && rows_overlap(reinterpret_cast<uintptr_t>(scores), (size_t)stride, reinterpret_cast<uintptr_t>(filtered), (size_t)filtered_stride, (size_t)vocab, (size_t)M, element))
+    return arg_fault(entry, "scores and what is left of them overlap");
   sample::Params p = {};
   p.scores = scores; p.stride = (size_t)stride; p.vocab = vocab; p.M = M; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p; p.r = r;
   p.tokens = tokens; p.logp = logp; p.out = filtered; p.out_stride = (size_t)filtered_stride; p.status = status;

@@ -280,3 +280,24 @@ def test_long_rows_of_all_kinds(dtype, V):
     for temperature in (0.7, 30.0, 1e5, 1e37, 1e-3):
         for k, p, least in ((0, 1.0, 0.0), (0, 0.83, 0.0), (V // 3, 1.0, 0.0), (V // 2, 0.71, 0.0), (40, 0.6, 0.0), (0, 0.9, 0.3), (0, 1.0, 0.2)):
             check(x.to(TORCH[dtype]), r.random(12), temperature=[temperature] * 12, top_k=[k] * 12, top_p=[p] * 12, min_p=[least] * 12)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,gap,swap", [(1000, 0, False), (1003, 5, False), (1003, 1, True), (40001, 3, True)])
+def test_what_is_left_between_the_rows_of_scores(dtype, V, gap, swap):
+    """Scores and what is left as two column ranges of one wide array, next to each other or apart, in either order: neither touches the other, nor what lies beside them."""
+    M, g = 5, torch.Generator().manual_seed(V)
+    wide = torch.full((M, 2 * V + gap + 7), 3.5, dtype=TORCH[dtype], device=DEV)
+    first, second = wide[:, 2: 2 + V], wide[:, 2 + V + gap: 2 + 2 * V + gap]
+    scores, out = (second, first) if swap else (first, second)
+    x = logits(M, V, dtype, V)
+    scores.copy_(x)
+    r, k = torch.rand(M, generator=g).to(DEV), torch.tensor([0, 5, 1, 300, V], dtype=torch.int32, device=DEV)
+    p = torch.tensor([0.9, 1.0, 0.5, 0.99, 0.2], device=DEV)
+    tokens, logp = binding.sample(scores, r, top_k=k, top_p=p, filtered=out)
+    want = torch.empty_like(x, device=DEV)
+    alone = binding.sample(x.to(DEV), r, top_k=k, top_p=p, filtered=want)
+    assert torch.equal(tokens, alone[0]) and torch.equal(logp, alone[1]) and torch.equal(out, want)
+    assert torch.equal(scores.cpu(), x) and bool((wide[:, :2] == 3.5).all()) and bool((wide[:, 2 + V: 2 + V + gap] == 3.5).all()) and bool((wide[:, 2 + 2 * V + gap:] == 3.5).all())
+    with pytest.raises(binding.AdError, match="overlap"):
+        binding.sample(scores, r, top_k=k, filtered=wide[:, 3: 3 + V] if not swap else wide[:, 1 + V + gap: 1 + 2 * V + gap])

@@ -291,3 +291,36 @@ def test_pools_of_more_blocks_than_32_bits_can_number(lib):
     assert lib.ad_cache_reserve_scratch_bytes(_pool(n_blocks=most), 3) > 12 * most and lib.ad_cache_compact_scratch_bytes(_pool(n_blocks=most)) > 18 * most - 4096
     # the last index of either list, and the last step of a walk
     assert 2 * most - 1 < 2 ** 31 and most + 2 * 256 < 2 ** 31
+
+
+OVERLAP = """
+#include <stdio.h>
+#include "cache_checks.h"
+int main() {
+  for (size_t element = 2; element <= 4; element += 2)
+    for (size_t vocab = 1; vocab <= 3; ++vocab)
+      for (size_t M = 1; M <= 3; ++M)
+        for (size_t sa = vocab; sa <= 8; ++sa)
+          for (size_t sb = vocab; sb <= 8; ++sb)
+            for (int d = -30; d <= 30; ++d) {
+              const uintptr_t a = 4096, b = a + d * (intptr_t)element;
+              bool touch = false;
+              for (size_t i = 0; i < M; ++i)
+                for (size_t j = 0; j < M; ++j) touch = touch || (a + i * sa * element < b + (j * sb + vocab) * element && b + j * sb * element < a + (i * sa + vocab) * element);
+              const bool itself = d == 0 && (sa == sb || M == 1), said = ad::rows_overlap(a, sa, b, sb, vocab, M, element);
+              // never let through what touches, and with one stride nothing else refused
+              if ((touch && !itself && !said) || (itself && said) || (sa == sb && !touch && said)) { printf("%zu %zu %zu %zu %zu %d\\n", element, vocab, M, sa, sb, d); return 1; }
+            }
+  return 0;
+}
+"""
+
+
+@pytest.mark.skipif(not os.path.exists(NVCC), reason="no CUDA compiler")
+def test_what_overlaps(tmp_path):
+    """Against every pair of rows: in place, apart, between the rows, partly over them."""
+    src, exe = tmp_path / "overlap.cu", tmp_path / "overlap"
+    src.write_text(OVERLAP)
+    subprocess.run([NVCC, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout
