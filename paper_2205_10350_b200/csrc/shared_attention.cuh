@@ -982,6 +982,7 @@ shared_join_kernel(const __grid_constant__ Params a) {
   if ((long long)blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5) >= (long long)row.n * a.n_heads) return;      // (below 2^30)
   const int w = blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5), i = w / a.n_heads, head = w - i * a.n_heads, kvh = head / per_kv;
   const Line grp = load_line(row.group);
+  if (grp.n == 0) return;                                      // (a group that overlaps others, and that there was no room for: left out)
   // the row's own positions, by one CTA or several
   const size_t own = (size_t)(row.o + i) * a.n_heads + head;
   const int r_own = i * per_kv + head % per_kv, pieces = a.own.granule && !own_whole ? (own_units(a, own_len, row.n) + a.own.fixed + a.own.granule / 2) / a.own.granule : 1;

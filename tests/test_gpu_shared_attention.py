@@ -304,3 +304,19 @@ def test_planned_for_one_length_and_replayed_for_others(dtype):
         want, weight, size, floor = model.attend(q.double().numpy(), offsets([2] * 4), now, True, 64 ** -0.5)
         assert (np.abs(out.double().cpu().numpy() - want) <= bound(dtype, want, weight, size, floor, max(now) + 2, 64)).all()
         assert torch.equal(out, call())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_groups_that_overlap_are_left_out_as_a_whole(dtype):
+    """Groups whose rows are others' as well: what there is no room for is left out, and does not come back as attention over its own positions alone."""
+    groups, shared, tails, new = [8, 4], [96, 96], [3, 0, 5, 6, 1, 2, 3, 4, 9, 8, 7, 40], [1] * 12
+    cache, model, first, lens, ends = batch(groups, shared, tails, new, 1, 64, 32, "int8", True)
+    q = numbers((12, 1, 64), dtype, 1).to(DEV)
+    want, status = run(cache, q, new, lens, first, shared, ends, True)
+    assert status == 0
+    for bounds, left in (([0, 8, 4, 12], range(8, 12)), ([0, 8, 0, 12], range(8, 12))):
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        out = torch.full_like(want, 7.0)
+        binding.cache_attention_shared(cache, q, ints(range(13)), ints(lens), ints(bounds), ints([96, 96, 96]), 1, FAR + max(ends), max_shared=FAR, out=out, status_t=status)
+        assert int(status.item()) == binding.AD_ERR_ARG and bool((out[list(left)] == 7).all())
+        assert torch.allclose(out[:8].float(), want[:8].float(), atol=0.02)
