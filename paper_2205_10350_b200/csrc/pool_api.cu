@@ -160,6 +160,23 @@ int scores_each(int32_t vocab, int cluster, size_t element) {
   const int64_t round = 32 * 16 / (int64_t)element, warps = (int64_t)cluster * sample::WARPS;
   return (int)((vocab + 16 / (int64_t)element + warps * round - 1) / (warps * round) * round);
 }
+// CTAs that share a row.  One up to 12 KB of scores, which eight take no sooner (a turn of a CTA costs as much as 40 KB of scores, of a cluster more).  Eight, or four, while all rows are under way at once
+// with them.  Beyond that as few as keep a row in half an SM, one or two, so that there are two CTAs an SM and few turns; four where two cannot.  Measured with 1 / 2 / 4 / 8, us, scores from memory
+// where they are 8 MB and more:
+//   few rows, top-p: 1 x 3000 FP32 13.4 / 14.5 / 14.0 / 14.4; 1 x 32000 48 / 35 / 24 / 20; 64 x 32000 54 / 43 / 32 / 47; 1 x 128000 BF16 106 / 50 / 37 / 26; 64 x 128000 143 / 62 / 55 / 71
+//   many: 512 x 3000 FP32, top-p 31 / 61 / 113 / 232; 256 x 16384 50 / 67 / 94 / 162; 256 x 32000 113 / 94 / 117 / 177; BF16 256 x 32000 53 / 68 / 98 / 211, 256 x 50265 100 / 92 / 130 / 196;
+//   256 x 128000, filters row by row and what is left, 193 / 185 / 158 / 218
+// Over 1352 such, of 500 to 160000 ids and 1 to 512 rows, the choice takes 4 % longer than the best of the four in the mean (eight or four from 2048 ids on: 24 %), and at the most twice as long: 512 x
+// 80000 FP32, top-k and top-p, 188 / 254 / 368 / 331.  A row's result is the same for all.
+int sample_cluster(int32_t M, int32_t vocab, size_t element) {
+  if ((size_t)vocab * element <= 12 * 1024) return 1;
+  const int64_t slots = 2 * (int64_t)op_num_sms();
+  for (int c = sample::MAX_CLUSTER; c >= 4; c /= 2)
+    if ((int64_t)M * c <= slots) return c;
+  for (int c = 1; c <= 2; ++c)
+    if ((size_t)scores_each(vocab, c, element) * sample::WARPS * element <= 76 * 1024) return c;
+  return 4;
+}
 template <typename T, bool KEPT>
 cudaError_t launch_sample_kept(const sample::Params& p, int cluster, size_t smem, cudaStream_t st) {
   static std::atomic<uint64_t> raised{0};
@@ -174,7 +191,7 @@ cudaError_t launch_sample_kept(const sample::Params& p, int cluster, size_t smem
 }
 template <typename T>
 cudaError_t launch_sample(sample::Params p, cudaStream_t st) {
-  const int cluster = p.vocab <= 2048 ? 1 : p.M * (int64_t)sample::MAX_CLUSTER <= 2 * op_num_sms() ? sample::MAX_CLUSTER : 4;
+  const int cluster = sample_cluster(p.M, p.vocab, sizeof(T));
   p.each = scores_each(p.vocab, cluster, sizeof(T));
   const size_t smem = (size_t)p.each * sample::WARPS * sizeof(T);
   return smem <= kScoresKept ? launch_sample_kept<T, true>(p, cluster, smem, st) : launch_sample_kept<T, false>(p, cluster, smem, st);

@@ -301,3 +301,33 @@ def test_what_is_left_between_the_rows_of_scores(dtype, V, gap, swap):
     assert torch.equal(scores.cpu(), x) and bool((wide[:, :2] == 3.5).all()) and bool((wide[:, 2 + V: 2 + V + gap] == 3.5).all()) and bool((wide[:, 2 + 2 * V + gap:] == 3.5).all())
     with pytest.raises(binding.AdError, match="overlap"):
         binding.sample(scores, r, top_k=k, filtered=wide[:, 3: 3 + V] if not swap else wide[:, 1 + V + gap: 1 + 2 * V + gap])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [700, 3000, 4096, 9001, 32000, 50265, 128000])
+def test_a_row_is_drawn_alike_in_batches_of_any_size(dtype, V):
+    """The same rows alone, among few and among many, which one, two, four or eight CTAs take together: the same tokens, log-probabilities and scores left, bit by bit."""
+    rows, g = 6, torch.Generator().manual_seed(V)
+    x = logits(rows, V, dtype, V)
+    x[1] = (x[1].float() * 4).round().div(4).to(x.dtype)         # many ties
+    x[2, ::3] = -math.inf
+    r = torch.rand(rows, generator=g)
+    t = dict(temperature=torch.tensor([1.0, 0.7, 1.3, 2.0, 0.5, 1.0]), top_k=torch.tensor([0, 40, 0, 300, V // 2, 0], dtype=torch.int32),
+             top_p=torch.tensor([0.9, 0.95, 0.5, 0.99, 1.0, 1.0]), min_p=torch.tensor([0.0, 0.0, 0.01, 0.0, 0.001, 0.0]))
+    want = None
+    for M in (6, 30, 60, 150, 300, 600):
+        if M * V > 40_000_000:
+            continue
+        many = lambda y: y.repeat((M // rows,) + (1,) * (y.dim() - 1)).to(DEV)
+        scores = many(x)
+        left = torch.empty_like(scores)
+        tokens, logp = binding.sample(scores, many(r), **{n: many(y) for n, y in t.items()}, filtered=left)
+        got = (tokens.view(-1, rows), logp.view(-1, rows), left.view(-1, rows, V))
+        if want is None:
+            want = [y[0].clone() for y in got]
+            for m in range(rows):
+                token, lp, ids = draw(x[m].double().numpy(), float(r[m]), **{n: y[m].item() for n, y in t.items()})
+                kept = np.full(V, -np.inf)
+                kept[ids] = x[m].double().numpy()[ids]
+                assert int(want[0][m]) == token and np.array_equal(want[2][m].double().cpu().numpy(), kept)
+        assert all(bool((y == w).all()) for y, w in zip(got, want)), M
