@@ -38,18 +38,18 @@ Scratch scratch_of(const ad_kv_cache* c, int32_t n_heads, int32_t B, int32_t M, 
   s.bytes = s.rows + rounded(cache_attention_scratch(c, n_heads, B, max_new, max_keys, true));
   return s;
 }
-// Whether the groups' positions are read once for all rows.  That saves units of 32 keys for 32 rows of queries and a key/value head, and costs the plan, a second pass over the rows and the join:
-// about as much as 13000 units (16000 of 128 wide BF16, which the attention row by row takes less long for), one for every row and key/value head, and 0.4 for
-// every query and head, whose parts are written and read again.
-// Row by row / shared in us, 8 key/value heads:
-//   128 wide, 4 query heads each, BF16: 16 rows of a query behind 4000 positions (15000 units) 46 / 39, 64 behind 1000 (15600) 39 / 44, 8 behind 16000 (28000) 63 / 49, 64 behind 16000 (252000)
-//   269 / 74; 16 rows of 8 behind 4000 (15000) 60 / 62, 8 groups of 16 of 8 behind 1000 (29800, 32800 queries) 131 / 129, 8 of 16 of 15 behind 330 (19200, 61400 queries) 107 / 185;
-//   64 wide, a query head each: 64 rows of a query behind 1000 (15600) 36 / 28, in FP32 41 / 29; 8 groups of 8 of 8 behind 1000 (13900) 38 / 36, in FP32 43 / 37; 16 behind 4000
-//   (15000) 33 / 32, in FP32 37 / 32; 8 of 32 of a query behind 250 (13900) 36 / 47, in FP32 41 / 49; 8 of 16 of 15 behind 330 (9600, 15400 queries) 28 / 54, in FP32 34 / 54.
+// Whether the groups' positions are read once for all rows.  Row by row they take units of 32 keys for 32 rows of queries and a key/value head; read once, a group's take about 1.9 rows' units.
+// What that saves has to outweigh the plan, a second pass over the rows and the join: about 9000 units (12000 of 128 wide BF16, which the attention row by row takes less long for), ten for every row and
+// key/value head, and 0.2 for every query and head, whose parts are written and read again.  Row by row / read once in us, own positions 20:
+//   128 wide, 32 heads on 8, BF16: 16 rows of a query behind 4000 positions 44 / 41, 64 behind 1000 38 / 45, 8 behind 16000 62 / 47, 64 behind 16000 273 / 73, 4 behind 30000 58 / 57, 3 50 / 56, 2 38 / 56;
+//   16 rows of 8 behind 4000 60 / 63, 8 groups of 16 of 8 behind 1000 130 / 133, 8 of 16 of 15 behind 330 105 / 189;
+//   64 wide, 8 heads on 8: 64 rows of a query behind 1000 35 / 28, in FP32 40 / 30; 8 groups of 8 of 8 behind 1000 38 / 37, in FP32 42 / 39; 16 of 8 behind 4000 33 / 37, in FP32 37 / 38; 8 groups of 32
+//   of a query behind 250 36 / 49, in FP32 41 / 50; 8 of 16 of 15 behind 330 27 / 56, in FP32 32 / 57; 4 of 2 of a query behind 14000 38 / 62; 16 heads, 8 of 2 of 4 behind 14000 100 / 170.
+// Over 420 others, of 50 to 20000 positions, 1 to 8 groups of 2 to 64 rows and 1 to 25 queries, the choice takes 0.6 % longer than the faster side in the mean and 28 % at the most.
 bool worth_sharing(const ad_kv_cache* c, int32_t dtype, int32_t n_heads, int32_t B, int32_t M, int32_t max_new, int32_t max_keys, int32_t G, int32_t max_shared) {
   const int64_t rows = (int64_t)max_new * (n_heads / c->n_kv_heads), keys = std::min<int64_t>(std::min(max_keys, max_shared), (int64_t)c->table_stride * c->block);
-  const double saved = (double)(B - G) * c->n_kv_heads * (double)((rows + 31) / 32) * (double)(keys / 32);
-  return saved >= (dtype == AD_DTYPE_BF16 && c->head_dim == 128 ? 16000.0 : 13000.0) + (double)B * c->n_kv_heads + 0.4 * M * (double)n_heads;
+  const double saved = (B - 1.9 * G) * c->n_kv_heads * (double)((rows + 31) / 32) * (double)(keys / 32);
+  return saved >= (dtype == AD_DTYPE_BF16 && c->head_dim == 128 ? 12000.0 : 9000.0) + 10.0 * B * c->n_kv_heads + 0.2 * M * (double)n_heads;
 }
 const char* shared_fault(int32_t n_heads, int32_t B, int32_t M, int32_t G, int32_t max_shared) {
   if (B < 1 || B > kSharedRows) return "1 to 8192 rows";

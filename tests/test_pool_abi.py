@@ -241,7 +241,7 @@ def test_pooled_append_of_pools_and_caches_that_do_not_belong_together(lib):
     assert lib.ad_cache_append_pooled(_pool(), C.byref(_cache()), *{**APPEND_POOLED, "M": 0, "k": None, "v": None}.values(), None, None) == binding.AD_OK
 
 
-@pytest.mark.parametrize("heads,B,max_new", [(4, 17, 1), (2, 65, 8), (8, 3, 64)])
+@pytest.mark.parametrize("heads,B,max_new", [(4, 17, 1), (2, 65, 8), (8, 7, 64)])
 def test_rows_own_positions_are_planned_for_whatever_others_share(lib, heads, B, max_new):
     """A row may share nothing and be as long as any (max_keys): the attention over its own positions is planned, and given scratch, as cache_attention's would be, whatever the longest
     prefix is."""
@@ -324,3 +324,16 @@ def test_what_overlaps(tmp_path):
     subprocess.run([NVCC, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+def test_pairs_are_read_row_by_row(lib):
+    """What a group's positions take when they are read once is nearly what two rows take: pairs are not worth it at lengths where more rows are."""
+    c = C.byref(_cache(table_stride=1 << 20, n_blocks=1 << 20))
+    for dtype in (0, 1):
+        for G, n, once in ((1, 2, False), (8, 2, False), (1, 16, True), (8, 16, True), (1, 64, True), (4, 3, True)):
+            B, new, keys = G * n, 4, 14000
+            sizes = (c, dtype, 2, B, B * new, new, keys + 300, G, keys)
+            alone = lib.ad_cache_attention_scratch_bytes(c, dtype, 2, B, new, keys + 300)
+            got = lib.ad_cache_attention_shared_scratch_bytes(*sizes)
+            assert (got > alone) == (once and (B - 1.9 * G) * 2 * (keys // 32) >= 9000 + 20 * B + 0.4 * B * new), (dtype, G, n)
+            assert once or got == alone
