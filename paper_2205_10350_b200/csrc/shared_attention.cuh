@@ -953,8 +953,8 @@ shared_attention_kernel(const __grid_constant__ Params a) {
 }
 
 // Joins the parts of every query: of its group's items, and of its row's own positions (one, or what several CTAs of the attention row by row left), with out = sum of mean_i s_i 2^(m_i - m) / sum of s_i 2^(m_i - m).  A warp a query and head.
-// Bound by latency: lines, maxima, means, one after another; five means under way and four CTAs an SM: 600 queries of 32 heads with 2 to 4 parts each 23 us, 64 with 20 parts 11 us.  (Eight
-// means and three CTAs: 33 and 9.7; with the parts' borders by 64-bit divisions besides: 34 and 12.5.)
+// Bound by latency: lines, maxima, means, one after another; five means under way and four CTAs an SM: 600 queries of 32 heads with 3 to 7 parts each 29 us alone and cold, 64 with about 20
+// 15 us.  (With the rows' own parts joined in front of it 25 and 13, and 14 and 6 for that.)  The parts' borders are worked out in 32 bits where they fit, as 64-bit divisions took a tenth of its time.
 // grid = (enough for max_new * n_heads warps, B), block = JOIN_THREADS.
 constexpr int JOIN_THREADS = 256;
 template <typename T, int DIM>
