@@ -514,7 +514,7 @@ class KvCache:
     b * row_blocks .. (b + 1) * row_blocks - 1.  `tensors` = (k_codes, v_codes, k_scale, v_scale) adopts existing memory; otherwise
     the cache is allocated here."""
 
-    pool = None                         # the KvPool whose blocks it has
+    _pool = None                        # the struct of the pool whose blocks it has, and its counts (not the pool itself, which holds its caches)
 
     def __init__(self, n_blocks, n_kv_heads, head_dim, block=32, fmt="e4m3", table=None, row_blocks=None, device="cuda:0", tensors=None):
         import torch
@@ -586,10 +586,10 @@ def cache_append(cache, k_t, v_t, off_t, len_t, max_new, status_t=None):
         _refuse(entry, "keys and values must agree in type, shape and stride")
     dtype, M, stride = tokens
     args = (k_t.data_ptr(), v_t.data_ptr(), dtype, stride, off_t.data_ptr(), len_t.data_ptr(), B, M, max_new, _status_pointer(entry, cache._dev, status_t))
-    if cache.pool is None:
+    if cache._pool is None:
         rc = _call_on(cache._dev, lib.ad_cache_append, cache._ref, *args)
     else:
-        rc = _call_on(cache._dev, lib.ad_cache_append_pooled, cache.pool._ref, cache._ref, *args)
+        rc = _call_on(cache._dev, lib.ad_cache_append_pooled, cache._pool[0], cache._ref, *args)
     if rc != AD_OK:
         _raise(lib, rc)
 
@@ -708,7 +708,7 @@ class KvPool:
     def add_cache(self, n_kv_heads, head_dim, fmt="e4m3", tensors=None):
         """A cache (of one layer) on the pool's blocks and table; cache_reserve and cache_compact move its contents from now on."""
         cache = KvCache(self.n_blocks, n_kv_heads, head_dim, self.block, fmt, table=self.table, row_blocks=self.row_blocks, device=self.device, tensors=tensors)
-        cache.pool = self
+        cache._pool = (self._ref, self.refs)
         self.caches.append(cache)
         self._structs = (KvCacheStruct * len(self.caches))(*(c.struct for c in self.caches))
         return cache

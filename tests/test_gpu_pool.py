@@ -351,3 +351,28 @@ def test_what_follows_a_refused_reservation_writes_nothing(captured, dtype):
         assert torch.equal(pool.table, p.table)
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip((c.k_codes, c.v_codes, c.k_scale, c.v_scale), (p.k_codes, p.v_codes, p.k_scale, p.v_scale)))
     assert int(st.item()) == 0 and not all(torch.equal(a, b) for a, b in zip(contents(pool), before))
+
+
+def test_a_pool_and_its_caches_go_when_nobody_has_them_any_more():
+    """Neither holds the other back until the collector comes by: their memory is torch's again at once, and a cache whose pool went can still be written."""
+    import gc
+    import weakref
+    torch.cuda.synchronize()
+    gc.collect()
+    gc.disable()
+    try:
+        before = torch.cuda.memory_allocated()
+        pool = binding.KvPool(2, 8, 2048, 64, device=DEV)
+        caches = [pool.add_cache(4, 128) for _ in range(2)]
+        st, ref = status(), weakref.ref(pool)
+        binding.cache_reserve(pool, ints([0, 3, 3]), ints([0, 0]), st)
+        del pool
+        assert ref() is None
+        x = torch.ones((3, 4, 128), device=DEV)
+        binding.cache_append(caches[0], x, x, ints([0, 3, 3]), ints([0, 0]), 3, st)
+        assert int(st.item()) == 0 and bool((caches[0].k_codes[0, :, :3].float() != 0).all())
+        assert torch.cuda.memory_allocated() - before > 2 * 2 * 2048 * 4 * 64 * 128
+        del caches, x, st
+        assert torch.cuda.memory_allocated() - before < 1 << 20
+    finally:
+        gc.enable()
