@@ -149,11 +149,11 @@ struct Weights {
     const u64 u = (u64)__double_as_longlong(w) & 0xfffffffffffffull;
     return infinite ? (x == topf ? 1ull << bits : 0ull) : any(x) ? u : 0ull;
   }
-  // w(x) >= least, in FP64
+  // w(x) >= least, in FP64; one is reached by the largest score alone, however close to it others' weights come
   __device__ __forceinline__ bool reaches(float x, double least) const {
     if (x == topf) return 1.0 >= least;
     if (infinite || x == -INFINITY) return 0.0 >= least;
-    return exp(((double)x - top) * (scale * (0.693147180559945309417 / 256.0))) >= least;
+    return least < 1.0 && exp(((double)x - top) * (scale * (0.693147180559945309417 / 256.0))) >= least;
   }
 };
 

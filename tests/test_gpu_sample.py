@@ -331,3 +331,23 @@ def test_a_row_is_drawn_alike_in_batches_of_any_size(dtype, V):
                 kept[ids] = x[m].double().numpy()[ids]
                 assert int(want[0][m]) == token and np.array_equal(want[2][m].double().cpu().numpy(), kept)
         assert all(bool((y == w).all()) for y, w in zip(got, want)), M
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [5, 5000, 50000])
+def test_min_p_of_one_leaves_what_ties_with_the_largest(dtype, V):
+    """Scores a step or some below the largest, at temperatures that leave all of them a weight of one in 64 bits: none of them ties with it."""
+    x = torch.full((6, V), 1.0).to(TORCH[dtype])
+    step = torch.finfo(TORCH[dtype]).eps / 2                    # what numbers below one are apart: 24 and 8 bits
+    for i, below in enumerate((1, 2, 3)):
+        x[:, i] = 1.0 - below * step
+    x[:, 4:] = 0.5
+    x[3:, 0] = 1.0
+    t = torch.tensor([1.0, 1e12, 1e30] * 2, device=DEV)
+    for p in (1.0, 5.0):
+        left, scores = torch.empty_like(x, device=DEV), x.to(DEV)
+        tokens, logp = binding.sample(scores, torch.full((6,), 0.75, device=DEV), temperature=t, min_p=torch.full((6,), p, device=DEV), filtered=left)
+        want = torch.where(x == 1, x, torch.full_like(x, -math.inf))
+        assert torch.equal(left.cpu(), want) and tokens.tolist() == [3] * 6
+        # (of one kept id, or of two that tie)
+        assert torch.allclose(logp.cpu(), torch.tensor([0.0] * 3 + [-math.log(2.0)] * 3), atol=2 ** -22)
