@@ -440,7 +440,7 @@ int ad_cache_fork(const ad_kv_pool* pool, const int32_t* parent, const int32_t* 
  * with the tokens in front of len[b] copied in all `n_caches` caches (0 .. 64; none: nothing is copied).  Where nobody else holds it, the first of the rows that write
  * a shared block keeps it.  Free blocks are taken in ascending order, for rows and for a row's blocks in order.  A pool without enough of them latches AD_ERR_CAPACITY and
  * stays as it is: rows go on sharing what they shared, which ad_cache_append_pooled respects without the host's doing, so that the sequence can be captured and *status read
- * behind it.  (ad_cache_append knows nothing of counts and must not follow a refusal: rows would write the same block at once.  Rows that own all they would write are written by either, and need not have been refused for.)  A row whose offsets or length make no sense, or that
+ * behind it.  (ad_cache_append knows nothing of counts and must not follow a refusal: rows would write the same block at once.  Rows that own all they would write are written all the same.)  A row whose offsets or length make no sense, or that
  * would pass its capacity, latches AD_ERR_ARG or AD_ERR_CAPACITY and is left alone.  Codes behind the copied
  * tokens stay as they were.  scratch: ad_cache_reserve_scratch_bytes() of device memory, 256-byte aligned; calls that may overlap need scratch of their own. */
 size_t ad_cache_reserve_scratch_bytes(const ad_kv_pool* pool, int32_t B);

@@ -585,11 +585,12 @@ def cache_append(cache, k_t, v_t, off_t, len_t, max_new, status_t=None):
     if cache._tokens(entry, v_t, cache.n_kv_heads) != tokens:
         _refuse(entry, "keys and values must agree in type, shape and stride")
     dtype, M, stride = tokens
-    args = (k_t.data_ptr(), v_t.data_ptr(), dtype, stride, off_t.data_ptr(), len_t.data_ptr(), B, M, max_new, _status_pointer(entry, cache._dev, status_t))
     if cache._pool is None:
-        rc = _call_on(cache._dev, lib.ad_cache_append, cache._ref, *args)
+        rc = _call_on(cache._dev, lib.ad_cache_append, cache._ref, k_t.data_ptr(), v_t.data_ptr(), dtype, stride, off_t.data_ptr(), len_t.data_ptr(), B, M,
+                      max_new, _status_pointer(entry, cache._dev, status_t))
     else:
-        rc = _call_on(cache._dev, lib.ad_cache_append_pooled, cache._pool[0], cache._ref, *args)
+        rc = _call_on(cache._dev, lib.ad_cache_append_pooled, cache._pool[0], cache._ref, k_t.data_ptr(), v_t.data_ptr(), dtype, stride, off_t.data_ptr(),
+                      len_t.data_ptr(), B, M, max_new, _status_pointer(entry, cache._dev, status_t))
     if rc != AD_OK:
         _raise(lib, rc)
 
